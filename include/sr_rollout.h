@@ -285,6 +285,92 @@ sr_status sr_graph_kernel_time(sr_graph* g, double* ms, int64_t* launches);
  * recorded, and is reported by every later call, until sr_graph_reset starts the rollout over. */
 sr_status sr_graph_sync_status(sr_graph* g, void* stream);
 
+/*
+ * Temporal head: what stands behind a rollout and carries a memory of its own over the frames (the network's only memory is its
+ * recurrent edges).  Operators on plain device buffers; sr_rollout_run's whole clips and sr_rollout_step's single frames have
+ * their counterparts in sr_linear_attention_run and sr_linear_attention_step, a node's dense edge in sr_microscale_product.
+ *
+ * Conventions beyond those above: the device that owns the buffers is current; all calls are asynchronous on `stream`, may be
+ * captured into CUDA graphs and touch nothing but the buffers they are given; buffers do not overlap unless a call allows it;
+ * a call with no rows, frames or sequences returns SR_OK and writes nothing (final states excepted).
+ *
+ * Microscaled formats.  A matrix [rows][cols] is cut along its columns into groups of 32 (the last one padded with zeros).  A group
+ * has one scale 2^k, the smallest power of two, not below 2^-127, with max|x| <= M * 2^k, where M = 6 for SR_FORMAT_MX4 (elements e2m1) and
+ * 448 for SR_FORMAT_MX8 (elements e4m3); it is held as the byte k + 127.  Elements are x / 2^k rounded to nearest even; none
+ * saturates.  A group with an infinity or a NaN has the byte 255 and stands for NaNs; one of zeros has the byte 0.
+ *   data    row by row, a multiple of 32 elements each: one byte per element (MX8), or two elements per byte, the one with
+ *           the lower index in the low half (MX4);
+ *   scales  tiles of 128 rows x 4 groups, 512 bytes each, tile (r / 128, g / 4) row by row; inside a tile the byte of row r, group g
+ *           at (r % 32) * 16 + (r % 128 / 32) * 4 + g % 4.  Bytes of groups behind the last one are 0, those of rows behind the last one anything.
+ */
+enum { SR_FORMAT_F32 = 0, SR_FORMAT_BF16 = 1, SR_FORMAT_MX8 = 2, SR_FORMAT_MX4 = 3 };
+
+/* Bytes of a matrix in a microscaled format.  Errors: INVALID_ARG. */
+sr_status sr_microscale_bytes(int64_t rows, int64_t cols, int format, size_t* data_bytes, size_t* scale_bytes);
+/* x [rows][cols] of `dtype`, rows row_stride elements apart, into a microscaled format.  data and scales 16-byte aligned.
+ * Errors: INVALID_ARG, CUDA. */
+sr_status sr_microscale_quantize(const void* x_dev, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int format, void* data_dev,
+                                 void* scales_dev, void* stream);
+/* The values that a microscaled matrix stands for, float [rows][cols].  Errors: INVALID_ARG, CUDA. */
+sr_status sr_microscale_values(const void* data_dev, const void* scales_dev, int format, int64_t rows, int64_t cols, float* out_dev, void* stream);
+/*
+ * A dense node's update on microscaled operands: out[r][o] = act(bias[o] + sum_c a[r][c] * w[o][c]), a [rows][cols], w [outs][cols], both of
+ * `format`, products and sums in 32 bits on the tensor cores.  bias: float [outs] or NULL; act: 0 identity, 1 ReLU; out: `out_dtype`, rows
+ * out_stride elements apart.  data and scales 16-byte aligned.
+ * Errors: INVALID_ARG (also a size beyond 2^31 - 1), CUDA.  A device-side wait that expires is reported by sr_operator_status.
+ */
+sr_status sr_microscale_product(const void* a_data_dev, const void* a_scales_dev, const void* w_data_dev, const void* w_scales_dev, int format,
+                                int64_t rows, int64_t cols, int64_t outs, const float* bias_dev, int act, void* out_dev, int out_dtype,
+                                int64_t out_stride, void* stream);
+
+/*
+ * Root-mean-square norm: s = x + residual (in 32 bits), out = s / sqrt(mean(s^2) + eps) * weight.
+ * x, residual [rows][cols] of `dtype` (residual may be NULL), rows x_stride / residual_stride elements apart; weight: float [cols] or NULL (ones).
+ * sum (may be NULL): s rounded to `dtype`, [rows][cols] without gaps; it may be x or residual if that has no gaps either.
+ * out: SR_FORMAT_F32 / BF16 must equal `dtype`, [rows][cols] without gaps; SR_FORMAT_MX8 / MX4: microscaled data, with `scales`
+ * (otherwise NULL), taken from the 32-bit result.  Errors: INVALID_ARG, CUDA.
+ */
+sr_status sr_rms_norm(const void* x_dev, const void* residual_dev, const float* weight_dev, float eps, int dtype, int64_t rows, int64_t cols,
+                      int64_t x_stride, int64_t residual_stride, void* sum_dev, void* out_dev, int out_format, void* scales_dev, void* stream);
+
+/*
+ * Linear attention with a decay for each head.  Per sequence and group a state S [dk][dv] (float), frame by frame
+ *     S_t = exp(log_decay_t) * S_{t-1} + k_t v_t^T,      out_t = scale * q_t S_t.
+ * heads (of queries and outputs) is a multiple of groups (of keys, values, decays and states): heads h * heads / groups ... share group h.
+ * Decays: log_decay <= 0, -INFINITY included (the state starts anew at that frame).
+ * Layout: element (frame, sequence, head, i) of q lies at frame * q.frame + sequence * q.sequence + head * q.head + i, in elements, the
+ * same for k, v, out (i < dk, dk, dv, dv) and log_decay (float; strides 0 repeat a value).
+ *   offsets NULL:  `batch` sequences of `frames` frames each (sr_rollout_run's [T][B][C] has frame = B * C, sequence = C);
+ *   offsets (device, int64 [batch + 1], not decreasing): packed sequences; sequence b has the frames offsets[b] .. offsets[b + 1] - 1 of
+ *                  `frames` in all and the strides `sequence` are not used.  Lengths may be 0.  Frames that no sequence has are left as they were.
+ *                  Offsets outside 0 .. frames are taken as the nearest of the two, a decreasing one as an empty sequence; sequences that
+ *                  overlap get undefined outputs.
+ * States [batch][groups][dk][dv] without gaps: state_in (NULL: zeros), state_out (NULL: not wanted; may be state_in).  A sequence without
+ * frames hands its state through.  Sizes: dk <= 256, heads / groups <= 128.
+ */
+typedef struct { int64_t frame, sequence, head; } sr_attention_strides;
+typedef struct {
+    int32_t dtype;                                  /* of q, k, v and out: SR_DTYPE_F32 or SR_DTYPE_BF16 */
+    int32_t batch, heads, groups, dk, dv;
+    int64_t frames;
+    float scale;
+    sr_attention_strides q, k, v, out, log_decay;
+} sr_attention_desc;
+/* Bytes of device memory (256-byte aligned) that sr_linear_attention_run needs for these sizes; may be 0.  packed: offsets will be given.
+ * Work of two runs that share a workspace must not overlap on the GPU.  Errors: INVALID_ARG, UNSUPPORTED. */
+sr_status sr_linear_attention_workspace_bytes(const sr_attention_desc* desc, int packed, size_t* bytes);
+/* All frames of all sequences.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sr_status sr_linear_attention_run(const sr_attention_desc* desc, const void* q_dev, const void* k_dev, const void* v_dev, const float* log_decay_dev,
+                                  const int64_t* offsets_dev, const float* state_in_dev, float* state_out_dev, void* out_dev,
+                                  void* workspace_dev, size_t workspace_bytes, void* stream);
+/* One frame of every sequence: desc->frames and the frame strides are not used; the states are updated in place.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sr_status sr_linear_attention_step(const sr_attention_desc* desc, const void* q_dev, const void* k_dev, const void* v_dev, const float* log_decay_dev,
+                                   float* state_dev, void* out_dev, void* stream);
+/* Synchronises `stream` and reports SR_ERR_CUDA if queued work failed, SR_ERR_TIMEOUT if a bounded wait inside one of the operators' kernels
+ * expired on the current device since the last call (its outputs are then not valid). */
+sr_status sr_operator_status(void* stream);
+
 const char* sr_status_str(sr_status s);
 
 #ifdef __cplusplus

@@ -300,11 +300,15 @@ class Graph:
     def sync_status(self):
         _check(self._lib.sr_graph_sync_status(self._h, self._stream()), "sr_graph_sync_status")
 
-    def rollout(self, frames):
+    def rollout(self, frames, head=None):
         """frames: one tensor [T+1][B][H][W][C] per input node (frames 0..T).  Resets to frame 0,
-        runs T updates, returns the outputs [T][B][C_out] (float32)."""
+        runs T updates, returns the outputs [T][B][C_out] (float32).  With a `TemporalHead` the outputs are its features: it is
+        reset, too, and what it gives for the T frames is returned."""
         T = int(frames[0].shape[0]) - 1
         out = self._torch.empty((T,) + self.out_shape(), dtype=self._torch.float32, device=self.device)
         self.reset([f[0] for f in frames])
         self.run([f[1:] for f in frames], out)
-        return out
+        if head is None:
+            return out
+        head.reset()
+        return head.run(out)

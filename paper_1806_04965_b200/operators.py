@@ -1,0 +1,409 @@
+"""Operators of the temporal head behind a rollout (the sr_microscale_*, sr_rms_norm and sr_linear_attention_* calls of include/sr_rollout.h).
+
+Argument marshalling only, like `Graph`: tensors live on a CUDA device, work goes to the current stream of that device, outputs and
+workspaces come from PyTorch's allocator, and every refusal is an `SrError`.  There is no backward pass: a tensor that
+requires a gradient is refused while gradients are recorded.
+
+  quantize, Microscaled, product   matrices in groups of 32 with a scale each, 4 ("mx4") or 8 ("mx8") bits per element; a dense node's update
+  rms_norm                         root-mean-square norm with the residual's addition, output in full or microscaled
+  linear_attention_run, _step      linear attention with a decay for each head: whole clips, single frames
+  TemporalHead                     norm, product, attention and product as one head on the features of a rollout (`Graph.rollout(frames, head=...)`)
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import binding
+from .binding import SrError
+
+FORMATS = {"mx8": 2, "mx4": 3}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+class _Strides(ctypes.Structure):
+    _fields_ = [("frame", ctypes.c_int64), ("sequence", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class _AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "batch", "heads", "groups", "dk", "dv")] + [("frames", ctypes.c_int64), ("scale", ctypes.c_float)] + \
+        [(n, _Strides) for n in ("q", "k", "v", "out", "log_decay")]
+
+
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = binding.load_library()
+        vp, i32, i64, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)
+        desc = ctypes.POINTER(_AttentionDesc)
+        for name, args in {
+            "sr_microscale_bytes": [i64, i64, i32, size, size],
+            "sr_microscale_quantize": [vp, i32, i64, i64, i64, i32, vp, vp, vp],
+            "sr_microscale_values": [vp, vp, i32, i64, i64, vp, vp],
+            "sr_microscale_product": [vp, vp, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp],
+            "sr_rms_norm": [vp, vp, vp, ctypes.c_float, i32, i64, i64, i64, i64, vp, vp, i32, vp, vp],
+            "sr_linear_attention_workspace_bytes": [desc, i32, size],
+            "sr_linear_attention_run": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
+            "sr_linear_attention_step": [desc, vp, vp, vp, vp, vp, vp, vp],
+            "sr_operator_status": [vp],
+        }.items():
+            f = getattr(lib, name)
+            f.argtypes, f.restype = args, i32
+        _lib = lib
+    return _lib
+
+
+def _refuse(call: str, why: str):
+    raise SrError(1, "%s: %s" % (call, why))
+
+
+def _check(code: int, call: str):
+    if code:
+        raise SrError(code, call)
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+class _on:
+    """Makes a tensor's device the current one for the calls inside (only where it is not) and gives that device's current stream."""
+    __slots__ = ("index", "before")
+
+    def __init__(self, t):
+        self.index = t.device.index
+
+    def __enter__(self):
+        before = torch.cuda.current_device()
+        self.before = None if before == self.index else before
+        if self.before is not None:
+            torch.cuda.set_device(self.index)
+        return _raw_stream(self.index)
+
+    def __exit__(self, *_):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
+
+
+def _tensors(call: str, first, *others):
+    """All on one CUDA device, none that a gradient is recorded for."""
+    device = first.device
+    if device.type != "cuda":
+        _refuse(call, "tensors on a CUDA device are required")
+    grad = torch.is_grad_enabled()
+    for t in (first,) + others:
+        if t is None:
+            continue
+        if t.device != device:
+            _refuse(call, "tensors lie on different devices")
+        if grad and t.requires_grad:
+            _refuse(call, "there is no backward pass (use torch.no_grad() or detach)")
+
+
+def _float_vector(call: str, name: str, t, n: int):
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        _refuse(call, "%s has to be float32 [%d] without gaps" % (name, n))
+    return t.data_ptr()
+
+
+def _rows(call: str, name: str, t):
+    """A matrix whose rows have no gaps inside; its row stride."""
+    if t.dim() != 2 or t.dtype not in _DTYPES:
+        _refuse(call, "%s has to be a float32 or bfloat16 matrix" % name)
+    rows, cols = t.shape
+    if cols < 1:
+        _refuse(call, "%s has no columns" % name)
+    a, b = t.stride()
+    if b != 1 and cols > 1:
+        _refuse(call, "the columns of %s have to lie side by side" % name)
+    return a if rows > 1 else cols
+
+
+class Microscaled:
+    """A matrix [rows][cols] in a microscaled format ("mx4" or "mx8"; layout in include/sr_rollout.h): `data` and `scales` are uint8 tensors."""
+    __slots__ = ("data", "scales", "rows", "cols", "format")
+
+    def __init__(self, data, scales, rows: int, cols: int, format: str):
+        if format not in FORMATS:
+            _refuse("Microscaled", "format is one of %s" % ", ".join(FORMATS))
+        if rows < 0 or cols < 1:
+            _refuse("Microscaled", "a size is out of range")
+        groups = -(-cols // 32)
+        if data.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or not data.is_contiguous() or not scales.is_contiguous() or \
+                data.numel() != rows * groups * (16 if format == "mx4" else 32) or scales.numel() != -(-rows // 128) * -(-groups // 4) * 512:
+            _refuse("Microscaled", "data and scales have to be uint8, without gaps, of the sizes that rows, cols and format make")
+        self.data, self.scales, self.rows, self.cols, self.format = data, scales, rows, cols, format
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, format: str, device):
+        m = cls.__new__(cls)
+        if format not in FORMATS:
+            _refuse("Microscaled", "format is one of %s" % ", ".join(FORMATS))
+        groups = -(-cols // 32)
+        m.data = torch.empty((rows, groups * (16 if format == "mx4" else 32)), dtype=torch.uint8, device=device)
+        m.scales = torch.empty(-(-rows // 128) * -(-groups // 4) * 512, dtype=torch.uint8, device=device)
+        m.rows, m.cols, m.format = rows, cols, format
+        return m
+
+    def values(self):
+        """The values it stands for, float32 [rows][cols]."""
+        _tensors("values", self.data, self.scales)
+        out = torch.empty((self.rows, self.cols), dtype=torch.float32, device=self.data.device)
+        with _on(out) as stream:
+            _check(_library().sr_microscale_values(self.data.data_ptr(), self.scales.data_ptr(), FORMATS[self.format], self.rows, self.cols, out.data_ptr(),
+                                                   stream), "sr_microscale_values")
+        return out
+
+
+def quantize(x, format: str = "mx4") -> Microscaled:
+    """x [rows][cols] (float32 or bfloat16; rows may have gaps between them) in a microscaled format."""
+    _tensors("quantize", x)
+    stride = _rows("quantize", "x", x)
+    m = Microscaled.empty(x.shape[0], x.shape[1], format, x.device)
+    with _on(x) as stream:
+        _check(_library().sr_microscale_quantize(x.data_ptr(), _DTYPES[x.dtype], m.rows, m.cols, stride, FORMATS[format], m.data.data_ptr(),
+                                                 m.scales.data_ptr(), stream), "sr_microscale_quantize")
+    return m
+
+
+def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype=torch.bfloat16, out=None):
+    """act(bias + a w^T), [a.rows][w.rows]: a dense node's update on microscaled operands of the same format.  `out` (rows may have
+    gaps between them) is written in place of a new tensor of `dtype`."""
+    if a.format != w.format or a.cols != w.cols:
+        _refuse("product", "both matrices have the same format and number of columns")
+    _tensors("product", a.data, a.scales, w.data, w.scales, bias, out)
+    b = _float_vector("product", "bias", bias, w.rows)
+    if out is None:
+        if dtype not in _DTYPES:
+            _refuse("product", "the output is float32 or bfloat16")
+        out = torch.empty((a.rows, w.rows), dtype=dtype, device=a.data.device)
+        stride = w.rows
+    else:
+        if tuple(out.shape) != (a.rows, w.rows):
+            _refuse("product", "out has to be [%d][%d]" % (a.rows, w.rows))
+        stride = _rows("product", "out", out) if w.rows else 0
+    with _on(out) as stream:
+        _check(_library().sr_microscale_product(a.data.data_ptr(), a.scales.data_ptr(), w.data.data_ptr(), w.scales.data_ptr(), FORMATS[a.format],
+                                                a.rows, a.cols, w.rows, b, 1 if relu else 0, out.data_ptr(), _DTYPES[out.dtype], stride, stream),
+               "sr_microscale_product")
+    return out
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, format: Optional[str] = None):
+    """s = x + residual, s / sqrt(mean(s^2) + eps) * weight for every row of x [rows][cols].  The output has x's type, or is `Microscaled` where
+    a format is given; with a residual the result is (output, s rounded to x's type)."""
+    _tensors("rms_norm", x, weight, residual)
+    xs = _rows("rms_norm", "x", x)
+    rows, cols = x.shape
+    rs, rp, total, tp = 0, None, None, None
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype is not x.dtype:
+            _refuse("rms_norm", "the residual has x's shape and type")
+        rs, rp = _rows("rms_norm", "residual", residual), residual.data_ptr()
+        total = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        tp = total.data_ptr()
+    w = _float_vector("rms_norm", "weight", weight, cols)
+    if format is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        op, code, sp = out.data_ptr(), _DTYPES[x.dtype], None
+    else:
+        out = Microscaled.empty(rows, cols, format, x.device)
+        op, code, sp = out.data.data_ptr(), FORMATS[format], out.scales.data_ptr()
+    with _on(x) as stream:
+        _check(_library().sr_rms_norm(x.data_ptr(), rp, w, eps, _DTYPES[x.dtype], rows, cols, xs, rs, tp, op, code, sp, stream), "sr_rms_norm")
+    return out if residual is None else (out, total)
+
+
+# Descriptions made so far, by everything that they hold (sizes, strides, type, scale), with the workspace they need.
+_descs: dict = {}
+
+
+def _desc(call: str, q, k, v, log_decay, out_strides, packed: bool, step: bool, batch: int, scale: float):
+    key = (q.dtype, k.dtype, v.dtype, log_decay.dtype, q.shape, k.shape, v.shape, log_decay.shape, q.stride(), k.stride(), v.stride(), log_decay.stride(),
+           out_strides, packed, step, batch, scale)
+    hit = _descs.get(key)
+    if hit is not None:
+        return hit
+    lead = q.dim() - 2
+    if q.dtype not in _DTYPES or k.dtype is not q.dtype or v.dtype is not q.dtype or log_decay.dtype is not torch.float32:
+        _refuse(call, "q, k and v have one type, float32 or bfloat16; log_decay is float32")
+    want = 1 if packed or step else 2
+    if lead != want or k.dim() != q.dim() or v.dim() != q.dim() or k.shape[:-2] != q.shape[:-2] or v.shape[:-2] != q.shape[:-2]:
+        _refuse(call, "q, k and v have to be %s[heads][size] with the same leading sizes" % ("[sequences]" if step else "[frames]" if packed else "[frames][sequences]"))
+    heads, dk = q.shape[-2:]
+    groups, dv = k.shape[-2], v.shape[-1]
+    if k.shape[-1] != dk or v.shape[-2] != groups or groups < 1 or heads % groups or heads < 1:
+        _refuse(call, "k has q's size, v has k's heads, and q's heads are a multiple of them")
+    if tuple(log_decay.shape) not in ((groups,), tuple(q.shape[:-2]) + (groups,)):
+        _refuse(call, "log_decay has to be [groups] or %s[groups]" % ("[sequences]" if step else "[frames]" if packed else "[frames][sequences]"))
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            _refuse(call, "the elements of a head of %s have to lie side by side" % name)
+
+    def strides(st):
+        s = _Strides()
+        if step:
+            s.sequence, s.head = st[0], st[1]
+        elif packed:
+            s.frame, s.head = st[0], st[1]
+        else:
+            s.frame, s.sequence, s.head = st[0], st[1], st[2]
+        return s
+
+    d = _AttentionDesc(_DTYPES[q.dtype], batch, heads, groups, dk, dv, 1 if step else q.shape[0], scale, strides(q.stride()), strides(k.stride()),
+                       strides(v.stride()), strides(out_strides))
+    ld = log_decay.stride()
+    d.log_decay = _Strides(0, 0, ld[0]) if log_decay.dim() == 1 else strides(ld)
+    size = ctypes.c_size_t()
+    _check(_library().sr_linear_attention_workspace_bytes(ctypes.byref(d), 1 if packed else 0, ctypes.byref(size)), call)
+    if len(_descs) >= 256:
+        _descs.clear()
+    _descs[key] = hit = (ctypes.byref(d), size.value, (batch, groups, dk, dv), d)
+    return hit
+
+
+def _state_pointer(call: str, state, shape):
+    if state.dtype is not torch.float32 or tuple(state.shape) != shape or not state.is_contiguous():
+        _refuse(call, "the state has to be float32 [%d][%d][%d][%d] without gaps" % shape)
+    return state.data_ptr()
+
+
+def linear_attention_run(q, k, v, log_decay, state=None, offsets=None, scale: float = 1.0, out=None, state_out=None):
+    """S_t = exp(log_decay_t) S_{t-1} + k_t v_t^T, out_t = scale * q_t S_t over all frames; returns (out, the states after the last frame).
+
+    q [frames][sequences][heads][dk], k [..][groups][dk], v [..][groups][dv] (a view of a larger tensor will do as long as the elements of a
+    head lie side by side), log_decay [groups] or [frames][sequences][groups]; with `offsets` (int64 [sequences + 1]) packed sequences
+    [frames][heads][size], sequence b the frames offsets[b] .. offsets[b + 1] - 1.  state: float32 [sequences][groups][dk][dv] before the first
+    frame (None: zeros).  `out` (without gaps; frames that no sequence has keep what it holds) and `state_out` (may be `state`) are written in
+    place of new tensors."""
+    call = "linear_attention_run"
+    _tensors(call, q, k, v, log_decay, state, offsets, out, state_out)
+    packed = offsets is not None
+    if packed and (offsets.dtype is not torch.int64 or offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous()):
+        _refuse(call, "offsets have to be int64 [sequences + 1] without gaps")
+    if q.dim() < 3 or v.dim() < 3:
+        _refuse(call, "q, k and v have to be [frames][sequences][heads][size], or [frames][heads][size] with offsets")
+    if out is None:
+        out = torch.empty(q.shape[:-1] + v.shape[-1:], dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape[:-1] + v.shape[-1:] or out.dtype is not q.dtype or not out.is_contiguous():
+        _refuse(call, "out has to be %s of q's type without gaps" % (tuple(q.shape[:-1] + v.shape[-1:]),))
+    batch = offsets.shape[0] - 1 if packed else q.shape[1]
+    desc, size, shape, _ = _desc(call, q, k, v, log_decay, out.stride(), packed, False, batch, scale)
+    sp = None if state is None else _state_pointer(call, state, shape)
+    last = torch.empty(shape, dtype=torch.float32, device=q.device) if state_out is None else state_out
+    lp = _state_pointer(call, last, shape)
+    work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+    with _on(q) as stream:
+        _check(_library().sr_linear_attention_run(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), offsets.data_ptr() if packed else None,
+                                                  sp, lp, out.data_ptr(), work.data_ptr() if size else None, size, stream), "sr_" + call)
+    return out, last
+
+
+def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0):
+    """One frame of every sequence: q [sequences][heads][dk], k [..][groups][dk], v [..][groups][dv], log_decay [groups] or [sequences][groups].
+    `state` (float32 [sequences][groups][dk][dv]) is updated in place; returns out [sequences][heads][dv]."""
+    call = "linear_attention_step"
+    _tensors(call, q, k, v, log_decay, state)
+    if q.dim() != 3 or v.dim() != 3:
+        _refuse(call, "q, k and v have to be [sequences][heads][size]")
+    out = torch.empty(q.shape[:-1] + v.shape[-1:], dtype=q.dtype, device=q.device)
+    desc, _, shape, _ = _desc(call, q, k, v, log_decay, out.stride(), False, True, q.shape[0], scale)
+    sp = _state_pointer(call, state, shape)
+    with _on(q) as stream:
+        _check(_library().sr_linear_attention_step(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), sp, out.data_ptr(), stream),
+               "sr_" + call)
+    return out
+
+
+def operator_status(device=None):
+    """Waits for the current stream's work; raises `SrError` if it failed or a bounded wait inside an operator's kernel expired."""
+    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    with torch.cuda.device(index):
+        _check(_library().sr_operator_status(_raw_stream(index)), "sr_operator_status")
+
+
+class TemporalHead:
+    """A head with a memory over the frames on the features that a rollout gives, per frame and sequence
+
+        q, k, v = Wqkv norm(x)      (microscaled operands)
+        S = exp(log_decay) S + k v^T,  o = q S / sqrt(dk)
+        h = x + Wo norm(o),   out = Wout norm(h) + bias
+
+    with x the features ([channels], what `Graph` hands out for its output node).  `run` takes whole clips and `step` single frames; both carry
+    the states S on, as a rollout carries a network's, and give the same values up to rounding.
+
+    weights: qkv [heads * dk + groups * (dk + dv)][channels], o [channels][heads * dv], out [outputs][channels], bias [outputs]; norm_x [channels],
+    norm_o [heads * dv], norm_h [channels]; log_decay [groups] (all float tensors, quantised here once)."""
+
+    def __init__(self, weights: dict, channels: int, heads: int, groups: int, dk: int, dv: int, batch: int, format: str = "mx4", dtype: str = "bf16",
+                 eps: float = 1e-6, device: str = "cuda:0"):
+        self.channels, self.heads, self.groups, self.dk, self.dv, self.batch, self.eps, self.format = channels, heads, groups, dk, dv, batch, eps, format
+        self.tdtype = {"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
+        shapes = {"qkv": (heads * dk + groups * (dk + dv), channels), "o": (channels, heads * dv), "out": (None, channels), "bias": (None,),
+                  "norm_x": (channels,), "norm_o": (heads * dv,), "norm_h": (channels,), "log_decay": (groups,)}
+        w = {}
+        for name, shape in shapes.items():
+            t = torch.as_tensor(weights[name], dtype=torch.float32).detach().to(device).contiguous()
+            if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+                _refuse("TemporalHead", "%s has shape %s" % (name, tuple(t.shape)))
+            w[name] = t
+        self.outputs = w["out"].shape[0]
+        if w["bias"].shape[0] != self.outputs:
+            _refuse("TemporalHead", "bias has another number of outputs than out")
+        for name in ("qkv", "o", "out"):
+            w[name] = quantize(w[name], format)
+        self._w = w
+        self.scale = float(dk) ** -0.5
+        self.state = torch.zeros((batch, groups, dk, dv), dtype=torch.float32, device=device)
+
+    def reset(self):
+        """Before the first frame: no memory."""
+        self.state.zero_()
+
+    def get_state(self):
+        return self.state.clone()
+
+    def set_state(self, state):
+        if state.shape != self.state.shape or state.dtype is not torch.float32:
+            _refuse("TemporalHead.set_state", "the state has to be float32 %s" % (tuple(self.state.shape),))
+        self.state.copy_(state)
+
+    def _attend(self, x):
+        n = self.heads * self.dk, self.groups * self.dk
+        qkv = product(rms_norm(x, self._w["norm_x"], eps=self.eps, format=self.format), self._w["qkv"], dtype=self.tdtype)
+        return qkv[:, :n[0]], qkv[:, n[0]:n[0] + n[1]], qkv[:, n[0] + n[1]:]
+
+    def _answer(self, x, o):
+        y = product(rms_norm(o.reshape(x.shape[0], self.heads * self.dv), self._w["norm_o"], eps=self.eps, format=self.format), self._w["o"], dtype=self.tdtype)
+        m, _ = rms_norm(y, self._w["norm_h"], residual=x, eps=self.eps, format=self.format)
+        return product(m, self._w["out"], bias=self._w["bias"], dtype=torch.float32)
+
+    @torch.no_grad()
+    def run(self, features):
+        """features [frames][batch][...channels] (float32 or the head's type) -> float32 [frames][batch][outputs]."""
+        T, B = features.shape[:2]
+        if B != self.batch:
+            _refuse("TemporalHead.run", "the head has %d sequences" % self.batch)
+        x = features.reshape(T * B, self.channels).to(self.tdtype)
+        q, k, v = self._attend(x)
+        o, _ = linear_attention_run(q.unflatten(0, (T, B)).unflatten(2, (self.heads, self.dk)), k.unflatten(0, (T, B)).unflatten(2, (self.groups, self.dk)),
+                                    v.unflatten(0, (T, B)).unflatten(2, (self.groups, self.dv)), self._w["log_decay"], state=self.state,
+                                    scale=self.scale, state_out=self.state)
+        return self._answer(x, o).view(T, B, self.outputs)
+
+    @torch.no_grad()
+    def step(self, features):
+        """features [batch][...channels] of one frame -> float32 [batch][outputs]."""
+        if features.shape[0] != self.batch:
+            _refuse("TemporalHead.step", "the head has %d sequences" % self.batch)
+        x = features.reshape(self.batch, self.channels).to(self.tdtype)
+        q, k, v = self._attend(x)
+        o = linear_attention_step(q.unflatten(1, (self.heads, self.dk)), k.unflatten(1, (self.groups, self.dk)), v.unflatten(1, (self.groups, self.dv)),
+                                  self._w["log_decay"], self.state, scale=self.scale)
+        return self._answer(x, o)
