@@ -1,54 +1,338 @@
-// Product of microscaled matrices: out[r][o] = act(bias[o] + sum_c a[r][c] * w[o][c]).
+// Product of microscaled matrices: out[r][o] = act(bias[o] + sum_c a[r][c] * w[o][c]), on the tensor cores' block-scaled MMAs (tcgen05.mma
+// kind::mxf8f6f4 and kind::mxf4: products of the elements times the two scales of their groups of 32, summed in 32 bits).
+//
+// Roles.  The weights are the M operand (128 outputs per tile: TMEM lane = output), the rows of a the N operand (NT of them: TMEM column = row), as in
+// the frame update's kernel: few rows then cost few columns, and a warp's stores are 32 neighbouring outputs of one row.
+// Stages.  One ring slot holds 128 bytes of every row of both operands (128 elements of 8 bits, 256 of 4), K-major with the 128-byte swizzle, by two
+// TMA copies (zero fill behind the last column and row), and their scales: the formats' scale tiles of 128 rows x 4 groups are what tcgen05.cp takes,
+// 512 bytes onto four TMEM columns (byte g of lane r % 32, column r / 32), so a stage's scales are one or two bulk copies per operand and one or two
+// tcgen05.cp.  An MMA takes 32 bytes of a row: one group of 8-bit elements, two of 4-bit ones.
+// Warps: 0 copies, 1 MMAs, 2 TMEM, 4..7 epilogue (bias, ReLU, rounding), which works on one accumulator while the MMAs fill the other.
+// Few tiles: the CTAs of a cluster share a tile's reduction; their sums meet in distributed shared memory, each CTA finishing its share of the
+// columns in a fixed order.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
 #include "sr_microscale.cuh"
+#include "sr_operators.h"
+#include "sr_ptx.cuh"
+
+__device__ int sr_operator_error;                     // 1: a bounded wait expired
 
 namespace {
+using namespace srx;
+
+constexpr int kThreads = 256, kOuts = 128, kMaxStages = 8;
+constexpr int kSmem = 200 * 1024;
 
 struct ProductArgs {
-    const uint8_t *a, *a_scales, *w, *w_scales;
+    CUtensorMap w_map, a_map;
+    const uint8_t *w_scales, *a_scales;
     const float* bias;
     void* out;
-    int64_t rows, cols, outs, out_stride, groups, tiles_g;
-    int act, out_bf16;
+    int64_t out_stride;
+    int32_t rows, outs, row_bytes, tiles_g, tiles_r;
+    int32_t out_tiles, row_tiles, stages, ring;       // stages of the whole reduction; ring slots
+    int32_t act, out_bf16, split;
+};
+
+template <int FMT, int NT>
+struct Shape {
+    static constexpr int TG = FMT == SR_FORMAT_MX4 ? 2 : 1;          // scale tiles of a stage along the groups
+    static constexpr int RT = NT > 128 ? 2 : 1;                      // ... along the rows of a
+    static constexpr int W = kOuts * 128, A = NT * 128, SW = TG * 512, SA = RT * TG * 512;
+    static constexpr int kStage = (W + A + SW + SA + 1023) / 1024 * 1024;
+    static constexpr int kAccs = 2;
+    static constexpr int kScaleCols = TG * 4 + TG * RT * 4;          // TMEM columns of a stage's scales
+    static constexpr int kScaleBase = kAccs * NT;
+    static constexpr int kCols = kScaleBase + 2 * kScaleCols;
+    static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+    static_assert(kCols <= 512, "TMEM has 512 columns");
 };
 
 template <int FMT>
-__device__ __forceinline__ float element(const uint8_t* data, const uint8_t* scales, int64_t row, int64_t c, const ProductArgs& P)
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate)
 {
-    const float s = sr_scale(scales[sr_scale_place(row, c >> 5, P.tiles_g)]);
-    if (FMT == SR_FORMAT_MX4) return s * sr_e2m1_value((data[row * P.groups * 16 + c / 2] >> (4 * (c & 1))) & 15u);
-    return s * sr_e4m3_value(data[row * P.groups * 32 + c]);
+    if constexpr (FMT == SR_FORMAT_MX4)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+// 512 bytes (32 lanes x 16 bytes, lane after lane) onto four TMEM columns, the same in all four quarters of the lanes.
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t smem)
+{
+    const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
-// 32 x 32 outputs per block, 32 columns of both matrices at a time.
-template <int FMT>
-__global__ void __launch_bounds__(256) sr_product_kernel(const __grid_constant__ ProductArgs P)
+template <int FMT, int NT>
+__global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_constant__ ProductArgs P)
 {
-    __shared__ float a[32][33], w[32][33];
-    const int64_t o0 = (int64_t)blockIdx.x * 32, r0 = (int64_t)blockIdx.y * 32;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    float sum[4] = {0, 0, 0, 0};
-    for (int64_t c0 = 0; c0 < P.groups * 32; c0 += 32) {
-        for (int i = 0; i < 4; ++i) {
-            const int64_t r = r0 + ty + 8 * i, o = o0 + ty + 8 * i, c = c0 + tx;
-            a[ty + 8 * i][tx] = r < P.rows ? element<FMT>(P.a, P.a_scales, r, c, P) : 0.0f;
-            w[ty + 8 * i][tx] = o < P.outs ? element<FMT>(P.w, P.w_scales, o, c, P) : 0.0f;
+    using S = Shape<FMT, NT>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kMaxStages + 4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int gave_up_flag;
+    volatile int* gave_up = &gave_up_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t full = smem_u32(&bars[0]), empty = smem_u32(&bars[kMaxStages]), tfull = smem_u32(&bars[2 * kMaxStages]), tempty = tfull + 16;
+    if (threadIdx.x == 0) {
+        gave_up_flag = 0;
+        for (int s = 0; s < P.ring; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
         }
-        __syncthreads();
-        for (int c = 0; c < 32; ++c)
-            for (int i = 0; i < 4; ++i) sum[i] = fmaf(a[ty + 8 * i][c], w[tx][c], sum[i]);
-        __syncthreads();
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tfull + 8 * a, 1);
+            mbar_init(tempty + 8 * a, 4);
+        }
+        mbar_init_done();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&P.w_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&P.a_map) : "memory");
     }
-    const int64_t o = o0 + tx;
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + ty + 8 * i;
-        if (r >= P.rows || o >= P.outs) continue;
-        float v = sum[i] + (P.bias ? P.bias[o] : 0.0f);
-        if (P.act && v < 0.0f) v = 0.0f;
-        if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[r * P.out_stride + o] = __float2bfloat16(v);
-        else static_cast<float*>(P.out)[r * P.out_stride + o] = v;
+    if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), S::kAlloc);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    begin();
+
+    const int rank = P.split > 1 ? (int)cluster_rank() : 0;
+    const int first = P.split > 1 ? (int)blockIdx.x / P.split : (int)blockIdx.x, step = P.split > 1 ? (int)gridDim.x / P.split : (int)gridDim.x;
+    const int tiles = P.out_tiles * P.row_tiles;
+    const int k0 = (int)((int64_t)P.stages * rank / P.split), k1 = (int)((int64_t)P.stages * (rank + 1) / P.split);
+
+    if (warp == 0) {
+        if (elect_one()) {
+            uint32_t n = 0, s = 0, ph = 1;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step) {
+                const int o0 = t % P.out_tiles * kOuts, r0 = t / P.out_tiles * NT;
+                const int rt0 = r0 >> 7, rts = min(S::RT, min(P.tiles_r - rt0, ((r0 & 127) + NT + 127) >> 7));
+                for (int k = k0; k < k1; ++k) {
+                    ok = mbar_wait(empty + 8 * s, ph, gave_up);
+                    if (!ok) break;
+                    const uint32_t at = ring + s * S::kStage, bar = full + 8 * s;
+                    const uint32_t sb = (uint32_t)min(S::TG, P.tiles_g - k * S::TG) * 512u;
+                    mbar_expect_tx(bar, S::W + S::A + sb * (1 + rts));
+                    tma_load_2d(at, &P.w_map, bar, k * 128, o0);
+                    tma_load_2d(at + S::W, &P.a_map, bar, k * 128, r0);
+                    bulk_load(at + S::W + S::A, P.w_scales + ((int64_t)(o0 >> 7) * P.tiles_g + k * S::TG) * 512, sb, bar);
+                    for (int q = 0; q < rts; ++q)
+                        bulk_load(at + S::W + S::A + S::SW + q * S::TG * 512, P.a_scales + ((int64_t)(rt0 + q) * P.tiles_g + k * S::TG) * 512, sb, bar);
+                    ++n;
+                    if (++s == (uint32_t)P.ring) { s = 0; ph ^= 1; }
+                }
+            }
+            for (uint32_t v = 0; v < (uint32_t)P.ring && v < n; ++v) mbar_drain(full + 8 * v, ((n - 1 - v) / P.ring) & 1);
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            // D = f32; A, B = e4m3 (code 0) or e2m1 (1); scales ue8m0; both operands K-major
+            const uint32_t type = FMT == SR_FORMAT_MX4 ? 1u : 0u;
+            const uint32_t idesc = (type << 7) | (type << 10) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)(kOuts >> 4) << 24);
+            uint32_t s = 0, ph = 0, it = 0;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step, ++it) {
+                const int r0 = t / P.out_tiles * NT;
+                const uint32_t acc = it & 1u, d = tmem + acc * NT;
+                ok = mbar_wait(tempty + 8 * acc, ((it >> 1) & 1u) ^ 1u, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                for (int k = k0; k < k1; ++k) {
+                    ok = mbar_wait(full + 8 * s, ph, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t at = ring + s * S::kStage;
+                    const uint32_t sw = tmem + S::kScaleBase + (uint32_t)(k & 1) * S::kScaleCols, sa = sw + S::TG * 4;
+#pragma unroll
+                    for (int g = 0; g < S::TG; ++g) {
+                        copy_scales(sw + 4 * g, at + S::W + S::A + 512 * g);
+#pragma unroll
+                        for (int q = 0; q < S::RT; ++q) copy_scales(sa + (g * S::RT + q) * 4, at + S::W + S::A + S::SW + (q * S::TG + g) * 512);
+                    }
+                    const uint64_t da = desc_k_major(at), db = desc_k_major(at + S::W);
+                    const int n = min(4, (P.row_bytes - k * 128 + 31) / 32);
+                    const uint32_t shift = (uint32_t)(r0 & 127) >> 5;                        // columns of 32 rows that the tile starts into its first scale tile
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (i >= n) break;
+                        const int g = FMT == SR_FORMAT_MX4 ? i / 2 : 0;
+                        const uint32_t id = FMT == SR_FORMAT_MX4 ? (uint32_t)(i & 1) * 2 : (uint32_t)i;
+                        mma_scaled<FMT>(d, da + 2 * i, db + 2 * i, idesc | (id << 4) | (id << 29), sw + 4 * g, sa + g * S::RT * 4 + shift, (k > k0 || i > 0) ? 1u : 0u);
+                    }
+                    tc_commit(empty + 8 * s);
+                    if (++s == (uint32_t)P.ring) { s = 0; ph ^= 1; }
+                }
+                if (!ok) break;
+                tc_commit(tfull + 8 * acc);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        constexpr int CW = NT < 32 ? NT : 32;
+        const int quarter = warp - 4;
+        uint32_t it = 0;
+        auto store = [&](int64_t row, int o, float v) {
+            if (P.act && v < 0.0f) v = 0.0f;
+            if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[row * P.out_stride + o] = __float2bfloat16(v);
+            else static_cast<float*>(P.out)[row * P.out_stride + o] = v;
+        };
+        if (P.split > 1) {
+            // (one tile per cluster) the partial sums lie in the ring, which is idle by now: [column][output]
+            bool ok = mbar_wait(tfull, 0, gave_up);
+            tc_fence_after();
+            float* mine = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
+            for (int c = 0; c < NT && ok; c += CW) {
+                uint32_t v[CW];
+                tc_ld(tmem + ((uint32_t)(quarter * 32) << 16) + c, v);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < CW; ++i) mine[(c + i) * kOuts + quarter * 32 + lane] = __uint_as_float(v[i]);
+            }
+        } else {
+            for (int t = first; t < tiles; t += step, ++it) {
+                const int o = t % P.out_tiles * kOuts + quarter * 32 + lane, r0 = t / P.out_tiles * NT;
+                const uint32_t acc = it & 1u;
+                if (!mbar_wait(tfull + 8 * acc, (it >> 1) & 1u, gave_up)) break;
+                tc_fence_after();
+                const float b = P.bias && o < P.outs ? P.bias[o] : 0.0f;
+                const int n = min(NT, P.rows - r0);
+                for (int c = 0; c < n; c += CW) {
+                    uint32_t v[CW];
+                    tc_ld(tmem + acc * NT + ((uint32_t)(quarter * 32) << 16) + c, v);
+                    tc_wait_ld();
+                    if (o < P.outs) {
+#pragma unroll
+                        for (int i = 0; i < CW; ++i)
+                            if (c + i < n) store(r0 + c + i, o, __uint_as_float(v[i]) + b);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tempty + 8 * acc);
+            }
+        }
+    }
+    if (P.split > 1) {
+        __syncwarp();
+        cluster_sync();
+        const int o0 = first % P.out_tiles * kOuts, r0 = first / P.out_tiles * NT;
+        const int share = NT / P.split;
+        for (int i = threadIdx.x; i < share * kOuts; i += kThreads) {
+            const int c = rank * share + i / kOuts, o = i % kOuts;
+            float v = 0.0f;
+            for (int q = 0; q < P.split; ++q) v += ld_cluster(ring + (uint32_t)(c * kOuts + o) * 4u, (uint32_t)q);
+            if (r0 + c < P.rows && o0 + o < P.outs) {
+                if (P.bias) v += P.bias[o0 + o];
+                if (P.act && v < 0.0f) v = 0.0f;
+                const int64_t at = (int64_t)(r0 + c) * P.out_stride + o0 + o;
+                if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[at] = __float2bfloat16(v);
+                else static_cast<float*>(P.out)[at] = v;
+            }
+        }
+        cluster_sync();                                // (nobody leaves while others read its memory)
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (threadIdx.x == 0 && *gave_up) atomicExch(&sr_operator_error, 1);
+    if (warp == 2) tmem_free(tmem, S::kAlloc);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn()
+{
+    static const EncodeTiledFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    return fn;
+}
+// Rows of bytes, box_rows rows x 128 bytes at a time.
+bool encode_rows(CUtensorMap* map, const void* data, int64_t row_bytes, int64_t rows, int box_rows)
+{
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Rows of a tile, and CTAs that share a tile's reduction: the pair with the least estimated time in cycles.  A stage costs its four MMAs (NT / 2 cycles each,
+// or (128 + NT) / 4 where the operands' way out of shared memory is longer) or its copies (60 bytes per cycle and SM).
+struct Plan {
+    int nt, split;
+};
+Plan plan_product(int64_t rows, int64_t outs, int stages, int sms)
+{
+    Plan best{16, 1};
+    double least = 1e300;
+    for (int nt : {16, 32, 64, 128, 192}) {
+        if (nt == 16 && rows > 16) continue;
+        if (nt == 32 && rows > 32) continue;          // (a tile starts at a multiple of 64 rows: two TMEM columns of scales)
+        const int64_t tiles = ((outs + kOuts - 1) / kOuts) * ((rows + nt - 1) / nt);
+        const double per_stage = std::max(4.0 * std::max(nt / 2.0, (128 + nt) / 4.0), (16384.0 + nt * 128.0) / 60.0);
+        const double drain = 16.0 * nt;
+        for (int split : {1, 2, 4, 8}) {
+            if (split > stages || (split > 1 && tiles * split > sms)) continue;
+            const double waves = (double)((tiles * split + sms - 1) / sms);
+            const double work = ((stages + split - 1) / split) * per_stage;
+            const double t = split > 1 ? work + drain / split + 1500.0 : waves * std::max(work, drain) + std::min(work, drain);
+            if (t < least) {
+                least = t;
+                best = {nt, split};
+            }
+        }
+    }
+    return best;
+}
+
+template <int FMT, int NT>
+cudaError_t launch(ProductArgs& P, int sms, cudaStream_t stream)
+{
+    using S = Shape<FMT, NT>;
+    P.ring = std::min(kMaxStages, (kSmem - 1024) / S::kStage);
+    const size_t smem = 1024 + (size_t)P.ring * S::kStage;
+    const cudaError_t e = cudaFuncSetAttribute(sr_product_kernel<FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = (int64_t)P.out_tiles * P.row_tiles;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)P.split;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(P.split > 1 ? tiles * P.split : std::min<int64_t>(tiles, sms)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = at;
+    cfg.numAttrs = P.split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, sr_product_kernel<FMT, NT>, P);
+}
+template <int FMT>
+cudaError_t launch_any(ProductArgs& P, int nt, int sms, cudaStream_t s)
+{
+    switch (nt) {
+        case 16: return launch<FMT, 16>(P, sms, s);
+        case 32: return launch<FMT, 32>(P, sms, s);
+        case 64: return launch<FMT, 64>(P, sms, s);
+        case 128: return launch<FMT, 128>(P, sms, s);
+        default: return launch<FMT, 192>(P, sms, s);
     }
 }
 
@@ -59,7 +343,7 @@ extern "C" {
 sr_status sr_microscale_product(const void* a_data, const void* a_scales, const void* w_data, const void* w_scales, int format, int64_t rows, int64_t cols,
                                 int64_t outs, const float* bias, int act, void* out, int out_dtype, int64_t out_stride, void* stream)
 {
-    const int64_t most = 0x7FFFFFFF;
+    const int64_t most = 0x7FFFFFFF - 256;
     if ((format != SR_FORMAT_MX8 && format != SR_FORMAT_MX4) || rows < 0 || outs < 0 || cols < 1 || rows > most || outs > most || cols > most ||
         (act != 0 && act != 1) || (out_dtype != SR_DTYPE_F32 && out_dtype != SR_DTYPE_BF16) || out_stride < outs)
         return SR_ERR_INVALID_ARG;
@@ -68,33 +352,54 @@ sr_status sr_microscale_product(const void* a_data, const void* a_scales, const 
     if (!a_data || !a_scales || !w_data || !w_scales || !out || (uintptr_t)out % el || ((uintptr_t)bias & 3) || ((uintptr_t)a_data & 15) ||
         ((uintptr_t)a_scales & 15) || ((uintptr_t)w_data & 15) || ((uintptr_t)w_scales & 15))
         return SR_ERR_INVALID_ARG;
+    const int sms = sr_device_sms();
+    if (sms < 1) return SR_ERR_CUDA;
     const SrScaled z = sr_scaled(rows, cols, format);
     ProductArgs P{};
-    P.a = static_cast<const uint8_t*>(a_data);
-    P.a_scales = static_cast<const uint8_t*>(a_scales);
-    P.w = static_cast<const uint8_t*>(w_data);
     P.w_scales = static_cast<const uint8_t*>(w_scales);
+    P.a_scales = static_cast<const uint8_t*>(a_scales);
     P.bias = bias;
     P.out = out;
-    P.rows = rows;
-    P.cols = cols;
-    P.outs = outs;
     P.out_stride = out_stride;
-    P.groups = z.groups;
-    P.tiles_g = z.tiles_g;
+    P.rows = (int32_t)rows;
+    P.outs = (int32_t)outs;
+    P.row_bytes = (int32_t)z.row_bytes;
+    P.tiles_g = (int32_t)z.tiles_g;
+    P.tiles_r = (int32_t)z.tiles_r;
+    P.stages = (int32_t)((z.row_bytes + 127) / 128);
+    const Plan plan = plan_product(rows, outs, P.stages, sms);
+    P.out_tiles = (int32_t)((outs + kOuts - 1) / kOuts);
+    P.row_tiles = (int32_t)((rows + plan.nt - 1) / plan.nt);
+    if ((int64_t)P.out_tiles * P.row_tiles > most) return SR_ERR_INVALID_ARG;
+    P.split = plan.split;
     P.act = act;
     P.out_bf16 = out_dtype == SR_DTYPE_BF16;
-    const dim3 grid((unsigned)((outs + 31) / 32), (unsigned)((rows + 31) / 32));
-    if (grid.y > 65535) return SR_ERR_INVALID_ARG;
+    if (!encode_rows(&P.w_map, w_data, z.row_bytes, outs, kOuts) || !encode_rows(&P.a_map, a_data, z.row_bytes, rows, plan.nt)) return SR_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (format == SR_FORMAT_MX4) sr_product_kernel<SR_FORMAT_MX4><<<grid, 256, 0, s>>>(P);
-    else sr_product_kernel<SR_FORMAT_MX8><<<grid, 256, 0, s>>>(P);
-    return cudaGetLastError() == cudaSuccess ? SR_OK : SR_ERR_CUDA;
+    const cudaError_t e = format == SR_FORMAT_MX4 ? launch_any<SR_FORMAT_MX4>(P, plan.nt, sms, s) : launch_any<SR_FORMAT_MX8>(P, plan.nt, sms, s);
+    return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
 }
 
 sr_status sr_operator_status(void* stream)
 {
-    return cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) == cudaSuccess ? SR_OK : SR_ERR_CUDA;
+    if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return SR_ERR_CUDA;
+    int expired = 0;
+    const int none = 0;
+    if (cudaMemcpyFromSymbol(&expired, sr_operator_error, sizeof(int)) != cudaSuccess) return SR_ERR_CUDA;
+    if (!expired) return SR_OK;
+    return cudaMemcpyToSymbol(sr_operator_error, &none, sizeof(int)) == cudaSuccess ? SR_ERR_TIMEOUT : SR_ERR_CUDA;
 }
 
 }  // extern "C"
+
+int sr_device_sms()
+{
+    static int known[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < 64 && known[dev]) return known[dev];
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev < 64) known[dev] = n;
+    return n;
+}
