@@ -25,7 +25,7 @@ __device__ int sr_operator_error;                     // 1: a bounded wait expir
 namespace {
 using namespace srx;
 
-constexpr int kThreads = 256, kOuts = 128, kMaxStages = 8;
+constexpr int kThreads = 384, kEpilogueWarps = 8, kOuts = 128, kMaxStages = 8;
 constexpr int kSmem = 200 * 1024;
 
 struct ProductArgs {
@@ -72,6 +72,52 @@ __device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t smem)
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+// max that hands a NaN on
+__device__ __forceinline__ float at_least(float v, float low)
+{
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(low));
+    return v;
+}
+
+// Epilogue of a warp: outputs of its lanes, every second chunk of CW columns, tile after tile.  A store of the warp is 32 neighbouring outputs of a row.
+template <int NT, int CW, typename T>
+__device__ __forceinline__ void drain(const ProductArgs& P, T* out, uint32_t taddr, int lane_out, int half, uint32_t tfull, uint32_t tempty, int first, int step,
+                                      int tiles, volatile int* gave_up)
+{
+    const float low = P.act ? 0.0f : -__int_as_float(0x7F800000);
+    uint32_t it = 0;
+    for (int t = first; t < tiles; t += step, ++it) {
+        const int o = t % P.out_tiles * kOuts + lane_out, r0 = t / P.out_tiles * NT;
+        const uint32_t acc = it & 1u;
+        const float b = P.bias && o < P.outs ? P.bias[o] : 0.0f;
+        if (!mbar_wait(tfull + 8 * acc, (it >> 1) & 1u, gave_up)) break;
+        tc_fence_after();
+        const int n = min(NT, P.rows - r0);
+        T* p = out + (int64_t)(r0 + half * CW) * P.out_stride + o;
+        for (int c = half * CW; c < n; c += 2 * CW, p += 2 * CW * P.out_stride) {
+            uint32_t v[CW];
+            tc_ld(taddr + acc * NT + c, v);
+            tc_wait_ld();
+            if (o < P.outs) {
+                T* q = p;
+                if (c + CW <= n) {
+#pragma unroll
+                    for (int i = 0; i < CW; ++i, q += P.out_stride) put(q, at_least(__uint_as_float(v[i]) + b, low));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < CW; ++i, q += P.out_stride)
+                        if (c + i < n) put(q, at_least(__uint_as_float(v[i]) + b, low));
+                }
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(tempty + 8 * acc);
+    }
+}
+
 template <int FMT, int NT>
 __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_constant__ ProductArgs P)
 {
@@ -92,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(tfull + 8 * a, 1);
-            mbar_init(tempty + 8 * a, 4);
+            mbar_init(tempty + 8 * a, kEpilogueWarps);
         }
         mbar_init_done();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&P.w_map) : "memory");
@@ -178,48 +224,26 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
         }
         __syncwarp();
     } else if (warp >= 4) {
+        // two warps per quarter of the lanes, which take its chunks of columns in turn
         constexpr int CW = NT < 32 ? NT : 32;
-        const int quarter = warp - 4;
-        uint32_t it = 0;
-        auto store = [&](int64_t row, int o, float v) {
-            if (P.act && v < 0.0f) v = 0.0f;
-            if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[row * P.out_stride + o] = __float2bfloat16(v);
-            else static_cast<float*>(P.out)[row * P.out_stride + o] = v;
-        };
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         if (P.split > 1) {
             // (one tile per cluster) the partial sums lie in the ring, which is idle by now: [column][output]
-            bool ok = mbar_wait(tfull, 0, gave_up);
+            const bool ok = mbar_wait(tfull, 0, gave_up);
             tc_fence_after();
             float* mine = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
-            for (int c = 0; c < NT && ok; c += CW) {
+            for (int c = half * CW; c < NT && ok; c += 2 * CW) {
                 uint32_t v[CW];
-                tc_ld(tmem + ((uint32_t)(quarter * 32) << 16) + c, v);
+                tc_ld(tmem + lanes + c, v);
                 tc_wait_ld();
 #pragma unroll
                 for (int i = 0; i < CW; ++i) mine[(c + i) * kOuts + quarter * 32 + lane] = __uint_as_float(v[i]);
             }
+        } else if (P.out_bf16) {
+            drain<NT, CW>(P, static_cast<__nv_bfloat16*>(P.out), tmem + lanes, quarter * 32 + lane, half, tfull, tempty, first, step, tiles, gave_up);
         } else {
-            for (int t = first; t < tiles; t += step, ++it) {
-                const int o = t % P.out_tiles * kOuts + quarter * 32 + lane, r0 = t / P.out_tiles * NT;
-                const uint32_t acc = it & 1u;
-                if (!mbar_wait(tfull + 8 * acc, (it >> 1) & 1u, gave_up)) break;
-                tc_fence_after();
-                const float b = P.bias && o < P.outs ? P.bias[o] : 0.0f;
-                const int n = min(NT, P.rows - r0);
-                for (int c = 0; c < n; c += CW) {
-                    uint32_t v[CW];
-                    tc_ld(tmem + acc * NT + ((uint32_t)(quarter * 32) << 16) + c, v);
-                    tc_wait_ld();
-                    if (o < P.outs) {
-#pragma unroll
-                        for (int i = 0; i < CW; ++i)
-                            if (c + i < n) store(r0 + c + i, o, __uint_as_float(v[i]) + b);
-                    }
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(tempty + 8 * acc);
-            }
+            drain<NT, CW>(P, static_cast<float*>(P.out), tmem + lanes, quarter * 32 + lane, half, tfull, tempty, first, step, tiles, gave_up);
         }
     }
     if (P.split > 1) {
@@ -233,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
             for (int q = 0; q < P.split; ++q) v += ld_cluster(ring + (uint32_t)(c * kOuts + o) * 4u, (uint32_t)q);
             if (r0 + c < P.rows && o0 + o < P.outs) {
                 if (P.bias) v += P.bias[o0 + o];
-                if (P.act && v < 0.0f) v = 0.0f;
+                if (P.act) v = at_least(v, 0.0f);
                 const int64_t at = (int64_t)(r0 + c) * P.out_stride + o0 + o;
                 if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[at] = __float2bfloat16(v);
                 else static_cast<float*>(P.out)[at] = v;
