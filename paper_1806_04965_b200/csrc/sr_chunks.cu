@@ -1,0 +1,803 @@
+// Linear attention over whole clips in bf16, chunk by chunk of 128 frames on the tensor cores.
+//
+// With G_i the sum of the log decays from a chunk's start up to frame i of it, S the state that enters the chunk and i, j frames of the chunk,
+//     out_i = scale * ( exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j ),
+//     S'    = exp(G_last) S + sum_j k_j (exp(G_last - G_j) v_j)^T:
+// four matrix products per chunk and group of 64 columns of v (the last one a CTA's: it holds DK x 64 values of a state), all of them tcgen05.mma
+// with M = 128:
+//   scores  Q K^T              128 frames x 128 frames, both from shared memory                       (TMEM columns 0 .. 127)
+//   near    P V                P = scores * decays, lower triangle, bf16, back in TMEM as the A operand (columns 320 .. 383)
+//   far     Q [S_hi | S_lo]    the state in two bf16 parts, 16 bits of it                             (columns 192 .. 319)
+//   state   K^T [V'_hi, V'_mid, V'_lo], V' = V exp(G_last - G_j) in three bf16 parts, 24 bits: the state itself is as exact as 32 bits make it
+//                              summed on top of the decayed state in TMEM                            (columns 128 .. 191)
+// K is read along both of its sides from the same tile.  Roundings to bf16: P (every product of it is rounded once, as the output is) and what the parts
+// leave out.
+// Decays never exceed one: exp(G_i - G_j) is a product of exp(G_i - G_e) and exp(G_e - G_j) with e the last frame of j's 32, where i lies behind them, and
+// one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
+//
+// Bound by memory (q, k, v, out once) where there are CTAs enough: a chunk of DK = 128 is 96 KiB per CTA, 2.6k cycles of MMAs.
+// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; warps 4..7 scores -> P, 8..11 state, 12..15 V', 16..19 outputs.
+// What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
+// the near product (whose zeros would spread it to earlier frames) and added by the outputs' warps; rows behind a sequence's last frame are zeroed.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "sr_memory.h"
+#include "sr_operators.h"
+#include "sr_ptx.cuh"
+
+namespace {
+using namespace srx;
+
+constexpr int kChunk = 128, kCols = 64, kThreads = 640;
+constexpr uint32_t kScores = 0, kState = 128, kFar = 192, kNear = 320;          // TMEM columns
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct ChunkArgs {
+    CUtensorMap q_map, k_map, v_map;
+    AttentionArgs A;
+    float* sums;                                       // [slot][group][dk][dv]: sums of a segment, then the states that enter it
+    float* decays;                                     // [slot][group]: decay over a segment
+    int64_t segment;                                   // frames of a segment (0: whole sequences)
+    int32_t slots, v_tiles, out_vec;
+    int* error;
+};
+
+// A CTA's work: frames t0 .. t0 + n - 1 of sequence b.
+struct Item {
+    int b, g, c0, slot;
+    int64_t t0, n, whole;                              // whole: frames of the sequence
+    AttentionSpan span;
+    bool there, last;
+};
+__device__ __forceinline__ int64_t segments_of(int64_t n, int64_t length) { return n > length ? (n + length - 1) / length : 1; }
+
+// The sequence and segment of a slot: slots count the segments of the sequences one after the other.  (All lanes of a warp.)
+__device__ __forceinline__ void find_slot(const ChunkArgs& C, int slot, int& b, int64_t& seg)
+{
+    const AttentionArgs& A = C.A;
+    if (!A.offsets) {
+        const int64_t per = segments_of(A.frames, C.segment);
+        b = (int)(slot / per);
+        seg = slot - b * per;
+        if (b >= A.batch) b = -1;
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    b = -1;
+    seg = 0;
+    for (int b0 = 0; b0 < A.batch; b0 += 32) {
+        const int64_t mine = b0 + lane < A.batch ? segments_of(attention_span(A, b0 + lane).n, C.segment) : 0;
+        int64_t sum = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+            if (lane >= d) sum += up;
+        }
+        const bool here = mine > 0 && before + sum - mine <= slot && slot < before + sum;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
+        if (who) {
+            const int w = __ffs(who) - 1;
+            b = b0 + w;
+            seg = slot - (before + __shfl_sync(0xFFFFFFFFu, sum - mine, w));
+            return;
+        }
+        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+}
+
+template <int MODE>
+__device__ __forceinline__ Item item_of(const ChunkArgs& C)
+{
+    const AttentionArgs& A = C.A;
+    Item it;
+    int x = blockIdx.x;
+    it.c0 = (x % C.v_tiles) * kCols;
+    x /= C.v_tiles;
+    it.g = x % A.groups;
+    x /= A.groups;
+    it.slot = x;
+    it.b = x;
+    int64_t seg = 0;
+    if (MODE != 0) find_slot(C, x, it.b, seg);
+    it.there = it.b >= 0;
+    if (!it.there) return it;
+    it.span = attention_span(A, it.b);
+    it.whole = it.span.n;
+    it.t0 = 0;
+    it.n = it.whole;
+    it.last = true;
+    if (MODE != 0) {
+        it.t0 = seg * C.segment;
+        it.n = min(C.segment, it.whole - it.t0);
+        it.last = it.t0 + it.n >= it.whole;
+    }
+    return it;
+}
+
+__device__ __forceinline__ float exp2_two(double x)   // 2^x, x as two floats
+{
+    const float hi = (float)x, lo = (float)(x - (double)hi);
+    const float y = exp2f(hi);
+    return fmaf(y, lo * kLn2, y);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
+// What a rounding left out; nothing where the value is not finite (the rounded part says so already).
+__device__ __forceinline__ float rest(float x, float rounded) { return finite(rounded) ? x - rounded : 0.0f; }
+
+struct alignas(16) Decays {                            // of a chunk (read four at a time); G in units of log 2
+    float hi[kChunk], lo[kChunk];                      // G_j in two floats
+    float col[kChunk];                                 // exp(G_e - G_j), e the last frame of j's 32
+    float rest[kChunk];                                // exp(G_last - G_j)
+    float row[kChunk];                                 // exp(G_i)
+    float whole;                                       // exp(G_last)
+};
+
+template <int DK, int MODE>
+__global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_constant__ ChunkArgs C)
+{
+    constexpr bool OUT = MODE != 1;                    // outputs are wanted
+    constexpr int NQ = DK == 64 ? 2 : 1;               // slots for queries
+    constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V, of a part of the state
+    constexpr int SW = DK / 32;                        // warps with rows of the state
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Decays decays[2];
+    __shared__ uint64_t bars[32];
+    __shared__ uint32_t odd_cols[2][2];                // columns of a chunk's values that are not all finite
+    __shared__ uint32_t tmem_slot;
+    __shared__ int gave_up_flag;
+    const AttentionArgs& A = C.A;
+    volatile int* gave_up = &gave_up_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    wait_for_predecessor();
+    const Item it = item_of<MODE>(C);
+    if (!it.there || (MODE == 1 && it.last)) return;
+    const int64_t state_at = ((int64_t)it.b * A.groups + it.g) * A.dk;
+    const int64_t slot_at = ((int64_t)it.slot * A.groups + it.g) * A.dk;
+    if (it.n == 0) {                                   // an empty sequence hands its state through
+        if (A.state_out && MODE != 1)
+            for (int i = threadIdx.x; i < A.dk * kCols; i += kThreads) {
+                const int r = i / kCols, j = it.c0 + i % kCols;
+                if (j < A.dv) A.state_out[(state_at + r) * A.dv + j] = A.state_in ? A.state_in[(state_at + r) * A.dv + j] : 0.0f;
+            }
+        return;
+    }
+    const int chunks = (int)((it.n + kChunk - 1) / kChunk);
+    const int share = OUT ? A.share : 1;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t k_tiles = base, v_tiles = k_tiles + 2 * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + NQ * KT, s_tiles = w_tiles + 3 * VT;
+    uint8_t* const generic = smem_raw + (base - smem_u32(smem_raw));
+    uint8_t *const k_mem = generic, *const v_mem = k_mem + 2 * KT, *const w_mem = v_mem + 2 * VT + NQ * KT, *const s_mem = w_mem + 3 * VT;
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    const uint32_t kv_full = bar(0), kv_empty = bar(2), q_full = bar(4), q_empty = bar(6), d_full = bar(8), d_empty = bar(10);
+    const uint32_t scored = bar(12), weighed = bar(13), far_near = bar(14), taken = bar(15), parted = bar(16), stated = bar(17), summed = bar(18), cleaned = bar(19);
+    if (threadIdx.x == 0) {
+        gave_up_flag = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(kv_full + 8 * i, 1);
+            mbar_init(kv_empty + 8 * i, 1);
+            mbar_init(q_full + 8 * i, 1);
+            mbar_init(q_empty + 8 * i, 1);
+            mbar_init(d_full + 8 * i, 1);
+            mbar_init(d_empty + 8 * i, 4 + SW + (OUT ? 8 : 0));
+        }
+        mbar_init(scored, 1);                          // scores are in TMEM
+        mbar_init(weighed, 4);                         // P is in TMEM
+        mbar_init(far_near, 1);                        // both parts of the outputs are in TMEM
+        mbar_init(taken, 4);                           // ... and have been read
+        mbar_init(parted, 4);                          // V' is in shared memory, V is fit for the near product
+        mbar_init(stated, SW);                         // the state's parts are in shared memory, the state in TMEM has decayed
+        mbar_init(summed, 1);                          // the chunk's sums are on top of the state
+        mbar_init(cleaned, 4);                         // rows behind the last frame are zeroed
+        mbar_init_done();
+    }
+    if (warp == 3) tmem_alloc(smem_u32(&tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    let_successor_start();
+    const uint32_t tmem = tmem_slot;
+    const int64_t f0 = it.span.first + it.t0;          // first frame
+    const int tail = (int)(it.n - (int64_t)(chunks - 1) * kChunk);       // frames of the last chunk
+    const bool clean = A.offsets && tail < kChunk;     // (otherwise there are zeros, or other frames of the sequence, only behind the tensor's end)
+    // In a segment of a sequence that does not end with it every chunk but the sequence's last is full, so the tail is the sequence's.
+
+    if (warp == 0) {
+        if (elect_one()) {
+            bool ok = true;
+            uint32_t n = 0;
+            auto load_kv = [&](int c) {
+                const uint32_t s = c & 1, b = kv_full + 8 * s;
+                ok = ok && mbar_wait(kv_empty + 8 * s, ((c >> 1) & 1) ^ 1, gave_up);
+                if (!ok) return;
+                mbar_expect_tx(b, KT + VT);
+                const int f = (int)(f0 + (int64_t)c * kChunk);
+#pragma unroll
+                for (int h = 0; h < DK / 64; ++h) tma_load_4d(k_tiles + s * KT + h * 16384, &C.k_map, b, h * 64, it.g, (int)it.span.b, f);
+                tma_load_4d(v_tiles + s * VT, &C.v_map, b, it.c0, it.g, (int)it.span.b, f);
+            };
+            load_kv(0);
+            for (int c = 0; c < chunks && ok; ++c) {
+                if (OUT) {
+                    for (int h = 0; h < share && ok; ++h, ++n) {
+                        const uint32_t s = n % NQ, b = q_full + 8 * s;
+                        ok = mbar_wait(q_empty + 8 * s, ((n / NQ) & 1) ^ 1, gave_up);
+                        if (!ok) break;
+                        mbar_expect_tx(b, KT);
+                        const int f = (int)(f0 + (int64_t)c * kChunk);
+#pragma unroll
+                        for (int p = 0; p < DK / 64; ++p) tma_load_4d(q_tiles + s * KT + p * 16384, &C.q_map, b, p * 64, it.g * A.share + h, (int)it.span.b, f);
+                        if (h == 0 && c + 1 < chunks) load_kv(c + 1);
+                    }
+                } else if (c + 1 < chunks) {
+                    load_kv(c + 1);
+                }
+            }
+            if (!ok) {                                 // what was asked for still has to land
+                for (int s = 0; s < 2; ++s) mbar_drain(kv_full + 8 * s, 0), mbar_drain(kv_full + 8 * s, 1);
+                for (int s = 0; s < NQ; ++s) mbar_drain(q_full + 8 * s, 0), mbar_drain(q_full + 8 * s, 1);
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            constexpr uint32_t i_scores = idesc_bf16(128, 0, 0), i_far = idesc_bf16(128, 0, 1), i_near = idesc_bf16(64, 0, 1), i_state = idesc_bf16(64, 1, 1);
+            bool ok = true;
+            uint32_t n = 0;                            // steps: chunks x heads
+            for (int c = 0; c < chunks && ok; ++c) {
+                const uint32_t s = c & 1, cp = (c >> 1) & 1;
+                const uint32_t k_at = k_tiles + s * KT, v_at = v_tiles + s * VT;
+                const int steps = ((c + 1 == chunks ? tail : kChunk) + 15) / 16;        // of 16 frames
+                ok = mbar_wait(kv_full + 8 * s, cp, gave_up);
+                if (clean && c + 1 == chunks) ok = ok && mbar_wait(cleaned, 0, gave_up);
+                for (int h = 0; h < share && ok; ++h, ++n) {
+                    const uint32_t qs = n % NQ, q_at = q_tiles + qs * KT;
+                    if (OUT) {
+                        ok = mbar_wait(q_full + 8 * qs, (n / NQ) & 1, gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < DK / 16; ++k)
+                            mma_bf16(tmem + kScores, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_k_major(k_at + (k / 4) * 16384) + 2 * (k % 4), i_scores, k > 0);
+                        tc_commit(scored);
+                    }
+                    if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
+                    if (OUT) {
+                        ok = ok && mbar_wait(taken, (n & 1) ^ 1, gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < DK / 16; ++k)
+                            mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, ST), i_far, k > 0);
+                        tc_commit(q_empty + 8 * qs);
+                    }
+                    if (h == 0) ok = ok && mbar_wait(parted, c & 1, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (h + 1 == share) {
+                        for (int p = 0; p < 3; ++p)
+                            for (int k = 0; k < steps; ++k)
+                                mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + p * VT + k * 2048, 0), i_state, 1);
+                        tc_commit(summed);
+                    }
+                    if (OUT) {
+                        ok = mbar_wait(weighed, n & 1, gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+                        for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kScores + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
+                        tc_commit(far_near);
+                    }
+                }
+                if (ok) tc_commit(kv_empty + 8 * s);
+            }
+        }
+    } else if (warp == 2) {
+        // decays of chunk after chunk
+        double carry = 0.0;                            // what the decays of whole chunks have lost by rounding, relative
+        const float* d = A.decay + it.span.b * A.sd.sequence + (int64_t)it.g * A.sd.head;
+        double log_whole = 0.0;
+        for (int c = 0; c < chunks; ++c) {
+            const int n = c + 1 == chunks ? tail : kChunk;
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = lane * 4 + e;
+                x[e] = 0.0f;
+                if (j < n) {
+                    x[e] = d[(f0 + (int64_t)c * kChunk + j) * A.sd.frame];
+                    if (x[e] < -128.0f) x[e] = -128.0f;          // (exp(-128) is zero in 32 bits; sums of infinities would be NaN)
+                }
+            }
+            double g[4];
+            g[0] = (double)x[0];
+#pragma unroll
+            for (int e = 1; e < 4; ++e) g[e] = g[e - 1] + (double)x[e];
+            double before = g[3];
+#pragma unroll
+            for (int m = 1; m < 32; m *= 2) {
+                const double up = __shfl_up_sync(0xFFFFFFFFu, before, m);
+                if (lane >= m) before += up;
+            }
+            const double total = __shfl_sync(0xFFFFFFFFu, before, 31);
+            before -= g[3];
+            log_whole += total;
+            constexpr double l2e = 1.4426950408889634074;
+            if (!mbar_wait_warp(d_empty + 8 * (c & 1), ((c >> 1) & 1) ^ 1, gave_up)) break;
+            Decays& D = decays[c & 1];
+            const double last = total * l2e;
+            double mine[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine[e] = (before + g[e]) * l2e;
+            const double block_end = __shfl_sync(0xFFFFFFFFu, mine[3], lane | 7);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = lane * 4 + e;
+                const float hi = (float)mine[e];
+                D.hi[j] = hi;
+                D.lo[j] = (float)(mine[e] - (double)hi);
+                D.col[j] = exp2_two(block_end - mine[e]);
+                D.rest[j] = exp2_two(last - mine[e]);
+                D.row[j] = exp2_two(mine[e]);
+            }
+            if (lane == 0) {
+                const double exact = exp2(last) * (1.0 + carry);
+                const float rounded = (float)exact;
+                D.whole = rounded;
+                carry = rounded > 1e-30f ? exact / (double)rounded - 1.0 : 0.0;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(d_full + 8 * (c & 1));
+        }
+        if (MODE == 1 && lane == 0 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
+    } else if (warp >= 4 && warp < 8) {
+        // scores -> P: a thread has a frame's row
+        if (OUT) {
+            const int w = warp - 4, i = w * 32 + lane;
+            const uint32_t at = tmem + kScores + ((uint32_t)(w * 32) << 16);
+            uint32_t n = 0;
+            bool ok = true;
+            for (int c = 0; c < chunks && ok; ++c) {
+                const Decays& D = decays[c & 1];
+                const int frames = c + 1 == chunks ? tail : kChunk, blocks = (frames + 31) / 32;
+                ok = mbar_wait_warp(d_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+                if (!ok) break;
+                const float hi = D.hi[i], lo = D.lo[i];
+                float rows[3];
+#pragma unroll
+                for (int m = 0; m < 3; ++m) rows[m] = m < w ? exp2f((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31])) : 0.0f;
+                for (int h = 0; h < share; ++h, ++n) {
+                    ok = mbar_wait_warp(scored, n & 1, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    for (int m = 0; m < blocks; ++m) {
+                        uint32_t p[16];
+                        if (m > w) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) p[e] = 0;
+                        } else {
+                            uint32_t x[32];
+                            tc_ld(at + m * 32, x);
+                            tc_wait_ld();
+                            if (m < w) {
+                                const float row = m == 0 ? rows[0] : m == 1 ? rows[1] : rows[2];
+#pragma unroll
+                                for (int e = 0; e < 32; e += 4) {
+                                    const float4 col = *reinterpret_cast<const float4*>(&D.col[m * 32 + e]);
+                                    p[e / 2] = pack_bf16(__uint_as_float(x[e]) * (row * col.x), __uint_as_float(x[e + 1]) * (row * col.y));
+                                    p[e / 2 + 1] = pack_bf16(__uint_as_float(x[e + 2]) * (row * col.z), __uint_as_float(x[e + 3]) * (row * col.w));
+                                }
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 32; e += 4) {
+                                    const float4 ch = *reinterpret_cast<const float4*>(&D.hi[m * 32 + e]), cl = *reinterpret_cast<const float4*>(&D.lo[m * 32 + e]);
+                                    const float y0 = __uint_as_float(x[e]) * exp2f((hi - ch.x) + (lo - cl.x)), y1 = __uint_as_float(x[e + 1]) * exp2f((hi - ch.y) + (lo - cl.y));
+                                    const float y2 = __uint_as_float(x[e + 2]) * exp2f((hi - ch.z) + (lo - cl.z)), y3 = __uint_as_float(x[e + 3]) * exp2f((hi - ch.w) + (lo - cl.w));
+                                    p[e / 2] = pack_bf16(e <= lane ? y0 : 0.0f, e + 1 <= lane ? y1 : 0.0f);
+                                    p[e / 2 + 1] = pack_bf16(e + 2 <= lane ? y2 : 0.0f, e + 3 <= lane ? y3 : 0.0f);
+                                }
+                            }
+                        }
+                        tc_st(at + m * 16, p);         // (over scores that this thread has read)
+                    }
+                    tc_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(weighed);
+                }
+                if (lane == 0) mbar_arrive(d_empty + 8 * (c & 1));
+            }
+        }
+    } else if (warp >= 8 && warp < 8 + SW) {
+        // the state: a thread has a row of it
+        const int w = warp - 8, r = w * 32 + lane;
+        const uint32_t at = tmem + kState + ((uint32_t)(w * 32) << 16);
+        const float* from = MODE == 2 ? C.sums + (slot_at + r) * A.dv : A.state_in ? A.state_in + (state_at + r) * A.dv : nullptr;
+        float* to = MODE == 1 ? C.sums + (slot_at + r) * A.dv : it.last && A.state_out ? A.state_out + (state_at + r) * A.dv : nullptr;
+        bool ok = true;
+        for (int c = 0; c <= chunks; ++c) {
+            float whole = 0.0f;
+            if (c < chunks) {
+                ok = mbar_wait_warp(d_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+                if (!ok) break;
+                whole = decays[c & 1].whole;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(d_empty + 8 * (c & 1));
+            }
+            if (c > 0) {
+                ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+            }
+#pragma unroll
+            for (int m = 0; m < kCols; m += 16) {
+                uint32_t x[16];
+                if (c > 0) {
+                    tc_ld(at + m, x);
+                    tc_wait_ld();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = it.c0 + m + e;
+                        x[e] = MODE != 1 && from && r < A.dk && j < A.dv ? __float_as_uint(from[j]) : 0u;
+                    }
+                }
+                if (c < chunks) {
+                    if (OUT) {
+                        uint32_t hi[8], lo[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float a = __uint_as_float(x[2 * e]), b = __uint_as_float(x[2 * e + 1]);
+                            hi[e] = pack_bf16(a, b);
+                            lo[e] = pack_bf16(rest(a, low_bf16(hi[e])), rest(b, high_bf16(hi[e])));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t place = (uint32_t)r * 128u + (((uint32_t)(m / 8 + e) ^ (r & 7)) << 4);
+                            *reinterpret_cast<uint4*>(s_mem + place) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
+                            *reinterpret_cast<uint4*>(s_mem + ST + place) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * whole);
+                    tc_st(at + m, x);
+                } else if (to && r < A.dk) {
+                    const int j = it.c0 + m;
+                    if (j + 16 <= A.dv && !((uintptr_t)(to + j) & 15)) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (j + e < A.dv) to[j + e] = __uint_as_float(x[e]);
+                    }
+                }
+                __syncwarp();
+            }
+            if (c < chunks) {
+                tc_wait_st();
+                fence_async_shared();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(stated);
+            }
+        }
+    } else if (warp >= 12 && warp < 16) {
+        // V': a thread has a frame's row
+        const int w = warp - 12, j = w * 32 + lane;
+        bool ok = true;
+        for (int c = 0; c < chunks && ok; ++c) {
+            const uint32_t s = c & 1;
+            const int frames = c + 1 == chunks ? tail : kChunk;
+            ok = mbar_wait_warp(kv_full + 8 * s, (c >> 1) & 1, gave_up);
+            if (!ok) break;
+            uint8_t* row = v_mem + s * VT + j * 128;
+            if (clean && c + 1 == chunks) {
+                if (j >= frames) {
+                    for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(row + x * 16) = make_uint4(0, 0, 0, 0);
+                    for (int h = 0; h < DK / 64; ++h)
+                        for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(k_mem + s * KT + h * 16384 + j * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(cleaned);
+            }
+            ok = mbar_wait_warp(d_full + 8 * s, (c >> 1) & 1, gave_up);
+            if (ok && c > 0) ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);               // (the parts of the chunk before have been read)
+            if (!ok) break;
+            const float weight = decays[s].rest[j];
+            if (OUT && threadIdx.x == 12 * 32) odd_cols[s][0] = odd_cols[s][1] = 0;
+            if (OUT) asm volatile("bar.sync 1, 128;" ::: "memory");
+            float zero = 0.0f;                         // NaN as soon as a value is not finite
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const uint32_t place = ((uint32_t)x ^ (j & 7)) << 4;
+                const uint4 v = *reinterpret_cast<const uint4*>(row + place);
+                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                uint32_t a[4], b[4], d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float y0 = low_bf16(in[e]), y1 = high_bf16(in[e]);
+                    zero = fmaf(y0, 0.0f, zero);
+                    zero = fmaf(y1, 0.0f, zero);
+                    y0 *= weight;
+                    y1 *= weight;
+                    a[e] = pack_bf16(y0, y1);
+                    y0 = rest(y0, low_bf16(a[e]));
+                    y1 = rest(y1, high_bf16(a[e]));
+                    b[e] = pack_bf16(y0, y1);
+                    d[e] = pack_bf16(y0 - low_bf16(b[e]), y1 - high_bf16(b[e]));
+                }
+                uint8_t* out = w_mem + j * 128 + place;
+                *reinterpret_cast<uint4*>(out) = make_uint4(a[0], a[1], a[2], a[3]);
+                *reinterpret_cast<uint4*>(out + VT) = make_uint4(b[0], b[1], b[2], b[3]);
+                *reinterpret_cast<uint4*>(out + 2 * VT) = make_uint4(d[0], d[1], d[2], d[3]);
+            }
+            if (OUT && !(zero == 0.0f)) {
+                for (int e = 0; e < kCols; ++e) {
+                    uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(e / 8) ^ (j & 7)) << 4)) + (e & 7);
+                    if ((*p & 0x7F80u) == 0x7F80u) {
+                        *p = 0;
+                        atomicOr(&odd_cols[s][e >> 5], 1u << (e & 31));
+                    }
+                }
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(parted);
+                mbar_arrive(d_empty + 8 * s);
+            }
+        }
+    } else if (OUT && warp >= 16) {
+        // outputs: a thread has a frame's row
+        const int w = warp - 16, i = w * 32 + lane;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        uint32_t n = 0;
+        bool ok = true;
+        for (int c = 0; c < chunks && ok; ++c) {
+            const Decays& D = decays[c & 1];
+            const int frames = c + 1 == chunks ? tail : kChunk;
+            const int64_t f = f0 + (int64_t)c * kChunk + i;
+            ok = mbar_wait_warp(d_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+            if (!ok) break;
+            const float row = D.row[i];
+            for (int h = 0; h < share; ++h, ++n) {
+                ok = mbar_wait_warp(far_near, n & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t odd[2] = {odd_cols[c & 1][0], odd_cols[c & 1][1]};
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + f * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + it.c0;
+#pragma unroll
+                for (int m = 0; m < kCols; m += 16) {
+                    uint32_t a[16], b[16], x[16];
+                    tc_ld(tmem + kFar + lanes + m, a);
+                    tc_ld(tmem + kFar + lanes + kCols + m, b);
+                    tc_ld(tmem + kNear + lanes + m, x);
+                    tc_wait_ld();
+                    if (m + 16 == kCols) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(taken);
+                    }
+                    __syncwarp();
+                    if (i < frames) {
+                    float y[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] = fmaf(row, __uint_as_float(a[e]) + __uint_as_float(b[e]), __uint_as_float(x[e]));
+                    if ((odd[m >> 5] >> (m & 31)) & 0xFFFFu) {
+                        // values that are not finite, left out above: their terms as the formula has them
+                        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(A.q) + it.span.b * A.sq.sequence + f * A.sq.frame + ((int64_t)it.g * A.share + h) * A.sq.head;
+#pragma unroll 1
+                        for (int j = 0; j <= i; ++j) {
+                            const int64_t fj = f0 + (int64_t)c * kChunk + j;
+                            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(A.v) + it.span.b * A.sv.sequence + fj * A.sv.frame + (int64_t)it.g * A.sv.head + it.c0 + m;
+                            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(A.k) + it.span.b * A.sk.sequence + fj * A.sk.frame + (int64_t)it.g * A.sk.head;
+                            float p = 0.0f;
+                            bool have = false;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const float value = it.c0 + m + e < A.dv ? __bfloat162float(v[e]) : 0.0f;
+                                if (finite(value)) continue;
+                                if (!have) {
+                                    for (int t = 0; t < A.dk; ++t) p = fmaf(__bfloat162float(q[t]), __bfloat162float(k[t]), p);
+                                    p *= exp2f((D.hi[i] - D.hi[j]) + (D.lo[i] - D.lo[j]));
+                                    have = true;
+                                }
+                                y[e] += p * value;
+                            }
+                        }
+                    }
+                    uint32_t z[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = pack_bf16(A.scale * y[2 * e], A.scale * y[2 * e + 1]);
+                    const int left = A.dv - it.c0 - m;
+                    if (left >= 16 && C.out_vec) {
+                        *reinterpret_cast<uint4*>(out + m) = make_uint4(z[0], z[1], z[2], z[3]);
+                        *reinterpret_cast<uint4*>(out + m + 8) = make_uint4(z[4], z[5], z[6], z[7]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (e < left) out[m + e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
+                    }
+                    }
+                    __syncwarp();
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(d_empty + 8 * (c & 1));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (threadIdx.x == 0 && *gave_up) atomicExch(C.error, 1);
+    if (warp == 3) tmem_free(tmem, 512);
+}
+
+// The states that enter the segments of a sequence, from their sums: one after the other, element by element.
+__global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant__ ChunkArgs C)
+{
+    __shared__ int64_t first_slot;
+    const AttentionArgs& A = C.A;
+    let_successor_start();
+    wait_for_predecessor();
+    const int b = blockIdx.y / A.groups, g = blockIdx.y % A.groups;
+    const AttentionSpan sp = attention_span(A, b);
+    const int64_t count = segments_of(sp.n, C.segment);
+    if (!A.offsets) {
+        if (threadIdx.x == 0) first_slot = (int64_t)b * count;
+    } else if (threadIdx.x < 32) {
+        int64_t before = 0;
+        for (int x = threadIdx.x; x < b; x += 32) before += segments_of(attention_span(A, x).n, C.segment);
+#pragma unroll
+        for (int m = 16; m; m /= 2) before += __shfl_xor_sync(0xFFFFFFFFu, before, m);
+        if (threadIdx.x == 0) first_slot = before;
+    }
+    __syncthreads();
+    const int64_t size = (int64_t)A.dk * A.dv, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= size) return;
+    float S = A.state_in ? A.state_in[((int64_t)b * A.groups + g) * size + i] : 0.0f;
+    for (int64_t s = 0; s < count && first_slot + s < C.slots; ++s) {                       // (offsets that overlap may ask for more slots than there are)
+        const int64_t slot = (first_slot + s) * A.groups + g;
+        float* p = C.sums + slot * size + i;
+        if (s + 1 < count) {
+            const float sum = *p;
+            *p = S;
+            S = fmaf(C.decays[slot], S, sum);
+        } else {
+            *p = S;
+        }
+    }
+}
+
+// [frames][sequences][heads][size] in boxes of 128 frames x 64 elements.
+bool encode(CUtensorMap* map, const void* data, const sr_attention_strides& st, int64_t size, int64_t heads, int64_t sequences, int64_t frames)
+{
+    const SrEncodeTiled fn = sr_encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)size, (cuuint64_t)heads, (cuuint64_t)sequences, (cuuint64_t)frames};
+    auto stride = [](int64_t s, int64_t n) { return (cuuint64_t)(n > 1 ? 2 * s : 16); };
+    const cuuint64_t strides[3] = {stride(st.head, heads), stride(st.sequence, sequences), stride(st.frame, frames)};
+    const cuuint32_t box[4] = {64, 1, 1, kChunk}, steps[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, int64_t sequences, int64_t frames)
+{
+    auto fits = [](int64_t s, int64_t n) { return n <= 1 || (s > 0 && s % 8 == 0 && s < ((int64_t)1 << 38)); };
+    return !((uintptr_t)p & 15) && fits(st.head, heads) && fits(st.sequence, sequences) && fits(st.frame, frames);
+}
+
+template <int DK, int MODE>
+cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
+{
+    constexpr int NQ = DK == 64 ? 2 : 1;
+    constexpr int smem = 1024 + 2 * DK * 256 + 2 * kCols * 256 + NQ * DK * 256 + 3 * kCols * 256 + 2 * DK * 128;
+    const cudaError_t e = cudaFuncSetAttribute(sr_chunks_kernel<DK, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sr_chunks_kernel<DK, MODE>, C);
+}
+template <int DK>
+cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
+{
+    const AttentionArgs& A = C.A;
+    const int64_t per_slot = (int64_t)A.groups * C.v_tiles;
+    if (!C.segment) return launch<DK, 0>(C, A.batch * per_slot, s);
+    cudaError_t e = launch<DK, 1>(C, C.slots * per_slot, s);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(((int64_t)A.dk * A.dv + 255) / 256), (unsigned)(A.batch * A.groups));
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, sr_segments_kernel, C);
+    return e != cudaSuccess ? e : launch<DK, 2>(C, C.slots * per_slot, s);
+}
+
+// Frames of a segment, 0: whole sequences.  Segments cost another pass over k and v and their states' way out and back, so they are for
+// launches that leave SMs without work.
+struct Cut {
+    int64_t segment, slots;
+};
+Cut cut_of(const sr_attention_desc* d, bool packed)
+{
+    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kCols - 1) / kCols);
+    const int64_t blocks = d->batch * per_slot, sms = std::max(1, sr_device_sms());
+    const int64_t total = packed ? d->frames : d->frames * d->batch;
+    Cut cut{0, 0};
+    if ((int64_t)d->batch * d->groups > 65535) return cut;
+    if (packed ? blocks >= 8 * sms : 2 * blocks > sms) return cut;
+    // about one wave of segments, of 512 frames at least
+    const int64_t want = std::max<int64_t>(1, (packed ? 4 : 1) * sms / per_slot);
+    int64_t length = (total + want - 1) / want;
+    length = std::max<int64_t>(512, (length + kChunk - 1) / kChunk * kChunk);
+    if (length >= d->frames) return cut;
+    cut.segment = length;
+    cut.slots = packed ? d->batch + d->frames / length : d->batch * ((d->frames + length - 1) / length);
+    return cut;
+}
+
+}  // namespace
+
+// Rows of q, k and v that TMA can copy, and sizes that the tiles hold.
+bool sr_chunks_fit(const sr_attention_desc* d, const void* q, const void* k, const void* v)
+{
+    return d->frames < 0x7FFFFF00 && copies_fit(q, d->q, d->heads, d->batch, d->frames) && copies_fit(k, d->k, d->groups, d->batch, d->frames) &&
+           copies_fit(v, d->v, d->groups, d->batch, d->frames);
+}
+bool sr_chunks_wanted(const sr_attention_desc* d)
+{
+    return d->dtype == SR_DTYPE_BF16 && d->dk <= 128 && d->frames >= 16 &&
+           (int64_t)(d->batch + d->frames) * d->groups * ((d->dv + kCols - 1) / kCols) <= 0x7FFFFFFF;
+}
+size_t sr_chunks_workspace(const sr_attention_desc* d, bool packed)
+{
+    const Cut cut = cut_of(d, packed);
+    return cut.segment ? (size_t)cut.slots * d->groups * ((size_t)d->dk * d->dv * 4 + 4) + 256 : 0;
+}
+
+cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d, void* workspace, cudaStream_t s)
+{
+    const Cut cut = cut_of(d, A.offsets != nullptr);
+    ChunkArgs C{};
+    C.A = A;
+    C.error = sr_operator_error_word();
+    if (!C.error) return cudaErrorUnknown;
+    C.segment = cut.segment;
+    C.slots = (int32_t)cut.slots;
+    C.v_tiles = (d->dv + kCols - 1) / kCols;
+    C.sums = static_cast<float*>(workspace);
+    C.decays = C.sums ? C.sums + (size_t)cut.slots * d->groups * d->dk * d->dv : nullptr;
+    auto whole = [](int64_t st, int64_t n) { return n <= 1 || st % 8 == 0; };
+    C.out_vec = !((uintptr_t)A.out & 15) && whole(A.so.frame, d->frames) && whole(A.so.sequence, d->batch) && whole(A.so.head, d->heads);
+    const int64_t sequences = A.offsets ? 1 : d->batch;
+    if (!encode(&C.q_map, A.q, A.sq, d->dk, d->heads, sequences, d->frames) || !encode(&C.k_map, A.k, A.sk, d->dk, d->groups, sequences, d->frames) ||
+        !encode(&C.v_map, A.v, A.sv, d->dv, d->groups, sequences, d->frames))
+        return cudaErrorInvalidValue;
+    return d->dk <= 64 ? launch_all<64>(C, s) : launch_all<128>(C, s);
+}

@@ -5,38 +5,9 @@
 #include <algorithm>
 #include <cstdint>
 
-#include "../../include/sr_rollout.h"
+#include "sr_memory.h"
 
 namespace {
-
-struct AttentionArgs {
-    const void *q, *k, *v;
-    const float* decay;
-    const int64_t* offsets;
-    const float* state_in;
-    float* state_out;
-    void* out;
-    int64_t frames;
-    int32_t batch, groups, share, dk, dv;              // share: heads per group
-    float scale;
-    sr_attention_strides sq, sk, sv, so, sd;
-};
-
-// First frame and number of frames of a sequence; base: what its strides `sequence` are multiplied with.
-struct Span {
-    int64_t first, n, b;
-};
-__device__ __forceinline__ Span span_of(const AttentionArgs& A, int b)
-{
-    Span s{0, A.frames, b};
-    if (A.offsets) {
-        const int64_t lo = min(max(A.offsets[b], (int64_t)0), A.frames), hi = min(max(A.offsets[b + 1], (int64_t)0), A.frames);
-        s.first = lo;
-        s.n = max(hi - lo, (int64_t)0);
-        s.b = 0;
-    }
-    return s;
-}
 
 // ------------------------------------------------------------------------------------------ frame by frame, any sizes
 // A block holds 64 columns of a group's state: thread (column, rs) the rows of split rs, four neighbouring rows out of every 4 * RS.
@@ -55,7 +26,7 @@ __global__ void __launch_bounds__(kRunCols * RS) sr_attention_frames_kernel(cons
     float* qs = ds + 16;                               // [ct][share][DK]
     const int b = blockIdx.x / A.groups, g = blockIdx.x % A.groups, c0 = blockIdx.y * kRunCols;
     const int col = threadIdx.x / RS, rs = threadIdx.x % RS, j = c0 + col;
-    const Span sp = span_of(A, b);
+    const AttentionSpan sp = attention_span(A, b);
     const T* q = static_cast<const T*>(A.q) + sp.b * A.sq.sequence + (int64_t)g * A.share * A.sq.head;
     const T* k = static_cast<const T*>(A.k) + sp.b * A.sk.sequence + (int64_t)g * A.sk.head;
     const T* v = static_cast<const T*>(A.v) + sp.b * A.sv.sequence + (int64_t)g * A.sv.head;
@@ -283,8 +254,7 @@ sr_status sr_linear_attention_workspace_bytes(const sr_attention_desc* d, int pa
     const sr_status st = check(d);
     if (st != SR_OK) return st;
     if (!bytes) return SR_ERR_INVALID_ARG;
-    (void)packed;
-    *bytes = 0;
+    *bytes = sr_chunks_wanted(d) ? sr_chunks_workspace(d, packed != 0) : 0;
     return SR_OK;
 }
 
@@ -298,14 +268,16 @@ sr_status sr_linear_attention_run(const sr_attention_desc* d, const void* q, con
     if (d->frames && (!q || !k || !v || !decay || !out || !aligned(q, d->dtype) || !aligned(k, d->dtype) || !aligned(v, d->dtype) || !aligned(out, d->dtype) ||
                       ((uintptr_t)decay & 3)))
         return SR_ERR_INVALID_ARG;
-    (void)workspace;
-    (void)workspace_bytes;
+    const size_t needed = sr_chunks_wanted(d) ? sr_chunks_workspace(d, offsets != nullptr) : 0;
+    if (needed && (!workspace || workspace_bytes < needed || ((uintptr_t)workspace & 255))) return SR_ERR_INVALID_ARG;
     AttentionArgs A = arguments(d, q, k, v, decay, out);
     A.offsets = offsets;
     A.state_in = state_in;
     A.state_out = state_out;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = d->dtype == SR_DTYPE_F32 ? launch_frames_any<float>(A, s) : launch_frames_any<__nv_bfloat16>(A, s);
+    cudaError_t e;
+    if (sr_chunks_wanted(d) && sr_chunks_fit(d, q, k, v)) e = sr_chunks_launch(A, d, workspace, s);
+    else e = d->dtype == SR_DTYPE_F32 ? launch_frames_any<float>(A, s) : launch_frames_any<__nv_bfloat16>(A, s);
     return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
 }
 

@@ -20,7 +20,7 @@
 #include "sr_operators.h"
 #include "sr_ptx.cuh"
 
-__device__ int sr_operator_error;                     // 1: a bounded wait expired
+static __device__ int sr_operator_error;              // 1: a bounded wait expired
 
 namespace {
 using namespace srx;
@@ -37,6 +37,7 @@ struct ProductArgs {
     int32_t rows, outs, row_bytes, tiles_g, tiles_r;
     int32_t out_tiles, row_tiles, stages, ring;       // stages of the whole reduction; ring slots
     int32_t act, out_bf16, split;
+    int* error;
 };
 
 template <int FMT, int NT>
@@ -92,7 +93,7 @@ __device__ __forceinline__ void drain(const ProductArgs& P, T* out, uint32_t tad
         const int o = t % P.out_tiles * kOuts + lane_out, r0 = t / P.out_tiles * NT;
         const uint32_t acc = it & 1u;
         const float b = P.bias && o < P.outs ? P.bias[o] : 0.0f;
-        if (!mbar_wait(tfull + 8 * acc, (it >> 1) & 1u, gave_up)) break;
+        if (!mbar_wait_warp(tfull + 8 * acc, (it >> 1) & 1u, gave_up)) break;
         tc_fence_after();
         const int n = min(NT, P.rows - r0);
         T* p = out + (int64_t)(r0 + half * CW) * P.out_stride + o;
@@ -144,12 +145,13 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
         asm volatile("prefetch.tensormap [%0];" ::"l"(&P.w_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&P.a_map) : "memory");
     }
+    wait_for_predecessor();
     if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), S::kAlloc);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    begin();
+    let_successor_start();
 
     const int rank = P.split > 1 ? (int)cluster_rank() : 0;
     const int first = P.split > 1 ? (int)blockIdx.x / P.split : (int)blockIdx.x, step = P.split > 1 ? (int)gridDim.x / P.split : (int)gridDim.x;
@@ -230,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         if (P.split > 1) {
             // (one tile per cluster) the partial sums lie in the ring, which is idle by now: [column][output]
-            const bool ok = mbar_wait(tfull, 0, gave_up);
+            const bool ok = mbar_wait_warp(tfull, 0, gave_up);
             tc_fence_after();
             float* mine = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
             for (int c = half * CW; c < NT && ok; c += 2 * CW) {
@@ -268,26 +270,14 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (threadIdx.x == 0 && *gave_up) atomicExch(&sr_operator_error, 1);
+    if (threadIdx.x == 0 && *gave_up) atomicExch(P.error, 1);
     if (warp == 2) tmem_free(tmem, S::kAlloc);
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_fn()
-{
-    static const EncodeTiledFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
-        return reinterpret_cast<EncodeTiledFn>(p);
-    }();
-    return fn;
-}
 // Rows of bytes, box_rows rows x 128 bytes at a time.
 bool encode_rows(CUtensorMap* map, const void* data, int64_t row_bytes, int64_t rows, int box_rows)
 {
-    const EncodeTiledFn fn = encode_fn();
+    const SrEncodeTiled fn = sr_encode_tiled();
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
     const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, steps[2] = {1, 1};
@@ -398,6 +388,8 @@ sr_status sr_microscale_product(const void* a_data, const void* a_scales, const 
     P.split = plan.split;
     P.act = act;
     P.out_bf16 = out_dtype == SR_DTYPE_BF16;
+    P.error = sr_operator_error_word();
+    if (!P.error) return SR_ERR_CUDA;
     if (!encode_rows(&P.w_map, w_data, z.row_bytes, outs, kOuts) || !encode_rows(&P.a_map, a_data, z.row_bytes, rows, plan.nt)) return SR_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = format == SR_FORMAT_MX4 ? launch_any<SR_FORMAT_MX4>(P, plan.nt, sms, s) : launch_any<SR_FORMAT_MX8>(P, plan.nt, sms, s);
@@ -415,6 +407,29 @@ sr_status sr_operator_status(void* stream)
 }
 
 }  // extern "C"
+
+int* sr_operator_error_word()
+{
+    static int* known[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+    if (dev < 64 && known[dev]) return known[dev];
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, sr_operator_error) != cudaSuccess) return nullptr;
+    if (dev < 64) known[dev] = static_cast<int*>(p);
+    return static_cast<int*>(p);
+}
+
+SrEncodeTiled sr_encode_tiled()
+{
+    static const SrEncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
+        return reinterpret_cast<SrEncodeTiled>(p);
+    }();
+    return fn;
+}
 
 int sr_device_sms()
 {

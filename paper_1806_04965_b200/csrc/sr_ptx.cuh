@@ -9,12 +9,11 @@ namespace srx {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// A kernel of this library may be scheduled while the one before it still runs; it reads and writes nothing of its caller's before this returns.
-__device__ __forceinline__ void begin()
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-}
+// These kernels may be scheduled while the one before them still runs (programmatic dependent launch): they touch nothing of their caller's before
+// wait_for_predecessor returns.  One that takes tensor memory does so between the two calls: it neither holds any while it waits, nor lets a successor, which
+// might hold some, start before it has its own.
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void mbar_init_done()
@@ -37,7 +36,7 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
 // Bounded wait: gives up after about a second, or once another role of the block has.  What waits for whom is a cycle-free chain of copies and MMAs, so
 // this never expires unless something is wrong; then the block still runs to its end and says so (see sr_operator_status).
 constexpr long long kWaitCycles = 2000000000ll;
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* gave_up)
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* gave_up)
 {
     const long long t0 = clock64();
     for (;;) {
@@ -55,8 +54,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 {
     return mbar_try_wait(bar, parity) || mbar_wait_slow(bar, parity, gave_up);
 }
+// All lanes of a warp, with one answer.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* gave_up)
+{
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, gave_up));
+}
 // For copies in flight, which have to land before the block gives its memory up: does not look at whether others gave up.
-__device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity)
+static __device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity)
 {
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, parity))
@@ -75,6 +79,11 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
 {
@@ -139,10 +148,40 @@ __device__ __forceinline__ void tc_ld(uint32_t taddr, uint32_t (&r)[32])
         : "r"(taddr) : "memory");
 }
 
+__device__ __forceinline__ void tc_st(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// bf16 MMAs, sums in 32 bits; A from shared memory or from tensor memory
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_bf16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Instruction descriptor: D = f32, A and B bf16, M = 128; a_mn, b_mn: the operand's rows in shared memory run along M or N instead of K
+__host__ __device__ constexpr uint32_t idesc_bf16(uint32_t n, uint32_t a_mn, uint32_t b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn << 15) | (b_mn << 16) | ((n >> 3) << 17) | (8u << 24);
+}
+
 // Descriptor of an operand in shared memory whose rows are 128 bytes, swizzled over 128 bytes, groups of 8 rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t addr)
 {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// The same memory read the other way: rows run along M or N, 64 elements each; `next`: bytes from one 64 elements of M or N to the next.  A step of
+// 16 along K is 2048 bytes.
+__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t next)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(next >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 
 }  // namespace srx
