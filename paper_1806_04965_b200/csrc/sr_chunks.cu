@@ -24,6 +24,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cstddef>
 
 #include "sr_memory.h"
 #include "sr_operators.h"
@@ -32,7 +33,7 @@
 namespace {
 using namespace srx;
 
-constexpr int kChunk = 128, kCols = 64, kThreads = 640;
+constexpr int kChunk = 128, kCols = 64, kThreads = 1024, kDecays = 4;
 constexpr uint32_t kScores = 0, kState = 128, kFar = 192, kNear = 320;          // TMEM columns
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -119,10 +120,16 @@ __device__ __forceinline__ Item item_of(const ChunkArgs& C)
     return it;
 }
 
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float exp2_two(double x)   // 2^x, x as two floats
 {
     const float hi = (float)x, lo = (float)(x - (double)hi);
-    const float y = exp2f(hi);
+    const float y = exp2_fast(hi);
     return fmaf(y, lo * kLn2, y);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
@@ -133,16 +140,43 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
-// What a rounding left out; nothing where the value is not finite (the rounded part says so already).
-__device__ __forceinline__ float rest(float x, float rounded) { return finite(rounded) ? x - rounded : 0.0f; }
+// What a rounding left out.  Where the value is infinite any finite number will do (the rounded part says so already): max makes one of the NaN.
+__device__ __forceinline__ float rest(float x, float rounded) { return fmaxf(x - rounded, -3.0e38f); }
 
 struct alignas(16) Decays {                            // of a chunk (read four at a time); G in units of log 2
     float hi[kChunk], lo[kChunk];                      // G_j in two floats
     float col[kChunk];                                 // exp(G_e - G_j), e the last frame of j's 32
     float rest[kChunk];                                // exp(G_last - G_j)
     float row[kChunk];                                 // exp(G_i)
+    uint32_t odd[8];                                   // columns of the chunk's values that are not all finite: a word of 32 columns for each of eight warps
     float whole;                                       // exp(G_last)
 };
+static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read as 16-byte words");
+
+// Values that are not finite have been left out of row i of a chunk's near product: their terms for 32 columns, as the formula has them, on top of the
+// stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
+__device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, __nv_bfloat16* out)
+{
+    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(A.q) + it.span.b * A.sq.sequence + (f0 + i) * A.sq.frame + ((int64_t)it.g * A.share + h) * A.sq.head;
+#pragma unroll 1
+    for (int j = 0; j <= i; ++j) {
+        const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(A.v) + it.span.b * A.sv.sequence + (f0 + j) * A.sv.frame + (int64_t)it.g * A.sv.head + c0;
+        const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(A.k) + it.span.b * A.sk.sequence + (f0 + j) * A.sk.frame + (int64_t)it.g * A.sk.head;
+        float p = 0.0f;
+        bool have = false;
+#pragma unroll 1
+        for (int e = 0; e < 32 && c0 + e < A.dv; ++e) {
+            const float value = __bfloat162float(v[e]);
+            if (finite(value)) continue;
+            if (!have) {
+                for (int t = 0; t < A.dk; ++t) p = fmaf(__bfloat162float(q[t]), __bfloat162float(k[t]), p);
+                p *= exp2_fast((D.hi[i] - D.hi[j]) + (D.lo[i] - D.lo[j])) * A.scale;
+                have = true;
+            }
+            out[e] = __float2bfloat16(__bfloat162float(out[e]) + p * value);
+        }
+    }
+}
 
 template <int DK, int MODE>
 __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_constant__ ChunkArgs C)
@@ -150,11 +184,10 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     constexpr bool OUT = MODE != 1;                    // outputs are wanted
     constexpr int NQ = DK == 64 ? 2 : 1;               // slots for queries
     constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V, of a part of the state
-    constexpr int SW = DK / 32;                        // warps with rows of the state
+    constexpr int SQ = DK / 32;                        // quarters of the TMEM lanes with rows of the state
     extern __shared__ uint8_t smem_raw[];
-    __shared__ Decays decays[2];
+    __shared__ Decays decays[kDecays];
     __shared__ uint64_t bars[32];
-    __shared__ uint32_t odd_cols[2][2];                // columns of a chunk's values that are not all finite
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_flag;
     const AttentionArgs& A = C.A;
@@ -181,8 +214,9 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     uint8_t* const generic = smem_raw + (base - smem_u32(smem_raw));
     uint8_t *const k_mem = generic, *const v_mem = k_mem + 2 * KT, *const w_mem = v_mem + 2 * VT + NQ * KT, *const s_mem = w_mem + 3 * VT;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
-    const uint32_t kv_full = bar(0), kv_empty = bar(2), q_full = bar(4), q_empty = bar(6), d_full = bar(8), d_empty = bar(10);
-    const uint32_t scored = bar(12), weighed = bar(13), far_near = bar(14), taken = bar(15), parted = bar(16), stated = bar(17), summed = bar(18), cleaned = bar(19);
+    const uint32_t kv_full = bar(0), kv_empty = bar(2), q_full = bar(4), q_empty = bar(6), d_full = bar(8), d_empty = bar(12);
+    const uint32_t scored = bar(16), weighed = bar(17), far_full = bar(18), far_free = bar(19), near_full = bar(20), near_free = bar(21);
+    const uint32_t parted = bar(22), decayed = bar(23), stated = bar(24), state_free = bar(25), summed = bar(26), cleaned = bar(27);
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int i = 0; i < 2; ++i) {
@@ -190,17 +224,23 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             mbar_init(kv_empty + 8 * i, 1);
             mbar_init(q_full + 8 * i, 1);
             mbar_init(q_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kDecays; ++i) {
             mbar_init(d_full + 8 * i, 1);
-            mbar_init(d_empty + 8 * i, 4 + SW + (OUT ? 8 : 0));
+            mbar_init(d_empty + 8 * i, 8 + 2 * SQ + (OUT ? 12 : 0));
         }
         mbar_init(scored, 1);                          // scores are in TMEM
         mbar_init(weighed, 4);                         // P is in TMEM
-        mbar_init(far_near, 1);                        // both parts of the outputs are in TMEM
-        mbar_init(taken, 4);                           // ... and have been read
-        mbar_init(parted, 4);                          // V' is in shared memory, V is fit for the near product
-        mbar_init(stated, SW);                         // the state's parts are in shared memory, the state in TMEM has decayed
-        mbar_init(summed, 1);                          // the chunk's sums are on top of the state
-        mbar_init(cleaned, 4);                         // rows behind the last frame are zeroed
+        mbar_init(far_full, 1);                        // the far part of the outputs is in TMEM
+        mbar_init(far_free, 8);                        // ... and has been read
+        mbar_init(near_full, 1);                       // the near part
+        mbar_init(near_free, 8);
+        mbar_init(parted, 8);                          // V' is in shared memory, V is fit for the near product
+        mbar_init(decayed, 2 * SQ);                    // the state in TMEM has decayed
+        mbar_init(stated, 2 * SQ);                     // the state's parts are in shared memory
+        mbar_init(state_free, 1);                      // ... and have been read
+        mbar_init(summed, 1);                          // the chunk's sums are on top of the state, V' has been read
+        mbar_init(cleaned, 8);                         // rows behind the last frame are zeroed
         mbar_init_done();
     }
     if (warp == 3) tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -211,8 +251,9 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     const uint32_t tmem = tmem_slot;
     const int64_t f0 = it.span.first + it.t0;          // first frame
     const int tail = (int)(it.n - (int64_t)(chunks - 1) * kChunk);       // frames of the last chunk
-    const bool clean = A.offsets && tail < kChunk;     // (otherwise there are zeros, or other frames of the sequence, only behind the tensor's end)
-    // In a segment of a sequence that does not end with it every chunk but the sequence's last is full, so the tail is the sequence's.
+    // Behind the last frame: zeros (the tensor's end), or frames of another packed sequence, which have to be.  (Chunks of a segment are full unless the
+    // sequence ends there.)
+    const bool clean = A.offsets && tail < kChunk;
 
     if (warp == 0) {
         if (elect_one()) {
@@ -272,53 +313,58 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                             mma_bf16(tmem + kScores, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_k_major(k_at + (k / 4) * 16384) + 2 * (k % 4), i_scores, k > 0);
                         tc_commit(scored);
                     }
-                    if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
-                    if (OUT) {
-                        ok = ok && mbar_wait(taken, (n & 1) ^ 1, gave_up);
+                    if (h == 0) {
+                        // ahead of everything that reads the state's parts: the next chunk's state waits for this
+                        ok = mbar_wait(decayed, c & 1, gave_up) && mbar_wait(parted, c & 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
-#pragma unroll
-                        for (int k = 0; k < DK / 16; ++k)
-                            mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, ST), i_far, k > 0);
-                        tc_commit(q_empty + 8 * qs);
-                    }
-                    if (h == 0) ok = ok && mbar_wait(parted, c & 1, gave_up);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (h + 1 == share) {
                         for (int p = 0; p < 3; ++p)
                             for (int k = 0; k < steps; ++k)
                                 mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + p * VT + k * 2048, 0), i_state, 1);
                         tc_commit(summed);
                     }
                     if (OUT) {
-                        ok = mbar_wait(weighed, n & 1, gave_up);
+                        if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
+                        ok = ok && mbar_wait(far_free, (n & 1) ^ 1, gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < DK / 16; ++k)
+                            mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, ST), i_far, k > 0);
+                        tc_commit(q_empty + 8 * qs);
+                        tc_commit(far_full);
+                        if (h + 1 == share) tc_commit(state_free);
+                        ok = mbar_wait(weighed, n & 1, gave_up) && mbar_wait(near_free, (n & 1) ^ 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
                         for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kScores + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
-                        tc_commit(far_near);
+                        tc_commit(near_full);
                     }
                 }
                 if (ok) tc_commit(kv_empty + 8 * s);
             }
         }
     } else if (warp == 2) {
-        // decays of chunk after chunk
+        // decays of chunk after chunk, a few chunks ahead of the others
         double carry = 0.0;                            // what the decays of whole chunks have lost by rounding, relative
         const float* d = A.decay + it.span.b * A.sd.sequence + (int64_t)it.g * A.sd.head;
         double log_whole = 0.0;
-        for (int c = 0; c < chunks; ++c) {
+        auto load = [&](int c, float (&x)[4]) {
             const int n = c + 1 == chunks ? tail : kChunk;
-            float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = lane * 4 + e;
-                x[e] = 0.0f;
-                if (j < n) {
-                    x[e] = d[(f0 + (int64_t)c * kChunk + j) * A.sd.frame];
-                    if (x[e] < -128.0f) x[e] = -128.0f;          // (exp(-128) is zero in 32 bits; sums of infinities would be NaN)
-                }
+                x[e] = c < chunks && j < n ? d[(f0 + (int64_t)c * kChunk + j) * A.sd.frame] : 0.0f;
             }
+        };
+        float next[4];
+        load(0, next);
+        for (int c = 0; c < chunks; ++c) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = next[e] < -128.0f ? -128.0f : next[e];    // (exp(-128) is zero in 32 bits; sums of infinities would be NaN)
+            load(c + 1, next);
+            constexpr double l2e = 1.4426950408889634074;
             double g[4];
             g[0] = (double)x[0];
 #pragma unroll
@@ -332,32 +378,37 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             const double total = __shfl_sync(0xFFFFFFFFu, before, 31);
             before -= g[3];
             log_whole += total;
-            constexpr double l2e = 1.4426950408889634074;
-            if (!mbar_wait_warp(d_empty + 8 * (c & 1), ((c >> 1) & 1) ^ 1, gave_up)) break;
-            Decays& D = decays[c & 1];
             const double last = total * l2e;
             double mine[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) mine[e] = (before + g[e]) * l2e;
             const double block_end = __shfl_sync(0xFFFFFFFFu, mine[3], lane | 7);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = lane * 4 + e;
-                const float hi = (float)mine[e];
-                D.hi[j] = hi;
-                D.lo[j] = (float)(mine[e] - (double)hi);
-                D.col[j] = exp2_two(block_end - mine[e]);
-                D.rest[j] = exp2_two(last - mine[e]);
-                D.row[j] = exp2_two(mine[e]);
-            }
-            if (lane == 0) {
-                const double exact = exp2(last) * (1.0 + carry);
-                const float rounded = (float)exact;
-                D.whole = rounded;
-                carry = rounded > 1e-30f ? exact / (double)rounded - 1.0 : 0.0;
-            }
+            const double exact = exp2(last) * (1.0 + carry);
+            const float rounded = (float)exact;
+            carry = rounded > 1e-30f ? exact / (double)rounded - 1.0 : 0.0;
+            const int slot = c % kDecays;
+            if (!mbar_wait_warp(d_empty + 8 * slot, ((c / kDecays) & 1) ^ 1, gave_up)) break;
+            Decays& D = decays[slot];
+            float4 hi, lo, col, rest, row;
+            auto fill = [&](double x, float& h, float& l, float& a, float& b, float& y) {
+                h = (float)x;
+                l = (float)(x - (double)h);
+                a = exp2_two(block_end - x);
+                b = exp2_two(last - x);
+                y = exp2_two(x);
+            };
+            fill(mine[0], hi.x, lo.x, col.x, rest.x, row.x);
+            fill(mine[1], hi.y, lo.y, col.y, rest.y, row.y);
+            fill(mine[2], hi.z, lo.z, col.z, rest.z, row.z);
+            fill(mine[3], hi.w, lo.w, col.w, rest.w, row.w);
+            reinterpret_cast<float4*>(D.hi)[lane] = hi;
+            reinterpret_cast<float4*>(D.lo)[lane] = lo;
+            reinterpret_cast<float4*>(D.col)[lane] = col;
+            reinterpret_cast<float4*>(D.rest)[lane] = rest;
+            reinterpret_cast<float4*>(D.row)[lane] = row;
+            if (lane == 0) D.whole = rounded;
             __syncwarp();
-            if (lane == 0) mbar_arrive(d_full + 8 * (c & 1));
+            if (lane == 0) mbar_arrive(d_full + 8 * slot);
         }
         if (MODE == 1 && lane == 0 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
     } else if (warp >= 4 && warp < 8) {
@@ -368,274 +419,282 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             uint32_t n = 0;
             bool ok = true;
             for (int c = 0; c < chunks && ok; ++c) {
-                const Decays& D = decays[c & 1];
-                const int frames = c + 1 == chunks ? tail : kChunk, blocks = (frames + 31) / 32;
-                ok = mbar_wait_warp(d_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+                const int slot = c % kDecays;
+                const Decays& D = decays[slot];
+                const int frames = c + 1 == chunks ? tail : kChunk, blocks = 2 * ((frames + 31) / 32);      // of 16 columns
+                ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
                 if (!ok) break;
                 const float hi = D.hi[i], lo = D.lo[i];
                 float rows[3];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) rows[m] = m < w ? exp2f((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31])) : 0.0f;
+                for (int m = 0; m < 3; ++m) rows[m] = m < w ? exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31])) : 0.0f;
                 for (int h = 0; h < share; ++h, ++n) {
                     ok = mbar_wait_warp(scored, n & 1, gave_up);
                     if (!ok) break;
                     tc_fence_after();
-                    for (int m = 0; m < blocks; ++m) {
-                        uint32_t p[16];
-                        if (m > w) {
+                    const int last = min(blocks, 2 * w + 2);             // blocks that reach to the diagonal
+                    uint32_t x[16];
+                    tc_ld(at, x);
+#pragma unroll 1
+                    for (int m = 0; m < last; ++m) {
+                        const int c0 = m * 16;
+                        float y[16];
+                        tc_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) p[e] = 0;
+                        for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(x[e]);
+                        if (m + 1 < last) tc_ld(at + c0 + 16, x);
+                        uint32_t p[8];
+                        if (m < 2 * w) {
+                            const float row = m < 2 ? rows[0] : m < 4 ? rows[1] : rows[2];
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 col = *reinterpret_cast<const float4*>(&D.col[c0 + e]);
+                                p[e / 2] = pack_bf16(y[e] * (row * col.x), y[e + 1] * (row * col.y));
+                                p[e / 2 + 1] = pack_bf16(y[e + 2] * (row * col.z), y[e + 3] * (row * col.w));
+                            }
                         } else {
-                            uint32_t x[32];
-                            tc_ld(at + m * 32, x);
-                            tc_wait_ld();
-                            if (m < w) {
-                                const float row = m == 0 ? rows[0] : m == 1 ? rows[1] : rows[2];
+                            const int d = i - c0;
 #pragma unroll
-                                for (int e = 0; e < 32; e += 4) {
-                                    const float4 col = *reinterpret_cast<const float4*>(&D.col[m * 32 + e]);
-                                    p[e / 2] = pack_bf16(__uint_as_float(x[e]) * (row * col.x), __uint_as_float(x[e + 1]) * (row * col.y));
-                                    p[e / 2 + 1] = pack_bf16(__uint_as_float(x[e + 2]) * (row * col.z), __uint_as_float(x[e + 3]) * (row * col.w));
-                                }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 32; e += 4) {
-                                    const float4 ch = *reinterpret_cast<const float4*>(&D.hi[m * 32 + e]), cl = *reinterpret_cast<const float4*>(&D.lo[m * 32 + e]);
-                                    const float y0 = __uint_as_float(x[e]) * exp2f((hi - ch.x) + (lo - cl.x)), y1 = __uint_as_float(x[e + 1]) * exp2f((hi - ch.y) + (lo - cl.y));
-                                    const float y2 = __uint_as_float(x[e + 2]) * exp2f((hi - ch.z) + (lo - cl.z)), y3 = __uint_as_float(x[e + 3]) * exp2f((hi - ch.w) + (lo - cl.w));
-                                    p[e / 2] = pack_bf16(e <= lane ? y0 : 0.0f, e + 1 <= lane ? y1 : 0.0f);
-                                    p[e / 2 + 1] = pack_bf16(e + 2 <= lane ? y2 : 0.0f, e + 3 <= lane ? y3 : 0.0f);
-                                }
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 ch = *reinterpret_cast<const float4*>(&D.hi[c0 + e]), cl = *reinterpret_cast<const float4*>(&D.lo[c0 + e]);
+                                const float z0 = y[e] * exp2_fast((hi - ch.x) + (lo - cl.x)), z1 = y[e + 1] * exp2_fast((hi - ch.y) + (lo - cl.y));
+                                const float z2 = y[e + 2] * exp2_fast((hi - ch.z) + (lo - cl.z)), z3 = y[e + 3] * exp2_fast((hi - ch.w) + (lo - cl.w));
+                                p[e / 2] = pack_bf16(e <= d ? z0 : 0.0f, e + 1 <= d ? z1 : 0.0f);
+                                p[e / 2 + 1] = pack_bf16(e + 2 <= d ? z2 : 0.0f, e + 3 <= d ? z3 : 0.0f);
                             }
                         }
-                        tc_st(at + m * 16, p);         // (over scores that this thread has read)
+                        tc_st(at + m * 8, p);          // (over scores that this thread has read)
                     }
+                    const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    for (int m = last; m < blocks; ++m) tc_st(at + m * 8, none);
                     tc_wait_st();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(weighed);
                 }
-                if (lane == 0) mbar_arrive(d_empty + 8 * (c & 1));
+                if (lane == 0) mbar_arrive(d_empty + 8 * slot);
             }
         }
-    } else if (warp >= 8 && warp < 8 + SW) {
-        // the state: a thread has a row of it
-        const int w = warp - 8, r = w * 32 + lane;
-        const uint32_t at = tmem + kState + ((uint32_t)(w * 32) << 16);
-        const float* from = MODE == 2 ? C.sums + (slot_at + r) * A.dv : A.state_in ? A.state_in + (state_at + r) * A.dv : nullptr;
-        float* to = MODE == 1 ? C.sums + (slot_at + r) * A.dv : it.last && A.state_out ? A.state_out + (state_at + r) * A.dv : nullptr;
-        bool ok = true;
-        for (int c = 0; c <= chunks; ++c) {
-            float whole = 0.0f;
-            if (c < chunks) {
-                ok = mbar_wait_warp(d_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
-                if (!ok) break;
-                whole = decays[c & 1].whole;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(d_empty + 8 * (c & 1));
-            }
-            if (c > 0) {
-                ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
-                if (!ok) break;
-                tc_fence_after();
-            }
-#pragma unroll
-            for (int m = 0; m < kCols; m += 16) {
-                uint32_t x[16];
-                if (c > 0) {
-                    tc_ld(at + m, x);
-                    tc_wait_ld();
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = it.c0 + m + e;
-                        x[e] = MODE != 1 && from && r < A.dk && j < A.dv ? __float_as_uint(from[j]) : 0u;
-                    }
-                }
+    } else if (warp >= 8 && warp < 16) {
+        // the state: a thread has 32 columns of a row of it
+        const int w = warp & 3, half = (warp - 8) >> 2, r = w * 32 + lane, j0 = it.c0 + half * 32;
+        if (w < SQ) {
+            const uint32_t at = tmem + kState + ((uint32_t)(w * 32) << 16) + half * 32;
+            const float* from = MODE == 2 ? C.sums + (slot_at + r) * A.dv : A.state_in ? A.state_in + (state_at + r) * A.dv : nullptr;
+            float* to = MODE == 1 ? C.sums + (slot_at + r) * A.dv : it.last && A.state_out ? A.state_out + (state_at + r) * A.dv : nullptr;
+            bool ok = true;
+            for (int c = 0; c <= chunks; ++c) {
+                float whole = 0.0f;
                 if (c < chunks) {
-                    if (OUT) {
-                        uint32_t hi[8], lo[8];
+                    const int slot = c % kDecays;
+                    ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
+                    if (!ok) break;
+                    whole = decays[slot].whole;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(d_empty + 8 * slot);
+                }
+                if (c > 0) {
+                    ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                uint32_t hi[16], lo[16];
+#pragma unroll
+                for (int m = 0; m < 32; m += 16) {
+                    uint32_t x[16];
+                    const int j = j0 + m;
+                    if (c > 0) {
+                        tc_ld(at + m, x);
+                        tc_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = MODE != 1 && from && r < A.dk && j + e < A.dv ? __float_as_uint(from[j + e]) : 0u;
+                    }
+                    if (c == chunks) {
+                        if (to && r < A.dk) {
+                            if (j + 16 <= A.dv && !((uintptr_t)(to + j) & 15)) {
+#pragma unroll
+                                for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e)
+                                    if (j + e < A.dv) to[j + e] = __uint_as_float(x[e]);
+                            }
+                        }
+                        __syncwarp();
+                        continue;
+                    }
+                    if (OUT)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const float a = __uint_as_float(x[2 * e]), b = __uint_as_float(x[2 * e + 1]);
-                            hi[e] = pack_bf16(a, b);
-                            lo[e] = pack_bf16(rest(a, low_bf16(hi[e])), rest(b, high_bf16(hi[e])));
+                            hi[m / 2 + e] = pack_bf16(a, b);
+                            lo[m / 2 + e] = pack_bf16(rest(a, low_bf16(hi[m / 2 + e])), rest(b, high_bf16(hi[m / 2 + e])));
                         }
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t place = (uint32_t)r * 128u + (((uint32_t)(m / 8 + e) ^ (r & 7)) << 4);
-                            *reinterpret_cast<uint4*>(s_mem + place) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
-                            *reinterpret_cast<uint4*>(s_mem + ST + place) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
-                        }
-                    }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * whole);
                     tc_st(at + m, x);
-                } else if (to && r < A.dk) {
-                    const int j = it.c0 + m;
-                    if (j + 16 <= A.dv && !((uintptr_t)(to + j) & 15)) {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (j + e < A.dv) to[j + e] = __uint_as_float(x[e]);
-                    }
                 }
-                __syncwarp();
-            }
-            if (c < chunks) {
+                if (c == chunks) break;
                 tc_wait_st();
-                fence_async_shared();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(stated);
+                if (lane == 0) mbar_arrive(decayed);
+                if (OUT) {
+                    if (c > 0) {
+                        ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
+                        if (!ok) break;
+                    }
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        const uint32_t place = (uint32_t)r * 128u + (((uint32_t)(half * 4 + m) ^ (r & 7)) << 4);
+                        *reinterpret_cast<uint4*>(s_mem + place) = make_uint4(hi[4 * m], hi[4 * m + 1], hi[4 * m + 2], hi[4 * m + 3]);
+                        *reinterpret_cast<uint4*>(s_mem + ST + place) = make_uint4(lo[4 * m], lo[4 * m + 1], lo[4 * m + 2], lo[4 * m + 3]);
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(stated);
+                }
             }
         }
-    } else if (warp >= 12 && warp < 16) {
-        // V': a thread has a frame's row
-        const int w = warp - 12, j = w * 32 + lane;
+    } else if (warp >= 16 && warp < 24) {
+        // V': a thread has 32 values of a frame's row
+        const int w = warp & 3, half = (warp - 16) >> 2, j = w * 32 + lane;
         bool ok = true;
         for (int c = 0; c < chunks && ok; ++c) {
             const uint32_t s = c & 1;
+            const int slot = c % kDecays;
             const int frames = c + 1 == chunks ? tail : kChunk;
             ok = mbar_wait_warp(kv_full + 8 * s, (c >> 1) & 1, gave_up);
             if (!ok) break;
             uint8_t* row = v_mem + s * VT + j * 128;
             if (clean && c + 1 == chunks) {
                 if (j >= frames) {
-                    for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(row + x * 16) = make_uint4(0, 0, 0, 0);
-                    for (int h = 0; h < DK / 64; ++h)
-                        for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(k_mem + s * KT + h * 16384 + j * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+                    for (int x = 0; x < 4; ++x) *reinterpret_cast<uint4*>(row + (half * 4 + x) * 16) = make_uint4(0, 0, 0, 0);
+                    for (int x = 0; x < 8; ++x)
+                        if (half < DK / 64) *reinterpret_cast<uint4*>(k_mem + s * KT + half * 16384 + j * 128 + x * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_async_shared();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(cleaned);
             }
-            ok = mbar_wait_warp(d_full + 8 * s, (c >> 1) & 1, gave_up);
-            if (ok && c > 0) ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);               // (the parts of the chunk before have been read)
+            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
             if (!ok) break;
-            const float weight = decays[s].rest[j];
-            if (OUT && threadIdx.x == 12 * 32) odd_cols[s][0] = odd_cols[s][1] = 0;
-            if (OUT) asm volatile("bar.sync 1, 128;" ::: "memory");
-            float zero = 0.0f;                         // NaN as soon as a value is not finite
+            const float weight = decays[slot].rest[j];
+            __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);      // NaN as soon as a value is not finite
+            uint32_t a[16], b[16], d[16];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const uint32_t place = ((uint32_t)x ^ (j & 7)) << 4;
-                const uint4 v = *reinterpret_cast<const uint4*>(row + place);
+            for (int x = 0; x < 4; ++x) {
+                const uint4 v = *reinterpret_cast<const uint4*>(row + (((uint32_t)(half * 4 + x) ^ (j & 7)) << 4));
                 const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                uint32_t a[4], b[4], d[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float y0 = low_bf16(in[e]), y1 = high_bf16(in[e]);
-                    zero = fmaf(y0, 0.0f, zero);
-                    zero = fmaf(y1, 0.0f, zero);
-                    y0 *= weight;
-                    y1 *= weight;
-                    a[e] = pack_bf16(y0, y1);
-                    y0 = rest(y0, low_bf16(a[e]));
-                    y1 = rest(y1, high_bf16(a[e]));
-                    b[e] = pack_bf16(y0, y1);
-                    d[e] = pack_bf16(y0 - low_bf16(b[e]), y1 - high_bf16(b[e]));
+                    if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
+                    float y0 = low_bf16(in[e]) * weight, y1 = high_bf16(in[e]) * weight;
+                    const uint32_t hi = pack_bf16(y0, y1);
+                    y0 = rest(y0, low_bf16(hi));
+                    y1 = rest(y1, high_bf16(hi));
+                    const uint32_t mid = pack_bf16(y0, y1);
+                    a[4 * x + e] = hi;
+                    b[4 * x + e] = mid;
+                    d[4 * x + e] = pack_bf16(y0 - low_bf16(mid), y1 - high_bf16(mid));
                 }
-                uint8_t* out = w_mem + j * 128 + place;
-                *reinterpret_cast<uint4*>(out) = make_uint4(a[0], a[1], a[2], a[3]);
-                *reinterpret_cast<uint4*>(out + VT) = make_uint4(b[0], b[1], b[2], b[3]);
-                *reinterpret_cast<uint4*>(out + 2 * VT) = make_uint4(d[0], d[1], d[2], d[3]);
             }
-            if (OUT && !(zero == 0.0f)) {
-                for (int e = 0; e < kCols; ++e) {
-                    uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(e / 8) ^ (j & 7)) << 4)) + (e & 7);
-                    if ((*p & 0x7F80u) == 0x7F80u) {
-                        *p = 0;
-                        atomicOr(&odd_cols[s][e >> 5], 1u << (e & 31));
+            if (OUT) {
+                uint32_t cols = 0;
+                if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
+#pragma unroll 1
+                    for (int e = 0; e < 32; ++e) {
+                        uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(half * 4 + e / 8) ^ (j & 7)) << 4)) + (e & 7);
+                        const bool is = (*p & 0x7F80u) == 0x7F80u;
+                        if (is) *p = 0;
+                        if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
                     }
                 }
+                if (lane == 0) decays[slot].odd[half * 4 + w] = cols;
+            }
+            if (c > 0) {
+                ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);       // the parts of the chunk before have been read
+                if (!ok) break;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                uint8_t* out = w_mem + j * 128 + (((uint32_t)(half * 4 + x) ^ (j & 7)) << 4);
+                *reinterpret_cast<uint4*>(out) = make_uint4(a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3]);
+                *reinterpret_cast<uint4*>(out + VT) = make_uint4(b[4 * x], b[4 * x + 1], b[4 * x + 2], b[4 * x + 3]);
+                *reinterpret_cast<uint4*>(out + 2 * VT) = make_uint4(d[4 * x], d[4 * x + 1], d[4 * x + 2], d[4 * x + 3]);
             }
             fence_async_shared();
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(parted);
-                mbar_arrive(d_empty + 8 * s);
+                mbar_arrive(d_empty + 8 * slot);
             }
         }
-    } else if (OUT && warp >= 16) {
-        // outputs: a thread has a frame's row
-        const int w = warp - 16, i = w * 32 + lane;
-        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+    } else if (OUT && warp >= 24) {
+        // outputs: a thread has 32 columns of a frame's row
+        const int w = warp & 3, half = (warp - 24) >> 2, i = w * 32 + lane, j0 = it.c0 + half * 32;
+        const uint32_t lanes = ((uint32_t)(w * 32) << 16) + half * 32;
         uint32_t n = 0;
         bool ok = true;
         for (int c = 0; c < chunks && ok; ++c) {
-            const Decays& D = decays[c & 1];
+            const int slot = c % kDecays;
+            const Decays& D = decays[slot];
             const int frames = c + 1 == chunks ? tail : kChunk;
             const int64_t f = f0 + (int64_t)c * kChunk + i;
-            ok = mbar_wait_warp(d_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
             if (!ok) break;
             const float row = D.row[i];
             for (int h = 0; h < share; ++h, ++n) {
-                ok = mbar_wait_warp(far_near, n & 1, gave_up);
+                ok = mbar_wait_warp(far_full, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t odd[2] = {odd_cols[c & 1][0], odd_cols[c & 1][1]};
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + f * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + it.c0;
+                float y[32];
 #pragma unroll
-                for (int m = 0; m < kCols; m += 16) {
-                    uint32_t a[16], b[16], x[16];
+                for (int m = 0; m < 32; m += 8) {
+                    uint32_t a[8], b[8];
                     tc_ld(tmem + kFar + lanes + m, a);
-                    tc_ld(tmem + kFar + lanes + kCols + m, b);
+                    tc_ld(tmem + kFar + kCols + lanes + m, b);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[m + e] = row * (__uint_as_float(a[e]) + __uint_as_float(b[e]));
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(far_free);
+                ok = mbar_wait_warp(near_full, n & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int m = 0; m < 32; m += 16) {
+                    uint32_t x[16];
                     tc_ld(tmem + kNear + lanes + m, x);
                     tc_wait_ld();
-                    if (m + 16 == kCols) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(taken);
-                    }
-                    __syncwarp();
-                    if (i < frames) {
-                    float y[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) y[e] = fmaf(row, __uint_as_float(a[e]) + __uint_as_float(b[e]), __uint_as_float(x[e]));
-                    if ((odd[m >> 5] >> (m & 31)) & 0xFFFFu) {
-                        // values that are not finite, left out above: their terms as the formula has them
-                        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(A.q) + it.span.b * A.sq.sequence + f * A.sq.frame + ((int64_t)it.g * A.share + h) * A.sq.head;
-#pragma unroll 1
-                        for (int j = 0; j <= i; ++j) {
-                            const int64_t fj = f0 + (int64_t)c * kChunk + j;
-                            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(A.v) + it.span.b * A.sv.sequence + fj * A.sv.frame + (int64_t)it.g * A.sv.head + it.c0 + m;
-                            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(A.k) + it.span.b * A.sk.sequence + fj * A.sk.frame + (int64_t)it.g * A.sk.head;
-                            float p = 0.0f;
-                            bool have = false;
+                    for (int e = 0; e < 16; ++e) y[m + e] += __uint_as_float(x[e]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(near_free);
+                const uint4 odd = *reinterpret_cast<const uint4*>(&D.odd[half * 4]);
+                if (i < frames) {
+                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + f * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + j0;
+                    const int left = A.dv - j0;
+                    if (left >= 32 && C.out_vec) {
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const float value = it.c0 + m + e < A.dv ? __bfloat162float(v[e]) : 0.0f;
-                                if (finite(value)) continue;
-                                if (!have) {
-                                    for (int t = 0; t < A.dk; ++t) p = fmaf(__bfloat162float(q[t]), __bfloat162float(k[t]), p);
-                                    p *= exp2f((D.hi[i] - D.hi[j]) + (D.lo[i] - D.lo[j]));
-                                    have = true;
-                                }
-                                y[e] += p * value;
-                            }
-                        }
-                    }
-                    uint32_t z[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = pack_bf16(A.scale * y[2 * e], A.scale * y[2 * e + 1]);
-                    const int left = A.dv - it.c0 - m;
-                    if (left >= 16 && C.out_vec) {
-                        *reinterpret_cast<uint4*>(out + m) = make_uint4(z[0], z[1], z[2], z[3]);
-                        *reinterpret_cast<uint4*>(out + m + 8) = make_uint4(z[4], z[5], z[6], z[7]);
+                        for (int e = 0; e < 32; e += 8)
+                            *reinterpret_cast<uint4*>(out + e) = make_uint4(pack_bf16(A.scale * y[e], A.scale * y[e + 1]), pack_bf16(A.scale * y[e + 2], A.scale * y[e + 3]),
+                                                                            pack_bf16(A.scale * y[e + 4], A.scale * y[e + 5]), pack_bf16(A.scale * y[e + 6], A.scale * y[e + 7]));
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (e < left) out[m + e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
+                        for (int e = 0; e < 32; ++e)
+                            if (e < left) out[e] = __float2bfloat16(A.scale * y[e]);
                     }
-                    }
-                    __syncwarp();
+                    if (odd.x | odd.y | odd.z | odd.w) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, out);
                 }
+                __syncwarp();
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(d_empty + 8 * (c & 1));
+            if (lane == 0) mbar_arrive(d_empty + 8 * slot);
         }
     }
     tc_fence_before();
@@ -765,10 +824,11 @@ Cut cut_of(const sr_attention_desc* d, bool packed)
 }  // namespace
 
 // Rows of q, k and v that TMA can copy, and sizes that the tiles hold.
-bool sr_chunks_fit(const sr_attention_desc* d, const void* q, const void* k, const void* v)
+bool sr_chunks_fit(const sr_attention_desc* d, bool packed, const void* q, const void* k, const void* v)
 {
-    return d->frames < 0x7FFFFF00 && copies_fit(q, d->q, d->heads, d->batch, d->frames) && copies_fit(k, d->k, d->groups, d->batch, d->frames) &&
-           copies_fit(v, d->v, d->groups, d->batch, d->frames);
+    const int64_t sequences = packed ? 1 : d->batch;
+    return d->frames < 0x7FFFFF00 && copies_fit(q, d->q, d->heads, sequences, d->frames) && copies_fit(k, d->k, d->groups, sequences, d->frames) &&
+           copies_fit(v, d->v, d->groups, sequences, d->frames);
 }
 bool sr_chunks_wanted(const sr_attention_desc* d)
 {
@@ -794,7 +854,7 @@ cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d,
     C.sums = static_cast<float*>(workspace);
     C.decays = C.sums ? C.sums + (size_t)cut.slots * d->groups * d->dk * d->dv : nullptr;
     auto whole = [](int64_t st, int64_t n) { return n <= 1 || st % 8 == 0; };
-    C.out_vec = !((uintptr_t)A.out & 15) && whole(A.so.frame, d->frames) && whole(A.so.sequence, d->batch) && whole(A.so.head, d->heads);
+    C.out_vec = !((uintptr_t)A.out & 15) && whole(A.so.frame, d->frames) && (A.offsets || whole(A.so.sequence, d->batch)) && whole(A.so.head, d->heads);
     const int64_t sequences = A.offsets ? 1 : d->batch;
     if (!encode(&C.q_map, A.q, A.sq, d->dk, d->heads, sequences, d->frames) || !encode(&C.k_map, A.k, A.sk, d->dk, d->groups, sequences, d->frames) ||
         !encode(&C.v_map, A.v, A.sv, d->dv, d->groups, sequences, d->frames))

@@ -276,7 +276,7 @@ sr_status sr_linear_attention_run(const sr_attention_desc* d, const void* q, con
     A.state_out = state_out;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    if (sr_chunks_wanted(d) && sr_chunks_fit(d, q, k, v)) e = sr_chunks_launch(A, d, workspace, s);
+    if (sr_chunks_wanted(d) && sr_chunks_fit(d, offsets != nullptr, q, k, v)) e = sr_chunks_launch(A, d, workspace, s);
     else e = d->dtype == SR_DTYPE_F32 ? launch_frames_any<float>(A, s) : launch_frames_any<__nv_bfloat16>(A, s);
     return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
 }

@@ -38,7 +38,7 @@ __device__ __forceinline__ AttentionSpan attention_span(const AttentionArgs& A, 
 #endif
 
 // sr_chunks.cu: bf16 on the tensor cores, chunks of 128 frames.
-bool sr_chunks_fit(const sr_attention_desc* d, const void* q, const void* k, const void* v);
+bool sr_chunks_fit(const sr_attention_desc* d, bool packed, const void* q, const void* k, const void* v);
 bool sr_chunks_wanted(const sr_attention_desc* d);
 size_t sr_chunks_workspace(const sr_attention_desc* d, bool packed);
 cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d, void* workspace, cudaStream_t s);
