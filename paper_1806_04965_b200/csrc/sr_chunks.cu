@@ -16,7 +16,7 @@
 // one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
 //
 // Bound by memory (q, k, v, out once) where there are CTAs enough: a chunk of DK = 128 is 96 KiB per CTA, 2.6k cycles of MMAs.
-// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; warps 4..7 scores -> P, 8..11 state, 12..15 V', 16..19 outputs.
+// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; sixteen workers for everything between the MMAs.
 // What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
 // the near product (whose zeros would spread it to earlier frames) and added by the outputs' warps; rows behind a sequence's last frame are zeroed.
 #include <cuda.h>
@@ -33,9 +33,9 @@
 namespace {
 using namespace srx;
 
-constexpr int kChunk = 128, kCols = 64, kThreads = 1024, kDecays = 4;
-constexpr uint32_t kScores = 0, kState = 128, kFar = 192, kNear = 320;          // TMEM columns
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kChunk = 128, kCols = 64, kWorkers = 16, kThreads = 128 + 32 * kWorkers, kDecays = 4;
+constexpr uint32_t kScores = 0, kState = 128, kFar = 192, kNear = 320, kWeights = 384;       // TMEM columns
+constexpr float kLn2 = 0.6931471805599453f;
 
 struct ChunkArgs {
     CUtensorMap q_map, k_map, v_map;
@@ -132,28 +132,66 @@ __device__ __forceinline__ float exp2_two(double x)   // 2^x, x as two floats
     const float y = exp2_fast(hi);
     return fmaf(y, lo * kLn2, y);
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+// Two floats in one register pair: one instruction for both.
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair(float lo, float hi)
 {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
 }
-__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ Pair pair(uint32_t lo, uint32_t hi)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi));
+    return p;
+}
+__device__ __forceinline__ float2 split(Pair p)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b)
+{
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t round_bf16(Pair p)
+{
+    const float2 f = split(p);
+    uint32_t w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(f.y), "f"(f.x));
+    return w;
+}
+// The two values of a word of bf16
+__device__ __forceinline__ Pair widen_bf16(uint32_t w) { return pair(w << 16, w & 0xFFFF0000u); }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
-// What a rounding left out.  Where the value is infinite any finite number will do (the rounded part says so already): max makes one of the NaN.
-__device__ __forceinline__ float rest(float x, float rounded) { return fmaxf(x - rounded, -3.0e38f); }
 
 struct alignas(16) Decays {                            // of a chunk (read four at a time); G in units of log 2
     float hi[kChunk], lo[kChunk];                      // G_j in two floats
     float col[kChunk];                                 // exp(G_e - G_j), e the last frame of j's 32
     float rest[kChunk];                                // exp(G_last - G_j)
     float row[kChunk];                                 // exp(G_i)
-    uint32_t odd[8];                                   // columns of the chunk's values that are not all finite: a word of 32 columns for each of eight warps
+    uint32_t odd[kWorkers];                            // columns of the chunk's values that are not all finite: 16 bits of each worker, [columns / 16][rows / 32]
     float whole;                                       // exp(G_last)
 };
 static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read as 16-byte words");
 
-// Values that are not finite have been left out of row i of a chunk's near product: their terms for 32 columns, as the formula has them, on top of the
+// Values that are not finite have been left out of row i of a chunk's near product: their terms for 16 columns, as the formula has them, on top of the
 // stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
 __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, __nv_bfloat16* out)
 {
@@ -165,7 +203,7 @@ __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays&
         float p = 0.0f;
         bool have = false;
 #pragma unroll 1
-        for (int e = 0; e < 32 && c0 + e < A.dv; ++e) {
+        for (int e = 0; e < 16 && c0 + e < A.dv; ++e) {
             const float value = __bfloat162float(v[e]);
             if (finite(value)) continue;
             if (!have) {
@@ -182,7 +220,7 @@ template <int DK, int MODE>
 __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_constant__ ChunkArgs C)
 {
     constexpr bool OUT = MODE != 1;                    // outputs are wanted
-    constexpr int NQ = DK == 64 ? 2 : 1;               // slots for queries
+    constexpr int NK = DK == 64 ? 2 : 1;               // slots for keys
     constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V, of a part of the state
     constexpr int SQ = DK / 32;                        // quarters of the TMEM lanes with rows of the state
     extern __shared__ uint8_t smem_raw[];
@@ -210,37 +248,37 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     const int share = OUT ? A.share : 1;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t k_tiles = base, v_tiles = k_tiles + 2 * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + NQ * KT, s_tiles = w_tiles + 3 * VT;
-    uint8_t* const generic = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t *const k_mem = generic, *const v_mem = k_mem + 2 * KT, *const w_mem = v_mem + 2 * VT + NQ * KT, *const s_mem = w_mem + 3 * VT;
+    const uint32_t k_tiles = base, v_tiles = k_tiles + NK * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + 2 * KT, s_tiles = w_tiles + 3 * VT;
+    uint8_t* const k_mem = smem_raw + (base - smem_u32(smem_raw));
+    uint8_t *const v_mem = k_mem + NK * KT, *const w_mem = v_mem + 2 * VT + 2 * KT, *const s_mem = w_mem + 3 * VT;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
-    const uint32_t kv_full = bar(0), kv_empty = bar(2), q_full = bar(4), q_empty = bar(6), d_full = bar(8), d_empty = bar(12);
-    const uint32_t scored = bar(16), weighed = bar(17), far_full = bar(18), far_free = bar(19), near_full = bar(20), near_free = bar(21);
-    const uint32_t parted = bar(22), decayed = bar(23), stated = bar(24), state_free = bar(25), summed = bar(26), cleaned = bar(27);
+    const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
+    const uint32_t scored = bar(20), weighed = bar(21), far_full = bar(22), near_full = bar(23), taken = bar(24);
+    const uint32_t parted = bar(25), stated = bar(26), state_free = bar(27), summed = bar(28), cleaned = bar(29);
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int i = 0; i < 2; ++i) {
-            mbar_init(kv_full + 8 * i, 1);
-            mbar_init(kv_empty + 8 * i, 1);
+            mbar_init(k_full + 8 * i, 1);
+            mbar_init(k_empty + 8 * i, 1);
+            mbar_init(v_full + 8 * i, 1);
+            mbar_init(v_empty + 8 * i, 1);
             mbar_init(q_full + 8 * i, 1);
             mbar_init(q_empty + 8 * i, 1);
         }
         for (int i = 0; i < kDecays; ++i) {
             mbar_init(d_full + 8 * i, 1);
-            mbar_init(d_empty + 8 * i, 8 + 2 * SQ + (OUT ? 12 : 0));
+            mbar_init(d_empty + 8 * i, kWorkers);
         }
         mbar_init(scored, 1);                          // scores are in TMEM
-        mbar_init(weighed, 4);                         // P is in TMEM
+        mbar_init(weighed, kWorkers);                  // P is in TMEM
         mbar_init(far_full, 1);                        // the far part of the outputs is in TMEM
-        mbar_init(far_free, 8);                        // ... and has been read
         mbar_init(near_full, 1);                       // the near part
-        mbar_init(near_free, 8);
-        mbar_init(parted, 8);                          // V' is in shared memory, V is fit for the near product
-        mbar_init(decayed, 2 * SQ);                    // the state in TMEM has decayed
-        mbar_init(stated, 2 * SQ);                     // the state's parts are in shared memory
+        mbar_init(taken, kWorkers);                    // both have been read
+        mbar_init(parted, kWorkers);                   // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
+        mbar_init(stated, kWorkers);                   // the state's parts are in shared memory
         mbar_init(state_free, 1);                      // ... and have been read
         mbar_init(summed, 1);                          // the chunk's sums are on top of the state, V' has been read
-        mbar_init(cleaned, 8);                         // rows behind the last frame are zeroed
+        mbar_init(cleaned, kWorkers);                  // rows behind the last frame are zeroed
         mbar_init_done();
     }
     if (warp == 3) tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -258,90 +296,104 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     if (warp == 0) {
         if (elect_one()) {
             bool ok = true;
-            uint32_t n = 0;
-            auto load_kv = [&](int c) {
-                const uint32_t s = c & 1, b = kv_full + 8 * s;
-                ok = ok && mbar_wait(kv_empty + 8 * s, ((c >> 1) & 1) ^ 1, gave_up);
+            uint32_t n = 0;                            // steps: chunks x heads
+            auto frame = [&](int c) { return (int)(f0 + (int64_t)c * kChunk); };
+            auto load_q = [&](int c, int h) {
+                const uint32_t s = n & 1, b = q_full + 8 * s;
+                ok = ok && mbar_wait(q_empty + 8 * s, ((n >> 1) & 1) ^ 1, gave_up);
                 if (!ok) return;
-                mbar_expect_tx(b, KT + VT);
-                const int f = (int)(f0 + (int64_t)c * kChunk);
+                mbar_expect_tx(b, KT);
 #pragma unroll
-                for (int h = 0; h < DK / 64; ++h) tma_load_4d(k_tiles + s * KT + h * 16384, &C.k_map, b, h * 64, it.g, (int)it.span.b, f);
-                tma_load_4d(v_tiles + s * VT, &C.v_map, b, it.c0, it.g, (int)it.span.b, f);
+                for (int p = 0; p < DK / 64; ++p) tma_load_4d(q_tiles + s * KT + p * 16384, &C.q_map, b, p * 64, it.g * A.share + h, (int)it.span.b, frame(c));
+                ++n;
             };
-            load_kv(0);
             for (int c = 0; c < chunks && ok; ++c) {
-                if (OUT) {
-                    for (int h = 0; h < share && ok; ++h, ++n) {
-                        const uint32_t s = n % NQ, b = q_full + 8 * s;
-                        ok = mbar_wait(q_empty + 8 * s, ((n / NQ) & 1) ^ 1, gave_up);
-                        if (!ok) break;
-                        mbar_expect_tx(b, KT);
-                        const int f = (int)(f0 + (int64_t)c * kChunk);
+                const uint32_t ks = c % NK, vs = c & 1;
+                ok = mbar_wait(v_empty + 8 * vs, ((c >> 1) & 1) ^ 1, gave_up);
+                if (!ok) break;
+                mbar_expect_tx(v_full + 8 * vs, VT);
+                tma_load_4d(v_tiles + vs * VT, &C.v_map, v_full + 8 * vs, it.c0, it.g, (int)it.span.b, frame(c));
+                if (OUT) load_q(c, 0);
+                ok = ok && mbar_wait(k_empty + 8 * ks, ((c / NK) & 1) ^ 1, gave_up);
+                if (!ok) break;
+                mbar_expect_tx(k_full + 8 * ks, KT);
 #pragma unroll
-                        for (int p = 0; p < DK / 64; ++p) tma_load_4d(q_tiles + s * KT + p * 16384, &C.q_map, b, p * 64, it.g * A.share + h, (int)it.span.b, f);
-                        if (h == 0 && c + 1 < chunks) load_kv(c + 1);
-                    }
-                } else if (c + 1 < chunks) {
-                    load_kv(c + 1);
+                for (int p = 0; p < DK / 64; ++p) {
+                    tma_load_4d(k_tiles + ks * KT + p * 16384, &C.k_map, k_full + 8 * ks, p * 64, it.g, (int)it.span.b, frame(c));
+                    if (c + 1 < chunks) tma_prefetch_4d(&C.k_map, p * 64, it.g, (int)it.span.b, frame(c + 1));
                 }
+                for (int h = 1; h < share && OUT; ++h) load_q(c, h);
             }
-            if (!ok) {                                 // what was asked for still has to land
-                for (int s = 0; s < 2; ++s) mbar_drain(kv_full + 8 * s, 0), mbar_drain(kv_full + 8 * s, 1);
-                for (int s = 0; s < NQ; ++s) mbar_drain(q_full + 8 * s, 0), mbar_drain(q_full + 8 * s, 1);
-            }
+            if (!ok)                                   // what was asked for still has to land
+                for (int s = 0; s < 2; ++s)
+                    for (int p = 0; p < 2; ++p) {
+                        mbar_drain(k_full + 8 * s, p);
+                        mbar_drain(v_full + 8 * s, p);
+                        mbar_drain(q_full + 8 * s, p);
+                    }
         }
     } else if (warp == 1) {
         if (elect_one()) {
             constexpr uint32_t i_scores = idesc_bf16(128, 0, 0), i_far = idesc_bf16(128, 0, 1), i_near = idesc_bf16(64, 0, 1), i_state = idesc_bf16(64, 1, 1);
             bool ok = true;
-            uint32_t n = 0;                            // steps: chunks x heads
-            for (int c = 0; c < chunks && ok; ++c) {
-                const uint32_t s = c & 1, cp = (c >> 1) & 1;
-                const uint32_t k_at = k_tiles + s * KT, v_at = v_tiles + s * VT;
-                const int steps = ((c + 1 == chunks ? tail : kChunk) + 15) / 16;        // of 16 frames
-                ok = mbar_wait(kv_full + 8 * s, cp, gave_up);
-                if (clean && c + 1 == chunks) ok = ok && mbar_wait(cleaned, 0, gave_up);
-                for (int h = 0; h < share && ok; ++h, ++n) {
-                    const uint32_t qs = n % NQ, q_at = q_tiles + qs * KT;
-                    if (OUT) {
-                        ok = mbar_wait(q_full + 8 * qs, (n / NQ) & 1, gave_up);
-                        if (!ok) break;
-                        tc_fence_after();
+            uint32_t n = 0;
+            // Scores of step m, the first of chunk c's if h is 0.
+            auto scores = [&](uint32_t m, int c, int h) {
+                const uint32_t ks = c % NK, q_at = q_tiles + (m & 1) * KT, k_at = k_tiles + ks * KT;
+                if (h == 0) {
+                    ok = ok && mbar_wait(k_full + 8 * ks, (c / NK) & 1, gave_up);
+                    if (clean && c + 1 == chunks) ok = ok && mbar_wait(cleaned, 0, gave_up);
+                }
+                if (OUT) {
+                    ok = ok && mbar_wait(q_full + 8 * (m & 1), (m >> 1) & 1, gave_up);
+                    if (!ok) return;
+                    tc_fence_after();
 #pragma unroll
-                        for (int k = 0; k < DK / 16; ++k)
-                            mma_bf16(tmem + kScores, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_k_major(k_at + (k / 4) * 16384) + 2 * (k % 4), i_scores, k > 0);
-                        tc_commit(scored);
-                    }
-                    if (h == 0) {
-                        // ahead of everything that reads the state's parts: the next chunk's state waits for this
-                        ok = mbar_wait(decayed, c & 1, gave_up) && mbar_wait(parted, c & 1, gave_up);
-                        if (!ok) break;
-                        tc_fence_after();
-                        for (int p = 0; p < 3; ++p)
-                            for (int k = 0; k < steps; ++k)
-                                mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + p * VT + k * 2048, 0), i_state, 1);
-                        tc_commit(summed);
-                    }
+                    for (int k = 0; k < DK / 16; ++k)
+                        mma_bf16(tmem + kScores, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_k_major(k_at + (k / 4) * 16384) + 2 * (k % 4), i_scores, k > 0);
+                    tc_commit(scored);
+                }
+            };
+            scores(0, 0, 0);
+            for (int c = 0; c < chunks && ok; ++c) {
+                const uint32_t ks = c % NK, k_at = k_tiles + ks * KT, v_at = v_tiles + (c & 1) * VT;
+                const int steps = ((c + 1 == chunks ? tail : kChunk) + 15) / 16;        // of 16 frames
+                // the state first: the next chunk waits for it
+                ok = mbar_wait(parted, c & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                for (int p = 0; p < 3; ++p)
+                    for (int k = 0; k < steps; ++k)
+                        mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + p * VT + k * 2048, 0), i_state, 1);
+                tc_commit(summed);
+                if (share == 1) tc_commit(k_empty + 8 * ks);
+                for (int h = 0; h < share && ok; ++h, ++n) {
                     if (OUT) {
+                        const uint32_t q_at = q_tiles + (n & 1) * KT;
                         if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
-                        ok = ok && mbar_wait(far_free, (n & 1) ^ 1, gave_up);
+                        ok = ok && mbar_wait(taken, (n & 1) ^ 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
                         for (int k = 0; k < DK / 16; ++k)
                             mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, ST), i_far, k > 0);
-                        tc_commit(q_empty + 8 * qs);
+                        tc_commit(q_empty + 8 * (n & 1));
                         tc_commit(far_full);
                         if (h + 1 == share) tc_commit(state_free);
-                        ok = mbar_wait(weighed, n & 1, gave_up) && mbar_wait(near_free, (n & 1) ^ 1, gave_up);
+                        ok = mbar_wait(weighed, n & 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
-                        for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kScores + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
+                        for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kWeights + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
                         tc_commit(near_full);
                     }
+                    if (h + 1 == share) tc_commit(v_empty + 8 * (c & 1));
+                    if (h + 1 < share) {
+                        scores(n + 1, c, h + 1);
+                        if (h + 2 == share) tc_commit(k_empty + 8 * ks);
+                    } else if (c + 1 < chunks) {
+                        scores(n + 1, c + 1, 0);
+                    }
                 }
-                if (ok) tc_commit(kv_empty + 8 * s);
             }
         }
     } else if (warp == 2) {
@@ -411,290 +463,253 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             if (lane == 0) mbar_arrive(d_full + 8 * slot);
         }
         if (MODE == 1 && lane == 0 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
-    } else if (warp >= 4 && warp < 8) {
-        // scores -> P: a thread has a frame's row
-        if (OUT) {
-            const int w = warp - 4, i = w * 32 + lane;
-            const uint32_t at = tmem + kScores + ((uint32_t)(w * 32) << 16);
-            uint32_t n = 0;
-            bool ok = true;
-            for (int c = 0; c < chunks && ok; ++c) {
-                const int slot = c % kDecays;
-                const Decays& D = decays[slot];
-                const int frames = c + 1 == chunks ? tail : kChunk, blocks = 2 * ((frames + 31) / 32);      // of 16 columns
-                ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
-                if (!ok) break;
-                const float hi = D.hi[i], lo = D.lo[i];
-                float rows[3];
+    } else if (warp >= 4) {
+        // A worker has 32 rows (those of its quarter w of the TMEM lanes) and a quarter u of the columns of everything: frames' rows of V and V', of the scores and of
+        // the outputs, rows of the state.  All of them do the same at the same time (roles of their own, at eight times the code, waited for instructions), in an
+        // order that leaves the tensor pipe no pause: while it sums a chunk's state they do the outputs of the step before, the weights of this one and the
+        // parts of the next chunk's values.
+        const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        const int j0 = it.c0 + u * 16;
+        const bool holds = w < SQ;                     // rows of the state
+        uint32_t n = 0;
+        // Outputs of the step before.
+        auto output = [&](int c, int h) {
+            const Decays& D = decays[c % kDecays];
+            const int frames = c + 1 == chunks ? tail : kChunk;
+            const int64_t f = f0 + (int64_t)c * kChunk + i;
+            const uint32_t m = n - 1;
+            if (!mbar_wait_warp(far_full, m & 1, gave_up) || !mbar_wait_warp(near_full, m & 1, gave_up)) return false;
+            tc_fence_after();
+            uint32_t a[16], b[16], x[16];
+            tc_ld(tmem + kFar + lanes + u * 16, a);
+            tc_ld(tmem + kFar + kCols + lanes + u * 16, b);
+            tc_ld(tmem + kNear + lanes + u * 16, x);
+            tc_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(taken);
+            const uint4 odd = *reinterpret_cast<const uint4*>(&D.odd[u * 4]);
+            if (i < frames) {
+                const float r = D.row[i] * A.scale;
+                const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
+                Pair y[8];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) rows[m] = m < w ? exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31])) : 0.0f;
-                for (int h = 0; h < share; ++h, ++n) {
-                    ok = mbar_wait_warp(scored, n & 1, gave_up);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const int last = min(blocks, 2 * w + 2);             // blocks that reach to the diagonal
-                    uint32_t x[16];
-                    tc_ld(at, x);
-#pragma unroll 1
-                    for (int m = 0; m < last; ++m) {
-                        const int c0 = m * 16;
-                        float y[16];
-                        tc_wait_ld();
+                for (int e = 0; e < 8; ++e)
+                    y[e] = fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, add2(pair(a[2 * e], a[2 * e + 1]), pair(b[2 * e], b[2 * e + 1]))));
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + f * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + j0;
+                const int left = A.dv - j0;
+                if (left >= 16 && C.out_vec) {
+                    *reinterpret_cast<uint4*>(out) = make_uint4(round_bf16(y[0]), round_bf16(y[1]), round_bf16(y[2]), round_bf16(y[3]));
+                    *reinterpret_cast<uint4*>(out + 8) = make_uint4(round_bf16(y[4]), round_bf16(y[5]), round_bf16(y[6]), round_bf16(y[7]));
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(x[e]);
-                        if (m + 1 < last) tc_ld(at + c0 + 16, x);
-                        uint32_t p[8];
-                        if (m < 2 * w) {
-                            const float row = m < 2 ? rows[0] : m < 4 ? rows[1] : rows[2];
-#pragma unroll
-                            for (int e = 0; e < 16; e += 4) {
-                                const float4 col = *reinterpret_cast<const float4*>(&D.col[c0 + e]);
-                                p[e / 2] = pack_bf16(y[e] * (row * col.x), y[e + 1] * (row * col.y));
-                                p[e / 2 + 1] = pack_bf16(y[e + 2] * (row * col.z), y[e + 3] * (row * col.w));
-                            }
-                        } else {
-                            const int d = i - c0;
-#pragma unroll
-                            for (int e = 0; e < 16; e += 4) {
-                                const float4 ch = *reinterpret_cast<const float4*>(&D.hi[c0 + e]), cl = *reinterpret_cast<const float4*>(&D.lo[c0 + e]);
-                                const float z0 = y[e] * exp2_fast((hi - ch.x) + (lo - cl.x)), z1 = y[e + 1] * exp2_fast((hi - ch.y) + (lo - cl.y));
-                                const float z2 = y[e + 2] * exp2_fast((hi - ch.z) + (lo - cl.z)), z3 = y[e + 3] * exp2_fast((hi - ch.w) + (lo - cl.w));
-                                p[e / 2] = pack_bf16(e <= d ? z0 : 0.0f, e + 1 <= d ? z1 : 0.0f);
-                                p[e / 2 + 1] = pack_bf16(e + 2 <= d ? z2 : 0.0f, e + 3 <= d ? z3 : 0.0f);
-                            }
-                        }
-                        tc_st(at + m * 8, p);          // (over scores that this thread has read)
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 z = split(y[e]);
+                        if (2 * e < left) out[2 * e] = __float2bfloat16(z.x);
+                        if (2 * e + 1 < left) out[2 * e + 1] = __float2bfloat16(z.y);
                     }
-                    const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    for (int m = last; m < blocks; ++m) tc_st(at + m * 8, none);
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(weighed);
                 }
-                if (lane == 0) mbar_arrive(d_empty + 8 * slot);
+                if (odd.x | odd.y | odd.z | odd.w) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, out);
             }
-        }
-    } else if (warp >= 8 && warp < 16) {
-        // the state: a thread has 32 columns of a row of it
-        const int w = warp & 3, half = (warp - 8) >> 2, r = w * 32 + lane, j0 = it.c0 + half * 32;
-        if (w < SQ) {
-            const uint32_t at = tmem + kState + ((uint32_t)(w * 32) << 16) + half * 32;
-            const float* from = MODE == 2 ? C.sums + (slot_at + r) * A.dv : A.state_in ? A.state_in + (state_at + r) * A.dv : nullptr;
-            float* to = MODE == 1 ? C.sums + (slot_at + r) * A.dv : it.last && A.state_out ? A.state_out + (state_at + r) * A.dv : nullptr;
-            bool ok = true;
-            for (int c = 0; c <= chunks; ++c) {
-                float whole = 0.0f;
-                if (c < chunks) {
-                    const int slot = c % kDecays;
-                    ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
+            __syncwarp();
+            return true;
+        };
+        bool ok = true;
+        for (int c = 0; c <= chunks && ok; ++c) {
+            const int slot = c % kDecays, frames = c + 1 == chunks ? tail : kChunk;
+            Decays& D = decays[slot];
+            uint32_t a[8], b[8], d[8];                 // parts of V'
+            if (c < chunks) {
+                uint8_t* row = v_mem + (c & 1) * VT + i * 128;
+                ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+                if (!ok) break;
+                if (clean && c + 1 == chunks) {
+                    ok = mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
                     if (!ok) break;
-                    whole = decays[slot].whole;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(d_empty + 8 * slot);
-                }
-                if (c > 0) {
-                    ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
-                    if (!ok) break;
-                    tc_fence_after();
-                }
-                uint32_t hi[16], lo[16];
-#pragma unroll
-                for (int m = 0; m < 32; m += 16) {
-                    uint32_t x[16];
-                    const int j = j0 + m;
-                    if (c > 0) {
-                        tc_ld(at + m, x);
-                        tc_wait_ld();
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = MODE != 1 && from && r < A.dk && j + e < A.dv ? __float_as_uint(from[j + e]) : 0u;
-                    }
-                    if (c == chunks) {
-                        if (to && r < A.dk) {
-                            if (j + 16 <= A.dv && !((uintptr_t)(to + j) & 15)) {
-#pragma unroll
-                                for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 16; ++e)
-                                    if (j + e < A.dv) to[j + e] = __uint_as_float(x[e]);
-                            }
+                    if (i >= frames) {
+                        for (int x = 2 * u; x < 2 * u + 2; ++x) {
+                            const uint32_t place = ((uint32_t)x ^ (i & 7)) << 4;
+                            *reinterpret_cast<uint4*>(row + place) = make_uint4(0, 0, 0, 0);
+                            for (int p = 0; p < DK / 64; ++p) *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + i * 128 + place) = make_uint4(0, 0, 0, 0);
                         }
-                        __syncwarp();
-                        continue;
-                    }
-                    if (OUT)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float a = __uint_as_float(x[2 * e]), b = __uint_as_float(x[2 * e + 1]);
-                            hi[m / 2 + e] = pack_bf16(a, b);
-                            lo[m / 2 + e] = pack_bf16(rest(a, low_bf16(hi[m / 2 + e])), rest(b, high_bf16(hi[m / 2 + e])));
-                        }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * whole);
-                    tc_st(at + m, x);
-                }
-                if (c == chunks) break;
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(decayed);
-                if (OUT) {
-                    if (c > 0) {
-                        ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
-                        if (!ok) break;
-                    }
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const uint32_t place = (uint32_t)r * 128u + (((uint32_t)(half * 4 + m) ^ (r & 7)) << 4);
-                        *reinterpret_cast<uint4*>(s_mem + place) = make_uint4(hi[4 * m], hi[4 * m + 1], hi[4 * m + 2], hi[4 * m + 3]);
-                        *reinterpret_cast<uint4*>(s_mem + ST + place) = make_uint4(lo[4 * m], lo[4 * m + 1], lo[4 * m + 2], lo[4 * m + 3]);
                     }
                     fence_async_shared();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(stated);
+                    if (lane == 0) mbar_arrive(cleaned);
                 }
-            }
-        }
-    } else if (warp >= 16 && warp < 24) {
-        // V': a thread has 32 values of a frame's row
-        const int w = warp & 3, half = (warp - 16) >> 2, j = w * 32 + lane;
-        bool ok = true;
-        for (int c = 0; c < chunks && ok; ++c) {
-            const uint32_t s = c & 1;
-            const int slot = c % kDecays;
-            const int frames = c + 1 == chunks ? tail : kChunk;
-            ok = mbar_wait_warp(kv_full + 8 * s, (c >> 1) & 1, gave_up);
-            if (!ok) break;
-            uint8_t* row = v_mem + s * VT + j * 128;
-            if (clean && c + 1 == chunks) {
-                if (j >= frames) {
-                    for (int x = 0; x < 4; ++x) *reinterpret_cast<uint4*>(row + (half * 4 + x) * 16) = make_uint4(0, 0, 0, 0);
-                    for (int x = 0; x < 8; ++x)
-                        if (half < DK / 64) *reinterpret_cast<uint4*>(k_mem + s * KT + half * 16384 + j * 128 + x * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(cleaned);
-            }
-            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
-            if (!ok) break;
-            const float weight = decays[slot].rest[j];
-            __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);      // NaN as soon as a value is not finite
-            uint32_t a[16], b[16], d[16];
+                ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
+                if (!ok) break;
+                const Pair weight = pair(D.rest[i], D.rest[i]), minus = pair(-1.0f, -1.0f);
+                __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);  // NaN as soon as a value is not finite
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint4 v = *reinterpret_cast<const uint4*>(row + (((uint32_t)(half * 4 + x) ^ (j & 7)) << 4));
-                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                for (int x = 0; x < 2; ++x) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(row + (((uint32_t)(2 * u + x) ^ (i & 7)) << 4));
+                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
-                    float y0 = low_bf16(in[e]) * weight, y1 = high_bf16(in[e]) * weight;
-                    const uint32_t hi = pack_bf16(y0, y1);
-                    y0 = rest(y0, low_bf16(hi));
-                    y1 = rest(y1, high_bf16(hi));
-                    const uint32_t mid = pack_bf16(y0, y1);
-                    a[4 * x + e] = hi;
-                    b[4 * x + e] = mid;
-                    d[4 * x + e] = pack_bf16(y0 - low_bf16(mid), y1 - high_bf16(mid));
-                }
-            }
-            if (OUT) {
-                uint32_t cols = 0;
-                if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
-#pragma unroll 1
-                    for (int e = 0; e < 32; ++e) {
-                        uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(half * 4 + e / 8) ^ (j & 7)) << 4)) + (e & 7);
-                        const bool is = (*p & 0x7F80u) == 0x7F80u;
-                        if (is) *p = 0;
-                        if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
+                    for (int e = 0; e < 4; ++e) {
+                        if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
+                        Pair y = mul2(widen_bf16(in[e]), weight);
+                        a[4 * x + e] = round_bf16(y);
+                        y = fma2(widen_bf16(a[4 * x + e]), minus, y);
+                        b[4 * x + e] = round_bf16(y);
+                        d[4 * x + e] = round_bf16(fma2(widen_bf16(b[4 * x + e]), minus, y));
                     }
                 }
-                if (lane == 0) decays[slot].odd[half * 4 + w] = cols;
+                if (OUT) {
+                    uint32_t cols = 0;
+                    if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
+#pragma unroll 1
+                        for (int e = 0; e < 16; ++e) {
+                            uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(2 * u + e / 8) ^ (i & 7)) << 4)) + (e & 7);
+                            const bool is = (*p & 0x7F80u) == 0x7F80u;
+                            if (is) *p = 0;
+                            if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {                    // the first part says what has to be said
+                            const uint32_t keep = ((a[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((a[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                            b[e] &= keep;
+                            d[e] &= keep;
+                        }
+                    }
+                    if (lane == 0) D.odd[u * 4 + w] = cols;
+                }
             }
             if (c > 0) {
-                ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);       // the parts of the chunk before have been read
+                ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            // the state that enters chunk c, or the last one
+            uint32_t x[16];
+            if (holds) {
+                if (c > 0) {
+                    tc_ld(tmem + kState + lanes + u * 16, x);
+                    tc_wait_ld();
+                } else {
+                    const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = from && i < A.dk && j0 + e < A.dv ? __float_as_uint(from[j0 + e]) : 0u;
+                }
+            }
+            if (c == chunks) {
+                float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
+                if (holds && to && i < A.dk) {
+                    if (j0 + 16 <= A.dv && !((uintptr_t)(to + j0) & 15)) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j0 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (j0 + e < A.dv) to[j0 + e] = __uint_as_float(x[e]);
+                    }
+                }
+                __syncwarp();
+                if (OUT) output(c - 1, share - 1);
+                break;
+            }
+            {
+                uint8_t* to = w_mem + i * 128;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t place = ((uint32_t)(2 * u + q) ^ (i & 7)) << 4;
+                    *reinterpret_cast<uint4*>(to + place) = make_uint4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
+                    *reinterpret_cast<uint4*>(to + VT + place) = make_uint4(b[4 * q], b[4 * q + 1], b[4 * q + 2], b[4 * q + 3]);
+                    *reinterpret_cast<uint4*>(to + 2 * VT + place) = make_uint4(d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]);
+                }
+            }
+            if (holds) {
+                const Pair whole = pair(D.whole, D.whole);
+                uint32_t y[16];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 z = split(mul2(pair(x[2 * e], x[2 * e + 1]), whole));
+                    y[2 * e] = __float_as_uint(z.x);
+                    y[2 * e + 1] = __float_as_uint(z.y);
+                }
+                tc_st(tmem + kState + lanes + u * 16, y);
+                tc_wait_st();
+            }
+            fence_async_shared();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(parted);
+            if (!OUT) {
+                if (lane == 0) mbar_arrive(d_empty + 8 * slot);
+                continue;
+            }
+            if (c > 0) {
+                ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
                 if (!ok) break;
             }
+            if (holds) {
+                uint32_t hi[8], lo[8];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                uint8_t* out = w_mem + j * 128 + (((uint32_t)(half * 4 + x) ^ (j & 7)) << 4);
-                *reinterpret_cast<uint4*>(out) = make_uint4(a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3]);
-                *reinterpret_cast<uint4*>(out + VT) = make_uint4(b[4 * x], b[4 * x + 1], b[4 * x + 2], b[4 * x + 3]);
-                *reinterpret_cast<uint4*>(out + 2 * VT) = make_uint4(d[4 * x], d[4 * x + 1], d[4 * x + 2], d[4 * x + 3]);
+                for (int e = 0; e < 8; ++e) {
+                    const Pair y = pair(x[2 * e], x[2 * e + 1]);
+                    hi[e] = round_bf16(y);
+                    const float2 left = split(fma2(widen_bf16(hi[e]), pair(-1.0f, -1.0f), y));
+                    // (an infinite value: max makes the NaN that is left over finite, the first part says what has to be said)
+                    lo[e] = round_bf16(pair(fmaxf(left.x, -3.0e38f), fmaxf(left.y, -3.0e38f)));
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t place = (uint32_t)i * 128u + (((uint32_t)(2 * u + q) ^ (i & 7)) << 4);
+                    *reinterpret_cast<uint4*>(s_mem + place) = make_uint4(hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]);
+                    *reinterpret_cast<uint4*>(s_mem + ST + place) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
+                }
             }
             fence_async_shared();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(parted);
-                mbar_arrive(d_empty + 8 * slot);
-            }
-        }
-    } else if (OUT && warp >= 24) {
-        // outputs: a thread has 32 columns of a frame's row
-        const int w = warp & 3, half = (warp - 24) >> 2, i = w * 32 + lane, j0 = it.c0 + half * 32;
-        const uint32_t lanes = ((uint32_t)(w * 32) << 16) + half * 32;
-        uint32_t n = 0;
-        bool ok = true;
-        for (int c = 0; c < chunks && ok; ++c) {
-            const int slot = c % kDecays;
-            const Decays& D = decays[slot];
-            const int frames = c + 1 == chunks ? tail : kChunk;
-            const int64_t f = f0 + (int64_t)c * kChunk + i;
-            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
-            if (!ok) break;
-            const float row = D.row[i];
-            for (int h = 0; h < share; ++h, ++n) {
-                ok = mbar_wait_warp(far_full, n & 1, gave_up);
+            if (lane == 0) mbar_arrive(stated);
+            for (int h = 0; h < share; ++h) {
+                if (n > 0) {
+                    ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1);
+                    if (!ok) break;
+                    if (h == 0 && lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
+                }
+                ok = mbar_wait_warp(scored, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                float y[32];
+                if (u * 32 < frames) {                 // scores -> P, 32 columns from u * 32 on
+                    uint32_t p[16];
+                    if (u > w) {
 #pragma unroll
-                for (int m = 0; m < 32; m += 8) {
-                    uint32_t a[8], b[8];
-                    tc_ld(tmem + kFar + lanes + m, a);
-                    tc_ld(tmem + kFar + kCols + lanes + m, b);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[m + e] = row * (__uint_as_float(a[e]) + __uint_as_float(b[e]));
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(far_free);
-                ok = mbar_wait_warp(near_full, n & 1, gave_up);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int m = 0; m < 32; m += 16) {
-                    uint32_t x[16];
-                    tc_ld(tmem + kNear + lanes + m, x);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) y[m + e] += __uint_as_float(x[e]);
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(near_free);
-                const uint4 odd = *reinterpret_cast<const uint4*>(&D.odd[half * 4]);
-                if (i < frames) {
-                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + f * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + j0;
-                    const int left = A.dv - j0;
-                    if (left >= 32 && C.out_vec) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4*>(out + e) = make_uint4(pack_bf16(A.scale * y[e], A.scale * y[e + 1]), pack_bf16(A.scale * y[e + 2], A.scale * y[e + 3]),
-                                                                            pack_bf16(A.scale * y[e + 4], A.scale * y[e + 5]), pack_bf16(A.scale * y[e + 6], A.scale * y[e + 7]));
+                        for (int e = 0; e < 16; ++e) p[e] = 0;
                     } else {
+                        uint32_t s[32];
+                        tc_ld(tmem + kScores + lanes + u * 32, s);
+                        tc_wait_ld();
+                        const float hi = D.hi[i], lo = D.lo[i];
+                        if (u < w) {
+                            const float r = exp2_fast((hi - D.hi[u * 32 + 31]) + (lo - D.lo[u * 32 + 31]));
+                            const Pair row = pair(r, r);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (e < left) out[e] = __float2bfloat16(A.scale * y[e]);
+                            for (int e = 0; e < 16; e += 2) {
+                                const ulonglong2 col = *reinterpret_cast<const ulonglong2*>(&D.col[u * 32 + 2 * e]);
+                                p[e] = round_bf16(mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, col.x)));
+                                p[e + 1] = round_bf16(mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, col.y)));
+                            }
+                        } else {
+                            const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo), minus = pair(-1.0f, -1.0f);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const Pair ch = *reinterpret_cast<const Pair*>(&D.hi[u * 32 + 2 * e]), cl = *reinterpret_cast<const Pair*>(&D.lo[u * 32 + 2 * e]);
+                                const float2 g = split(add2(fma2(ch, minus, hi2), fma2(cl, minus, lo2)));
+                                const float2 z = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g.x), exp2_fast(g.y))));
+                                p[e] = round_bf16(pair(2 * e <= lane ? z.x : 0.0f, 2 * e + 1 <= lane ? z.y : 0.0f));
+                            }
+                        }
                     }
-                    if (odd.x | odd.y | odd.z | odd.w) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, out);
+                    tc_st(tmem + kWeights + lanes + u * 16, p);
+                    tc_wait_st();
                 }
+                tc_fence_before();
                 __syncwarp();
+                if (lane == 0) mbar_arrive(weighed);
+                ++n;
             }
-            if (lane == 0) mbar_arrive(d_empty + 8 * slot);
         }
     }
     tc_fence_before();
@@ -761,8 +776,8 @@ bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, in
 template <int DK, int MODE>
 cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 {
-    constexpr int NQ = DK == 64 ? 2 : 1;
-    constexpr int smem = 1024 + 2 * DK * 256 + 2 * kCols * 256 + NQ * DK * 256 + 3 * kCols * 256 + 2 * DK * 128;
+    constexpr int NK = DK == 64 ? 2 : 1;
+    constexpr int smem = 1024 + NK * DK * 256 + 2 * kCols * 256 + 2 * DK * 256 + 3 * kCols * 256 + 2 * DK * 128;
     const cudaError_t e = cudaFuncSetAttribute(sr_chunks_kernel<DK, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
