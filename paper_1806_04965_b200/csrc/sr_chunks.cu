@@ -16,7 +16,7 @@
 // one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
 //
 // Bound by memory (q, k, v, out once) where there are CTAs enough: a chunk of DK = 128 is 96 KiB per CTA, 2.6k cycles of MMAs.
-// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; sixteen workers for everything between the MMAs.
+// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; 4..11 state and V', 12..19 scores -> P and outputs.
 // What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
 // the near product (whose zeros would spread it to earlier frames) and added by the outputs' warps; rows behind a sequence's last frame are zeroed.
 #include <cuda.h>
@@ -33,7 +33,8 @@
 namespace {
 using namespace srx;
 
-constexpr int kChunk = 128, kCols = 64, kWorkers = 16, kThreads = 128 + 32 * kWorkers, kDecays = 4;
+constexpr int kChunk = 128, kCols = 64, kDecays = 4;
+constexpr int kStateWarps = 8, kOutWarps = 8, kThreads = 128 + 32 * (kStateWarps + kOutWarps);
 constexpr uint32_t kScores = 0, kState = 128, kFar = 192, kNear = 320, kWeights = 384;       // TMEM columns
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -186,12 +187,12 @@ struct alignas(16) Decays {                            // of a chunk (read four 
     float col[kChunk];                                 // exp(G_e - G_j), e the last frame of j's 32
     float rest[kChunk];                                // exp(G_last - G_j)
     float row[kChunk];                                 // exp(G_i)
-    uint32_t odd[kWorkers];                            // columns of the chunk's values that are not all finite: 16 bits of each worker, [columns / 16][rows / 32]
+    uint32_t odd[8];                                   // columns of the chunk's values that are not all finite: a word for [columns / 32][rows / 32]
     float whole;                                       // exp(G_last)
 };
 static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read as 16-byte words");
 
-// Values that are not finite have been left out of row i of a chunk's near product: their terms for 16 columns, as the formula has them, on top of the
+// Values that are not finite have been left out of row i of a chunk's near product: their terms for 32 columns, as the formula has them, on top of the
 // stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
 __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, __nv_bfloat16* out)
 {
@@ -203,7 +204,7 @@ __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays&
         float p = 0.0f;
         bool have = false;
 #pragma unroll 1
-        for (int e = 0; e < 16 && c0 + e < A.dv; ++e) {
+        for (int e = 0; e < 32 && c0 + e < A.dv; ++e) {
             const float value = __bfloat162float(v[e]);
             if (finite(value)) continue;
             if (!have) {
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
     const uint32_t scored = bar(20), weighed = bar(21), far_full = bar(22), near_full = bar(23), taken = bar(24);
-    const uint32_t parted = bar(25), stated = bar(26), state_free = bar(27), summed = bar(28), cleaned = bar(29);
+    const uint32_t parted = bar(25), stated = bar(26), state_free = bar(27), cleaned = bar(28), part_free = bar(29), summed = bar(31);
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int i = 0; i < 2; ++i) {
@@ -267,18 +268,20 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         }
         for (int i = 0; i < kDecays; ++i) {
             mbar_init(d_full + 8 * i, 1);
-            mbar_init(d_empty + 8 * i, kWorkers);
+            mbar_init(d_empty + 8 * i, kStateWarps + (OUT ? kOutWarps : 0));
         }
         mbar_init(scored, 1);                          // scores are in TMEM
-        mbar_init(weighed, kWorkers);                  // P is in TMEM
+        mbar_init(weighed, kOutWarps);                 // P is in TMEM
         mbar_init(far_full, 1);                        // the far part of the outputs is in TMEM
         mbar_init(near_full, 1);                       // the near part
-        mbar_init(taken, kWorkers);                    // both have been read
-        mbar_init(parted, kWorkers);                   // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
-        mbar_init(stated, kWorkers);                   // the state's parts are in shared memory
+        mbar_init(taken, kOutWarps);                   // both have been read
+        mbar_init(parted, kStateWarps);                // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
+        mbar_init(stated, kStateWarps);                // the state's parts are in shared memory
         mbar_init(state_free, 1);                      // ... and have been read
-        mbar_init(summed, 1);                          // the chunk's sums are on top of the state, V' has been read
-        mbar_init(cleaned, kWorkers);                  // rows behind the last frame are zeroed
+        mbar_init(part_free, 1);                       // the first part of V' has been read
+        mbar_init(part_free + 8, 1);                   // ... the second
+        mbar_init(summed, 1);                          // ... the third, and the chunk's sums are on top of the state
+        mbar_init(cleaned, kStateWarps);                // rows behind the last frame are zeroed
         mbar_init_done();
     }
     if (warp == 3) tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -362,10 +365,11 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ok = mbar_wait(parted, c & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                for (int p = 0; p < 3; ++p)
+                for (int p = 0; p < 3; ++p) {
                     for (int k = 0; k < steps; ++k)
                         mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + p * VT + k * 2048, 0), i_state, 1);
-                tc_commit(summed);
+                    tc_commit(part_free + 8 * p);      // (summed behind the third)
+                }
                 if (share == 1) tc_commit(k_empty + 8 * ks);
                 for (int h = 0; h < share && ok; ++h, ++n) {
                     if (OUT) {
@@ -463,63 +467,18 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             if (lane == 0) mbar_arrive(d_full + 8 * slot);
         }
         if (MODE == 1 && lane == 0 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
-    } else if (warp >= 4) {
-        // A worker has 32 rows (those of its quarter w of the TMEM lanes) and a quarter u of the columns of everything: frames' rows of V and V', of the scores and of
-        // the outputs, rows of the state.  All of them do the same at the same time (roles of their own, at eight times the code, waited for instructions), in an
-        // order that leaves the tensor pipe no pause: while it sums a chunk's state they do the outputs of the step before, the weights of this one and the
-        // parts of the next chunk's values.
-        const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane;
-        const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        const int j0 = it.c0 + u * 16;
+    } else if (warp >= 4 && warp < 4 + kStateWarps) {
+        // The state, and V'.  A thread has half (32 columns) of a row of each.
+        const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane, j0 = it.c0 + u * 32;
+        const uint32_t at = tmem + kState + ((uint32_t)(w * 32) << 16) + u * 32;
         const bool holds = w < SQ;                     // rows of the state
-        uint32_t n = 0;
-        // Outputs of the step before.
-        auto output = [&](int c, int h) {
-            const Decays& D = decays[c % kDecays];
-            const int frames = c + 1 == chunks ? tail : kChunk;
-            const int64_t f = f0 + (int64_t)c * kChunk + i;
-            const uint32_t m = n - 1;
-            if (!mbar_wait_warp(far_full, m & 1, gave_up) || !mbar_wait_warp(near_full, m & 1, gave_up)) return false;
-            tc_fence_after();
-            uint32_t a[16], b[16], x[16];
-            tc_ld(tmem + kFar + lanes + u * 16, a);
-            tc_ld(tmem + kFar + kCols + lanes + u * 16, b);
-            tc_ld(tmem + kNear + lanes + u * 16, x);
-            tc_wait_ld();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(taken);
-            const uint4 odd = *reinterpret_cast<const uint4*>(&D.odd[u * 4]);
-            if (i < frames) {
-                const float r = D.row[i] * A.scale;
-                const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
-                Pair y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    y[e] = fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, add2(pair(a[2 * e], a[2 * e + 1]), pair(b[2 * e], b[2 * e + 1]))));
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + f * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + j0;
-                const int left = A.dv - j0;
-                if (left >= 16 && C.out_vec) {
-                    *reinterpret_cast<uint4*>(out) = make_uint4(round_bf16(y[0]), round_bf16(y[1]), round_bf16(y[2]), round_bf16(y[3]));
-                    *reinterpret_cast<uint4*>(out + 8) = make_uint4(round_bf16(y[4]), round_bf16(y[5]), round_bf16(y[6]), round_bf16(y[7]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 z = split(y[e]);
-                        if (2 * e < left) out[2 * e] = __float2bfloat16(z.x);
-                        if (2 * e + 1 < left) out[2 * e + 1] = __float2bfloat16(z.y);
-                    }
-                }
-                if (odd.x | odd.y | odd.z | odd.w) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, out);
-            }
-            __syncwarp();
-            return true;
-        };
+        const Pair minus = pair(-1.0f, -1.0f);
         bool ok = true;
-        for (int c = 0; c <= chunks && ok; ++c) {
-            const int slot = c % kDecays, frames = c + 1 == chunks ? tail : kChunk;
+        for (int c = 0; c <= chunks; ++c) {
+            const int slot = c % kDecays;
             Decays& D = decays[slot];
-            uint32_t a[8], b[8], d[8];                 // parts of V'
+            uint32_t b[16], d[16];                     // second and third part of V'
+            uint8_t* const parts = w_mem + i * 128;
             if (c < chunks) {
                 uint8_t* row = v_mem + (c & 1) * VT + i * 128;
                 ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
@@ -527,8 +486,8 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 if (clean && c + 1 == chunks) {
                     ok = mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
                     if (!ok) break;
-                    if (i >= frames) {
-                        for (int x = 2 * u; x < 2 * u + 2; ++x) {
+                    if (i >= tail) {
+                        for (int x = 4 * u; x < 4 * u + 4; ++x) {
                             const uint32_t place = ((uint32_t)x ^ (i & 7)) << 4;
                             *reinterpret_cast<uint4*>(row + place) = make_uint4(0, 0, 0, 0);
                             for (int p = 0; p < DK / 64; ++p) *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + i * 128 + place) = make_uint4(0, 0, 0, 0);
@@ -540,148 +499,165 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 }
                 ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
                 if (!ok) break;
-                const Pair weight = pair(D.rest[i], D.rest[i]), minus = pair(-1.0f, -1.0f);
+                const Pair weight = pair(D.rest[i], D.rest[i]);
+                if (c > 0) {
+                    ok = mbar_wait_warp(part_free, (c - 1) & 1, gave_up);
+                    if (!ok) break;
+                }
                 __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);  // NaN as soon as a value is not finite
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(row + (((uint32_t)(2 * u + x) ^ (i & 7)) << 4));
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t place = ((uint32_t)(4 * u + x) ^ (i & 7)) << 4;
+                    const uint4 v = *reinterpret_cast<const uint4*>(row + place);
                     const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                    uint32_t a[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
                         Pair y = mul2(widen_bf16(in[e]), weight);
-                        a[4 * x + e] = round_bf16(y);
-                        y = fma2(widen_bf16(a[4 * x + e]), minus, y);
+                        a[e] = round_bf16(y);
+                        y = fma2(widen_bf16(a[e]), minus, y);
                         b[4 * x + e] = round_bf16(y);
                         d[4 * x + e] = round_bf16(fma2(widen_bf16(b[4 * x + e]), minus, y));
                     }
+                    *reinterpret_cast<uint4*>(parts + place) = make_uint4(a[0], a[1], a[2], a[3]);
                 }
                 if (OUT) {
                     uint32_t cols = 0;
                     if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
 #pragma unroll 1
-                        for (int e = 0; e < 16; ++e) {
-                            uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(2 * u + e / 8) ^ (i & 7)) << 4)) + (e & 7);
+                        for (int e = 0; e < 32; ++e) {
+                            uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(4 * u + e / 8) ^ (i & 7)) << 4)) + (e & 7);
                             const bool is = (*p & 0x7F80u) == 0x7F80u;
                             if (is) *p = 0;
                             if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
                         }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {                    // the first part says what has to be said
-                            const uint32_t keep = ((a[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((a[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                        for (int e = 0; e < 16; ++e) {                   // the first part says what has to be said; what is left over is NaN
+                            const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
                             b[e] &= keep;
                             d[e] &= keep;
                         }
                     }
                     if (lane == 0) D.odd[u * 4 + w] = cols;
                 }
+                if (c > 0) {
+                    ok = mbar_wait_warp(part_free + 8, (c - 1) & 1, gave_up);
+                    if (!ok) break;
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    *reinterpret_cast<uint4*>(parts + VT + (((uint32_t)(4 * u + x) ^ (i & 7)) << 4)) = make_uint4(b[4 * x], b[4 * x + 1], b[4 * x + 2], b[4 * x + 3]);
             }
             if (c > 0) {
                 ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
             }
-            // the state that enters chunk c, or the last one
-            uint32_t x[16];
+            if (c == chunks) {                         // the last state
+                float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
+                if (holds && to) {
+                    uint32_t x[32];
+                    tc_ld(at, x);
+                    if (i < A.dk) {
+                        if (j0 + 32 <= A.dv && !((uintptr_t)(to + j0) & 15)) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(to + j0 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (j0 + e < A.dv) to[j0 + e] = __uint_as_float(x[e]);
+                        }
+                    }
+                }
+                break;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint4*>(parts + 2 * VT + (((uint32_t)(4 * u + q) ^ (i & 7)) << 4)) = make_uint4(d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]);
+            uint32_t x[32];                            // the state that enters the chunk
             if (holds) {
                 if (c > 0) {
-                    tc_ld(tmem + kState + lanes + u * 16, x);
-                    tc_wait_ld();
+                    tc_ld(at, x);
                 } else {
                     const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[e] = from && i < A.dk && j0 + e < A.dv ? __float_as_uint(from[j0 + e]) : 0u;
+                    for (int e = 0; e < 32; ++e) x[e] = from && i < A.dk && j0 + e < A.dv ? __float_as_uint(from[j0 + e]) : 0u;
                 }
-            }
-            if (c == chunks) {
-                float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
-                if (holds && to && i < A.dk) {
-                    if (j0 + 16 <= A.dv && !((uintptr_t)(to + j0) & 15)) {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j0 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (j0 + e < A.dv) to[j0 + e] = __uint_as_float(x[e]);
-                    }
-                }
-                __syncwarp();
-                if (OUT) output(c - 1, share - 1);
-                break;
-            }
-            {
-                uint8_t* to = w_mem + i * 128;
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t place = ((uint32_t)(2 * u + q) ^ (i & 7)) << 4;
-                    *reinterpret_cast<uint4*>(to + place) = make_uint4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
-                    *reinterpret_cast<uint4*>(to + VT + place) = make_uint4(b[4 * q], b[4 * q + 1], b[4 * q + 2], b[4 * q + 3]);
-                    *reinterpret_cast<uint4*>(to + 2 * VT + place) = make_uint4(d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]);
-                }
-            }
-            if (holds) {
                 const Pair whole = pair(D.whole, D.whole);
-                uint32_t y[16];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 z = split(mul2(pair(x[2 * e], x[2 * e + 1]), whole));
-                    y[2 * e] = __float_as_uint(z.x);
-                    y[2 * e + 1] = __float_as_uint(z.y);
+                for (int m = 0; m < 2; ++m) {
+                    uint32_t y[16];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 z = split(mul2(pair(x[16 * m + 2 * e], x[16 * m + 2 * e + 1]), whole));
+                        y[2 * e] = __float_as_uint(z.x);
+                        y[2 * e + 1] = __float_as_uint(z.y);
+                    }
+                    tc_st(at + 16 * m, y);
                 }
-                tc_st(tmem + kState + lanes + u * 16, y);
                 tc_wait_st();
             }
             fence_async_shared();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(parted);
-            if (!OUT) {
-                if (lane == 0) mbar_arrive(d_empty + 8 * slot);
-                continue;
+            if (lane == 0) {
+                mbar_arrive(parted);
+                mbar_arrive(d_empty + 8 * slot);
             }
+            if (!OUT) continue;
             if (c > 0) {
                 ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
                 if (!ok) break;
             }
             if (holds) {
-                uint32_t hi[8], lo[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const Pair y = pair(x[2 * e], x[2 * e + 1]);
-                    hi[e] = round_bf16(y);
-                    const float2 left = split(fma2(widen_bf16(hi[e]), pair(-1.0f, -1.0f), y));
-                    // (an infinite value: max makes the NaN that is left over finite, the first part says what has to be said)
-                    lo[e] = round_bf16(pair(fmaxf(left.x, -3.0e38f), fmaxf(left.y, -3.0e38f)));
-                }
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t hi[4], lo[4];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t place = (uint32_t)i * 128u + (((uint32_t)(2 * u + q) ^ (i & 7)) << 4);
-                    *reinterpret_cast<uint4*>(s_mem + place) = make_uint4(hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]);
-                    *reinterpret_cast<uint4*>(s_mem + ST + place) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
+                    for (int e = 0; e < 4; ++e) {
+                        const Pair y = pair(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
+                        hi[e] = round_bf16(y);
+                        const float2 left = split(fma2(widen_bf16(hi[e]), minus, y));
+                        // (an infinite value: max makes the NaN that is left over finite, the first part says what has to be said)
+                        lo[e] = round_bf16(pair(fmaxf(left.x, -3.0e38f), fmaxf(left.y, -3.0e38f)));
+                    }
+                    uint8_t* to = s_mem + i * 128 + (((uint32_t)(4 * u + q) ^ (i & 7)) << 4);
+                    *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4*>(to + ST) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 }
             }
             fence_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(stated);
-            for (int h = 0; h < share; ++h) {
-                if (n > 0) {
-                    ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1);
-                    if (!ok) break;
-                    if (h == 0 && lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
-                }
+        }
+    } else if (OUT && warp >= 4) {
+        // Scores -> P, and outputs.  A thread has half of a frame's row: 64 columns of the scores, 32 of the outputs.
+        const int w = warp & 3, half = (warp - 4 - kStateWarps) >> 2, i = w * 32 + lane, j0 = it.c0 + half * 32;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + i) * A.so.frame + (int64_t)it.g * A.share * A.so.head + j0;
+        const int left = A.dv - j0;                    // columns that there are
+        uint32_t n = 0;
+        bool ok = true;
+        for (int c = 0; c < chunks && ok; ++c, out += kChunk * A.so.frame) {
+            const int slot = c % kDecays, frames = c + 1 == chunks ? tail : kChunk;
+            const Decays& D = decays[slot];
+            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
+            if (!ok) break;
+            for (int h = 0; h < share; ++h, ++n) {
                 ok = mbar_wait_warp(scored, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                if (u * 32 < frames) {                 // scores -> P, 32 columns from u * 32 on
+#pragma unroll 1
+                for (int u = 2 * half; u < 2 * half + 2 && u * 32 < frames; ++u) {         // 32 columns at a time
                     uint32_t p[16];
                     if (u > w) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) p[e] = 0;
                     } else {
+                        const float hi = D.hi[i], lo = D.lo[i];
                         uint32_t s[32];
                         tc_ld(tmem + kScores + lanes + u * 32, s);
-                        tc_wait_ld();
-                        const float hi = D.hi[i], lo = D.lo[i];
                         if (u < w) {
                             const float r = exp2_fast((hi - D.hi[u * 32 + 31]) + (lo - D.lo[u * 32 + 31]));
                             const Pair row = pair(r, r);
@@ -694,22 +670,62 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                         } else {
                             const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo), minus = pair(-1.0f, -1.0f);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const Pair ch = *reinterpret_cast<const Pair*>(&D.hi[u * 32 + 2 * e]), cl = *reinterpret_cast<const Pair*>(&D.lo[u * 32 + 2 * e]);
-                                const float2 g = split(add2(fma2(ch, minus, hi2), fma2(cl, minus, lo2)));
-                                const float2 z = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g.x), exp2_fast(g.y))));
-                                p[e] = round_bf16(pair(2 * e <= lane ? z.x : 0.0f, 2 * e + 1 <= lane ? z.y : 0.0f));
+                            for (int e = 0; e < 16; e += 2) {
+                                const ulonglong2 ch = *reinterpret_cast<const ulonglong2*>(&D.hi[u * 32 + 2 * e]), cl = *reinterpret_cast<const ulonglong2*>(&D.lo[u * 32 + 2 * e]);
+                                const float2 g0 = split(add2(fma2(ch.x, minus, hi2), fma2(cl.x, minus, lo2))), g1 = split(add2(fma2(ch.y, minus, hi2), fma2(cl.y, minus, lo2)));
+                                const float2 z0 = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g0.x), exp2_fast(g0.y))));
+                                const float2 z1 = split(mul2(pair(s[2 * e + 2], s[2 * e + 3]), pair(exp2_fast(g1.x), exp2_fast(g1.y))));
+                                p[e] = round_bf16(pair(2 * e <= lane ? z0.x : 0.0f, 2 * e + 1 <= lane ? z0.y : 0.0f));
+                                p[e + 1] = round_bf16(pair(2 * e + 2 <= lane ? z1.x : 0.0f, 2 * e + 3 <= lane ? z1.y : 0.0f));
                             }
                         }
                     }
                     tc_st(tmem + kWeights + lanes + u * 16, p);
-                    tc_wait_st();
                 }
+                tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(weighed);
-                ++n;
+                ok = mbar_wait_warp(far_full, n & 1, gave_up) && mbar_wait_warp(near_full, n & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                __nv_bfloat16* to = out + h * A.so.head;
+                const float r = D.row[i] * A.scale;
+                const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
+#pragma unroll 1
+                for (int m = 0; m < 32; m += 16) {
+                    uint32_t a[16], b[16], x[16];
+                    const uint32_t at = tmem + lanes + half * 32 + m;
+                    tc_ld(at + kFar, at + kFar + kCols, at + kNear, a, b, x);
+                    if (m == 16) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(taken);
+                    }
+                    if (i < frames) {
+                        Pair y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            y[e] = fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, add2(pair(a[2 * e], a[2 * e + 1]), pair(b[2 * e], b[2 * e + 1]))));
+                        if (left >= 32 && C.out_vec) {
+                            *reinterpret_cast<uint4*>(to + m) = make_uint4(round_bf16(y[0]), round_bf16(y[1]), round_bf16(y[2]), round_bf16(y[3]));
+                            *reinterpret_cast<uint4*>(to + m + 8) = make_uint4(round_bf16(y[4]), round_bf16(y[5]), round_bf16(y[6]), round_bf16(y[7]));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float2 z = split(y[e]);
+                                if (m + 2 * e < left) to[m + 2 * e] = __float2bfloat16(z.x);
+                                if (m + 2 * e + 1 < left) to[m + 2 * e + 1] = __float2bfloat16(z.y);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+                const uint4 odd = *reinterpret_cast<const uint4*>(&D.odd[half * 4]);
+                if ((odd.x | odd.y | odd.z | odd.w) && i < frames) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
+                __syncwarp();
             }
+            if (lane == 0) mbar_arrive(d_empty + 8 * slot);
         }
     }
     tc_fence_before();

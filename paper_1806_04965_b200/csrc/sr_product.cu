@@ -100,7 +100,6 @@ __device__ __forceinline__ void drain(const ProductArgs& P, T* out, uint32_t tad
         for (int c = half * CW; c < n; c += 2 * CW, p += 2 * CW * P.out_stride) {
             uint32_t v[CW];
             tc_ld(taddr + acc * NT + c, v);
-            tc_wait_ld();
             if (o < P.outs) {
                 T* q = p;
                 if (c + CW <= n) {
@@ -238,7 +237,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
             for (int c = half * CW; c < NT && ok; c += 2 * CW) {
                 uint32_t v[CW];
                 tc_ld(tmem + lanes + c, v);
-                tc_wait_ld();
 #pragma unroll
                 for (int i = 0; i < CW; ++i) mine[(c + i) * kOuts + quarter * 32 + lane] = __uint_as_float(v[i]);
             }
