@@ -6,12 +6,12 @@
 // four matrix products per chunk and group of 64 columns of v (the last one a CTA's: it holds DK x 64 values of a state), all of them tcgen05.mma
 // with M = 128:
 //   scores  Q K^T              128 frames x 128 frames, both from shared memory                       (TMEM columns 0 .. 127)
-//   near    P V                P = scores * decays, lower triangle, bf16, back in TMEM as the A operand (columns 320 .. 383)
-//   far     Q [S_hi | S_lo]    the state in two bf16 parts, 16 bits of it                             (columns 192 .. 319)
-//   state   K^T [V'_hi, V'_mid, V'_lo], V' = V exp(G_last - G_j) in three bf16 parts, 24 bits: the state itself is as exact as 32 bits make it
-//                              summed on top of the decayed state in TMEM                            (columns 128 .. 191)
-// K is read along both of its sides from the same tile.  Roundings to bf16: P (every product of it is rounded once, as the output is) and what the parts
-// leave out.
+//   near    P V                P = scores * decays, lower triangle, bf16, back in TMEM as the A operand (columns 448 .. 511, sums in 384 .. 447)
+//   far     Q S                the state rounded to bf16 for this product                             (columns 320 .. 383)
+//   state   K^T [V'_hi | V'_mid | V'_lo], V' = V exp(G_last - G_j) in three bf16 parts, 24 bits: the state itself is as exact as 32 bits make it.  The
+//                              decayed state and the parts' sums are three accumulators side by side (columns 128 .. 319), added up once per chunk
+// K is read along both of its sides from the same tile.  Roundings to bf16: P and the state as factors of the outputs, one each, on different terms of the sum
+// (the outputs are as far off as one rounding more of the output makes them; with the state in two parts it was 1.37 times one rounding, so 1.41).
 // Decays never exceed one: exp(G_i - G_j) is a product of exp(G_i - G_e) and exp(G_e - G_j) with e the last frame of j's 32, where i lies behind them, and
 // one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
 //
@@ -35,16 +35,17 @@ using namespace srx;
 
 constexpr int kChunk = 128, kCols = 64, kDecays = 4;
 constexpr int kStateWarps = 8, kOutWarps = 8, kThreads = 128 + 32 * (kStateWarps + kOutWarps);
-constexpr uint32_t kScores = 0, kState = 128, kFar = 192, kNear = 320, kWeights = 384;       // TMEM columns
+constexpr uint32_t kScores = 0, kState = 128, kFar = 320, kNear = 384, kWeights = 448;       // TMEM columns
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct ChunkArgs {
-    CUtensorMap q_map, k_map, v_map;
+    CUtensorMap q_map, k_map, v_map, out_map;
     AttentionArgs A;
     float* sums;                                       // [slot][group][dk][dv]: sums of a segment, then the states that enter it
     float* decays;                                     // [slot][group]: decay over a segment
     int64_t segment;                                   // frames of a segment (0: whole sequences)
-    int32_t slots, v_tiles, out_vec;
+    int32_t slots, v_tiles;
+    int32_t out_copies;                                // outputs leave by TMA
     int* error;
 };
 
@@ -221,8 +222,8 @@ template <int DK, int MODE>
 __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_constant__ ChunkArgs C)
 {
     constexpr bool OUT = MODE != 1;                    // outputs are wanted
-    constexpr int NK = DK == 64 ? 2 : 1;               // slots for keys
-    constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V, of a part of the state
+    constexpr int NQ = DK == 64 ? 2 : 1;               // slots for queries
+    constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V (or outputs), of the state
     constexpr int SQ = DK / 32;                        // quarters of the TMEM lanes with rows of the state
     extern __shared__ uint8_t smem_raw[];
     __shared__ Decays decays[kDecays];
@@ -249,13 +250,14 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     const int share = OUT ? A.share : 1;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t k_tiles = base, v_tiles = k_tiles + NK * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + 2 * KT, s_tiles = w_tiles + 3 * VT;
+    const uint32_t k_tiles = base, v_tiles = k_tiles + 2 * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + NQ * KT, s_tiles = w_tiles + 3 * VT;
+    const uint32_t o_tile = s_tiles + ST;
     uint8_t* const k_mem = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t *const v_mem = k_mem + NK * KT, *const w_mem = v_mem + 2 * VT + 2 * KT, *const s_mem = w_mem + 3 * VT;
+    uint8_t *const v_mem = k_mem + 2 * KT, *const w_mem = v_mem + 2 * VT + NQ * KT, *const s_mem = w_mem + 3 * VT, *const o_mem = s_mem + ST;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
     const uint32_t scored = bar(20), weighed = bar(21), far_full = bar(22), near_full = bar(23), taken = bar(24);
-    const uint32_t parted = bar(25), stated = bar(26), state_free = bar(27), cleaned = bar(28), part_free = bar(29), summed = bar(31);
+    const uint32_t parted = bar(25), stated = bar(26), state_free = bar(27), cleaned = bar(28), summed = bar(29);
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int i = 0; i < 2; ++i) {
@@ -278,9 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         mbar_init(parted, kStateWarps);                // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
         mbar_init(stated, kStateWarps);                // the state's parts are in shared memory
         mbar_init(state_free, 1);                      // ... and have been read
-        mbar_init(part_free, 1);                       // the first part of V' has been read
-        mbar_init(part_free + 8, 1);                   // ... the second
-        mbar_init(summed, 1);                          // ... the third, and the chunk's sums are on top of the state
+        mbar_init(summed, 1);                          // the chunk's sums are on top of the state, V' has been read
         mbar_init(cleaned, kStateWarps);                // rows behind the last frame are zeroed
         mbar_init_done();
     }
@@ -302,8 +302,8 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             uint32_t n = 0;                            // steps: chunks x heads
             auto frame = [&](int c) { return (int)(f0 + (int64_t)c * kChunk); };
             auto load_q = [&](int c, int h) {
-                const uint32_t s = n & 1, b = q_full + 8 * s;
-                ok = ok && mbar_wait(q_empty + 8 * s, ((n >> 1) & 1) ^ 1, gave_up);
+                const uint32_t s = n % NQ, b = q_full + 8 * s;
+                ok = ok && mbar_wait(q_empty + 8 * s, ((n / NQ) & 1) ^ 1, gave_up);
                 if (!ok) return;
                 mbar_expect_tx(b, KT);
 #pragma unroll
@@ -311,20 +311,17 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ++n;
             };
             for (int c = 0; c < chunks && ok; ++c) {
-                const uint32_t ks = c % NK, vs = c & 1;
-                ok = mbar_wait(v_empty + 8 * vs, ((c >> 1) & 1) ^ 1, gave_up);
+                const uint32_t s = c & 1;
+                ok = mbar_wait(k_empty + 8 * s, ((c >> 1) & 1) ^ 1, gave_up);
                 if (!ok) break;
-                mbar_expect_tx(v_full + 8 * vs, VT);
-                tma_load_4d(v_tiles + vs * VT, &C.v_map, v_full + 8 * vs, it.c0, it.g, (int)it.span.b, frame(c));
-                if (OUT) load_q(c, 0);
-                ok = ok && mbar_wait(k_empty + 8 * ks, ((c / NK) & 1) ^ 1, gave_up);
-                if (!ok) break;
-                mbar_expect_tx(k_full + 8 * ks, KT);
+                mbar_expect_tx(k_full + 8 * s, KT);
 #pragma unroll
-                for (int p = 0; p < DK / 64; ++p) {
-                    tma_load_4d(k_tiles + ks * KT + p * 16384, &C.k_map, k_full + 8 * ks, p * 64, it.g, (int)it.span.b, frame(c));
-                    if (c + 1 < chunks) tma_prefetch_4d(&C.k_map, p * 64, it.g, (int)it.span.b, frame(c + 1));
-                }
+                for (int p = 0; p < DK / 64; ++p) tma_load_4d(k_tiles + s * KT + p * 16384, &C.k_map, k_full + 8 * s, p * 64, it.g, (int)it.span.b, frame(c));
+                ok = mbar_wait(v_empty + 8 * s, ((c >> 1) & 1) ^ 1, gave_up);
+                if (!ok) break;
+                mbar_expect_tx(v_full + 8 * s, VT);
+                tma_load_4d(v_tiles + s * VT, &C.v_map, v_full + 8 * s, it.c0, it.g, (int)it.span.b, frame(c));
+                if (OUT) load_q(c, 0);
                 for (int h = 1; h < share && OUT; ++h) load_q(c, h);
             }
             if (!ok)                                   // what was asked for still has to land
@@ -337,18 +334,18 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         }
     } else if (warp == 1) {
         if (elect_one()) {
-            constexpr uint32_t i_scores = idesc_bf16(128, 0, 0), i_far = idesc_bf16(128, 0, 1), i_near = idesc_bf16(64, 0, 1), i_state = idesc_bf16(64, 1, 1);
+            constexpr uint32_t i_scores = idesc_bf16(128, 0, 0), i_far = idesc_bf16(64, 0, 1), i_near = idesc_bf16(64, 0, 1), i_state = idesc_bf16(192, 1, 1);
             bool ok = true;
             uint32_t n = 0;
             // Scores of step m, the first of chunk c's if h is 0.
             auto scores = [&](uint32_t m, int c, int h) {
-                const uint32_t ks = c % NK, q_at = q_tiles + (m & 1) * KT, k_at = k_tiles + ks * KT;
+                const uint32_t q_at = q_tiles + (m % NQ) * KT, k_at = k_tiles + (c & 1) * KT;
                 if (h == 0) {
-                    ok = ok && mbar_wait(k_full + 8 * ks, (c / NK) & 1, gave_up);
+                    ok = ok && mbar_wait(k_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
                     if (clean && c + 1 == chunks) ok = ok && mbar_wait(cleaned, 0, gave_up);
                 }
                 if (OUT) {
-                    ok = ok && mbar_wait(q_full + 8 * (m & 1), (m >> 1) & 1, gave_up);
+                    ok = ok && mbar_wait(q_full + 8 * (m % NQ), (m / NQ) & 1, gave_up);
                     if (!ok) return;
                     tc_fence_after();
 #pragma unroll
@@ -359,31 +356,33 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             };
             scores(0, 0, 0);
             for (int c = 0; c < chunks && ok; ++c) {
-                const uint32_t ks = c % NK, k_at = k_tiles + ks * KT, v_at = v_tiles + (c & 1) * VT;
+                const uint32_t k_at = k_tiles + (c & 1) * KT, v_at = v_tiles + (c & 1) * VT;
                 const int steps = ((c + 1 == chunks ? tail : kChunk) + 15) / 16;        // of 16 frames
-                // the state first: the next chunk waits for it
-                ok = mbar_wait(parted, c & 1, gave_up);
-                if (!ok) break;
-                tc_fence_after();
-                for (int p = 0; p < 3; ++p) {
-                    for (int k = 0; k < steps; ++k)
-                        mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + p * VT + k * 2048, 0), i_state, 1);
-                    tc_commit(part_free + 8 * p);      // (summed behind the third)
-                }
-                if (share == 1) tc_commit(k_empty + 8 * ks);
                 for (int h = 0; h < share && ok; ++h, ++n) {
                     if (OUT) {
-                        const uint32_t q_at = q_tiles + (n & 1) * KT;
+                        // the far part ahead of the state's sums: the queries of the next step come in meanwhile, and the weights of this one are worked out
+                        const uint32_t q_at = q_tiles + (n % NQ) * KT;
                         if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
                         ok = ok && mbar_wait(taken, (n & 1) ^ 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
                         for (int k = 0; k < DK / 16; ++k)
-                            mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, ST), i_far, k > 0);
-                        tc_commit(q_empty + 8 * (n & 1));
+                            mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, 0), i_far, k > 0);
+                        tc_commit(q_empty + 8 * (n % NQ));
                         tc_commit(far_full);
                         if (h + 1 == share) tc_commit(state_free);
+                    }
+                    if (h == 0) {
+                        ok = mbar_wait(parted, c & 1, gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+                        for (int k = 0; k < steps; ++k)
+                            mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + k * 2048, VT), i_state, 1);
+                        tc_commit(summed);
+                        if (share == 1) tc_commit(k_empty + 8 * (c & 1));
+                    }
+                    if (OUT) {
                         ok = mbar_wait(weighed, n & 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
@@ -393,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     if (h + 1 == share) tc_commit(v_empty + 8 * (c & 1));
                     if (h + 1 < share) {
                         scores(n + 1, c, h + 1);
-                        if (h + 2 == share) tc_commit(k_empty + 8 * ks);
+                        if (h + 2 == share) tc_commit(k_empty + 8 * (c & 1));
                     } else if (c + 1 < chunks) {
                         scores(n + 1, c + 1, 0);
                     }
@@ -477,20 +476,20 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         for (int c = 0; c <= chunks; ++c) {
             const int slot = c % kDecays;
             Decays& D = decays[slot];
-            uint32_t b[16], d[16];                     // second and third part of V'
+            uint32_t a[16], b[16], d[16];              // parts of V'
             uint8_t* const parts = w_mem + i * 128;
             if (c < chunks) {
                 uint8_t* row = v_mem + (c & 1) * VT + i * 128;
                 ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
                 if (!ok) break;
                 if (clean && c + 1 == chunks) {
-                    ok = mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
+                    ok = mbar_wait_warp(k_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
                     if (!ok) break;
                     if (i >= tail) {
                         for (int x = 4 * u; x < 4 * u + 4; ++x) {
                             const uint32_t place = ((uint32_t)x ^ (i & 7)) << 4;
                             *reinterpret_cast<uint4*>(row + place) = make_uint4(0, 0, 0, 0);
-                            for (int p = 0; p < DK / 64; ++p) *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + i * 128 + place) = make_uint4(0, 0, 0, 0);
+                            for (int p = 0; p < DK / 64; ++p) *reinterpret_cast<uint4*>(k_mem + (c & 1) * KT + p * 16384 + i * 128 + place) = make_uint4(0, 0, 0, 0);
                         }
                     }
                     fence_async_shared();
@@ -500,27 +499,21 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
                 if (!ok) break;
                 const Pair weight = pair(D.rest[i], D.rest[i]);
-                if (c > 0) {
-                    ok = mbar_wait_warp(part_free, (c - 1) & 1, gave_up);
-                    if (!ok) break;
-                }
                 __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);  // NaN as soon as a value is not finite
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const uint32_t place = ((uint32_t)(4 * u + x) ^ (i & 7)) << 4;
                     const uint4 v = *reinterpret_cast<const uint4*>(row + place);
                     const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t a[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
                         Pair y = mul2(widen_bf16(in[e]), weight);
-                        a[e] = round_bf16(y);
-                        y = fma2(widen_bf16(a[e]), minus, y);
+                        a[4 * x + e] = round_bf16(y);
+                        y = fma2(widen_bf16(a[4 * x + e]), minus, y);
                         b[4 * x + e] = round_bf16(y);
                         d[4 * x + e] = round_bf16(fma2(widen_bf16(b[4 * x + e]), minus, y));
                     }
-                    *reinterpret_cast<uint4*>(parts + place) = make_uint4(a[0], a[1], a[2], a[3]);
                 }
                 if (OUT) {
                     uint32_t cols = 0;
@@ -541,95 +534,93 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     }
                     if (lane == 0) D.odd[u * 4 + w] = cols;
                 }
-                if (c > 0) {
-                    ok = mbar_wait_warp(part_free + 8, (c - 1) & 1, gave_up);
-                    if (!ok) break;
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    *reinterpret_cast<uint4*>(parts + VT + (((uint32_t)(4 * u + x) ^ (i & 7)) << 4)) = make_uint4(b[4 * x], b[4 * x + 1], b[4 * x + 2], b[4 * x + 3]);
             }
             if (c > 0) {
                 ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
             }
-            if (c == chunks) {                         // the last state
+            if (c < chunks) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    uint8_t* to = parts + (((uint32_t)(4 * u + x) ^ (i & 7)) << 4);
+                    *reinterpret_cast<uint4*>(to) = make_uint4(a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3]);
+                    *reinterpret_cast<uint4*>(to + VT) = make_uint4(b[4 * x], b[4 * x + 1], b[4 * x + 2], b[4 * x + 3]);
+                    *reinterpret_cast<uint4*>(to + 2 * VT) = make_uint4(d[4 * x], d[4 * x + 1], d[4 * x + 2], d[4 * x + 3]);
+                }
+                if (OUT && c > 0) {
+                    ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
+                    if (!ok) break;
+                }
+            }
+            if (holds) {
+                const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
                 float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
-                if (holds && to) {
-                    uint32_t x[32];
-                    tc_ld(at, x);
-                    if (i < A.dk) {
-                        if (j0 + 32 <= A.dv && !((uintptr_t)(to + j0) & 15)) {
+                const Pair whole = c < chunks ? pair(D.whole, D.whole) : 0;
+                const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(to + j0 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                        } else {
+                for (int m = 0; m < 32; m += 16) {
+                    const int j = j0 + m;
+                    Pair y[8];                         // the state that enters the chunk: the sum of what its three parts have become
+                    if (c > 0) {
+                        uint32_t x0[16], x1[16], x2[16];
+                        tc_ld(at + m, at + kCols + m, at + 2 * kCols + m, x0, x1, x2);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (j0 + e < A.dv) to[j0 + e] = __uint_as_float(x[e]);
+                        for (int e = 0; e < 8; ++e)
+                            y[e] = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool there = from && i < A.dk;
+                            y[e] = pair(there && j + 2 * e < A.dv ? from[j + 2 * e] : 0.0f, there && j + 2 * e + 1 < A.dv ? from[j + 2 * e + 1] : 0.0f);
                         }
                     }
-                }
-                break;
-            }
+                    if (c < chunks) {
+                        uint32_t x[16];
+                        if (OUT) {
+                            uint8_t* part = s_mem + i * 128;
+                            const int q = 4 * u + m / 8;
+                            *reinterpret_cast<uint4*>(part + (((uint32_t)q ^ (i & 7)) << 4)) = make_uint4(round_bf16(y[0]), round_bf16(y[1]), round_bf16(y[2]), round_bf16(y[3]));
+                            *reinterpret_cast<uint4*>(part + (((uint32_t)(q + 1) ^ (i & 7)) << 4)) = make_uint4(round_bf16(y[4]), round_bf16(y[5]), round_bf16(y[6]), round_bf16(y[7]));
+                        }
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<uint4*>(parts + 2 * VT + (((uint32_t)(4 * u + q) ^ (i & 7)) << 4)) = make_uint4(d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]);
-            uint32_t x[32];                            // the state that enters the chunk
-            if (holds) {
-                if (c > 0) {
-                    tc_ld(at, x);
-                } else {
-                    const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
+                        for (int e = 0; e < 8; ++e) {
+                            const float2 z = split(mul2(y[e], whole));
+                            x[2 * e] = __float_as_uint(z.x);
+                            x[2 * e + 1] = __float_as_uint(z.y);
+                        }
+                        tc_st(at + m, x);
+                        tc_st(at + kCols + m, none);
+                        tc_st(at + 2 * kCols + m, none);
+                    } else if (to && i < A.dk) {
+                        if (j + 16 <= A.dv && !((uintptr_t)(to + j) & 15)) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = from && i < A.dk && j0 + e < A.dv ? __float_as_uint(from[j0 + e]) : 0u;
-                }
-                const Pair whole = pair(D.whole, D.whole);
+                            for (int e = 0; e < 8; e += 2) {
+                                const float2 z0 = split(y[e]), z1 = split(y[e + 1]);
+                                *reinterpret_cast<float4*>(to + j + 2 * e) = make_float4(z0.x, z0.y, z1.x, z1.y);
+                            }
+                        } else {
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    uint32_t y[16];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 z = split(mul2(pair(x[16 * m + 2 * e], x[16 * m + 2 * e + 1]), whole));
-                        y[2 * e] = __float_as_uint(z.x);
-                        y[2 * e + 1] = __float_as_uint(z.y);
+                            for (int e = 0; e < 8; ++e) {
+                                const float2 z = split(y[e]);
+                                if (j + 2 * e < A.dv) to[j + 2 * e] = z.x;
+                                if (j + 2 * e + 1 < A.dv) to[j + 2 * e + 1] = z.y;
+                            }
+                        }
                     }
-                    tc_st(at + 16 * m, y);
+                    __syncwarp();
                 }
                 tc_wait_st();
             }
+            if (c == chunks) break;
             fence_async_shared();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(parted);
+                if (OUT) mbar_arrive(stated);
                 mbar_arrive(d_empty + 8 * slot);
             }
-            if (!OUT) continue;
-            if (c > 0) {
-                ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
-                if (!ok) break;
-            }
-            if (holds) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const Pair y = pair(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
-                        hi[e] = round_bf16(y);
-                        const float2 left = split(fma2(widen_bf16(hi[e]), minus, y));
-                        // (an infinite value: max makes the NaN that is left over finite, the first part says what has to be said)
-                        lo[e] = round_bf16(pair(fmaxf(left.x, -3.0e38f), fmaxf(left.y, -3.0e38f)));
-                    }
-                    uint8_t* to = s_mem + i * 128 + (((uint32_t)(4 * u + q) ^ (i & 7)) << 4);
-                    *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *reinterpret_cast<uint4*>(to + ST) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                }
-            }
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(stated);
         }
     } else if (OUT && warp >= 4) {
         // Scores -> P, and outputs.  A thread has half of a frame's row: 64 columns of the scores, 32 of the outputs.
@@ -637,6 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + i) * A.so.frame + (int64_t)it.g * A.share * A.so.head + j0;
         const int left = A.dv - j0;                    // columns that there are
+        const bool leads = warp == 4 + kStateWarps && lane == 0;
         uint32_t n = 0;
         bool ok = true;
         for (int c = 0; c < chunks && ok; ++c, out += kChunk * A.so.frame) {
@@ -689,44 +681,48 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ok = mbar_wait_warp(far_full, n & 1, gave_up) && mbar_wait_warp(near_full, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                __nv_bfloat16* to = out + h * A.so.head;
                 const float r = D.row[i] * A.scale;
                 const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
-#pragma unroll 1
+                const uint32_t at = tmem + lanes + half * 32;
+                uint32_t z[16];
+#pragma unroll
                 for (int m = 0; m < 32; m += 16) {
-                    uint32_t a[16], b[16], x[16];
-                    const uint32_t at = tmem + lanes + half * 32 + m;
-                    tc_ld(at + kFar, at + kFar + kCols, at + kNear, a, b, x);
-                    if (m == 16) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(taken);
-                    }
+                    uint32_t a[16], x[16];
+                    tc_ld(at + kFar + m, at + kNear + m, a, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        z[m / 2 + e] = round_bf16(fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, pair(a[2 * e], a[2 * e + 1]))));
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(taken);
+                const uint4 odd0 = *reinterpret_cast<const uint4*>(&D.odd[0]), odd1 = *reinterpret_cast<const uint4*>(&D.odd[4]);
+                const bool odd = odd0.x | odd0.y | odd0.z | odd0.w | odd1.x | odd1.y | odd1.z | odd1.w;
+                if (C.out_copies && !odd && !(clean && c + 1 == chunks)) {
+                    // through shared memory: a thread's stores would be 64 bytes of a row each
+                    if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<uint4*>(o_mem + i * 128 + (((uint32_t)(4 * half + q) ^ (i & 7)) << 4)) = make_uint4(z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]);
+                    fence_async_shared();
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    if (leads) tma_store_4d(&C.out_map, o_tile, it.c0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk));
+                    __syncwarp();
+                } else {
+                    __nv_bfloat16* to = out + h * A.so.head;
                     if (i < frames) {
-                        Pair y[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            y[e] = fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, add2(pair(a[2 * e], a[2 * e + 1]), pair(b[2 * e], b[2 * e + 1]))));
-                        if (left >= 32 && C.out_vec) {
-                            *reinterpret_cast<uint4*>(to + m) = make_uint4(round_bf16(y[0]), round_bf16(y[1]), round_bf16(y[2]), round_bf16(y[3]));
-                            *reinterpret_cast<uint4*>(to + m + 8) = make_uint4(round_bf16(y[4]), round_bf16(y[5]), round_bf16(y[6]), round_bf16(y[7]));
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float2 z = split(y[e]);
-                                if (m + 2 * e < left) to[m + 2 * e] = __float2bfloat16(z.x);
-                                if (m + 2 * e + 1 < left) to[m + 2 * e + 1] = __float2bfloat16(z.y);
-                            }
-                        }
+                        for (int e = 0; e < 32; ++e)
+                            if (e < left) to[e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
+                        if (odd) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
                     }
                     __syncwarp();
                 }
-                const uint4 odd = *reinterpret_cast<const uint4*>(&D.odd[half * 4]);
-                if ((odd.x | odd.y | odd.z | odd.w) && i < frames) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
-                __syncwarp();
             }
             if (lane == 0) mbar_arrive(d_empty + 8 * slot);
         }
+        if (leads) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -792,8 +788,8 @@ bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, in
 template <int DK, int MODE>
 cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 {
-    constexpr int NK = DK == 64 ? 2 : 1;
-    constexpr int smem = 1024 + NK * DK * 256 + 2 * kCols * 256 + 2 * DK * 256 + 3 * kCols * 256 + 2 * DK * 128;
+    constexpr int NQ = DK == 64 ? 2 : 1;
+    constexpr int smem = 1024 + 2 * DK * 256 + 2 * kCols * 256 + NQ * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256;
     const cudaError_t e = cudaFuncSetAttribute(sr_chunks_kernel<DK, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
@@ -884,11 +880,11 @@ cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d,
     C.v_tiles = (d->dv + kCols - 1) / kCols;
     C.sums = static_cast<float*>(workspace);
     C.decays = C.sums ? C.sums + (size_t)cut.slots * d->groups * d->dk * d->dv : nullptr;
-    auto whole = [](int64_t st, int64_t n) { return n <= 1 || st % 8 == 0; };
-    C.out_vec = !((uintptr_t)A.out & 15) && whole(A.so.frame, d->frames) && (A.offsets || whole(A.so.sequence, d->batch)) && whole(A.so.head, d->heads);
     const int64_t sequences = A.offsets ? 1 : d->batch;
     if (!encode(&C.q_map, A.q, A.sq, d->dk, d->heads, sequences, d->frames) || !encode(&C.k_map, A.k, A.sk, d->dk, d->groups, sequences, d->frames) ||
         !encode(&C.v_map, A.v, A.sv, d->dv, d->groups, sequences, d->frames))
         return cudaErrorInvalidValue;
+    C.out_copies = copies_fit(A.out, A.so, d->heads, sequences, d->frames);
+    if (C.out_copies && !encode(&C.out_map, A.out, A.so, d->dv, d->heads, sequences, d->frames)) return cudaErrorInvalidValue;
     return d->dk <= 64 ? launch_all<64>(C, s) : launch_all<128>(C, s);
 }
