@@ -16,7 +16,7 @@
 // one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
 //
 // Bound by memory (q, k, v, out once) where there are CTAs enough: a chunk of DK = 128 is 96 KiB per CTA, 2.6k cycles of MMAs.
-// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; 4..11 state and V', 12..19 scores -> P and outputs.
+// Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; sixteen workers for everything between the MMAs.
 // What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
 // the near product (whose zeros would spread it to earlier frames) and added by the outputs' warps; rows behind a sequence's last frame are zeroed.
 #include <cuda.h>
@@ -34,7 +34,7 @@ namespace {
 using namespace srx;
 
 constexpr int kChunk = 128, kCols = 64, kDecays = 4;
-constexpr int kStateWarps = 8, kOutWarps = 8, kThreads = 128 + 32 * (kStateWarps + kOutWarps);
+constexpr int kWorkers = 16, kThreads = 128 + 32 * kWorkers;
 constexpr uint32_t kScores = 0, kState = 128, kFar = 320, kNear = 384, kWeights = 448;       // TMEM columns
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -188,12 +188,12 @@ struct alignas(16) Decays {                            // of a chunk (read four 
     float col[kChunk];                                 // exp(G_e - G_j), e the last frame of j's 32
     float rest[kChunk];                                // exp(G_last - G_j)
     float row[kChunk];                                 // exp(G_i)
-    uint32_t odd[8];                                   // columns of the chunk's values that are not all finite: a word for [columns / 32][rows / 32]
+    uint32_t odd[kWorkers];                            // columns of the chunk's values that are not all finite: 16 bits for [columns / 16][rows / 32]
     float whole;                                       // exp(G_last)
 };
 static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read as 16-byte words");
 
-// Values that are not finite have been left out of row i of a chunk's near product: their terms for 32 columns, as the formula has them, on top of the
+// Values that are not finite have been left out of row i of a chunk's near product: their terms for 16 columns, as the formula has them, on top of the
 // stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
 __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, __nv_bfloat16* out)
 {
@@ -205,7 +205,7 @@ __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays&
         float p = 0.0f;
         bool have = false;
 #pragma unroll 1
-        for (int e = 0; e < 32 && c0 + e < A.dv; ++e) {
+        for (int e = 0; e < 16 && c0 + e < A.dv; ++e) {
             const float value = __bfloat162float(v[e]);
             if (finite(value)) continue;
             if (!have) {
@@ -222,7 +222,7 @@ template <int DK, int MODE>
 __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_constant__ ChunkArgs C)
 {
     constexpr bool OUT = MODE != 1;                    // outputs are wanted
-    constexpr int NQ = DK == 64 ? 2 : 1;               // slots for queries
+    constexpr int NK = DK == 64 ? 2 : 1;               // slots for keys
     constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V (or outputs), of the state
     constexpr int SQ = DK / 32;                        // quarters of the TMEM lanes with rows of the state
     extern __shared__ uint8_t smem_raw[];
@@ -250,14 +250,14 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     const int share = OUT ? A.share : 1;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t k_tiles = base, v_tiles = k_tiles + 2 * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + NQ * KT, s_tiles = w_tiles + 3 * VT;
+    const uint32_t k_tiles = base, v_tiles = k_tiles + NK * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + 2 * KT, s_tiles = w_tiles + 3 * VT;
     const uint32_t o_tile = s_tiles + ST;
     uint8_t* const k_mem = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t *const v_mem = k_mem + 2 * KT, *const w_mem = v_mem + 2 * VT + NQ * KT, *const s_mem = w_mem + 3 * VT, *const o_mem = s_mem + ST;
+    uint8_t *const v_mem = k_mem + NK * KT, *const w_mem = v_mem + 2 * VT + 2 * KT, *const s_mem = w_mem + 3 * VT, *const o_mem = s_mem + ST;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
-    const uint32_t scored = bar(20), weighed = bar(21), far_full = bar(22), near_full = bar(23), taken = bar(24);
-    const uint32_t parted = bar(25), stated = bar(26), state_free = bar(27), cleaned = bar(28), summed = bar(29);
+    const uint32_t scored = bar(20), weighed = bar(21), answered = bar(22), taken = bar(24);
+    const uint32_t parted = bar(25), cleaned = bar(26), summed = bar(27), stated = bar(28);
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int i = 0; i < 2; ++i) {
@@ -270,18 +270,16 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         }
         for (int i = 0; i < kDecays; ++i) {
             mbar_init(d_full + 8 * i, 1);
-            mbar_init(d_empty + 8 * i, kStateWarps + (OUT ? kOutWarps : 0));
+            mbar_init(d_empty + 8 * i, kWorkers);
         }
         mbar_init(scored, 1);                          // scores are in TMEM
-        mbar_init(weighed, kOutWarps);                 // P is in TMEM
-        mbar_init(far_full, 1);                        // the far part of the outputs is in TMEM
-        mbar_init(near_full, 1);                       // the near part
-        mbar_init(taken, kOutWarps);                   // both have been read
-        mbar_init(parted, kStateWarps);                // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
-        mbar_init(stated, kStateWarps);                // the state's parts are in shared memory
-        mbar_init(state_free, 1);                      // ... and have been read
+        mbar_init(weighed, kWorkers);                 // P is in TMEM
+        mbar_init(answered, 1);                        // both parts of the outputs are in TMEM
+        mbar_init(taken, kWorkers);                   // ... and have been read
+        mbar_init(parted, kWorkers);                   // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
+        mbar_init(stated, kWorkers);                   // the state is in shared memory
         mbar_init(summed, 1);                          // the chunk's sums are on top of the state, V' has been read
-        mbar_init(cleaned, kStateWarps);                // rows behind the last frame are zeroed
+        mbar_init(cleaned, kWorkers);                // rows behind the last frame are zeroed
         mbar_init_done();
     }
     if (warp == 3) tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -302,8 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             uint32_t n = 0;                            // steps: chunks x heads
             auto frame = [&](int c) { return (int)(f0 + (int64_t)c * kChunk); };
             auto load_q = [&](int c, int h) {
-                const uint32_t s = n % NQ, b = q_full + 8 * s;
-                ok = ok && mbar_wait(q_empty + 8 * s, ((n / NQ) & 1) ^ 1, gave_up);
+                const uint32_t s = n & 1, b = q_full + 8 * s;
+                ok = ok && mbar_wait(q_empty + 8 * s, ((n >> 1) & 1) ^ 1, gave_up);
                 if (!ok) return;
                 mbar_expect_tx(b, KT);
 #pragma unroll
@@ -311,17 +309,20 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ++n;
             };
             for (int c = 0; c < chunks && ok; ++c) {
-                const uint32_t s = c & 1;
-                ok = mbar_wait(k_empty + 8 * s, ((c >> 1) & 1) ^ 1, gave_up);
+                const uint32_t vs = c & 1, ks = c % NK;
+                ok = mbar_wait(v_empty + 8 * vs, ((c >> 1) & 1) ^ 1, gave_up);
                 if (!ok) break;
-                mbar_expect_tx(k_full + 8 * s, KT);
-#pragma unroll
-                for (int p = 0; p < DK / 64; ++p) tma_load_4d(k_tiles + s * KT + p * 16384, &C.k_map, k_full + 8 * s, p * 64, it.g, (int)it.span.b, frame(c));
-                ok = mbar_wait(v_empty + 8 * s, ((c >> 1) & 1) ^ 1, gave_up);
-                if (!ok) break;
-                mbar_expect_tx(v_full + 8 * s, VT);
-                tma_load_4d(v_tiles + s * VT, &C.v_map, v_full + 8 * s, it.c0, it.g, (int)it.span.b, frame(c));
+                mbar_expect_tx(v_full + 8 * vs, VT);
+                tma_load_4d(v_tiles + vs * VT, &C.v_map, v_full + 8 * vs, it.c0, it.g, (int)it.span.b, frame(c));
                 if (OUT) load_q(c, 0);
+                ok = ok && mbar_wait(k_empty + 8 * ks, ((c / NK) & 1) ^ 1, gave_up);
+                if (!ok) break;
+                mbar_expect_tx(k_full + 8 * ks, KT);
+#pragma unroll
+                for (int p = 0; p < DK / 64; ++p) {
+                    tma_load_4d(k_tiles + ks * KT + p * 16384, &C.k_map, k_full + 8 * ks, p * 64, it.g, (int)it.span.b, frame(c));
+                    if (NK == 1 && c + 1 < chunks) tma_prefetch_4d(&C.k_map, p * 64, it.g, (int)it.span.b, frame(c + 1));
+                }
                 for (int h = 1; h < share && OUT; ++h) load_q(c, h);
             }
             if (!ok)                                   // what was asked for still has to land
@@ -339,13 +340,13 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             uint32_t n = 0;
             // Scores of step m, the first of chunk c's if h is 0.
             auto scores = [&](uint32_t m, int c, int h) {
-                const uint32_t q_at = q_tiles + (m % NQ) * KT, k_at = k_tiles + (c & 1) * KT;
+                const uint32_t q_at = q_tiles + (m & 1) * KT, k_at = k_tiles + (c % NK) * KT;
                 if (h == 0) {
-                    ok = ok && mbar_wait(k_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+                    ok = ok && mbar_wait(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
                     if (clean && c + 1 == chunks) ok = ok && mbar_wait(cleaned, 0, gave_up);
                 }
                 if (OUT) {
-                    ok = ok && mbar_wait(q_full + 8 * (m % NQ), (m / NQ) & 1, gave_up);
+                    ok = ok && mbar_wait(q_full + 8 * (m & 1), (m >> 1) & 1, gave_up);
                     if (!ok) return;
                     tc_fence_after();
 #pragma unroll
@@ -356,12 +357,19 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             };
             scores(0, 0, 0);
             for (int c = 0; c < chunks && ok; ++c) {
-                const uint32_t k_at = k_tiles + (c & 1) * KT, v_at = v_tiles + (c & 1) * VT;
+                const uint32_t k_at = k_tiles + (c % NK) * KT, v_at = v_tiles + (c & 1) * VT;
                 const int steps = ((c + 1 == chunks ? tail : kChunk) + 15) / 16;        // of 16 frames
+                // the state first: the next chunk waits for it
+                ok = mbar_wait(parted, c & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                for (int k = 0; k < steps; ++k)
+                    mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + k * 2048, VT), i_state, 1);
+                tc_commit(summed);
+                if (share == 1) tc_commit(k_empty + 8 * (c % NK));
                 for (int h = 0; h < share && ok; ++h, ++n) {
                     if (OUT) {
-                        // the far part ahead of the state's sums: the queries of the next step come in meanwhile, and the weights of this one are worked out
-                        const uint32_t q_at = q_tiles + (n % NQ) * KT;
+                        const uint32_t q_at = q_tiles + (n & 1) * KT;
                         if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
                         ok = ok && mbar_wait(taken, (n & 1) ^ 1, gave_up);
                         if (!ok) break;
@@ -369,30 +377,17 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
 #pragma unroll
                         for (int k = 0; k < DK / 16; ++k)
                             mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, 0), i_far, k > 0);
-                        tc_commit(q_empty + 8 * (n % NQ));
-                        tc_commit(far_full);
-                        if (h + 1 == share) tc_commit(state_free);
-                    }
-                    if (h == 0) {
-                        ok = mbar_wait(parted, c & 1, gave_up);
-                        if (!ok) break;
-                        tc_fence_after();
-                        for (int k = 0; k < steps; ++k)
-                            mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + k * 2048, VT), i_state, 1);
-                        tc_commit(summed);
-                        if (share == 1) tc_commit(k_empty + 8 * (c & 1));
-                    }
-                    if (OUT) {
+                        tc_commit(q_empty + 8 * (n & 1));
                         ok = mbar_wait(weighed, n & 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
                         for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kWeights + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
-                        tc_commit(near_full);
+                        tc_commit(answered);
                     }
                     if (h + 1 == share) tc_commit(v_empty + 8 * (c & 1));
                     if (h + 1 < share) {
                         scores(n + 1, c, h + 1);
-                        if (h + 2 == share) tc_commit(k_empty + 8 * (c & 1));
+                        if (h + 2 == share) tc_commit(k_empty + 8 * (c % NK));
                     } else if (c + 1 < chunks) {
                         scores(n + 1, c + 1, 0);
                     }
@@ -466,30 +461,74 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             if (lane == 0) mbar_arrive(d_full + 8 * slot);
         }
         if (MODE == 1 && lane == 0 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
-    } else if (warp >= 4 && warp < 4 + kStateWarps) {
-        // The state, and V'.  A thread has half (32 columns) of a row of each.
-        const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane, j0 = it.c0 + u * 32;
-        const uint32_t at = tmem + kState + ((uint32_t)(w * 32) << 16) + u * 32;
+    } else if (warp >= 4) {
+        // A worker has 32 rows (those of its quarter w of the TMEM lanes) and a quarter u of the columns of everything: frames' rows of V', of the scores and of the
+        // outputs, rows of the state.  All of them do the same at the same time: warps with roles of their own, each with a loop of a few hundred
+        // instructions, waited for instructions a third of their time (4096 frames, 148 CTAs of DK = 128: 128 us, so ...).  While the tensor pipe sums a chunk's
+        // state they do the outputs of the step before, the weights of this one and the parts of the next chunk's values.
+        const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane, j0 = it.c0 + u * 16;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const bool holds = w < SQ;                     // rows of the state
+        const bool leads = warp == 4 && lane == 0;
         const Pair minus = pair(-1.0f, -1.0f);
+        const uint32_t place0 = (uint32_t)i * 128u + (((uint32_t)(2 * u) ^ (i & 7)) << 4), place1 = (uint32_t)i * 128u + (((uint32_t)(2 * u + 1) ^ (i & 7)) << 4);
+        uint32_t n = 0;                                // steps: chunks x heads
+        // Outputs of the step before.
+        auto output = [&](int c, int h) {
+            const Decays& D = decays[c % kDecays];
+            if (!mbar_wait_warp(answered, (n - 1) & 1, gave_up)) return false;
+            tc_fence_after();
+            uint32_t a[16], x[16], z[8];
+            tc_ld(tmem + lanes + kFar + u * 16, tmem + lanes + kNear + u * 16, a, x);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(taken);
+            const float r = D.row[i] * A.scale;
+            const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = round_bf16(fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, pair(a[2 * e], a[2 * e + 1]))));
+            const uint4* odds = reinterpret_cast<const uint4*>(D.odd);
+            const uint4 o0 = odds[0], o1 = odds[1], o2 = odds[2], o3 = odds[3];
+            const bool odd = o0.x | o0.y | o0.z | o0.w | o1.x | o1.y | o1.z | o1.w | o2.x | o2.y | o2.z | o2.w | o3.x | o3.y | o3.z | o3.w;
+            if (C.out_copies && !odd && !(clean && c + 1 == chunks)) {
+                // through shared memory: a thread's own stores would be 32 bytes of a row each
+                if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * kWorkers) : "memory");
+                *reinterpret_cast<uint4*>(o_mem + place0) = make_uint4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<uint4*>(o_mem + place1) = make_uint4(z[4], z[5], z[6], z[7]);
+                fence_async_shared();
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * kWorkers) : "memory");
+                if (leads) tma_store_4d(&C.out_map, o_tile, it.c0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk));
+            } else if (i < (c + 1 == chunks ? tail : kChunk)) {
+                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + (int64_t)c * kChunk + i) * A.so.frame +
+                                    ((int64_t)it.g * A.share + h) * A.so.head + j0;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (j0 + e < A.dv) to[e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
+                if (odd) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
+            }
+            __syncwarp();
+            return true;
+        };
         bool ok = true;
-        for (int c = 0; c <= chunks; ++c) {
-            const int slot = c % kDecays;
+        for (int c = 0; c <= chunks && ok; ++c) {
+            const int slot = c % kDecays, frames = c + 1 == chunks ? tail : kChunk;
             Decays& D = decays[slot];
-            uint32_t a[16], b[16], d[16];              // parts of V'
-            uint8_t* const parts = w_mem + i * 128;
+            uint32_t a[8], b[8], d[8];                 // parts of V'
             if (c < chunks) {
-                uint8_t* row = v_mem + (c & 1) * VT + i * 128;
+                uint8_t* const v = v_mem + (c & 1) * VT;
                 ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
                 if (!ok) break;
                 if (clean && c + 1 == chunks) {
-                    ok = mbar_wait_warp(k_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+                    ok = mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
                     if (!ok) break;
                     if (i >= tail) {
-                        for (int x = 4 * u; x < 4 * u + 4; ++x) {
-                            const uint32_t place = ((uint32_t)x ^ (i & 7)) << 4;
-                            *reinterpret_cast<uint4*>(row + place) = make_uint4(0, 0, 0, 0);
-                            for (int p = 0; p < DK / 64; ++p) *reinterpret_cast<uint4*>(k_mem + (c & 1) * KT + p * 16384 + i * 128 + place) = make_uint4(0, 0, 0, 0);
+                        const uint4 none = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4*>(v + place0) = none;
+                        *reinterpret_cast<uint4*>(v + place1) = none;
+                        for (int p = 0; p < DK / 64; ++p) {
+                            *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + place0) = none;
+                            *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + place1) = none;
                         }
                     }
                     fence_async_shared();
@@ -501,32 +540,31 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 const Pair weight = pair(D.rest[i], D.rest[i]);
                 __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);  // NaN as soon as a value is not finite
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint32_t place = ((uint32_t)(4 * u + x) ^ (i & 7)) << 4;
-                    const uint4 v = *reinterpret_cast<const uint4*>(row + place);
-                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                for (int q = 0; q < 2; ++q) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(v + (q ? place1 : place0));
+                    const uint32_t in[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
                         Pair y = mul2(widen_bf16(in[e]), weight);
-                        a[4 * x + e] = round_bf16(y);
-                        y = fma2(widen_bf16(a[4 * x + e]), minus, y);
-                        b[4 * x + e] = round_bf16(y);
-                        d[4 * x + e] = round_bf16(fma2(widen_bf16(b[4 * x + e]), minus, y));
+                        a[4 * q + e] = round_bf16(y);
+                        y = fma2(widen_bf16(a[4 * q + e]), minus, y);
+                        b[4 * q + e] = round_bf16(y);
+                        d[4 * q + e] = round_bf16(fma2(widen_bf16(b[4 * q + e]), minus, y));
                     }
                 }
                 if (OUT) {
                     uint32_t cols = 0;
                     if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
 #pragma unroll 1
-                        for (int e = 0; e < 32; ++e) {
-                            uint16_t* p = reinterpret_cast<uint16_t*>(row + (((uint32_t)(4 * u + e / 8) ^ (i & 7)) << 4)) + (e & 7);
+                        for (int e = 0; e < 16; ++e) {
+                            uint16_t* p = reinterpret_cast<uint16_t*>(v + (e < 8 ? place0 : place1)) + (e & 7);
                             const bool is = (*p & 0x7F80u) == 0x7F80u;
                             if (is) *p = 0;
                             if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
                         }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {                   // the first part says what has to be said; what is left over is NaN
+                        for (int e = 0; e < 8; ++e) {                    // the first part says what has to be said; what is left over is NaN
                             const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
                             b[e] &= keep;
                             d[e] &= keep;
@@ -541,188 +579,135 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 tc_fence_after();
             }
             if (c < chunks) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    uint8_t* to = parts + (((uint32_t)(4 * u + x) ^ (i & 7)) << 4);
-                    *reinterpret_cast<uint4*>(to) = make_uint4(a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3]);
-                    *reinterpret_cast<uint4*>(to + VT) = make_uint4(b[4 * x], b[4 * x + 1], b[4 * x + 2], b[4 * x + 3]);
-                    *reinterpret_cast<uint4*>(to + 2 * VT) = make_uint4(d[4 * x], d[4 * x + 1], d[4 * x + 2], d[4 * x + 3]);
-                }
-                if (OUT && c > 0) {
-                    ok = mbar_wait_warp(state_free, (c - 1) & 1, gave_up);
-                    if (!ok) break;
-                }
+                *reinterpret_cast<uint4*>(w_mem + place0) = make_uint4(a[0], a[1], a[2], a[3]);
+                *reinterpret_cast<uint4*>(w_mem + place1) = make_uint4(a[4], a[5], a[6], a[7]);
+                *reinterpret_cast<uint4*>(w_mem + VT + place0) = make_uint4(b[0], b[1], b[2], b[3]);
+                *reinterpret_cast<uint4*>(w_mem + VT + place1) = make_uint4(b[4], b[5], b[6], b[7]);
+                *reinterpret_cast<uint4*>(w_mem + 2 * VT + place0) = make_uint4(d[0], d[1], d[2], d[3]);
+                *reinterpret_cast<uint4*>(w_mem + 2 * VT + place1) = make_uint4(d[4], d[5], d[6], d[7]);
             }
+            uint32_t part[8];                          // the state, rounded
             if (holds) {
-                const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
-                float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
-                const Pair whole = c < chunks ? pair(D.whole, D.whole) : 0;
-                const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+                Pair y[8];                             // the state that enters the chunk: the sum of what its three parts have become
+                const uint32_t at = tmem + kState + lanes + u * 16;
+                if (c > 0) {
+                    uint32_t x0[16], x1[16], x2[16];
+                    tc_ld(at, at + kCols, at + 2 * kCols, x0, x1, x2);
 #pragma unroll
-                for (int m = 0; m < 32; m += 16) {
-                    const int j = j0 + m;
-                    Pair y[8];                         // the state that enters the chunk: the sum of what its three parts have become
-                    if (c > 0) {
-                        uint32_t x0[16], x1[16], x2[16];
-                        tc_ld(at + m, at + kCols + m, at + 2 * kCols + m, x0, x1, x2);
+                    for (int e = 0; e < 8; ++e)
+                        y[e] = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
+                } else {
+                    const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
+                    const bool there = from && i < A.dk;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            y[e] = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
-                    } else {
+                    for (int e = 0; e < 8; ++e)
+                        y[e] = pair(there && j0 + 2 * e < A.dv ? from[j0 + 2 * e] : 0.0f, there && j0 + 2 * e + 1 < A.dv ? from[j0 + 2 * e + 1] : 0.0f);
+                }
+                if (c < chunks) {
+                    const Pair whole = pair(D.whole, D.whole);
+                    uint32_t x[16];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const bool there = from && i < A.dk;
-                            y[e] = pair(there && j + 2 * e < A.dv ? from[j + 2 * e] : 0.0f, there && j + 2 * e + 1 < A.dv ? from[j + 2 * e + 1] : 0.0f);
-                        }
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 z = split(mul2(y[e], whole));
+                        x[2 * e] = __float_as_uint(z.x);
+                        x[2 * e + 1] = __float_as_uint(z.y);
                     }
-                    if (c < chunks) {
-                        uint32_t x[16];
-                        if (OUT) {
-                            uint8_t* part = s_mem + i * 128;
-                            const int q = 4 * u + m / 8;
-                            *reinterpret_cast<uint4*>(part + (((uint32_t)q ^ (i & 7)) << 4)) = make_uint4(round_bf16(y[0]), round_bf16(y[1]), round_bf16(y[2]), round_bf16(y[3]));
-                            *reinterpret_cast<uint4*>(part + (((uint32_t)(q + 1) ^ (i & 7)) << 4)) = make_uint4(round_bf16(y[4]), round_bf16(y[5]), round_bf16(y[6]), round_bf16(y[7]));
-                        }
+                    const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+                    tc_st(at, x);
+                    tc_st(at + kCols, none);
+                    tc_st(at + 2 * kCols, none);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float2 z = split(mul2(y[e], whole));
-                            x[2 * e] = __float_as_uint(z.x);
-                            x[2 * e + 1] = __float_as_uint(z.y);
-                        }
-                        tc_st(at + m, x);
-                        tc_st(at + kCols + m, none);
-                        tc_st(at + 2 * kCols + m, none);
-                    } else if (to && i < A.dk) {
-                        if (j + 16 <= A.dv && !((uintptr_t)(to + j) & 15)) {
+                    for (int e = 0; e < 8; ++e) part[e] = round_bf16(y[e]);
+                    tc_wait_st();
+                } else {
+                    float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
+                    if (to && i < A.dk) {
+                        if (j0 + 16 <= A.dv && !((uintptr_t)(to + j0) & 15)) {
 #pragma unroll
                             for (int e = 0; e < 8; e += 2) {
                                 const float2 z0 = split(y[e]), z1 = split(y[e + 1]);
-                                *reinterpret_cast<float4*>(to + j + 2 * e) = make_float4(z0.x, z0.y, z1.x, z1.y);
+                                *reinterpret_cast<float4*>(to + j0 + 2 * e) = make_float4(z0.x, z0.y, z1.x, z1.y);
                             }
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
                                 const float2 z = split(y[e]);
-                                if (j + 2 * e < A.dv) to[j + 2 * e] = z.x;
-                                if (j + 2 * e + 1 < A.dv) to[j + 2 * e + 1] = z.y;
+                                if (j0 + 2 * e < A.dv) to[j0 + 2 * e] = z.x;
+                                if (j0 + 2 * e + 1 < A.dv) to[j0 + 2 * e + 1] = z.y;
                             }
                         }
                     }
-                    __syncwarp();
                 }
-                tc_wait_st();
             }
-            if (c == chunks) break;
+            if (c == chunks) {
+                __syncwarp();
+                if (OUT) output(c - 1, share - 1);
+                break;
+            }
             fence_async_shared();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(parted);
-                if (OUT) mbar_arrive(stated);
-                mbar_arrive(d_empty + 8 * slot);
+            if (lane == 0) mbar_arrive(parted);
+            if (!OUT) {
+                if (lane == 0) mbar_arrive(d_empty + 8 * slot);
+                continue;
             }
-        }
-    } else if (OUT && warp >= 4) {
-        // Scores -> P, and outputs.  A thread has half of a frame's row: 64 columns of the scores, 32 of the outputs.
-        const int w = warp & 3, half = (warp - 4 - kStateWarps) >> 2, i = w * 32 + lane, j0 = it.c0 + half * 32;
-        const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + i) * A.so.frame + (int64_t)it.g * A.share * A.so.head + j0;
-        const int left = A.dv - j0;                    // columns that there are
-        const bool leads = warp == 4 + kStateWarps && lane == 0;
-        uint32_t n = 0;
-        bool ok = true;
-        for (int c = 0; c < chunks && ok; ++c, out += kChunk * A.so.frame) {
-            const int slot = c % kDecays, frames = c + 1 == chunks ? tail : kChunk;
-            const Decays& D = decays[slot];
-            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
-            if (!ok) break;
             for (int h = 0; h < share; ++h, ++n) {
+                if (n > 0) {
+                    ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1);
+                    if (!ok) break;
+                    if (h == 0 && lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
+                }
+                if (h == 0) {                          // (the products that read the state before have been waited for with the outputs)
+                    if (holds) {
+                        *reinterpret_cast<uint4*>(s_mem + place0) = make_uint4(part[0], part[1], part[2], part[3]);
+                        *reinterpret_cast<uint4*>(s_mem + place1) = make_uint4(part[4], part[5], part[6], part[7]);
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(stated);
+                }
                 ok = mbar_wait_warp(scored, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
+                // scores -> P: eight columns of every 32, so that all workers of a quarter have a share of the diagonal's
+                const float hi = D.hi[i], lo = D.lo[i];
 #pragma unroll 1
-                for (int u = 2 * half; u < 2 * half + 2 && u * 32 < frames; ++u) {         // 32 columns at a time
-                    uint32_t p[16];
-                    if (u > w) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) p[e] = 0;
-                    } else {
-                        const float hi = D.hi[i], lo = D.lo[i];
-                        uint32_t s[32];
-                        tc_ld(tmem + kScores + lanes + u * 32, s);
-                        if (u < w) {
-                            const float r = exp2_fast((hi - D.hi[u * 32 + 31]) + (lo - D.lo[u * 32 + 31]));
+                for (int m = 0; m * 32 < frames; ++m) {
+                    const int c0 = m * 32 + u * 8;
+                    uint32_t p[4] = {0, 0, 0, 0};
+                    if (m <= w) {
+                        uint32_t s[8];
+                        tc_ld(tmem + kScores + lanes + c0, s);
+                        if (m < w) {
+                            const float r = exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31]));
                             const Pair row = pair(r, r);
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const ulonglong2 col = *reinterpret_cast<const ulonglong2*>(&D.col[u * 32 + 2 * e]);
-                                p[e] = round_bf16(mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, col.x)));
-                                p[e + 1] = round_bf16(mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, col.y)));
-                            }
+                            const ulonglong2 g0 = *reinterpret_cast<const ulonglong2*>(&D.col[c0]), g1 = *reinterpret_cast<const ulonglong2*>(&D.col[c0 + 4]);
+                            p[0] = round_bf16(mul2(pair(s[0], s[1]), mul2(row, g0.x)));
+                            p[1] = round_bf16(mul2(pair(s[2], s[3]), mul2(row, g0.y)));
+                            p[2] = round_bf16(mul2(pair(s[4], s[5]), mul2(row, g1.x)));
+                            p[3] = round_bf16(mul2(pair(s[6], s[7]), mul2(row, g1.y)));
                         } else {
-                            const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo), minus = pair(-1.0f, -1.0f);
+                            const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo);
+                            const int far = lane - u * 8;                // columns up to the diagonal
 #pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const ulonglong2 ch = *reinterpret_cast<const ulonglong2*>(&D.hi[u * 32 + 2 * e]), cl = *reinterpret_cast<const ulonglong2*>(&D.lo[u * 32 + 2 * e]);
-                                const float2 g0 = split(add2(fma2(ch.x, minus, hi2), fma2(cl.x, minus, lo2))), g1 = split(add2(fma2(ch.y, minus, hi2), fma2(cl.y, minus, lo2)));
-                                const float2 z0 = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g0.x), exp2_fast(g0.y))));
-                                const float2 z1 = split(mul2(pair(s[2 * e + 2], s[2 * e + 3]), pair(exp2_fast(g1.x), exp2_fast(g1.y))));
-                                p[e] = round_bf16(pair(2 * e <= lane ? z0.x : 0.0f, 2 * e + 1 <= lane ? z0.y : 0.0f));
-                                p[e + 1] = round_bf16(pair(2 * e + 2 <= lane ? z1.x : 0.0f, 2 * e + 3 <= lane ? z1.y : 0.0f));
+                            for (int e = 0; e < 4; ++e) {
+                                const Pair gh = *reinterpret_cast<const Pair*>(&D.hi[c0 + 2 * e]), gl = *reinterpret_cast<const Pair*>(&D.lo[c0 + 2 * e]);
+                                const float2 g = split(add2(fma2(gh, minus, hi2), fma2(gl, minus, lo2)));
+                                const float2 z = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g.x), exp2_fast(g.y))));
+                                p[e] = round_bf16(pair(2 * e <= far ? z.x : 0.0f, 2 * e + 1 <= far ? z.y : 0.0f));
                             }
                         }
                     }
-                    tc_st(tmem + kWeights + lanes + u * 16, p);
+                    tc_st(tmem + kWeights + lanes + m * 16 + u * 4, p);
                 }
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(weighed);
-                ok = mbar_wait_warp(far_full, n & 1, gave_up) && mbar_wait_warp(near_full, n & 1, gave_up);
-                if (!ok) break;
-                tc_fence_after();
-                const float r = D.row[i] * A.scale;
-                const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
-                const uint32_t at = tmem + lanes + half * 32;
-                uint32_t z[16];
-#pragma unroll
-                for (int m = 0; m < 32; m += 16) {
-                    uint32_t a[16], x[16];
-                    tc_ld(at + kFar + m, at + kNear + m, a, x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        z[m / 2 + e] = round_bf16(fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, pair(a[2 * e], a[2 * e + 1]))));
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(taken);
-                const uint4 odd0 = *reinterpret_cast<const uint4*>(&D.odd[0]), odd1 = *reinterpret_cast<const uint4*>(&D.odd[4]);
-                const bool odd = odd0.x | odd0.y | odd0.z | odd0.w | odd1.x | odd1.y | odd1.z | odd1.w;
-                if (C.out_copies && !odd && !(clean && c + 1 == chunks)) {
-                    // through shared memory: a thread's stores would be 64 bytes of a row each
-                    if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    asm volatile("bar.sync 1, 256;" ::: "memory");
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        *reinterpret_cast<uint4*>(o_mem + i * 128 + (((uint32_t)(4 * half + q) ^ (i & 7)) << 4)) = make_uint4(z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]);
-                    fence_async_shared();
-                    asm volatile("bar.sync 1, 256;" ::: "memory");
-                    if (leads) tma_store_4d(&C.out_map, o_tile, it.c0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk));
-                    __syncwarp();
-                } else {
-                    __nv_bfloat16* to = out + h * A.so.head;
-                    if (i < frames) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (e < left) to[e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
-                        if (odd) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
-                    }
-                    __syncwarp();
-                }
             }
-            if (lane == 0) mbar_arrive(d_empty + 8 * slot);
         }
-        if (leads) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (OUT && leads) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -788,8 +773,8 @@ bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, in
 template <int DK, int MODE>
 cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 {
-    constexpr int NQ = DK == 64 ? 2 : 1;
-    constexpr int smem = 1024 + 2 * DK * 256 + 2 * kCols * 256 + NQ * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256;
+    constexpr int NK = DK == 64 ? 2 : 1;
+    constexpr int smem = 1024 + NK * DK * 256 + 2 * kCols * 256 + 2 * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256;
     const cudaError_t e = cudaFuncSetAttribute(sr_chunks_kernel<DK, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
