@@ -469,12 +469,18 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane, j0 = it.c0 + u * 16;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const bool holds = w < SQ;                     // rows of the state
-        const bool leads = warp == 4 && lane == 0;
         const Pair minus = pair(-1.0f, -1.0f);
         const uint32_t place0 = (uint32_t)i * 128u + (((uint32_t)(2 * u) ^ (i & 7)) << 4), place1 = (uint32_t)i * 128u + (((uint32_t)(2 * u + 1) ^ (i & 7)) << 4);
         uint32_t n = 0;                                // steps: chunks x heads
-        // Outputs of the step before.
-        auto output = [&](int c, int h) {
+        uint32_t part[8];                              // the state that enters the chunk, rounded
+        auto state_there = [&] {
+            if (holds) {
+                *reinterpret_cast<uint4*>(s_mem + place0) = make_uint4(part[0], part[1], part[2], part[3]);
+                *reinterpret_cast<uint4*>(s_mem + place1) = make_uint4(part[4], part[5], part[6], part[7]);
+            }
+        };
+        // Outputs of the step before; meanwhile: with them the state for the far products (those that read the one before are done when the outputs are there).
+        auto output = [&](int c, int h, bool meanwhile) {
             const Decays& D = decays[c % kDecays];
             if (!mbar_wait_warp(answered, (n - 1) & 1, gave_up)) return false;
             tc_fence_after();
@@ -490,15 +496,14 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             const uint4* odds = reinterpret_cast<const uint4*>(D.odd);
             const uint4 o0 = odds[0], o1 = odds[1], o2 = odds[2], o3 = odds[3];
             const bool odd = o0.x | o0.y | o0.z | o0.w | o1.x | o1.y | o1.z | o1.w | o2.x | o2.y | o2.z | o2.w | o3.x | o3.y | o3.z | o3.w;
-            if (C.out_copies && !odd && !(clean && c + 1 == chunks)) {
-                // through shared memory: a thread's own stores would be 32 bytes of a row each
-                if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                asm volatile("bar.sync 1, %0;" ::"n"(32 * kWorkers) : "memory");
-                *reinterpret_cast<uint4*>(o_mem + place0) = make_uint4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<uint4*>(o_mem + place1) = make_uint4(z[4], z[5], z[6], z[7]);
-                fence_async_shared();
-                asm volatile("bar.sync 1, %0;" ::"n"(32 * kWorkers) : "memory");
-                if (leads) tma_store_4d(&C.out_map, o_tile, it.c0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk));
+            const bool copies = C.out_copies && !odd && !(clean && c + 1 == chunks);
+            if (copies) {
+                // through shared memory, every warp its own box: a thread's stores would be 32 bytes of a row each
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();
+                uint8_t* to = o_mem + (warp - 4) * 1024 + lane * 32;
+                *reinterpret_cast<uint4*>(to) = make_uint4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<uint4*>(to + 16) = make_uint4(z[4], z[5], z[6], z[7]);
             } else if (i < (c + 1 == chunks ? tail : kChunk)) {
                 __nv_bfloat16* to = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + (int64_t)c * kChunk + i) * A.so.frame +
                                     ((int64_t)it.g * A.share + h) * A.so.head + j0;
@@ -507,7 +512,13 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     if (j0 + e < A.dv) to[e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
                 if (odd) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
             }
+            if (meanwhile) state_there();
+            fence_async_shared();
             __syncwarp();
+            if (lane == 0) {
+                if (meanwhile) mbar_arrive(stated);
+                if (copies) tma_store_4d(&C.out_map, o_tile + (warp - 4) * 1024, j0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk + w * 32));
+            }
             return true;
         };
         bool ok = true;
@@ -586,7 +597,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 *reinterpret_cast<uint4*>(w_mem + 2 * VT + place0) = make_uint4(d[0], d[1], d[2], d[3]);
                 *reinterpret_cast<uint4*>(w_mem + 2 * VT + place1) = make_uint4(d[4], d[5], d[6], d[7]);
             }
-            uint32_t part[8];                          // the state, rounded
             if (holds) {
                 Pair y[8];                             // the state that enters the chunk: the sum of what its three parts have become
                 const uint32_t at = tmem + kState + lanes + u * 16;
@@ -641,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             }
             if (c == chunks) {
                 __syncwarp();
-                if (OUT) output(c - 1, share - 1);
+                if (OUT) output(c - 1, share - 1, false);
                 break;
             }
             fence_async_shared();
@@ -654,15 +664,11 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             }
             for (int h = 0; h < share; ++h, ++n) {
                 if (n > 0) {
-                    ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1);
+                    ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1, h == 0);
                     if (!ok) break;
                     if (h == 0 && lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
-                }
-                if (h == 0) {                          // (the products that read the state before have been waited for with the outputs)
-                    if (holds) {
-                        *reinterpret_cast<uint4*>(s_mem + place0) = make_uint4(part[0], part[1], part[2], part[3]);
-                        *reinterpret_cast<uint4*>(s_mem + place1) = make_uint4(part[4], part[5], part[6], part[7]);
-                    }
+                } else {
+                    state_there();
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(stated);
@@ -670,36 +676,46 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ok = mbar_wait_warp(scored, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                // scores -> P: eight columns of every 32, so that all workers of a quarter have a share of the diagonal's
+                // scores -> P: two workers of a quarter have 16 columns of the diagonal's 32 each, the other two 16 of all 32s to its left
                 const float hi = D.hi[i], lo = D.lo[i];
-#pragma unroll 1
-                for (int m = 0; m * 32 < frames; ++m) {
-                    const int c0 = m * 32 + u * 8;
-                    uint32_t p[4] = {0, 0, 0, 0};
-                    if (m <= w) {
-                        uint32_t s[8];
+                const int half = (u & 1) * 16;
+                if (u < 2) {
+                    if (w * 32 < frames) {
+                        const int c0 = w * 32 + half, far = lane - half;         // columns up to the diagonal
+                        const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo);
+                        uint32_t s[16], p[8];
                         tc_ld(tmem + kScores + lanes + c0, s);
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            const ulonglong2 gh = *reinterpret_cast<const ulonglong2*>(&D.hi[c0 + 2 * e]), gl = *reinterpret_cast<const ulonglong2*>(&D.lo[c0 + 2 * e]);
+                            const float2 g0 = split(add2(fma2(gh.x, minus, hi2), fma2(gl.x, minus, lo2))), g1 = split(add2(fma2(gh.y, minus, hi2), fma2(gl.y, minus, lo2)));
+                            const float2 z0 = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g0.x), exp2_fast(g0.y))));
+                            const float2 z1 = split(mul2(pair(s[2 * e + 2], s[2 * e + 3]), pair(exp2_fast(g1.x), exp2_fast(g1.y))));
+                            p[e] = round_bf16(pair(2 * e <= far ? z0.x : 0.0f, 2 * e + 1 <= far ? z0.y : 0.0f));
+                            p[e + 1] = round_bf16(pair(2 * e + 2 <= far ? z1.x : 0.0f, 2 * e + 3 <= far ? z1.y : 0.0f));
+                        }
+                        tc_st(tmem + kWeights + lanes + c0 / 2, p);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int m = 0; m * 32 < frames; ++m) {
+                        const int c0 = m * 32 + half;
+                        uint32_t p[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                        if (m == w) continue;
                         if (m < w) {
+                            uint32_t s[16];
+                            tc_ld(tmem + kScores + lanes + c0, s);
                             const float r = exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31]));
                             const Pair row = pair(r, r);
-                            const ulonglong2 g0 = *reinterpret_cast<const ulonglong2*>(&D.col[c0]), g1 = *reinterpret_cast<const ulonglong2*>(&D.col[c0 + 4]);
-                            p[0] = round_bf16(mul2(pair(s[0], s[1]), mul2(row, g0.x)));
-                            p[1] = round_bf16(mul2(pair(s[2], s[3]), mul2(row, g0.y)));
-                            p[2] = round_bf16(mul2(pair(s[4], s[5]), mul2(row, g1.x)));
-                            p[3] = round_bf16(mul2(pair(s[6], s[7]), mul2(row, g1.y)));
-                        } else {
-                            const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo);
-                            const int far = lane - u * 8;                // columns up to the diagonal
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const Pair gh = *reinterpret_cast<const Pair*>(&D.hi[c0 + 2 * e]), gl = *reinterpret_cast<const Pair*>(&D.lo[c0 + 2 * e]);
-                                const float2 g = split(add2(fma2(gh, minus, hi2), fma2(gl, minus, lo2)));
-                                const float2 z = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g.x), exp2_fast(g.y))));
-                                p[e] = round_bf16(pair(2 * e <= far ? z.x : 0.0f, 2 * e + 1 <= far ? z.y : 0.0f));
+                            for (int e = 0; e < 8; e += 2) {
+                                const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(&D.col[c0 + 2 * e]);
+                                p[e] = round_bf16(mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, g.x)));
+                                p[e + 1] = round_bf16(mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, g.y)));
                             }
                         }
+                        tc_st(tmem + kWeights + lanes + c0 / 2, p);
                     }
-                    tc_st(tmem + kWeights + lanes + m * 16 + u * 4, p);
                 }
                 tc_wait_st();
                 tc_fence_before();
@@ -707,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 if (lane == 0) mbar_arrive(weighed);
             }
         }
-        if (OUT && leads) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (OUT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -752,17 +768,17 @@ __global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant_
     }
 }
 
-// [frames][sequences][heads][size] in boxes of 128 frames x 64 elements.
-bool encode(CUtensorMap* map, const void* data, const sr_attention_strides& st, int64_t size, int64_t heads, int64_t sequences, int64_t frames)
+// [frames][sequences][heads][size] in boxes of 128 frames x 64 elements, or (outputs) of 32 x 16.
+bool encode(CUtensorMap* map, const void* data, const sr_attention_strides& st, int64_t size, int64_t heads, int64_t sequences, int64_t frames, bool out = false)
 {
     const SrEncodeTiled fn = sr_encode_tiled();
     if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)size, (cuuint64_t)heads, (cuuint64_t)sequences, (cuuint64_t)frames};
     auto stride = [](int64_t s, int64_t n) { return (cuuint64_t)(n > 1 ? 2 * s : 16); };
     const cuuint64_t strides[3] = {stride(st.head, heads), stride(st.sequence, sequences), stride(st.frame, frames)};
-    const cuuint32_t box[4] = {64, 1, 1, kChunk}, steps[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {out ? 16u : 64u, 1, 1, out ? 32u : (cuuint32_t)kChunk}, steps[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              out ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, int64_t sequences, int64_t frames)
 {
@@ -870,6 +886,6 @@ cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d,
         !encode(&C.v_map, A.v, A.sv, d->dv, d->groups, sequences, d->frames))
         return cudaErrorInvalidValue;
     C.out_copies = copies_fit(A.out, A.so, d->heads, sequences, d->frames);
-    if (C.out_copies && !encode(&C.out_map, A.out, A.so, d->dv, d->heads, sequences, d->frames)) return cudaErrorInvalidValue;
+    if (C.out_copies && !encode(&C.out_map, A.out, A.so, d->dv, d->heads, sequences, d->frames, true)) return cudaErrorInvalidValue;
     return d->dk <= 64 ? launch_all<64>(C, s) : launch_all<128>(C, s);
 }
