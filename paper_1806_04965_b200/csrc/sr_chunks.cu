@@ -193,10 +193,18 @@ struct alignas(16) Decays {                            // of a chunk (read four 
 };
 static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read as 16-byte words");
 
-// Values that are not finite have been left out of row i of a chunk's near product: their terms for 16 columns, as the formula has them, on top of the
-// stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
-__device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, __nv_bfloat16* out)
+// What follows is out of line: it is rarely run, and the loop that every chunk goes through has to stay small.
+
+// 16 outputs of row i of a chunk, one by one.  odd: values that are not finite have been left out of the chunk's near product; their terms as the formula has
+// them go on top of the stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
+__device__ __noinline__ void store_row(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, bool odd, uint4 lo, uint4 hi)
 {
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + i) * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + c0;
+    const uint32_t z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (c0 + e < A.dv) out[e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
+    if (!odd) return;
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(A.q) + it.span.b * A.sq.sequence + (f0 + i) * A.sq.frame + ((int64_t)it.g * A.share + h) * A.sq.head;
 #pragma unroll 1
     for (int j = 0; j <= i; ++j) {
@@ -215,6 +223,44 @@ __device__ __noinline__ void add_odd_terms(const AttentionArgs& A, const Decays&
             }
             out[e] = __float2bfloat16(__bfloat162float(out[e]) + p * value);
         }
+    }
+}
+// Takes what is not finite out of a thread's 16 values and says in which columns its warp had any.
+__device__ __noinline__ uint32_t clear_odd(uint4* first, uint4* second)
+{
+    uint32_t cols = 0;
+#pragma unroll 1
+    for (int e = 0; e < 16; ++e) {
+        uint16_t* p = reinterpret_cast<uint16_t*>(e < 8 ? first : second) + (e & 7);
+        const bool is = (*p & 0x7F80u) == 0x7F80u;
+        if (is) *p = 0;
+        if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
+    }
+    return cols;
+}
+// 16 values of a state's row between global memory and two TMEM lanes' registers.
+__device__ __noinline__ void load_state(const float* from, int j0, int dv, uint32_t taddr)
+{
+    uint32_t x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = from && j0 + e < dv ? __float_as_uint(from[j0 + e]) : 0u;
+    __syncwarp();
+    tc_st(taddr, x);
+}
+__device__ __noinline__ void store_state(float* to, int j0, int dv, uint32_t taddr)
+{
+    uint32_t x0[16], x1[16], x2[16];
+    tc_ld(taddr, taddr + kCols, taddr + 2 * kCols, x0, x1, x2);
+    if (!to) return;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x0[e] = __float_as_uint(__uint_as_float(x0[e]) + (__uint_as_float(x1[e]) + __uint_as_float(x2[e])));
+    if (j0 + 16 <= dv && !((uintptr_t)(to + j0) & 15)) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j0 + e) = make_uint4(x0[e], x0[e + 1], x0[e + 2], x0[e + 3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (j0 + e < dv) to[j0 + e] = __uint_as_float(x0[e]);
     }
 }
 
@@ -505,12 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 *reinterpret_cast<uint4*>(to) = make_uint4(z[0], z[1], z[2], z[3]);
                 *reinterpret_cast<uint4*>(to + 16) = make_uint4(z[4], z[5], z[6], z[7]);
             } else if (i < (c + 1 == chunks ? tail : kChunk)) {
-                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + (int64_t)c * kChunk + i) * A.so.frame +
-                                    ((int64_t)it.g * A.share + h) * A.so.head + j0;
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (j0 + e < A.dv) to[e] = __ushort_as_bfloat16((unsigned short)(e & 1 ? z[e / 2] >> 16 : z[e / 2] & 0xFFFFu));
-                if (odd) add_odd_terms(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, to);
+                store_row(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, odd, make_uint4(z[0], z[1], z[2], z[3]), make_uint4(z[4], z[5], z[6], z[7]));
             }
             if (meanwhile) state_there();
             fence_async_shared();
@@ -521,138 +562,100 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             }
             return true;
         };
+        // Ahead of the first chunk: the state as the first of its three parts, zeros for the others and for the weights behind the diagonal.
+        const uint32_t state = tmem + kState + lanes + u * 16;
+        const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        if (holds) {
+            const float* from = MODE == 1 || i >= A.dk ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
+            load_state(from, j0, A.dv, state);
+            __syncwarp();
+            tc_st(state + kCols, none);
+            tc_st(state + 2 * kCols, none);
+        }
+        if (OUT && u > w) tc_st(tmem + kWeights + lanes + u * 16, none);
+        tc_wait_st();
         bool ok = true;
-        for (int c = 0; c <= chunks && ok; ++c) {
+        for (int c = 0; c < chunks; ++c) {
             const int slot = c % kDecays, frames = c + 1 == chunks ? tail : kChunk;
             Decays& D = decays[slot];
             uint32_t a[8], b[8], d[8];                 // parts of V'
-            if (c < chunks) {
-                uint8_t* const v = v_mem + (c & 1) * VT;
-                ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+            uint8_t* const v = v_mem + (c & 1) * VT;
+            ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+            if (clean && c + 1 == chunks) {
+                ok = ok && mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
                 if (!ok) break;
-                if (clean && c + 1 == chunks) {
-                    ok = mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
-                    if (!ok) break;
-                    if (i >= tail) {
-                        const uint4 none = make_uint4(0, 0, 0, 0);
-                        *reinterpret_cast<uint4*>(v + place0) = none;
-                        *reinterpret_cast<uint4*>(v + place1) = none;
-                        for (int p = 0; p < DK / 64; ++p) {
-                            *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + place0) = none;
-                            *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + place1) = none;
-                        }
-                    }
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(cleaned);
-                }
-                ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
-                if (!ok) break;
-                const Pair weight = pair(D.rest[i], D.rest[i]);
-                __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);  // NaN as soon as a value is not finite
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(v + (q ? place1 : place0));
-                    const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
-                        Pair y = mul2(widen_bf16(in[e]), weight);
-                        a[4 * q + e] = round_bf16(y);
-                        y = fma2(widen_bf16(a[4 * q + e]), minus, y);
-                        b[4 * q + e] = round_bf16(y);
-                        d[4 * q + e] = round_bf16(fma2(widen_bf16(b[4 * q + e]), minus, y));
+                if (i >= tail) {
+                    const uint4 zero = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(v + place0) = zero;
+                    *reinterpret_cast<uint4*>(v + place1) = zero;
+                    for (int p = 0; p < DK / 64; ++p) {
+                        *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + place0) = zero;
+                        *reinterpret_cast<uint4*>(k_mem + (c % NK) * KT + p * 16384 + place1) = zero;
                     }
                 }
-                if (OUT) {
-                    uint32_t cols = 0;
-                    if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
-#pragma unroll 1
-                        for (int e = 0; e < 16; ++e) {
-                            uint16_t* p = reinterpret_cast<uint16_t*>(v + (e < 8 ? place0 : place1)) + (e & 7);
-                            const bool is = (*p & 0x7F80u) == 0x7F80u;
-                            if (is) *p = 0;
-                            if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
-                        }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(cleaned);
+            }
+            ok = ok && mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
+            if (!ok) break;
+            const Pair weight = pair(D.rest[i], D.rest[i]);
+            __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);      // NaN as soon as a value is not finite
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {                    // the first part says what has to be said; what is left over is NaN
-                            const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
-                            b[e] &= keep;
-                            d[e] &= keep;
-                        }
-                    }
-                    if (lane == 0) D.odd[u * 4 + w] = cols;
+            for (int q = 0; q < 2; ++q) {
+                const uint4 x = *reinterpret_cast<const uint4*>(v + (q ? place1 : place0));
+                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (OUT) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&in[e]), __floats2bfloat162_rn(0.0f, 0.0f), odd);
+                    Pair y = mul2(widen_bf16(in[e]), weight);
+                    a[4 * q + e] = round_bf16(y);
+                    y = fma2(widen_bf16(a[4 * q + e]), minus, y);
+                    b[4 * q + e] = round_bf16(y);
+                    d[4 * q + e] = round_bf16(fma2(widen_bf16(b[4 * q + e]), minus, y));
                 }
+            }
+            if (OUT) {
+                uint32_t cols = 0;
+                if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
+                    cols = clear_odd(reinterpret_cast<uint4*>(v + place0), reinterpret_cast<uint4*>(v + place1));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {                        // the first part says what has to be said; what is left over is NaN
+                        const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                        b[e] &= keep;
+                        d[e] &= keep;
+                    }
+                }
+                if (lane == 0) D.odd[u * 4 + w] = cols;
             }
             if (c > 0) {
                 ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
             }
-            if (c < chunks) {
-                *reinterpret_cast<uint4*>(w_mem + place0) = make_uint4(a[0], a[1], a[2], a[3]);
-                *reinterpret_cast<uint4*>(w_mem + place1) = make_uint4(a[4], a[5], a[6], a[7]);
-                *reinterpret_cast<uint4*>(w_mem + VT + place0) = make_uint4(b[0], b[1], b[2], b[3]);
-                *reinterpret_cast<uint4*>(w_mem + VT + place1) = make_uint4(b[4], b[5], b[6], b[7]);
-                *reinterpret_cast<uint4*>(w_mem + 2 * VT + place0) = make_uint4(d[0], d[1], d[2], d[3]);
-                *reinterpret_cast<uint4*>(w_mem + 2 * VT + place1) = make_uint4(d[4], d[5], d[6], d[7]);
-            }
+            *reinterpret_cast<uint4*>(w_mem + place0) = make_uint4(a[0], a[1], a[2], a[3]);
+            *reinterpret_cast<uint4*>(w_mem + place1) = make_uint4(a[4], a[5], a[6], a[7]);
+            *reinterpret_cast<uint4*>(w_mem + VT + place0) = make_uint4(b[0], b[1], b[2], b[3]);
+            *reinterpret_cast<uint4*>(w_mem + VT + place1) = make_uint4(b[4], b[5], b[6], b[7]);
+            *reinterpret_cast<uint4*>(w_mem + 2 * VT + place0) = make_uint4(d[0], d[1], d[2], d[3]);
+            *reinterpret_cast<uint4*>(w_mem + 2 * VT + place1) = make_uint4(d[4], d[5], d[6], d[7]);
             if (holds) {
-                Pair y[8];                             // the state that enters the chunk: the sum of what its three parts have become
-                const uint32_t at = tmem + kState + lanes + u * 16;
-                if (c > 0) {
-                    uint32_t x0[16], x1[16], x2[16];
-                    tc_ld(at, at + kCols, at + 2 * kCols, x0, x1, x2);
+                // the state that enters the chunk is the sum of what its three parts have become
+                uint32_t x0[16], x1[16], x2[16];
+                tc_ld(state, state + kCols, state + 2 * kCols, x0, x1, x2);
+                const Pair whole = pair(D.whole, D.whole);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        y[e] = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
-                } else {
-                    const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
-                    const bool there = from && i < A.dk;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        y[e] = pair(there && j0 + 2 * e < A.dv ? from[j0 + 2 * e] : 0.0f, there && j0 + 2 * e + 1 < A.dv ? from[j0 + 2 * e + 1] : 0.0f);
+                for (int e = 0; e < 8; ++e) {
+                    const Pair y = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
+                    part[e] = round_bf16(y);
+                    const float2 z = split(mul2(y, whole));
+                    x0[2 * e] = __float_as_uint(z.x);
+                    x0[2 * e + 1] = __float_as_uint(z.y);
                 }
-                if (c < chunks) {
-                    const Pair whole = pair(D.whole, D.whole);
-                    uint32_t x[16];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 z = split(mul2(y[e], whole));
-                        x[2 * e] = __float_as_uint(z.x);
-                        x[2 * e + 1] = __float_as_uint(z.y);
-                    }
-                    const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-                    tc_st(at, x);
-                    tc_st(at + kCols, none);
-                    tc_st(at + 2 * kCols, none);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) part[e] = round_bf16(y[e]);
-                    tc_wait_st();
-                } else {
-                    float* to = MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
-                    if (to && i < A.dk) {
-                        if (j0 + 16 <= A.dv && !((uintptr_t)(to + j0) & 15)) {
-#pragma unroll
-                            for (int e = 0; e < 8; e += 2) {
-                                const float2 z0 = split(y[e]), z1 = split(y[e + 1]);
-                                *reinterpret_cast<float4*>(to + j0 + 2 * e) = make_float4(z0.x, z0.y, z1.x, z1.y);
-                            }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float2 z = split(y[e]);
-                                if (j0 + 2 * e < A.dv) to[j0 + 2 * e] = z.x;
-                                if (j0 + 2 * e + 1 < A.dv) to[j0 + 2 * e + 1] = z.y;
-                            }
-                        }
-                    }
-                }
-            }
-            if (c == chunks) {
-                __syncwarp();
-                if (OUT) output(c - 1, share - 1, false);
-                break;
+                tc_st(state, x0);
+                tc_st(state + kCols, none);
+                tc_st(state + 2 * kCols, none);
+                tc_wait_st();
             }
             fence_async_shared();
             tc_fence_before();
@@ -662,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 if (lane == 0) mbar_arrive(d_empty + 8 * slot);
                 continue;
             }
-            for (int h = 0; h < share; ++h, ++n) {
+            for (int h = 0; h < share && ok; ++h, ++n) {
                 if (n > 0) {
                     ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1, h == 0);
                     if (!ok) break;
@@ -698,21 +701,17 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     }
                 } else {
 #pragma unroll 1
-                    for (int m = 0; m * 32 < frames; ++m) {
+                    for (int m = 0; m < w && m * 32 < frames; ++m) {             // (to its right are the zeros of the start)
                         const int c0 = m * 32 + half;
-                        uint32_t p[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                        if (m == w) continue;
-                        if (m < w) {
-                            uint32_t s[16];
-                            tc_ld(tmem + kScores + lanes + c0, s);
-                            const float r = exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31]));
-                            const Pair row = pair(r, r);
+                        uint32_t s[16], p[8];
+                        tc_ld(tmem + kScores + lanes + c0, s);
+                        const float r = exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31]));
+                        const Pair row = pair(r, r);
 #pragma unroll
-                            for (int e = 0; e < 8; e += 2) {
-                                const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(&D.col[c0 + 2 * e]);
-                                p[e] = round_bf16(mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, g.x)));
-                                p[e + 1] = round_bf16(mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, g.y)));
-                            }
+                        for (int e = 0; e < 8; e += 2) {
+                            const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(&D.col[c0 + 2 * e]);
+                            p[e] = round_bf16(mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, g.x)));
+                            p[e + 1] = round_bf16(mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, g.y)));
                         }
                         tc_st(tmem + kWeights + lanes + c0 / 2, p);
                     }
@@ -722,6 +721,17 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(weighed);
             }
+            if (!ok) break;
+        }
+        ok = ok && mbar_wait_warp(summed, (chunks - 1) & 1, gave_up);
+        if (ok) {
+            tc_fence_after();
+            if (holds) {
+                float* to = i >= A.dk ? nullptr : MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
+                store_state(to, j0, A.dv, state);
+                __syncwarp();
+            }
+            if (OUT) output(chunks - 1, share - 1, false);
         }
         if (OUT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
