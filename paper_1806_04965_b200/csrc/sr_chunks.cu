@@ -801,7 +801,8 @@ cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 {
     constexpr int NK = DK == 64 ? 2 : 1;
     constexpr int smem = 1024 + NK * DK * 256 + 2 * kCols * 256 + 2 * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256;
-    const cudaError_t e = cudaFuncSetAttribute(sr_chunks_kernel<DK, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static SrSharedLimit limit;
+    const cudaError_t e = limit.raise(sr_chunks_kernel<DK, MODE>, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

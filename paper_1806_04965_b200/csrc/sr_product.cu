@@ -318,7 +318,8 @@ cudaError_t launch(ProductArgs& P, int sms, cudaStream_t stream)
     using S = Shape<FMT, NT>;
     P.ring = std::min(kMaxStages, (kSmem - 1024) / S::kStage);
     const size_t smem = 1024 + (size_t)P.ring * S::kStage;
-    const cudaError_t e = cudaFuncSetAttribute(sr_product_kernel<FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static SrSharedLimit limit;
+    const cudaError_t e = limit.raise(sr_product_kernel<FMT, NT>, (int)smem);
     if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)P.out_tiles * P.row_tiles;
     cudaLaunchAttribute at[2];

@@ -12,6 +12,7 @@ requires a gradient is refused while gradients are recorded.
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional
 
 import torch
@@ -62,46 +63,34 @@ def _refuse(call: str, why: str):
     raise SrError(1, "%s: %s" % (call, why))
 
 
-def _check(code: int, call: str):
+# The current device and a device's current stream without the objects around them (a call's host time is a few microseconds).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_grad = torch.is_grad_enabled
+
+
+def _call(call: str, device: int, function, *args):
+    """function(*args, stream) with `device` as the current one, on its current stream."""
+    if _current_device() == device:
+        code = function(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            code = function(*args, _raw_stream(device))
     if code:
         raise SrError(code, call)
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
-class _on:
-    """Makes a tensor's device the current one for the calls inside (only where it is not) and gives that device's current stream."""
-    __slots__ = ("index", "before")
-
-    def __init__(self, t):
-        self.index = t.device.index
-
-    def __enter__(self):
-        before = torch.cuda.current_device()
-        self.before = None if before == self.index else before
-        if self.before is not None:
-            torch.cuda.set_device(self.index)
-        return _raw_stream(self.index)
-
-    def __exit__(self, *_):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
-
-
-def _tensors(call: str, first, *others):
-    """All on one CUDA device, none that a gradient is recorded for."""
-    device = first.device
-    if device.type != "cuda":
+def _tensors(call: str, first, *others) -> int:
+    """All on one CUDA device (its index is returned), none that a gradient is recorded for."""
+    device = first.get_device()
+    if device < 0 or not first.is_cuda:
         _refuse(call, "tensors on a CUDA device are required")
-    grad = torch.is_grad_enabled()
-    for t in (first,) + others:
-        if t is None:
-            continue
-        if t.device != device:
+    for t in others:
+        if t is not None and t.get_device() != device:
             _refuse(call, "tensors lie on different devices")
-        if grad and t.requires_grad:
-            _refuse(call, "there is no backward pass (use torch.no_grad() or detach)")
+    if _grad() and (first.requires_grad or any(t is not None and t.requires_grad for t in others)):
+        _refuse(call, "there is no backward pass (use torch.no_grad() or detach)")
+    return device
 
 
 def _float_vector(call: str, name: str, t, n: int):
@@ -142,33 +131,36 @@ class Microscaled:
 
     @classmethod
     def empty(cls, rows: int, cols: int, format: str, device):
+        return cls._like(torch.empty(0, device=device), rows, cols, format)
+
+    @classmethod
+    def _like(cls, x, rows: int, cols: int, format: str):
+        """One without values on x's device."""
         m = cls.__new__(cls)
         if format not in FORMATS:
             _refuse("Microscaled", "format is one of %s" % ", ".join(FORMATS))
-        groups = -(-cols // 32)
-        m.data = torch.empty((rows, groups * (16 if format == "mx4" else 32)), dtype=torch.uint8, device=device)
-        m.scales = torch.empty(-(-rows // 128) * -(-groups // 4) * 512, dtype=torch.uint8, device=device)
+        groups = (cols + 31) // 32
+        m.data = x.new_empty((rows, groups * (16 if format == "mx4" else 32)), dtype=torch.uint8)
+        m.scales = x.new_empty((rows + 127) // 128 * ((groups + 3) // 4) * 512, dtype=torch.uint8)
         m.rows, m.cols, m.format = rows, cols, format
         return m
 
     def values(self):
         """The values it stands for, float32 [rows][cols]."""
-        _tensors("values", self.data, self.scales)
-        out = torch.empty((self.rows, self.cols), dtype=torch.float32, device=self.data.device)
-        with _on(out) as stream:
-            _check(_library().sr_microscale_values(self.data.data_ptr(), self.scales.data_ptr(), FORMATS[self.format], self.rows, self.cols, out.data_ptr(),
-                                                   stream), "sr_microscale_values")
+        device = _tensors("values", self.data, self.scales)
+        out = self.data.new_empty((self.rows, self.cols), dtype=torch.float32)
+        _call("sr_microscale_values", device, _library().sr_microscale_values, self.data.data_ptr(), self.scales.data_ptr(), FORMATS[self.format], self.rows,
+              self.cols, out.data_ptr())
         return out
 
 
 def quantize(x, format: str = "mx4") -> Microscaled:
     """x [rows][cols] (float32 or bfloat16; rows may have gaps between them) in a microscaled format."""
-    _tensors("quantize", x)
+    device = _tensors("quantize", x)
     stride = _rows("quantize", "x", x)
-    m = Microscaled.empty(x.shape[0], x.shape[1], format, x.device)
-    with _on(x) as stream:
-        _check(_library().sr_microscale_quantize(x.data_ptr(), _DTYPES[x.dtype], m.rows, m.cols, stride, FORMATS[format], m.data.data_ptr(),
-                                                 m.scales.data_ptr(), stream), "sr_microscale_quantize")
+    m = Microscaled._like(x, x.shape[0], x.shape[1], format)
+    _call("sr_microscale_quantize", device, _library().sr_microscale_quantize, x.data_ptr(), _DTYPES[x.dtype], m.rows, m.cols, stride, FORMATS[format],
+          m.data.data_ptr(), m.scales.data_ptr())
     return m
 
 
@@ -177,28 +169,26 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
     gaps between them) is written in place of a new tensor of `dtype`."""
     if a.format != w.format or a.cols != w.cols:
         _refuse("product", "both matrices have the same format and number of columns")
-    _tensors("product", a.data, a.scales, w.data, w.scales, bias, out)
+    device = _tensors("product", a.data, a.scales, w.data, w.scales, bias, out)
     b = _float_vector("product", "bias", bias, w.rows)
     if out is None:
         if dtype not in _DTYPES:
             _refuse("product", "the output is float32 or bfloat16")
-        out = torch.empty((a.rows, w.rows), dtype=dtype, device=a.data.device)
+        out = a.data.new_empty((a.rows, w.rows), dtype=dtype)
         stride = w.rows
     else:
         if tuple(out.shape) != (a.rows, w.rows):
             _refuse("product", "out has to be [%d][%d]" % (a.rows, w.rows))
         stride = _rows("product", "out", out) if w.rows else 0
-    with _on(out) as stream:
-        _check(_library().sr_microscale_product(a.data.data_ptr(), a.scales.data_ptr(), w.data.data_ptr(), w.scales.data_ptr(), FORMATS[a.format],
-                                                a.rows, a.cols, w.rows, b, 1 if relu else 0, out.data_ptr(), _DTYPES[out.dtype], stride, stream),
-               "sr_microscale_product")
+    _call("sr_microscale_product", device, _library().sr_microscale_product, a.data.data_ptr(), a.scales.data_ptr(), w.data.data_ptr(), w.scales.data_ptr(),
+          FORMATS[a.format], a.rows, a.cols, w.rows, b, 1 if relu else 0, out.data_ptr(), _DTYPES[out.dtype], stride)
     return out
 
 
 def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, format: Optional[str] = None):
     """s = x + residual, s / sqrt(mean(s^2) + eps) * weight for every row of x [rows][cols].  The output has x's type, or is `Microscaled` where
     a format is given; with a residual the result is (output, s rounded to x's type)."""
-    _tensors("rms_norm", x, weight, residual)
+    device = _tensors("rms_norm", x, weight, residual)
     xs = _rows("rms_norm", "x", x)
     rows, cols = x.shape
     rs, rp, total, tp = 0, None, None, None
@@ -206,17 +196,16 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, format: Optional[
         if residual.shape != x.shape or residual.dtype is not x.dtype:
             _refuse("rms_norm", "the residual has x's shape and type")
         rs, rp = _rows("rms_norm", "residual", residual), residual.data_ptr()
-        total = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        total = x.new_empty((rows, cols))
         tp = total.data_ptr()
     w = _float_vector("rms_norm", "weight", weight, cols)
     if format is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        out = x.new_empty((rows, cols))
         op, code, sp = out.data_ptr(), _DTYPES[x.dtype], None
     else:
-        out = Microscaled.empty(rows, cols, format, x.device)
+        out = Microscaled._like(x, rows, cols, format)
         op, code, sp = out.data.data_ptr(), FORMATS[format], out.scales.data_ptr()
-    with _on(x) as stream:
-        _check(_library().sr_rms_norm(x.data_ptr(), rp, w, eps, _DTYPES[x.dtype], rows, cols, xs, rs, tp, op, code, sp, stream), "sr_rms_norm")
+    _call("sr_rms_norm", device, _library().sr_rms_norm, x.data_ptr(), rp, w, eps, _DTYPES[x.dtype], rows, cols, xs, rs, tp, op, code, sp)
     return out if residual is None else (out, total)
 
 
@@ -224,9 +213,9 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, format: Optional[
 _descs: dict = {}
 
 
-def _desc(call: str, q, k, v, log_decay, out_strides, packed: bool, step: bool, batch: int, scale: float):
+def _desc(call: str, device: int, q, k, v, log_decay, packed: bool, step: bool, batch: int, scale: float):
     key = (q.dtype, k.dtype, v.dtype, log_decay.dtype, q.shape, k.shape, v.shape, log_decay.shape, q.stride(), k.stride(), v.stride(), log_decay.stride(),
-           out_strides, packed, step, batch, scale)
+           packed, step, batch, scale, device)
     hit = _descs.get(key)
     if hit is not None:
         return hit
@@ -256,12 +245,16 @@ def _desc(call: str, q, k, v, log_decay, out_strides, packed: bool, step: bool, 
             s.frame, s.sequence, s.head = st[0], st[1], st[2]
         return s
 
+    out = tuple(q.shape[:-1]) + (dv,)                # without gaps
     d = _AttentionDesc(_DTYPES[q.dtype], batch, heads, groups, dk, dv, 1 if step else q.shape[0], scale, strides(q.stride()), strides(k.stride()),
-                       strides(v.stride()), strides(out_strides))
+                       strides(v.stride()), strides(tuple(math.prod(out[i + 1:]) for i in range(len(out)))))
     ld = log_decay.stride()
     d.log_decay = _Strides(0, 0, ld[0]) if log_decay.dim() == 1 else strides(ld)
     size = ctypes.c_size_t()
-    _check(_library().sr_linear_attention_workspace_bytes(ctypes.byref(d), 1 if packed else 0, ctypes.byref(size)), call)
+    with torch.cuda.device(device):                  # (the workspace goes by the device's SMs)
+        code = _library().sr_linear_attention_workspace_bytes(ctypes.byref(d), 1 if packed else 0, ctypes.byref(size))
+    if code:
+        raise SrError(code, call)
     if len(_descs) >= 256:
         _descs.clear()
     _descs[key] = hit = (ctypes.byref(d), size.value, (batch, groups, dk, dv), d)
@@ -283,25 +276,24 @@ def linear_attention_run(q, k, v, log_decay, state=None, offsets=None, scale: fl
     frame (None: zeros).  `out` (without gaps; frames that no sequence has keep what it holds) and `state_out` (may be `state`) are written in
     place of new tensors."""
     call = "linear_attention_run"
-    _tensors(call, q, k, v, log_decay, state, offsets, out, state_out)
+    device = _tensors(call, q, k, v, log_decay, state, offsets, out, state_out)
     packed = offsets is not None
     if packed and (offsets.dtype is not torch.int64 or offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous()):
         _refuse(call, "offsets have to be int64 [sequences + 1] without gaps")
     if q.dim() < 3 or v.dim() < 3:
         _refuse(call, "q, k and v have to be [frames][sequences][heads][size], or [frames][heads][size] with offsets")
     if out is None:
-        out = torch.empty(q.shape[:-1] + v.shape[-1:], dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape[:-1] + v.shape[-1:])
     elif out.shape != q.shape[:-1] + v.shape[-1:] or out.dtype is not q.dtype or not out.is_contiguous():
         _refuse(call, "out has to be %s of q's type without gaps" % (tuple(q.shape[:-1] + v.shape[-1:]),))
     batch = offsets.shape[0] - 1 if packed else q.shape[1]
-    desc, size, shape, _ = _desc(call, q, k, v, log_decay, out.stride(), packed, False, batch, scale)
+    desc, size, shape, _ = _desc(call, device, q, k, v, log_decay, packed, False, batch, scale)
     sp = None if state is None else _state_pointer(call, state, shape)
-    last = torch.empty(shape, dtype=torch.float32, device=q.device) if state_out is None else state_out
+    last = q.new_empty(shape, dtype=torch.float32) if state_out is None else state_out
     lp = _state_pointer(call, last, shape)
-    work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
-    with _on(q) as stream:
-        _check(_library().sr_linear_attention_run(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), offsets.data_ptr() if packed else None,
-                                                  sp, lp, out.data_ptr(), work.data_ptr() if size else None, size, stream), "sr_" + call)
+    work = q.new_empty(size, dtype=torch.uint8) if size else None
+    _call("sr_linear_attention_run", device, _library().sr_linear_attention_run, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
+          offsets.data_ptr() if packed else None, sp, lp, out.data_ptr(), work.data_ptr() if size else None, size)
     return out, last
 
 
@@ -309,23 +301,20 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0):
     """One frame of every sequence: q [sequences][heads][dk], k [..][groups][dk], v [..][groups][dv], log_decay [groups] or [sequences][groups].
     `state` (float32 [sequences][groups][dk][dv]) is updated in place; returns out [sequences][heads][dv]."""
     call = "linear_attention_step"
-    _tensors(call, q, k, v, log_decay, state)
+    device = _tensors(call, q, k, v, log_decay, state)
     if q.dim() != 3 or v.dim() != 3:
         _refuse(call, "q, k and v have to be [sequences][heads][size]")
-    out = torch.empty(q.shape[:-1] + v.shape[-1:], dtype=q.dtype, device=q.device)
-    desc, _, shape, _ = _desc(call, q, k, v, log_decay, out.stride(), False, True, q.shape[0], scale)
-    sp = _state_pointer(call, state, shape)
-    with _on(q) as stream:
-        _check(_library().sr_linear_attention_step(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), sp, out.data_ptr(), stream),
-               "sr_" + call)
+    out = q.new_empty(q.shape[:-1] + v.shape[-1:])
+    desc, _, shape, _ = _desc(call, device, q, k, v, log_decay, False, True, q.shape[0], scale)
+    _call("sr_linear_attention_step", device, _library().sr_linear_attention_step, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
+          _state_pointer(call, state, shape), out.data_ptr())
     return out
 
 
 def operator_status(device=None):
     """Waits for the current stream's work; raises `SrError` if it failed or a bounded wait inside an operator's kernel expired."""
     index = torch.cuda.current_device() if device is None else torch.device(device).index
-    with torch.cuda.device(index):
-        _check(_library().sr_operator_status(_raw_stream(index)), "sr_operator_status")
+    _call("sr_operator_status", index, _library().sr_operator_status)
 
 
 class TemporalHead:
