@@ -24,6 +24,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstddef>
 
 #include "sr_memory.h"
@@ -837,26 +838,32 @@ cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
     return e != cudaSuccess ? e : launch<DK, 2>(C, C.slots * per_slot, s);
 }
 
-// Frames of a segment, 0: whole sequences.  Segments cost another pass over k and v and their states' way out and back, so they are for
-// launches that leave SMs without work.
+// Frames of a segment, 0: whole sequences.  Segments are read twice (k and v for their sums, then everything for the outputs) and cost two launches and the
+// way of their states out and back, about as much as eight chunks; they are for launches that would leave SMs without work, or wait for
+// one long sequence.  A step (a chunk for one head) is the unit; a chunk's sums alone are three quarters of one.  Of packed sequences only the mean is known: the longest
+// is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 616 / 166, 4096 frames 86 / 51; 8 sequences of 1024, 4 heads of 64
+// 25 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 596 / 334; 32 of 1000, 8 heads of 64 90 / 120.  More than one wave of segments lost: 32768 frames 210, 263 with two, three.
 struct Cut {
     int64_t segment, slots;
 };
 Cut cut_of(const sr_attention_desc* d, bool packed)
 {
-    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kCols - 1) / kCols);
-    const int64_t blocks = d->batch * per_slot, sms = std::max(1, sr_device_sms());
-    const int64_t total = packed ? d->frames : d->frames * d->batch;
     Cut cut{0, 0};
-    if ((int64_t)d->batch * d->groups > 65535) return cut;
-    if (packed ? blocks >= 8 * sms : 2 * blocks > sms) return cut;
-    // about one wave of segments, of 512 frames at least
-    const int64_t want = std::max<int64_t>(1, (packed ? 4 : 1) * sms / per_slot);
-    int64_t length = (total + want - 1) / want;
-    length = std::max<int64_t>(512, (length + kChunk - 1) / kChunk * kChunk);
+    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kCols - 1) / kCols), sms = std::max(1, sr_device_sms());
+    if (d->batch < 1 || d->frames < 1 || (int64_t)d->batch * d->groups > 65535) return cut;
+    const double share = (double)(d->heads / d->groups);
+    const double total = packed ? (double)d->frames : (double)d->frames * d->batch, mean = total / d->batch;
+    const double longest = packed ? std::min(total, 3.0 * mean) : mean;
+    const double waves = (double)(((int64_t)d->batch * per_slot + sms - 1) / sms);
+    const double whole = std::max(longest, waves * mean) / kChunk * share;
+    const int64_t want = std::max<int64_t>(1, sms / per_slot);
+    const int64_t length = std::max<int64_t>(512, ((int64_t)(total / (double)want) + kChunk - 1) / kChunk * kChunk);
     if (length >= d->frames) return cut;
+    const int64_t slots = packed ? d->batch + d->frames / length : d->batch * ((d->frames + length - 1) / length);
+    const double pieces = packed ? total / (double)length + 0.5 * d->batch : (double)slots;
+    if (std::ceil(pieces * (double)per_slot / (double)sms) * (double)(length / kChunk) * (share + 0.75) + 8.0 > 0.9 * whole) return cut;
     cut.segment = length;
-    cut.slots = packed ? d->batch + d->frames / length : d->batch * ((d->frames + length - 1) / length);
+    cut.slots = slots;
     return cut;
 }
 
