@@ -41,87 +41,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 struct ChunkArgs {
     CUtensorMap q_map, k_map, v_map, out_map;
-    AttentionArgs A;
-    float* sums;                                       // [slot][group][dk][dv]: sums of a segment, then the states that enter it
-    float* decays;                                     // [slot][group]: decay over a segment
-    int64_t segment;                                   // frames of a segment (0: whole sequences)
-    int32_t slots, v_tiles;
+    SegmentArgs S;
     int32_t out_copies;                                // outputs leave by TMA
     int* error;
 };
-
-// A CTA's work: frames t0 .. t0 + n - 1 of sequence b.
-struct Item {
-    int b, g, c0, slot;
-    int64_t t0, n, whole;                              // whole: frames of the sequence
-    AttentionSpan span;
-    bool there, last;
-};
-__device__ __forceinline__ int64_t segments_of(int64_t n, int64_t length) { return n > length ? (n + length - 1) / length : 1; }
-
-// The sequence and segment of a slot: slots count the segments of the sequences one after the other.  (All lanes of a warp.)
-__device__ __forceinline__ void find_slot(const ChunkArgs& C, int slot, int& b, int64_t& seg)
-{
-    const AttentionArgs& A = C.A;
-    if (!A.offsets) {
-        const int64_t per = segments_of(A.frames, C.segment);
-        b = (int)(slot / per);
-        seg = slot - b * per;
-        if (b >= A.batch) b = -1;
-        return;
-    }
-    const int lane = threadIdx.x & 31;
-    int64_t before = 0;
-    b = -1;
-    seg = 0;
-    for (int b0 = 0; b0 < A.batch; b0 += 32) {
-        const int64_t mine = b0 + lane < A.batch ? segments_of(attention_span(A, b0 + lane).n, C.segment) : 0;
-        int64_t sum = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-            if (lane >= d) sum += up;
-        }
-        const bool here = mine > 0 && before + sum - mine <= slot && slot < before + sum;
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
-        if (who) {
-            const int w = __ffs(who) - 1;
-            b = b0 + w;
-            seg = slot - (before + __shfl_sync(0xFFFFFFFFu, sum - mine, w));
-            return;
-        }
-        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
-    }
-}
-
-template <int MODE>
-__device__ __forceinline__ Item item_of(const ChunkArgs& C)
-{
-    const AttentionArgs& A = C.A;
-    Item it;
-    int x = blockIdx.x;
-    it.c0 = (x % C.v_tiles) * kCols;
-    x /= C.v_tiles;
-    it.g = x % A.groups;
-    x /= A.groups;
-    it.slot = x;
-    it.b = x;
-    int64_t seg = 0;
-    if (MODE != 0) find_slot(C, x, it.b, seg);
-    it.there = it.b >= 0;
-    if (!it.there) return it;
-    it.span = attention_span(A, it.b);
-    it.whole = it.span.n;
-    it.t0 = 0;
-    it.n = it.whole;
-    it.last = true;
-    if (MODE != 0) {
-        it.t0 = seg * C.segment;
-        it.n = min(C.segment, it.whole - it.t0);
-        it.last = it.t0 + it.n >= it.whole;
-    }
-    return it;
-}
 
 __device__ __forceinline__ float exp2_fast(float x)
 {
@@ -198,7 +121,7 @@ static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read
 
 // 16 outputs of row i of a chunk, one by one.  odd: values that are not finite have been left out of the chunk's near product; their terms as the formula has
 // them go on top of the stored outputs (what comes out is not finite, so the outputs' rounding does not matter).
-__device__ __noinline__ void store_row(const AttentionArgs& A, const Decays& D, const Item& it, int64_t f0, int i, int h, int c0, bool odd, uint4 lo, uint4 hi)
+__device__ __noinline__ void store_row(const AttentionArgs& A, const Decays& D, const AttentionItem& it, int64_t f0, int i, int h, int c0, bool odd, uint4 lo, uint4 hi)
 {
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f0 + i) * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + c0;
     const uint32_t z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
@@ -277,11 +200,11 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     __shared__ uint64_t bars[32];
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_flag;
-    const AttentionArgs& A = C.A;
+    const AttentionArgs& A = C.S.A;
     volatile int* gave_up = &gave_up_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     wait_for_predecessor();
-    const Item it = item_of<MODE>(C);
+    const AttentionItem it = attention_item(C.S, MODE != 0, kCols);
     if (!it.there || (MODE == 1 && it.last)) return;
     const int64_t state_at = ((int64_t)it.b * A.groups + it.g) * A.dk;
     const int64_t slot_at = ((int64_t)it.slot * A.groups + it.g) * A.dk;
@@ -507,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(d_full + 8 * slot);
         }
-        if (MODE == 1 && lane == 0 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
+        if (MODE == 1 && lane == 0 && it.c0 == 0) C.S.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
     } else if (warp >= 4) {
         // A worker has 32 rows (those of its quarter w of the TMEM lanes) and a quarter u of the columns of everything: frames' rows of V', of the scores and of the
         // outputs, rows of the state.  All of them do the same at the same time: warps with roles of their own, each with a loop of a few hundred
@@ -567,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         const uint32_t state = tmem + kState + lanes + u * 16;
         const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         if (holds) {
-            const float* from = MODE == 1 || i >= A.dk ? nullptr : MODE == 2 ? C.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
+            const float* from = MODE == 1 || i >= A.dk ? nullptr : MODE == 2 ? C.S.sums + (slot_at + i) * A.dv : A.state_in ? A.state_in + (state_at + i) * A.dv : nullptr;
             load_state(from, j0, A.dv, state);
             __syncwarp();
             tc_st(state + kCols, none);
@@ -728,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         if (ok) {
             tc_fence_after();
             if (holds) {
-                float* to = i >= A.dk ? nullptr : MODE == 1 ? C.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
+                float* to = i >= A.dk ? nullptr : MODE == 1 ? C.S.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
                 store_state(to, j0, A.dv, state);
                 __syncwarp();
             }
@@ -744,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
 }
 
 // The states that enter the segments of a sequence, from their sums: one after the other, element by element.
-__global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant__ ChunkArgs C)
+__global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant__ SegmentArgs C)
 {
     __shared__ int64_t first_slot;
     const AttentionArgs& A = C.A;
@@ -766,16 +689,13 @@ __global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant_
     const int64_t size = (int64_t)A.dk * A.dv, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= size) return;
     float S = A.state_in ? A.state_in[((int64_t)b * A.groups + g) * size + i] : 0.0f;
-    for (int64_t s = 0; s < count && first_slot + s < C.slots; ++s) {                       // (offsets that overlap may ask for more slots than there are)
+    // (offsets that overlap may ask for more slots than there are)
+    for (int64_t s = 0; s < count && first_slot + s < C.slots; ++s) {
         const int64_t slot = (first_slot + s) * A.groups + g;
         float* p = C.sums + slot * size + i;
-        if (s + 1 < count) {
-            const float sum = *p;
-            *p = S;
-            S = fmaf(C.decays[slot], S, sum);
-        } else {
-            *p = S;
-        }
+        const float sum = s + 1 < count ? *p : 0.0f;
+        *p = S;
+        if (s + 1 < count) S = fmaf(C.decays[slot], S, sum);
     }
 }
 
@@ -820,22 +740,13 @@ cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 template <int DK>
 cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
 {
-    const AttentionArgs& A = C.A;
-    const int64_t per_slot = (int64_t)A.groups * C.v_tiles;
-    if (!C.segment) return launch<DK, 0>(C, A.batch * per_slot, s);
-    cudaError_t e = launch<DK, 1>(C, C.slots * per_slot, s);
+    const AttentionArgs& A = C.S.A;
+    const int64_t per_slot = (int64_t)A.groups * C.S.v_tiles;
+    if (!C.S.segment) return launch<DK, 0>(C, A.batch * per_slot, s);
+    cudaError_t e = launch<DK, 1>(C, C.S.slots * per_slot, s);
     if (e != cudaSuccess) return e;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(((int64_t)A.dk * A.dv + 255) / 256), (unsigned)(A.batch * A.groups));
-    cfg.blockDim = dim3(256);
-    cfg.stream = s;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, sr_segments_kernel, C);
-    return e != cudaSuccess ? e : launch<DK, 2>(C, C.slots * per_slot, s);
+    e = sr_segments_launch(C.S, s);
+    return e != cudaSuccess ? e : launch<DK, 2>(C, C.S.slots * per_slot, s);
 }
 
 // Frames of a segment, 0: whole sequences.  Segments are read twice (k and v for their sums, then everything for the outputs) and cost two launches and the
@@ -843,12 +754,9 @@ cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
 // one long sequence.  A step (a chunk for one head) is the unit; a chunk's sums alone are three quarters of one.  Of packed sequences only the mean is known: the longest
 // is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 616 / 166, 4096 frames 86 / 51; 8 sequences of 1024, 4 heads of 64
 // 25 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 596 / 334; 32 of 1000, 8 heads of 64 90 / 120.  More than one wave of segments lost: 32768 frames 210, 263 with two, three.
-struct Cut {
-    int64_t segment, slots;
-};
-Cut cut_of(const sr_attention_desc* d, bool packed)
+AttentionCut cut_of(const sr_attention_desc* d, bool packed)
 {
-    Cut cut{0, 0};
+    AttentionCut cut{0, 0};
     const int64_t per_slot = (int64_t)d->groups * ((d->dv + kCols - 1) / kCols), sms = std::max(1, sr_device_sms());
     if (d->batch < 1 || d->frames < 1 || (int64_t)d->batch * d->groups > 65535) return cut;
     const double share = (double)(d->heads / d->groups);
@@ -881,24 +789,41 @@ bool sr_chunks_wanted(const sr_attention_desc* d)
     return d->dtype == SR_DTYPE_BF16 && d->dk <= 128 && d->frames >= 16 &&
            (int64_t)(d->batch + d->frames) * d->groups * ((d->dv + kCols - 1) / kCols) <= 0x7FFFFFFF;
 }
-size_t sr_chunks_workspace(const sr_attention_desc* d, bool packed)
-{
-    const Cut cut = cut_of(d, packed);
-    return cut.segment ? (size_t)cut.slots * d->groups * ((size_t)d->dk * d->dv * 4 + 4) + 256 : 0;
-}
+AttentionCut sr_chunks_cut(const sr_attention_desc* d, bool packed) { return cut_of(d, packed); }
 
-cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d, void* workspace, cudaStream_t s)
+SegmentArgs sr_segment_args(const AttentionArgs& A, AttentionCut cut, int cols, void* workspace)
 {
-    const Cut cut = cut_of(d, A.offsets != nullptr);
-    ChunkArgs C{};
+    SegmentArgs C{};
     C.A = A;
-    C.error = sr_operator_error_word();
-    if (!C.error) return cudaErrorUnknown;
     C.segment = cut.segment;
     C.slots = (int32_t)cut.slots;
-    C.v_tiles = (d->dv + kCols - 1) / kCols;
+    C.v_tiles = (A.dv + cols - 1) / cols;
     C.sums = static_cast<float*>(workspace);
-    C.decays = C.sums ? C.sums + (size_t)cut.slots * d->groups * d->dk * d->dv : nullptr;
+    C.decays = C.sums ? C.sums + (size_t)cut.slots * A.groups * A.dk * A.dv : nullptr;
+    return C;
+}
+
+cudaError_t sr_segments_launch(const SegmentArgs& C, cudaStream_t s)
+{
+    const AttentionArgs& A = C.A;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(((int64_t)A.dk * A.dv + 255) / 256), (unsigned)(A.batch * A.groups));
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sr_segments_kernel, C);
+}
+
+cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d, AttentionCut cut, void* workspace, cudaStream_t s)
+{
+    ChunkArgs C{};
+    C.S = sr_segment_args(A, cut, kCols, workspace);
+    C.error = sr_operator_error_word();
+    if (!C.error) return cudaErrorUnknown;
     const int64_t sequences = A.offsets ? 1 : d->batch;
     if (!encode(&C.q_map, A.q, A.sq, d->dk, d->heads, sequences, d->frames) || !encode(&C.k_map, A.k, A.sk, d->dk, d->groups, sequences, d->frames) ||
         !encode(&C.v_map, A.v, A.sv, d->dv, d->groups, sequences, d->frames))

@@ -6,107 +6,272 @@
 #include <cstdint>
 
 #include "sr_memory.h"
+#include "sr_operators.h"
+#include "sr_ptx.cuh"
 
 namespace {
 
-// ------------------------------------------------------------------------------------------ frame by frame, any sizes
-// A block holds 64 columns of a group's state: thread (column, rs) the rows of split rs, four neighbouring rows out of every 4 * RS.
-// Frames come in through shared memory, kRunRows rows of queries at a time.
-constexpr int kRunRows = 32, kRunCols = 64;
+// ------------------------------------------------------------------------------------------ whole clips, any sizes
+// CUDA cores, everything in 32 bits: fp32 clips, and what the tensor-core kernel does not take (heads of more than 128, rows that TMA cannot copy, a few
+// frames).  The same chunks, of 16 frames:  out_i = scale * (exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j),
+// S' = exp(G_last) S + sum_j exp(G_last - G_j) k_j v_j^T, so that a state's value costs two fused multiply-adds per frame (q S and k v^T) and one product per chunk.
+// A CTA has 64 columns of a group's state: thread (row group, column group) ROWS x 4 values of it in registers, so that a frame's 2 * 4 * ROWS multiply-adds take
+// 2 * ROWS / 4 + 1 loads of 16 bytes from shared memory.  Bound by the multiply-adds: 128 cycles per frame for dk = 128, besides the scores.  Before that, frame by
+// frame with a column per thread, 500 frames of 5 sequences, 6 heads of 40 and 72 took 320 us.
+// The partial sums of q S over the row groups of a warp are added with a shuffle, those of the warps in shared memory.
+constexpr int kFrames = 16, kRunCols = 64, kRunThreads = 256;
 
-template <typename T, int RS>
-__global__ void __launch_bounds__(kRunCols * RS) sr_attention_frames_kernel(const __grid_constant__ AttentionArgs A)
+template <int DK>
+struct FramesShared {
+    float k[kFrames][DK], q[kFrames][DK], v[kFrames][kRunCols];
+    float part[8][kFrames][kRunCols];
+    float p[kFrames][kFrames + 1];                     // weights of the frames before
+    double g[kFrames];                                 // log decay since the chunk's start
+    float near[kFrames], rest[kFrames];                // exp(G_i), exp(G_last - G_j)
+    float whole;                                       // exp(G_last)
+};
+
+template <typename T, int DK, int MODE>                // DK: rows of the state, padded; MODE as in the tensor-core kernel: 0 whole, 1 sums of segments, 2 their outputs
+__global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const __grid_constant__ SegmentArgs C)
 {
-    constexpr int DK = RS * 32;
-    extern __shared__ float smem[];
-    const int ct = max(1, min(16, kRunRows / A.share));
-    float* ks = smem;                                  // [ct][DK]
-    float* vs = ks + ct * DK;                          // [ct][kRunCols]
-    float* ds = vs + ct * kRunCols;                    // [16]
-    float* qs = ds + 16;                               // [ct][share][DK]
-    const int b = blockIdx.x / A.groups, g = blockIdx.x % A.groups, c0 = blockIdx.y * kRunCols;
-    const int col = threadIdx.x / RS, rs = threadIdx.x % RS, j = c0 + col;
-    const AttentionSpan sp = attention_span(A, b);
-    const T* q = static_cast<const T*>(A.q) + sp.b * A.sq.sequence + (int64_t)g * A.share * A.sq.head;
-    const T* k = static_cast<const T*>(A.k) + sp.b * A.sk.sequence + (int64_t)g * A.sk.head;
-    const T* v = static_cast<const T*>(A.v) + sp.b * A.sv.sequence + (int64_t)g * A.sv.head;
-    T* out = static_cast<T*>(A.out) + sp.b * A.so.sequence + (int64_t)g * A.share * A.so.head;
-    const float* d = A.decay + sp.b * A.sd.sequence + (int64_t)g * A.sd.head;
-    const int64_t at = ((int64_t)b * A.groups + g) * A.dk;
-    auto row_of = [&](int r) { return (r >> 2) * (4 * RS) + rs * 4 + (r & 3); };
-    float S[32];
+    constexpr int ROWS = DK / 16;                      // of a thread
+    constexpr bool OUT = MODE != 1;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    FramesShared<DK>& M = *reinterpret_cast<FramesShared<DK>*>(smem_raw);
+    const AttentionArgs& A = C.A;
+    srx::let_successor_start();
+    srx::wait_for_predecessor();
+    const AttentionItem it = attention_item(C, MODE != 0, kRunCols);
+    if (!it.there || (MODE == 1 && it.last)) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cg = tid & 15, rg = tid >> 4;
+    const int64_t sequence = it.span.b;
+    const T* k = static_cast<const T*>(A.k) + sequence * A.sk.sequence + (int64_t)it.g * A.sk.head;
+    const T* v = static_cast<const T*>(A.v) + sequence * A.sv.sequence + (int64_t)it.g * A.sv.head + it.c0;
+    const float* d = A.decay + sequence * A.sd.sequence + (int64_t)it.g * A.sd.head;
+    const int64_t state_at = ((int64_t)it.b * A.groups + it.g) * A.dk, slot_at = ((int64_t)it.slot * A.groups + it.g) * A.dk;
+    const int64_t f0 = it.span.first + it.t0;
+    const int cols = min(kRunCols, A.dv - it.c0);
+    // row r of a thread: neighbouring fours of the row groups lie side by side, so that a warp's two row groups read different banks
+    auto row_of = [&](int r) { return (r >> 2) * 64 + rg * 4 + (r & 3); };
+    constexpr int R4 = ROWS < 4 ? 1 : ROWS / 4;
+    auto row = [&](int r) { return ROWS < 4 ? rg * ROWS + r : row_of(r); };
+    float S[ROWS][4];
+    {
+        const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + slot_at * A.dv : A.state_in ? A.state_in + state_at * A.dv : nullptr;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) S[r] = A.state_in && row_of(r) < A.dk && j < A.dv ? A.state_in[(at + row_of(r)) * A.dv + j] : 0.0f;
-    for (int64_t t0 = 0; t0 < sp.n; t0 += ct) {
-        const int n = (int)min((int64_t)ct, sp.n - t0);
-        const int64_t f = sp.first + t0;
-        for (int i = threadIdx.x; i < n * DK; i += blockDim.x) {
-            const int t = i / DK, c = i % DK;
-            ks[i] = c < A.dk ? (float)k[(f + t) * A.sk.frame + c] : 0.0f;
-        }
-        for (int i = threadIdx.x; i < n * A.share * DK; i += blockDim.x) {
-            const int th = i / DK, c = i % DK, t = th / A.share, h = th % A.share;
-            qs[i] = c < A.dk ? (float)q[(f + t) * A.sq.frame + h * A.sq.head + c] : 0.0f;
-        }
-        for (int i = threadIdx.x; i < n * kRunCols; i += blockDim.x) {
-            const int t = i / kRunCols, c = i % kRunCols;
-            vs[i] = c0 + c < A.dv ? (float)v[(f + t) * A.sv.frame + c0 + c] : 0.0f;
-        }
-        if (threadIdx.x < n) ds[threadIdx.x] = expf(d[(f + threadIdx.x) * A.sd.frame]);
-        __syncthreads();
-        for (int t = 0; t < n; ++t) {
-            const float decay = ds[t], x = vs[t * kRunCols + col];
+        for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-            for (int r = 0; r < 32; r += 4) {
-                const float4 y = *reinterpret_cast<const float4*>(&ks[t * DK + row_of(r)]);
-                S[r] = fmaf(decay, S[r], y.x * x);
-                S[r + 1] = fmaf(decay, S[r + 1], y.y * x);
-                S[r + 2] = fmaf(decay, S[r + 2], y.z * x);
-                S[r + 3] = fmaf(decay, S[r + 3], y.w * x);
+            for (int e = 0; e < 4; ++e)
+                S[r][e] = from && row(r) < A.dk && cg * 4 + e < cols ? from[(int64_t)row(r) * A.dv + it.c0 + cg * 4 + e] : 0.0f;
+    }
+    double carry = 0.0, log_whole = 0.0;               // (thread 0) what the decays of whole chunks have lost by rounding, relative; the logarithm of all
+    const int steps = OUT ? A.share : 1;
+    for (int64_t t0 = 0; t0 < it.n; t0 += kFrames) {
+        const int n = (int)min((int64_t)kFrames, it.n - t0);
+        const int64_t f = f0 + t0;
+        __syncthreads();                               // (the chunk before has been read)
+        for (int x = tid; x < kFrames * DK; x += kRunThreads) {
+            const int t = x / DK, c = x % DK;
+            M.k[t][c] = t < n && c < A.dk ? (float)k[(f + t) * A.sk.frame + c] : 0.0f;
+        }
+        for (int x = tid; x < kFrames * kRunCols; x += kRunThreads) {
+            const int t = x / kRunCols, c = x % kRunCols;
+            M.v[t][c] = t < n && c < cols ? (float)v[(f + t) * A.sv.frame + c] : 0.0f;
+        }
+        if (warp == 7) {
+            float x = lane < n ? d[(f + lane) * A.sd.frame] : 0.0f;
+            if (x < -128.0f) x = -128.0f;              // (exp(-128) is zero in 32 bits; sums of infinities would be NaN)
+            double g = (double)x;
+#pragma unroll
+            for (int m = 1; m < kFrames; m *= 2) {
+                const double up = __shfl_up_sync(0xFFFFFFFFu, g, m);
+                if (lane >= m) g += up;
             }
-            for (int h = 0; h < A.share; ++h) {
-                float o = 0.0f;
+            const double last = __shfl_sync(0xFFFFFFFFu, g, kFrames - 1);
+            if (lane < kFrames) {
+                M.g[lane] = g;
+                M.near[lane] = expf((float)g);
+                M.rest[lane] = expf((float)(last - g));
+            }
+            if (lane == 0) {
+                const double exact = exp(last) * (1.0 + carry);
+                const float rounded = (float)exact;
+                M.whole = rounded;
+                carry = rounded > 1e-30f ? exact / (double)rounded - 1.0 : 0.0;
+                log_whole += last;
+            }
+        }
+        for (int h = 0; h < steps; ++h) {
+            if (OUT) {
+                const T* q = static_cast<const T*>(A.q) + sequence * A.sq.sequence + ((int64_t)it.g * A.share + h) * A.sq.head;
+                for (int x = tid; x < kFrames * DK; x += kRunThreads) {
+                    const int t = x / DK, c = x % DK;
+                    M.q[t][c] = t < n && c < A.dk ? (float)q[(f + t) * A.sq.frame + c] : 0.0f;
+                }
+            }
+            __syncthreads();
+            if (!OUT) break;
+            {   // weights: thread (i, j)
+                const int i = tid >> 4, j = tid & 15;
+                float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (j <= i) {
+#pragma unroll 4
+                    for (int c = 0; c < DK; c += 4) {
+                        // (every thread starts at another place: rows lie a multiple of 128 bytes apart)
+                        const int at = (c + 4 * j) % DK;
+                        const float4 a = *reinterpret_cast<const float4*>(&M.q[i][at]), b = *reinterpret_cast<const float4*>(&M.k[j][at]);
+                        x[0] = fmaf(a.x, b.x, x[0]);
+                        x[1] = fmaf(a.y, b.y, x[1]);
+                        x[2] = fmaf(a.z, b.z, x[2]);
+                        x[3] = fmaf(a.w, b.w, x[3]);
+                    }
+                }
+                M.p[i][j] = j <= i ? ((x[0] + x[1]) + (x[2] + x[3])) * expf((float)(M.g[i] - M.g[j])) : 0.0f;
+            }
+#pragma unroll 2
+            for (int t = 0; t < kFrames; ++t) {        // q S over the thread's rows
+                float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int r = 0; r < 32; r += 4) {
-                    const float4 y = *reinterpret_cast<const float4*>(&qs[(t * A.share + h) * DK + row_of(r)]);
-                    o = fmaf(y.x, S[r], o);
-                    o = fmaf(y.y, S[r + 1], o);
-                    o = fmaf(y.z, S[r + 2], o);
-                    o = fmaf(y.w, S[r + 3], o);
+                for (int r4 = 0; r4 < R4; ++r4) {
+                    float y[4];
+                    if constexpr (ROWS >= 4) {
+                        const float4 z = *reinterpret_cast<const float4*>(&M.q[t][row(4 * r4)]);
+                        y[0] = z.x; y[1] = z.y; y[2] = z.z; y[3] = z.w;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < ROWS; ++r) y[r] = M.q[t][row(r)];
+                    }
+#pragma unroll
+                    for (int r = 0; r < (ROWS < 4 ? ROWS : 4); ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[r], S[4 * r4 + r][e], o[e]);
                 }
 #pragma unroll
-                for (int m = 1; m < RS; m *= 2) o += __shfl_xor_sync(0xFFFFFFFFu, o, m);
-                if (rs == 0 && j < A.dv) out[(f + t) * A.so.frame + h * A.so.head + j] = (T)(A.scale * o);
+                for (int e = 0; e < 4; ++e) o[e] += __shfl_xor_sync(0xFFFFFFFFu, o[e], 16);
+                if (lane < 16) *reinterpret_cast<float4*>(&M.part[warp][t][cg * 4]) = make_float4(o[0], o[1], o[2], o[3]);
+            }
+            __syncthreads();
+            {   // outputs: thread (frame, four columns)
+                const int t = tid >> 4;
+                float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    const float4 z = *reinterpret_cast<const float4*>(&M.part[w][t][cg * 4]);
+                    o[0] += z.x; o[1] += z.y; o[2] += z.z; o[3] += z.w;
+                }
+                const float near = M.near[t];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] *= near;
+                for (int j = 0; j <= t; ++j) {
+                    const float p = M.p[t][j];
+                    const float4 z = *reinterpret_cast<const float4*>(&M.v[j][cg * 4]);
+                    o[0] = fmaf(p, z.x, o[0]);
+                    o[1] = fmaf(p, z.y, o[1]);
+                    o[2] = fmaf(p, z.z, o[2]);
+                    o[3] = fmaf(p, z.w, o[3]);
+                }
+                if (t < n) {
+                    T* out = static_cast<T*>(A.out) + sequence * A.so.sequence + (f + t) * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + it.c0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (cg * 4 + e < cols) out[cg * 4 + e] = (T)(A.scale * o[e]);
+                }
+            }
+            __syncthreads();
+        }
+        const float whole = M.whole;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[r][e] *= whole;
+#pragma unroll 2
+        for (int t = 0; t < kFrames; ++t) {
+            const float w = M.rest[t];
+            const float4 z = *reinterpret_cast<const float4*>(&M.v[t][cg * 4]);
+            const float x[4] = {w * z.x, w * z.y, w * z.z, w * z.w};
+#pragma unroll
+            for (int r4 = 0; r4 < R4; ++r4) {
+                float y[4];
+                if constexpr (ROWS >= 4) {
+                    const float4 u = *reinterpret_cast<const float4*>(&M.k[t][row(4 * r4)]);
+                    y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) y[r] = M.k[t][row(r)];
+                }
+#pragma unroll
+                for (int r = 0; r < (ROWS < 4 ? ROWS : 4); ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[4 * r4 + r][e] = fmaf(y[r], x[e], S[4 * r4 + r][e]);
             }
         }
-        __syncthreads();
     }
-    if (A.state_out)
+    if (MODE == 1 && tid == 7 * 32 && it.c0 == 0) C.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
+    float* to = MODE == 1 ? C.sums + slot_at * A.dv : it.last && A.state_out ? A.state_out + state_at * A.dv : nullptr;
+    if (to)
 #pragma unroll
-        for (int r = 0; r < 32; ++r)
-            if (row_of(r) < A.dk && j < A.dv) A.state_out[(at + row_of(r)) * A.dv + j] = S[r];
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (row(r) < A.dk && cg * 4 + e < cols) to[(int64_t)row(r) * A.dv + it.c0 + cg * 4 + e] = S[r][e];
 }
 
-template <typename T, int RS>
-cudaError_t launch_frames(const AttentionArgs& A, cudaStream_t s)
+template <typename T, int DK, int MODE>
+cudaError_t launch_frames(const SegmentArgs& C, cudaStream_t s)
 {
-    const int ct = std::max(1, std::min(16, kRunRows / A.share));
-    const size_t bytes = sizeof(float) * ((size_t)ct * RS * 32 * (1 + A.share) + (size_t)ct * kRunCols + 16);
-    if (bytes > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(sr_attention_frames_kernel<T, RS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != cudaSuccess) return e;
-    }
-    const dim3 grid((unsigned)(A.batch * A.groups), (unsigned)((A.dv + kRunCols - 1) / kRunCols));
-    sr_attention_frames_kernel<T, RS><<<grid, kRunCols * RS, bytes, s>>>(A);
-    return cudaGetLastError();
+    constexpr int smem = (int)sizeof(FramesShared<DK>);
+    static SrSharedLimit limit;
+    const cudaError_t e = limit.raise(sr_attention_frames_kernel<T, DK, MODE>, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((MODE ? (int64_t)C.slots : (int64_t)C.A.batch) * C.A.groups * C.v_tiles));
+    cfg.blockDim = dim3(kRunThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sr_attention_frames_kernel<T, DK, MODE>, C);
+}
+template <typename T, int DK>
+cudaError_t launch_frames_cut(const SegmentArgs& C, cudaStream_t s)
+{
+    if (!C.segment) return launch_frames<T, DK, 0>(C, s);
+    cudaError_t e = launch_frames<T, DK, 1>(C, s);
+    if (e == cudaSuccess) e = sr_segments_launch(C, s);
+    return e == cudaSuccess ? launch_frames<T, DK, 2>(C, s) : e;
 }
 template <typename T>
-cudaError_t launch_frames_any(const AttentionArgs& A, cudaStream_t s)
+cudaError_t launch_frames_any(const SegmentArgs& C, cudaStream_t s)
 {
-    if (A.dk <= 32) return launch_frames<T, 1>(A, s);
-    if (A.dk <= 64) return launch_frames<T, 2>(A, s);
-    if (A.dk <= 128) return launch_frames<T, 4>(A, s);
-    return launch_frames<T, 8>(A, s);
+    if (C.A.dk <= 32) return launch_frames_cut<T, 32>(C, s);
+    if (C.A.dk <= 64) return launch_frames_cut<T, 64>(C, s);
+    if (C.A.dk <= 128) return launch_frames_cut<T, 128>(C, s);
+    return launch_frames_cut<T, 256>(C, s);
+}
+// Segments for this kernel, by the same reasoning as for the other one: two CTAs to an SM, a piece of 128 frames at least, and about 160 frames' time for the two
+// launches more and the states' way.
+AttentionCut frames_cut(const sr_attention_desc* d, bool packed)
+{
+    AttentionCut cut{0, 0};
+    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kRunCols - 1) / kRunCols), held = 2 * std::max(1, sr_device_sms());
+    if (d->batch < 1 || d->frames < 1 || (int64_t)d->batch * d->groups > 65535) return cut;
+    const double share = (double)(d->heads / d->groups);
+    const double total = packed ? (double)d->frames : (double)d->frames * d->batch, mean = total / d->batch;
+    const double longest = packed ? std::min(total, 3.0 * mean) : mean;
+    const double waves = (double)(((int64_t)d->batch * per_slot + held - 1) / held);
+    const int64_t want = std::max<int64_t>(1, held / per_slot);
+    const int64_t length = std::max<int64_t>(128, ((int64_t)(total / (double)want) + kFrames - 1) / kFrames * kFrames);
+    if (length >= d->frames) return cut;
+    const int64_t slots = packed ? d->batch + d->frames / length : d->batch * ((d->frames + length - 1) / length);
+    const double pieces = packed ? total / (double)length + 0.5 * d->batch : (double)slots;
+    if (std::ceil(pieces * (double)per_slot / (double)held) * (double)length * (share + 0.5) + 160.0 > 0.9 * std::max(longest, waves * mean) * share) return cut;
+    if (slots * per_slot > 0x7FFFFFFF) return cut;
+    cut.segment = length;
+    cut.slots = slots;
+    return cut;
 }
 
 // ------------------------------------------------------------------------------------------ one frame
@@ -216,7 +381,9 @@ sr_status check(const sr_attention_desc* d)
         d->dk < 1 || d->dv < 1 || d->frames < 0 || !strides_fit(d->q) || !strides_fit(d->k) || !strides_fit(d->v) || !strides_fit(d->out) ||
         !strides_fit(d->log_decay))
         return SR_ERR_INVALID_ARG;
-    if ((int64_t)d->batch * d->groups > 0x7FFFFFFF || d->dv > 65535 * kStepCols) return SR_ERR_INVALID_ARG;
+    if ((int64_t)d->batch * d->groups > 0x7FFFFFFF || d->dv > 65535 * kStepCols ||
+        (int64_t)d->batch * d->groups * ((d->dv + kRunCols - 1) / kRunCols) > 0x7FFFFFFF)
+        return SR_ERR_INVALID_ARG;
     if (d->dk > 256 || d->heads / d->groups > 128) return SR_ERR_UNSUPPORTED;
     return SR_OK;
 }
@@ -254,7 +421,8 @@ sr_status sr_linear_attention_workspace_bytes(const sr_attention_desc* d, int pa
     const sr_status st = check(d);
     if (st != SR_OK) return st;
     if (!bytes) return SR_ERR_INVALID_ARG;
-    *bytes = sr_chunks_wanted(d) ? sr_chunks_workspace(d, packed != 0) : 0;
+    // (whether the tensor-core kernel can take the tensors is known when they are)
+    *bytes = std::max(sr_chunks_wanted(d) ? sr_cut_bytes(d, sr_chunks_cut(d, packed != 0)) : 0, sr_cut_bytes(d, frames_cut(d, packed != 0)));
     return SR_OK;
 }
 
@@ -268,7 +436,9 @@ sr_status sr_linear_attention_run(const sr_attention_desc* d, const void* q, con
     if (d->frames && (!q || !k || !v || !decay || !out || !aligned(q, d->dtype) || !aligned(k, d->dtype) || !aligned(v, d->dtype) || !aligned(out, d->dtype) ||
                       ((uintptr_t)decay & 3)))
         return SR_ERR_INVALID_ARG;
-    const size_t needed = sr_chunks_wanted(d) ? sr_chunks_workspace(d, offsets != nullptr) : 0;
+    const bool chunks = sr_chunks_wanted(d) && sr_chunks_fit(d, offsets != nullptr, q, k, v);
+    const AttentionCut cut = chunks ? sr_chunks_cut(d, offsets != nullptr) : frames_cut(d, offsets != nullptr);
+    const size_t needed = sr_cut_bytes(d, cut);
     if (needed && (!workspace || workspace_bytes < needed || ((uintptr_t)workspace & 255))) return SR_ERR_INVALID_ARG;
     AttentionArgs A = arguments(d, q, k, v, decay, out);
     A.offsets = offsets;
@@ -276,8 +446,12 @@ sr_status sr_linear_attention_run(const sr_attention_desc* d, const void* q, con
     A.state_out = state_out;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    if (sr_chunks_wanted(d) && sr_chunks_fit(d, offsets != nullptr, q, k, v)) e = sr_chunks_launch(A, d, workspace, s);
-    else e = d->dtype == SR_DTYPE_F32 ? launch_frames_any<float>(A, s) : launch_frames_any<__nv_bfloat16>(A, s);
+    if (chunks) {
+        e = sr_chunks_launch(A, d, cut, workspace, s);
+    } else {
+        const SegmentArgs C = sr_segment_args(A, cut, kRunCols, workspace);
+        e = d->dtype == SR_DTYPE_F32 ? launch_frames_any<float>(C, s) : launch_frames_any<__nv_bfloat16>(C, s);
+    }
     return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
 }
 
