@@ -66,20 +66,39 @@ __global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const 
     }
     double carry = 0.0, log_whole = 0.0;               // (thread 0) what the decays of whole chunks have lost by rounding, relative; the logarithm of all
     const int steps = OUT ? A.share : 1;
+    // A chunk's frames are in registers while the one before is worked on.
+    const T* q0 = static_cast<const T*>(A.q) + sequence * A.sq.sequence + (int64_t)it.g * A.share * A.sq.head;
+    T k_next[ROWS], q_next[ROWS], v_next[4];
+    float d_next = 0.0f;
+    auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int x = 0; x < ROWS; ++x) {
+            const int t = (tid + x * kRunThreads) / DK, c = (tid + x * kRunThreads) % DK;
+            const bool there = t0 + t < it.n && c < A.dk;
+            k_next[x] = there ? k[(f0 + t0 + t) * A.sk.frame + c] : (T)0.0f;
+            if (OUT) q_next[x] = there ? q0[(f0 + t0 + t) * A.sq.frame + c] : (T)0.0f;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int t = (tid + x * kRunThreads) / kRunCols, c = (tid + x * kRunThreads) % kRunCols;
+            v_next[x] = t0 + t < it.n && c < cols ? v[(f0 + t0 + t) * A.sv.frame + c] : (T)0.0f;
+        }
+        if (warp == 7) d_next = lane < kFrames && t0 + lane < it.n ? d[(f0 + t0 + lane) * A.sd.frame] : 0.0f;
+    };
+    fetch(0);
     for (int64_t t0 = 0; t0 < it.n; t0 += kFrames) {
         const int n = (int)min((int64_t)kFrames, it.n - t0);
         const int64_t f = f0 + t0;
         __syncthreads();                               // (the chunk before has been read)
-        for (int x = tid; x < kFrames * DK; x += kRunThreads) {
-            const int t = x / DK, c = x % DK;
-            M.k[t][c] = t < n && c < A.dk ? (float)k[(f + t) * A.sk.frame + c] : 0.0f;
+#pragma unroll
+        for (int x = 0; x < ROWS; ++x) {
+            (&M.k[0][0])[tid + x * kRunThreads] = (float)k_next[x];
+            if (OUT) (&M.q[0][0])[tid + x * kRunThreads] = (float)q_next[x];
         }
-        for (int x = tid; x < kFrames * kRunCols; x += kRunThreads) {
-            const int t = x / kRunCols, c = x % kRunCols;
-            M.v[t][c] = t < n && c < cols ? (float)v[(f + t) * A.sv.frame + c] : 0.0f;
-        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) (&M.v[0][0])[tid + x * kRunThreads] = (float)v_next[x];
         if (warp == 7) {
-            float x = lane < n ? d[(f + lane) * A.sd.frame] : 0.0f;
+            float x = d_next;
             if (x < -128.0f) x = -128.0f;              // (exp(-128) is zero in 32 bits; sums of infinities would be NaN)
             double g = (double)x;
 #pragma unroll
@@ -102,14 +121,15 @@ __global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const 
             }
         }
         for (int h = 0; h < steps; ++h) {
-            if (OUT) {
-                const T* q = static_cast<const T*>(A.q) + sequence * A.sq.sequence + ((int64_t)it.g * A.share + h) * A.sq.head;
+            if (h > 0) {
+                const T* q = q0 + h * A.sq.head;
                 for (int x = tid; x < kFrames * DK; x += kRunThreads) {
                     const int t = x / DK, c = x % DK;
                     M.q[t][c] = t < n && c < A.dk ? (float)q[(f + t) * A.sq.frame + c] : 0.0f;
                 }
             }
             __syncthreads();
+            if (h == 0) fetch(t0 + kFrames);
             if (!OUT) break;
             {   // weights: thread (i, j)
                 const int i = tid >> 4, j = tid & 15;
