@@ -29,6 +29,7 @@
 
 #include "sr_memory.h"
 #include "sr_operators.h"
+#include "sr_pair.cuh"
 #include "sr_ptx.cuh"
 
 namespace {
@@ -58,53 +59,6 @@ __device__ __forceinline__ float exp2_two(double x)   // 2^x, x as two floats
     const float y = exp2_fast(hi);
     return fmaf(y, lo * kLn2, y);
 }
-// Two floats in one register pair: one instruction for both.
-typedef unsigned long long Pair;
-__device__ __forceinline__ Pair pair(float lo, float hi)
-{
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
-    return p;
-}
-__device__ __forceinline__ Pair pair(uint32_t lo, uint32_t hi)
-{
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi));
-    return p;
-}
-__device__ __forceinline__ float2 split(Pair p)
-{
-    float2 f;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
-    return f;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b)
-{
-    Pair d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b)
-{
-    Pair d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
-{
-    Pair d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t round_bf16(Pair p)
-{
-    const float2 f = split(p);
-    uint32_t w;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(f.y), "f"(f.x));
-    return w;
-}
-// The two values of a word of bf16
-__device__ __forceinline__ Pair widen_bf16(uint32_t w) { return pair(w << 16, w & 0xFFFF0000u); }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
 struct alignas(16) Decays {                            // of a chunk (read four at a time); G in units of log 2

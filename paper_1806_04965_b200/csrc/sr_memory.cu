@@ -7,6 +7,7 @@
 
 #include "sr_memory.h"
 #include "sr_operators.h"
+#include "sr_pair.cuh"
 #include "sr_ptx.cuh"
 
 namespace {
@@ -55,14 +56,31 @@ __global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const 
     auto row_of = [&](int r) { return (r >> 2) * 64 + rg * 4 + (r & 3); };
     constexpr int R4 = ROWS < 4 ? 1 : ROWS / 4;
     auto row = [&](int r) { return ROWS < 4 ? rg * ROWS + r : row_of(r); };
-    float S[ROWS][4];
+    // four of a thread's rows of a frame's queries or keys
+    auto rows_of = [&](const float* from, int r4, float (&y)[4]) {
+        if constexpr (ROWS >= 4) {
+            const float4 z = *reinterpret_cast<const float4*>(from + row(4 * r4));
+            y[0] = z.x; y[1] = z.y; y[2] = z.z; y[3] = z.w;
+        } else {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) y[r] = from[row(r)];
+        }
+    };
+    using srx::Pair;
+    using srx::pair;
+    Pair S[ROWS][2];
     {
         const float* from = MODE == 1 ? nullptr : MODE == 2 ? C.sums + slot_at * A.dv : A.state_in ? A.state_in + state_at * A.dv : nullptr;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                S[r][e] = from && row(r) < A.dk && cg * 4 + e < cols ? from[(int64_t)row(r) * A.dv + it.c0 + cg * 4 + e] : 0.0f;
+            for (int e = 0; e < 4; e += 2) {
+                float y[2];
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    y[z] = from && row(r) < A.dk && cg * 4 + e + z < cols ? from[(int64_t)row(r) * A.dv + it.c0 + cg * 4 + e + z] : 0.0f;
+                S[r][e / 2] = pair(y[0], y[1]);
+            }
     }
     double carry = 0.0, log_whole = 0.0;               // (thread 0) what the decays of whole chunks have lost by rounding, relative; the logarithm of all
     const int steps = OUT ? A.share : 1;
@@ -148,27 +166,24 @@ __global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const 
                 }
                 M.p[i][j] = j <= i ? ((x[0] + x[1]) + (x[2] + x[3])) * expf((float)(M.g[i] - M.g[j])) : 0.0f;
             }
-#pragma unroll 2
+#pragma unroll
             for (int t = 0; t < kFrames; ++t) {        // q S over the thread's rows
-                float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                Pair o[2] = {0, 0};
 #pragma unroll
                 for (int r4 = 0; r4 < R4; ++r4) {
                     float y[4];
-                    if constexpr (ROWS >= 4) {
-                        const float4 z = *reinterpret_cast<const float4*>(&M.q[t][row(4 * r4)]);
-                        y[0] = z.x; y[1] = z.y; y[2] = z.z; y[3] = z.w;
-                    } else {
+                    rows_of(&M.q[t][0], r4, y);
 #pragma unroll
-                        for (int r = 0; r < ROWS; ++r) y[r] = M.q[t][row(r)];
+                    for (int r = 0; r < (ROWS < 4 ? ROWS : 4); ++r) {
+                        o[0] = srx::fma2(pair(y[r], y[r]), S[4 * r4 + r][0], o[0]);
+                        o[1] = srx::fma2(pair(y[r], y[r]), S[4 * r4 + r][1], o[1]);
                     }
-#pragma unroll
-                    for (int r = 0; r < (ROWS < 4 ? ROWS : 4); ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[r], S[4 * r4 + r][e], o[e]);
                 }
+                const float2 o0 = srx::split(o[0]), o1 = srx::split(o[1]);
+                float z[4] = {o0.x, o0.y, o1.x, o1.y};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += __shfl_xor_sync(0xFFFFFFFFu, o[e], 16);
-                if (lane < 16) *reinterpret_cast<float4*>(&M.part[warp][t][cg * 4]) = make_float4(o[0], o[1], o[2], o[3]);
+                for (int e = 0; e < 4; ++e) z[e] += __shfl_xor_sync(0xFFFFFFFFu, z[e], 16);
+                if (lane < 16) *reinterpret_cast<float4*>(&M.part[warp][t][cg * 4]) = make_float4(z[0], z[1], z[2], z[3]);
             }
             __syncthreads();
             {   // outputs: thread (frame, four columns)
@@ -199,30 +214,26 @@ __global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const 
             }
             __syncthreads();
         }
-        const float whole = M.whole;
+        const Pair whole = pair(M.whole, M.whole);
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
+        for (int r = 0; r < ROWS; ++r) {
+            S[r][0] = srx::mul2(S[r][0], whole);
+            S[r][1] = srx::mul2(S[r][1], whole);
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[r][e] *= whole;
-#pragma unroll 2
         for (int t = 0; t < kFrames; ++t) {
             const float w = M.rest[t];
             const float4 z = *reinterpret_cast<const float4*>(&M.v[t][cg * 4]);
-            const float x[4] = {w * z.x, w * z.y, w * z.z, w * z.w};
+            const Pair x0 = srx::mul2(pair(w, w), pair(z.x, z.y)), x1 = srx::mul2(pair(w, w), pair(z.z, z.w));
 #pragma unroll
             for (int r4 = 0; r4 < R4; ++r4) {
                 float y[4];
-                if constexpr (ROWS >= 4) {
-                    const float4 u = *reinterpret_cast<const float4*>(&M.k[t][row(4 * r4)]);
-                    y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w;
-                } else {
+                rows_of(&M.k[t][0], r4, y);
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) y[r] = M.k[t][row(r)];
+                for (int r = 0; r < (ROWS < 4 ? ROWS : 4); ++r) {
+                    S[4 * r4 + r][0] = srx::fma2(pair(y[r], y[r]), x0, S[4 * r4 + r][0]);
+                    S[4 * r4 + r][1] = srx::fma2(pair(y[r], y[r]), x1, S[4 * r4 + r][1]);
                 }
-#pragma unroll
-                for (int r = 0; r < (ROWS < 4 ? ROWS : 4); ++r)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) S[4 * r4 + r][e] = fmaf(y[r], x[e], S[4 * r4 + r][e]);
             }
         }
     }
@@ -230,10 +241,13 @@ __global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const 
     float* to = MODE == 1 ? C.sums + slot_at * A.dv : it.last && A.state_out ? A.state_out + state_at * A.dv : nullptr;
     if (to)
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
+        for (int r = 0; r < ROWS; ++r) {
+            const float2 lo = srx::split(S[r][0]), hi = srx::split(S[r][1]);
+            const float y[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (row(r) < A.dk && cg * 4 + e < cols) to[(int64_t)row(r) * A.dv + it.c0 + cg * 4 + e] = S[r][e];
+                if (row(r) < A.dk && cg * 4 + e < cols) to[(int64_t)row(r) * A.dv + it.c0 + cg * 4 + e] = y[e];
+        }
 }
 
 template <typename T, int DK, int MODE>
