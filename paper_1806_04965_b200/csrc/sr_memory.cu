@@ -19,6 +19,8 @@ namespace {
 // A CTA has 64 columns of a group's state: thread (row group, column group) ROWS x 4 values of it in registers, so that a frame's 2 * 4 * ROWS multiply-adds take
 // 2 * ROWS / 4 + 1 loads of 16 bytes from shared memory.  Bound by the multiply-adds: 128 cycles per frame for dk = 128, besides the scores.  Before that, frame by
 // frame with a column per thread, 500 frames of 5 sequences, 6 heads of 40 and 72 took 320 us.
+// (Two CTAs to an SM, 128 registers, for segments, which fill the device: 16384 frames, 8 heads of 128 755 -> 660 us; one, unlimited, for whole sequences, whose time is
+// that of one CTA: 512 frames x 16 sequences, 16 heads on 4 of 128 597, with two 800.)
 // The partial sums of q S over the row groups of a warp are added with a shuffle, those of the warps in shared memory.
 constexpr int kFrames = 16, kRunCols = 64, kRunThreads = 256;
 
@@ -33,7 +35,7 @@ struct FramesShared {
 };
 
 template <typename T, int DK, int MODE>                // DK: rows of the state, padded; MODE as in the tensor-core kernel: 0 whole, 1 sums of segments, 2 their outputs
-__global__ void __launch_bounds__(kRunThreads) sr_attention_frames_kernel(const __grid_constant__ SegmentArgs C)
+__global__ void __launch_bounds__(kRunThreads, MODE != 0 && DK <= 128 ? 2 : 1) sr_attention_frames_kernel(const __grid_constant__ SegmentArgs C)
 {
     constexpr int ROWS = DK / 16;                      // of a thread
     constexpr bool OUT = MODE != 1;
@@ -310,14 +312,17 @@ AttentionCut frames_cut(const sr_attention_desc* d, bool packed)
 
 // ------------------------------------------------------------------------------------------ one frame
 // Bound by the states: 8 bytes per element, read and written once.  A block of 256 threads has 32 columns of a group's state, so that a row of
-// it is a whole line, and few sequences still make many blocks.  VEC columns per thread.
+// it is a whole line, and few sequences still make many blocks.  VEC columns per thread.  Six blocks to an SM (40 registers): 256 sequences, 16 heads of 128
+// 92 us, 5.8 TB/s; with what the compiler takes by itself 104, with eight 110 (spills).
 constexpr int kStepCols = 32, kStepHeads = 8;
 
 template <typename T, int VEC, int ROWS>               // ROWS: rows of a thread
-__global__ void __launch_bounds__(256) sr_attention_step_kernel(const __grid_constant__ AttentionArgs A)
+__global__ void __launch_bounds__(256, ROWS <= 8 ? 6 : 1) sr_attention_step_kernel(const __grid_constant__ AttentionArgs A)
 {
     constexpr int CT = kStepCols / VEC, RL = 256 / CT; // threads per row; rows side by side
     __shared__ float part[kStepHeads][8][kStepCols];
+    srx::let_successor_start();
+    srx::wait_for_predecessor();
     const int b = blockIdx.x / A.groups, g = blockIdx.x % A.groups;
     const int tc = threadIdx.x % CT, rl = threadIdx.x / CT, j = blockIdx.y * kStepCols + tc * VEC;
     const bool there = j < A.dv;
@@ -388,17 +393,29 @@ __global__ void __launch_bounds__(256) sr_attention_step_kernel(const __grid_con
     }
 }
 
+template <typename T, int VEC, int ROWS>
+cudaError_t launch_step_rows(const AttentionArgs& A, cudaStream_t s)
+{
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(A.batch * A.groups), (unsigned)((A.dv + kStepCols - 1) / kStepCols));
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sr_attention_step_kernel<T, VEC, ROWS>, A);
+}
 template <typename T, int VEC>
 cudaError_t launch_step(const AttentionArgs& A, cudaStream_t s)
 {
     constexpr int RL = 256 / (kStepCols / VEC);
-    const dim3 grid((unsigned)(A.batch * A.groups), (unsigned)((A.dv + kStepCols - 1) / kStepCols));
     const int rows = (A.dk + RL - 1) / RL;
-    if (rows <= 2) sr_attention_step_kernel<T, VEC, 2><<<grid, 256, 0, s>>>(A);
-    else if (rows <= 4) sr_attention_step_kernel<T, VEC, 4><<<grid, 256, 0, s>>>(A);
-    else if (rows <= 8) sr_attention_step_kernel<T, VEC, 8><<<grid, 256, 0, s>>>(A);
-    else sr_attention_step_kernel<T, VEC, 32><<<grid, 256, 0, s>>>(A);
-    return cudaGetLastError();
+    if (rows <= 2) return launch_step_rows<T, VEC, 2>(A, s);
+    if (rows <= 4) return launch_step_rows<T, VEC, 4>(A, s);
+    if (rows <= 8) return launch_step_rows<T, VEC, 8>(A, s);
+    return launch_step_rows<T, VEC, 32>(A, s);
 }
 template <typename T>
 cudaError_t launch_step_any(const AttentionArgs& A, cudaStream_t s)

@@ -3,7 +3,7 @@
 //
 //     s = x + residual,   out = s / sqrt(mean(s^2) + eps) * weight,   out rounded to its type, or to groups of 32 with a scale.
 //
-// A row lies in the registers of the threads that share it (32 to 1024 of them, up to kHold units of VEC elements each) between the
+// A row lies in the registers of the threads that share it (32 to 1024 of them, a few units of VEC elements each) between the
 // sum of squares and the output, so that nothing is read twice; longer rows are read again (they come out of L2).  The
 // lanes of a group of 32 columns find its largest magnitude with shuffles.
 #include <cuda_bf16.h>
@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "sr_microscale.cuh"
+#include "sr_ptx.cuh"
 
 namespace {
 
@@ -108,13 +109,14 @@ __device__ __forceinline__ void store_scaled(const RowArgs& A, int64_t row, int6
     }
 }
 
-constexpr int kHold = 4;                               // units of a thread that stay in registers
-
-// HOLD 0: rows of any length, read twice.  FMT F32: the type of x.
-template <typename T, int VEC, int HOLD, bool NORM, int FMT>
+// HOLD: units of a thread that stay in registers; 0: rows of any length, read twice.  FMT F32: the type of x.
+// SHIFT: rows that do not start on 16 bytes, but alike in all buffers: a thread's units do, the first of a row may begin ahead of it.
+template <typename T, int VEC, int HOLD, bool NORM, int FMT, bool SHIFT>
 __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ RowArgs A)
 {
     __shared__ float part[32];
+    srx::let_successor_start();
+    srx::wait_for_predecessor();
     const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const bool row_there = row < A.rows;
     const int64_t r0 = row_there ? row : 0;
@@ -123,12 +125,20 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
     const int tpr = blockDim.x, tid = threadIdx.x;
     const int64_t end = FMT >= SR_FORMAT_MX8 ? A.tiles_g * 128 : A.cols;
     const int n_it = HOLD ? HOLD : (int)((end + (int64_t)tpr * VEC - 1) / ((int64_t)tpr * VEC));
+    const int64_t shift = SHIFT ? (int64_t)(((uintptr_t)x & 15) / sizeof(T)) : 0;
+    auto column = [&](int it) { return ((int64_t)it * tpr + tid) * VEC - shift; };
+    // the whole unit, or its columns that there are
+    auto whole = [&](int64_t c) { return !SHIFT || (c >= 0 && c + VEC <= A.cols); };
 
     auto load = [&](int it, float (&f)[VEC]) {
-        const int64_t c = ((int64_t)it * tpr + tid) * VEC;
+        const int64_t c = column(it);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) f[i] = 0.0f;
-        if (row_there && c < A.cols) {
+        if (row_there && c < A.cols && !whole(c)) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (c + i >= 0 && c + i < A.cols) f[i] = (float)x[c + i] + (res ? (float)res[c + i] : 0.0f);
+        } else if (row_there && c < A.cols) {
             load_unit<T, VEC>(x + c, f);
             if (NORM && res) {
                 float g[VEC];
@@ -170,15 +180,28 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
         inv = 1.0f / sqrtf(ss / (float)A.cols + A.eps);
     }
     auto finish = [&](int it, float (&s)[VEC]) {
-        const int64_t c = ((int64_t)it * tpr + tid) * VEC;
-        const bool there = row_there && c < A.cols;
-        if (NORM && there && A.sum) store_unit<T, VEC>(static_cast<T*>(A.sum) + row * A.cols + c, s);
+        const int64_t c = column(it);
+        const bool there = row_there && c < A.cols, all = there && whole(c);
+        auto put = [&](T* to) {
+            if (all) {
+                store_unit<T, VEC>(to + row * A.cols + c, s);
+            } else if (SHIFT && there) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (c + i >= 0 && c + i < A.cols) to[row * A.cols + c + i] = (T)s[i];
+            }
+        };
+        if (NORM && A.sum) put(static_cast<T*>(A.sum));
         if (NORM) {
             float w[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) w[i] = 1.0f;
             if (there && A.weight) {
-                if constexpr (VEC == 8) {
+                if constexpr (SHIFT) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (c + i >= 0 && c + i < A.cols) w[i] = A.weight[c + i];
+                } else if constexpr (VEC == 8) {
                     float lo[4], hi[4];
                     load_unit<float, 4>(A.weight + c, lo);
                     load_unit<float, 4>(A.weight + c + 4, hi);
@@ -192,7 +215,7 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
             for (int i = 0; i < VEC; ++i) s[i] = s[i] * inv * w[i];
         }
         if constexpr (FMT >= SR_FORMAT_MX8) store_scaled<VEC, FMT>(A, row, c, s, row_there);
-        else if (there) store_unit<T, VEC>(static_cast<T*>(A.out) + row * A.cols + c, s);
+        else put(static_cast<T*>(A.out));
     };
     if (HOLD) {
 #pragma unroll
@@ -205,38 +228,62 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
     }
 }
 
-template <typename T, int VEC, bool NORM, int FMT>
-cudaError_t launch_rows(const RowArgs& A, cudaStream_t s)
+template <typename T, int VEC, int HOLD, bool NORM, int FMT, bool SHIFT>
+cudaError_t launch_one(const RowArgs& A, int tpr, cudaStream_t s)
 {
-    const int64_t end = FMT >= SR_FORMAT_MX8 ? A.tiles_g * 128 : A.cols;
-    const int64_t units = (end + VEC - 1) / VEC;
-    int tpr = 32;
-    while (tpr < 1024 && (int64_t)tpr * kHold < units) tpr *= 2;
-    const int rpb = tpr < 128 && tpr == 32 ? 4 : 1;
+    const int rpb = tpr == 32 ? 4 : 1;
     const int64_t blocks = (A.rows + rpb - 1) / rpb;
     if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
-    const dim3 block((unsigned)tpr, (unsigned)rpb);
-    if ((int64_t)tpr * kHold >= units) sr_row_kernel<T, VEC, kHold, NORM, FMT><<<(unsigned)blocks, block, 0, s>>>(A);
-    else sr_row_kernel<T, VEC, 0, NORM, FMT><<<(unsigned)blocks, block, 0, s>>>(A);
-    return cudaGetLastError();
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)tpr, (unsigned)rpb);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sr_row_kernel<T, VEC, HOLD, NORM, FMT, SHIFT>, A);
+}
+// Threads of a row: as many as give each of them HOLD units.  One unit of 16 bytes is best as long as 1024 threads reach (with four, 16384 x 1024 of bf16 took 31 us,
+// so 23; 8 x 1024 4.6, so 2.6); single values want eight (16384 x 2001 of bf16 111, with four 126, with one 329).
+template <typename T, int VEC, bool NORM, int FMT, bool SHIFT>
+cudaError_t launch_rows(const RowArgs& A, cudaStream_t s)
+{
+    constexpr int FEW = VEC > 1 ? 1 : 8, MANY = VEC > 1 ? 4 : 16;
+    const int64_t end = FMT >= SR_FORMAT_MX8 ? A.tiles_g * 128 : A.cols;
+    const int64_t units = (end + VEC - 1) / VEC + (SHIFT ? 1 : 0);
+    for (const int hold : {FEW, MANY}) {
+        int tpr = 32;
+        while (tpr < 1024 && (int64_t)tpr * hold < units) tpr *= 2;
+        if ((int64_t)tpr * hold >= units) return hold == FEW ? launch_one<T, VEC, FEW, NORM, FMT, SHIFT>(A, tpr, s) : launch_one<T, VEC, MANY, NORM, FMT, SHIFT>(A, tpr, s);
+    }
+    return launch_one<T, VEC, 0, NORM, FMT, SHIFT>(A, 1024, s);
 }
 template <typename T, int VEC>
 cudaError_t launch_any(const RowArgs& A, bool norm, int fmt, cudaStream_t s)
 {
-    if (!norm) return fmt == SR_FORMAT_MX4 ? launch_rows<T, VEC, false, SR_FORMAT_MX4>(A, s) : launch_rows<T, VEC, false, SR_FORMAT_MX8>(A, s);
-    if (fmt == SR_FORMAT_MX4) return launch_rows<T, VEC, true, SR_FORMAT_MX4>(A, s);
-    if (fmt == SR_FORMAT_MX8) return launch_rows<T, VEC, true, SR_FORMAT_MX8>(A, s);
-    return launch_rows<T, VEC, true, SR_FORMAT_F32>(A, s);
+    if (!norm) return fmt == SR_FORMAT_MX4 ? launch_rows<T, VEC, false, SR_FORMAT_MX4, false>(A, s) : launch_rows<T, VEC, false, SR_FORMAT_MX8, false>(A, s);
+    if (fmt == SR_FORMAT_MX4) return launch_rows<T, VEC, true, SR_FORMAT_MX4, false>(A, s);
+    if (fmt == SR_FORMAT_MX8) return launch_rows<T, VEC, true, SR_FORMAT_MX8, false>(A, s);
+    return launch_rows<T, VEC, true, SR_FORMAT_F32, false>(A, s);
 }
-// 16-byte accesses where every row of every buffer allows them.
+// 16-byte accesses where every row of every buffer allows them, or all of them start equally far from where it would.
+template <typename T>
+cudaError_t launch(const RowArgs& A, bool norm, int fmt, cudaStream_t s)
+{
+    constexpr int el = sizeof(T), vec = 16 / el;
+    auto fits = [&](const void* p, int64_t stride) { return !((uintptr_t)p & 15) && stride % vec == 0; };
+    if (A.cols % vec == 0 && fits(A.x, A.x_stride) && (!A.residual || fits(A.residual, A.r_stride)) && !((uintptr_t)A.sum & 15) && !((uintptr_t)A.out & 15) &&
+        !((uintptr_t)A.weight & 15))
+        return launch_any<T, vec>(A, norm, fmt, s);
+    auto like = [&](const void* p, int64_t stride) { return !p || (((uintptr_t)p ^ (uintptr_t)A.x) % 16 == 0 && (stride - A.x_stride) % vec == 0); };
+    if (norm && fmt < SR_FORMAT_MX8 && like(A.residual, A.r_stride) && like(A.sum, A.cols) && like(A.out, A.cols)) return launch_rows<T, vec, true, SR_FORMAT_F32, true>(A, s);
+    return launch_any<T, 1>(A, norm, fmt, s);
+}
 cudaError_t launch(const RowArgs& A, bool norm, int dtype, int fmt, cudaStream_t s)
 {
-    const int el = dtype == SR_DTYPE_F32 ? 4 : 2, vec = 16 / el;
-    auto fits = [&](const void* p, int64_t stride) { return !((uintptr_t)p & 15) && stride % vec == 0; };
-    const bool wide = A.cols % vec == 0 && fits(A.x, A.x_stride) && (!A.residual || fits(A.residual, A.r_stride)) &&
-                      !((uintptr_t)A.sum & 15) && !((uintptr_t)A.out & 15) && !((uintptr_t)A.weight & 15);
-    if (dtype == SR_DTYPE_F32) return wide ? launch_any<float, 4>(A, norm, fmt, s) : launch_any<float, 1>(A, norm, fmt, s);
-    return wide ? launch_any<__nv_bfloat16, 8>(A, norm, fmt, s) : launch_any<__nv_bfloat16, 1>(A, norm, fmt, s);
+    return dtype == SR_DTYPE_F32 ? launch<float>(A, norm, fmt, s) : launch<__nv_bfloat16>(A, norm, fmt, s);
 }
 
 // Two elements per thread.
