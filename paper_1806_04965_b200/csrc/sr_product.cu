@@ -251,16 +251,25 @@ __global__ void __launch_bounds__(kThreads, 1) sr_product_kernel(const __grid_co
         cluster_sync();
         const int o0 = first % P.out_tiles * kOuts, r0 = first / P.out_tiles * NT;
         const int share = NT / P.split;
-        for (int i = threadIdx.x; i < share * kOuts; i += kThreads) {
-            const int c = rank * share + i / kOuts, o = i % kOuts;
-            float v = 0.0f;
-            for (int q = 0; q < P.split; ++q) v += ld_cluster(ring + (uint32_t)(c * kOuts + o) * 4u, (uint32_t)q);
-            if (r0 + c < P.rows && o0 + o < P.outs) {
-                if (P.bias) v += P.bias[o0 + o];
-                if (P.act) v = at_least(v, 0.0f);
-                const int64_t at = (int64_t)(r0 + c) * P.out_stride + o0 + o;
-                if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[at] = __float2bfloat16(v);
-                else static_cast<float*>(P.out)[at] = v;
+        for (int i = threadIdx.x; i < share * (kOuts / 4); i += kThreads) {
+            const int c = rank * share + i / (kOuts / 4), o = i % (kOuts / 4) * 4;
+            const uint32_t at = ring + (uint32_t)(c * kOuts + o) * 4u;
+            float4 v = ld_cluster(at, 0);
+#pragma unroll
+            for (int q = 1; q < 8; ++q) {
+                if (q >= P.split) break;
+                const float4 x = ld_cluster(at, (uint32_t)q);
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            if (r0 + c >= P.rows) continue;
+            const float y[4] = {v.x, v.y, v.z, v.w};
+            const int64_t to = (int64_t)(r0 + c) * P.out_stride + o0 + o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (o0 + o + e >= P.outs) break;
+                const float z = at_least(y[e] + (P.bias ? P.bias[o0 + o + e] : 0.0f), P.act ? 0.0f : -__int_as_float(0x7F800000));
+                if (P.out_bf16) put(static_cast<__nv_bfloat16*>(P.out) + to + e, z);
+                else put(static_cast<float*>(P.out) + to + e, z);
             }
         }
         cluster_sync();                                // (nobody leaves while others read its memory)
@@ -284,7 +293,10 @@ bool encode_rows(CUtensorMap* map, const void* data, int64_t row_bytes, int64_t 
 }
 
 // Rows of a tile, and CTAs that share a tile's reduction: the pair with the least estimated time in cycles.  A stage costs its four MMAs (NT / 2 cycles each,
-// or (128 + NT) / 4 where the operands' way out of shared memory is longer) or its copies (60 bytes per cycle and SM).
+// or (128 + NT) / 4 where the operands' way out of shared memory is longer) or its copies (60 bytes per cycle and SM).  Draining a tile costs 16 cycles per
+// column, beside the next tile's MMAs, the exchange of a shared reduction 36.  Us, one CTA per tile / shared by four: 1 x 4096 x 4096 in 4 bits 6.8 / 5.9 (tiles of 16),
+// 64 x 4096 x 4096 7.0 / 7.0 (64); shared by two with tiles of 128 200 x 4096 x 4096 7.9 / 9.4.  Tiles of 64 / 128 / 192 rows: 777 x 1000 x 1111 in 8 bits 5.5 / 5.9 / 6.7,
+// 4096 x 1024 x 4608 40 / 24 / 22.
 struct Plan {
     int nt, split;
 };
@@ -302,7 +314,7 @@ Plan plan_product(int64_t rows, int64_t outs, int stages, int sms)
             if (split > stages || (split > 1 && tiles * split > sms)) continue;
             const double waves = (double)((tiles * split + sms - 1) / sms);
             const double work = ((stages + split - 1) / split) * per_stage;
-            const double t = split > 1 ? work + drain / split + 1500.0 : waves * std::max(work, drain) + std::min(work, drain);
+            const double t = split > 1 ? work + drain / split + 36.0 * nt : waves * (std::max(work, drain) + 300.0) + std::min(work, drain);
             if (t < least) {
                 least = t;
                 best = {nt, split};
