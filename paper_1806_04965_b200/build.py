@@ -1,4 +1,4 @@
-"""Builds libsr_rollout.so (the C-ABI library) in-tree with nvcc for sm_100a."""
+"""Builds libsr_rollout.so (the C-ABI library) in-tree with nvcc for sm_100a, and the Python extension of its operators."""
 from __future__ import annotations
 
 import os
@@ -8,6 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsr_rollout.so")
+EXTENSION = os.path.join(HERE, "_operators.so")         # the operators' calls from Python (csrc/sr_python.cpp)
 SOURCES = ["sr_compile.cpp", "sr_api.cu", "sr_input.cu", "sr_direct.cu", "sr_tc.cu", "sr_resident.cu", "sr_dense.cu",
            "sr_norm.cu", "sr_product.cu", "sr_memory.cu", "sr_chunks.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -15,9 +16,9 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a",
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(EXTENSION):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(EXTENSION))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "sr_rollout.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -45,7 +46,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.check_call([nvcc, "-shared", "-cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a",
                            "-o", tmp] + objs)
     os.replace(tmp, LIB)
+    build_extension()
     return LIB
+
+
+def build_extension() -> str:
+    """Compiles the CPython extension against the installed PyTorch; it finds the library beside it."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    include = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), "/usr/local/cuda/include",
+               sysconfig.get_paths()["include"]]
+    tmp = EXTENSION + ".%d.tmp" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+                           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] + ["-I" + i for i in include] +
+                          [os.path.join(CSRC, "sr_python.cpp"), "-o", tmp, "-L" + HERE, "-l:libsr_rollout.so", "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch",
+                           "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(base, "lib")])
+    os.replace(tmp, EXTENSION)
+    return EXTENSION
 
 
 if __name__ == "__main__":

@@ -1,6 +1,7 @@
 """Operators of the temporal head behind a rollout (the sr_microscale_*, sr_rms_norm and sr_linear_attention_* calls of include/sr_rollout.h).
 
-Argument marshalling only, like `Graph`: tensors live on a CUDA device, work goes to the current stream of that device, outputs and
+Argument marshalling only, like `Graph`, and a call's common case in compiled code (csrc/sr_python.cpp; what that does not take comes back
+here to be done or refused): tensors live on a CUDA device, work goes to the current stream of that device, outputs and
 workspaces come from PyTorch's allocator, and every refusal is an `SrError`.  There is no backward pass: a tensor that
 requires a gradient is refused while gradients are recorded.
 
@@ -19,6 +20,14 @@ import torch
 
 from . import binding
 from .binding import SrError
+
+binding.load_library()
+try:
+    from . import _operators as _compiled
+except ImportError:                                    # not built yet
+    from . import build as _build
+    _build.build()
+    from . import _operators as _compiled
 
 FORMATS = {"mx8": 2, "mx4": 3}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
@@ -156,6 +165,13 @@ class Microscaled:
 
 def quantize(x, format: str = "mx4") -> Microscaled:
     """x [rows][cols] (float32 or bfloat16; rows may have gaps between them) in a microscaled format."""
+    fast = _compiled.quantize(x, FORMATS.get(format, 0))
+    if fast is not None:
+        m = Microscaled.__new__(Microscaled)
+        m.data, m.scales = fast
+        m.rows, m.cols = x.shape
+        m.format = format
+        return m
     device = _tensors("quantize", x)
     stride = _rows("quantize", "x", x)
     m = Microscaled._like(x, x.shape[0], x.shape[1], format)
@@ -169,6 +185,10 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
     gaps between them) is written in place of a new tensor of `dtype`."""
     if a.format != w.format or a.cols != w.cols:
         _refuse("product", "both matrices have the same format and number of columns")
+    fast = _compiled.product(a.data, a.scales, a.rows, w.data, w.scales, w.rows, a.cols, FORMATS[a.format], bias, relu, _DTYPES.get(dtype, -1), out) \
+        if out is not None or dtype in _DTYPES else None
+    if fast is not None:
+        return fast
     device = _tensors("product", a.data, a.scales, w.data, w.scales, bias, out)
     b = _float_vector("product", "bias", bias, w.rows)
     if out is None:
@@ -188,6 +208,16 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
 def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, format: Optional[str] = None):
     """s = x + residual, s / sqrt(mean(s^2) + eps) * weight for every row of x [rows][cols].  The output has x's type, or is `Microscaled` where
     a format is given; with a residual the result is (output, s rounded to x's type)."""
+    fast = _compiled.rms_norm(x, weight, residual, eps, 0 if format is None else FORMATS[format]) if format is None or format in FORMATS else None
+    if fast is not None:
+        out, total = fast
+        if format is not None:
+            m = Microscaled.__new__(Microscaled)
+            m.data, m.scales = out
+            m.rows, m.cols = x.shape
+            m.format = format
+            out = m
+        return out if residual is None else (out, total)
     device = _tensors("rms_norm", x, weight, residual)
     xs = _rows("rms_norm", "x", x)
     rows, cols = x.shape
@@ -275,6 +305,9 @@ def linear_attention_run(q, k, v, log_decay, state=None, offsets=None, scale: fl
     [frames][heads][size], sequence b the frames offsets[b] .. offsets[b + 1] - 1.  state: float32 [sequences][groups][dk][dv] before the first
     frame (None: zeros).  `out` (without gaps; frames that no sequence has keep what it holds) and `state_out` (may be `state`) are written in
     place of new tensors."""
+    fast = _compiled.run(q, k, v, log_decay, state, offsets, scale, out, state_out)
+    if fast is not None:
+        return (fast[0] if out is None else out), (fast[1] if state_out is None else state_out)
     call = "linear_attention_run"
     device = _tensors(call, q, k, v, log_decay, state, offsets, out, state_out)
     packed = offsets is not None
@@ -300,6 +333,9 @@ def linear_attention_run(q, k, v, log_decay, state=None, offsets=None, scale: fl
 def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0):
     """One frame of every sequence: q [sequences][heads][dk], k [..][groups][dk], v [..][groups][dv], log_decay [groups] or [sequences][groups].
     `state` (float32 [sequences][groups][dk][dv]) is updated in place; returns out [sequences][heads][dv]."""
+    fast = _compiled.step(q, k, v, log_decay, state, scale)
+    if fast is not None:
+        return fast
     call = "linear_attention_step"
     device = _tensors(call, q, k, v, log_decay, state)
     if q.dim() != 3 or v.dim() != 3:

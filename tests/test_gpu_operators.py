@@ -365,6 +365,27 @@ def test_calls_are_captured_and_replayed_on_another_stream():
         assert not torch.equal(got[0], other[0])
 
 
+def test_calls_without_the_compiled_marshalling_give_the_same(monkeypatch):
+    q, k, v, d = inputs((70, 2), 4, 2, 64, 48, "bf16", True)
+    x, w = torch.randn(9, 200, generator=gen(33), device=DEV), torch.rand(200, generator=gen(34), device=DEV)
+
+    def calls():
+        state = torch.ones(2, 2, 64, 48, device=DEV)
+        out, last = sr.linear_attention_run(q, k, v, d, state=state, scale=0.3)
+        flat = [t.flatten(0, 1) for t in (q, k, v, d)]
+        packed = sr.linear_attention_run(*flat, offsets=torch.tensor([0, 30, 140], device=DEV), state=state, out=torch.zeros(140, 4, 48, dtype=torch.bfloat16, device=DEV))
+        one = sr.linear_attention_step(q[0], k[0], v[0], d[0], last)
+        m, total = sr.rms_norm(x, w, residual=x, format="mx8")
+        n = sr.quantize(x, "mx8")
+        return [out, last, one, *packed, m.values(), total, sr.rms_norm(x), n.values(), sr.product(m, n, bias=w[:9].contiguous(), relu=True, dtype=torch.float32),
+                sr.product(m, n, out=torch.zeros(9, 12, dtype=torch.bfloat16, device=DEV)[:, :9])]
+    want = calls()
+    for name in ("quantize", "product", "rms_norm", "run", "step"):
+        monkeypatch.setattr(sr.operators._compiled, name, lambda *_: None)
+    for a, b in zip(calls(), want):
+        assert torch.equal(a, b)
+
+
 def test_refusals():
     q, k, v, d = inputs((4, 2), 4, 2, 64, 64, "bf16", True)
     state = torch.zeros(2, 2, 64, 64, device=DEV)
