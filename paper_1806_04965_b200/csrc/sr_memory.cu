@@ -438,6 +438,8 @@ sr_status check(const sr_attention_desc* d)
     if (d->dk > 256 || d->heads / d->groups > 128) return SR_ERR_UNSUPPORTED;
     return SR_OK;
 }
+// (overlaps of other kinds are the caller's to avoid)
+bool apart(const void* out, const void* q, const void* k, const void* v) { return !out || (out != q && out != k && out != v); }
 bool aligned(const void* p, int dtype) { return !((uintptr_t)p & (dtype == SR_DTYPE_F32 ? 3 : 1)); }
 
 AttentionArgs arguments(const sr_attention_desc* d, const void* q, const void* k, const void* v, const float* decay, void* out)
@@ -485,7 +487,7 @@ sr_status sr_linear_attention_run(const sr_attention_desc* d, const void* q, con
     if (!d->batch) return SR_OK;
     if (((uintptr_t)state_in & 3) || ((uintptr_t)state_out & 3) || ((uintptr_t)offsets & 7)) return SR_ERR_INVALID_ARG;
     if (d->frames && (!q || !k || !v || !decay || !out || !aligned(q, d->dtype) || !aligned(k, d->dtype) || !aligned(v, d->dtype) || !aligned(out, d->dtype) ||
-                      ((uintptr_t)decay & 3)))
+                      ((uintptr_t)decay & 3) || !apart(out, q, k, v)))
         return SR_ERR_INVALID_ARG;
     const bool chunks = sr_chunks_wanted(d) && sr_chunks_fit(d, offsets != nullptr, q, k, v);
     const AttentionCut cut = chunks ? sr_chunks_cut(d, offsets != nullptr) : frames_cut(d, offsets != nullptr);
@@ -513,7 +515,7 @@ sr_status sr_linear_attention_step(const sr_attention_desc* d, const void* q, co
     if (st != SR_OK) return st;
     if (!d->batch) return SR_OK;
     if (!q || !k || !v || !decay || !state || !out || !aligned(q, d->dtype) || !aligned(k, d->dtype) || !aligned(v, d->dtype) ||
-        !aligned(out, d->dtype) || ((uintptr_t)decay & 3) || ((uintptr_t)state & 3))
+        !aligned(out, d->dtype) || ((uintptr_t)decay & 3) || ((uintptr_t)state & 3) || !apart(out, q, k, v))
         return SR_ERR_INVALID_ARG;
     AttentionArgs A = arguments(d, q, k, v, decay, out);
     A.state_out = state;

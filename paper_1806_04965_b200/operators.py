@@ -409,12 +409,15 @@ class TemporalHead:
         m, _ = rms_norm(y, self._w["norm_h"], residual=x, eps=self.eps, format=self.format)
         return product(m, self._w["out"], bias=self._w["bias"], dtype=torch.float32)
 
+    def _fits(self, call: str, features, lead: int):
+        if features.dim() <= lead or features.shape[lead - 1] != self.batch or math.prod(features.shape[lead:]) != self.channels:
+            _refuse("TemporalHead." + call, "the head takes %s[%d sequences][%d channels]" % ("[frames]" if lead == 2 else "", self.batch, self.channels))
+
     @torch.no_grad()
     def run(self, features):
         """features [frames][batch][...channels] (float32 or the head's type) -> float32 [frames][batch][outputs]."""
+        self._fits("run", features, 2)
         T, B = features.shape[:2]
-        if B != self.batch:
-            _refuse("TemporalHead.run", "the head has %d sequences" % self.batch)
         x = features.reshape(T * B, self.channels).to(self.tdtype)
         q, k, v = self._attend(x)
         o, _ = linear_attention_run(q.unflatten(0, (T, B)).unflatten(2, (self.heads, self.dk)), k.unflatten(0, (T, B)).unflatten(2, (self.groups, self.dk)),
@@ -425,8 +428,7 @@ class TemporalHead:
     @torch.no_grad()
     def step(self, features):
         """features [batch][...channels] of one frame -> float32 [batch][outputs]."""
-        if features.shape[0] != self.batch:
-            _refuse("TemporalHead.step", "the head has %d sequences" % self.batch)
+        self._fits("step", features, 1)
         x = features.reshape(self.batch, self.channels).to(self.tdtype)
         q, k, v = self._attend(x)
         o = linear_attention_step(q.unflatten(1, (self.heads, self.dk)), k.unflatten(1, (self.groups, self.dk)), v.unflatten(1, (self.groups, self.dv)),

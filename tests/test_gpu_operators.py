@@ -305,6 +305,21 @@ def test_step(B, heads, groups, dk, dv, dtype):
             within(state[b], S, 8 * 2.0 ** -23 * A)
 
 
+def test_runs_without_frames_or_sequences():
+    for dtype in ("bf16", "fp32"):
+        q, k, v, d = inputs((0, 3), 2, 2, 64, 64, dtype, True)
+        state = torch.randn(3, 2, 64, 64, generator=gen(28), device=DEV)
+        out, last = sr.linear_attention_run(q, k, v, d, state=state)
+        assert out.shape == (0, 3, 2, 64) and torch.equal(last, state)
+        assert (sr.linear_attention_run(q, k, v, d)[1] == 0).all()
+        out, last = sr.linear_attention_run(q[:, 0], k[:, 0], v[:, 0], d[:, 0], offsets=torch.zeros(4, dtype=torch.int64, device=DEV), state=state)
+        assert torch.equal(last, state)
+        q, k, v, d = inputs((40,), 2, 2, 64, 64, dtype, True)
+        out, last = sr.linear_attention_run(q, k, v, d, offsets=torch.zeros(1, dtype=torch.int64, device=DEV), out=torch.full((40, 2, 64), 3.0, dtype=TYPES[dtype], device=DEV))
+        assert last.shape == (0, 2, 64, 64) and (out == 3).all()
+        assert sr.linear_attention_step(q[:0], k[:0], v[:0], d[:0], last).shape == (0, 2, 64)
+
+
 def test_steps_are_a_run():
     T, B, H, dk, dv = 150, 2, 2, 64, 64
     q, k, v, d = inputs((T, B), H, H, dk, dv, "fp32", True)
@@ -365,6 +380,49 @@ def test_calls_are_captured_and_replayed_on_another_stream():
         assert not torch.equal(got[0], other[0])
 
 
+def test_infinite_values_give_what_the_formula_gives():
+    # +inf in the values: earlier frames do not see it, later ones are infinite with the weights' signs or NaN where those meet
+    T, D = 150, 64
+    for dtype in ("bf16", "fp32"):
+        q, k, v, d = inputs((T, 1), 1, 1, D, D, dtype, False)
+        q, k = q.abs(), k.abs()
+        clean, _ = sr.linear_attention_run(q, k, v, d)
+        v[40, 0, 0, 3], v[140, 0, 0, 9] = float("inf"), float("-inf")
+        out, last = sr.linear_attention_run(q, k, v, d)
+        assert torch.equal(out[:40], clean[:40])
+        assert (out[40:, 0, 0, 3] == float("inf")).all() and (out[140:, 0, 0, 9] == float("-inf")).all() and torch.equal(out[:140, 0, 0, 9], clean[:140, 0, 0, 9])
+        assert (last[0, 0, :, 3] == float("inf")).all() and (last[0, 0, :, 9] == float("-inf")).all()
+
+
+def test_first_calls_of_a_process_may_be_captured():
+    import subprocess
+    import sys
+    code = """
+import torch
+import paper_1806_04965_b200 as sr
+q = torch.randn(200, 2, 2, 64, device="cuda:0").bfloat16()
+d = -torch.rand(2, device="cuda:0")
+x = torch.randn(20, 256, device="cuda:0").bfloat16()
+g = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(g):
+    out, last = sr.linear_attention_run(q, q, q, d)
+    one = sr.linear_attention_step(q[0], q[0], q[0], d, last)
+    m = sr.rms_norm(x, format="mx4")
+    y = sr.product(m, sr.quantize(x))
+g.replay()
+torch.cuda.synchronize()
+want = sr.linear_attention_run(q, q, q, d)
+assert torch.equal(out, want[0])
+assert torch.equal(y, sr.product(sr.rms_norm(x, format="mx4"), sr.quantize(x)))
+print("ok")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=root)
+    assert out.returncode == 0 and out.stdout.strip() == "ok", out.stderr[-1500:]
+
+
 def test_calls_without_the_compiled_marshalling_give_the_same(monkeypatch):
     q, k, v, d = inputs((70, 2), 4, 2, 64, 48, "bf16", True)
     x, w = torch.randn(9, 200, generator=gen(33), device=DEV), torch.rand(200, generator=gen(34), device=DEV)
@@ -398,7 +456,7 @@ def test_refusals():
                 lambda: sr.linear_attention_run(q.clone().requires_grad_(), k, v, d), lambda: sr.quantize(q[0, 0].t()), lambda: sr.quantize(q[0, 0].half()), lambda: sr.quantize(q[0, 0], "mx6"),
                 lambda: sr.rms_norm(q[0, 0], torch.ones(63, device=DEV)), lambda: sr.rms_norm(q[0, 0], residual=q[0, 0].float()),
                 lambda: sr.product(sr.quantize(q[0, 0]), sr.quantize(q[0, 0], "mx8")), lambda: sr.product(sr.quantize(q[0, 0]), sr.quantize(q[0, 0]), bias=torch.ones(3, device=DEV)),
-                lambda: sr.product(sr.quantize(q[0, 0]), sr.quantize(q[0, 0]), dtype=torch.float16)):
+                lambda: sr.product(sr.quantize(q[0, 0]), sr.quantize(q[0, 0]), dtype=torch.float16), lambda: sr.linear_attention_run(k, k, v, d, out=v)):
         with pytest.raises(SrError):
             bad()
     assert torch.isfinite(sr.linear_attention_run(q, k, v, d)[0].float()).all()

@@ -11,6 +11,7 @@ from tests import operator_oracle as oracle
 
 INVALID, UNSUPPORTED = 1, 5
 P = ctypes.c_void_p(1 << 20)                      # never read: every call here is refused, or has nothing to do
+P2 = ctypes.c_void_p(1 << 21)
 
 
 def desc(dtype=1, batch=2, heads=4, groups=2, dk=64, dv=64, frames=8, **strides):
@@ -20,11 +21,11 @@ def desc(dtype=1, batch=2, heads=4, groups=2, dk=64, dv=64, frames=8, **strides)
     return d
 
 
-def run(d, q=P, k=P, v=P, decay=P, offsets=None, s_in=None, s_out=None, out=P, ws=None, size=0):
+def run(d, q=P, k=P, v=P, decay=P, offsets=None, s_in=None, s_out=None, out=P2, ws=None, size=0):
     return ops._library().sr_linear_attention_run(ctypes.byref(d) if d else None, q, k, v, decay, offsets, s_in, s_out, out, ws, size, None)
 
 
-def step(d, q=P, k=P, v=P, decay=P, state=P, out=P):
+def step(d, q=P, k=P, v=P, decay=P, state=P, out=P2):
     return ops._library().sr_linear_attention_step(ctypes.byref(d) if d else None, q, k, v, decay, state, out, None)
 
 
@@ -39,6 +40,8 @@ def test_attention_refuses_sizes_and_pointers(call):
     for name in ("q", "k", "v", "decay", "out"):
         assert call(desc(), **{name: None}) == INVALID, name
         assert call(desc(), **{name: ctypes.c_void_p((1 << 20) + 1)}) == INVALID, name
+    for name in ("q", "k", "v"):
+        assert call(desc(), **{name: P2}) == INVALID, name            # the outputs would lie on them
     assert call(desc(batch=0)) == 0
 
 
