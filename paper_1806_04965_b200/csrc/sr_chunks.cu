@@ -66,10 +66,10 @@ struct alignas(16) Decays {                            // of a chunk (read four 
     float col[kChunk];                                 // exp(G_e - G_j), e the last frame of j's 32
     float rest[kChunk];                                // exp(G_last - G_j)
     float row[kChunk];                                 // exp(G_i)
-    uint32_t odd[kWorkers];                            // columns of the chunk's values that are not all finite: 16 bits for [columns / 16][rows / 32]
     float whole;                                       // exp(G_last)
+    uint32_t odd;                                      // 1: some of the chunk's values are not finite
 };
-static_assert(offsetof(Decays, odd) % 16 == 0 && sizeof(Decays) % 16 == 0, "read as 16-byte words");
+static_assert(sizeof(Decays) % 16 == 0, "read as 16-byte words");
 
 // What follows is out of line: it is rarely run, and the loop that every chunk goes through has to stay small.
 
@@ -103,18 +103,14 @@ __device__ __noinline__ void store_row(const AttentionArgs& A, const Decays& D, 
         }
     }
 }
-// Takes what is not finite out of a thread's 16 values and says in which columns its warp had any.
-__device__ __noinline__ uint32_t clear_odd(uint4* first, uint4* second)
+// Takes what is not finite out of a thread's 16 values.
+__device__ __noinline__ void clear_odd(uint4* first, uint4* second)
 {
-    uint32_t cols = 0;
 #pragma unroll 1
     for (int e = 0; e < 16; ++e) {
         uint16_t* p = reinterpret_cast<uint16_t*>(e < 8 ? first : second) + (e & 7);
-        const bool is = (*p & 0x7F80u) == 0x7F80u;
-        if (is) *p = 0;
-        if (__any_sync(0xFFFFFFFFu, is)) cols |= 1u << e;
+        if ((*p & 0x7F80u) == 0x7F80u) *p = 0;
     }
-    return cols;
 }
 // 16 values of a state's row between global memory and two TMEM lanes' registers.
 __device__ __noinline__ void load_state(const float* from, int j0, int dv, uint32_t taddr)
@@ -306,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                         if (!ok) break;
                         tc_fence_after();
                         for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kWeights + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
-                        tc_commit(answered);
+                        if (c + 1 == chunks && h + 1 == share) tc_commit(answered);
                     }
                     if (h + 1 == share) tc_commit(v_empty + 8 * (c & 1));
                     if (h + 1 < share) {
@@ -380,8 +376,12 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             reinterpret_cast<float4*>(D.col)[lane] = col;
             reinterpret_cast<float4*>(D.rest)[lane] = rest;
             reinterpret_cast<float4*>(D.row)[lane] = row;
-            if (lane == 0) D.whole = rounded;
-            __syncwarp();
+            if (lane == 0) {
+                D.whole = rounded;
+                D.odd = 0;
+            }
+            // (the workers wait for both at once)
+            if (!mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up)) break;
             if (lane == 0) mbar_arrive(d_full + 8 * slot);
         }
         if (MODE == 1 && lane == 0 && it.c0 == 0) C.S.decays[(int64_t)it.slot * A.groups + it.g] = (float)exp(log_whole);
@@ -406,8 +406,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         // Outputs of the step before; meanwhile: with them the state for the far products (those that read the one before are done when the outputs are there).
         auto output = [&](int c, int h, bool meanwhile) {
             const Decays& D = decays[c % kDecays];
-            if (!mbar_wait_warp(answered, (n - 1) & 1, gave_up)) return false;
-            tc_fence_after();
             uint32_t a[16], x[16], z[8];
             tc_ld(tmem + lanes + kFar + u * 16, tmem + lanes + kNear + u * 16, a, x);
             tc_fence_before();
@@ -417,9 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] = round_bf16(fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, pair(a[2 * e], a[2 * e + 1]))));
-            const uint4* odds = reinterpret_cast<const uint4*>(D.odd);
-            const uint4 o0 = odds[0], o1 = odds[1], o2 = odds[2], o3 = odds[3];
-            const bool odd = o0.x | o0.y | o0.z | o0.w | o1.x | o1.y | o1.z | o1.w | o2.x | o2.y | o2.z | o2.w | o3.x | o3.y | o3.z | o3.w;
+            const bool odd = D.odd != 0;
             const bool copies = C.out_copies && !odd && !(clean && c + 1 == chunks);
             if (copies) {
                 // through shared memory, every warp its own box: a thread's stores would be 32 bytes of a row each
@@ -438,7 +434,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 if (meanwhile) mbar_arrive(stated);
                 if (copies) tma_store_4d(&C.out_map, o_tile + (warp - 4) * 1024, j0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk + w * 32));
             }
-            return true;
         };
         // Ahead of the first chunk: the state as the first of its three parts, zeros for the others and for the weights behind the diagonal.
         const uint32_t state = tmem + kState + lanes + u * 16;
@@ -458,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             Decays& D = decays[slot];
             uint32_t a[8], b[8], d[8];                 // parts of V'
             uint8_t* const v = v_mem + (c & 1) * VT;
-            ok = mbar_wait_warp(v_full + 8 * (c & 1), (c >> 1) & 1, gave_up);
+            ok = mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);          // decays and values
             if (clean && c + 1 == chunks) {
                 ok = ok && mbar_wait_warp(k_full + 8 * (c % NK), (c / NK) & 1, gave_up);
                 if (!ok) break;
@@ -475,7 +470,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(cleaned);
             }
-            ok = ok && mbar_wait_warp(d_full + 8 * slot, (c / kDecays) & 1, gave_up);
             if (!ok) break;
             const Pair weight = pair(D.rest[i], D.rest[i]);
             __nv_bfloat162 odd = __floats2bfloat162_rn(0.0f, 0.0f);      // NaN as soon as a value is not finite
@@ -493,18 +487,15 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     d[4 * q + e] = round_bf16(fma2(widen_bf16(b[4 * q + e]), minus, y));
                 }
             }
-            if (OUT) {
-                uint32_t cols = 0;
-                if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
-                    cols = clear_odd(reinterpret_cast<uint4*>(v + place0), reinterpret_cast<uint4*>(v + place1));
+            if (OUT && __any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&odd) & 0x7FFF7FFFu)) {
+                clear_odd(reinterpret_cast<uint4*>(v + place0), reinterpret_cast<uint4*>(v + place1));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {                        // the first part says what has to be said; what is left over is NaN
-                        const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
-                        b[e] &= keep;
-                        d[e] &= keep;
-                    }
+                for (int e = 0; e < 8; ++e) {                            // the first part says what has to be said; what is left over is NaN
+                    const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                    b[e] &= keep;
+                    d[e] &= keep;
                 }
-                if (lane == 0) D.odd[u * 4 + w] = cols;
+                D.odd = 1;
             }
             if (c > 0) {
                 ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
@@ -544,9 +535,12 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 continue;
             }
             for (int h = 0; h < share && ok; ++h, ++n) {
+                // (the scores come behind the products of the step before: with them that step's outputs are there)
+                ok = mbar_wait_warp(scored, n & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
                 if (n > 0) {
-                    ok = output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1, h == 0);
-                    if (!ok) break;
+                    output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1, h == 0);
                     if (h == 0 && lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
                 } else {
                     state_there();
@@ -554,9 +548,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     __syncwarp();
                     if (lane == 0) mbar_arrive(stated);
                 }
-                ok = mbar_wait_warp(scored, n & 1, gave_up);
-                if (!ok) break;
-                tc_fence_after();
                 // scores -> P: two workers of a quarter have 16 columns of the diagonal's 32 each, the other two 16 of all 32s to its left
                 const float hi = D.hi[i], lo = D.lo[i];
                 const int half = (u & 1) * 16;
@@ -609,7 +600,10 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 store_state(to, j0, A.dv, state);
                 __syncwarp();
             }
-            if (OUT) output(chunks - 1, share - 1, false);
+            if (OUT && mbar_wait_warp(answered, 0, gave_up)) {
+                tc_fence_after();
+                output(chunks - 1, share - 1, false);
+            }
         }
         if (OUT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
