@@ -17,10 +17,12 @@
 //
 // (Persistent CTAs that walk over items, with a warp that hands them out, lost to one CTA per item but where every item is one chunk: 32 sequences of 128 frames, 8 heads of
 // 64 14.8 / 13.7 us, packed sequences 90 / 124 and 116 / 194.)
-// Bound by memory (q, k, v, out once) where there are CTAs enough: a chunk of DK = 128 is 96 KiB per CTA, 2.6k cycles of MMAs.
+// A chunk of DK = 128 is 96 KiB of loads and stores and 1.8k cycles of MMAs per CTA, 2.2k cycles' worth of memory with every SM at it, and takes 5.4k (4096 frames, 148 CTAs:
+// 92 us, 3.4 TB/s): what bounds it is the chain from one chunk to the next, values' parts -> sums -> state -> weights, which no other chunk of the CTA may overtake, and two CTAs
+// to an SM do not fit (208 KiB of tiles, all of TMEM).
 // Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; sixteen workers for everything between the MMAs.
 // What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
-// the near product (whose zeros would spread it to earlier frames) and added by the outputs' warps; rows behind a sequence's last frame are zeroed.
+// the near product (whose zeros would spread it to earlier frames) and added where the outputs are stored; rows behind a sequence's last frame are zeroed.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -391,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     } else if (warp >= 4) {
         // A worker has 32 rows (those of its quarter w of the TMEM lanes) and a quarter u of the columns of everything: frames' rows of V', of the scores and of the
         // outputs, rows of the state.  All of them do the same at the same time: warps with roles of their own, each with a loop of a few hundred
-        // instructions, waited for instructions a third of their time (4096 frames, 148 CTAs of DK = 128: 128 us, so ...).  While the tensor pipe sums a chunk's
+        // instructions, waited for instructions a third of their time (4096 frames, 148 CTAs of DK = 128: 128 us, and 92).  While the tensor pipe sums a chunk's
         // state they do the outputs of the step before, the weights of this one and the parts of the next chunk's values.
         const int w = warp & 3, u = (warp - 4) >> 2, i = w * 32 + lane, j0 = it.c0 + u * 16;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;

@@ -17,8 +17,8 @@ namespace {
 // frames).  The same chunks, of 16 frames:  out_i = scale * (exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j),
 // S' = exp(G_last) S + sum_j exp(G_last - G_j) k_j v_j^T, so that a state's value costs two fused multiply-adds per frame (q S and k v^T) and one product per chunk.
 // A CTA has 64 columns of a group's state: thread (row group, column group) ROWS x 4 values of it in registers, so that a frame's 2 * 4 * ROWS multiply-adds take
-// 2 * ROWS / 4 + 1 loads of 16 bytes from shared memory.  Bound by the multiply-adds: 128 cycles per frame for dk = 128, besides the scores.  Before that, frame by
-// frame with a column per thread, 500 frames of 5 sequences, 6 heads of 40 and 72 took 320 us.
+// 2 * ROWS / 4 + 1 loads of 16 bytes from shared memory.  Bound by the issue of those: 512 frames of 32 sequences, 8 heads of 64, fp32 235 us, 16384 frames of one, 8 of
+// 128 660.  500 frames of 5 sequences, 6 heads of 40 and 72 on 3: 72 us; frame by frame, with a column per thread, 320.
 // (Two CTAs to an SM, 128 registers, for segments, which fill the device: 16384 frames, 8 heads of 128 755 -> 660 us; one, unlimited, for whole sequences, whose time is
 // that of one CTA: 512 frames x 16 sequences, 16 heads on 4 of 128 597, with two 800.)
 // The partial sums of q S over the row groups of a warp are added with a shuffle, those of the warps in shared memory.

@@ -1,5 +1,5 @@
 // The operators' calls from Python without ctypes and its marshalling: a call on small tensors is host time before anything else (one frame of one sequence 10.4 us
-// through ctypes, so ...).  Every function here checks its arguments, allocates the outputs, calls the C ABI and hands the outputs over; where anything is not as it has to
+// through ctypes, 4.8 here).  Every function here checks its arguments, allocates the outputs, calls the C ABI and hands the outputs over; where anything is not as it has to
 // be it returns None and has done nothing, and operators.py, which knows the same rules, says what is wrong.
 #include <Python.h>
 
@@ -45,6 +45,13 @@ bool rows_of(const at::Tensor& t, int64_t& stride)
 bool floats(const at::Tensor* t, int64_t n) { return t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == n && t->is_contiguous(); }
 
 PyObject* none() { Py_RETURN_NONE; }
+// Without the interpreter's lock: an allocation or a launch may have to wait for the device, which may wait for another thread's launch.
+struct Unlocked {
+    PyThreadState* const state = PyEval_SaveThread();
+    Unlocked() = default;
+    Unlocked(const Unlocked&) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
 PyObject* two(PyObject* a, PyObject* b)
 {
     PyObject* r = a && b ? PyTuple_New(2) : nullptr;
@@ -88,9 +95,14 @@ PyObject* py_quantize(PyObject*, PyObject* const* a, Py_ssize_t n)
         Device d;
         int64_t stride;
         if (!d.fits(x) || !d.current() || !rows_of(*x, stride)) return none();
-        Scaled m = new_scaled(*x, x->size(0), x->size(1), format);
-        if (sr_microscale_quantize(x->data_ptr(), type_of(*x), x->size(0), x->size(1), stride, format, m.data.data_ptr(), m.scales.data_ptr(), d.stream()) != SR_OK)
-            return none();
+        Scaled m;
+        sr_status st;
+        {
+            Unlocked u;
+            m = new_scaled(*x, x->size(0), x->size(1), format);
+            st = sr_microscale_quantize(x->data_ptr(), type_of(*x), x->size(0), x->size(1), stride, format, m.data.data_ptr(), m.scales.data_ptr(), d.stream());
+        }
+        if (st != SR_OK) return none();
         return two(wrap(m.data), wrap(m.scales));
     })
 }
@@ -112,12 +124,15 @@ PyObject* py_product(PyObject*, PyObject* const* a, Py_ssize_t n)
         if (a[11] != Py_None) {
             if (!d.fits(given) || outs < 1 || !rows_of(*given, stride) || given->size(0) != rows || given->size(1) != outs) return none();
             out = *given;
-        } else {
-            out = at::empty({rows, outs}, ad->options().dtype(dtype == SR_DTYPE_F32 ? at::kFloat : at::kBFloat16));
         }
-        if (sr_microscale_product(ad->data_ptr(), as->data_ptr(), wd->data_ptr(), ws->data_ptr(), format, rows, cols, outs,
-                                  bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, relu ? 1 : 0, out.data_ptr(), type_of(out), stride, d.stream()) != SR_OK)
-            return none();
+        sr_status st;
+        {
+            Unlocked u;
+            if (!given) out = at::empty({rows, outs}, ad->options().dtype(dtype == SR_DTYPE_F32 ? at::kFloat : at::kBFloat16));
+            st = sr_microscale_product(ad->data_ptr(), as->data_ptr(), wd->data_ptr(), ws->data_ptr(), format, rows, cols, outs,
+                                       bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, relu ? 1 : 0, out.data_ptr(), type_of(out), stride, d.stream());
+        }
+        if (st != SR_OK) return none();
         return wrap(out);
     })
 }
@@ -141,16 +156,19 @@ PyObject* py_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
         const int64_t rows = x->size(0), cols = x->size(1);
         if (a[1] != Py_None && (!d.fits(w) || !floats(w, cols))) return none();
         if (a[2] != Py_None && (!d.fits(r) || !rows_of(*r, rs) || r->size(0) != rows || r->size(1) != cols || r->scalar_type() != x->scalar_type())) return none();
-        at::Tensor sum;
-        if (r) sum = at::empty({rows, cols}, x->options());
-        at::Tensor out;
+        at::Tensor sum, out;
         Scaled m;
-        if (format) m = new_scaled(*x, rows, cols, format);
-        else out = at::empty({rows, cols}, x->options());
-        if (sr_rms_norm(x->data_ptr(), r ? r->data_ptr() : nullptr, w ? static_cast<const float*>(w->data_ptr()) : nullptr, (float)eps, type_of(*x), rows, cols, xs, rs,
-                        r ? sum.data_ptr() : nullptr, format ? m.data.data_ptr() : out.data_ptr(), format ? format : type_of(*x),
-                        format ? m.scales.data_ptr() : nullptr, d.stream()) != SR_OK)
-            return none();
+        sr_status st;
+        {
+            Unlocked u;
+            if (r) sum = at::empty({rows, cols}, x->options());
+            if (format) m = new_scaled(*x, rows, cols, format);
+            else out = at::empty({rows, cols}, x->options());
+            st = sr_rms_norm(x->data_ptr(), r ? r->data_ptr() : nullptr, w ? static_cast<const float*>(w->data_ptr()) : nullptr, (float)eps, type_of(*x), rows, cols, xs, rs,
+                             r ? sum.data_ptr() : nullptr, format ? m.data.data_ptr() : out.data_ptr(), format ? format : type_of(*x),
+                             format ? m.scales.data_ptr() : nullptr, d.stream());
+        }
+        if (st != SR_OK) return none();
         PyObject* first = format ? two(wrap(m.data), wrap(m.scales)) : wrap(out);
         PyObject* second = r ? wrap(sum) : none();
         return two(first, second);
@@ -219,11 +237,16 @@ PyObject* py_step(PyObject*, PyObject* const* a, Py_ssize_t n)
         if (!describe(d, dev, q, k, v, decay, 1, true, scale) || q->size(0) > 0x7FFFFFFF) return none();
         d.batch = (int32_t)q->size(0);
         if (!state_fits(dev, state, d)) return none();
-        const at::Tensor out = at::empty({d.batch, d.heads, d.dv}, q->options());
         d.out = {0, (int64_t)d.heads * d.dv, d.dv};
-        if (sr_linear_attention_step(&d, q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const float*>(decay->data_ptr()), static_cast<float*>(state->data_ptr()),
-                                     out.data_ptr(), dev.stream()) != SR_OK)
-            return none();
+        at::Tensor out;
+        sr_status st;
+        {
+            Unlocked u;
+            out = at::empty({d.batch, d.heads, d.dv}, q->options());
+            st = sr_linear_attention_step(&d, q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const float*>(decay->data_ptr()),
+                                          static_cast<float*>(state->data_ptr()), out.data_ptr(), dev.stream());
+        }
+        if (st != SR_OK) return none();
         return wrap(out);
     })
 }
@@ -259,18 +282,23 @@ PyObject* py_run(PyObject*, PyObject* const* a, Py_ssize_t n)
             for (int i = 0; i < q->dim(); ++i)
                 if (given->size(i) != (i + 1 < q->dim() ? q->size(i) : d.dv)) return none();
             out = *given;
-        } else {
-            out = packed ? at::empty({q->size(0), d.heads, d.dv}, q->options()) : at::empty({q->size(0), batch, d.heads, d.dv}, q->options());
         }
-        const at::Tensor last = to ? *to : at::empty({batch, d.groups, d.dk, d.dv}, q->options().dtype(at::kFloat));
-        size_t bytes = 0;
-        if (sr_linear_attention_workspace_bytes(&d, packed ? 1 : 0, &bytes) != SR_OK) return none();
-        at::Tensor work;
-        if (bytes) work = at::empty({(int64_t)bytes}, q->options().dtype(at::kByte));
-        if (sr_linear_attention_run(&d, q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const float*>(decay->data_ptr()),
-                                    packed ? static_cast<const int64_t*>(offsets->data_ptr()) : nullptr, state ? static_cast<const float*>(state->data_ptr()) : nullptr,
-                                    static_cast<float*>(last.data_ptr()), out.data_ptr(), bytes ? work.data_ptr() : nullptr, bytes, dev.stream()) != SR_OK)
-            return none();
+        at::Tensor last = to ? *to : at::Tensor();
+        sr_status st;
+        {
+            Unlocked u;
+            if (!given) out = packed ? at::empty({q->size(0), d.heads, d.dv}, q->options()) : at::empty({q->size(0), batch, d.heads, d.dv}, q->options());
+            if (!to) last = at::empty({batch, d.groups, d.dk, d.dv}, q->options().dtype(at::kFloat));
+            size_t bytes = 0;
+            st = sr_linear_attention_workspace_bytes(&d, packed ? 1 : 0, &bytes);
+            at::Tensor work;
+            if (st == SR_OK && bytes) work = at::empty({(int64_t)bytes}, q->options().dtype(at::kByte));
+            if (st == SR_OK)
+                st = sr_linear_attention_run(&d, q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const float*>(decay->data_ptr()),
+                                             packed ? static_cast<const int64_t*>(offsets->data_ptr()) : nullptr, state ? static_cast<const float*>(state->data_ptr()) : nullptr,
+                                             static_cast<float*>(last.data_ptr()), out.data_ptr(), bytes ? work.data_ptr() : nullptr, bytes, dev.stream());
+        }
+        if (st != SR_OK) return none();
         return two(wrap(out), wrap(last));
     })
 }
