@@ -344,6 +344,103 @@ def test_values_that_are_not_finite_stay_in_their_sequence_and_head():
         assert torch.equal(out[:, 0, 1][:, keep], clean[:, 0, 1][:, keep])
 
 
+# ------------------------------------------------------------------------------------------ places beyond 2^31 elements, inputs repeated by strides
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_frames_that_lie_far_apart(dtype):
+    T, B, H, D, gap = 300, 2, 2, 64, 7_500_000
+    q, k, v, d = inputs((T, B), H, H, D, D, dtype, True)
+    room = torch.empty(T * gap, dtype=TYPES[dtype], device=DEV)
+    far = []
+    for i, x in enumerate((q, k, v)):
+        far.append(room[i * 4096:].as_strided((T, B, H, D), (gap, H * D, D, 1)))
+        far[i].copy_(x)
+    out, last = sr.linear_attention_run(*far, d, scale=0.2)
+    check_run(q, k, v, d, None, out, last, 0.2, dtype, [(slice(None), b) for b in range(B)])
+
+
+def test_states_of_more_than_2_31_elements():
+    B, G, D, T = 2 ** 31 // (16 * 128 * 128) + 1, 16, 128, 16
+    state = torch.zeros(B, G, D, D, device=DEV)
+    state[-1].normal_(generator=gen(40))
+    was = state[-1:].clone()
+    q, k, v, d = inputs((B,), G, G, D, D, "bf16", False)
+    out = sr.linear_attention_step(q, k, v, d, state, scale=0.5)
+    want, S, mag, A = oracle.attention(host(q[-1:]), host(k[-1:]), host(v[-1:]), host(d), host(was[0]), 0.5)
+    within(out[-1:], want, 2.0 ** -8 * np.abs(want) + (D + 20) * 2.0 ** -23 * mag)
+    within(state[-1], S, 8 * 2.0 ** -23 * A)
+    was = state[-2:].clone()
+    q, k, v, d = inputs((T, B), G, G, D, D, "bf16", False)
+    out, _ = sr.linear_attention_run(q, k, v, d, state=state, scale=0.5, state_out=state)
+    check_run(q[:, -2:], k[:, -2:], v[:, -2:], d, was, out[:, -2:], state[-2:], 0.5, "bf16", [(slice(None), 0), (slice(None), 1)])
+
+
+def test_rows_beyond_2_31_elements():
+    rows, cols = 2 ** 16 + 131, 2 ** 15
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV).normal_(generator=gen(41))
+    w = torch.randn(cols, generator=gen(42), device=DEV)
+    out, total = sr.rms_norm(x, w, residual=x, eps=1e-5)
+    want, s = oracle.norm(host(x[-3:]), host(w), host(x[-3:]), 1e-5)
+    assert torch.equal(total[-3:], x[-3:] * 2)
+    within(out[-3:], want, (2.0 ** -8 + ((cols + 3) / 2 + 8) * 2.0 ** -23) * np.abs(want))        # (the sums of equal rows are exact)
+    del out, total
+    m = sr.quantize(x, "mx4")
+    few = sr.quantize(x[-131:].contiguous(), "mx4")              # (the first row of a tile of scales)
+    assert torch.equal(m.data[-131:], few.data)
+    full = (rows // 128 - 1) * (cols // 128) * 512               # the last two tiles of rows: 128 and 3 of them
+    a, b = m.scales[full:].view(2, -1, 32, 4, 4), few.scales.view(2, -1, 32, 4, 4)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1, :, :3, 0], b[1, :, :3, 0])
+    del m, few
+    narrow, wide = sr.quantize(x[:, :64], "mx8"), sr.quantize(x[:2 ** 15, :64], "mx8")
+    y = sr.product(narrow, wide)
+    va, vw = host(narrow.values()[-3:]), host(wide.values())
+    within(y[-3:], va @ vw.T, 2.0 ** -8 * np.abs(va @ vw.T) + 65 * 2.0 ** -23 * (np.abs(va) @ np.abs(vw).T))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_inputs_that_strides_repeat(dtype):
+    T, B, H, D = 140, 3, 4, 64
+    q, k, v, d = inputs((T, 1), H, H, D, D, dtype, True)
+    q = torch.randn(T, B, H, D, generator=gen(43), device=DEV).to(TYPES[dtype])
+    k, v, d = k.expand(T, B, H, D), v[:, :, :1].expand(T, B, H, D), d.expand(T, B, H)
+    out, last = sr.linear_attention_run(q, k, v, d, scale=0.2)
+    check_run(q, k, v, d, None, out, last, 0.2, dtype, [(slice(None), b) for b in range(B)])
+    state = torch.zeros(B, H, D, D, device=DEV)
+    one = sr.linear_attention_step(q[0], k[0], v[0], d[0], state, scale=0.2)
+    for b in range(B):
+        want, S, mag, A = oracle.attention(host(q[:1, b]), host(k[:1, b]), host(v[:1, b]), host(d[:1, b]), None, 0.2)
+        within(one[b:b + 1], want, oracle.HALF_STEP[dtype] * np.abs(want) + (D + 20) * 2.0 ** -23 * mag)
+        within(state[b], S, 8 * 2.0 ** -23 * A)
+
+
+def test_threads_call_at_the_same_time_on_their_own_streams():
+    import threading
+    cases = []
+    for i in range(4):
+        q, k, v, d = inputs((3000, 1), 2, 2, 64, 64, "bf16" if i % 2 else "fp32", True, seed=50 + i)     # (cut: with a workspace)
+        x = torch.randn(30 + i, 512, generator=gen(60 + i), device=DEV).bfloat16()
+        cases.append((q, k, v, d, x, sr.quantize(torch.randn(200, 512, generator=gen(70 + i), device=DEV))))
+
+    def calls(c):
+        out, last = sr.linear_attention_run(*c[:4])
+        return out, last, sr.linear_attention_step(c[0][0], c[1][0], c[2][0], c[3][0], last), sr.product(sr.rms_norm(c[4], format="mx4"), c[5])
+    want = [calls(c) for c in cases]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got = calls(cases[i])
+                torch.cuda.current_stream().synchronize()
+                bad.extend((i, n) for n, (a, b) in enumerate(zip(got, want[i])) if not torch.equal(a, b))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
 # ------------------------------------------------------------------------------------------ streams, graphs, refusals, the head
 def test_calls_are_captured_and_replayed_on_another_stream():
     T, B, H, D = 200, 2, 2, 64
