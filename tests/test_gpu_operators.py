@@ -88,7 +88,7 @@ def test_a_group_that_is_not_finite_stands_for_nans_and_touches_its_row_only(fmt
 @pytest.mark.parametrize("fmt", ["mx4", "mx8"])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows, cols, outs", [(1, 32, 1), (1, 1, 5), (3, 100, 17), (8, 4096, 128), (16, 1000, 1111), (33, 64, 130), (129, 129, 257), (300, 2048, 72),
-                                              (513, 96, 600), (1000, 288, 40), (70, 5000, 300), (2100, 160, 1300)])
+                                              (513, 96, 600), (1000, 288, 40), (70, 5000, 300), (2100, 160, 1300), (1900, 1000, 2600), (1000, 4100, 2700), (577, 2048, 8300)])
 def test_product(rows, cols, outs, fmt, dtype):
     a = torch.randn(rows, cols, generator=gen(5), device=DEV) * torch.exp(torch.randn(rows, cols, generator=gen(6), device=DEV))
     w = torch.randn(outs, cols, generator=gen(7), device=DEV)
