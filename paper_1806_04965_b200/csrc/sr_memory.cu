@@ -17,10 +17,10 @@ namespace {
 // frames).  The same chunks, of 16 frames:  out_i = scale * (exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j),
 // S' = exp(G_last) S + sum_j exp(G_last - G_j) k_j v_j^T, so that a state's value costs two fused multiply-adds per frame (q S and k v^T) and one product per chunk.
 // A CTA has 64 columns of a group's state: thread (row group, column group) ROWS x 4 values of it in registers, so that a frame's 2 * 4 * ROWS multiply-adds take
-// 2 * ROWS / 4 + 1 loads of 16 bytes from shared memory.  Bound by the issue of those: 512 frames of 32 sequences, 8 heads of 64, fp32 235 us, 16384 frames of one, 8 of
-// 128 660.  500 frames of 5 sequences, 6 heads of 40 and 72 on 3: 72 us; frame by frame, with a column per thread, 320.
-// (Two CTAs to an SM, 128 registers, for segments, which fill the device: 16384 frames, 8 heads of 128 755 -> 660 us; one, unlimited, for whole sequences, whose time is
-// that of one CTA: 512 frames x 16 sequences, 16 heads on 4 of 128 597, with two 800.)
+// 2 * ROWS / 4 + 1 loads of 16 bytes from shared memory.  Bound by the latency of those in few
+// warps (issue slots 31 % used with one CTA to an SM).  500 frames of 5 sequences, 6 heads of 40 and 72 on 3: 72 us; frame by frame, with a column per thread, 320.
+// Two CTAs to an SM, 128 registers, where there are more CTAs than SMs, segments always: 512 frames of 32 sequences, 8 heads of 64 248 -> 181 us, 16384 frames, 8 heads
+// of 128 755 -> 660; otherwise one, unlimited, since the time is that of one CTA: 512 frames of 16 sequences, 16 heads on 4 of 128 597, with two 800.
 // The partial sums of q S over the row groups of a warp are added with a shuffle, those of the warps in shared memory.
 constexpr int kFrames = 16, kRunCols = 64, kRunThreads = 256;
 
@@ -34,8 +34,9 @@ struct FramesShared {
     float whole;                                       // exp(G_last)
 };
 
-template <typename T, int DK, int MODE>                // DK: rows of the state, padded; MODE as in the tensor-core kernel: 0 whole, 1 sums of segments, 2 their outputs
-__global__ void __launch_bounds__(kRunThreads, MODE != 0 && DK <= 128 ? 2 : 1) sr_attention_frames_kernel(const __grid_constant__ SegmentArgs C)
+// DK: rows of the state, padded; MODE as in the tensor-core kernel: 0 whole, 1 sums of segments, 2 their outputs; HELD: CTAs of an SM
+template <typename T, int DK, int MODE, int HELD>
+__global__ void __launch_bounds__(kRunThreads, HELD) sr_attention_frames_kernel(const __grid_constant__ SegmentArgs C)
 {
     constexpr int ROWS = DK / 16;                      // of a thread
     constexpr bool OUT = MODE != 1;
@@ -252,12 +253,12 @@ __global__ void __launch_bounds__(kRunThreads, MODE != 0 && DK <= 128 ? 2 : 1) s
         }
 }
 
-template <typename T, int DK, int MODE>
+template <typename T, int DK, int MODE, int HELD>
 cudaError_t launch_frames(const SegmentArgs& C, cudaStream_t s)
 {
     constexpr int smem = (int)sizeof(FramesShared<DK>);
     static SrSharedLimit limit;
-    const cudaError_t e = limit.raise(sr_attention_frames_kernel<T, DK, MODE>, smem);
+    const cudaError_t e = limit.raise(sr_attention_frames_kernel<T, DK, MODE, HELD>, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -269,15 +270,17 @@ cudaError_t launch_frames(const SegmentArgs& C, cudaStream_t s)
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sr_attention_frames_kernel<T, DK, MODE>, C);
+    return cudaLaunchKernelEx(&cfg, sr_attention_frames_kernel<T, DK, MODE, HELD>, C);
 }
 template <typename T, int DK>
 cudaError_t launch_frames_cut(const SegmentArgs& C, cudaStream_t s)
 {
-    if (!C.segment) return launch_frames<T, DK, 0>(C, s);
-    cudaError_t e = launch_frames<T, DK, 1>(C, s);
+    constexpr int HELD = DK <= 128 ? 2 : 1;
+    if (!C.segment && (int64_t)C.A.batch * C.A.groups * C.v_tiles <= sr_device_sms()) return launch_frames<T, DK, 0, 1>(C, s);
+    if (!C.segment) return launch_frames<T, DK, 0, HELD>(C, s);
+    cudaError_t e = launch_frames<T, DK, 1, HELD>(C, s);
     if (e == cudaSuccess) e = sr_segments_launch(C, s);
-    return e == cudaSuccess ? launch_frames<T, DK, 2>(C, s) : e;
+    return e == cudaSuccess ? launch_frames<T, DK, 2, HELD>(C, s) : e;
 }
 template <typename T>
 cudaError_t launch_frames_any(const SegmentArgs& C, cudaStream_t s)

@@ -227,6 +227,15 @@ def test_run(T, B, heads, groups, dk, dv, gated, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T, B, heads, groups, dk, dv", [(9, 80, 4, 4, 25, 30), (15, 60, 4, 4, 64, 64), (33, 50, 6, 3, 128, 72), (7, 100, 2, 2, 200, 20)])
+def test_run_of_many_sequences(T, B, heads, groups, dk, dv, dtype):
+    q, k, v, d = inputs((T, B), heads, groups, dk, dv, dtype, True)
+    state = torch.randn(B, groups, dk, dv, generator=gen(28), device=DEV)
+    out, last = sr.linear_attention_run(q, k, v, d, state=state, scale=0.3)
+    check_run(q, k, v, d, state, out, last, 0.3, dtype, [(slice(None), b) for b in range(B)])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("lengths, heads, groups, dk, dv", [([0, 1, 130, 0, 64, 700, 3], 4, 2, 64, 64), ([5], 1, 1, 128, 128), ([0, 0], 2, 2, 64, 64), ([1] * 9, 2, 1, 40, 24),
                                                             ([900, 2, 0, 129], 2, 2, 128, 128)])
 def test_run_of_packed_sequences(lengths, heads, groups, dk, dv, dtype):
