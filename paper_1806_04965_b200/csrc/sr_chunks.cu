@@ -143,10 +143,14 @@ __device__ __noinline__ void store_state(float* to, int j0, int dv, uint32_t tad
 }
 
 template <int DK, int MODE>
+constexpr int kKeySlots = DK == 64 || MODE == 1 ? 2 : 1;
+
+// MODE 0: whole sequences; 1: sums of segments; 2: outputs of segments.
+template <int DK, int MODE>
 __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_constant__ ChunkArgs C)
 {
     constexpr bool OUT = MODE != 1;                    // outputs are wanted
-    constexpr int NK = DK == 64 ? 2 : 1;               // slots for keys
+    constexpr int NK = kKeySlots<DK, MODE>, NW = OUT ? 1 : 2;          // slots for keys, for the parts of values
     constexpr int KT = DK * 256, VT = kCols * 256, ST = DK * 128;        // bytes of a tile of K or Q, of V (or outputs), of the state
     constexpr int SQ = DK / 32;                        // quarters of the TMEM lanes with rows of the state
     extern __shared__ uint8_t smem_raw[];
@@ -174,14 +178,18 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     const int share = OUT ? A.share : 1;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t k_tiles = base, v_tiles = k_tiles + NK * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + 2 * KT, s_tiles = w_tiles + 3 * VT;
+    const uint32_t k_tiles = base, v_tiles = k_tiles + NK * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + (OUT ? 2 * KT : 0), s_tiles = w_tiles + 3 * VT;
     const uint32_t o_tile = s_tiles + ST;
     uint8_t* const k_mem = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t *const v_mem = k_mem + NK * KT, *const w_mem = v_mem + 2 * VT + 2 * KT, *const s_mem = w_mem + 3 * VT, *const o_mem = s_mem + ST;
+    uint8_t *const v_mem = k_mem + NK * KT, *const w_first = v_mem + 2 * VT + (OUT ? 2 * KT : 0), *const s_mem = w_first + 3 * VT, *const o_mem = s_mem + ST;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
     const uint32_t scored = bar(20), weighed = bar(21), answered = bar(22), taken = bar(24);
-    const uint32_t parted = bar(25), cleaned = bar(26), summed = bar(27), stated = bar(28);
+    const uint32_t cleaned = bar(26), stated = bar(28);
+    // The sums alone, which no state goes through, are a chunk ahead: two of each of these in turn.
+    auto parted = [&](int c) { return bar(!OUT && (c & 1) ? 29 : 25); };
+    auto summed = [&](int c) { return bar(!OUT && (c & 1) ? 30 : 27); };
+    auto turn = [](int c) { return (uint32_t)(OUT ? c : c >> 1) & 1u; };
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int i = 0; i < 2; ++i) {
@@ -200,9 +208,11 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         mbar_init(weighed, kWorkers);                  // P is in TMEM
         mbar_init(answered, 1);                        // the last step's outputs are in TMEM
         mbar_init(taken, kWorkers);                    // a step's outputs have been read
-        mbar_init(parted, kWorkers);                   // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
+        mbar_init(bar(25), kWorkers);                  // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
         mbar_init(stated, kWorkers);                   // the state is in shared memory
-        mbar_init(summed, 1);                          // the chunk's sums are on top of the state, V' has been read
+        mbar_init(bar(27), 1);                         // the chunk's sums are on top of the state, V' has been read
+        mbar_init(bar(29), kWorkers);
+        mbar_init(bar(30), 1);
         mbar_init(cleaned, kWorkers);                  // rows behind the last frame are zeroed
         mbar_init_done();
     }
@@ -222,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         if (elect_one()) {
             bool ok = true;
             uint32_t n = 0;                            // steps: chunks x heads
-            auto frame = [&](int c) { return (int)(f0 + (int64_t)c * kChunk); };
+            auto frame = [&](int c) { return (int)(f0 + (int64_t)(OUT ? c : chunks - 1 - c) * kChunk); };
             auto load_q = [&](int c, int h) {
                 const uint32_t s = n & 1, b = q_full + 8 * s;
                 ok = ok && mbar_wait(q_empty + 8 * s, ((n >> 1) & 1) ^ 1, gave_up);
@@ -284,12 +294,12 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 const uint32_t k_at = k_tiles + (c % NK) * KT, v_at = v_tiles + (c & 1) * VT;
                 const int steps = ((c + 1 == chunks ? tail : kChunk) + 15) / 16;        // of 16 frames
                 // the state first: the next chunk waits for it
-                ok = mbar_wait(parted, c & 1, gave_up);
+                ok = mbar_wait(parted(c), turn(c), gave_up);
                 if (!ok) break;
                 tc_fence_after();
                 for (int k = 0; k < steps; ++k)
-                    mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + k * 2048, VT), i_state, 1);
-                tc_commit(summed);
+                    mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + (c % NW) * 3 * VT + k * 2048, VT), i_state, 1);
+                tc_commit(summed(c));
                 if (share == 1) tc_commit(k_empty + 8 * (c % NK));
                 for (int h = 0; h < share && ok; ++h, ++n) {
                     if (OUT) {
@@ -328,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = lane * 4 + e;
-                x[e] = c < chunks && j < n ? d[(f0 + (int64_t)c * kChunk + j) * A.sd.frame] : 0.0f;
+                x[e] = c < chunks && j < n ? d[(f0 + (int64_t)(OUT ? c : chunks - 1 - c) * kChunk + j) * A.sd.frame] : 0.0f;
             }
         };
         float next[4];
@@ -351,6 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             }
             const double total = __shfl_sync(0xFFFFFFFFu, before, 31);
             before -= g[3];
+            const double behind = OUT ? 0.0 : log_whole * l2e;           // (sums alone, from the last chunk to the first: the decays of the chunks behind this one)
             log_whole += total;
             const double last = total * l2e;
             double mine[4];
@@ -365,22 +376,25 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             Decays& D = decays[slot];
             float4 hi, lo, col, rest, row;
             auto fill = [&](double x, float& h, float& l, float& a, float& b, float& y) {
+                b = exp2_two(last - x + behind);
+                if (!OUT) return;
                 h = (float)x;
                 l = (float)(x - (double)h);
                 a = exp2_two(block_end - x);
-                b = exp2_two(last - x);
                 y = exp2_two(x);
             };
             fill(mine[0], hi.x, lo.x, col.x, rest.x, row.x);
             fill(mine[1], hi.y, lo.y, col.y, rest.y, row.y);
             fill(mine[2], hi.z, lo.z, col.z, rest.z, row.z);
             fill(mine[3], hi.w, lo.w, col.w, rest.w, row.w);
-            reinterpret_cast<float4*>(D.hi)[lane] = hi;
-            reinterpret_cast<float4*>(D.lo)[lane] = lo;
-            reinterpret_cast<float4*>(D.col)[lane] = col;
             reinterpret_cast<float4*>(D.rest)[lane] = rest;
-            reinterpret_cast<float4*>(D.row)[lane] = row;
-            if (lane == 0) {
+            if (OUT) {
+                reinterpret_cast<float4*>(D.hi)[lane] = hi;
+                reinterpret_cast<float4*>(D.lo)[lane] = lo;
+                reinterpret_cast<float4*>(D.col)[lane] = col;
+                reinterpret_cast<float4*>(D.row)[lane] = row;
+            }
+            if (OUT && lane == 0) {
                 D.whole = rounded;
                 D.odd = 0;
             }
@@ -502,18 +516,19 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 }
                 D.odd = 1;
             }
-            if (c > 0) {
-                ok = mbar_wait_warp(summed, (c - 1) & 1, gave_up);
+            if (c >= NW) {
+                ok = mbar_wait_warp(summed(c - NW), turn(c - NW), gave_up);
                 if (!ok) break;
                 tc_fence_after();
             }
+            uint8_t* const w_mem = w_first + (c % NW) * 3 * VT;
             *reinterpret_cast<uint4*>(w_mem + place0) = make_uint4(a[0], a[1], a[2], a[3]);
             *reinterpret_cast<uint4*>(w_mem + place1) = make_uint4(a[4], a[5], a[6], a[7]);
             *reinterpret_cast<uint4*>(w_mem + VT + place0) = make_uint4(b[0], b[1], b[2], b[3]);
             *reinterpret_cast<uint4*>(w_mem + VT + place1) = make_uint4(b[4], b[5], b[6], b[7]);
             *reinterpret_cast<uint4*>(w_mem + 2 * VT + place0) = make_uint4(d[0], d[1], d[2], d[3]);
             *reinterpret_cast<uint4*>(w_mem + 2 * VT + place1) = make_uint4(d[4], d[5], d[6], d[7]);
-            if (holds) {
+            if (OUT && holds) {
                 // the state that enters the chunk is the sum of what its three parts have become
                 uint32_t x0[16], x1[16], x2[16];
                 tc_ld(state, state + kCols, state + 2 * kCols, x0, x1, x2);
@@ -534,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             fence_async_shared();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(parted);
+            if (lane == 0) mbar_arrive(parted(c));
             if (!OUT) {
                 if (lane == 0) mbar_arrive(d_empty + 8 * slot);
                 continue;
@@ -597,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             }
             if (!ok) break;
         }
-        ok = ok && mbar_wait_warp(summed, (chunks - 1) & 1, gave_up);
+        ok = ok && mbar_wait_warp(summed(chunks - 1), turn(chunks - 1), gave_up);
         if (ok) {
             tc_fence_after();
             if (holds) {
@@ -643,12 +658,23 @@ __global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant_
     if (i >= size) return;
     float S = A.state_in ? A.state_in[((int64_t)b * A.groups + g) * size + i] : 0.0f;
     // (offsets that overlap may ask for more slots than there are)
-    for (int64_t s = 0; s < count && first_slot + s < C.slots; ++s) {
-        const int64_t slot = (first_slot + s) * A.groups + g;
-        float* p = C.sums + slot * size + i;
-        const float sum = s + 1 < count ? *p : 0.0f;
-        *p = S;
-        if (s + 1 < count) S = fmaf(C.decays[slot], S, sum);
+    const int64_t n = min(count, (int64_t)C.slots - first_slot);
+    constexpr int kAhead = 8;                          // segments whose sums are read at once: one after the other each would wait for memory
+    for (int64_t s0 = 0; s0 < n; s0 += kAhead) {
+        float sum[kAhead], decay[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int64_t slot = (first_slot + s0 + e) * A.groups + g;
+            const bool wanted = s0 + e < n && s0 + e + 1 < count;        // (the last segment's sums are not made)
+            sum[e] = wanted ? C.sums[slot * size + i] : 0.0f;
+            decay[e] = wanted ? C.decays[slot] : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+            if (s0 + e < n) {
+                C.sums[((first_slot + s0 + e) * A.groups + g) * size + i] = S;
+                S = fmaf(decay[e], S, sum[e]);
+            }
     }
 }
 
@@ -673,8 +699,8 @@ bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, in
 template <int DK, int MODE>
 cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 {
-    constexpr int NK = DK == 64 ? 2 : 1;
-    constexpr int smem = 1024 + NK * DK * 256 + 2 * kCols * 256 + 2 * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256;
+    constexpr int tiles = kKeySlots<DK, MODE> * DK * 256 + 2 * kCols * 256;
+    constexpr int smem = 1024 + tiles + (MODE == 1 ? 2 * 3 * kCols * 256 : 2 * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256);
     static SrSharedLimit limit;
     const cudaError_t e = limit.raise(sr_chunks_kernel<DK, MODE>, smem);
     if (e != cudaSuccess) return e;
