@@ -10,6 +10,7 @@
 //   far     Q S                the state rounded to bf16 for this product                             (columns 320 .. 383)
 //   state   K^T [V'_hi | V'_mid | V'_lo], V' = V exp(G_last - G_j) in three bf16 parts, 24 bits: the state itself is as exact as 32 bits make it.  The
 //                              decayed state and the parts' sums are three accumulators side by side (columns 128 .. 319), added up once per chunk
+// Sums of segments, whose state nothing reads, leave it alone until the end: their chunks go from the last to the first, values weighted by all the decays behind them.
 // K is read along both of its sides from the same tile.  Roundings to bf16: P and the state as factors of the outputs, one each, on different terms of the sum
 // (the outputs are as far off as one rounding more of the output makes them; with the state in two parts it was 1.37 times one rounding, so 1.41).
 // Decays never exceed one: exp(G_i - G_j) is a product of exp(G_i - G_e) and exp(G_e - G_j) with e the last frame of j's 32, where i lies behind them, and
@@ -729,10 +730,11 @@ cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
 }
 
 // Frames of a segment, 0: whole sequences.  Segments are read twice (k and v for their sums, then everything for the outputs) and cost two launches and the
-// way of their states out and back, about as much as eight chunks; they are for launches that would leave SMs without work, or wait for
-// one long sequence.  A step (a chunk for one head) is the unit; a chunk's sums alone are three quarters of one.  Of packed sequences only the mean is known: the longest
-// is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 616 / 166, 4096 frames 86 / 51; 8 sequences of 1024, 4 heads of 64
-// 25 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 596 / 334; 32 of 1000, 8 heads of 64 90 / 120.  More than one wave of segments lost: 32768 frames 210, 263 with two, three.
+// way of their states out and back, about as much as five chunks; they are for launches that would leave SMs without work, or wait for
+// one long sequence.  A step (a chunk for one head) is the unit; a chunk's sums alone are 0.6 of one.  Of packed sequences only the mean is known: the longest
+// is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 616 / 142, 4096 frames 86 / 39; 4 of 8192, 4 heads of 128 160 / 89; 8 of 1024,
+// 4 heads of 64 23 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 596 / 345; 32 of 1000, 8 heads of 64 90 / 120.  More than one wave of segments lost:
+// 32768 frames 210, 263 with two, three waves instead of 166, packed 355, 364, 396 instead of 353 (all measured alike, before the sums went without a state).
 AttentionCut cut_of(const sr_attention_desc* d, bool packed)
 {
     AttentionCut cut{0, 0};
@@ -744,11 +746,13 @@ AttentionCut cut_of(const sr_attention_desc* d, bool packed)
     const double waves = (double)(((int64_t)d->batch * per_slot + sms - 1) / sms);
     const double whole = std::max(longest, waves * mean) / kChunk * share;
     const int64_t want = std::max<int64_t>(1, sms / per_slot);
-    const int64_t length = std::max<int64_t>(512, ((int64_t)(total / (double)want) + kChunk - 1) / kChunk * kChunk);
+    // whole segments of every sequence, no more than there are SMs for
+    const int64_t each = packed ? (int64_t)(total / (double)want) : (d->frames + std::max<int64_t>(1, want / d->batch) - 1) / std::max<int64_t>(1, want / d->batch);
+    const int64_t length = std::max<int64_t>(512, (each + kChunk - 1) / kChunk * kChunk);
     if (length >= d->frames) return cut;
     const int64_t slots = packed ? d->batch + d->frames / length : d->batch * ((d->frames + length - 1) / length);
     const double pieces = packed ? total / (double)length + 0.5 * d->batch : (double)slots;
-    if (std::ceil(pieces * (double)per_slot / (double)sms) * (double)(length / kChunk) * (share + 0.75) + 8.0 > 0.9 * whole) return cut;
+    if (std::ceil(pieces * (double)per_slot / (double)sms) * (double)(length / kChunk) * (share + 0.6) + 5.0 > 0.9 * whole) return cut;
     cut.segment = length;
     cut.slots = slots;
     return cut;

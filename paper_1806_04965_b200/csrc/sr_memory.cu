@@ -302,7 +302,8 @@ AttentionCut frames_cut(const sr_attention_desc* d, bool packed)
     const double longest = packed ? std::min(total, 3.0 * mean) : mean;
     const double waves = (double)(((int64_t)d->batch * per_slot + held - 1) / held);
     const int64_t want = std::max<int64_t>(1, held / per_slot);
-    const int64_t length = std::max<int64_t>(128, ((int64_t)(total / (double)want) + kFrames - 1) / kFrames * kFrames);
+    const int64_t each = packed ? (int64_t)(total / (double)want) : (d->frames + std::max<int64_t>(1, want / d->batch) - 1) / std::max<int64_t>(1, want / d->batch);
+    const int64_t length = std::max<int64_t>(128, (each + kFrames - 1) / kFrames * kFrames);
     if (length >= d->frames) return cut;
     const int64_t slots = packed ? d->batch + d->frames / length : d->batch * ((d->frames + length - 1) / length);
     const double pieces = packed ? total / (double)length + 0.5 * d->batch : (double)slots;
