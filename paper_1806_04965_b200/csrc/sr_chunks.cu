@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
     const uint32_t scored = bar(20), weighed = bar(21), answered = bar(22), taken = bar(24);
-    const uint32_t cleaned = bar(26), stated = bar(28);
+    const uint32_t cleaned = bar(26);
     // The sums alone, which no state goes through, are a chunk ahead: two of each of these in turn.
     auto parted = [&](int c) { return bar(!OUT && (c & 1) ? 29 : 25); };
     auto summed = [&](int c) { return bar(!OUT && (c & 1) ? 30 : 27); };
@@ -210,7 +210,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         mbar_init(answered, 1);                        // the last step's outputs are in TMEM
         mbar_init(taken, kWorkers);                    // a step's outputs have been read
         mbar_init(bar(25), kWorkers);                  // V' is in shared memory, V is fit for the near product, the state in TMEM has decayed
-        mbar_init(stated, kWorkers);                   // the state is in shared memory
         mbar_init(bar(27), 1);                         // the chunk's sums are on top of the state, V' has been read
         mbar_init(bar(29), kWorkers);
         mbar_init(bar(30), 1);
@@ -305,8 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 for (int h = 0; h < share && ok; ++h, ++n) {
                     if (OUT) {
                         const uint32_t q_at = q_tiles + (n & 1) * KT;
-                        if (h == 0) ok = mbar_wait(stated, c & 1, gave_up);
-                        ok = ok && mbar_wait(taken, (n & 1) ^ 1, gave_up);
+                        ok = mbar_wait(taken, (n & 1) ^ 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
@@ -416,43 +414,34 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         const Pair minus = pair(-1.0f, -1.0f);
         const uint32_t place0 = (uint32_t)i * 128u + (((uint32_t)(2 * u) ^ (i & 7)) << 4), place1 = (uint32_t)i * 128u + (((uint32_t)(2 * u + 1) ^ (i & 7)) << 4);
         uint32_t n = 0;                                // steps: chunks x heads
-        uint32_t part[8];                              // the state that enters the chunk, rounded
-        auto state_there = [&] {
-            if (holds) {
-                *reinterpret_cast<uint4*>(s_mem + place0) = make_uint4(part[0], part[1], part[2], part[3]);
-                *reinterpret_cast<uint4*>(s_mem + place1) = make_uint4(part[4], part[5], part[6], part[7]);
-            }
-        };
-        // Outputs of the step before; meanwhile: with them the state for the far products (those that read the one before are done when the outputs are there).
-        auto output = [&](int c, int h, bool meanwhile) {
-            const Decays& D = decays[c % kDecays];
-            uint32_t a[16], x[16], z[8];
+        // Outputs of the step before, in two parts: out of the accumulators, which the MMAs wait for, and, behind this step's weights, on their way.
+        uint32_t z[8];
+        auto take = [&](int c) {
+            uint32_t a[16], x[16];
             tc_ld(tmem + lanes + kFar + u * 16, tmem + lanes + kNear + u * 16, a, x);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(taken);
-            const float r = D.row[i] * A.scale;
+            const float r = decays[c % kDecays].row[i] * A.scale;
             const Pair row = pair(r, r), scale = pair(A.scale, A.scale);
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] = round_bf16(fma2(pair(x[2 * e], x[2 * e + 1]), scale, mul2(row, pair(a[2 * e], a[2 * e + 1]))));
+        };
+        auto store = [&](int c, int h) {
+            const Decays& D = decays[c % kDecays];
             const bool odd = D.odd != 0;
-            const bool copies = C.out_copies && !odd && !(clean && c + 1 == chunks);
-            if (copies) {
+            if (C.out_copies && !odd && !(clean && c + 1 == chunks)) {
                 // through shared memory, every warp its own box: a thread's stores would be 32 bytes of a row each
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 __syncwarp();
                 uint8_t* to = o_mem + (warp - 4) * 1024 + lane * 32;
                 *reinterpret_cast<uint4*>(to) = make_uint4(z[0], z[1], z[2], z[3]);
                 *reinterpret_cast<uint4*>(to + 16) = make_uint4(z[4], z[5], z[6], z[7]);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) tma_store_4d(&C.out_map, o_tile + (warp - 4) * 1024, j0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk + w * 32));
             } else if (i < (c + 1 == chunks ? tail : kChunk)) {
                 store_row(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, odd, make_uint4(z[0], z[1], z[2], z[3]), make_uint4(z[4], z[5], z[6], z[7]));
-            }
-            if (meanwhile) state_there();
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) {
-                if (meanwhile) mbar_arrive(stated);
-                if (copies) tma_store_4d(&C.out_map, o_tile + (warp - 4) * 1024, j0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk + w * 32));
             }
         };
         // Ahead of the first chunk: the state as the first of its three parts, zeros for the others and for the weights behind the diagonal.
@@ -534,6 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 uint32_t x0[16], x1[16], x2[16];
                 tc_ld(state, state + kCols, state + 2 * kCols, x0, x1, x2);
                 const Pair whole = pair(D.whole, D.whole);
+                uint32_t part[8];                      // the state that enters the chunk, rounded
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const Pair y = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
@@ -545,6 +535,11 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 tc_st(state, x0);
                 tc_st(state + kCols, none);
                 tc_st(state + 2 * kCols, none);
+                // (the far products that read the one before are long done)
+                if (c > 0) ok = mbar_wait_warp(q_empty + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, gave_up);
+                if (!ok) break;
+                *reinterpret_cast<uint4*>(s_mem + place0) = make_uint4(part[0], part[1], part[2], part[3]);
+                *reinterpret_cast<uint4*>(s_mem + place1) = make_uint4(part[4], part[5], part[6], part[7]);
                 tc_wait_st();
             }
             fence_async_shared();
@@ -560,15 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ok = mbar_wait_warp(scored, n & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                if (n > 0) {
-                    output(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1, h == 0);
-                    if (h == 0 && lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
-                } else {
-                    state_there();
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(stated);
-                }
+                if (n > 0) take(h > 0 ? c : c - 1);
                 // scores -> P: two workers of a quarter have 16 columns of the diagonal's 32 each, the other two 16 of all 32s to its left
                 const float hi = D.hi[i], lo = D.lo[i];
                 const int half = (u & 1) * 16;
@@ -610,6 +597,13 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(weighed);
+                if (n > 0) {
+                    store(h > 0 ? c : c - 1, h > 0 ? h - 1 : share - 1);
+                    if (h == 0) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(d_empty + 8 * ((c - 1) % kDecays));
+                    }
+                }
             }
             if (!ok) break;
         }
@@ -623,7 +617,8 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             }
             if (OUT && mbar_wait_warp(answered, 0, gave_up)) {
                 tc_fence_after();
-                output(chunks - 1, share - 1, false);
+                take(chunks - 1);
+                store(chunks - 1, share - 1);
             }
         }
         if (OUT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
