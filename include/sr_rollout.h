@@ -338,6 +338,7 @@ sr_status sr_rms_norm(const void* x_dev, const void* residual_dev, const float* 
  *     S_t = exp(log_decay_t) * S_{t-1} + k_t v_t^T,      out_t = scale * q_t S_t.
  * heads (of queries and outputs) is a multiple of groups (of keys, values, decays and states): heads h * heads / groups ... share group h.
  * Decays: log_decay <= 0, -INFINITY included (the state starts anew at that frame).
+ * What is not finite stays in its sequence, its head and, for values, its column; where the formula has an infinity the result may be NaN.
  * Layout: element (frame, sequence, head, i) of q lies at frame * q.frame + sequence * q.sequence + head * q.head + i, in elements, the
  * same for k, v, out (i < dk, dk, dv, dv) and log_decay (float; strides 0 repeat a value).
  *   offsets NULL:  `batch` sequences of `frames` frames each (sr_rollout_run's [T][B][C] has frame = B * C, sequence = C);

@@ -16,11 +16,10 @@
 // Decays never exceed one: exp(G_i - G_j) is a product of exp(G_i - G_e) and exp(G_e - G_j) with e the last frame of j's 32, where i lies behind them, and
 // one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
 //
-// (Persistent CTAs that walk over items, with a warp that hands them out, lost to one CTA per item but where every item is one chunk: 32 sequences of 128 frames, 8 heads of
-// 64 14.8 / 13.7 us, packed sequences 90 / 124 and 116 / 194.)
 // A chunk of DK = 128 is 96 KiB of loads and stores and 1.8k cycles of MMAs per CTA, 2.2k cycles' worth of memory with every SM at it, and takes 5.4k (4096 frames, 148 CTAs:
-// 92 us, 3.4 TB/s): what bounds it is the chain from one chunk to the next, values' parts -> sums -> state -> weights, which no other chunk of the CTA may overtake, and two CTAs
-// to an SM do not fit (208 KiB of tiles, all of TMEM).
+// 91 us, 3.4 TB/s); further heads of the chunk 1.3 us each (1024 frames x 37, 8 heads on 2: 61 us).  What bounds it are the workers: about 790 instructions per warp and chunk, four warps to a scheduler, which the
+// barriers keep in step, so that half of the issue slots are used; two CTAs to an SM do not fit (208 KiB of tiles, all of TMEM).  Not faster: roles of their own for the
+// workers (128 us), persistent CTAs (packed sequences 90 / 124 us, 116 / 194), the state in registers instead of TMEM (91).
 // Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; sixteen workers for everything between the MMAs.
 // What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
 // the near product (whose zeros would spread it to earlier frames) and added where the outputs are stored; rows behind a sequence's last frame are zeroed.
