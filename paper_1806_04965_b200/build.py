@@ -62,7 +62,7 @@ def build_extension() -> str:
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] + ["-I" + i for i in include] +
                           [os.path.join(CSRC, "sr_python.cpp"), "-o", tmp, "-L" + HERE, "-l:libsr_rollout.so", "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch",
-                           "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(base, "lib")])
+                           "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(base, "lib")])
     os.replace(tmp, EXTENSION)
     return EXTENSION
 

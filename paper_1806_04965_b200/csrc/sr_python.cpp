@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -66,14 +67,16 @@ PyObject* two(PyObject* a, PyObject* b)
 }
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 
+// A tensor without values on x's device, by the allocator's own entry (through the dispatcher each costs most of a microsecond more).
+at::Tensor new_tensor(const at::Tensor& x, at::IntArrayRef sizes, at::ScalarType type) { return at::Tensor(at::detail::empty_cuda(sizes, type, x.device(), std::nullopt)); }
+
 struct Scaled {
     at::Tensor data, scales;
 };
 Scaled new_scaled(const at::Tensor& like, int64_t rows, int64_t cols, int format)
 {
     const int64_t groups = (cols + 31) / 32;
-    const auto options = like.options().dtype(at::kByte);
-    return {at::empty({rows, groups * (format == SR_FORMAT_MX4 ? 16 : 32)}, options), at::empty({(rows + 127) / 128 * ((groups + 3) / 4) * 512}, options)};
+    return {new_tensor(like, {rows, groups * (format == SR_FORMAT_MX4 ? 16 : 32)}, at::kByte), new_tensor(like, {(rows + 127) / 128 * ((groups + 3) / 4) * 512}, at::kByte)};
 }
 
 // No exception of the allocator's leaves through a C function: None, and operators.py meets it again.
@@ -128,7 +131,7 @@ PyObject* py_product(PyObject*, PyObject* const* a, Py_ssize_t n)
         sr_status st;
         {
             Unlocked u;
-            if (!given) out = at::empty({rows, outs}, ad->options().dtype(dtype == SR_DTYPE_F32 ? at::kFloat : at::kBFloat16));
+            if (!given) out = new_tensor(*ad, {rows, outs}, dtype == SR_DTYPE_F32 ? at::kFloat : at::kBFloat16);
             st = sr_microscale_product(ad->data_ptr(), as->data_ptr(), wd->data_ptr(), ws->data_ptr(), format, rows, cols, outs,
                                        bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, relu ? 1 : 0, out.data_ptr(), type_of(out), stride, d.stream());
         }
@@ -161,9 +164,9 @@ PyObject* py_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
         sr_status st;
         {
             Unlocked u;
-            if (r) sum = at::empty({rows, cols}, x->options());
+            if (r) sum = new_tensor(*x, {rows, cols}, x->scalar_type());
             if (format) m = new_scaled(*x, rows, cols, format);
-            else out = at::empty({rows, cols}, x->options());
+            else out = new_tensor(*x, {rows, cols}, x->scalar_type());
             st = sr_rms_norm(x->data_ptr(), r ? r->data_ptr() : nullptr, w ? static_cast<const float*>(w->data_ptr()) : nullptr, (float)eps, type_of(*x), rows, cols, xs, rs,
                              r ? sum.data_ptr() : nullptr, format ? m.data.data_ptr() : out.data_ptr(), format ? format : type_of(*x),
                              format ? m.scales.data_ptr() : nullptr, d.stream());
@@ -242,7 +245,7 @@ PyObject* py_step(PyObject*, PyObject* const* a, Py_ssize_t n)
         sr_status st;
         {
             Unlocked u;
-            out = at::empty({d.batch, d.heads, d.dv}, q->options());
+            out = new_tensor(*q, {d.batch, d.heads, d.dv}, q->scalar_type());
             st = sr_linear_attention_step(&d, q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const float*>(decay->data_ptr()),
                                           static_cast<float*>(state->data_ptr()), out.data_ptr(), dev.stream());
         }
@@ -287,12 +290,12 @@ PyObject* py_run(PyObject*, PyObject* const* a, Py_ssize_t n)
         sr_status st;
         {
             Unlocked u;
-            if (!given) out = packed ? at::empty({q->size(0), d.heads, d.dv}, q->options()) : at::empty({q->size(0), batch, d.heads, d.dv}, q->options());
-            if (!to) last = at::empty({batch, d.groups, d.dk, d.dv}, q->options().dtype(at::kFloat));
+            if (!given) out = packed ? new_tensor(*q, {q->size(0), d.heads, d.dv}, q->scalar_type()) : new_tensor(*q, {q->size(0), batch, d.heads, d.dv}, q->scalar_type());
+            if (!to) last = new_tensor(*q, {batch, d.groups, d.dk, d.dv}, at::kFloat);
             size_t bytes = 0;
             st = sr_linear_attention_workspace_bytes(&d, packed ? 1 : 0, &bytes);
             at::Tensor work;
-            if (st == SR_OK && bytes) work = at::empty({(int64_t)bytes}, q->options().dtype(at::kByte));
+            if (st == SR_OK && bytes) work = new_tensor(*q, {(int64_t)bytes}, at::kByte);
             if (st == SR_OK)
                 st = sr_linear_attention_run(&d, q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const float*>(decay->data_ptr()),
                                              packed ? static_cast<const int64_t*>(offsets->data_ptr()) : nullptr, state ? static_cast<const float*>(state->data_ptr()) : nullptr,
