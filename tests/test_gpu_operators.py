@@ -486,6 +486,36 @@ def test_calls_are_captured_and_replayed_on_another_stream():
         assert not torch.equal(got[0], other[0])
 
 
+def test_large_products_and_runs_side_by_side_on_streams():
+    # tiles of pairs of CTAs and chunks, which want whole SMs, and what is captured of them replayed beside the calls themselves
+    cases = []
+    for i, (rows, cols, outs, fmt) in enumerate([(1000, 4100, 2700, "mx4"), (1900, 1000, 2600, "mx8")]):
+        x, w = torch.randn(rows, cols, generator=gen(80 + i), device=DEV), torch.randn(outs, cols, generator=gen(82 + i), device=DEV)
+        cases.append((sr.quantize(x, fmt), sr.quantize(w, fmt)))
+    q, k, v, d = inputs((300, 40), 4, 4, 64, 64, "bf16", True, seed=84)
+    calls = [lambda: sr.product(*cases[0]), lambda: sr.product(*cases[1]), lambda: sr.linear_attention_run(q, k, v, d)[0]]
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    graphs = []
+    for c, s in zip(calls, streams):
+        with torch.cuda.stream(s):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                graphs.append([g, c()])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for c, s, (g, _) in zip(calls, streams, graphs):
+            with torch.cuda.stream(s):
+                got.append(c())
+                g.replay()
+        torch.cuda.synchronize()
+        for a, (_, b), e in zip(got, graphs, want):
+            assert torch.equal(a, e) and torch.equal(b, e)
+    sr.operator_status()
+
+
 def test_infinite_values_give_what_the_formula_gives():
     # +inf in the values: earlier frames do not see it, later ones are infinite with the weights' signs or NaN where those meet
     T, D = 150, 64
