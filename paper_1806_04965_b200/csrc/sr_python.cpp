@@ -1,5 +1,5 @@
 // The operators' calls from Python without ctypes and its marshalling: a call on small tensors is host time before anything else (one frame of one sequence 10.4 us
-// through ctypes, 4.8 here).  Every function here checks its arguments, allocates the outputs, calls the C ABI and hands the outputs over; where anything is not as it has to
+// through ctypes, 4.2 here).  Every function here checks its arguments, allocates the outputs, calls the C ABI and hands the outputs over; where anything is not as it has to
 // be it returns None and has done nothing, and operators.py, which knows the same rules, says what is wrong.
 #include <Python.h>
 
