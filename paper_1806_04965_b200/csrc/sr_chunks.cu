@@ -6,20 +6,24 @@
 // four matrix products per chunk and group of 64 columns of v (the last one a CTA's: it holds DK x 64 values of a state), all of them tcgen05.mma
 // with M = 128:
 //   scores  Q K^T              128 frames x 128 frames, both from shared memory                       (TMEM columns 0 .. 127)
-//   near    P V                P = scores * decays, lower triangle, bf16, back in TMEM as the A operand (columns 448 .. 511, sums in 384 .. 447)
-//   far     Q S                the state rounded to bf16 for this product                             (columns 320 .. 383)
-//   state   K^T [V'_hi | V'_mid | V'_lo], V' = V exp(G_last - G_j) in three bf16 parts, 24 bits: the state itself is as exact as 32 bits make it.  The
-//                              decayed state and the parts' sums are three accumulators side by side (columns 128 .. 319), added up once per chunk
+//   near    (P_hi + P_lo) V    P = scores * decays, lower triangle, in two bf16 parts, back in TMEM as the A operand (columns 448 .. 511 and 256 .. 319, sums
+//                              in 384 .. 447)
+//   far     Q (S_hi + S_lo)    the state in two bf16 parts for this product                           (columns 320 .. 383)
+//   state   K^T V', V' = V exp(G_last - G_j) in three bf16 parts, 24 bits: the state itself is as exact as 32 bits make it.  Two accumulators side by
+//                              side (columns 128 .. 255), the decayed state with the first parts' sums and the sums of the others, added up once per chunk
 // Sums of segments, whose state nothing reads, leave it alone until the end: their chunks go from the last to the first, values weighted by all the decays behind them.
-// K is read along both of its sides from the same tile.  Roundings to bf16: P and the state as factors of the outputs, one each, on different terms of the sum
-// (the outputs are as far off as one rounding more of the output makes them; with the state in two parts it was 1.37 times one rounding, so 1.41).
+// They have three accumulators, one to each part, and one MMA for all of them.
+// K is read along both of its sides from the same tile.  Nothing but the outputs is rounded to bf16 once: two parts hold a factor to 2^-16 of itself, so that the outputs are as far
+// off as their own rounding makes them (1.7e-3 of their size; with one part each 2.3e-3).  Us with one part each / two: 32 clips of 128 frames, 8 heads of 64 16.4 / 17.8; packed 16 of 3000,
+// 16 heads on 4 of 128 301 / 324; one of 32768, 8 heads of 128 153 / 170; 1024 frames x 37, 8 heads on 2 of 128 67 / 84.
 // Decays never exceed one: exp(G_i - G_j) is a product of exp(G_i - G_e) and exp(G_e - G_j) with e the last frame of j's 32, where i lies behind them, and
 // one exponential where it does not.  G is summed in 64 bits and held in two floats, so that a frame that forgets everything costs the ones behind it nothing.
 //
-// A chunk of DK = 128 is 96 KiB of loads and stores and 1.8k cycles of MMAs per CTA, 2.2k cycles' worth of memory with every SM at it, and takes 5.4k (4096 frames, 148 CTAs:
-// 91 us, 3.4 TB/s); further heads of the chunk 1.3 us each (1024 frames x 37, 8 heads on 2: 61 us).  What bounds it are the workers: about 790 instructions per warp and chunk, four warps to a scheduler, which the
-// barriers keep in step, so that half of the issue slots are used; two CTAs to an SM do not fit (208 KiB of tiles, all of TMEM).  Not faster: roles of their own for the
-// workers (128 us), persistent CTAs (packed sequences 90 / 124 us, 116 / 194), the state in registers instead of TMEM (91).
+// A chunk of DK = 128 is 96 KiB of loads and stores and 2.9k cycles of MMAs per CTA, 2.2k cycles' worth of memory with every SM at it, and takes 6.6k (4096 frames, 148 CTAs:
+// 112 us, 2.8 TB/s; without the MMAs of the second parts 99, without its stores 108); further heads of the chunk about 2 us each (1024 frames x 37, 8 heads on 2: 84 us; 79 and 79).  What bounds it is the
+// chain from scores over weights to outputs, which workers (four warps to a scheduler, kept in step by the barriers) and MMAs go along in turn; two CTAs to an SM do not fit (209 KiB of tiles, all
+// of TMEM).  Not faster, with one part each: roles of their own for the workers (128 us instead of 91), the state in registers instead of TMEM (91); persistent CTAs gained only where sequences are
+// a chunk long (32 clips of 128 frames 14.8 -> 13.7; packed sequences 90 -> 124, 116 -> 194).
 // Roles: warp 0 copies, 1 MMAs, 2 decays, 3 TMEM; sixteen workers for everything between the MMAs.
 // What is not finite stays where the formula has it: scores behind the diagonal are replaced, not multiplied; a value of v that is not finite is taken out of
 // the near product (whose zeros would spread it to earlier frames) and added where the outputs are stored; rows behind a sequence's last frame are zeroed.
@@ -41,13 +45,13 @@ using namespace srx;
 
 constexpr int kChunk = 128, kCols = 64, kDecays = 4;
 constexpr int kWorkers = 16, kThreads = 128 + 32 * kWorkers;
-constexpr uint32_t kScores = 0, kState = 128, kFar = 320, kNear = 384, kWeights = 448;       // TMEM columns
+constexpr uint32_t kScores = 0, kState = 128, kRest = 256, kFar = 320, kNear = 384, kWeights = 448;      // TMEM columns
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct ChunkArgs {
-    CUtensorMap q_map, k_map, v_map, out_map;
+    CUtensorMap q_map, k_map, v_map;
     SegmentArgs S;
-    int32_t out_copies;                                // outputs leave by TMA
+    int32_t out_align;                                 // bytes on which a row's pieces of 16 outputs start: 32, 16 or 0 (any)
     int* error;
 };
 
@@ -62,6 +66,14 @@ __device__ __forceinline__ float exp2_two(double x)   // 2^x, x as two floats
     const float hi = (float)x, lo = (float)(x - (double)hi);
     const float y = exp2_fast(hi);
     return fmaf(y, lo * kLn2, y);
+}
+// What rounding a pair to bf16 left over, rounded, and the halves of a word of bf16 that are finite
+__device__ __forceinline__ uint32_t left_bf16(Pair y, uint32_t rounded) { return round_bf16(fma2(widen_bf16(rounded), pair(-1.0f, -1.0f), y)); }
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) { return ((w & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u); }
+__device__ __forceinline__ void store_32_bytes(void* to, const uint32_t (&z)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]), "r"(z[4]), "r"(z[5]), "r"(z[6]), "r"(z[7]) : "memory");
 }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
@@ -125,13 +137,18 @@ __device__ __noinline__ void load_state(const float* from, int j0, int dv, uint3
     __syncwarp();
     tc_st(taddr, x);
 }
+template <int ACCS>
 __device__ __noinline__ void store_state(float* to, int j0, int dv, uint32_t taddr)
 {
     uint32_t x0[16], x1[16], x2[16];
-    tc_ld(taddr, taddr + kCols, taddr + 2 * kCols, x0, x1, x2);
+    if constexpr (ACCS == 3) tc_ld(taddr, taddr + kCols, taddr + 2 * kCols, x0, x1, x2);
+    else tc_ld(taddr, taddr + kCols, x0, x1);
     if (!to) return;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x0[e] = __float_as_uint(__uint_as_float(x0[e]) + (__uint_as_float(x1[e]) + __uint_as_float(x2[e])));
+    for (int e = 0; e < 16; ++e) {
+        const float more = ACCS == 3 ? __uint_as_float(x1[e]) + __uint_as_float(x2[e]) : __uint_as_float(x1[e]);
+        x0[e] = __float_as_uint(__uint_as_float(x0[e]) + more);
+    }
     if (j0 + 16 <= dv && !((uintptr_t)(to + j0) & 15)) {
 #pragma unroll
         for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + j0 + e) = make_uint4(x0[e], x0[e + 1], x0[e + 2], x0[e + 3]);
@@ -179,9 +196,8 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t k_tiles = base, v_tiles = k_tiles + NK * KT, q_tiles = v_tiles + 2 * VT, w_tiles = q_tiles + (OUT ? 2 * KT : 0), s_tiles = w_tiles + 3 * VT;
-    const uint32_t o_tile = s_tiles + ST;
     uint8_t* const k_mem = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t *const v_mem = k_mem + NK * KT, *const w_first = v_mem + 2 * VT + (OUT ? 2 * KT : 0), *const s_mem = w_first + 3 * VT, *const o_mem = s_mem + ST;
+    uint8_t *const v_mem = k_mem + NK * KT, *const w_first = v_mem + 2 * VT + (OUT ? 2 * KT : 0), *const s_mem = w_first + 3 * VT;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     const uint32_t k_full = bar(0), k_empty = bar(2), v_full = bar(4), v_empty = bar(6), q_full = bar(8), q_empty = bar(10), d_full = bar(12), d_empty = bar(16);
     const uint32_t scored = bar(20), weighed = bar(21), answered = bar(22), taken = bar(24);
@@ -268,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         }
     } else if (warp == 1) {
         if (elect_one()) {
-            constexpr uint32_t i_scores = idesc_bf16(128, 0, 0), i_far = idesc_bf16(64, 0, 1), i_near = idesc_bf16(64, 0, 1), i_state = idesc_bf16(192, 1, 1);
+            constexpr uint32_t i_scores = idesc_bf16(128, 0, 0), i_far = idesc_bf16(64, 0, 1), i_near = idesc_bf16(64, 0, 1), i_state = idesc_bf16(OUT ? 64 : 192, 1, 1);
             bool ok = true;
             uint32_t n = 0;
             // Scores of step m, the first of chunk c's if h is 0.
@@ -296,8 +312,16 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 ok = mbar_wait(parted(c), turn(c), gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                for (int k = 0; k < steps; ++k)
-                    mma_bf16(tmem + kState, desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384), desc_mn_major(w_tiles + (c % NW) * 3 * VT + k * 2048, VT), i_state, 1);
+                for (int k = 0; k < steps; ++k) {
+                    const uint64_t keys = desc_mn_major(k_at + k * 2048, DK == 64 ? 0 : 16384);
+                    const uint32_t parts = w_tiles + (c % NW) * 3 * VT + k * 2048;
+                    if (OUT) {
+#pragma unroll
+                        for (int p = 0; p < 3; ++p) mma_bf16(tmem + kState + (p ? kCols : 0), keys, desc_mn_major(parts + p * VT, 0), i_state, 1);
+                    } else {
+                        mma_bf16(tmem + kState, keys, desc_mn_major(parts, VT), i_state, 1);
+                    }
+                }
                 tc_commit(summed(c));
                 if (share == 1) tc_commit(k_empty + 8 * (c % NK));
                 for (int h = 0; h < share && ok; ++h, ++n) {
@@ -308,12 +332,16 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                         tc_fence_after();
 #pragma unroll
                         for (int k = 0; k < DK / 16; ++k)
-                            mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + k * 2048, 0), i_far, k > 0);
+                            for (int p = 0; p < 2; ++p)
+                                mma_bf16(tmem + kFar, desc_k_major(q_at + (k / 4) * 16384) + 2 * (k % 4), desc_mn_major(s_tiles + p * ST + k * 2048, 0), i_far, k > 0 || p > 0);
                         tc_commit(q_empty + 8 * (n & 1));
                         ok = mbar_wait(weighed, n & 1, gave_up);
                         if (!ok) break;
                         tc_fence_after();
-                        for (int k = 0; k < steps; ++k) mma_bf16_ta(tmem + kNear, tmem + kWeights + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
+                        for (int k = 0; k < steps; ++k) {
+                            mma_bf16_ta(tmem + kNear, tmem + kWeights + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, k > 0);
+                            mma_bf16_ta(tmem + kNear, tmem + kRest + k * 8, desc_mn_major(v_at + k * 2048, 0), i_near, 1);
+                        }
                         if (c + 1 == chunks && h + 1 == share) tc_commit(answered);
                     }
                     if (h + 1 == share) tc_commit(v_empty + 8 * (c & 1));
@@ -429,21 +457,22 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
         auto store = [&](int c, int h) {
             const Decays& D = decays[c % kDecays];
             const bool odd = D.odd != 0;
-            if (C.out_copies && !odd && !(clean && c + 1 == chunks)) {
-                // through shared memory, every warp its own box: a thread's stores would be 32 bytes of a row each
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                __syncwarp();
-                uint8_t* to = o_mem + (warp - 4) * 1024 + lane * 32;
-                *reinterpret_cast<uint4*>(to) = make_uint4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<uint4*>(to + 16) = make_uint4(z[4], z[5], z[6], z[7]);
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) tma_store_4d(&C.out_map, o_tile + (warp - 4) * 1024, j0, it.g * A.share + h, (int)it.span.b, (int)(f0 + (int64_t)c * kChunk + w * 32));
-            } else if (i < (c + 1 == chunks ? tail : kChunk)) {
-                store_row(A, D, it, f0 + (int64_t)c * kChunk, i, h, j0, odd, make_uint4(z[0], z[1], z[2], z[3]), make_uint4(z[4], z[5], z[6], z[7]));
+            const int64_t f = f0 + (int64_t)c * kChunk;
+            if (i >= (c + 1 == chunks ? tail : kChunk)) return;
+            if (C.out_align && !odd && j0 + 16 <= A.dv) {
+                // 32 bytes of a row, a whole sector of memory: in two stores packed sequences 336 us instead of 324
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + it.span.b * A.so.sequence + (f + i) * A.so.frame + ((int64_t)it.g * A.share + h) * A.so.head + j0;
+                if (C.out_align == 32) {
+                    store_32_bytes(out, z);
+                } else {
+                    *reinterpret_cast<uint4*>(out) = make_uint4(z[0], z[1], z[2], z[3]);
+                    *reinterpret_cast<uint4*>(out + 8) = make_uint4(z[4], z[5], z[6], z[7]);
+                }
+            } else {
+                store_row(A, D, it, f, i, h, j0, odd, make_uint4(z[0], z[1], z[2], z[3]), make_uint4(z[4], z[5], z[6], z[7]));
             }
         };
-        // Ahead of the first chunk: the state as the first of its three parts, zeros for the others and for the weights behind the diagonal.
+        // Ahead of the first chunk: the state in the first of its two accumulators, zeros in the other and for the weights behind the diagonal.
         const uint32_t state = tmem + kState + lanes + u * 16;
         const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         if (holds) {
@@ -451,9 +480,12 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             load_state(from, j0, A.dv, state);
             __syncwarp();
             tc_st(state + kCols, none);
-            tc_st(state + 2 * kCols, none);
+            if (!OUT) tc_st(state + 2 * kCols, none);
         }
-        if (OUT && u > w) tc_st(tmem + kWeights + lanes + u * 16, none);
+        if (OUT && u > w) {
+            tc_st(tmem + kWeights + lanes + u * 16, none);
+            tc_st(tmem + kRest + lanes + u * 16, none);
+        }
         tc_wait_st();
         bool ok = true;
         for (int c = 0; c < chunks; ++c) {
@@ -499,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 clear_odd(reinterpret_cast<uint4*>(v + place0), reinterpret_cast<uint4*>(v + place1));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {                            // the first part says what has to be said; what is left over is NaN
-                    const uint32_t keep = ((b[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((b[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                    const uint32_t keep = finite_halves(b[e]);
                     b[e] &= keep;
                     d[e] &= keep;
                 }
@@ -518,27 +550,35 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             *reinterpret_cast<uint4*>(w_mem + 2 * VT + place0) = make_uint4(d[0], d[1], d[2], d[3]);
             *reinterpret_cast<uint4*>(w_mem + 2 * VT + place1) = make_uint4(d[4], d[5], d[6], d[7]);
             if (OUT && holds) {
-                // the state that enters the chunk is the sum of what its three parts have become
-                uint32_t x0[16], x1[16], x2[16];
-                tc_ld(state, state + kCols, state + 2 * kCols, x0, x1, x2);
+                // the state that enters the chunk is the sum of its two accumulators
+                uint32_t x0[16], x1[16];
+                tc_ld(state, state + kCols, x0, x1);
                 const Pair whole = pair(D.whole, D.whole);
-                uint32_t part[8];                      // the state that enters the chunk, rounded
+                uint32_t part[8], rest[8];             // the state that enters the chunk in two parts
+                __nv_bfloat162 far = __floats2bfloat162_rn(0.0f, 0.0f);  // NaN as soon as a value is not finite
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const Pair y = add2(pair(x0[2 * e], x0[2 * e + 1]), add2(pair(x1[2 * e], x1[2 * e + 1]), pair(x2[2 * e], x2[2 * e + 1])));
+                    const Pair y = add2(pair(x0[2 * e], x0[2 * e + 1]), pair(x1[2 * e], x1[2 * e + 1]));
                     part[e] = round_bf16(y);
+                    rest[e] = left_bf16(y, part[e]);
+                    far = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&part[e]), __floats2bfloat162_rn(0.0f, 0.0f), far);
                     const float2 z = split(mul2(y, whole));
                     x0[2 * e] = __float_as_uint(z.x);
                     x0[2 * e + 1] = __float_as_uint(z.y);
                 }
+                if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<uint32_t*>(&far) & 0x7FFF7FFFu)) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) rest[e] &= finite_halves(part[e]);       // (the first part says what has to be said)
+                }
                 tc_st(state, x0);
                 tc_st(state + kCols, none);
-                tc_st(state + 2 * kCols, none);
                 // (the far products that read the one before are long done)
                 if (c > 0) ok = mbar_wait_warp(q_empty + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, gave_up);
                 if (!ok) break;
                 *reinterpret_cast<uint4*>(s_mem + place0) = make_uint4(part[0], part[1], part[2], part[3]);
                 *reinterpret_cast<uint4*>(s_mem + place1) = make_uint4(part[4], part[5], part[6], part[7]);
+                *reinterpret_cast<uint4*>(s_mem + ST + place0) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+                *reinterpret_cast<uint4*>(s_mem + ST + place1) = make_uint4(rest[4], rest[5], rest[6], rest[7]);
                 tc_wait_st();
             }
             fence_async_shared();
@@ -562,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                     if (w * 32 < frames) {
                         const int c0 = w * 32 + half, far = lane - half;         // columns up to the diagonal
                         const Pair hi2 = pair(hi, hi), lo2 = pair(lo, lo);
-                        uint32_t s[16], p[8];
+                        uint32_t s[16], p[8], rest[8];
                         tc_ld(tmem + kScores + lanes + c0, s);
 #pragma unroll
                         for (int e = 0; e < 8; e += 2) {
@@ -570,26 +610,34 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                             const float2 g0 = split(add2(fma2(gh.x, minus, hi2), fma2(gl.x, minus, lo2))), g1 = split(add2(fma2(gh.y, minus, hi2), fma2(gl.y, minus, lo2)));
                             const float2 z0 = split(mul2(pair(s[2 * e], s[2 * e + 1]), pair(exp2_fast(g0.x), exp2_fast(g0.y))));
                             const float2 z1 = split(mul2(pair(s[2 * e + 2], s[2 * e + 3]), pair(exp2_fast(g1.x), exp2_fast(g1.y))));
-                            p[e] = round_bf16(pair(2 * e <= far ? z0.x : 0.0f, 2 * e + 1 <= far ? z0.y : 0.0f));
-                            p[e + 1] = round_bf16(pair(2 * e + 2 <= far ? z1.x : 0.0f, 2 * e + 3 <= far ? z1.y : 0.0f));
+                            const Pair y0 = pair(2 * e <= far ? z0.x : 0.0f, 2 * e + 1 <= far ? z0.y : 0.0f), y1 = pair(2 * e + 2 <= far ? z1.x : 0.0f, 2 * e + 3 <= far ? z1.y : 0.0f);
+                            p[e] = round_bf16(y0);
+                            p[e + 1] = round_bf16(y1);
+                            rest[e] = left_bf16(y0, p[e]);
+                            rest[e + 1] = left_bf16(y1, p[e + 1]);
                         }
                         tc_st(tmem + kWeights + lanes + c0 / 2, p);
+                        tc_st(tmem + kRest + lanes + c0 / 2, rest);
                     }
                 } else {
 #pragma unroll 1
                     for (int m = 0; m < w && m * 32 < frames; ++m) {             // (to its right are the zeros of the start)
                         const int c0 = m * 32 + half;
-                        uint32_t s[16], p[8];
+                        uint32_t s[16], p[8], rest[8];
                         tc_ld(tmem + kScores + lanes + c0, s);
                         const float r = exp2_fast((hi - D.hi[m * 32 + 31]) + (lo - D.lo[m * 32 + 31]));
                         const Pair row = pair(r, r);
 #pragma unroll
                         for (int e = 0; e < 8; e += 2) {
                             const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(&D.col[c0 + 2 * e]);
-                            p[e] = round_bf16(mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, g.x)));
-                            p[e + 1] = round_bf16(mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, g.y)));
+                            const Pair y0 = mul2(pair(s[2 * e], s[2 * e + 1]), mul2(row, g.x)), y1 = mul2(pair(s[2 * e + 2], s[2 * e + 3]), mul2(row, g.y));
+                            p[e] = round_bf16(y0);
+                            p[e + 1] = round_bf16(y1);
+                            rest[e] = left_bf16(y0, p[e]);
+                            rest[e + 1] = left_bf16(y1, p[e + 1]);
                         }
                         tc_st(tmem + kWeights + lanes + c0 / 2, p);
+                        tc_st(tmem + kRest + lanes + c0 / 2, rest);
                     }
                 }
                 tc_wait_st();
@@ -611,7 +659,7 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
             tc_fence_after();
             if (holds) {
                 float* to = i >= A.dk ? nullptr : MODE == 1 ? C.S.sums + (slot_at + i) * A.dv : it.last && A.state_out ? A.state_out + (state_at + i) * A.dv : nullptr;
-                store_state(to, j0, A.dv, state);
+                store_state<OUT ? 2 : 3>(to, j0, A.dv, state);
                 __syncwarp();
             }
             if (OUT && mbar_wait_warp(answered, 0, gave_up)) {
@@ -620,7 +668,6 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 store(chunks - 1, share - 1);
             }
         }
-        if (OUT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -673,29 +720,30 @@ __global__ void __launch_bounds__(256) sr_segments_kernel(const __grid_constant_
     }
 }
 
-// [frames][sequences][heads][size] in boxes of 128 frames x 64 elements, or (outputs) of 32 x 16.
-bool encode(CUtensorMap* map, const void* data, const sr_attention_strides& st, int64_t size, int64_t heads, int64_t sequences, int64_t frames, bool out = false)
+// [frames][sequences][heads][size] in boxes of 128 frames x 64 elements.
+bool encode(CUtensorMap* map, const void* data, const sr_attention_strides& st, int64_t size, int64_t heads, int64_t sequences, int64_t frames)
 {
     const SrEncodeTiled fn = sr_encode_tiled();
     if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)size, (cuuint64_t)heads, (cuuint64_t)sequences, (cuuint64_t)frames};
     auto stride = [](int64_t s, int64_t n) { return (cuuint64_t)(n > 1 ? 2 * s : 16); };
     const cuuint64_t strides[3] = {stride(st.head, heads), stride(st.sequence, sequences), stride(st.frame, frames)};
-    const cuuint32_t box[4] = {out ? 16u : 64u, 1, 1, out ? 32u : (cuuint32_t)kChunk}, steps[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64u, 1, 1, (cuuint32_t)kChunk}, steps[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              out ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, int64_t sequences, int64_t frames)
+// Whether everything starts on `bytes` and TMA could copy it.
+bool copies_fit(const void* p, const sr_attention_strides& st, int64_t heads, int64_t sequences, int64_t frames, int bytes = 16)
 {
-    auto fits = [](int64_t s, int64_t n) { return n <= 1 || (s > 0 && s % 8 == 0 && s < ((int64_t)1 << 38)); };
-    return !((uintptr_t)p & 15) && fits(st.head, heads) && fits(st.sequence, sequences) && fits(st.frame, frames);
+    auto fits = [bytes](int64_t s, int64_t n) { return n <= 1 || (s > 0 && s % (bytes / 2) == 0 && s < ((int64_t)1 << 38)); };
+    return (uintptr_t)p % bytes == 0 && fits(st.head, heads) && fits(st.sequence, sequences) && fits(st.frame, frames);
 }
 
 template <int DK, int MODE>
 cudaError_t launch(const ChunkArgs& C, int64_t blocks, cudaStream_t s)
 {
     constexpr int tiles = kKeySlots<DK, MODE> * DK * 256 + 2 * kCols * 256;
-    constexpr int smem = 1024 + tiles + (MODE == 1 ? 2 * 3 * kCols * 256 : 2 * DK * 256 + 3 * kCols * 256 + DK * 128 + kCols * 256);
+    constexpr int smem = 1024 + tiles + (MODE == 1 ? 2 * 3 * kCols * 256 : 2 * DK * 256 + 3 * kCols * 256 + 2 * DK * 128);
     static SrSharedLimit limit;
     const cudaError_t e = limit.raise(sr_chunks_kernel<DK, MODE>, smem);
     if (e != cudaSuccess) return e;
@@ -726,9 +774,9 @@ cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
 // Frames of a segment, 0: whole sequences.  Segments are read twice (k and v for their sums, then everything for the outputs) and cost two launches and the
 // way of their states out and back, about as much as five chunks; they are for launches that would leave SMs without work, or wait for
 // one long sequence.  A step (a chunk for one head) is the unit; a chunk's sums alone are 0.6 of one.  Of packed sequences only the mean is known: the longest
-// is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 616 / 142, 4096 frames 86 / 39; 4 of 8192, 4 heads of 128 160 / 89; 8 of 1024,
-// 4 heads of 64 23 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 596 / 345; 32 of 1000, 8 heads of 64 90 / 120.  More than one wave of segments lost:
-// 32768 frames 210, 263 with two, three waves instead of 166, packed 355, 364, 396 instead of 353 (all measured alike, before the sums went without a state).
+// is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 760 / 157, 4096 frames 104 / 42; 4 of 8192, 4 heads of 128 200 / 99; 8 of 1024,
+// 4 heads of 64 28 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 538 / 317; 32 of 1000, 8 heads of 64 87 / 118.  More than one wave of segments lost:
+// 32768 frames 210, 263 with two, three waves instead of 166, packed 355, 364, 396 instead of 353 (measured alike, on an earlier form of the kernel).
 AttentionCut cut_of(const sr_attention_desc* d, bool packed)
 {
     AttentionCut cut{0, 0};
@@ -805,7 +853,8 @@ cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d,
     if (!encode(&C.q_map, A.q, A.sq, d->dk, d->heads, sequences, d->frames) || !encode(&C.k_map, A.k, A.sk, d->dk, d->groups, sequences, d->frames) ||
         !encode(&C.v_map, A.v, A.sv, d->dv, d->groups, sequences, d->frames))
         return cudaErrorInvalidValue;
-    C.out_copies = copies_fit(A.out, A.so, d->heads, sequences, d->frames);
-    if (C.out_copies && !encode(&C.out_map, A.out, A.so, d->dv, d->heads, sequences, d->frames, true)) return cudaErrorInvalidValue;
+    C.out_align = 0;
+    for (const int bytes : {16, 32})
+        if (copies_fit(A.out, A.so, d->heads, sequences, d->frames, bytes)) C.out_align = bytes;
     return d->dk <= 64 ? launch_all<64>(C, s) : launch_all<128>(C, s);
 }
