@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
     const T* x = static_cast<const T*>(A.x) + r0 * A.x_stride;
     const T* res = NORM && A.residual ? static_cast<const T*>(A.residual) + r0 * A.r_stride : nullptr;
     const int tpr = blockDim.x, tid = threadIdx.x;
-    const int64_t end = FMT >= SR_FORMAT_MX8 ? A.tiles_g * 128 : A.cols;
+    const int64_t end = FMT >= SR_FORMAT_MX8 ? A.tiles_g * 128 : A.cols + (SHIFT ? VEC : 0);          // (units may begin a part of one ahead of the row)
     const int n_it = HOLD ? HOLD : (int)((end + (int64_t)tpr * VEC - 1) / ((int64_t)tpr * VEC));
     const int64_t shift = SHIFT ? (int64_t)(((uintptr_t)x & 15) / sizeof(T)) : 0;
     auto column = [&](int it) { return ((int64_t)it * tpr + tid) * VEC - shift; };

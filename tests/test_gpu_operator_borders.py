@@ -35,3 +35,21 @@ def test_bf16_runs_are_as_exact_as_their_outputs(T, B, heads, groups, dk, dv, ga
     state = torch.randn(B, groups, dk, dv, generator=gen(91), device=DEV)
     out, last = sr.linear_attention_run(q, k, v, d, state=state, scale=0.3)
     compare(q, k, v, d, state, out, last, 0.3, "bf16", [(slice(None), b) for b in range(B)])
+
+
+# ------------------------------------------------------------------------------------------ norm
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows, cols, dtype", [(3, 40959, "bf16"), (9, 40953, "bf16"), (2, 32769, "bf16"), (3, 20479, "fp32"), (5, 20477, "fp32"), (2, 16385, "fp32")])
+def test_norm_of_wide_rows_that_start_off_16_bytes(rows, cols, dtype, residual):
+    # wider than the registers of 1024 threads hold, the row's last unit behind the last whole pass of them
+    x = torch.randn(rows, cols, generator=gen(92), device=DEV).to(TYPES[dtype])
+    r = torch.randn(rows, cols, generator=gen(93), device=DEV).to(TYPES[dtype]) if residual else None
+    w = torch.randn(cols, generator=gen(94), device=DEV)
+    got = sr.rms_norm(x, w, residual=r, eps=1e-5)
+    y, s = oracle.norm(host(x), host(w), None if r is None else host(r), 1e-5)
+    bound = (oracle.HALF_STEP[dtype] + ((cols + 3) / 2 + 8) * 2.0 ** -23) * np.abs(y)
+    if residual:
+        bound = bound + 2.0 ** -23 * np.abs(host(w)) * (np.abs(host(x)) + np.abs(host(r))) / np.sqrt((s * s).mean(-1, keepdims=True) + 1e-5)
+        within(got[1], s, (oracle.HALF_STEP[dtype] + 2.0 ** -24) * np.abs(s))
+        got = got[0]
+    within(got, y, bound)
