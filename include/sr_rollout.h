@@ -325,6 +325,7 @@ sr_status sr_microscale_product(const void* a_data_dev, const void* a_scales_dev
 
 /*
  * Root-mean-square norm: s = x + residual (in 32 bits), out = s / sqrt(mean(s^2) + eps) * weight.
+ * Squares that leave the range of 32 bits do not matter: a row of 1e20 or of 1e-30 (eps = 0) is as exact as others.
  * x, residual [rows][cols] of `dtype` (residual may be NULL), rows x_stride / residual_stride elements apart; weight: float [cols] or NULL (ones).
  * sum (may be NULL): s rounded to `dtype`, [rows][cols] without gaps; it may be x or residual if that has no gaps either.
  * out: SR_FORMAT_F32 / BF16 must equal `dtype`, [rows][cols] without gaps; SR_FORMAT_MX8 / MX4: microscaled data, with `scales`

@@ -82,7 +82,7 @@ __device__ __forceinline__ void store_scaled(const RowArgs& A, int64_t row, int6
 #pragma unroll
     for (int d = 1; d < 32 / VEC; d *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
     const uint32_t byte = sr_scale_byte<FMT>(most);
-    const float inv = sr_inverse_scale(byte);          // (of a group that is not finite: anything, its scale says NaN)
+    const float inv = sr_inverse_scale(byte);
     const int64_t g = c >> 5;
     float z[VEC];
     if constexpr (VEC == 1) {
@@ -134,9 +134,10 @@ __device__ __forceinline__ void store_scaled(const RowArgs& A, int64_t row, int6
 }
 
 // HOLD: units of a thread that stay in registers; 0: rows of any length, read twice.  FMT F32: the type of x.
+// Two blocks to an SM (32 registers) where single values are held or rows are read again: the code for rare rows would take 46 (16384 x 1003 fp32 to 8 bits 88 us and 104).
 // SHIFT: rows that do not start on 16 bytes, but alike in all buffers: a thread's units do, the first of a row may begin ahead of it.
 template <typename T, int VEC, int HOLD, bool NORM, int FMT, bool SHIFT>
-__global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ RowArgs A)
+__global__ void __launch_bounds__(1024, NORM && (HOLD == 0 || (VEC == 1 && HOLD == 8)) ? 2 : 0) sr_row_kernel(const __grid_constant__ RowArgs A)
 {
     __shared__ float part[32];
     srx::let_successor_start();
@@ -172,8 +173,19 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
             }
         }
     };
+    // a unit, or its columns that there are
+    auto put = [&](T* to, int64_t c, const float (&s)[VEC]) {
+        const bool there = row_there && c < A.cols;
+        if (there && whole(c)) {
+            store_unit<T, VEC>(to + row * A.cols + c, s);
+        } else if (SHIFT && there) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (c + i >= 0 && c + i < A.cols) to[row * A.cols + c + i] = (T)s[i];
+        }
+    };
     float f[HOLD ? HOLD : 1][VEC];
-    float inv = 1.0f;
+    float inv = 1.0f, by = 1.0f;                       // what a row is multiplied with; ahead of that (rows that are read again)
     if (HOLD) {
 #pragma unroll
         for (int it = 0; it < (HOLD ? HOLD : 1); ++it) load(it, f[it]);
@@ -192,30 +204,65 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
                 for (int i = 0; i < VEC; ++i) ss = fmaf(f[0][i], f[0][i], ss);
             }
         }
+        auto over_row = [&](float mine, auto join) {   // over the row's threads; 0 joins nothing
 #pragma unroll
-        for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, d);
-        if (tpr > 32) {                                // (one row per block)
-            if (!(tid & 31)) part[tid >> 5] = ss;
-            __syncthreads();
-            ss = (tid & 31) < (tpr >> 5) ? part[tid & 31] : 0.0f;
+            for (int d = 16; d; d /= 2) mine = join(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, d));
+            if (tpr > 32) {                            // (one row per block)
+                if (!(tid & 31)) part[tid >> 5] = mine;
+                __syncthreads();
+                mine = (tid & 31) < (tpr >> 5) ? part[tid & 31] : 0.0f;
 #pragma unroll
-            for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, d);
+                for (int d = 16; d; d /= 2) mine = join(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, d));
+            }
+            return mine;
+        };
+        auto add = [](float a, float b) { return a + b; };
+        ss = over_row(ss, add);
+        const float mean = ss / (float)A.cols + A.eps;
+        inv = 1.0f / sqrtf(mean);
+        if (HOLD && A.sum)                             // (ahead of what a rare row does to its values)
+#pragma unroll
+            for (int it = 0; it < (HOLD ? HOLD : 1); ++it) put(static_cast<T*>(A.sum), column(it), f[it]);
+        if (!(mean >= 0x1p-100f && ss <= 3.4028234e38f)) {
+            // (the same for all threads of the row) Squares that 32 bits do not hold, or so small that they have lost bits: once more with the row divided by the power of two
+            // of its largest value, or of sqrt(eps).
+            auto each = [&](auto what) {
+                if (HOLD) {
+#pragma unroll
+                    for (int it = 0; it < (HOLD ? HOLD : 1); ++it)
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) what(f[it][i], column(it) + i < A.cols);
+                } else {
+#pragma unroll 1
+                    for (int it = 0; it < n_it; ++it) {
+                        load(it, f[0]);
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) what(f[0][i], true);
+                    }
+                }
+            };
+            const float root = sqrtf(A.eps);
+            uint32_t most = __float_as_uint(root);
+            each([&](float& y, bool) { most = max(most, __float_as_uint(y) & 0x7FFFFFFFu); });
+            if (tpr > 32) __syncthreads();
+            most = __float_as_uint(over_row(__uint_as_float(most), [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
+            // (what is not finite: as the formula has it)
+            if (most < 0x7F800000u) by = __uint_as_float((254u - min(max(most >> 23, 1u), 253u)) << 23);
+            ss = 0.0f;
+            each([&](float& y, bool) { ss = fmaf(y * by, y * by, ss); });
+            if (tpr > 32) __syncthreads();
+            ss = over_row(ss, add);
+            inv = 1.0f / sqrtf(ss / (float)A.cols + root * by * (root * by));
+            if (HOLD) {
+                each([&](float& y, bool there) { y = there ? y * by * inv : 0.0f; });      // (zeros behind the last column whatever inv is)
+                inv = 1.0f;
+            }
         }
-        inv = 1.0f / sqrtf(ss / (float)A.cols + A.eps);
     }
     auto finish = [&](int it, float (&s)[VEC]) {
         const int64_t c = column(it);
-        const bool there = row_there && c < A.cols, all = there && whole(c);
-        auto put = [&](T* to) {
-            if (all) {
-                store_unit<T, VEC>(to + row * A.cols + c, s);
-            } else if (SHIFT && there) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    if (c + i >= 0 && c + i < A.cols) to[row * A.cols + c + i] = (T)s[i];
-            }
-        };
-        if (NORM && A.sum) put(static_cast<T*>(A.sum));
+        const bool there = row_there && c < A.cols;
+        if (NORM && !HOLD && A.sum) put(static_cast<T*>(A.sum), c, s);
         if (NORM) {
             float w[VEC];
 #pragma unroll
@@ -236,10 +283,13 @@ __global__ void __launch_bounds__(1024) sr_row_kernel(const __grid_constant__ Ro
                 }
             }
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s[i] = s[i] * inv * w[i];
+            for (int i = 0; i < VEC; ++i) {
+                if (HOLD) s[i] = s[i] * inv * w[i];
+                else s[i] = there ? s[i] * by * inv * w[i] : 0.0f;
+            }
         }
         if constexpr (FMT >= SR_FORMAT_MX8) store_scaled<VEC, FMT>(A, row, c, s, largest(s), row_there);
-        else put(static_cast<T*>(A.out));
+        else put(static_cast<T*>(A.out), c, s);
     };
     if (HOLD) {
 #pragma unroll

@@ -53,3 +53,23 @@ def test_norm_of_wide_rows_that_start_off_16_bytes(rows, cols, dtype, residual):
         within(got[1], s, (oracle.HALF_STEP[dtype] + 2.0 ** -24) * np.abs(s))
         got = got[0]
     within(got, y, bound)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("cols", [1, 7, 96, 1003, 4096, 40959])
+def test_norm_of_rows_whose_squares_leave_32_bits(cols, dtype):
+    sizes = [1e20, 3e38, 2e19, 1e-30, 1e-42, 1e-20, 1.0, 1e19]
+    x = torch.empty(len(sizes), cols, device=DEV).uniform_(0.5, 1.0, generator=gen(95)) * torch.tensor(sizes, device=DEV)[:, None]
+    x = (x * torch.where(torch.rand(x.shape, generator=gen(96), device=DEV) < 0.5, -1.0, 1.0)).to(TYPES[dtype])
+    w = torch.randn(cols, generator=gen(97), device=DEV)
+    for eps in (0.0, 1e-12, 1e-30, 1e-44):
+        eps = float(np.float32(eps))
+        y = oracle.norm(host(x), host(w), eps=eps)[0]
+        # as for other rows, and three steps more for the root of eps, its square and the row's division
+        bound = (oracle.HALF_STEP[dtype] + ((cols + 3) / 2 + 11) * 2.0 ** -23) * np.abs(y) + 2.0 ** -148
+        bound = np.nan_to_num(bound) + (2.0 ** -133 if dtype == "bf16" else 0.0)           # (zeros over zero are NaN on both sides)
+        within(sr.rms_norm(x, w, eps=eps), y, bound)
+        if dtype == "fp32":
+            got = sr.rms_norm(x, w, eps=eps, format="mx8")
+            again = sr.quantize(sr.rms_norm(x, w, eps=eps), "mx8")
+            assert torch.equal(got.data, again.data) and torch.equal(got.values(), again.values())
