@@ -20,8 +20,8 @@ __device__ __forceinline__ uint32_t sr_scale_byte(uint32_t amax_bits)
     const int k = FMT == SR_FORMAT_MX4 ? e - 2 + ((amax_bits & 0x7FFFFFu) > 0x400000u) : e - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u);
     return (uint32_t)(k > 0 ? k : 0);
 }
-// 2^-(byte - 127), exact for every byte but 255 (254 and 253 do not occur: amax < 2^128)
-__device__ __forceinline__ float sr_inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+// 2^-(byte - 127), exact for every byte up to 253 (254 does not occur: amax < 2^128); 0 for 255, so that zeros that pad a group which is not finite stay zeros
+__device__ __forceinline__ float sr_inverse_scale(uint32_t byte) { return byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23); }
 // 2^(byte - 127); 2^-127 is subnormal
 __device__ __forceinline__ float sr_scale(uint32_t byte)
 {

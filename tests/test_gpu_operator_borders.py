@@ -73,3 +73,21 @@ def test_norm_of_rows_whose_squares_leave_32_bits(cols, dtype):
             got = sr.rms_norm(x, w, eps=eps, format="mx8")
             again = sr.quantize(sr.rms_norm(x, w, eps=eps), "mx8")
             assert torch.equal(got.data, again.data) and torch.equal(got.values(), again.values())
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("cols", [5, 72, 200, 1000])
+def test_padding_is_zero_in_rows_that_are_not_finite(cols, dtype, fmt):
+    x = torch.randn(6, cols, generator=gen(98), device=DEV).to(TYPES[dtype])
+    x[1, cols // 2], x[2, cols - 1], x[3] = float("nan"), float("inf"), 0.0
+    groups = -(-cols // 32)
+    tiles = -(-groups // 4)
+    for m in (sr.rms_norm(x, eps=0.0, format=fmt), sr.quantize(x, fmt)):
+        scales = m.scales.view(tiles, 32, 4, 4)[:, :6, 0].permute(1, 0, 2).reshape(6, tiles * 4)
+        assert (scales[:, groups:] == 0).all()
+        data = m.data.view(6, -1)
+        pad = data[:, (cols + 1) // 2:] if fmt == "mx4" else data[:, cols:]
+        assert ((pad & (0x77 if fmt == "mx4" else 0x7F)) == 0).all()
+        if fmt == "mx4" and cols % 2:
+            assert ((data[:, cols // 2] >> 4 & 7) == 0).all()
