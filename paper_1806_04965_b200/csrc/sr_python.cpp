@@ -45,6 +45,14 @@ bool rows_of(const at::Tensor& t, int64_t& stride)
 }
 bool floats(const at::Tensor* t, int64_t n) { return t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == n && t->is_contiguous(); }
 
+// Whether a microscaled matrix's buffers have the sizes that its rows, columns and format make.
+bool scaled_fits(const at::Tensor* data, const at::Tensor* scales, int64_t rows, int64_t cols, int format)
+{
+    size_t data_bytes = 0, scale_bytes = 0;
+    return sr_microscale_bytes(rows, cols, format, &data_bytes, &scale_bytes) == SR_OK && data->scalar_type() == at::kByte && scales->scalar_type() == at::kByte &&
+           data->is_contiguous() && scales->is_contiguous() && (size_t)data->numel() == data_bytes && (size_t)scales->numel() == scale_bytes;
+}
+
 PyObject* none() { Py_RETURN_NONE; }
 // Without the interpreter's lock: an allocation or a launch may have to wait for the device, which may wait for another thread's launch.
 struct Unlocked {
@@ -118,9 +126,14 @@ PyObject* py_product(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor *ad = tensor(a[0]), *as = tensor(a[1]), *wd = tensor(a[3]), *ws = tensor(a[4]);
         const int64_t rows = PyLong_AsLongLong(a[2]), outs = PyLong_AsLongLong(a[5]), cols = PyLong_AsLongLong(a[6]);
         const int format = (int)PyLong_AsLong(a[7]), relu = PyObject_IsTrue(a[9]), dtype = (int)PyLong_AsLong(a[10]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
         const at::Tensor *bias = a[8] == Py_None ? nullptr : tensor(a[8]), *given = a[11] == Py_None ? nullptr : tensor(a[11]);
         Device d;
         if (!d.fits(ad) || !d.fits(as) || !d.fits(wd) || !d.fits(ws) || !d.current()) return none();
+        if (!scaled_fits(ad, as, rows, cols, format) || !scaled_fits(wd, ws, outs, cols, format)) return none();
         if (a[8] != Py_None && (!d.fits(bias) || !floats(bias, outs))) return none();
         at::Tensor out;
         int64_t stride = outs;

@@ -128,15 +128,20 @@ class Microscaled:
     __slots__ = ("data", "scales", "rows", "cols", "format")
 
     def __init__(self, data, scales, rows: int, cols: int, format: str):
+        self.data, self.scales, self.rows, self.cols, self.format = data, scales, rows, cols, format
+        self._check("Microscaled")
+
+    def _check(self, call: str):
+        """Whether data and scales have the sizes that rows, cols and format make (all of them can be assigned)."""
+        data, scales, rows, cols, format = self.data, self.scales, self.rows, self.cols, self.format
         if format not in FORMATS:
-            _refuse("Microscaled", "format is one of %s" % ", ".join(FORMATS))
+            _refuse(call, "format is one of %s" % ", ".join(FORMATS))
         if rows < 0 or cols < 1:
-            _refuse("Microscaled", "a size is out of range")
+            _refuse(call, "a size is out of range")
         groups = -(-cols // 32)
         if data.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or not data.is_contiguous() or not scales.is_contiguous() or \
                 data.numel() != rows * groups * (16 if format == "mx4" else 32) or scales.numel() != -(-rows // 128) * -(-groups // 4) * 512:
-            _refuse("Microscaled", "data and scales have to be uint8, without gaps, of the sizes that rows, cols and format make")
-        self.data, self.scales, self.rows, self.cols, self.format = data, scales, rows, cols, format
+            _refuse(call, "data and scales have to be uint8, without gaps, of the sizes that rows, cols and format make")
 
     @classmethod
     def empty(cls, rows: int, cols: int, format: str, device):
@@ -156,6 +161,7 @@ class Microscaled:
 
     def values(self):
         """The values it stands for, float32 [rows][cols]."""
+        self._check("values")
         device = _tensors("values", self.data, self.scales)
         out = self.data.new_empty((self.rows, self.cols), dtype=torch.float32)
         _call("sr_microscale_values", device, _library().sr_microscale_values, self.data.data_ptr(), self.scales.data_ptr(), FORMATS[self.format], self.rows,
@@ -185,10 +191,12 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
     gaps between them) is written in place of a new tensor of `dtype`."""
     if a.format != w.format or a.cols != w.cols:
         _refuse("product", "both matrices have the same format and number of columns")
-    fast = _compiled.product(a.data, a.scales, a.rows, w.data, w.scales, w.rows, a.cols, FORMATS[a.format], bias, relu, _DTYPES.get(dtype, -1), out) \
+    fast = _compiled.product(a.data, a.scales, a.rows, w.data, w.scales, w.rows, a.cols, FORMATS.get(a.format, 0), bias, relu, _DTYPES.get(dtype, -1), out) \
         if out is not None or dtype in _DTYPES else None
     if fast is not None:
         return fast
+    a._check("product")
+    w._check("product")
     device = _tensors("product", a.data, a.scales, w.data, w.scales, bias, out)
     b = _float_vector("product", "bias", bias, w.rows)
     if out is None:
