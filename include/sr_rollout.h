@@ -370,8 +370,11 @@ sr_status sr_linear_attention_run(const sr_attention_desc* desc, const void* q_d
 sr_status sr_linear_attention_step(const sr_attention_desc* desc, const void* q_dev, const void* k_dev, const void* v_dev, const float* log_decay_dev,
                                    float* state_dev, void* out_dev, void* stream);
 /* Synchronises `stream` and reports SR_ERR_CUDA if queued work failed, SR_ERR_TIMEOUT if a bounded wait inside one of the operators' kernels
- * expired on the current device since the last call (its outputs are then not valid). */
+ * has expired on the current device, on whichever stream (outputs since then may not be valid); every later call, of any thread, reports it again until
+ * sr_operator_reset.  SR_ERR_STATE: the stream is being captured. */
 sr_status sr_operator_status(void* stream);
+/* Forgets, in `stream`'s order, that a wait expired on the current device.  Errors: CUDA. */
+sr_status sr_operator_reset(void* stream);
 
 const char* sr_status_str(sr_status s);
 

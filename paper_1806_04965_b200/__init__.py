@@ -8,7 +8,7 @@ operators.py binds the operators of the temporal head that may stand behind a ro
 from .binding import Graph, SrError, load_library, STATUS  # noqa: F401
 
 
-_OPERATORS = ("Microscaled", "TemporalHead", "linear_attention_run", "linear_attention_step", "operator_status", "product", "quantize", "rms_norm")
+_OPERATORS = ("Microscaled", "TemporalHead", "linear_attention_run", "linear_attention_step", "operator_reset", "operator_status", "product", "quantize", "rms_norm")
 
 
 def __getattr__(name):

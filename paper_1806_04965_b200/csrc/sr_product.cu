@@ -23,7 +23,7 @@
 #include "sr_operators.h"
 #include "sr_ptx.cuh"
 
-static __device__ int sr_operator_error;              // 1: a bounded wait expired
+static __device__ int sr_operator_error;              // 1: a bounded wait expired since the last sr_operator_reset
 
 namespace {
 using namespace srx;
@@ -469,25 +469,35 @@ sr_status sr_microscale_product(const void* a_data, const void* a_scales, const 
 
 sr_status sr_operator_status(void* stream)
 {
-    if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return SR_ERR_CUDA;
+    // read in the stream's own order and left as it is: another stream's owner has to see it, too
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) return SR_ERR_CUDA;
+    if (capturing != cudaStreamCaptureStatusNone) return SR_ERR_STATE;
     int expired = 0;
-    const int none = 0;
-    if (cudaMemcpyFromSymbol(&expired, sr_operator_error, sizeof(int)) != cudaSuccess) return SR_ERR_CUDA;
-    if (!expired) return SR_OK;
-    return cudaMemcpyToSymbol(sr_operator_error, &none, sizeof(int)) == cudaSuccess ? SR_ERR_TIMEOUT : SR_ERR_CUDA;
+    const int* word = sr_operator_error_word();
+    if (!word || cudaMemcpyAsync(&expired, word, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return SR_ERR_CUDA;
+    return expired ? SR_ERR_TIMEOUT : SR_OK;
+}
+
+sr_status sr_operator_reset(void* stream)
+{
+    int* word = sr_operator_error_word();
+    return word && cudaMemsetAsync(word, 0, sizeof(int), static_cast<cudaStream_t>(stream)) == cudaSuccess ? SR_OK : SR_ERR_CUDA;
 }
 
 }  // extern "C"
 
 int* sr_operator_error_word()
 {
-    static int* known[64];
+    static std::atomic<int*> known[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
-    if (dev < 64 && known[dev]) return known[dev];
+    if (dev < 64)
+        if (int* had = known[dev].load(std::memory_order_relaxed)) return had;
     void* p = nullptr;
     if (cudaGetSymbolAddress(&p, sr_operator_error) != cudaSuccess) return nullptr;
-    if (dev < 64) known[dev] = static_cast<int*>(p);
+    if (dev < 64) known[dev].store(static_cast<int*>(p), std::memory_order_relaxed);
     return static_cast<int*>(p);
 }
 
@@ -504,12 +514,13 @@ SrEncodeTiled sr_encode_tiled()
 
 int sr_device_sms()
 {
-    static int known[64];
+    static std::atomic<int> known[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    if (dev < 64 && known[dev]) return known[dev];
+    if (dev < 64)
+        if (const int had = known[dev].load(std::memory_order_relaxed)) return had;
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    if (dev < 64) known[dev] = n;
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
     return n;
 }

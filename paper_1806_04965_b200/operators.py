@@ -61,6 +61,7 @@ def _library():
             "sr_linear_attention_run": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
             "sr_linear_attention_step": [desc, vp, vp, vp, vp, vp, vp, vp],
             "sr_operator_status": [vp],
+            "sr_operator_reset": [vp],
         }.items():
             f = getattr(lib, name)
             f.argtypes, f.restype = args, i32
@@ -355,10 +356,22 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0):
     return out
 
 
+def _device_index(call: str, device) -> int:
+    d = torch.device("cuda" if device is None else device)
+    if d.type != "cuda":
+        _refuse(call, "a CUDA device is required")
+    return torch.cuda.current_device() if d.index is None else d.index
+
+
 def operator_status(device=None):
-    """Waits for the current stream's work; raises `SrError` if it failed or a bounded wait inside an operator's kernel expired."""
-    index = torch.cuda.current_device() if device is None else torch.device(device).index
-    _call("sr_operator_status", index, _library().sr_operator_status)
+    """Waits for the current stream's work; raises `SrError` if it failed or a bounded wait inside an operator's kernel has expired on the device (until
+    `operator_reset`)."""
+    _call("sr_operator_status", _device_index("operator_status", device), _library().sr_operator_status)
+
+
+def operator_reset(device=None):
+    """Forgets that a wait expired."""
+    _call("sr_operator_reset", _device_index("operator_reset", device), _library().sr_operator_reset)
 
 
 class TemporalHead:

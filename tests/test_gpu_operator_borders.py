@@ -91,3 +91,82 @@ def test_padding_is_zero_in_rows_that_are_not_finite(cols, dtype, fmt):
         assert ((pad & (0x77 if fmt == "mx4" else 0x7F)) == 0).all()
         if fmt == "mx4" and cols % 2:
             assert ((data[:, cols // 2] >> 4 & 7) == 0).all()
+
+
+# ------------------------------------------------------------------------------------------ waits that run out
+WAIT = r"""
+#include "sr_ptx.cuh"
+// A wait as the operators' kernels have it, on a barrier at which nothing arrives.
+__global__ void wait_for_nothing(int* error)
+{
+    __shared__ uint64_t bar;
+    __shared__ int gave_up;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        srx::mbar_init(srx::smem_u32(&bar), 1);
+        srx::mbar_init_done();
+    }
+    __syncthreads();
+    srx::mbar_wait_warp(srx::smem_u32(&bar), 0, &gave_up);
+    __syncthreads();
+    if (threadIdx.x == 0 && gave_up) atomicExch(error, 1);
+}
+extern "C" int run(int* error, void* stream)
+{
+    wait_for_nothing<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(error);
+    return cudaGetLastError();
+}
+"""
+
+
+def test_a_wait_that_runs_out_is_reported_to_everyone_until_it_is_reset(tmp_path):
+    import ctypes
+    import os
+    import subprocess
+    import threading
+    from paper_1806_04965_b200 import build, operators
+    source, lib = tmp_path / "wait.cu", tmp_path / "wait.so"
+    source.write_text(WAIT)
+    subprocess.check_call([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-shared", *build.NVCC_FLAGS, "-I", build.CSRC, str(source), "-o", str(lib)])
+    word = operators._library()._Z22sr_operator_error_wordv
+    word.restype = ctypes.c_void_p
+    sr.operator_status()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    wait = ctypes.CDLL(str(lib))
+    assert wait.run(ctypes.c_void_p(word()), ctypes.c_void_p(a.cuda_stream)) == 0
+    a.synchronize()
+    seen = []
+
+    def ask(stream):
+        with torch.cuda.stream(stream):
+            try:
+                sr.operator_status()
+                seen.append("ok")
+            except sr.SrError as e:
+                seen.append(e.status)
+    try:
+        ask(b)                                                  # another stream's owner first
+        ask(a)
+        t = threading.Thread(target=ask, args=(torch.cuda.Stream(),))
+        t.start()
+        t.join()
+        assert seen == ["SR_ERR_TIMEOUT"] * 3
+    finally:
+        sr.operator_reset()
+        torch.cuda.synchronize()
+    for device in (None, 0, "cuda", "cuda:0", torch.device("cuda"), torch.device("cuda:0")):
+        sr.operator_status(device)
+
+
+def test_status_of_a_stream_that_is_captured_is_refused_and_the_capture_lives():
+    x = torch.randn(4, 64, device=DEV)
+    want = sr.rms_norm(x)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        out = sr.rms_norm(x)
+        with pytest.raises(sr.SrError):
+            sr.operator_status()
+    g.replay()
+    assert torch.equal(out, want)
+    sr.operator_status()

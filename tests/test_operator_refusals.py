@@ -23,3 +23,9 @@ def test_an_argument_without_a_truth_value_raises_its_own_error():
     m = sr.Microscaled.empty(4, 64, "mx4", "cpu")
     with pytest.raises((SrError, ValueError)):                  # not a SystemError of a call that returned with an exception set
         sr.product(m, m, relu=np.array([1, 2]))
+
+
+def test_status_of_something_that_is_no_cuda_device_is_refused():
+    for call in (sr.operator_status, sr.operator_reset):
+        with pytest.raises(SrError, match="CUDA device"):
+            call("cpu")
