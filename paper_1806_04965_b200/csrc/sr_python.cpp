@@ -17,12 +17,14 @@ namespace {
 // The tensor behind an argument; null where there is none.
 const at::Tensor* tensor(PyObject* o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 
-// Tensors on the current device that no gradient is recorded for.
+// Tensors on the current device that no gradient is recorded for, in either direction.
 struct Device {
     int index = -1;
     bool fits(const at::Tensor* t)
     {
-        if (!t || !t->defined() || !t->is_cuda() || t->layout() != at::kStrided || (c10::GradMode::is_enabled() && t->requires_grad())) return false;
+        if (!t || !t->defined() || !t->is_cuda() || t->layout() != at::kStrided || (c10::GradMode::is_enabled() && t->requires_grad()) ||
+            t->_fw_grad(0).defined())
+            return false;
         if (index < 0) index = (int)t->get_device();
         return t->get_device() == index;
     }

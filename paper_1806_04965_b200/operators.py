@@ -2,8 +2,8 @@
 
 Argument marshalling only, like `Graph`, and a call's common case in compiled code (csrc/sr_python.cpp; what that does not take comes back
 here to be done or refused): tensors live on a CUDA device, work goes to the current stream of that device, outputs and
-workspaces come from PyTorch's allocator, and every refusal is an `SrError`.  There is no backward pass: a tensor that
-requires a gradient is refused while gradients are recorded.
+workspaces come from PyTorch's allocator, and every refusal is an `SrError`.  There are no derivatives: a tensor that
+requires a gradient is refused while gradients are recorded, one with a tangent always.
 
   quantize, Microscaled, product   matrices in groups of 32 with a scale each, 4 ("mx4") or 8 ("mx8") bits per element; a dense node's update
   rms_norm                         root-mean-square norm with the residual's addition, output in full or microscaled
@@ -17,6 +17,8 @@ import math
 from typing import Optional
 
 import torch
+
+from torch.autograd import forward_ad as _forward_ad
 
 from . import binding
 from .binding import SrError
@@ -77,6 +79,7 @@ def _refuse(call: str, why: str):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _grad = torch.is_grad_enabled
+_wrapped = torch._C._functorch.is_functorch_wrapped_tensor
 
 
 def _call(call: str, device: int, function, *args):
@@ -91,15 +94,17 @@ def _call(call: str, device: int, function, *args):
 
 
 def _tensors(call: str, first, *others) -> int:
-    """All on one CUDA device (its index is returned), none that a gradient is recorded for."""
+    """All on one CUDA device (its index is returned), none that a gradient is recorded for, in either direction."""
+    if _grad() and (first.requires_grad or any(t is not None and t.requires_grad for t in others)):
+        _refuse(call, "there is no backward pass (use torch.no_grad() or detach)")
+    if any(t is not None and (_wrapped(t) or _forward_ad.unpack_dual(t).tangent is not None) for t in (first,) + others):
+        _refuse(call, "there is no forward derivative (use the primal, or detach)")
     device = first.get_device()
     if device < 0 or not first.is_cuda:
         _refuse(call, "tensors on a CUDA device are required")
     for t in others:
         if t is not None and t.get_device() != device:
             _refuse(call, "tensors lie on different devices")
-    if _grad() and (first.requires_grad or any(t is not None and t.requires_grad for t in others)):
-        _refuse(call, "there is no backward pass (use torch.no_grad() or detach)")
     return device
 
 

@@ -29,3 +29,49 @@ def test_status_of_something_that_is_no_cuda_device_is_refused():
     for call in (sr.operator_status, sr.operator_reset):
         with pytest.raises(SrError, match="CUDA device"):
             call("cpu")
+
+
+def calls(x):
+    """Every call with x (a float32 tensor of at least 2 x 64 elements) as one of its inputs."""
+    m = sr.Microscaled.empty(4, 64, "mx4", "cpu") if not x.is_cuda else sr.quantize(torch.zeros(4, 64, device=x.device))
+    v = torch.zeros(64, device=x.device)
+    h = x.reshape(-1)[:128].view(1, 2, 64)
+    o = torch.zeros(1, 2, 64, device=x.device)
+    d, s = torch.zeros(2, device=x.device), torch.zeros(1, 2, 64, 64, device=x.device)
+    row = x.reshape(-1)[:64]
+    return [lambda: sr.quantize(x), lambda: sr.rms_norm(x), lambda: sr.rms_norm(x.detach(), row), lambda: sr.rms_norm(x.detach(), v, residual=x),
+            lambda: sr.product(m, m, bias=row[:4]), lambda: sr.linear_attention_step(h, o, o, d, s), lambda: sr.linear_attention_step(o, h, o, d, s),
+            lambda: sr.linear_attention_step(o, o, h, d, s), lambda: sr.linear_attention_step(o, o, o, row[:2], s),
+            lambda: sr.linear_attention_run(h[None], o[None], o[None], d), lambda: sr.linear_attention_run(o[None], o[None], h[None], d),
+            lambda: sr.linear_attention_run(o[None], o[None], o[None], row[:2])]
+
+
+@pytest.mark.parametrize("device", ["cpu", pytest.param("cuda:0", marks=pytest.mark.gpu)])
+def test_derivatives_are_refused_in_both_directions(device):
+    import torch.autograd.forward_ad as forward_ad
+    x = torch.ones(4, 64, device=device)
+    for call in calls(x.clone().requires_grad_()):
+        with pytest.raises(SrError, match="no backward pass"):
+            call()
+    with forward_ad.dual_level():
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad):
+                for call in calls(forward_ad.make_dual(x, torch.ones_like(x))):
+                    with pytest.raises(SrError, match="no forward derivative"):
+                        call()
+    with pytest.raises(SrError, match="no forward derivative"):
+        torch.func.jvp(lambda y: sr.rms_norm(y), (x,), (x,))
+
+
+@pytest.mark.gpu
+def test_what_has_no_derivative_recorded_is_still_taken():
+    x = torch.ones(4, 64, device="cuda:0")
+    for y in (x, x.clone().requires_grad_().detach()):
+        for call in calls(y):
+            call()
+    with torch.no_grad():
+        for call in calls(x.clone().requires_grad_()):
+            call()
+    with torch.inference_mode():
+        for call in calls(torch.ones(4, 64, device="cuda:0")):
+            call()
