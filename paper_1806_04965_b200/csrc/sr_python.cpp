@@ -55,6 +55,12 @@ bool scaled_fits(const at::Tensor* data, const at::Tensor* scales, int64_t rows,
            data->is_contiguous() && scales->is_contiguous() && (size_t)data->numel() == data_bytes && (size_t)scales->numel() == scale_bytes;
 }
 
+// What was written in place: whoever has kept the tensor for a gradient learns of it.  (Tensors of inference mode have no versions.)
+void written(const at::Tensor& t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject* none() { Py_RETURN_NONE; }
 // Without the interpreter's lock: an allocation or a launch may have to wait for the device, which may wait for another thread's launch.
 struct Unlocked {
@@ -151,6 +157,7 @@ PyObject* py_product(PyObject*, PyObject* const* a, Py_ssize_t n)
                                        bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, relu ? 1 : 0, out.data_ptr(), type_of(out), stride, d.stream());
         }
         if (st != SR_OK) return none();
+        if (given) written(*given);
         return wrap(out);
     })
 }
@@ -265,6 +272,7 @@ PyObject* py_step(PyObject*, PyObject* const* a, Py_ssize_t n)
                                           static_cast<float*>(state->data_ptr()), out.data_ptr(), dev.stream());
         }
         if (st != SR_OK) return none();
+        written(*state);
         return wrap(out);
     })
 }
@@ -317,6 +325,8 @@ PyObject* py_run(PyObject*, PyObject* const* a, Py_ssize_t n)
                                              static_cast<float*>(last.data_ptr()), out.data_ptr(), bytes ? work.data_ptr() : nullptr, bytes, dev.stream());
         }
         if (st != SR_OK) return none();
+        if (given) written(*given);
+        if (to) written(*to);
         return two(wrap(out), wrap(last));
     })
 }

@@ -108,6 +108,13 @@ def _tensors(call: str, first, *others) -> int:
     return device
 
 
+def _written(*tensors):
+    """Written in place: whoever has kept one for a gradient learns of it.  (Tensors of inference mode have no versions.)"""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _float_vector(call: str, name: str, t, n: int):
     if t is None:
         return None
@@ -205,6 +212,7 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
     w._check("product")
     device = _tensors("product", a.data, a.scales, w.data, w.scales, bias, out)
     b = _float_vector("product", "bias", bias, w.rows)
+    given = out
     if out is None:
         if dtype not in _DTYPES:
             _refuse("product", "the output is float32 or bfloat16")
@@ -216,6 +224,7 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
         stride = _rows("product", "out", out) if w.rows else 0
     _call("sr_microscale_product", device, _library().sr_microscale_product, a.data.data_ptr(), a.scales.data_ptr(), w.data.data_ptr(), w.scales.data_ptr(),
           FORMATS[a.format], a.rows, a.cols, w.rows, b, 1 if relu else 0, out.data_ptr(), _DTYPES[out.dtype], stride)
+    _written(given)
     return out
 
 
@@ -329,6 +338,7 @@ def linear_attention_run(q, k, v, log_decay, state=None, offsets=None, scale: fl
         _refuse(call, "offsets have to be int64 [sequences + 1] without gaps")
     if q.dim() < 3 or v.dim() < 3:
         _refuse(call, "q, k and v have to be [frames][sequences][heads][size], or [frames][heads][size] with offsets")
+    given = out
     if out is None:
         out = q.new_empty(q.shape[:-1] + v.shape[-1:])
     elif out.shape != q.shape[:-1] + v.shape[-1:] or out.dtype is not q.dtype or not out.is_contiguous():
@@ -341,6 +351,7 @@ def linear_attention_run(q, k, v, log_decay, state=None, offsets=None, scale: fl
     work = q.new_empty(size, dtype=torch.uint8) if size else None
     _call("sr_linear_attention_run", device, _library().sr_linear_attention_run, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
           offsets.data_ptr() if packed else None, sp, lp, out.data_ptr(), work.data_ptr() if size else None, size)
+    _written(given, state_out)
     return out, last
 
 
@@ -358,6 +369,7 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0):
     desc, _, shape, _ = _desc(call, device, q, k, v, log_decay, False, True, q.shape[0], scale)
     _call("sr_linear_attention_step", device, _library().sr_linear_attention_step, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
           _state_pointer(call, state, shape), out.data_ptr())
+    _written(state)
     return out
 
 

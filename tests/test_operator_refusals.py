@@ -75,3 +75,34 @@ def test_what_has_no_derivative_recorded_is_still_taken():
     with torch.inference_mode():
         for call in calls(torch.ones(4, 64, device="cuda:0")):
             call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("compiled", [True, False])
+def test_what_is_written_in_place_gets_a_new_version(compiled, monkeypatch):
+    if not compiled:
+        for name in ("quantize", "product", "rms_norm", "run", "step"):
+            monkeypatch.setattr(sr.operators._compiled, name, lambda *_: None)
+    D = "cuda:0"
+    h, d = torch.ones(3, 1, 2, 64, device=D), torch.zeros(2, device=D)
+    state, out = torch.zeros(1, 2, 64, 64, device=D), torch.zeros(3, 1, 2, 64, device=D)
+    versions = [t._version for t in (state, out, h, d)]
+    sr.linear_attention_step(h[0], h[0], h[0], d, state)
+    sr.linear_attention_run(h, h, h, d, state=state)
+    assert [t._version for t in (state, out, h, d)] == [versions[0] + 1] + versions[1:]
+    sr.linear_attention_run(h, h, h, d, state=state, out=out, state_out=state)
+    assert [t._version for t in (state, out, h, d)] == [versions[0] + 2, versions[1] + 1] + versions[2:]
+    m, y = sr.quantize(torch.ones(4, 64, device=D)), torch.zeros(4, 8, device=D)
+    sr.product(m, m, out=y[:, :4])
+    assert y._version == 1 and m.data._version == 0
+    with torch.inference_mode():
+        frozen = torch.zeros(1, 2, 64, 64, device=D)
+    sr.linear_attention_step(h[0], h[0], h[0], d, frozen)       # as before: written, there is no version
+    assert (frozen != 0).any()
+    w = torch.zeros(1, 2, 64, 64, device=D, requires_grad=True)
+    kept = w * 1
+    loss = (kept * kept).sum()
+    with torch.no_grad():
+        sr.linear_attention_step(h[0], h[0], h[0], d, kept)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
