@@ -55,7 +55,7 @@ def load_library(path: Optional[str] = None):
     p = path or _LIB_PATH
     if not os.path.exists(p):
         from . import build as _build
-        _build.build()
+        _build.build_library()
     lib = ctypes.CDLL(p)
     vp, ip = ctypes.c_void_p, ctypes.c_int
     lib.sr_graph_create.argtypes = [ctypes.POINTER(_NodeDesc), ip, ctypes.POINTER(_EdgeDesc), ip,

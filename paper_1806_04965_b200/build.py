@@ -15,16 +15,32 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a",
               "-Xcompiler", "-fPIC", "-cudart", "static"]
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(EXTENSION):
+EXTENSION_SOURCE = "sr_python.cpp"
+
+
+def _stale(built: str, sources) -> bool:
+    if not os.path.exists(built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(EXTENSION))
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "sr_rollout.h")]
+    t = os.path.getmtime(built)
+    deps = [os.path.join(CSRC, f) for f in sources] + [os.path.join(HERE, "..", "include", "sr_rollout.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
+    """The library, which needs nvcc only, and the operators' extension, which needs PyTorch, a host compiler and Python's headers: where one of these is missing
+    there is a warning, and importing the operators says why it fails."""
+    build_library(force, verbose)
+    if force or _stale(EXTENSION, [EXTENSION_SOURCE]):
+        try:
+            build_extension()
+        except (ImportError, OSError, subprocess.CalledProcessError) as e:
+            import warnings
+            warnings.warn("the operators' extension is not built: %s" % e)
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    if not force and not _stale(LIB, [f for f in os.listdir(CSRC) if f != EXTENSION_SOURCE]):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     objdir = os.path.join(HERE, "_build")
@@ -46,7 +62,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.check_call([nvcc, "-shared", "-cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a",
                            "-o", tmp] + objs)
     os.replace(tmp, LIB)
-    build_extension()
     return LIB
 
 
@@ -61,7 +76,7 @@ def build_extension() -> str:
     tmp = EXTENSION + ".%d.tmp" % os.getpid()
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] + ["-I" + i for i in include] +
-                          [os.path.join(CSRC, "sr_python.cpp"), "-o", tmp, "-L" + HERE, "-l:libsr_rollout.so", "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch",
+                          [os.path.join(CSRC, EXTENSION_SOURCE), "-o", tmp, "-L" + HERE, "-l:libsr_rollout.so", "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch",
                            "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(base, "lib")])
     os.replace(tmp, EXTENSION)
     return EXTENSION

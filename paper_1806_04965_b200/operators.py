@@ -26,10 +26,13 @@ from .binding import SrError
 binding.load_library()
 try:
     from . import _operators as _compiled
-except ImportError:                                    # not built yet
+except ImportError as _first:                          # not built yet, or for another PyTorch or Python
     from . import build as _build
-    _build.build()
-    from . import _operators as _compiled
+    try:
+        _build.build_extension()
+        from . import _operators as _compiled
+    except Exception as _second:
+        raise ImportError("the operators' extension cannot be loaded (%s) and building it failed (%s)" % (_first, _second)) from _second
 
 FORMATS = {"mx8": 2, "mx4": 3}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
