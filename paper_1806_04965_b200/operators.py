@@ -409,12 +409,18 @@ class TemporalHead:
 
     def __init__(self, weights: dict, channels: int, heads: int, groups: int, dk: int, dv: int, batch: int, format: str = "mx4", dtype: str = "bf16",
                  eps: float = 1e-6, device: str = "cuda:0"):
+        if min(channels, heads, groups, dk, dv) < 1 or batch < 0 or heads % groups or heads // groups > 128 or dk > 256:
+            _refuse("TemporalHead", "sizes are positive, heads a multiple of groups (128 times them at most), dk at most 256")
+        if dtype not in ("bf16", "fp32") or format not in FORMATS or not eps >= 0:
+            _refuse("TemporalHead", "dtype is bf16 or fp32, format one of %s, eps not negative" % ", ".join(FORMATS))
         self.channels, self.heads, self.groups, self.dk, self.dv, self.batch, self.eps, self.format = channels, heads, groups, dk, dv, batch, eps, format
         self.tdtype = {"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
         shapes = {"qkv": (heads * dk + groups * (dk + dv), channels), "o": (channels, heads * dv), "out": (None, channels), "bias": (None,),
                   "norm_x": (channels,), "norm_o": (heads * dv,), "norm_h": (channels,), "log_decay": (groups,)}
         w = {}
         for name, shape in shapes.items():
+            if name not in weights:
+                _refuse("TemporalHead", "%s is missing" % name)
             t = torch.as_tensor(weights[name], dtype=torch.float32).detach().to(device).contiguous()
             if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
                 _refuse("TemporalHead", "%s has shape %s" % (name, tuple(t.shape)))
@@ -453,6 +459,13 @@ class TemporalHead:
     def _fits(self, call: str, features, lead: int):
         if features.dim() <= lead or features.shape[lead - 1] != self.batch or math.prod(features.shape[lead:]) != self.channels:
             _refuse("TemporalHead." + call, "the head takes %s[%d sequences][%d channels]" % ("[frames]" if lead == 2 else "", self.batch, self.channels))
+
+    def check_features(self, shape, device):
+        """Refuses features of one frame that the head cannot take: [batch][...channels], on its device."""
+        if len(shape) < 1 or shape[0] != self.batch or math.prod(shape[1:]) != self.channels:
+            _refuse("TemporalHead", "the head takes [%d sequences][%d channels]" % (self.batch, self.channels))
+        if _device_index("TemporalHead", device) != self.state.get_device():
+            _refuse("TemporalHead", "the head lies on %s" % self.state.device)
 
     @torch.no_grad()
     def run(self, features):

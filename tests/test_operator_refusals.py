@@ -106,3 +106,45 @@ def test_what_is_written_in_place_gets_a_new_version(compiled, monkeypatch):
         sr.linear_attention_step(h[0], h[0], h[0], d, kept)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def weights(channels=10, heads=4, groups=2, dk=32, dv=48, outputs=7):
+    shapes = {"qkv": (heads * dk + groups * (dk + dv), channels), "o": (channels, heads * dv), "out": (outputs, channels), "bias": (outputs,), "norm_x": (channels,),
+              "norm_o": (heads * dv,), "norm_h": (channels,), "log_decay": (groups,)}
+    return {n: torch.full(s, -0.1) for n, s in shapes.items()}
+
+
+def test_head_refuses_what_none_of_its_calls_would_take():
+    sizes = dict(channels=10, heads=4, groups=2, dk=32, dv=48, batch=4, device="cpu")
+    for bad in (dict(heads=3), dict(groups=0), dict(heads=0), dict(dk=257), dict(dv=0), dict(batch=-1), dict(dtype="fp16"), dict(format="mx6"), dict(eps=-1.0), dict(eps=float("nan")),
+                dict(heads=258, groups=2)):
+        with pytest.raises(SrError, match="TemporalHead: (sizes|dtype)"):
+            sr.TemporalHead(weights(), **{**sizes, **bad})
+    for name in weights():
+        w = weights()
+        del w[name]
+        with pytest.raises(SrError, match="%s is missing" % name):
+            sr.TemporalHead(w, **sizes)
+        w = weights()
+        w[name] = w[name][None]
+        with pytest.raises(SrError, match="%s has shape" % name):
+            sr.TemporalHead(w, **sizes)
+
+
+@pytest.mark.gpu
+def test_rollout_with_a_head_that_does_not_fit_changes_nothing():
+    from tests.parity import make_graph, to_device
+    from workloads import data, graphs
+    spec = graphs.build("c2", batch=4, frames=5)
+    G = make_graph(spec, "streaming", weights=data.make_weights(spec), biases=data.make_biases(spec))
+    frames = [to_device(spec, data.make_inputs(spec)[v]) for v in G.input_nodes]
+    want = G.rollout(frames)
+    t, state = G.frame(), G.get_state(G.output_node)
+    for kw in (dict(batch=3), dict(channels=11)):
+        c = kw.get("channels", 10)
+        head = sr.TemporalHead(weights(channels=c), c, 4, 2, 32, 48, batch=kw.get("batch", 4))
+        head.state.fill_(2.0)
+        with pytest.raises(SrError, match="the head takes"):
+            G.rollout(frames, head=head)
+        assert (head.state == 2).all() and G.frame() == t and torch.equal(torch.as_tensor(G.get_state(G.output_node)), torch.as_tensor(state))
+    assert torch.equal(G.rollout(frames), want)
