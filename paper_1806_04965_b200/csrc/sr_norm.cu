@@ -393,7 +393,7 @@ cudaError_t launch(const RowArgs& A, bool norm, int dtype, int fmt, cudaStream_t
 {
     const int64_t strips = (A.tiles_g * 128 + 511) / 512, blocks = (A.rows * strips + 7) / 8;
     if (!norm && dtype == SR_DTYPE_BF16 && A.cols % 8 == 0 && !((uintptr_t)A.x & 15) && A.x_stride % 8 == 0) {
-        if (blocks > 0x7FFFFFF) return cudaErrorInvalidValue;
+        if (blocks > 0x1FFFFFFF) return cudaErrorInvalidValue;       // (the warps' numbers have 32 bits; so many strips are more than a terabyte)
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at[0].val.programmaticStreamSerializationAllowed = 1;

@@ -93,6 +93,16 @@ def test_padding_is_zero_in_rows_that_are_not_finite(cols, dtype, fmt):
             assert ((data[:, cols // 2] >> 4 & 7) == 0).all()
 
 
+def test_quantisation_of_more_than_2_30_rows():
+    few = torch.randn(2, 8, generator=gen(99), device=DEV).bfloat16()
+    want = sr.quantize(few[:1], "mx4")
+    rows = 2 ** 30 + 3
+    m = sr.quantize(few[:1].expand(rows, 8), "mx4")
+    assert torch.equal(m.data[-1], want.data[0]) and torch.equal(m.data[::2 ** 20 + 7].unique(dim=0), want.data)
+    last = (rows - 1) // 128 * 512 + (rows - 1) % 32 * 16 + (rows - 1) % 128 // 32 * 4
+    assert torch.equal(m.scales[last:last + 4], want.scales[:4])
+
+
 # ------------------------------------------------------------------------------------------ waits that run out
 WAIT = r"""
 #include "sr_ptx.cuh"
