@@ -322,6 +322,14 @@ sr_status sr_microscale_values(const void* data_dev, const void* scales_dev, int
 sr_status sr_microscale_product(const void* a_data_dev, const void* a_scales_dev, const void* w_data_dev, const void* w_scales_dev, int format,
                                 int64_t rows, int64_t cols, int64_t outs, const float* bias_dev, int act, void* out_dev, int out_dtype,
                                 int64_t out_stride, void* stream);
+/* How a product of these sizes is cut on a device of `sms` SMs (0: the current one): what a test looks at to know the path that it takes.
+ * Errors: INVALID_ARG, CUDA (no device). */
+typedef struct {
+    int32_t rows, outs;       /* of a tile */
+    int32_t parts;            /* CTAs of a cluster that share a tile's reduction (1: none) */
+    int32_t pair;             /* 1: two CTAs share a tile's outputs */
+} sr_product_plan;
+sr_status sr_microscale_product_plan(int format, int64_t rows, int64_t cols, int64_t outs, int sms, sr_product_plan* plan);
 
 /*
  * Root-mean-square norm: s = x + residual (in 32 bits), out = s / sqrt(mean(s^2) + eps) * weight.
@@ -361,6 +369,13 @@ typedef struct {
 /* Bytes of device memory (256-byte aligned) that sr_linear_attention_run needs for these sizes; may be 0.  packed: offsets will be given.
  * Work of two runs that share a workspace must not overlap on the GPU.  Errors: INVALID_ARG, UNSUPPORTED. */
 sr_status sr_linear_attention_workspace_bytes(const sr_attention_desc* desc, int packed, size_t* bytes);
+/* How a run is cut on a device of `sms` SMs (0: the current one), for tensors whose rows start on 16 bytes.  Errors: INVALID_ARG, UNSUPPORTED, CUDA (no device). */
+typedef struct {
+    int32_t chunk;            /* frames of a chunk: 128 on the tensor cores, else 16 */
+    int64_t segment;          /* frames of a segment; 0: sequences are whole */
+    int64_t segments;         /* that there is room for */
+} sr_attention_plan;
+sr_status sr_linear_attention_plan(const sr_attention_desc* desc, int packed, int sms, sr_attention_plan* plan);
 /* All frames of all sequences.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 sr_status sr_linear_attention_run(const sr_attention_desc* desc, const void* q_dev, const void* k_dev, const void* v_dev, const float* log_decay_dev,
                                   const int64_t* offsets_dev, const float* state_in_dev, float* state_out_dev, void* out_dev,

@@ -777,10 +777,10 @@ cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
 // is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 760 / 157, 4096 frames 104 / 42; 4 of 8192, 4 heads of 128 200 / 99; 8 of 1024,
 // 4 heads of 64 28 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 538 / 317; 32 of 1000, 8 heads of 64 87 / 118.  More than one wave of segments lost:
 // 32768 frames 210, 263 with two, three waves instead of 166, packed 355, 364, 396 instead of 353 (measured alike, on an earlier form of the kernel).
-AttentionCut cut_of(const sr_attention_desc* d, bool packed)
+AttentionCut cut_of(const sr_attention_desc* d, bool packed, int64_t sms)
 {
     AttentionCut cut{0, 0};
-    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kCols - 1) / kCols), sms = std::max(1, sr_device_sms());
+    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kCols - 1) / kCols);
     if (d->batch < 1 || d->frames < 1 || (int64_t)d->batch * d->groups > 65535) return cut;
     const double share = (double)(d->heads / d->groups);
     const double total = packed ? (double)d->frames : (double)d->frames * d->batch, mean = total / d->batch;
@@ -814,7 +814,7 @@ bool sr_chunks_wanted(const sr_attention_desc* d)
     return d->dtype == SR_DTYPE_BF16 && d->dk <= 128 && d->frames >= 16 &&
            (int64_t)(d->batch + d->frames) * d->groups * ((d->dv + kCols - 1) / kCols) <= 0x7FFFFFFF;
 }
-AttentionCut sr_chunks_cut(const sr_attention_desc* d, bool packed) { return cut_of(d, packed); }
+AttentionCut sr_chunks_cut(const sr_attention_desc* d, bool packed, int sms) { return cut_of(d, packed, std::max(1, sms)); }
 
 SegmentArgs sr_segment_args(const AttentionArgs& A, AttentionCut cut, int cols, void* workspace)
 {

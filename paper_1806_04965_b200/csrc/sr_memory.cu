@@ -292,10 +292,10 @@ cudaError_t launch_frames_any(const SegmentArgs& C, cudaStream_t s)
 }
 // Segments for this kernel, by the same reasoning as for the other one: two CTAs to an SM, a piece of 128 frames at least, and about 160 frames' time for the two
 // launches more and the states' way.
-AttentionCut frames_cut(const sr_attention_desc* d, bool packed)
+AttentionCut frames_cut(const sr_attention_desc* d, bool packed, int sms)
 {
     AttentionCut cut{0, 0};
-    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kRunCols - 1) / kRunCols), held = 2 * std::max(1, sr_device_sms());
+    const int64_t per_slot = (int64_t)d->groups * ((d->dv + kRunCols - 1) / kRunCols), held = 2 * std::max(1, sms);
     if (d->batch < 1 || d->frames < 1 || (int64_t)d->batch * d->groups > 65535) return cut;
     const double share = (double)(d->heads / d->groups);
     const double total = packed ? (double)d->frames : (double)d->frames * d->batch, mean = total / d->batch;
@@ -479,7 +479,21 @@ sr_status sr_linear_attention_workspace_bytes(const sr_attention_desc* d, int pa
     if (st != SR_OK) return st;
     if (!bytes) return SR_ERR_INVALID_ARG;
     // (whether the tensor-core kernel can take the tensors is known when they are)
-    *bytes = std::max(sr_chunks_wanted(d) ? sr_cut_bytes(d, sr_chunks_cut(d, packed != 0)) : 0, sr_cut_bytes(d, frames_cut(d, packed != 0)));
+    const int sms = sr_device_sms();
+    *bytes = std::max(sr_chunks_wanted(d) ? sr_cut_bytes(d, sr_chunks_cut(d, packed != 0, sms)) : 0, sr_cut_bytes(d, frames_cut(d, packed != 0, sms)));
+    return SR_OK;
+}
+
+sr_status sr_linear_attention_plan(const sr_attention_desc* d, int packed, int sms, sr_attention_plan* plan)
+{
+    const sr_status st = check(d);
+    if (st != SR_OK) return st;
+    if (!plan || sms < 0) return SR_ERR_INVALID_ARG;
+    if (!sms) sms = sr_device_sms();
+    if (sms < 1) return SR_ERR_CUDA;
+    const bool chunks = sr_chunks_wanted(d);
+    const AttentionCut cut = chunks ? sr_chunks_cut(d, packed != 0, sms) : frames_cut(d, packed != 0, sms);
+    *plan = sr_attention_plan{chunks ? 128 : kFrames, cut.segment, cut.slots};
     return SR_OK;
 }
 
@@ -494,7 +508,8 @@ sr_status sr_linear_attention_run(const sr_attention_desc* d, const void* q, con
                       ((uintptr_t)decay & 3) || !apart(out, q, k, v)))
         return SR_ERR_INVALID_ARG;
     const bool chunks = sr_chunks_wanted(d) && sr_chunks_fit(d, offsets != nullptr, q, k, v);
-    const AttentionCut cut = chunks ? sr_chunks_cut(d, offsets != nullptr) : frames_cut(d, offsets != nullptr);
+    const int sms = sr_device_sms();
+    const AttentionCut cut = chunks ? sr_chunks_cut(d, offsets != nullptr, sms) : frames_cut(d, offsets != nullptr, sms);
     const size_t needed = sr_cut_bytes(d, cut);
     if (needed && (!workspace || workspace_bytes < needed || ((uintptr_t)workspace & 255))) return SR_ERR_INVALID_ARG;
     AttentionArgs A = arguments(d, q, k, v, decay, out);

@@ -119,7 +119,7 @@ __device__ __forceinline__ AttentionItem attention_item(const SegmentArgs& C, bo
 // sr_chunks.cu: bf16 on the tensor cores, chunks of 128 frames.
 bool sr_chunks_fit(const sr_attention_desc* d, bool packed, const void* q, const void* k, const void* v);
 bool sr_chunks_wanted(const sr_attention_desc* d);
-AttentionCut sr_chunks_cut(const sr_attention_desc* d, bool packed);
+AttentionCut sr_chunks_cut(const sr_attention_desc* d, bool packed, int sms);
 cudaError_t sr_chunks_launch(const AttentionArgs& A, const sr_attention_desc* d, AttentionCut cut, void* workspace, cudaStream_t s);
 cudaError_t sr_segments_launch(const SegmentArgs& C, cudaStream_t s);       // the states that enter the segments, from their sums
 SegmentArgs sr_segment_args(const AttentionArgs& A, AttentionCut cut, int cols, void* workspace);

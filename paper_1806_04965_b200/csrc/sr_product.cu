@@ -30,6 +30,7 @@ using namespace srx;
 
 constexpr int kThreads = 384, kEpilogueWarps = 8, kOuts = 128, kMaxStages = 8;
 constexpr int kSmem = 200 * 1024;
+constexpr int64_t kMost = 0x7FFFFFFF - 256;           // rows, outputs, columns
 
 struct ProductArgs {
     CUtensorMap w_map, a_map;
@@ -422,11 +423,21 @@ cudaError_t launch_any(ProductArgs& P, const Plan& plan, int sms, cudaStream_t s
 
 extern "C" {
 
+sr_status sr_microscale_product_plan(int format, int64_t rows, int64_t cols, int64_t outs, int sms, sr_product_plan* plan)
+{
+    if (!plan || (format != SR_FORMAT_MX8 && format != SR_FORMAT_MX4) || rows < 1 || outs < 1 || cols < 1 || rows > kMost || outs > kMost || cols > kMost || sms < 0)
+        return SR_ERR_INVALID_ARG;
+    if (!sms) sms = sr_device_sms();
+    if (sms < 1) return SR_ERR_CUDA;
+    const Plan p = plan_product(rows, outs, (int)((sr_scaled(rows, cols, format).row_bytes + 127) / 128), sms);
+    *plan = sr_product_plan{p.nt, p.pair ? 2 * kOuts : kOuts, p.split, p.pair ? 1 : 0};
+    return SR_OK;
+}
+
 sr_status sr_microscale_product(const void* a_data, const void* a_scales, const void* w_data, const void* w_scales, int format, int64_t rows, int64_t cols,
                                 int64_t outs, const float* bias, int act, void* out, int out_dtype, int64_t out_stride, void* stream)
 {
-    const int64_t most = 0x7FFFFFFF - 256;
-    if ((format != SR_FORMAT_MX8 && format != SR_FORMAT_MX4) || rows < 0 || outs < 0 || cols < 1 || rows > most || outs > most || cols > most ||
+    if ((format != SR_FORMAT_MX8 && format != SR_FORMAT_MX4) || rows < 0 || outs < 0 || cols < 1 || rows > kMost || outs > kMost || cols > kMost ||
         (act != 0 && act != 1) || (out_dtype != SR_DTYPE_F32 && out_dtype != SR_DTYPE_BF16) || out_stride < outs)
         return SR_ERR_INVALID_ARG;
     if (!rows || !outs) return SR_OK;
@@ -452,7 +463,7 @@ sr_status sr_microscale_product(const void* a_data, const void* a_scales, const 
     const Plan plan = plan_product(rows, outs, P.stages, sms);
     P.out_tiles = (int32_t)(plan.pair ? (outs + 2 * kOuts - 1) / (2 * kOuts) : (outs + kOuts - 1) / kOuts);
     P.row_tiles = (int32_t)((rows + plan.nt - 1) / plan.nt);
-    if ((int64_t)P.out_tiles * P.row_tiles > most) return SR_ERR_INVALID_ARG;
+    if ((int64_t)P.out_tiles * P.row_tiles > kMost) return SR_ERR_INVALID_ARG;
     P.split = plan.split;
     P.act = act;
     P.out_bf16 = out_dtype == SR_DTYPE_BF16;

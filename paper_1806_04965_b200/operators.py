@@ -47,6 +47,14 @@ class _AttentionDesc(ctypes.Structure):
         [(n, _Strides) for n in ("q", "k", "v", "out", "log_decay")]
 
 
+class _ProductPlan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "outs", "parts", "pair")]
+
+
+class _AttentionPlan(ctypes.Structure):
+    _fields_ = [("chunk", ctypes.c_int32), ("segment", ctypes.c_int64), ("segments", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -61,6 +69,8 @@ def _library():
             "sr_microscale_quantize": [vp, i32, i64, i64, i64, i32, vp, vp, vp],
             "sr_microscale_values": [vp, vp, i32, i64, i64, vp, vp],
             "sr_microscale_product": [vp, vp, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp],
+            "sr_microscale_product_plan": [i32, i64, i64, i64, i32, ctypes.POINTER(_ProductPlan)],
+            "sr_linear_attention_plan": [desc, i32, i32, ctypes.POINTER(_AttentionPlan)],
             "sr_rms_norm": [vp, vp, vp, ctypes.c_float, i32, i64, i64, i64, i64, vp, vp, i32, vp, vp],
             "sr_linear_attention_workspace_bytes": [desc, i32, size],
             "sr_linear_attention_run": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
@@ -231,6 +241,15 @@ def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype
     return out
 
 
+def product_plan(rows: int, cols: int, outs: int, format: str = "mx4", sms: int = 0) -> dict:
+    """How a product of these sizes is cut (sr_microscale_product_plan) on the current device or one of `sms` SMs."""
+    p = _ProductPlan()
+    code = _library().sr_microscale_product_plan(FORMATS.get(format, 0), rows, cols, outs, sms, ctypes.byref(p))
+    if code:
+        raise SrError(code, "sr_microscale_product_plan")
+    return {n: getattr(p, n) for n, _ in _ProductPlan._fields_}
+
+
 def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, format: Optional[str] = None):
     """s = x + residual, s / sqrt(mean(s^2) + eps) * weight for every row of x [rows][cols].  The output has x's type, or is `Microscaled` where
     a format is given; with a residual the result is (output, s rounded to x's type)."""
@@ -315,6 +334,16 @@ def _desc(call: str, device: int, q, k, v, log_decay, packed: bool, step: bool, 
         _descs.clear()
     _descs[key] = hit = (ctypes.byref(d), size.value, (batch, groups, dk, dv), d)
     return hit
+
+
+def attention_plan(dtype, batch: int, frames: int, heads: int, groups: int, dk: int, dv: int, packed: bool = False, sms: int = 0) -> dict:
+    """How a run over tensors of these sizes is cut (sr_linear_attention_plan) on the current device or one of `sms` SMs; packed: `frames` in all."""
+    d = _AttentionDesc(_DTYPES[dtype], batch, heads, groups, dk, dv, frames, 1.0)
+    p = _AttentionPlan()
+    code = _library().sr_linear_attention_plan(ctypes.byref(d), 1 if packed else 0, sms, ctypes.byref(p))
+    if code:
+        raise SrError(code, "sr_linear_attention_plan")
+    return {n: getattr(p, n) for n, _ in _AttentionPlan._fields_}
 
 
 def _state_pointer(call: str, state, shape):

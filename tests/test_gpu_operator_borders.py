@@ -8,6 +8,7 @@ import torch
 import paper_1806_04965_b200 as sr
 from tests import operator_oracle as oracle
 from tests.test_gpu_operators import DEV, TYPES, gen, host, inputs, within
+from tests.test_operator_plans import PRODUCTS, RUNS, plan
 
 pytestmark = pytest.mark.gpu
 
@@ -35,6 +36,99 @@ def test_bf16_runs_are_as_exact_as_their_outputs(T, B, heads, groups, dk, dv, ga
     state = torch.randn(B, groups, dk, dv, generator=gen(91), device=DEV)
     out, last = sr.linear_attention_run(q, k, v, d, state=state, scale=0.3)
     compare(q, k, v, d, state, out, last, 0.3, "bf16", [(slice(None), b) for b in range(B)])
+
+
+# ------------------------------------------------------------------------------------------ segments
+def offsets_of(lengths):
+    first = [sum(lengths[:i]) for i in range(len(lengths) + 1)]
+    return torch.tensor(first, dtype=torch.int64, device=DEV), [slice(a, b) for a, b in zip(first, first[1:])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lengths, heads, groups, dk, dv, segment", RUNS)
+def test_packed_sequences_that_are_cut(lengths, heads, groups, dk, dv, segment, dtype):
+    spare, total = 40, sum(lengths)
+    p = sr.operators.attention_plan(TYPES[dtype], len(lengths), total + spare, heads, groups, dk, dv, packed=True)
+    assert p["segment"] > 0 and p["chunk"] == (128 if dtype == "bf16" else 16)
+    q, k, v, d = inputs((total + spare,), heads, groups, dk, dv, dtype, True, seed=100)
+    d = d / 50                                                  # (memories of hundreds of frames: what goes from segment to segment matters)
+    for t in (q, k, v):
+        t[total:] = float("nan")
+    offsets, at = offsets_of(lengths)
+    state = torch.randn(len(lengths), groups, dk, dv, generator=gen(101), device=DEV)
+    out = torch.full((total + spare, heads, dv), 5.0, dtype=TYPES[dtype], device=DEV)
+    _, last = sr.linear_attention_run(q, k, v, d, state=state, offsets=offsets, scale=0.5, out=out)
+    compare(q, k, v, d, state, out, last, 0.5, dtype, at)
+    assert (out[total:] == 5).all()
+    for b, n in enumerate(lengths):
+        if n == 0:
+            assert torch.equal(last[b], state[b])
+    kept = state.clone()
+    sr.linear_attention_run(q, k, v, d, state=kept, offsets=offsets, scale=0.5, out=out, state_out=kept)
+    assert torch.equal(kept, last)
+    sr.operator_status()
+
+
+@pytest.mark.parametrize("T, B, heads, groups, dk, dv", [(5000, 1, 4, 1, 64, 64), (3001, 2, 4, 2, 128, 128), (4097, 1, 6, 3, 40, 72)])
+def test_cut_runs_with_heads_that_share_a_state(T, B, heads, groups, dk, dv):
+    assert sr.operators.attention_plan(torch.bfloat16, B, T, heads, groups, dk, dv)["segment"] > 0
+    q, k, v, d = inputs((T, B), heads, groups, dk, dv, "bf16", True, seed=102)
+    d = d / 50
+    state = torch.randn(B, groups, dk, dv, generator=gen(103), device=DEV)
+    out, last = sr.linear_attention_run(q, k, v, d, state=state, scale=0.3)
+    compare(q, k, v, d, state, out, last, 0.3, "bf16", [(slice(None), b) for b in range(B)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_states_that_start_anew_at_borders_of_segments(dtype):
+    lengths, heads, groups, dk, dv, segment = RUNS[0]
+    offsets, at = offsets_of(lengths)
+    q, k, v, d = inputs((sum(lengths),), heads, groups, dk, dv, dtype, True, seed=104)
+    d = d / 50
+    for f in (segment - 1, segment, 2 * segment + 1, 3 * segment + 127, 4 * segment + 128, 5000, 5001, 5000 + segment):
+        d[f] = float("-inf")
+    d[6 * segment:7 * segment] = -200.0
+    state = torch.randn(len(lengths), groups, dk, dv, generator=gen(105), device=DEV)
+    out, last = sr.linear_attention_run(q, k, v, d, state=state, offsets=offsets)
+    compare(q, k, v, d, state, out, last, 1.0, dtype, at)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("frame", [511, 512, 700, 5002, 5000 + 512])
+def test_values_that_are_not_finite_stay_behind_their_frame_across_segments(frame, dtype):
+    lengths, heads, groups, dk, dv, segment = RUNS[0]
+    offsets, at = offsets_of(lengths)
+    q, k, v, d = inputs((sum(lengths),), heads, groups, dk, dv, dtype, True, seed=106)
+    d = d / 50
+    clean, end = sr.linear_attention_run(q, k, v, d, offsets=offsets)
+    v[frame, 0, 5] = float("nan")
+    out, last = sr.linear_attention_run(q, k, v, d, offsets=offsets)
+    b = next(i for i, s in enumerate(at) if s.start <= frame < s.stop)
+    other = [c for c in range(dv) if c != 5]
+    assert torch.isnan(out[frame:at[b].stop, :, 5]).all() and torch.isnan(last[b, 0, :, 5]).all()
+    assert torch.equal(out[:frame], clean[:frame]) and torch.equal(out[at[b].stop:], clean[at[b].stop:])
+    assert torch.equal(out[:, :, other], clean[:, :, other]) and torch.equal(last[:, :, :, other], end[:, :, :, other])
+    assert torch.equal(torch.cat((last[:b], last[b + 1:])), torch.cat((end[:b], end[b + 1:])))
+
+
+# ------------------------------------------------------------------------------------------ products
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows, cols, outs, fmt, want", PRODUCTS)
+def test_every_way_to_cut_a_product(rows, cols, outs, fmt, want, dtype):
+    assert plan(rows, cols, outs, fmt, 0) == want               # on this device
+    a = torch.randn(rows, cols, generator=gen(110), device=DEV) * torch.exp(torch.randn(rows, 1, generator=gen(111), device=DEV))
+    w = torch.randn(outs, cols, generator=gen(112), device=DEV)
+    bias = torch.randn(outs, generator=gen(113), device=DEV)
+    qa, qw = sr.quantize(a, fmt), sr.quantize(w, fmt)
+    va, vw = qa.values().double(), qw.values().double()
+    exact, mag = va @ vw.t() + bias, va.abs() @ vw.abs().t() + bias.abs()
+    bound = host(oracle.HALF_STEP[dtype] * exact.abs() + (cols + 1) * 2.0 ** -23 * mag)
+    within(sr.product(qa, qw, bias=bias, dtype=TYPES[dtype]), host(exact), bound)
+    out = torch.full((rows, outs + 3), 7.0, dtype=TYPES[dtype], device=DEV)
+    sr.product(qa, qw, bias=bias, relu=True, out=out[:, :outs])  # rows with gaps
+    assert (out[:, outs:] == 7).all()
+    within(out[:, :outs], host(exact.clamp_min(0)), bound)
+    sr.operator_status()
 
 
 # ------------------------------------------------------------------------------------------ norm
@@ -180,3 +274,70 @@ def test_status_of_a_stream_that_is_captured_is_refused_and_the_capture_lives():
     g.replay()
     assert torch.equal(out, want)
     sr.operator_status()
+
+
+# ------------------------------------------------------------------------------------------ the head
+def head_of(fmt, dtype, change=None, **kw):
+    C, H, K, dk, dv, O = 70, 4, 2, 32, 48, 7
+    r = np.random.RandomState(3)
+    w = {"qkv": r.randn(H * dk + K * (dk + dv), C) / C ** 0.5, "o": r.randn(C, H * dv) / (H * dv) ** 0.5, "out": r.randn(O, C), "bias": r.randn(O),
+         "norm_x": 1 + 0.3 * r.randn(C), "norm_o": 1 + 0.3 * r.randn(H * dv), "norm_h": 1 + 0.3 * r.randn(C), "log_decay": -np.array([0.05, 0.3])}
+    if change:
+        w[change] = w[change] * (1 + 0.5 * (np.arange(w[change].size).reshape(w[change].shape) % 2 == 0))
+    return sr.TemporalHead(w, C, H, K, dk, dv, batch=3, format=fmt, dtype=dtype, **kw), w, (C, H, K, dk, dv, O)
+
+
+@pytest.mark.parametrize("T", [1, 40, 150])
+@pytest.mark.parametrize("fmt, dtype", [("mx4", "bf16"), ("mx8", "fp32"), ("mx4", "fp32"), ("mx8", "bf16")])
+def test_head_is_the_public_calls_in_a_row(fmt, dtype, T):
+    head, w, (C, H, K, dk, dv, O) = head_of(fmt, dtype, eps=1e-5)
+    B, dt = 3, TYPES[dtype]
+    w = {n: torch.tensor(x, dtype=torch.float32, device=DEV) for n, x in w.items()}
+    wq = {n: sr.quantize(w[n], fmt) for n in ("qkv", "o", "out")}
+    features = torch.randn(T, B, C, generator=gen(120), device=DEV)
+    state = torch.zeros(B, K, dk, dv, device=DEV)
+
+    def before(x):
+        qkv = sr.product(sr.rms_norm(x, w["norm_x"], eps=1e-5, format=fmt), wq["qkv"], dtype=dt)
+        return [t.reshape(len(x), -1, n) for t, n in zip(qkv.split((H * dk, K * dk, K * dv), dim=1), (dk, dk, dv))]
+
+    def behind(x, o):
+        y = sr.product(sr.rms_norm(o.reshape(len(x), H * dv), w["norm_o"], eps=1e-5, format=fmt), wq["o"], dtype=dt)
+        return sr.product(sr.rms_norm(y, w["norm_h"], residual=x, eps=1e-5, format=fmt)[0], wq["out"], bias=w["bias"], dtype=torch.float32)
+    x = features.view(T * B, C).to(dt)
+    q, k, v = [t.view(T, B, *t.shape[1:]) for t in before(x)]
+    o, last = sr.linear_attention_run(q, k, v, w["log_decay"], scale=dk ** -0.5)
+    compare(q, k, v, w["log_decay"], None, o, last, dk ** -0.5, dtype, [(slice(None), b) for b in range(B)])
+    assert torch.equal(head.run(features), behind(x, o).view(T, B, O)) and torch.equal(head.state, last)
+    head.reset()
+    for t in range(min(T, 20)):
+        x = features[t].to(dt)
+        o = sr.linear_attention_step(*before(x), w["log_decay"], state, scale=dk ** -0.5)
+        assert torch.equal(head.step(features[t]), behind(x, o)) and torch.equal(head.state, state)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T, cuts", [(300, (128, 129)), (300, (1, 299)), (2000, (700, 1999))])
+def test_clips_in_parts_and_frames_carry_the_whole_state_on(T, cuts, dtype):
+    B, H, K, dk, dv = 2, 4, 2, 64, 48
+    q, k, v, d = inputs((T, B), H, K, dk, dv, dtype, True, seed=121)
+    d = d / 20
+    state, outs, t0 = torch.zeros(B, K, dk, dv, device=DEV), [], 0
+    for t1 in cuts + (T,):
+        out, _ = sr.linear_attention_run(q[t0:t1], k[t0:t1], v[t0:t1], d[t0:t1], state=state, state_out=state, scale=0.2)
+        outs.append(out)
+        t0 = t1
+    at = [(slice(None), b) for b in range(B)]
+    compare(q, k, v, d, None, torch.cat(outs), state, 0.2, dtype, at)
+    state.zero_()
+    out, _ = sr.linear_attention_run(q[:T // 2], k[:T // 2], v[:T // 2], d[:T // 2], state=state, state_out=state, scale=0.2)
+    outs = [out] + [sr.linear_attention_step(q[t], k[t], v[t], d[t], state, scale=0.2)[None] for t in range(T // 2, T)]
+    compare(q, k, v, d, None, torch.cat(outs), state, 0.2, dtype, at)
+
+
+@pytest.mark.parametrize("name", ["qkv", "o", "out", "bias", "norm_x", "norm_o", "norm_h", "log_decay"])
+def test_every_weight_of_the_head_matters(name):
+    features = torch.randn(30, 3, 70, generator=gen(122), device=DEV)
+    a, b = head_of("mx8", "fp32")[0].run(features), head_of("mx8", "fp32", change=name)[0].run(features)
+    # every second of its values is half as much again: outputs change by far more than what an element's rounding (2^-4) would move in one of 70 terms
+    assert torch.linalg.vector_norm(a - b) > 0.02 * torch.linalg.vector_norm(a)
