@@ -386,7 +386,8 @@ __global__ void __launch_bounds__(kThreads, 1) sr_chunks_kernel(const __grid_con
                 if (lane >= m) before += up;
             }
             const double total = __shfl_sync(0xFFFFFFFFu, before, 31);
-            before -= g[3];
+            before = __shfl_up_sync(0xFFFFFFFFu, before, 1);             // (not by subtraction: a NaN would reach the lane's frames ahead of it)
+            if (lane == 0) before = 0.0;
             const double behind = OUT ? 0.0 : log_whole * l2e;           // (sums alone, from the last chunk to the first: the decays of the chunks behind this one)
             log_whole += total;
             const double last = total * l2e;

@@ -111,6 +111,17 @@ def test_values_that_are_not_finite_stay_behind_their_frame_across_segments(fram
     assert torch.equal(torch.cat((last[:b], last[b + 1:])), torch.cat((end[:b], end[b + 1:])))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T, frame", [(140, 2), (140, 63), (140, 131), (3000, 1027)])
+def test_a_decay_that_is_nan_reaches_no_earlier_frame(T, frame, dtype):
+    q, k, v, d = inputs((T, 2), 2, 1, 64, 64, dtype, True, seed=107)
+    clean, end = sr.linear_attention_run(q, k, v, d)
+    d[frame, 0] = float("nan")
+    out, last = sr.linear_attention_run(q, k, v, d)
+    assert torch.equal(out[:frame], clean[:frame]) and torch.equal(out[:, 1], clean[:, 1]) and torch.equal(last[1], end[1])
+    assert torch.isnan(out[frame:, 0]).all() and torch.isnan(last[0]).all()
+
+
 # ------------------------------------------------------------------------------------------ products
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows, cols, outs, fmt, want", PRODUCTS)
