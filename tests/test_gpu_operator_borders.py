@@ -122,6 +122,35 @@ def test_a_decay_that_is_nan_reaches_no_earlier_frame(T, frame, dtype):
     assert torch.isnan(out[frame:, 0]).all() and torch.isnan(last[0]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T, frame", [(140, 5), (140, 130), (3000, 1500)])
+def test_queries_keys_and_states_that_are_not_finite_stay_where_they_are(T, frame, bad, dtype):
+    H, G, D = 4, 2, 64                                          # heads 0 and 1 share group 0
+    q, k, v, d = inputs((T, 2), H, G, D, D, dtype, True, seed=108)
+    state = torch.randn(2, G, D, D, generator=gen(109), device=DEV)
+    clean, end = sr.linear_attention_run(q, k, v, d, state=state)
+    q2 = q.clone()
+    q2[frame, 0, 1, 7] = bad
+    out, last = sr.linear_attention_run(q2, k, v, d, state=state)
+    touched = torch.zeros(T, 2, H, dtype=torch.bool, device=DEV)
+    touched[frame, 0, 1] = True
+    assert torch.equal(out[~touched], clean[~touched]) and torch.equal(last, end) and not torch.isfinite(out[frame, 0, 1]).any()
+    k2 = k.clone()
+    k2[frame, 0, 0, 7] = bad
+    out, last = sr.linear_attention_run(q, k2, v, d, state=state)
+    touched[frame:, 0, :2] = True
+    assert torch.equal(out[~touched], clean[~touched]) and not torch.isfinite(out[frame, 0, :2]).any()
+    rows = [i for i in range(D) if i != 7]
+    assert torch.equal(last[1], end[1]) and torch.equal(last[0, 1], end[0, 1]) and torch.equal(last[0, 0, rows], end[0, 0, rows])
+    state2 = state.clone()
+    state2[0, 1, 3, 9] = bad
+    out, last = sr.linear_attention_run(q, k, v, d, state=state2)
+    columns = [j for j in range(D) if j != 9]
+    assert torch.equal(out[:, 1], clean[:, 1]) and torch.equal(out[:, 0, :2], clean[:, 0, :2]) and torch.equal(out[:, 0, 2:][..., columns], clean[:, 0, 2:][..., columns])
+    assert torch.equal(last[0, 1][:, columns], end[0, 1][:, columns]) and not torch.isfinite(out[0, 0, 2:, 9]).any()
+
+
 # ------------------------------------------------------------------------------------------ products
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows, cols, outs, fmt, want", PRODUCTS)
