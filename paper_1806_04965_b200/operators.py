@@ -108,6 +108,8 @@ def _call(call: str, device: int, function, *args):
 
 def _tensors(call: str, first, *others) -> int:
     """All on one CUDA device (its index is returned), none that a gradient is recorded for, in either direction."""
+    if not isinstance(first, torch.Tensor) or any(t is not None and not isinstance(t, torch.Tensor) for t in others):
+        _refuse(call, "tensors are required")
     if _grad() and (first.requires_grad or any(t is not None and t.requires_grad for t in others)):
         _refuse(call, "there is no backward pass (use torch.no_grad() or detach)")
     if any(t is not None and (_wrapped(t) or _forward_ad.unpack_dual(t).tangent is not None) for t in (first,) + others):
@@ -160,6 +162,8 @@ class Microscaled:
     def _check(self, call: str):
         """Whether data and scales have the sizes that rows, cols and format make (all of them can be assigned)."""
         data, scales, rows, cols, format = self.data, self.scales, self.rows, self.cols, self.format
+        if not isinstance(data, torch.Tensor) or not isinstance(scales, torch.Tensor):
+            _refuse(call, "tensors are required")
         if format not in FORMATS:
             _refuse(call, "format is one of %s" % ", ".join(FORMATS))
         if rows < 0 or cols < 1:
@@ -215,6 +219,8 @@ def quantize(x, format: str = "mx4") -> Microscaled:
 def product(a: Microscaled, w: Microscaled, bias=None, relu: bool = False, dtype=torch.bfloat16, out=None):
     """act(bias + a w^T), [a.rows][w.rows]: a dense node's update on microscaled operands of the same format.  `out` (rows may have
     gaps between them) is written in place of a new tensor of `dtype`."""
+    if not isinstance(a, Microscaled) or not isinstance(w, Microscaled):
+        _refuse("product", "microscaled matrices are required")
     if a.format != w.format or a.cols != w.cols:
         _refuse("product", "both matrices have the same format and number of columns")
     fast = _compiled.product(a.data, a.scales, a.rows, w.data, w.scales, w.rows, a.cols, FORMATS.get(a.format, 0), bias, relu, _DTYPES.get(dtype, -1), out) \

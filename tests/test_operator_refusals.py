@@ -148,3 +148,17 @@ def test_rollout_with_a_head_that_does_not_fit_changes_nothing():
             G.rollout(frames, head=head)
         assert (head.state == 2).all() and G.frame() == t and torch.equal(torch.as_tensor(G.get_state(G.output_node)), torch.as_tensor(state))
     assert torch.equal(G.rollout(frames), want)
+
+
+def test_what_is_no_tensor_is_refused():
+    import numpy as np
+    m, t, d = sr.Microscaled.empty(4, 64, "mx4", "cpu"), torch.zeros(1, 2, 8), torch.zeros(2)
+    for no in ([1.0], np.zeros((4, 64), np.float32), 3, "x", None):
+        for call in (lambda: sr.quantize(no), lambda: sr.rms_norm(no), lambda: sr.product(no, m), lambda: sr.product(m, no), lambda: sr.linear_attention_step(no, t, t, d, t),
+                     lambda: sr.linear_attention_run(no, t, t, d), lambda: sr.Microscaled(no, m.scales, 4, 64, "mx4")):
+            with pytest.raises(SrError, match="required"):
+                call()
+        if no is not None:
+            for call in (lambda: sr.rms_norm(t[0], no), lambda: sr.product(m, m, bias=no), lambda: sr.product(m, m, out=no), lambda: sr.linear_attention_run(t, t, t, d, state=no)):
+                with pytest.raises(SrError, match="required"):
+                    call()
