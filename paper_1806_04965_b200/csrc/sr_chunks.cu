@@ -775,7 +775,7 @@ cudaError_t launch_all(ChunkArgs& C, cudaStream_t s)
 // Frames of a segment, 0: whole sequences.  Segments are read twice (k and v for their sums, then everything for the outputs) and cost two launches and the
 // way of their states out and back, about as much as five chunks; they are for launches that would leave SMs without work, or wait for
 // one long sequence.  A step (a chunk for one head) is the unit; a chunk's sums alone are 0.6 of one.  Of packed sequences only the mean is known: the longest
-// is taken for three times that.  Us whole / cut: one sequence, 8 heads of 128, 32768 frames 760 / 157, 4096 frames 104 / 42; 4 of 8192, 4 heads of 128 200 / 99; 8 of 1024,
+// is taken for three times that.  Us whole / cut, calls back to back on three sets of inputs: one sequence, 8 heads of 128, 32768 frames 760 / 157, 4096 frames 104 / 42; 4 of 8192, 4 heads of 128 200 / 99; 8 of 1024,
 // 4 heads of 64 28 / 33; packed, 16 of 3000 on average, 16 heads on 4 of 128 538 / 317; 32 of 1000, 8 heads of 64 87 / 118.  More than one wave of segments lost:
 // 32768 frames 210, 263 with two, three waves instead of 166, packed 355, 364, 396 instead of 353 (measured alike, on an earlier form of the kernel).
 AttentionCut cut_of(const sr_attention_desc* d, bool packed, int64_t sms)

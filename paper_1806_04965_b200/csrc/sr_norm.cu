@@ -5,8 +5,8 @@
 //
 // A row lies in the registers of the threads that share it (32 to 1024 of them, a few units of VEC elements each) between the
 // sum of squares and the output, so that nothing is read twice; longer rows are read again (they come out of L2).  The
-// lanes of a group of 32 columns find its largest magnitude with shuffles.  16384 x 1024 fp32 with residual and sum 40.6 us (6.6 TB/s), bf16 22.0 (6.1);
-// rows of 1003, which no 16-byte access fits by itself, 52.6.
+// lanes of a group of 32 columns find its largest magnitude with shuffles.  16384 x 1024 fp32 with residual and sum 41.2 us (6.5 TB/s), bf16 22.7 (5.9);
+// rows of 1003, which no 16-byte access fits by itself, 53.2.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(1024, NORM && (HOLD == 0 || (VEC == 1 && HOLD 
 }
 
 // Quantisation of bf16 rows whose 16-byte units can be read as they lie: what the kernel above does, without a row's reduction, and with the largest magnitude
-// taken from pairs of bf16.  A thread has two units, 256 columns apart.  Bound by instructions rather than memory: 8192 x 4096 to 4 bits 19.1 us (4.5 TB/s); 26 with the
+// taken from pairs of bf16.  A thread has two units, 256 columns apart.  Bound by instructions rather than memory: 8192 x 4096 to 4 bits 19.9 us (4.3 TB/s); 26 with the
 // kernel above, which issues 162 instructions per 8 values.
 template <int FMT>
 __global__ void __launch_bounds__(256) sr_quantize_kernel(const __grid_constant__ RowArgs A, uint32_t strips)

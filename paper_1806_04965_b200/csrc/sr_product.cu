@@ -7,7 +7,7 @@
 // TMA copies (zero fill behind the last column and row), and their scales: the formats' scale tiles of 128 rows x 4 groups are what tcgen05.cp takes,
 // 512 bytes onto four TMEM columns (byte g of lane r % 32, column r / 32), so a stage's scales are one or two bulk copies per operand and one or two
 // tcgen05.cp.  An MMA takes 32 bytes of a row: one group of 8-bit elements, two of 4-bit ones.
-// Warps: 0 copies, 1 MMAs, 2 TMEM, 4..7 epilogue (bias, ReLU, rounding), which works on one accumulator while the MMAs fill the other.
+// Warps: 0 copies, 1 MMAs, 2 TMEM, 4..11 epilogue (bias, ReLU, rounding), which works on one accumulator while the MMAs fill the other.
 // Many tiles: two CTAs as a pair (cta_group::2) share a tile of 256 outputs.  Each brings its 128 outputs' weights and half of the rows and has its outputs' sums; the first
 // one issues the MMAs, which read both CTAs' memory.  8192 x 4096 x 8192 in 4 bits 117 -> 106 us (5.2 PFLOP/s), in 8 bits 229 -> 205 (2.7).  MMAs want to follow
 // one another: with the next stage's scales or only the wait for it between them 117 and 223, with two stages at a time 112 and 217.
