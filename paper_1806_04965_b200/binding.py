@@ -304,8 +304,9 @@ class Graph:
         """frames: one tensor [T+1][B][H][W][C] per input node (frames 0..T).  Resets to frame 0,
         runs T updates, returns the outputs [T][B][C_out] (float32).  With a `TemporalHead` the outputs are its features: it is
         reset, too, and what it gives for the T frames is returned."""
-        if head is not None:
-            head.check_features(self.out_shape(), self.device)       # ahead of anything that is changed
+        check = getattr(head, "check_features", None)               # (anything with reset and run may stand behind a rollout)
+        if check is not None:
+            check(self.out_shape(), self.device)                    # ahead of anything that is changed
         T = int(frames[0].shape[0]) - 1
         out = self._torch.empty((T,) + self.out_shape(), dtype=self._torch.float32, device=self.device)
         self.reset([f[0] for f in frames])

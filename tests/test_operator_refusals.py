@@ -162,3 +162,21 @@ def test_what_is_no_tensor_is_refused():
             for call in (lambda: sr.rms_norm(t[0], no), lambda: sr.product(m, m, bias=no), lambda: sr.product(m, m, out=no), lambda: sr.linear_attention_run(t, t, t, d, state=no)):
                 with pytest.raises(SrError, match="required"):
                     call()
+
+
+@pytest.mark.gpu
+def test_anything_with_reset_and_run_may_stand_behind_a_rollout():
+    from tests.parity import make_graph, to_device
+    from workloads import data, graphs
+    spec = graphs.build("c2", batch=4, frames=3)
+    G = make_graph(spec, "streaming", weights=data.make_weights(spec), biases=data.make_biases(spec))
+    frames = [to_device(spec, data.make_inputs(spec)[v]) for v in G.input_nodes]
+
+    class Sum:
+        def reset(self):
+            self.total = 0.0
+
+        def run(self, features):
+            self.total = self.total + features.sum(0)
+            return self.total
+    assert torch.equal(G.rollout(frames, head=Sum()), G.rollout(frames).sum(0))
