@@ -384,6 +384,85 @@ sr_status sr_linear_attention_run(const sr_attention_desc* desc, const void* q_d
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 sr_status sr_linear_attention_step(const sr_attention_desc* desc, const void* q_dev, const void* k_dev, const void* v_dev, const float* log_decay_dev,
                                    float* state_dev, void* out_dev, void* stream);
+
+/*
+ * Selective head: blocks of a projection, a short convolution over the frames, a selective scan and the way back onto the stream.
+ * Conventions are those of the temporal head's operators; sequences side by side or packed (offsets) as in sr_linear_attention_run.
+ *
+ * Causal convolution of every channel over the frames:
+ *     out[t, c] = act(bias[c] + sum_{j < width} weight[c, j] * x[t - (width - 1) + j, c]),   act: 0 identity, 1 x * sigmoid(x).
+ * Ahead of a sequence's first frame lie the width - 1 frames of its state [batch][width - 1][channels] (type `dtype`, without gaps, oldest first); afterwards the state is
+ * the last width - 1 frames, exactly.  weight: float [channels][width], bias: float [channels] or NULL.  1 <= width <= 8.
+ * Element (frame, sequence, channel) of x and out lies at frame * .frame + sequence * .sequence + channel.
+ */
+typedef struct { int64_t frame, sequence; } sr_frame_strides;
+typedef struct {
+    int32_t dtype;                                  /* of x, out and states: SR_DTYPE_F32 or SR_DTYPE_BF16 */
+    int32_t batch, channels, width, act;
+    int64_t frames;
+    sr_frame_strides x, out;
+} sr_conv_desc;
+/* All frames of all sequences.  state_in NULL: zeros; state_out NULL: not wanted, may be state_in.  A sequence without frames hands its state through.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sr_status sr_causal_conv_run(const sr_conv_desc* desc, const void* x_dev, const float* weight_dev, const float* bias_dev, const int64_t* offsets_dev,
+                             const void* state_in_dev, void* state_out_dev, void* out_dev, void* stream);
+/* One frame of every sequence: desc->frames and the frame strides are not used; the states are updated in place (width 1 has none).
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sr_status sr_causal_conv_step(const sr_conv_desc* desc, const void* x_dev, const float* weight_dev, const float* bias_dev, void* state_dev, void* out_dev, void* stream);
+
+/*
+ * Selective scan: a state of `states` values for every channel whose decay and input go by the frame,
+ *     r = dt[t, i] + dt_bias[i]  (softplus of it where desc->softplus),
+ *     h[i, n] <- exp(r * a[i, n]) * h[i, n] + r * u[t, i] * b[t, g, n],
+ *     out[t, i] = (sum_n c[t, g, n] * h[i, n] + d[i] * u[t, i]) * z[t, i] * sigmoid(z[t, i]),     g = i / (channels / groups),
+ * held and summed in 32 bits.  a: float [channels][states]; dt_bias, d: float [channels] or NULL (zeros); z NULL: no gate.  u, dt, z, out of `dtype`, channels side by
+ * side; b, c of `dtype`, element (frame, sequence, group, n) at frame * .frame + sequence * .sequence + group * .head + n.  States [batch][channels][states] (float, without
+ * gaps): state_in NULL: zeros; state_out NULL: not wanted, may be state_in.  A sequence without frames hands its state through.  1 <= states <= 128.
+ * What is not finite stays in its sequence and, for u, dt and z, in its channel; where the formula has an infinity the result may be NaN.
+ */
+typedef struct {
+    int32_t dtype;
+    int32_t batch, channels, states, groups, softplus;
+    int64_t frames;
+    sr_frame_strides u, dt, z, out;
+    sr_attention_strides b, c;
+} sr_scan_desc;
+/* Bytes of device memory (256-byte aligned) that sr_selective_scan_run needs for these sizes; may be 0.  packed: offsets will be given.
+ * Work of two runs that share a workspace must not overlap on the GPU.  Errors: INVALID_ARG, UNSUPPORTED. */
+sr_status sr_selective_scan_workspace_bytes(const sr_scan_desc* desc, int packed, size_t* bytes);
+/* How a run is cut on a device of `sms` SMs (0: the current one).  Errors: INVALID_ARG, UNSUPPORTED, CUDA (no device). */
+typedef struct {
+    int32_t held, lanes;      /* states of a channel that one thread holds; threads that share a channel */
+    int64_t segment;          /* frames of a segment; 0: sequences are whole */
+    int64_t segments;         /* that there is room for */
+} sr_scan_plan;
+sr_status sr_selective_scan_plan(const sr_scan_desc* desc, int packed, int sms, sr_scan_plan* plan);
+/* All frames of all sequences.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sr_status sr_selective_scan_run(const sr_scan_desc* desc, const void* u_dev, const void* dt_dev, const float* a_dev, const void* b_dev, const void* c_dev,
+                                const float* d_dev, const void* z_dev, const float* dt_bias_dev, const int64_t* offsets_dev, const float* state_in_dev,
+                                float* state_out_dev, void* out_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+/* One frame of every sequence: desc->frames and the frame strides are not used; the states are updated in place.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sr_status sr_selective_scan_step(const sr_scan_desc* desc, const void* u_dev, const void* dt_dev, const float* a_dev, const void* b_dev, const void* c_dev,
+                                 const float* d_dev, const void* z_dev, const float* dt_bias_dev, float* state_dev, void* out_dev, void* stream);
+
+/*
+ * The way out of a block and into the next one, rows [rows][cols]:
+ *     p = y / sqrt(mean(y^2) + eps) * weight_after      (norms & SR_NORM_AFTER; otherwise p = y)
+ *     h = residual + scale * act(gate) * p              (gate NULL: ones; gate_act: 0 identity, 1 sigmoid(x), 2 x * sigmoid(x))
+ *     out = h / sqrt(mean(h^2) + eps) * weight_before   (norms & SR_NORM_BEFORE; otherwise there is no out)
+ * in 32 bits; out is taken from h before its rounding.  Rows whose squares leave the range of 32 bits are as exact as others, as in sr_rms_norm.
+ * y, residual, gate of `dtype`, rows *_stride elements apart (0: one row for all); weights: float [cols] or NULL (ones).  h: `dtype`, [rows][cols] without gaps.
+ * out: SR_FORMAT_F32 / BF16 must equal `dtype`, without gaps; SR_FORMAT_MX8 / MX4: microscaled data, with `scales` (otherwise NULL).  Errors: INVALID_ARG, CUDA.
+ */
+enum { SR_NORM_AFTER = 1, SR_NORM_BEFORE = 2 };
+typedef struct {
+    int32_t dtype, norms, gate_act, out_format;
+    float scale, eps;
+    int64_t rows, cols, y_stride, residual_stride, gate_stride;
+} sr_block_desc;
+sr_status sr_block_norm(const sr_block_desc* desc, const void* y_dev, const void* residual_dev, const void* gate_dev, const float* weight_after_dev,
+                        const float* weight_before_dev, void* h_dev, void* out_dev, void* scales_dev, void* stream);
+
 /* Synchronises `stream` and reports SR_ERR_CUDA if queued work failed, SR_ERR_TIMEOUT if a bounded wait inside one of the operators' kernels
  * has expired on the current device, on whichever stream (outputs since then may not be valid); every later call, of any thread, reports it again until
  * sr_operator_reset.  SR_ERR_STATE: the stream is being captured. */

@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsr_rollout.so")
 EXTENSION = os.path.join(HERE, "_operators.so")         # the operators' calls from Python (csrc/sr_python.cpp)
 SOURCES = ["sr_compile.cpp", "sr_api.cu", "sr_input.cu", "sr_direct.cu", "sr_tc.cu", "sr_resident.cu", "sr_dense.cu",
-           "sr_norm.cu", "sr_product.cu", "sr_memory.cu", "sr_chunks.cu"]
+           "sr_norm.cu", "sr_product.cu", "sr_memory.cu", "sr_chunks.cu", "sr_conv.cu", "sr_scan.cu", "sr_block.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-cudart", "static"]
 

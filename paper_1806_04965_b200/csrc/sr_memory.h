@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "../../include/sr_rollout.h"
+#include "sr_spans.cuh"
 
 struct AttentionArgs {
     const void *q, *k, *v;
@@ -19,10 +20,7 @@ struct AttentionArgs {
     sr_attention_strides sq, sk, sv, so, sd;
 };
 
-// First frame and number of frames of a sequence; b: what its strides `sequence` are multiplied with.
-struct AttentionSpan {
-    int64_t first, n, b;
-};
+typedef FrameSpan AttentionSpan;
 
 // Long sequences are cut into segments: their sums first (with no state entering), then the states that enter them, then their outputs.  Slots count the
 // segments of all sequences one after the other.
@@ -38,19 +36,8 @@ struct AttentionCut {
 };
 
 #ifdef __CUDACC__
-__device__ __forceinline__ AttentionSpan attention_span(const AttentionArgs& A, int b)
-{
-    AttentionSpan s{0, A.frames, b};
-    if (A.offsets) {
-        const int64_t lo = min(max(A.offsets[b], (int64_t)0), A.frames), hi = min(max(A.offsets[b + 1], (int64_t)0), A.frames);
-        s.first = lo;
-        s.n = max(hi - lo, (int64_t)0);
-        s.b = 0;
-    }
-    return s;
-}
-__device__ __forceinline__ int64_t segments_of(int64_t n, int64_t length) { return n > length ? (n + length - 1) / length : 1; }
-
+__device__ __forceinline__ AttentionSpan attention_span(const AttentionArgs& A, int b) { return frame_span(A.offsets, A.frames, b); }
+__device__ __forceinline__ void find_slot(const SegmentArgs& C, int slot, int& b, int64_t& seg) { find_slot(C.A.offsets, C.A.frames, C.A.batch, C.segment, slot, b, seg); }
 // A CTA's work: frames t0 .. t0 + n - 1 of sequence b, group g, columns of v from c0 on.
 struct AttentionItem {
     int b, g, c0, slot;
@@ -58,40 +45,6 @@ struct AttentionItem {
     AttentionSpan span;
     bool there, last;                                  // last: the sequence ends with it
 };
-// The sequence and segment of a slot.  (All lanes of a warp.)
-__device__ __forceinline__ void find_slot(const SegmentArgs& C, int slot, int& b, int64_t& seg)
-{
-    const AttentionArgs& A = C.A;
-    if (!A.offsets) {
-        const int64_t per = segments_of(A.frames, C.segment);
-        b = (int)(slot / per);
-        seg = slot - b * per;
-        if (b >= A.batch) b = -1;
-        return;
-    }
-    const int lane = threadIdx.x & 31;
-    int64_t before = 0;
-    b = -1;
-    seg = 0;
-    for (int b0 = 0; b0 < A.batch; b0 += 32) {
-        const int64_t mine = b0 + lane < A.batch ? segments_of(attention_span(A, b0 + lane).n, C.segment) : 0;
-        int64_t sum = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-            if (lane >= d) sum += up;
-        }
-        const bool here = mine > 0 && before + sum - mine <= slot && slot < before + sum;
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
-        if (who) {
-            const int w = __ffs(who) - 1;
-            b = b0 + w;
-            seg = slot - (before + __shfl_sync(0xFFFFFFFFu, sum - mine, w));
-            return;
-        }
-        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
-    }
-}
 // cut: the launch is one of segments.
 __device__ __forceinline__ AttentionItem attention_item(const SegmentArgs& C, bool cut, int cols)
 {

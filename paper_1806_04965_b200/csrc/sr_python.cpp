@@ -1,6 +1,6 @@
 // The operators' calls from Python without ctypes and its marshalling: a call on small tensors is host time before anything else (one frame of one sequence 10.4 us
 // through ctypes, 4.2 here).  Every function here checks its arguments, allocates the outputs, calls the C ABI and hands the outputs over; where anything is not as it has to
-// be it returns None and has done nothing, and operators.py, which knows the same rules, says what is wrong.
+// be it returns None and has done nothing, and operators.py or selective.py, which know the same rules, say what is wrong.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -331,14 +331,294 @@ PyObject* py_run(PyObject*, PyObject* const* a, Py_ssize_t n)
     })
 }
 
+// ------------------------------------------------------------------------------------------ the selective head's operators
+// An argument that may be None: null then, and true; false where it is no tensor that fits.
+bool optional(PyObject* o, Device& dev, const at::Tensor*& t)
+{
+    t = nullptr;
+    if (o == Py_None) return true;
+    t = tensor(o);
+    return dev.fits(t);
+}
+bool floats_or_none(const at::Tensor* t, int64_t n) { return !t || floats(t, n); }
+// Frames whose last elements lie side by side, of like's type and leading sizes.
+bool frames_of(const at::Tensor& t, const at::Tensor& like, int lead, int tail)
+{
+    if (t.dim() != lead + tail || t.scalar_type() != like.scalar_type() || (t.stride(lead + tail - 1) != 1 && t.size(lead + tail - 1) > 1)) return false;
+    for (int i = 0; i < lead; ++i)
+        if (t.size(i) != like.size(i)) return false;
+    return true;
+}
+sr_frame_strides frame_strides(const at::Tensor& t, int lead, bool step)
+{
+    return step ? sr_frame_strides{0, t.stride(0)} : sr_frame_strides{t.stride(0), lead == 2 ? t.stride(1) : 0};
+}
+bool plain(const at::Tensor& t, at::ScalarType type, at::IntArrayRef sizes) { return t.scalar_type() == type && t.sizes() == sizes && t.is_contiguous(); }
+// The sequences of frames: -1 where the offsets, or the frames' dimensions, do not fit.
+int64_t sequences(const at::Tensor& x, const at::Tensor* offsets, int lead)
+{
+    if (type_of(x) < 0 || x.dim() != lead + 1 || x.size(lead) < 1 || x.size(lead) > 0x7FFFFFFF) return -1;
+    if (offsets && (offsets->scalar_type() != at::kLong || offsets->dim() != 1 || offsets->size(0) < 1 || !offsets->is_contiguous())) return -1;
+    const int64_t n = offsets ? offsets->size(0) - 1 : x.size(lead - 1);
+    return n > 0x7FFFFFFF ? -1 : n;
+}
+
+bool describe_conv(sr_conv_desc& d, const at::Tensor* x, const at::Tensor* w, const at::Tensor* bias, int silu, int lead, bool step, int64_t batch)
+{
+    if (batch < 0 || silu < 0 || !frames_of(*x, *x, lead, 1)) return false;
+    const int64_t channels = x->size(lead);
+    if (w->dim() != 2 || w->size(1) < 1 || w->size(1) > 0x7FFFFFFF || !plain(*w, at::kFloat, {channels, w->size(1)}) || !floats_or_none(bias, channels)) return false;
+    d.dtype = type_of(*x);
+    d.batch = (int32_t)batch;
+    d.channels = (int32_t)channels;
+    d.width = (int32_t)w->size(1);
+    d.act = silu;
+    d.frames = step ? 1 : x->size(0);
+    d.x = frame_strides(*x, lead, step);
+    d.out = step || lead == 1 ? sr_frame_strides{channels, channels} : sr_frame_strides{channels * batch, channels};
+    if (!step && lead == 1) d.out.sequence = 0;
+    return true;
+}
+
+// conv_run(x, weight, bias or None, silu, state or None, offsets or None, out or None, state_out or None) -> (out, last)
+PyObject* py_conv_run(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 8) return none();
+    SR_GUARDED({
+        Device dev;
+        const at::Tensor *x = tensor(a[0]), *w = tensor(a[1]), *bias, *state, *offsets, *given, *to;
+        const int silu = PyObject_IsTrue(a[3]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
+        if (!dev.fits(x) || !dev.fits(w) || !optional(a[2], dev, bias) || !optional(a[4], dev, state) || !optional(a[5], dev, offsets) || !optional(a[6], dev, given) ||
+            !optional(a[7], dev, to) || !dev.current())
+            return none();
+        const int lead = offsets ? 1 : 2;
+        sr_conv_desc d{};
+        if (!describe_conv(d, x, w, bias, silu, lead, false, sequences(*x, offsets, lead))) return none();
+        const int64_t sizes[3] = {d.batch, d.width - 1, d.channels};
+        const auto type = x->scalar_type();
+        if ((state && !plain(*state, type, sizes)) || (to && !plain(*to, type, sizes)) || (given && !plain(*given, type, x->sizes()))) return none();
+        at::Tensor out = given ? *given : at::Tensor(), last = to ? *to : at::Tensor();
+        sr_status st;
+        {
+            Unlocked u;
+            if (!given) out = new_tensor(*x, x->sizes(), type);
+            if (!to) last = new_tensor(*x, sizes, type);
+            st = sr_causal_conv_run(&d, x->data_ptr(), static_cast<const float*>(w->data_ptr()), bias ? static_cast<const float*>(bias->data_ptr()) : nullptr,
+                                    offsets ? static_cast<const int64_t*>(offsets->data_ptr()) : nullptr, state ? state->data_ptr() : nullptr, last.data_ptr(), out.data_ptr(),
+                                    dev.stream());
+        }
+        if (st != SR_OK) return none();
+        if (given) written(*given);
+        if (to) written(*to);
+        return two(wrap(out), wrap(last));
+    })
+}
+
+// conv_step(x, weight, state, bias or None, silu) -> out
+PyObject* py_conv_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 5) return none();
+    SR_GUARDED({
+        Device dev;
+        const at::Tensor *x = tensor(a[0]), *w = tensor(a[1]), *state = tensor(a[2]), *bias;
+        const int silu = PyObject_IsTrue(a[4]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
+        if (!dev.fits(x) || !dev.fits(w) || !dev.fits(state) || !optional(a[3], dev, bias) || !dev.current()) return none();
+        sr_conv_desc d{};
+        if (!describe_conv(d, x, w, bias, silu, 1, true, sequences(*x, nullptr, 1))) return none();
+        if (!plain(*state, x->scalar_type(), {d.batch, d.width - 1, d.channels})) return none();
+        at::Tensor out;
+        sr_status st;
+        {
+            Unlocked u;
+            out = new_tensor(*x, x->sizes(), x->scalar_type());
+            st = sr_causal_conv_step(&d, x->data_ptr(), static_cast<const float*>(w->data_ptr()), bias ? static_cast<const float*>(bias->data_ptr()) : nullptr,
+                                     state->data_ptr(), out.data_ptr(), dev.stream());
+        }
+        if (st != SR_OK) return none();
+        written(*state);
+        return wrap(out);
+    })
+}
+
+struct Scan {
+    const at::Tensor *u, *dt, *a, *b, *c, *d, *z, *bias;
+    const float* f(const at::Tensor* t) const { return t ? static_cast<const float*>(t->data_ptr()) : nullptr; }
+};
+bool describe_scan(sr_scan_desc& d, const Scan& s, int softplus, int lead, bool step, int64_t batch)
+{
+    if (batch < 0 || softplus < 0) return false;
+    const int64_t channels = s.u->size(lead);
+    for (const at::Tensor* t : {s.u, s.dt, s.z})
+        if (t && (!frames_of(*t, *s.u, lead, 1) || t->size(lead) != channels)) return false;
+    if (!frames_of(*s.b, *s.u, lead, 2) || !frames_of(*s.c, *s.u, lead, 2)) return false;
+    const int64_t groups = s.b->size(lead), states = s.b->size(lead + 1);
+    if (s.c->size(lead) != groups || s.c->size(lead + 1) != states || groups < 1 || states < 1 || states > 0x7FFFFFFF || channels % groups) return false;
+    if (!plain(*s.a, at::kFloat, {channels, states}) || !floats_or_none(s.d, channels) || !floats_or_none(s.bias, channels)) return false;
+    auto three = [&](const at::Tensor& t) {
+        const sr_frame_strides f = frame_strides(t, lead, step);
+        return sr_attention_strides{f.frame, f.sequence, t.stride(lead)};
+    };
+    d.dtype = type_of(*s.u);
+    d.batch = (int32_t)batch;
+    d.channels = (int32_t)channels;
+    d.states = (int32_t)states;
+    d.groups = (int32_t)groups;
+    d.softplus = softplus;
+    d.frames = step ? 1 : s.u->size(0);
+    d.u = frame_strides(*s.u, lead, step);
+    d.dt = frame_strides(*s.dt, lead, step);
+    if (s.z) d.z = frame_strides(*s.z, lead, step);
+    d.out = step ? sr_frame_strides{0, channels} : lead == 1 ? sr_frame_strides{channels, 0} : sr_frame_strides{channels * batch, channels};
+    d.b = three(*s.b);
+    d.c = three(*s.c);
+    return true;
+}
+
+// scan_run(u, dt, a, b, c, d, z, dt_bias (each or None), softplus, state or None, offsets or None, out or None, state_out or None) -> (out, last)
+PyObject* py_scan_run(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 13) return none();
+    SR_GUARDED({
+        Device dev;
+        Scan s{tensor(a[0]), tensor(a[1]), tensor(a[2]), tensor(a[3]), tensor(a[4]), nullptr, nullptr, nullptr};
+        const at::Tensor *state, *offsets, *given, *to;
+        const int softplus = PyObject_IsTrue(a[8]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
+        if (!dev.fits(s.u) || !dev.fits(s.dt) || !dev.fits(s.a) || !dev.fits(s.b) || !dev.fits(s.c) || !optional(a[5], dev, s.d) || !optional(a[6], dev, s.z) ||
+            !optional(a[7], dev, s.bias) || !optional(a[9], dev, state) || !optional(a[10], dev, offsets) || !optional(a[11], dev, given) || !optional(a[12], dev, to) ||
+            !dev.current())
+            return none();
+        const int lead = offsets ? 1 : 2;
+        const int64_t batch = sequences(*s.u, offsets, lead);
+        sr_scan_desc d{};
+        if (batch < 0 || !describe_scan(d, s, softplus, lead, false, batch)) return none();
+        const int64_t sizes[3] = {d.batch, d.channels, d.states};
+        if ((state && !plain(*state, at::kFloat, sizes)) || (to && !plain(*to, at::kFloat, sizes)) || (given && !plain(*given, s.u->scalar_type(), s.u->sizes()))) return none();
+        at::Tensor out = given ? *given : at::Tensor(), last = to ? *to : at::Tensor();
+        sr_status st;
+        {
+            Unlocked u;
+            if (!given) out = new_tensor(*s.u, s.u->sizes(), s.u->scalar_type());
+            if (!to) last = new_tensor(*s.u, sizes, at::kFloat);
+            size_t bytes = 0;
+            st = sr_selective_scan_workspace_bytes(&d, offsets ? 1 : 0, &bytes);
+            at::Tensor work;
+            if (st == SR_OK && bytes) work = new_tensor(*s.u, {(int64_t)bytes}, at::kByte);
+            if (st == SR_OK)
+                st = sr_selective_scan_run(&d, s.u->data_ptr(), s.dt->data_ptr(), s.f(s.a), s.b->data_ptr(), s.c->data_ptr(), s.f(s.d), s.z ? s.z->data_ptr() : nullptr, s.f(s.bias),
+                                           offsets ? static_cast<const int64_t*>(offsets->data_ptr()) : nullptr, s.f(state), static_cast<float*>(last.data_ptr()), out.data_ptr(),
+                                           bytes ? work.data_ptr() : nullptr, bytes, dev.stream());
+        }
+        if (st != SR_OK) return none();
+        if (given) written(*given);
+        if (to) written(*to);
+        return two(wrap(out), wrap(last));
+    })
+}
+
+// scan_step(u, dt, a, b, c, state, d, z, dt_bias (each or None), softplus) -> out
+PyObject* py_scan_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 10) return none();
+    SR_GUARDED({
+        Device dev;
+        Scan s{tensor(a[0]), tensor(a[1]), tensor(a[2]), tensor(a[3]), tensor(a[4]), nullptr, nullptr, nullptr};
+        const at::Tensor* state = tensor(a[5]);
+        const int softplus = PyObject_IsTrue(a[9]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
+        if (!dev.fits(s.u) || !dev.fits(s.dt) || !dev.fits(s.a) || !dev.fits(s.b) || !dev.fits(s.c) || !dev.fits(state) || !optional(a[6], dev, s.d) ||
+            !optional(a[7], dev, s.z) || !optional(a[8], dev, s.bias) || !dev.current())
+            return none();
+        const int64_t batch = sequences(*s.u, nullptr, 1);
+        sr_scan_desc d{};
+        if (batch < 0 || !describe_scan(d, s, softplus, 1, true, batch) || !plain(*state, at::kFloat, {d.batch, d.channels, d.states})) return none();
+        at::Tensor out;
+        sr_status st;
+        {
+            Unlocked u;
+            out = new_tensor(*s.u, s.u->sizes(), s.u->scalar_type());
+            st = sr_selective_scan_step(&d, s.u->data_ptr(), s.dt->data_ptr(), s.f(s.a), s.b->data_ptr(), s.c->data_ptr(), s.f(s.d), s.z ? s.z->data_ptr() : nullptr, s.f(s.bias),
+                                        static_cast<float*>(state->data_ptr()), out.data_ptr(), dev.stream());
+        }
+        if (st != SR_OK) return none();
+        written(*state);
+        return wrap(out);
+    })
+}
+
+// block_norm(y, residual, weight_after or None, weight_before or None, gate or None, gate_act, scale, eps, norms, format or 0) -> (out, or data and scales, or None; h)
+PyObject* py_block_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 10) return none();
+    SR_GUARDED({
+        Device dev;
+        const at::Tensor *y = tensor(a[0]), *r = tensor(a[1]), *after, *before, *gate;
+        const int act = (int)PyLong_AsLong(a[5]), norms = (int)PyLong_AsLong(a[8]), format = (int)PyLong_AsLong(a[9]);
+        const double scale = PyFloat_AsDouble(a[6]), eps = PyFloat_AsDouble(a[7]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
+        if (!dev.fits(y) || !dev.fits(r) || !optional(a[2], dev, after) || !optional(a[3], dev, before) || !optional(a[4], dev, gate) || !dev.current()) return none();
+        sr_block_desc d{};
+        if (norms < 0 || norms > 3 || (format && !(norms & SR_NORM_BEFORE)) || !rows_of(*y, d.y_stride)) return none();
+        d.rows = y->size(0);
+        d.cols = y->size(1);
+        if (!rows_of(*r, d.residual_stride) || r->sizes() != y->sizes() || r->scalar_type() != y->scalar_type()) return none();
+        if (gate && (!rows_of(*gate, d.gate_stride) || gate->sizes() != y->sizes() || gate->scalar_type() != y->scalar_type())) return none();
+        if (!floats_or_none(after, d.cols) || !floats_or_none(before, d.cols)) return none();
+        d.dtype = type_of(*y);
+        d.norms = norms;
+        d.gate_act = act;
+        d.out_format = format ? format : d.dtype;
+        d.scale = (float)scale;
+        d.eps = (float)eps;
+        const bool next = norms & SR_NORM_BEFORE;
+        at::Tensor h, out;
+        Scaled m;
+        sr_status st;
+        {
+            Unlocked u;
+            h = new_tensor(*y, {d.rows, d.cols}, y->scalar_type());
+            if (next && format) m = new_scaled(*y, d.rows, d.cols, format);
+            else if (next) out = new_tensor(*y, {d.rows, d.cols}, y->scalar_type());
+            st = sr_block_norm(&d, y->data_ptr(), r->data_ptr(), gate ? gate->data_ptr() : nullptr, after ? static_cast<const float*>(after->data_ptr()) : nullptr,
+                               before ? static_cast<const float*>(before->data_ptr()) : nullptr, h.data_ptr(), !next ? nullptr : format ? m.data.data_ptr() : out.data_ptr(),
+                               next && format ? m.scales.data_ptr() : nullptr, dev.stream());
+        }
+        if (st != SR_OK) return none();
+        PyObject* first = !next ? none() : format ? two(wrap(m.data), wrap(m.scales)) : wrap(out);
+        return two(first, wrap(h));
+    })
+}
+
 PyMethodDef methods[] = {
+    {"conv_run", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_conv_run)), METH_FASTCALL, nullptr},
+    {"conv_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_conv_step)), METH_FASTCALL, nullptr},
+    {"scan_run", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_scan_run)), METH_FASTCALL, nullptr},
+    {"scan_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_scan_step)), METH_FASTCALL, nullptr},
+    {"block_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_block_norm)), METH_FASTCALL, nullptr},
     {"quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_quantize)), METH_FASTCALL, nullptr},
     {"product", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_product)), METH_FASTCALL, nullptr},
     {"rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_norm)), METH_FASTCALL, nullptr},
     {"step", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_step)), METH_FASTCALL, nullptr},
     {"run", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_run)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_operators", "Fast path of operators.py.", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_operators", "Fast path of operators.py and selective.py.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -1,0 +1,70 @@
+// Sequences of frames, side by side or packed one behind the other, and their segments: what kernels over the frames share.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+// First frame and number of frames of a sequence; b: what its strides `sequence` are multiplied with.
+struct FrameSpan {
+    int64_t first, n, b;
+};
+
+#ifdef __CUDACC__
+// offsets NULL: sequences of `frames` frames side by side.  Offsets outside 0 .. frames are taken as the nearest of the two, a decreasing one as an empty sequence.
+__device__ __forceinline__ FrameSpan frame_span(const int64_t* offsets, int64_t frames, int64_t b)
+{
+    FrameSpan s{0, frames, b};
+    if (offsets) {
+        const int64_t lo = min(max(offsets[b], (int64_t)0), frames), hi = min(max(offsets[b + 1], (int64_t)0), frames);
+        s.first = lo;
+        s.n = max(hi - lo, (int64_t)0);
+        s.b = 0;
+    }
+    return s;
+}
+__host__ __device__ __forceinline__ int64_t segments_of(int64_t n, int64_t length) { return n > length ? (n + length - 1) / length : 1; }
+
+// The sequence (-1: none) and segment of a slot; slots count the segments of all sequences one after the other.  (All lanes of a warp.)
+__device__ __forceinline__ void find_slot(const int64_t* offsets, int64_t frames, int batch, int64_t segment, int64_t slot, int& b, int64_t& seg)
+{
+    if (!offsets) {
+        const int64_t per = segments_of(frames, segment);
+        const int64_t at = slot / per;
+        b = at < batch ? (int)at : -1;
+        seg = slot - at * per;
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    b = -1;
+    seg = 0;
+    for (int b0 = 0; b0 < batch; b0 += 32) {
+        const int64_t mine = b0 + lane < batch ? segments_of(frame_span(offsets, frames, b0 + lane).n, segment) : 0;
+        int64_t sum = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+            if (lane >= d) sum += up;
+        }
+        const bool here = mine > 0 && before + sum - mine <= slot && slot < before + sum;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
+        if (who) {
+            const int w = __ffs(who) - 1;
+            b = b0 + w;
+            seg = slot - (before + __shfl_sync(0xFFFFFFFFu, sum - mine, w));
+            return;
+        }
+        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+}
+// The first slot of sequence b.  (All lanes of a warp.)
+__device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int64_t frames, int64_t segment, int b)
+{
+    if (!offsets) return b * segments_of(frames, segment);
+    int64_t sum = 0;
+    for (int i = threadIdx.x & 31; i < b; i += 32) sum += segments_of(frame_span(offsets, frames, i).n, segment);
+#pragma unroll
+    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    return sum;
+}
+#endif

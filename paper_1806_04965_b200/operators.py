@@ -429,7 +429,22 @@ def operator_reset(device=None):
     _call("sr_operator_reset", _device_index("operator_reset", device), _library().sr_operator_reset)
 
 
-class TemporalHead:
+class _Head:
+    """What heads behind a rollout share: `batch` sequences, `channels` features of a frame, and a device."""
+
+    def _fits(self, call: str, features, lead: int):
+        if features.dim() <= lead or features.shape[lead - 1] != self.batch or math.prod(features.shape[lead:]) != self.channels:
+            _refuse("%s.%s" % (type(self).__name__, call), "the head takes %s[%d sequences][%d channels]" % ("[frames]" if lead == 2 else "", self.batch, self.channels))
+
+    def check_features(self, shape, device):
+        """Refuses features of one frame that the head cannot take: [batch][...channels], on its device."""
+        if len(shape) < 1 or shape[0] != self.batch or math.prod(shape[1:]) != self.channels:
+            _refuse(type(self).__name__, "the head takes [%d sequences][%d channels]" % (self.batch, self.channels))
+        if _device_index(type(self).__name__, device) != self.device.index:
+            _refuse(type(self).__name__, "the head lies on %s" % self.device)
+
+
+class TemporalHead(_Head):
     """A head with a memory over the frames on the features that a rollout gives, per frame and sequence
 
         q, k, v = Wqkv norm(x)      (microscaled operands)
@@ -469,6 +484,10 @@ class TemporalHead:
         self.scale = float(dk) ** -0.5
         self.state = torch.zeros((batch, groups, dk, dv), dtype=torch.float32, device=device)
 
+    @property
+    def device(self):
+        return self.state.device
+
     def reset(self):
         """Before the first frame: no memory."""
         self.state.zero_()
@@ -490,17 +509,6 @@ class TemporalHead:
         y = product(rms_norm(o.reshape(x.shape[0], self.heads * self.dv), self._w["norm_o"], eps=self.eps, format=self.format), self._w["o"], dtype=self.tdtype)
         m, _ = rms_norm(y, self._w["norm_h"], residual=x, eps=self.eps, format=self.format)
         return product(m, self._w["out"], bias=self._w["bias"], dtype=torch.float32)
-
-    def _fits(self, call: str, features, lead: int):
-        if features.dim() <= lead or features.shape[lead - 1] != self.batch or math.prod(features.shape[lead:]) != self.channels:
-            _refuse("TemporalHead." + call, "the head takes %s[%d sequences][%d channels]" % ("[frames]" if lead == 2 else "", self.batch, self.channels))
-
-    def check_features(self, shape, device):
-        """Refuses features of one frame that the head cannot take: [batch][...channels], on its device."""
-        if len(shape) < 1 or shape[0] != self.batch or math.prod(shape[1:]) != self.channels:
-            _refuse("TemporalHead", "the head takes [%d sequences][%d channels]" % (self.batch, self.channels))
-        if _device_index("TemporalHead", device) != self.state.get_device():
-            _refuse("TemporalHead", "the head lies on %s" % self.state.device)
 
     @torch.no_grad()
     def run(self, features):
