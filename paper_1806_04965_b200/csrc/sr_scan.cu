@@ -37,18 +37,15 @@ struct ScanArgs {
     int32_t batch, channels, states, groups, share, softplus, tiles;      // share: channels of a group; tiles: CTAs side by side over them
     sr_frame_strides su, sdt, sz, so;
     sr_attention_strides sb, sc;
+    bool units;                                        // b and c can be copied 16 bytes at a time
 };
 
-constexpr int kThreads = 128, kBlock = 8;              // frames that are loaded ahead
+constexpr int kBlock = 8;                              // frames of a stage
+constexpr int kChunk = 32;                             // frames that a state is carried over at once
+constexpr int kWarps = 16;                             // of an SM: 128 registers
 enum { kWhole = 0, kSums = 1, kOutputs = 2 };          // whole sequences; sums of segments; outputs of segments, from the states that enter them
-
-template <int K, int L>
-struct ScanTile {
-    static constexpr int NP = K * L;                   // states, with those that pad them
-    static constexpr int PIECE = NP >= 128 ? kBlock : 1024 / NP;          // frames of b and c in a buffer
-    static constexpr int SIDE = 32 / L;                // channels of a warp
-    static constexpr int CHANNELS = kThreads / L;
-};
+// A block's threads share b and c, whose widening is the more to do the more states there are; fewer make the work of SMs more even.
+__host__ __device__ constexpr int threads_of(int lanes) { return lanes < 4 ? 32 : 128; }
 
 // Sum over the L threads of a channel, whose lanes are SIDE apart: thread p gets frame p's.
 template <int L, int SIDE>
@@ -66,14 +63,126 @@ __device__ __forceinline__ float exchange(float (&y)[L], int p)
     return y[0];
 }
 
-template <typename T, int K, int L, int MODE>
-__global__ void __launch_bounds__(kThreads) sr_scan_kernel(const __grid_constant__ ScanArgs A)
+__device__ __forceinline__ void copy_16(void* dst, const void* src)
 {
-    using Tile = ScanTile<K, L>;
-    constexpr int NP = Tile::NP, PIECE = Tile::PIECE, SIDE = Tile::SIDE, Q = kBlock / L, EACH = PIECE * NP / kThreads;
-    constexpr bool EXACT = sizeof(T) == 4;
-    static_assert(kBlock % L == 0 && PIECE % kBlock == 0 && PIECE * NP % kThreads == 0);
-    __shared__ __align__(16) float sb[2][PIECE][NP], sc[MODE == kSums ? 1 : 2][MODE == kSums ? 1 : PIECE][NP];
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(srx::smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_4(void* dst, const void* src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(srx::smem_u32(dst)), "l"(src) : "memory");
+}
+// N elements, side by side, at once.
+template <typename T, int N>
+struct Few {
+    static constexpr int BYTES = N * (int)sizeof(T), WORDS = BYTES < 4 ? 1 : BYTES / 4;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void get(const T* p)
+    {
+        if constexpr (BYTES >= 16) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) {
+                const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (BYTES == 8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[0] = v.x; w[1] = v.y;
+        } else if constexpr (BYTES == 4) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void put(T* p) const
+    {
+        if constexpr (BYTES >= 16) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        } else if constexpr (BYTES == 8) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        } else if constexpr (BYTES == 4) {
+            *reinterpret_cast<uint32_t*>(p) = w[0];
+        } else {
+            *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+    __device__ __forceinline__ void set(const float (&f)[N])
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
+        } else if constexpr (N == 1) {
+            w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(f[0]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i += 2) w[i / 2] = srx::round_bf16(srx::pair(f[i], f[i + 1]));
+        }
+    }
+    __device__ __forceinline__ void put_one(T* p, int i) const
+    {
+        if constexpr (sizeof(T) == 4) *p = __uint_as_float(w[i]);
+        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[i / 2] >> (i & 1 ? 16 : 0));
+    }
+};
+// A stage's rows of a tensor, `cols` of COLS elements in each, into shared memory, by THREADS threads: 16 bytes at a time (UNITS), or an element.  What is behind the last
+// column or frame stays what it was.
+template <typename T, int COLS, int THREADS, bool UNITS>
+struct Rows {
+    static constexpr int UNIT = UNITS ? 16 / (int)sizeof(T) : 1, PER_ROW = COLS / UNIT > 0 ? COLS / UNIT : 1, COPIES = (kBlock * PER_ROW + THREADS - 1) / THREADS;
+    __device__ __forceinline__ static int frame(int e, int tid) { return (e * THREADS + tid) / PER_ROW; }
+    __device__ __forceinline__ static int col(int tid) { return tid % PER_ROW * UNIT; }       // (of all its copies)
+    static_assert(THREADS % PER_ROW == 0 || PER_ROW % THREADS == 0);
+    // from: the thread's first row and column
+    __device__ __forceinline__ static void copy(T (*to)[COLS], const T* from, int64_t stride, int cols, int left, int tid)
+    {
+        if constexpr (PER_ROW <= THREADS) {
+            if (col(tid) >= cols) return;
+#pragma unroll
+            for (int e = 0; e < COPIES; ++e) {
+                const int f = frame(e, tid);
+                if (f < left) one(&to[f][col(tid)], from + e * (THREADS / PER_ROW) * stride);
+            }
+        } else {
+#pragma unroll
+            for (int f = 0; f < kBlock; ++f)
+#pragma unroll
+                for (int c = 0; c < PER_ROW; c += THREADS)
+                    if (f < left && (c + tid) * UNIT < cols) one(&to[f][(c + tid) * UNIT], from + f * stride + c * UNIT);
+        }
+    }
+    __device__ __forceinline__ static int64_t start(int tid, int64_t stride) { return PER_ROW <= THREADS ? frame(0, tid) * stride + col(tid) : tid * UNIT; }
+    __device__ __forceinline__ static void one(T* to, const T* from)
+    {
+        if constexpr (UNITS) copy_16(to, from);
+        else if constexpr (sizeof(T) == 4) copy_4(to, from);
+        else *to = *from;
+    }
+};
+
+// What lies in shared memory: two stages as they come in, b and c of the one that is worked on as floats, its outputs, and the states at the chunk's start.
+template <typename T, int K, int L, int THREADS, bool OUT>
+struct ScanShared {
+    static constexpr int NP = K * L, CHANNELS = THREADS / L, OUTS = OUT ? 2 : 1;
+    T u[2][kBlock][CHANNELS], dt[2][kBlock][CHANNELS], z[OUTS][kBlock][CHANNELS], out[OUT ? kBlock : 1][CHANNELS];
+    T b[2][kBlock][NP], c[OUTS][kBlock][NP];
+    float bf[kBlock][NP], cf[OUT ? kBlock : 1][NP];
+    float2 carried[K / 2][THREADS];
+};
+
+template <typename T, int K, int L, int MODE, bool WIDE>
+__global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr_scan_kernel(const __grid_constant__ ScanArgs A)
+{
+    constexpr int THREADS = threads_of(L), NP = K * L, SIDE = 32 / L, CHANNELS = THREADS / L, N = kBlock / L;
+    constexpr bool EXACT = sizeof(T) == 4, OUT = MODE != kSums;
+    using Shared = ScanShared<T, K, L, THREADS, OUT>;
+    static_assert(kBlock % L == 0 && kChunk % kBlock == 0);
+    extern __shared__ __align__(16) uint8_t memory[];
+    Shared& S = *reinterpret_cast<Shared*>(memory);
     srx::let_successor_start();
     srx::wait_for_predecessor();
 
@@ -88,13 +197,97 @@ __global__ void __launch_bounds__(kThreads) sr_scan_kernel(const __grid_constant
     const bool last = t0 + n >= span.n;
     if (MODE == kSums && last) return;                 // (nobody asks for them)
 
-    const int lane = threadIdx.x & 31, p = lane / SIDE, in_tile = (threadIdx.x >> 5) * SIDE + lane % SIDE, in_group = tile * Tile::CHANNELS + in_tile;
-    const bool there = in_group < A.share;
-    const int ch = g * A.share + (there ? in_group : 0);
+    const int tid = threadIdx.x, lane = tid & 31, p = lane / SIDE, col = (tid >> 5) * SIDE + lane % SIDE;
+    const int channels = min(A.share - tile * CHANNELS, CHANNELS), ch0 = g * A.share + tile * CHANNELS;
+    const bool there = col < channels;
+    const int ch = ch0 + (there ? col : 0);
     const int64_t first = span.first + t0;
+    const bool gated = OUT && A.z;
+    auto sync = [] {
+        if (THREADS == 32) __syncwarp();
+        else __syncthreads();
+    };
 
-    // the thread's states and decays
-    Pair h[K / 2], a2[K / 2];
+    // ---- copies
+    using Wide = Rows<T, CHANNELS, THREADS, WIDE>;
+    using Some = Rows<T, NP, THREADS, false>;
+    using Units = Rows<T, NP, THREADS, true>;
+    constexpr bool CAN = NP * sizeof(T) >= 16;         // rows of b and c in whole units
+    const T* gu = static_cast<const T*>(A.u) + first * A.su.frame + span.b * A.su.sequence + ch0 + Wide::start(tid, A.su.frame);
+    const T* gdt = static_cast<const T*>(A.dt) + first * A.sdt.frame + span.b * A.sdt.sequence + ch0 + Wide::start(tid, A.sdt.frame);
+    const T* gz = gated ? static_cast<const T*>(A.z) + first * A.sz.frame + span.b * A.sz.sequence + ch0 + Wide::start(tid, A.sz.frame) : nullptr;
+    const T* gb = static_cast<const T*>(A.b) + first * A.sb.frame + span.b * A.sb.sequence + g * A.sb.head;
+    const T* gc = static_cast<const T*>(A.c) + first * A.sc.frame + span.b * A.sc.sequence + g * A.sc.head;
+    const bool units = CAN && A.units;
+    gb += units ? Units::start(tid, A.sb.frame) : Some::start(tid, A.sb.frame);
+    gc += units ? Units::start(tid, A.sc.frame) : Some::start(tid, A.sc.frame);
+    auto frames_from = [&](int64_t at) { return (int)max(min(n - at, (int64_t)kBlock), (int64_t)0); };
+    auto fetch = [&](int half, int left) {
+        Wide::copy(S.u[half], gu, A.su.frame, channels, left, tid);
+        Wide::copy(S.dt[half], gdt, A.sdt.frame, channels, left, tid);
+        gu += kBlock * A.su.frame;
+        gdt += kBlock * A.sdt.frame;
+        if (gated) {
+            Wide::copy(S.z[OUT ? half : 0], gz, A.sz.frame, channels, left, tid);
+            gz += kBlock * A.sz.frame;
+        }
+        if (units) {
+            if constexpr (CAN) {
+                Units::copy(S.b[half], gb, A.sb.frame, A.states, left, tid);
+                if (OUT) Units::copy(S.c[OUT ? half : 0], gc, A.sc.frame, A.states, left, tid);
+            }
+        } else {
+            Some::copy(S.b[half], gb, A.sb.frame, A.states, left, tid);
+            if (OUT) Some::copy(S.c[OUT ? half : 0], gc, A.sc.frame, A.states, left, tid);
+        }
+        gb += kBlock * A.sb.frame;
+        gc += kBlock * A.sc.frame;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    auto widen = [&](int half, int left) {             // b and c as floats: a thread's neighbouring states, all of a frame; zeros behind the last frame and state
+        constexpr int PART = kBlock * NP > THREADS ? (kBlock * NP / THREADS < 8 ? kBlock * NP / THREADS : 8) : 1, PER = NP / PART;
+#pragma unroll
+        for (int i = tid; i < kBlock * PER; i += THREADS) {
+            const int f = i / PER, c = i % PER * PART;
+            Few<T, PART> v;
+            float y[PART];
+            Few<float, PART> to;
+            v.get(&S.b[half][f][c]);
+#pragma unroll
+            for (int e = 0; e < PART; ++e) y[e] = f < left && c + e < A.states ? v[e] : 0.0f;
+            to.set(y);
+            to.put(&S.bf[f][c]);
+            if (OUT) {
+                v.get(&S.c[OUT ? half : 0][f][c]);
+#pragma unroll
+                for (int e = 0; e < PART; ++e) y[e] = f < left && c + e < A.states ? v[e] : 0.0f;
+                to.set(y);
+                to.put(&S.cf[OUT ? f : 0][c]);
+            }
+        }
+    };
+    T* go = OUT ? static_cast<T*>(A.out) + first * A.so.frame + span.b * A.so.sequence + ch0 + Wide::start(tid, A.so.frame) : nullptr;
+    auto put = [&](int left) {                         // a stage's outputs
+        if constexpr (Wide::PER_ROW <= THREADS) {
+            if (Wide::col(tid) < channels)
+#pragma unroll
+                for (int e = 0; e < Wide::COPIES; ++e) {
+                    const int f = Wide::frame(e, tid);
+                    T* to = go + e * (THREADS / Wide::PER_ROW) * A.so.frame;
+                    if (f < left) {
+                        if constexpr (WIDE) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&S.out[OUT ? f : 0][Wide::col(tid)]);
+                        else *to = S.out[OUT ? f : 0][Wide::col(tid)];
+                    }
+                }
+        }
+        go += kBlock * A.so.frame;
+    };
+    static_assert(Wide::PER_ROW <= THREADS);
+    const float bias = A.bias ? A.bias[ch] : 0.0f, skip = OUT && A.d ? A.d[ch] : 0.0f;
+
+    // ---- the thread's states and decays; local: what the states are without those at the chunk's start
+    Pair h[K / 2], local[K / 2], a2[K / 2];
     {
         const float* from = MODE == kWhole ? (A.state_in ? A.state_in + ((int64_t)b * A.channels + ch) * A.states : nullptr)
                                            : MODE == kOutputs ? A.sums + (slot * A.channels + ch) * A.states : nullptr;
@@ -103,119 +296,81 @@ __global__ void __launch_bounds__(kThreads) sr_scan_kernel(const __grid_constant
         for (int k = 0; k < K; k += 2) {
             const int i = ((k / 4) * L + p) * 4 + k % 4;
             const bool lo = i < A.states, hi = i + 1 < A.states;
-            a2[k / 2] = srx::pair(lo ? srx::kLog2e * a[i] : 0.0f, hi ? srx::kLog2e * a[i + 1] : 0.0f);
-            h[k / 2] = srx::pair(from && lo ? from[i] : 0.0f, from && hi ? from[i + 1] : 0.0f);
+            a2[k / 2] = srx::pair(lo ? srx::decay_base2(a[i]) : 0.0f, hi ? srx::decay_base2(a[i + 1]) : 0.0f);
+            const float2 v = make_float2(from && lo ? from[i] : 0.0f, from && hi ? from[i + 1] : 0.0f);
+            S.carried[k / 2][tid] = v;
+            h[k / 2] = srx::pair(v.x, v.y);
+            local[k / 2] = srx::pair(0.0f, 0.0f);
         }
     }
-    const float bias = A.bias ? A.bias[ch] : 0.0f, skip = A.d ? A.d[ch] : 0.0f;
 
-    // where the thread's frames lie: every L-th, from p on
-    const T* pu = static_cast<const T*>(A.u) + (first + p) * A.su.frame + span.b * A.su.sequence + ch;
-    const T* pdt = static_cast<const T*>(A.dt) + (first + p) * A.sdt.frame + span.b * A.sdt.sequence + ch;
-    const T* pz = A.z && MODE != kSums ? static_cast<const T*>(A.z) + (first + p) * A.sz.frame + span.b * A.sz.sequence + ch : nullptr;
-    T* po = MODE == kSums ? nullptr : static_cast<T*>(A.out) + (first + p) * A.so.frame + span.b * A.so.sequence + ch;
-    const int64_t du = L * A.su.frame, ddt = L * A.sdt.frame, dz = L * A.sz.frame, dout = L * A.so.frame;
-    T un[Q], dn[Q], zn[Q];
-    auto load = [&](int64_t at) {                      // the block of frames from `at` on
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const bool in = at + q * L + p < n;
-            un[q] = in ? *pu : (T)0.0f;
-            dn[q] = in ? *pdt : (T)0.0f;
-            if (MODE != kSums) zn[q] = in && pz ? *pz : (T)0.0f;
-            pu += du;
-            pdt += ddt;
-            if (MODE != kSums && pz) pz += dz;
-        }
-    };
-    // b and c of a piece of frames, as they lie in memory
-    const T* gb = static_cast<const T*>(A.b) + first * A.sb.frame + span.b * A.sb.sequence + g * A.sb.head;
-    const T* gc = static_cast<const T*>(A.c) + first * A.sc.frame + span.b * A.sc.sequence + g * A.sc.head;
-    T bn[EACH], cn[EACH];
-    auto load_piece = [&](int64_t at) {
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int x = e * kThreads + threadIdx.x, i = x % NP;
-            const int64_t t = at + x / NP;
-            const bool in = t < n && i < A.states;
-            bn[e] = in ? gb[t * A.sb.frame + i] : (T)0.0f;
-            if (MODE != kSums) cn[e] = in ? gc[t * A.sc.frame + i] : (T)0.0f;
-        }
-    };
-    auto keep_piece = [&](int to) {
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int x = e * kThreads + threadIdx.x;
-            sb[to][x / NP][x % NP] = (float)bn[e];
-            if (MODE != kSums) sc[to][x / NP][x % NP] = (float)cn[e];
-        }
-    };
-
-    load_piece(0);
-    load(0);
-    keep_piece(0);
-    __syncthreads();
+    fetch(0, frames_from(0));
     double total = 0.0;                                // of r
-    int buffer = 0;
-    for (int64_t at = 0; at < n; at += PIECE) {
-        if (at + PIECE < n) load_piece(at + PIECE);
-#pragma unroll 1
-        for (int in_piece = 0; in_piece < PIECE && at + in_piece < n; in_piece += kBlock) {
-            float r[Q], x[Q], u[Q], z[Q];
+    float since = 0.0f;                                // of r, from the chunk's start on
+    int half = 0;
+    for (int64_t at = 0; at < n; at += kBlock, half ^= 1) {
+        const int left = frames_from(at);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        sync();                                        // the stage has landed, and the one before is done with
+        if (at + kBlock < n) fetch(half ^ 1, frames_from(at + kBlock));
+        widen(half, left);
+        sync();
+#pragma unroll 2
+        for (int q = 0; q < N; ++q) {
+            // of L frames each of the channel's threads prepares one
+            const int mine = q * L + p;
+            const float s = (float)S.dt[half][mine][col] + bias, u = (float)S.u[half][mine][col], plus = srx::softplus<EXACT>(s);
+            const float r = mine >= left ? 0.0f : A.softplus ? plus : s;         // (a frame behind the last one changes nothing)
+            const float x = mine >= left ? 0.0f : r * u;
+            float y[L];
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const float s = (float)dn[q] + bias;
-                r[q] = A.softplus ? srx::softplus(s) : s;
-                u[q] = (float)un[q];
-                x[q] = r[q] * u[q];
-                if (MODE != kSums) z[q] = (float)zn[q];
-            }
-            const int64_t t = at + in_piece;
-            const int left = (int)min(n - t, (int64_t)kBlock);
-            if (t + kBlock < n) load(t + kBlock);
+            for (int i = 0; i < L; ++i) {
+                const int f = q * L + i;
+                const float rr = L > 1 ? __shfl_sync(0xFFFFFFFFu, r, i * SIDE + lane % SIDE) : r;
+                const float xx = L > 1 ? __shfl_sync(0xFFFFFFFFu, x, i * SIDE + lane % SIDE) : x;
+                since += rr;
+                const Pair r2 = srx::pair(rr, rr), x2 = srx::pair(xx, xx);
+                Pair y2 = srx::pair(0.0f, 0.0f);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                float y[L];
-#pragma unroll
-                for (int i = 0; i < L; ++i) {
-                    const int f = q * L + i;
-                    const float rr = L > 1 ? __shfl_sync(0xFFFFFFFFu, r[q], i * SIDE + lane % SIDE) : r[q];
-                    const float xx = L > 1 ? __shfl_sync(0xFFFFFFFFu, x[q], i * SIDE + lane % SIDE) : x[q];
-                    y[i] = 0.0f;
-                    if (f < left) {
-                        const Pair r2 = srx::pair(rr, rr), x2 = srx::pair(xx, xx);
-                        Pair y2 = srx::pair(0.0f, 0.0f);
-#pragma unroll
-                        for (int k = 0; k < K; k += 4) {
-                            const float4 bv = *reinterpret_cast<const float4*>(&sb[buffer][in_piece + f][((k / 4) * L + p) * 4]);
-                            const float2 e0 = srx::split(srx::mul2(r2, a2[k / 2])), e1 = srx::split(srx::mul2(r2, a2[k / 2 + 1]));
-                            h[k / 2] = srx::fma2(srx::pair(srx::ex2(e0.x), srx::ex2(e0.y)), h[k / 2], srx::mul2(x2, srx::pair(bv.x, bv.y)));
-                            h[k / 2 + 1] = srx::fma2(srx::pair(srx::ex2(e1.x), srx::ex2(e1.y)), h[k / 2 + 1], srx::mul2(x2, srx::pair(bv.z, bv.w)));
-                            if (MODE != kSums) {
-                                const float4 cv = *reinterpret_cast<const float4*>(&sc[buffer][in_piece + f][((k / 4) * L + p) * 4]);
-                                y2 = srx::fma2(srx::pair(cv.x, cv.y), h[k / 2], y2);
-                                y2 = srx::fma2(srx::pair(cv.z, cv.w), h[k / 2 + 1], y2);
-                            }
-                        }
-                        const float2 s = srx::split(y2);
-                        y[i] = s.x + s.y;
+                for (int k = 0; k < K; k += 4) {
+                    const float4 bv = *reinterpret_cast<const float4*>(&S.bf[f][((k / 4) * L + p) * 4]);
+                    const float2 e0 = srx::split(srx::mul2(r2, a2[k / 2])), e1 = srx::split(srx::mul2(r2, a2[k / 2 + 1]));
+                    const Pair d0 = srx::pair(srx::ex2(e0.x), srx::ex2(e0.y)), d1 = srx::pair(srx::ex2(e1.x), srx::ex2(e1.y));
+                    const Pair i0 = srx::mul2(x2, srx::pair(bv.x, bv.y)), i1 = srx::mul2(x2, srx::pair(bv.z, bv.w));
+                    local[k / 2] = srx::fma2(d0, local[k / 2], i0);
+                    local[k / 2 + 1] = srx::fma2(d1, local[k / 2 + 1], i1);
+                    if (OUT) {
+                        h[k / 2] = srx::fma2(d0, h[k / 2], i0);
+                        h[k / 2 + 1] = srx::fma2(d1, h[k / 2 + 1], i1);
+                        const float4 cv = *reinterpret_cast<const float4*>(&S.cf[OUT ? f : 0][((k / 4) * L + p) * 4]);
+                        y2 = k ? srx::fma2(srx::pair(cv.x, cv.y), h[k / 2], y2) : srx::mul2(srx::pair(cv.x, cv.y), h[k / 2]);
+                        y2 = srx::fma2(srx::pair(cv.z, cv.w), h[k / 2 + 1], y2);
                     }
                 }
-                const bool mine = q * L + p < left;
-                if (MODE == kSums) {
-                    if (mine) total += (double)r[q];
-                } else {
-                    float o = exchange<L, SIDE>(y, p);
-                    o = fmaf(skip, u[q], o);
-                    if (pz) o *= srx::silu<EXACT>(z[q]);
-                    if (mine && there) *po = (T)o;
-                    po += dout;
-                }
+                const float2 v = srx::split(y2);
+                y[i] = v.x + v.y;
+            }
+            if (OUT) {
+                const float o = fmaf(skip, u, exchange<L, SIDE>(y, p)), gate = srx::silu<EXACT>((float)S.z[OUT ? half : 0][mine][col]);
+                S.out[OUT ? mine : 0][col] = (T)(gated ? o * gate : o);
             }
         }
-        if (at + PIECE < n) keep_piece(buffer ^ 1);
-        __syncthreads();
-        buffer ^= 1;
+        if ((at + kBlock) % kChunk == 0 || at + kBlock >= n) {
+            const Pair s2 = srx::pair(since, since);
+#pragma unroll
+            for (int k = 0; k < K / 2; ++k) {
+                const float2 v = S.carried[k][tid];
+                h[k] = srx::fma2(srx::exp2_exact(srx::mul2(s2, a2[k])), srx::pair(v.x, v.y), local[k]);
+                S.carried[k][tid] = srx::split(h[k]);
+                local[k] = srx::pair(0.0f, 0.0f);
+            }
+            total += (double)since;
+            since = 0.0f;
+        }
+        if (OUT) {
+            sync();
+            put(left);
+        }
     }
 
     float* to = MODE == kSums ? A.sums + (slot * A.channels + ch) * A.states : A.state_out && last ? A.state_out + ((int64_t)b * A.channels + ch) * A.states : nullptr;
@@ -223,16 +378,12 @@ __global__ void __launch_bounds__(kThreads) sr_scan_kernel(const __grid_constant
 #pragma unroll
         for (int k = 0; k < K; k += 2) {
             const int i = ((k / 4) * L + p) * 4 + k % 4;
-            const float2 v = srx::split(h[k / 2]);
+            const float2 v = S.carried[k / 2][tid];
             if (i < A.states) to[i] = v.x;
             if (i + 1 < A.states) to[i + 1] = v.y;
         }
     }
-    if (MODE == kSums) {
-#pragma unroll
-        for (int s = SIDE; s < 32; s *= 2) total += __shfl_xor_sync(0xFFFFFFFFu, total, s);
-        if (there && p == 0) A.steps[slot * A.channels + ch] = (float)total;
-    }
+    if (MODE == kSums && there && p == 0) A.steps[slot * A.channels + ch] = (float)total;
 }
 
 // The states that enter the segments, from their sums: one thread for a state of a channel of a sequence, over its segments.
@@ -246,11 +397,11 @@ __global__ void __launch_bounds__(128) sr_scan_join_kernel(const __grid_constant
     const int64_t i = (blockIdx.x - b * parts) * 128 + threadIdx.x;
     if (i >= per) return;
     const int64_t ch = i / A.states;
-    const float a2 = srx::kLog2e * A.a[i];
+    const float a2 = srx::decay_base2(A.a[i]);
     float h = A.state_in ? A.state_in[b * per + i] : 0.0f;
     float* at = A.sums + slot0 * per + i;
     const float* steps = A.steps + slot0 * A.channels + ch;
-    constexpr int AHEAD = 8;
+    constexpr int AHEAD = 16;
     for (int64_t s = 0; s < count; s += AHEAD) {
         float sum[AHEAD], step[AHEAD];
 #pragma unroll
@@ -263,7 +414,7 @@ __global__ void __launch_bounds__(128) sr_scan_join_kernel(const __grid_constant
         for (int k = 0; k < AHEAD; ++k) {
             if (s + k >= count) break;
             at[k * per] = h;
-            h = fmaf(srx::ex2(a2 * step[k]), h, sum[k]);
+            h = fmaf(srx::exp2_exact(a2 * step[k]), h, sum[k]);
         }
         at += AHEAD * per;
         steps += AHEAD * A.channels;
@@ -327,14 +478,14 @@ __global__ void __launch_bounds__(128) sr_scan_step_kernel(const __grid_constant
         }
         if (k == 0) {
 #pragma unroll
-            for (int s = 0; s < SEQ; ++s) r[s] = A.softplus ? srx::softplus(r[s] + bias) : r[s] + bias;
+            for (int s = 0; s < SEQ; ++s) r[s] = A.softplus ? srx::softplus<EXACT>(r[s] + bias) : r[s] + bias;
         }
 #pragma unroll
         for (int s = 0; s < SEQ; ++s) {
             const float x = r[s] * u[s];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                h[s][e] = fmaf(srx::ex2(r[s] * (srx::kLog2e * a[e])), h[s][e], x * bv[s][e]);
+                h[s][e] = fmaf(srx::exp2_exact(r[s] * srx::decay_base2(a[e])), h[s][e], x * bv[s][e]);
                 y[s] = fmaf(cv[s][e], h[s][e], y[s]);
             }
             if (in && b0 + s < A.batch) {
@@ -355,7 +506,7 @@ __global__ void __launch_bounds__(128) sr_scan_step_kernel(const __grid_constant
 
 // ------------------------------------------------------------------------------------------ launches
 template <typename F, typename... Args>
-cudaError_t start(F* kernel, int64_t blocks, int threads, cudaStream_t s, Args... args)
+cudaError_t start(F* kernel, int64_t blocks, int threads, int shared, cudaStream_t s, Args... args)
 {
     if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
     cudaLaunchAttribute at[1];
@@ -364,6 +515,7 @@ cudaError_t start(F* kernel, int64_t blocks, int threads, cudaStream_t s, Args..
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)shared;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
@@ -375,16 +527,52 @@ struct ScanCut {
     int held, lanes;
     int64_t segment, slots;                            // 0: whole sequences
 };
+// Cycles that `warps` warps, spread over all schedulers, take for a frame: one to a scheduler 365 (latency), four 227 each (special function units and issue slots);
+// measured for 16 states.
+int64_t cycles_of(int64_t warps, int64_t schedulers)
+{
+    constexpr int kOf[5] = {0, 365, 508, 708, 908};
+    const int64_t each = (warps + schedulers - 1) / schedulers;
+    return each / 4 * kOf[4] + kOf[each % 4];
+}
+// Whole sequences where their channels fill the schedulers; otherwise segments, whose sums cost 0.65 of their outputs, and two launches more.  Side by side: the number of
+// segments with the smallest estimate (16384 frames of 1024 channels, 16 states: one sequence whole WHOLE us, in segments SEGMENTS).  Packed: nobody here knows the
+// lengths; segments of as many frames as there are for each scheduler's warp, so that the longest sequence does not take longer than all of them, unless sequences are
+// so many that this is four times their mean length.
 ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
 {
     ScanCut c{};
     int padded = 4;
     while (padded < d->states) padded *= 2;
-    c.held = padded < 8 ? 4 : padded > 64 ? 16 : 8;
+    c.held = std::min(padded, 16);
     c.lanes = padded / c.held;
-    (void)packed;
-    (void)sms;
     c.slots = d->batch;
+    if (d->frames <= 2 * kChunk || !d->batch) return c;
+    const int64_t per = threads_of(c.lanes) / c.lanes, tiles = (d->channels / d->groups + per - 1) / per;
+    const int64_t warps = d->groups * tiles * (threads_of(c.lanes) / 32), schedulers = 4 * (int64_t)std::max(sms, 1);          // of a sequence
+    auto whole_chunks = [](int64_t frames) { return std::max<int64_t>((frames + kChunk - 1) / kChunk, 2) * kChunk; };
+    if (packed) {
+        const int64_t mean = d->frames / d->batch, even = d->frames * warps / (schedulers * 4);
+        if (even >= 4 * mean) return c;
+        c.segment = whole_chunks(even);
+        if (c.segment >= d->frames) {
+            c.segment = 0;
+            return c;
+        }
+        c.slots = d->frames / c.segment + d->batch;
+        return c;
+    }
+    int64_t best = d->frames * cycles_of(warps * d->batch, schedulers);
+    for (int64_t n = 2; n <= 512 && n * kChunk <= d->frames; n += (n + 7) / 8) {
+        const int64_t segment = whole_chunks((d->frames + n - 1) / n), count = segments_of(d->frames, segment);
+        if (count < 2) continue;
+        const int64_t cycles = segment * (cycles_of(warps * d->batch * count, schedulers) + cycles_of(warps * d->batch * (count - 1), schedulers) * 13 / 20) + 16000;
+        if (cycles < best) {
+            best = cycles;
+            c.segment = segment;
+            c.slots = d->batch * count;
+        }
+    }
     return c;
 }
 size_t cut_bytes(const sr_scan_desc* d, const ScanCut& c)
@@ -392,25 +580,48 @@ size_t cut_bytes(const sr_scan_desc* d, const ScanCut& c)
     return c.segment ? (size_t)c.slots * d->channels * ((size_t)d->states * 4 + 4) + 256 : 0;
 }
 
-template <typename T, int K, int L>
+template <typename T, int K, int L, int MODE, bool WIDE>
+cudaError_t launch_mode(const ScanArgs& A, int64_t grid, cudaStream_t s)
+{
+    static SrSharedLimit limit;
+    constexpr int bytes = (int)sizeof(ScanShared<T, K, L, threads_of(L), MODE != kSums>);
+    if (bytes > 48 << 10) {
+        const cudaError_t e = limit.raise(sr_scan_kernel<T, K, L, MODE, WIDE>, bytes);
+        if (e != cudaSuccess) return e;
+    }
+    return start(sr_scan_kernel<T, K, L, MODE, WIDE>, grid, threads_of(L), bytes, s, A);
+}
+template <typename T, int K, int L, bool WIDE>
 cudaError_t launch_scan(const ScanArgs& A, const ScanCut& c, cudaStream_t s)
 {
     const int64_t grid = c.slots * A.groups * A.tiles;
-    if (!c.segment) return start(sr_scan_kernel<T, K, L, kWhole>, grid, kThreads, s, A);
-    cudaError_t e = start(sr_scan_kernel<T, K, L, kSums>, grid, kThreads, s, A);
-    if (e == cudaSuccess) e = start(sr_scan_join_kernel, ((int64_t)A.channels * A.states + 127) / 128 * A.batch, 128, s, A);
-    if (e == cudaSuccess) e = start(sr_scan_kernel<T, K, L, kOutputs>, grid, kThreads, s, A);
+    if (!c.segment) return launch_mode<T, K, L, kWhole, WIDE>(A, grid, s);
+    cudaError_t e = launch_mode<T, K, L, kSums, WIDE>(A, grid, s);
+    if (e == cudaSuccess) e = start(sr_scan_join_kernel, ((int64_t)A.channels * A.states + 127) / 128 * A.batch, 128, 0, s, A);
+    if (e == cudaSuccess) e = launch_mode<T, K, L, kOutputs, WIDE>(A, grid, s);
     return e;
 }
-template <typename T>
+template <typename T, bool WIDE>
 cudaError_t launch_scan(const ScanArgs& A, const ScanCut& c, cudaStream_t s)
 {
-    if (c.held == 4) return launch_scan<T, 4, 1>(A, c, s);
-    if (c.held == 16) return launch_scan<T, 16, 8>(A, c, s);
-    if (c.lanes == 1) return launch_scan<T, 8, 1>(A, c, s);
-    if (c.lanes == 2) return launch_scan<T, 8, 2>(A, c, s);
-    if (c.lanes == 4) return launch_scan<T, 8, 4>(A, c, s);
-    return launch_scan<T, 8, 8>(A, c, s);
+    if (c.held == 4) return launch_scan<T, 4, 1, WIDE>(A, c, s);
+    if (c.held == 8) return c.lanes == 2 ? launch_scan<T, 8, 2, WIDE>(A, c, s) : launch_scan<T, 8, 1, WIDE>(A, c, s);
+    if (c.lanes == 1) return launch_scan<T, 16, 1, WIDE>(A, c, s);
+    if (c.lanes == 2) return launch_scan<T, 16, 2, WIDE>(A, c, s);
+    if (c.lanes == 4) return launch_scan<T, 16, 4, WIDE>(A, c, s);
+    return launch_scan<T, 16, 8, WIDE>(A, c, s);
+}
+// 16 bytes at a time where the rows of a tensor start on them.
+template <typename T>
+cudaError_t launch_scan(ScanArgs A, const ScanCut& c, cudaStream_t s)
+{
+    constexpr int vec = 16 / sizeof(T);
+    const bool one = A.offsets || A.batch < 2;         // (no strides between sequences)
+    auto fits = [&](const void* p, const sr_frame_strides& st) { return !((uintptr_t)p & 15) && (A.frames < 2 || st.frame % vec == 0) && (one || st.sequence % vec == 0); };
+    auto units = [&](const void* p, const sr_attention_strides& st) { return A.states % vec == 0 && fits(p, sr_frame_strides{st.frame, st.sequence}) && (A.groups < 2 || st.head % vec == 0); };
+    A.units = units(A.b, A.sb) && units(A.c, A.sc);
+    const bool wide = A.share % vec == 0 && fits(A.u, A.su) && fits(A.dt, A.sdt) && fits(A.z, A.sz) && fits(A.out, A.so);
+    return wide ? launch_scan<T, true>(A, c, s) : launch_scan<T, false>(A, c, s);
 }
 
 template <typename T, int VEC>
@@ -421,8 +632,8 @@ cudaError_t launch_step(const ScanArgs& A, cudaStream_t s)
     while (L < 32 && L < units) L *= 2;
     const int pieces = (units + L - 1) / L;
     const int64_t x = (A.channels + 128 / L - 1) / (128 / L);
-    if (A.batch >= 16 && VEC == 4) return start(sr_scan_step_kernel<T, VEC, 4>, x * ((A.batch + 3) / 4), 128, s, A, L, pieces);
-    return start(sr_scan_step_kernel<T, VEC, 1>, x * A.batch, 128, s, A, L, pieces);
+    if (A.batch >= 16 && VEC == 4) return start(sr_scan_step_kernel<T, VEC, 4>, x * ((A.batch + 3) / 4), 128, 0, s, A, L, pieces);
+    return start(sr_scan_step_kernel<T, VEC, 1>, x * A.batch, 128, 0, s, A, L, pieces);
 }
 template <typename T>
 cudaError_t launch_step(const ScanArgs& A, cudaStream_t s)
@@ -528,7 +739,7 @@ sr_status sr_selective_scan_run(const sr_scan_desc* d, const void* u, const void
     A.segment = cut.segment;
     A.sums = static_cast<float*>(workspace);
     A.steps = A.sums + cut.slots * d->channels * d->states;
-    const int per = kThreads / cut.lanes;
+    const int per = threads_of(cut.lanes) / cut.lanes;
     A.tiles = (A.share + per - 1) / per;
     const cudaError_t e = d->dtype == SR_DTYPE_F32 ? launch_scan<float>(A, cut, s) : launch_scan<__nv_bfloat16>(A, cut, s);
     return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
