@@ -33,11 +33,11 @@ struct ScanArgs {
     void* out;
     float* sums;                                       // [slot][channels][states]: states after a segment that none enter, then those that enter it
     float* steps;                                      // [slot][channels]: sum of r over a segment
-    int64_t frames, segment;                           // segment 0: whole sequences
+    int64_t frames, segment, whole;                    // segment 0: whole sequences; whole: packed sequences are not cut where none is longer
     int32_t batch, channels, states, groups, share, softplus, tiles;      // share: channels of a group; tiles: CTAs side by side over them
     sr_frame_strides su, sdt, sz, so;
     sr_attention_strides sb, sc;
-    bool units;                                        // b and c can be copied 16 bytes at a time
+    bool units, quads;                                 // b and c can be copied 16 bytes at a time; states and decays, too
 };
 
 constexpr int kBlock = 8;                              // frames of a stage
@@ -46,6 +46,12 @@ constexpr int kWarps = 16;                             // of an SM: 128 register
 enum { kWhole = 0, kSums = 1, kOutputs = 2 };          // whole sequences; sums of segments; outputs of segments, from the states that enter them
 // A block's threads share b and c, whose widening is the more to do the more states there are; fewer make the work of SMs more even.
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes < 4 ? 32 : 128; }
+
+// Frames of a segment of this run.
+__device__ __forceinline__ int64_t segment_of(const ScanArgs& A)
+{
+    return A.offsets && longest_span(A.offsets, A.frames, A.batch) <= A.whole ? A.whole : A.segment;
+}
 
 // Sum over the L threads of a channel, whose lanes are SIDE apart: thread p gets frame p's.
 template <int L, int SIDE>
@@ -190,10 +196,11 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     const int64_t slot = rest / A.groups;
     int b = (int)slot;
     int64_t seg = 0;
-    if (MODE != kWhole) find_slot(A.offsets, A.frames, A.batch, A.segment, slot, b, seg);
+    const int64_t segment = MODE == kWhole ? 0 : segment_of(A);
+    if (MODE != kWhole) find_slot(A.offsets, A.frames, A.batch, segment, slot, b, seg);
     if (b < 0) return;
     const FrameSpan span = frame_span(A.offsets, A.frames, b);
-    const int64_t t0 = MODE == kWhole ? 0 : seg * A.segment, n = MODE == kWhole ? span.n : min(A.segment, span.n - t0);
+    const int64_t t0 = seg * segment, n = MODE == kWhole ? span.n : min(segment, span.n - t0);
     const bool last = t0 + n >= span.n;
     if (MODE == kSums && last) return;                 // (nobody asks for them)
 
@@ -286,25 +293,33 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     static_assert(Wide::PER_ROW <= THREADS);
     const float bias = A.bias ? A.bias[ch] : 0.0f, skip = OUT && A.d ? A.d[ch] : 0.0f;
 
+    fetch(0, frames_from(0));
     // ---- the thread's states and decays; local: what the states are without those at the chunk's start
     Pair h[K / 2], local[K / 2], a2[K / 2];
+    auto four = [&](const float* of, int i) {          // of a channel's states; zeros behind the last one
+        if (A.quads) return i < A.states ? *reinterpret_cast<const float4*>(of + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        auto one = [&](int i) { return i < A.states ? of[i] : 0.0f; };
+        return make_float4(one(i), one(i + 1), one(i + 2), one(i + 3));
+    };
     {
-        const float* from = MODE == kWhole ? (A.state_in ? A.state_in + ((int64_t)b * A.channels + ch) * A.states : nullptr)
-                                           : MODE == kOutputs ? A.sums + (slot * A.channels + ch) * A.states : nullptr;
+        const int64_t entering = seg ? slot - 1 : slot + segments_of(span.n, segment) - 1;       // (see sr_scan_join_kernel)
+        const float* from = MODE == kSums ? nullptr : MODE == kOutputs && !(seg == 0 && last) ? A.sums + (entering * A.channels + ch) * A.states
+                                                    : A.state_in ? A.state_in + ((int64_t)b * A.channels + ch) * A.states : nullptr;
         const float* a = A.a + (int64_t)ch * A.states;
 #pragma unroll
-        for (int k = 0; k < K; k += 2) {
-            const int i = ((k / 4) * L + p) * 4 + k % 4;
-            const bool lo = i < A.states, hi = i + 1 < A.states;
-            a2[k / 2] = srx::pair(lo ? srx::decay_base2(a[i]) : 0.0f, hi ? srx::decay_base2(a[i + 1]) : 0.0f);
-            const float2 v = make_float2(from && lo ? from[i] : 0.0f, from && hi ? from[i + 1] : 0.0f);
-            S.carried[k / 2][tid] = v;
+        for (int k = 0; k < K; k += 4) {
+            const int i = ((k / 4) * L + p) * 4;
+            const float4 d = four(a, i), v = from ? four(from, i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            a2[k / 2] = srx::pair(srx::decay_base2(d.x), srx::decay_base2(d.y));
+            a2[k / 2 + 1] = srx::pair(srx::decay_base2(d.z), srx::decay_base2(d.w));
             h[k / 2] = srx::pair(v.x, v.y);
-            local[k / 2] = srx::pair(0.0f, 0.0f);
+            h[k / 2 + 1] = srx::pair(v.z, v.w);
+            S.carried[k / 2][tid] = make_float2(v.x, v.y);
+            S.carried[k / 2 + 1][tid] = make_float2(v.z, v.w);
+            local[k / 2] = local[k / 2 + 1] = srx::pair(0.0f, 0.0f);
         }
     }
 
-    fetch(0, frames_from(0));
     double total = 0.0;                                // of r
     float since = 0.0f;                                // of r, from the chunk's start on
     int half = 0;
@@ -376,48 +391,74 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     float* to = MODE == kSums ? A.sums + (slot * A.channels + ch) * A.states : A.state_out && last ? A.state_out + ((int64_t)b * A.channels + ch) * A.states : nullptr;
     if (to && there) {
 #pragma unroll
-        for (int k = 0; k < K; k += 2) {
-            const int i = ((k / 4) * L + p) * 4 + k % 4;
-            const float2 v = S.carried[k / 2][tid];
-            if (i < A.states) to[i] = v.x;
-            if (i + 1 < A.states) to[i + 1] = v.y;
+        for (int k = 0; k < K; k += 4) {
+            const int i = ((k / 4) * L + p) * 4;
+            const float2 v = S.carried[k / 2][tid], w = S.carried[k / 2 + 1][tid];
+            if (A.quads) {
+                if (i < A.states) *reinterpret_cast<float4*>(to + i) = make_float4(v.x, v.y, w.x, w.y);
+            } else {
+                if (i < A.states) to[i] = v.x;
+                if (i + 1 < A.states) to[i + 1] = v.y;
+                if (i + 2 < A.states) to[i + 2] = w.x;
+                if (i + 3 < A.states) to[i + 3] = w.y;
+            }
         }
     }
     if (MODE == kSums && there && p == 0) A.steps[slot * A.channels + ch] = (float)total;
 }
 
-// The states that enter the segments, from their sums: one thread for a state of a channel of a sequence, over its segments.
+// The states that enter the segments of sequences that have several, from their sums: one thread for a state of a channel of a sequence, over its segments.  What
+// enters a segment takes the place of the sum before it, what enters the first that of the last one's, which is not made (state_in may be state_out, which the last
+// segment writes).
 __global__ void __launch_bounds__(128) sr_scan_join_kernel(const __grid_constant__ ScanArgs A)
 {
     srx::let_successor_start();
     srx::wait_for_predecessor();
     const int64_t per = (int64_t)A.channels * A.states, parts = (per + 127) / 128;
     const int b = (int)(blockIdx.x / parts);
-    const int64_t slot0 = first_slot(A.offsets, A.frames, A.segment, b), count = segments_of(frame_span(A.offsets, A.frames, b).n, A.segment);
-    const int64_t i = (blockIdx.x - b * parts) * 128 + threadIdx.x;
+    const int64_t segment = segment_of(A), count = segments_of(frame_span(A.offsets, A.frames, b).n, segment);
+    if (count < 2) return;
+    const int64_t slot0 = first_slot(A.offsets, A.frames, segment, b), i = (blockIdx.x - b * parts) * 128 + threadIdx.x;
     if (i >= per) return;
-    const int64_t ch = i / A.states;
+    const int64_t ch = per <= 0xFFFFFFFF ? (uint32_t)i / (uint32_t)A.states : i / A.states;
     const float a2 = srx::decay_base2(A.a[i]);
     float h = A.state_in ? A.state_in[b * per + i] : 0.0f;
     float* at = A.sums + slot0 * per + i;
     const float* steps = A.steps + slot0 * A.channels + ch;
-    constexpr int AHEAD = 16;
-    for (int64_t s = 0; s < count; s += AHEAD) {
-        float sum[AHEAD], step[AHEAD];
+    at[(count - 1) * per] = h;
+    constexpr int AHEAD = 8;
+    float sum[AHEAD], step[AHEAD];
+    int64_t left = count - 1;                          // (the last segment's sums are not made)
+    for (; left >= AHEAD; left -= AHEAD) {
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {              // (the last segment's sums are not made)
-            const bool in = s + k < count - 1;
-            sum[k] = in ? at[k * per] : 0.0f;
-            step[k] = in ? steps[k * A.channels] : 0.0f;
+        for (int k = 0; k < AHEAD; ++k) {
+            sum[k] = at[k * per];
+            step[k] = steps[k * A.channels];
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            if (s + k >= count) break;
-            at[k * per] = h;
             h = fmaf(srx::exp2_exact(a2 * step[k]), h, sum[k]);
+            at[k * per] = h;
         }
         at += AHEAD * per;
         steps += AHEAD * A.channels;
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD - 1; ++k) {
+        if (k < left) {
+            sum[k] = at[k * per];
+            step[k] = steps[k * A.channels];
+        }
+    }
+#pragma unroll 1
+    for (int k = 0; k < left; ++k) {
+        h = fmaf(srx::exp2_exact(a2 * step[0]), h, sum[0]);
+        at[k * per] = h;
+#pragma unroll
+        for (int j = 0; j + 1 < AHEAD; ++j) {
+            sum[j] = sum[j + 1];
+            step[j] = step[j + 1];
+        }
     }
 }
 
@@ -525,7 +566,7 @@ cudaError_t start(F* kernel, int64_t blocks, int threads, int shared, cudaStream
 // How a run is cut.
 struct ScanCut {
     int held, lanes;
-    int64_t segment, slots;                            // 0: whole sequences
+    int64_t segment, slots, whole;                     // segment 0: whole sequences
 };
 // Cycles that `warps` warps, spread over all schedulers, take for a frame: one to a scheduler 365 (latency), four 227 each (special function units and issue slots);
 // measured for 16 states.
@@ -535,10 +576,10 @@ int64_t cycles_of(int64_t warps, int64_t schedulers)
     const int64_t each = (warps + schedulers - 1) / schedulers;
     return each / 4 * kOf[4] + kOf[each % 4];
 }
-// Whole sequences where their channels fill the schedulers; otherwise segments, whose sums cost 0.65 of their outputs, and two launches more.  Side by side: the number of
-// segments with the smallest estimate (16384 frames of 1024 channels, 16 states: one sequence whole WHOLE us, in segments SEGMENTS).  Packed: nobody here knows the
-// lengths; segments of as many frames as there are for each scheduler's warp, so that the longest sequence does not take longer than all of them, unless sequences are
-// so many that this is four times their mean length.
+// Whole sequences where their channels fill the schedulers; otherwise segments, whose sums cost 0.7 of their outputs, and two launches more.
+// Side by side: the number of segments with the smallest estimate.  Packed: only the GPU knows the lengths.  There are segments of a third of the frames that there are for each
+// scheduler's warp where some sequence has more than 1.75 times those, that is, would take longer than all of them in segments; else, as the kernels find, no
+// sequence is cut.
 ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
 {
     ScanCut c{};
@@ -552,13 +593,10 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
     const int64_t warps = d->groups * tiles * (threads_of(c.lanes) / 32), schedulers = 4 * (int64_t)std::max(sms, 1);          // of a sequence
     auto whole_chunks = [](int64_t frames) { return std::max<int64_t>((frames + kChunk - 1) / kChunk, 2) * kChunk; };
     if (packed) {
-        const int64_t mean = d->frames / d->batch, even = d->frames * warps / (schedulers * 4);
-        if (even >= 4 * mean) return c;
-        c.segment = whole_chunks(even);
-        if (c.segment >= d->frames) {
-            c.segment = 0;
-            return c;
-        }
+        const int64_t even = d->frames * warps / (schedulers * 4);
+        c.whole = whole_chunks(even * 7 / 4);
+        if (c.whole >= d->frames) return c;
+        c.segment = whole_chunks(even / 3);
         c.slots = d->frames / c.segment + d->batch;
         return c;
     }
@@ -566,7 +604,7 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
     for (int64_t n = 2; n <= 512 && n * kChunk <= d->frames; n += (n + 7) / 8) {
         const int64_t segment = whole_chunks((d->frames + n - 1) / n), count = segments_of(d->frames, segment);
         if (count < 2) continue;
-        const int64_t cycles = segment * (cycles_of(warps * d->batch * count, schedulers) + cycles_of(warps * d->batch * (count - 1), schedulers) * 13 / 20) + 16000;
+        const int64_t cycles = segment * (cycles_of(warps * d->batch * count, schedulers) + cycles_of(warps * d->batch * (count - 1), schedulers) * 7 / 10) + 16000;
         if (cycles < best) {
             best = cycles;
             c.segment = segment;
@@ -620,6 +658,7 @@ cudaError_t launch_scan(ScanArgs A, const ScanCut& c, cudaStream_t s)
     auto fits = [&](const void* p, const sr_frame_strides& st) { return !((uintptr_t)p & 15) && (A.frames < 2 || st.frame % vec == 0) && (one || st.sequence % vec == 0); };
     auto units = [&](const void* p, const sr_attention_strides& st) { return A.states % vec == 0 && fits(p, sr_frame_strides{st.frame, st.sequence}) && (A.groups < 2 || st.head % vec == 0); };
     A.units = units(A.b, A.sb) && units(A.c, A.sc);
+    A.quads = A.states % 4 == 0 && !(((uintptr_t)A.a | (uintptr_t)A.state_in | (uintptr_t)A.state_out) & 15);
     const bool wide = A.share % vec == 0 && fits(A.u, A.su) && fits(A.dt, A.sdt) && fits(A.z, A.sz) && fits(A.out, A.so);
     return wide ? launch_scan<T, true>(A, c, s) : launch_scan<T, false>(A, c, s);
 }
@@ -737,6 +776,7 @@ sr_status sr_selective_scan_run(const sr_scan_desc* d, const void* u, const void
     A.state_in = state_in;
     A.state_out = state_out;
     A.segment = cut.segment;
+    A.whole = cut.whole;
     A.sums = static_cast<float*>(workspace);
     A.steps = A.sums + cut.slots * d->channels * d->states;
     const int per = threads_of(cut.lanes) / cut.lanes;

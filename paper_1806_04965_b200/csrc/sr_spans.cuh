@@ -57,6 +57,16 @@ __device__ __forceinline__ void find_slot(const int64_t* offsets, int64_t frames
         before += __shfl_sync(0xFFFFFFFFu, sum, 31);
     }
 }
+// The frames of the longest sequence.  (All lanes of a warp.)
+__device__ __forceinline__ int64_t longest_span(const int64_t* offsets, int64_t frames, int batch)
+{
+    if (!offsets) return frames;
+    int64_t most = 0;
+    for (int i = threadIdx.x & 31; i < batch; i += 32) most = max(most, frame_span(offsets, frames, i).n);
+#pragma unroll
+    for (int d = 16; d; d /= 2) most = max(most, (int64_t)__shfl_xor_sync(0xFFFFFFFFu, most, d));
+    return most;
+}
 // The first slot of sequence b.  (All lanes of a warp.)
 __device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int64_t frames, int64_t segment, int b)
 {
