@@ -1,12 +1,13 @@
 // Causal convolution of every channel over the last frames: out[t, c] = act(bias[c] + sum_j weight[c, j] x[t - (W - 1) + j, c]).
 //
 // Bound by memory: x once, out once.  A thread has VEC neighbouring channels and goes over a segment of frames with the last W - 1 of them in registers, so that only
-// the W - 1 frames ahead of a segment are read twice; eight frames are loaded at a time.
+// the W - 1 frames ahead of a segment are read twice; eight frames are loaded at a time, and stay as they lie in memory until they are used.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/sr_rollout.h"
 #include "sr_operators.h"
@@ -29,30 +30,55 @@ struct ConvArgs {
     sr_frame_strides sx, so;
 };
 
-constexpr int kThreads = 128, kAhead = 8;
+constexpr int kThreads = 128, kRing = 3;
+// Frames that a thread loads at a time, and batches of them: in its ring in shared memory (16-byte units), or two in registers.
+__host__ __device__ constexpr int ahead_of(int bytes) { return bytes == 16 ? 4 : 8; }
 
+// The weights of a thread's channels.  VEC > 1: through shared memory, where a thread's units of 16 bytes lie an odd number of them from the next thread's; read straight from
+// global memory every load would touch as many lines as there are lanes (64 sequences of 128 frames, 4096 channels, four taps: 64 us).
 template <typename T, int VEC, int W>
 struct Taps {
+    static constexpr int UNITS = VEC * W / 4, STRIDE = UNITS | 1, SHARED = VEC > 2 ? kThreads * STRIDE : 1;
     float w[W][VEC], bias[VEC];
-    __device__ __forceinline__ Taps(const ConvArgs& A, int64_t c)
+    __device__ __forceinline__ void get(const ConvArgs& A, int64_t c0, float4* shared)          // c0: the block's first channel
     {
+        const int64_t c = c0 + (int64_t)threadIdx.x * VEC;
+        const bool there = c < A.channels;
+        if constexpr (VEC > 2) {
+            const int units = (int)min((int64_t)kThreads * UNITS, (A.channels - c0) * W / 4);      // (VEC > 2: the channels are a multiple of 4)
+            const float4* from = reinterpret_cast<const float4*>(A.weight + c0 * W);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            bias[e] = A.bias ? A.bias[c + e] : 0.0f;
+            for (int i = 0; i < UNITS; ++i) {
+                const int m = i * kThreads + threadIdx.x;
+                if (m < units) shared[m / UNITS * STRIDE + m % UNITS] = from[m];
+            }
+            __syncthreads();
+            float flat[VEC * W];
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[j][e] = A.weight[(c + e) * W + j];
+            for (int i = 0; i < UNITS; ++i) *reinterpret_cast<float4*>(&flat[4 * i]) = shared[threadIdx.x * STRIDE + i];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+#pragma unroll
+                for (int j = 0; j < W; ++j) w[j][e] = flat[e * W + j];
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+#pragma unroll
+                for (int j = 0; j < W; ++j) w[j][e] = there ? A.weight[(c + e) * W + j] : 0.0f;
         }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) bias[e] = there && A.bias ? A.bias[c + e] : 0.0f;
     }
-    // seen: W frames, oldest first
-    template <typename F>
-    __device__ __forceinline__ void apply(const ConvArgs& A, F seen, float (&y)[VEC]) const
+    // seen: the last W frames, oldest first
+    __device__ __forceinline__ void apply(bool act, const float (&seen)[W][VEC], float (&y)[VEC]) const
     {
         if constexpr (VEC > 1) {
 #pragma unroll
             for (int e = 0; e < VEC; e += 2) {
                 srx::Pair s = srx::pair(bias[e], bias[e + 1]);
 #pragma unroll
-                for (int j = 0; j < W; ++j) s = srx::fma2(srx::pair(w[j][e], w[j][e + 1]), srx::pair(seen(j)[e], seen(j)[e + 1]), s);
+                for (int j = 0; j < W; ++j) s = srx::fma2(srx::pair(w[j][e], w[j][e + 1]), srx::pair(seen[j][e], seen[j][e + 1]), s);
+                if (act) s = srx::silu<sizeof(T) == 4>(s);
                 const float2 v = srx::split(s);
                 y[e] = v.x;
                 y[e + 1] = v.y;
@@ -60,99 +86,177 @@ struct Taps {
         } else {
             y[0] = bias[0];
 #pragma unroll
-            for (int j = 0; j < W; ++j) y[0] = fmaf(w[j][0], seen(j)[0], y[0]);
-        }
-        if (A.act) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) y[e] = srx::silu<sizeof(T) == 4>(y[e]);
+            for (int j = 0; j < W; ++j) y[0] = fmaf(w[j][0], seen[j][0], y[0]);
+            if (act) y[0] = srx::silu<sizeof(T) == 4>(y[0]);
         }
     }
 };
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from)
+{
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(srx::smem_u32(to)), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(srx::smem_u32(to)), "l"(from), "n"(BYTES) : "memory");
+}
+// `next` becomes the last of W frames.
+template <typename T, int VEC, int W>
+__device__ __forceinline__ void see(float (&seen)[W][VEC], const srx::Few<T, VEC>& next)
+{
+#pragma unroll
+    for (int j = 0; j + 1 < W; ++j)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) seen[j][e] = seen[j + 1][e];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) seen[W - 1][e] = next[e];
+}
 
 template <typename T, int VEC, int W>
-__global__ void __launch_bounds__(kThreads) sr_conv_run_kernel(const __grid_constant__ ConvArgs A)
+__global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? 4 : 1) sr_conv_run_kernel(const __grid_constant__ ConvArgs A)
 {
+    using srx::Few;
+    constexpr int kAhead = ahead_of(VEC * (int)sizeof(T));
+    __shared__ float4 shared[Taps<T, VEC, W>::SHARED];
     srx::let_successor_start();
     srx::wait_for_predecessor();
     const int64_t slot = blockIdx.x / A.tiles;
     int b;
     int64_t seg;
     find_slot(A.offsets, A.frames, A.batch, A.segment, slot, b, seg);
-    const int64_t c = ((int64_t)(blockIdx.x % A.tiles) * kThreads + threadIdx.x) * VEC;
-    if (b < 0 || c >= A.channels) return;
+    if (b < 0) return;
+    const int64_t c0 = (int64_t)(blockIdx.x % A.tiles) * kThreads * VEC, c = c0 + threadIdx.x * VEC;
     const FrameSpan span = frame_span(A.offsets, A.frames, b);
     const int64_t t0 = seg * A.segment, n = min(A.segment, span.n - t0);
+    if (span.n == 0 && !A.state_out) return;
+    Taps<T, VEC, W> taps;
+    taps.get(A, c0, shared);
+    if (c >= A.channels) return;
     const T* x = static_cast<const T*>(A.x) + span.first * A.sx.frame + span.b * A.sx.sequence + c;
     T* out = static_cast<T*>(A.out) + (span.first + t0) * A.so.frame + span.b * A.so.sequence + c;
     const int64_t old = (int64_t)b * (W - 1) * A.channels + c;       // the sequence's state
-    auto frame = [&](int64_t t, float (&f)[VEC]) {     // one of the sequence's, or of its state's
+    auto frame = [&](int64_t t, Few<T, VEC>& f) {      // one of the sequence's, or of its state's
         if (t >= 0) {
-            srx::load_unit<T, VEC>(x + t * A.sx.frame, f);
+            f.get(x + t * A.sx.frame);
         } else if (A.state_in) {
-            srx::load_unit<T, VEC>(static_cast<const T*>(A.state_in) + old + (W - 1 + t) * A.channels, f);
+            f.get(static_cast<const T*>(A.state_in) + old + (W - 1 + t) * A.channels);
         } else {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = 0.0f;
+            for (int e = 0; e < Few<T, VEC>::WORDS; ++e) f.w[e] = 0;
         }
     };
-    const Taps<T, VEC, W> taps(A, c);
-    float seen[W - 1 + kAhead][VEC];
+    float seen[W][VEC] = {};
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) frame(t0 - (W - 1) + j, seen[j]);
+    for (int j = 0; j < W - 1; ++j) {
+        Few<T, VEC> f;
+        frame(t0 - (W - 1) + j, f);
+        see<T, VEC, W>(seen, f);
+    }
+    // kAhead frames at a time: of 16-byte units kRing - 1 times as many are on their way to places in shared memory that are the thread's own, of others as many in registers
+    constexpr bool ASYNC = VEC * sizeof(T) == 16;
+    constexpr int UNIT = VEC * (int)sizeof(T);
+    extern __shared__ __align__(16) uint8_t memory[];
+    uint8_t* mine = memory + threadIdx.x * UNIT;
+    Few<T, VEC> next[ASYNC ? 1 : kAhead], held[ASYNC ? 1 : kAhead];
     const T* px = x + t0 * A.sx.frame;
-    for (int64_t t = 0; t < n; t += kAhead) {
+    auto load = [&](int64_t t, int place) {            // the eight frames from t on
+        const int there = (int)min(n - t, (int64_t)kAhead);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (t + k < n) srx::load_unit<T, VEC>(px, seen[W - 1 + k]);
-            px += A.sx.frame;
+            if (k < there) {
+                if constexpr (ASYNC) copy_async<UNIT>(mine + (place * kAhead + k) * kThreads * UNIT, px + k * A.sx.frame);
+                else next[k].get(px + k * A.sx.frame);
+            }
         }
+        px += kAhead * A.sx.frame;
+        if (ASYNC) asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto work = [&](auto usual, int left, int place) { // usual: eight frames, with their activation
+        constexpr bool USUAL = decltype(usual)::value;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
+            Few<T, VEC> in;
+            if constexpr (ASYNC) in.get(reinterpret_cast<const T*>(mine + (place * kAhead + k) * kThreads * UNIT));
+            else in = held[k];
+            see<T, VEC, W>(seen, in);
             float y[VEC];
-            taps.apply(A, [&](int j) -> const float(&)[VEC] { return seen[k + j]; }, y);
-            if (t + k < n) srx::store_unit<T, VEC>(out, y);
-            out += A.so.frame;
+            taps.apply(USUAL || A.act, seen, y);
+            Few<T, VEC> o;
+            o.set(y);
+            if (USUAL || k < left) o.put(out + k * A.so.frame);
         }
+    };
+    constexpr int RING = ASYNC ? kRing : 1;
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j)
+    for (int i = 0; i < (ASYNC ? RING - 1 : 1); ++i) load(i * kAhead, i);
+    int place = 0;
+    for (int64_t t = 0; t < n; t += kAhead) {
+        if constexpr (!ASYNC) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) seen[j][e] = seen[j + kAhead][e];
+            for (int k = 0; k < kAhead; ++k) held[k] = next[k];
+            if (t + kAhead < n) load(t + kAhead, 0);
+        }
+        if constexpr (ASYNC) {
+            load(t + (RING - 1) * kAhead, place ? place - 1 : RING - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+        }
+        const int left = (int)min(n - t, (int64_t)kAhead);
+        if (left == kAhead && A.act) work(std::true_type{}, left, place);
+        else work(std::false_type{}, left, place);
+        out += kAhead * A.so.frame;
+        place = place + 1 == RING ? 0 : place + 1;
     }
     // The thread that has read the old state writes the new one, so that they may be the same: place i then holds what frame n - (W - 1) + i was, read from place n + i at
     // the earliest.
     if (seg == 0 && A.state_out) {
         T* to = static_cast<T*>(A.state_out) + old;
         for (int i = 0; i < W - 1; ++i) {
-            float f[VEC];
+            Few<T, VEC> f;
             frame(span.n - (W - 1) + i, f);
-            srx::store_unit<T, VEC>(to + (int64_t)i * A.channels, f);
+            f.put(to + (int64_t)i * A.channels);
         }
     }
 }
 
-template <typename T, int VEC, int W>
+// A thread goes over SEQ sequences with the same weights.
+template <typename T, int VEC, int W, int SEQ>
 __global__ void __launch_bounds__(kThreads) sr_conv_step_kernel(const __grid_constant__ ConvArgs A)
 {
+    using srx::Few;
+    __shared__ float4 shared[Taps<T, VEC, W>::SHARED];
     srx::let_successor_start();
     srx::wait_for_predecessor();
-    const int64_t b = blockIdx.x / A.tiles;
-    const int64_t c = ((int64_t)(blockIdx.x % A.tiles) * kThreads + threadIdx.x) * VEC;
-    if (c >= A.channels) return;
-    T* state = static_cast<T*>(A.state_out) + b * (W - 1) * A.channels + c;
-    float seen[W][VEC];
+    const int64_t b0 = (int64_t)(blockIdx.x / A.tiles) * SEQ;
+    const int64_t c0 = (int64_t)(blockIdx.x % A.tiles) * kThreads * VEC, c = c0 + threadIdx.x * VEC;
+    const bool there = c < A.channels;
+    Few<T, VEC> in[SEQ][W];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) srx::load_unit<T, VEC>(state + (int64_t)j * A.channels, seen[j]);
-    srx::load_unit<T, VEC>(static_cast<const T*>(A.x) + b * A.sx.sequence + c, seen[W - 1]);
-    const Taps<T, VEC, W> taps(A, c);
-    float y[VEC];
-    taps.apply(A, [&](int j) -> const float(&)[VEC] { return seen[j]; }, y);
-    srx::store_unit<T, VEC>(static_cast<T*>(A.out) + b * A.so.sequence + c, y);
+    for (int s = 0; s < SEQ; ++s) {
+        if (!there || b0 + s >= A.batch) continue;
+        const T* state = static_cast<const T*>(A.state_out) + (b0 + s) * (W - 1) * A.channels + c;
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) srx::store_unit<T, VEC>(state + (int64_t)j * A.channels, seen[j + 1]);
+        for (int j = 0; j < W - 1; ++j) in[s][j].get(state + (int64_t)j * A.channels);
+        in[s][W - 1].get(static_cast<const T*>(A.x) + (b0 + s) * A.sx.sequence + c);
+    }
+    Taps<T, VEC, W> taps;
+    taps.get(A, c0, shared);
+#pragma unroll
+    for (int s = 0; s < SEQ; ++s) {
+        if (!there || b0 + s >= A.batch) continue;
+        float y[VEC], seen[W][VEC];
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) seen[j][e] = in[s][j][e];
+        taps.apply(A.act, seen, y);
+        Few<T, VEC> o;
+        o.set(y);
+        o.put(static_cast<T*>(A.out) + (b0 + s) * A.so.sequence + c);
+        T* state = static_cast<T*>(A.state_out) + (b0 + s) * (W - 1) * A.channels + c;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) in[s][j + 1].put(state + (int64_t)j * A.channels);
+    }
 }
 
 template <typename F>
-cudaError_t start(F* kernel, int64_t blocks, ConvArgs A, cudaStream_t s)
+cudaError_t start(F* kernel, int64_t blocks, int shared, ConvArgs A, cudaStream_t s)
 {
     if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
     cudaLaunchAttribute at[1];
@@ -161,6 +265,7 @@ cudaError_t start(F* kernel, int64_t blocks, ConvArgs A, cudaStream_t s)
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)shared;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
@@ -170,11 +275,26 @@ cudaError_t start(F* kernel, int64_t blocks, ConvArgs A, cudaStream_t s)
 template <typename T, int VEC, int W>
 cudaError_t launch(ConvArgs A, bool step, cudaStream_t s)
 {
+    constexpr bool RUNS = VEC == 1 || VEC * sizeof(T) == 16, STEPS = VEC * sizeof(T) < 16;
     A.tiles = (int32_t)((A.channels + (int64_t)kThreads * VEC - 1) / (kThreads * VEC));
-    if (step) return start(sr_conv_step_kernel<T, VEC, W>, (int64_t)A.batch * A.tiles, A, s);
-    A.segment = 32;
-    const int64_t slots = A.offsets ? A.frames / A.segment + A.batch : A.batch * segments_of(A.frames, A.segment);
-    return start(sr_conv_run_kernel<T, VEC, W>, slots * A.tiles, A, s);
+    const int sms = sr_device_sms();
+    if constexpr (STEPS) {
+        if (step) {
+            if (A.batch >= 32) return start(sr_conv_step_kernel<T, VEC, W, 4>, (A.batch + 3) / 4 * (int64_t)A.tiles, 0, A, s);
+            return start(sr_conv_step_kernel<T, VEC, W, 1>, (int64_t)A.batch * A.tiles, 0, A, s);
+        }
+    }
+    if constexpr (RUNS) {
+        // as long segments as leave three blocks to an SM (64 sequences of 128 frames, 4096 channels: 29.9 us with 64 frames, 30.2 with 32, 31.3 with 16)
+        A.segment = 64;
+        while (A.segment > 8 && (A.offsets ? A.frames / A.segment : A.batch * segments_of(A.frames, A.segment)) * A.tiles < 3 * sms) A.segment /= 2;
+        const int64_t slots = A.offsets ? A.frames / A.segment + A.batch : A.batch * segments_of(A.frames, A.segment);
+        constexpr int bytes = VEC * sizeof(T) == 16 ? kRing * ahead_of(16) * kThreads * VEC * (int)sizeof(T) : 0;
+        static SrSharedLimit limit;
+        const cudaError_t e = bytes ? limit.raise(sr_conv_run_kernel<T, VEC, W>, bytes) : cudaSuccess;
+        return e == cudaSuccess ? start(sr_conv_run_kernel<T, VEC, W>, slots * A.tiles, bytes, A, s) : e;
+    }
+    return cudaErrorInvalidValue;
 }
 template <typename T, int VEC>
 cudaError_t launch(const ConvArgs& A, int width, bool step, cudaStream_t s)
@@ -190,16 +310,23 @@ cudaError_t launch(const ConvArgs& A, int width, bool step, cudaStream_t s)
         default: return launch<T, VEC, 8>(A, step, s);
     }
 }
-// 16 bytes at a time where every row of every tensor allows it.
+// 16 bytes at a time where every row of every tensor allows it.  Single frames: 8 bytes, for more threads (256 sequences of 4096 channels 3.9 us, with 16 bytes 5.3), and where there
+// are few sequences pairs of bf16 (one of 4096 channels 1.7, with 16 bytes 2.2).
 template <typename T>
 cudaError_t launch(const ConvArgs& A, int width, bool step, cudaStream_t s)
 {
     constexpr int vec = 16 / sizeof(T);
-    auto fits = [&](const void* p, const sr_frame_strides& st) {
-        return !((uintptr_t)p & 15) && (step || st.frame % vec == 0) && (A.offsets || A.batch < 2 || st.sequence % vec == 0);
+    auto fits = [&](int vec) {
+        auto lies = [&](const void* p, const sr_frame_strides& st) {
+            return (uintptr_t)p % (vec * sizeof(T)) == 0 && (step || st.frame % vec == 0) && (A.offsets || A.batch < 2 || st.sequence % vec == 0);
+        };
+        return A.channels % vec == 0 && lies(A.x, A.sx) && lies(A.out, A.so) && ((uintptr_t)A.state_in | (uintptr_t)A.state_out) % (vec * sizeof(T)) == 0;
     };
-    const bool wide = A.channels % vec == 0 && fits(A.x, A.sx) && fits(A.out, A.so) && !(((uintptr_t)A.state_in | (uintptr_t)A.state_out) & 15);
-    return wide ? launch<T, vec>(A, width, step, s) : launch<T, 1>(A, width, step, s);
+    if constexpr (sizeof(T) == 2) {
+        if (step && (int64_t)A.batch * A.channels <= (int64_t)sr_device_sms() * kThreads * 4 && fits(2)) return launch<T, 2>(A, width, step, s);
+    }
+    if (step && !((uintptr_t)A.weight & 15) && fits(vec / 2)) return launch<T, vec / 2>(A, width, step, s);
+    return !step && !((uintptr_t)A.weight & 15) && fits(vec) ? launch<T, vec>(A, width, step, s) : launch<T, 1>(A, width, step, s);
 }
 
 sr_status check(const sr_conv_desc* d)

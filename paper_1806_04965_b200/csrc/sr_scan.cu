@@ -17,11 +17,13 @@
 #include "sr_operators.h"
 #include "sr_pair.cuh"
 #include "sr_ptx.cuh"
+#include "sr_row.cuh"
 #include "sr_selective.cuh"
 #include "sr_spans.cuh"
 
 namespace {
 
+using srx::Few;
 using srx::Pair;
 
 struct ScanArgs {
@@ -77,64 +79,6 @@ __device__ __forceinline__ void copy_4(void* dst, const void* src)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(srx::smem_u32(dst)), "l"(src) : "memory");
 }
-// N elements, side by side, at once.
-template <typename T, int N>
-struct Few {
-    static constexpr int BYTES = N * (int)sizeof(T), WORDS = BYTES < 4 ? 1 : BYTES / 4;
-    uint32_t w[WORDS];
-    __device__ __forceinline__ void get(const T* p)
-    {
-        if constexpr (BYTES >= 16) {
-#pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) {
-                const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-            }
-        } else if constexpr (BYTES == 8) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            w[0] = v.x; w[1] = v.y;
-        } else if constexpr (BYTES == 4) {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
-        } else {
-            w[0] = *reinterpret_cast<const uint16_t*>(p);
-        }
-    }
-    __device__ __forceinline__ void put(T* p) const
-    {
-        if constexpr (BYTES >= 16) {
-#pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-        } else if constexpr (BYTES == 8) {
-            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-        } else if constexpr (BYTES == 4) {
-            *reinterpret_cast<uint32_t*>(p) = w[0];
-        } else {
-            *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
-        }
-    }
-    __device__ __forceinline__ float operator[](int i) const
-    {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-        else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
-    }
-    __device__ __forceinline__ void set(const float (&f)[N])
-    {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
-        } else if constexpr (N == 1) {
-            w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(f[0]));
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; i += 2) w[i / 2] = srx::round_bf16(srx::pair(f[i], f[i + 1]));
-        }
-    }
-    __device__ __forceinline__ void put_one(T* p, int i) const
-    {
-        if constexpr (sizeof(T) == 4) *p = __uint_as_float(w[i]);
-        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[i / 2] >> (i & 1 ? 16 : 0));
-    }
-};
 // A stage's rows of a tensor, `cols` of COLS elements in each, into shared memory, by THREADS threads: 16 bytes at a time (UNITS), or an element.  What is behind the last
 // column or frame stays what it was.
 template <typename T, int COLS, int THREADS, bool UNITS>

@@ -83,12 +83,11 @@ __device__ __forceinline__ Pair softplus(Pair x)
     return fma2(s, p, pair(fmaxf(v.x, 0.0f), fmaxf(v.y, 0.0f)));
 }
 
-// 1 / (1 + exp(-x)); EXACT: to the last bits of 32, else to more than those of bf16
+// 1 / (1 + exp(-x)); EXACT: to the last two bits of 32 (the approximate reciprocal is off by one), else to more than those of bf16
 template <bool EXACT>
 __device__ __forceinline__ float sigmoid(float x)
 {
-    if constexpr (EXACT) return 1.0f / (1.0f + expf(-x));
-    return reciprocal(1.0f + ex2(-kLog2e * x));
+    return reciprocal(1.0f + (EXACT ? expf(-x) : ex2(-kLog2e * x)));
 }
 template <bool EXACT>
 __device__ __forceinline__ float silu(float x)
@@ -96,14 +95,19 @@ __device__ __forceinline__ float silu(float x)
     return x * sigmoid<EXACT>(x);
 }
 template <bool EXACT>
-__device__ __forceinline__ Pair silu(Pair x)
+__device__ __forceinline__ Pair sigmoid(Pair x)
 {
     if constexpr (EXACT) {
         const float2 v = split(x);
-        return pair(silu<true>(v.x), silu<true>(v.y));
+        return pair(sigmoid<true>(v.x), sigmoid<true>(v.y));
     }
     const float2 e = split(mul2(x, pair(-kLog2e, -kLog2e))), n = split(add2(pair(ex2(e.x), ex2(e.y)), pair(1.0f, 1.0f)));
-    return mul2(x, pair(reciprocal(n.x), reciprocal(n.y)));
+    return pair(reciprocal(n.x), reciprocal(n.y));
+}
+template <bool EXACT>
+__device__ __forceinline__ Pair silu(Pair x)
+{
+    return mul2(x, sigmoid<EXACT>(x));
 }
 
 }  // namespace srx
