@@ -407,104 +407,141 @@ __global__ void __launch_bounds__(128) sr_scan_join_kernel(const __grid_constant
 }
 
 // ------------------------------------------------------------------------------------------ single frames
-// One frame: the states are read and written once.  L threads have VEC states each of a channel (more where L is 32 already), the warp's other threads the next
-// channels; a thread goes over SEQ sequences with the same decays.
-template <typename T, int VEC, int SEQ>
-__global__ void __launch_bounds__(128) sr_scan_step_kernel(const __grid_constant__ ScanArgs A, int L, int pieces)
+// One frame: the states are read and written once.  L threads have VEC states each of a channel (more where L is 32 already: PIECES), the warp's other threads the next
+// channels; a block goes over `per` sequences with the same decays, the loads of AHEAD of them under way.  UNITS: b and c can be read VEC at a time.  Bound by memory where there are
+// many sequences, but not far from the issue of its instructions, of which most are for a channel and not for a state: hence eight states to a thread.
+template <typename T, int VEC, int PIECES, int AHEAD, bool UNITS>
+__global__ void __launch_bounds__(128, 4) sr_scan_step_kernel(const __grid_constant__ ScanArgs A, int L, int per)
 {
     constexpr bool EXACT = sizeof(T) == 4;
     srx::let_successor_start();
     srx::wait_for_predecessor();
-    const int p = threadIdx.x % L;
-    const int parts = (A.channels + 128 / L - 1) / (128 / L);
-    const int64_t ch0 = (int64_t)(blockIdx.x % parts) * (128 / L) + threadIdx.x / L;
+    const int p = threadIdx.x % L;                     // (L: a power of two)
+    const int64_t ch0 = (int64_t)blockIdx.x * (128 / L) + threadIdx.x / L;
     const bool there = ch0 < A.channels;
-    const int64_t ch = there ? ch0 : 0;
-    const int g = (int)(ch / A.share);
-    const int b0 = (int)(blockIdx.x / parts) * SEQ;
-    const float bias = A.bias ? A.bias[ch] : 0.0f, skip = A.d ? A.d[ch] : 0.0f;
-    float u[SEQ], r[SEQ], z[SEQ], y[SEQ];
-#pragma unroll
-    for (int s = 0; s < SEQ; ++s) {
-        const int64_t b = min(b0 + s, A.batch - 1);
-        u[s] = (float)static_cast<const T*>(A.u)[b * A.su.sequence + ch];
-        r[s] = (float)static_cast<const T*>(A.dt)[b * A.sdt.sequence + ch];
-        z[s] = A.z ? (float)static_cast<const T*>(A.z)[b * A.sz.sequence + ch] : 0.0f;
-        y[s] = 0.0f;
-    }
-    for (int k = 0; k < pieces; ++k) {
-        const int i = (k * L + p) * VEC;
-        const bool in = there && i < A.states;         // (VEC 4: the states are a multiple of 4)
-        float a[VEC], h[SEQ][VEC], bv[SEQ][VEC], cv[SEQ][VEC];
-        if constexpr (VEC == 4) {
-            const float4 v = in ? *reinterpret_cast<const float4*>(A.a + ch * A.states + i) : make_float4(0, 0, 0, 0);
-            a[0] = v.x; a[1] = v.y; a[2] = v.z; a[3] = v.w;
+    const int ch = there ? (int)ch0 : 0, g = A.groups > 1 ? ch / A.share : 0, b0 = (int)blockIdx.y * per, seqs = min(A.batch - b0, per);
+    const int64_t apart = (int64_t)A.channels * A.states;
+    const T* pu = static_cast<const T*>(A.u) + b0 * A.su.sequence + ch;
+    const T* pdt = static_cast<const T*>(A.dt) + b0 * A.sdt.sequence + ch;
+    const T* pz = A.z ? static_cast<const T*>(A.z) + b0 * A.sz.sequence + ch : nullptr;
+    const T* pb = static_cast<const T*>(A.b) + b0 * A.sb.sequence + g * A.sb.head + p * VEC;
+    const T* pc = static_cast<const T*>(A.c) + b0 * A.sc.sequence + g * A.sc.head + p * VEC;
+    const float* from = A.state_out + b0 * apart + (int64_t)ch * A.states + p * VEC;
+    float* to = A.state_out + b0 * apart + (int64_t)ch * A.states + p * VEC;
+    T* out = static_cast<T*>(A.out) + b0 * A.so.sequence + ch;
+    auto is = [&](int k) { return there && (k * L + p) * VEC < A.states; };         // (VEC 4, 8: the states are a multiple of it)
+    struct Item {
+        T u, dt, z;
+        Few<float, VEC> h[PIECES];
+        Few<T, VEC> b[PIECES], c[PIECES];
+    } items[AHEAD];
+    auto get = [&](Few<T, VEC>& v, const T* of) {
+        if constexpr (UNITS || VEC == 1) {
+            v.get(of);
         } else {
-            a[0] = in ? A.a[ch * A.states + i] : 0.0f;
+            float f[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = (float)of[e];
+            v.set(f);
         }
+    };
+    auto load = [&](Item& item) {
+        item.u = *pu;
+        item.dt = *pdt;
+        if (pz) item.z = *pz;
 #pragma unroll
-        for (int s = 0; s < SEQ; ++s) {
-            const bool is = in && b0 + s < A.batch;
-            const int64_t b = min(b0 + s, A.batch - 1);
-            const float* state = A.state_out + (b * A.channels + ch) * A.states + i;
-            if constexpr (VEC == 4) {
-                const float4 v = is ? *reinterpret_cast<const float4*>(state) : make_float4(0, 0, 0, 0);
-                h[s][0] = v.x; h[s][1] = v.y; h[s][2] = v.z; h[s][3] = v.w;
-            } else {
-                h[s][0] = is ? state[0] : 0.0f;
-            }
-            const T* pb = static_cast<const T*>(A.b) + b * A.sb.sequence + g * A.sb.head + i;
-            const T* pc = static_cast<const T*>(A.c) + b * A.sc.sequence + g * A.sc.head + i;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                bv[s][e] = is ? (float)pb[e] : 0.0f;
-                cv[s][e] = is ? (float)pc[e] : 0.0f;
-            }
+        for (int k = 0; k < PIECES; ++k) {
+            if (!is(k)) continue;
+            item.h[k].get(from + k * L * VEC);
+            get(item.b[k], pb + k * L * VEC);
+            get(item.c[k], pc + k * L * VEC);
         }
-        if (k == 0) {
+        pu += A.su.sequence;
+        pdt += A.sdt.sequence;
+        if (pz) pz += A.sz.sequence;
+        pb += A.sb.sequence;
+        pc += A.sc.sequence;
+        from += apart;
+    };
 #pragma unroll
-            for (int s = 0; s < SEQ; ++s) r[s] = A.softplus ? srx::softplus<EXACT>(r[s] + bias) : r[s] + bias;
-        }
+    for (int j = 0; j < AHEAD; ++j)
+        if (j < seqs) load(items[j]);
+    const float bias = A.bias ? A.bias[ch] : 0.0f, skip = A.d ? A.d[ch] : 0.0f;
+    float a2[PIECES][VEC];
 #pragma unroll
-        for (int s = 0; s < SEQ; ++s) {
-            const float x = r[s] * u[s];
+    for (int k = 0; k < PIECES; ++k) {
+        Few<float, VEC> a = {};
+        if (is(k)) a.get(A.a + (int64_t)ch * A.states + (k * L + p) * VEC);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                h[s][e] = fmaf(srx::exp2_exact(r[s] * srx::decay_base2(a[e])), h[s][e], x * bv[s][e]);
-                y[s] = fmaf(cv[s][e], h[s][e], y[s]);
-            }
-            if (in && b0 + s < A.batch) {
-                float* state = A.state_out + ((int64_t)(b0 + s) * A.channels + ch) * A.states + i;
-                if constexpr (VEC == 4) *reinterpret_cast<float4*>(state) = make_float4(h[s][0], h[s][1], h[s][2], h[s][3]);
-                else state[0] = h[s][0];
-            }
-        }
+        for (int e = 0; e < VEC; ++e) a2[k][e] = srx::decay_base2(a[e]);
     }
+    auto work = [&](const Item& item) {
+        const float s = (float)item.dt + bias, r = A.softplus ? srx::softplus<EXACT>(s) : s, u = (float)item.u, x = r * u;
+        float y = 0.0f;
 #pragma unroll
-    for (int s = 0; s < SEQ; ++s) {
-        for (int d = 1; d < L; d *= 2) y[s] += __shfl_xor_sync(0xFFFFFFFFu, y[s], d);
-        float o = fmaf(skip, u[s], y[s]);
-        if (A.z) o *= srx::silu<EXACT>(z[s]);
-        if (there && p == 0 && b0 + s < A.batch) static_cast<T*>(A.out)[(int64_t)(b0 + s) * A.so.sequence + ch] = (T)o;
+        for (int k = 0; k < PIECES; ++k) {
+            if (!is(k)) continue;
+            float h[VEC];
+            if constexpr (VEC > 1) {
+                Pair sum = srx::pair(0.0f, 0.0f);
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const Pair decay = srx::exp2_exact(srx::mul2(srx::pair(r, r), srx::pair(a2[k][e], a2[k][e + 1])));
+                    const Pair v = srx::fma2(decay, srx::pair(item.h[k][e], item.h[k][e + 1]), srx::mul2(srx::pair(x, x), srx::pair(item.b[k][e], item.b[k][e + 1])));
+                    sum = srx::fma2(srx::pair(item.c[k][e], item.c[k][e + 1]), v, sum);
+                    const float2 f = srx::split(v);
+                    h[e] = f.x;
+                    h[e + 1] = f.y;
+                }
+                const float2 f = srx::split(sum);
+                y += f.x + f.y;
+            } else {
+                h[0] = fmaf(srx::exp2_exact(r * a2[k][0]), item.h[k][0], x * item.b[k][0]);
+                y = fmaf(item.c[k][0], h[0], y);
+            }
+            Few<float, VEC> o;
+            o.set(h);
+            o.put(to + k * L * VEC);
+        }
+        to += apart;
+#pragma unroll 1
+        for (int d = 1; d < L; d *= 2) y += __shfl_xor_sync(0xFFFFFFFFu, y, d);
+        float o = fmaf(skip, u, y);
+        if (pz) o *= srx::silu<EXACT>((float)item.z);
+        if (p == 0 && there) *out = (T)o;
+        out += A.so.sequence;
+    };
+#pragma unroll 1
+    for (int s = 0; s < seqs; s += AHEAD) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (s + j >= seqs) break;
+            work(items[j]);
+            if (s + j + AHEAD < seqs) load(items[j]);
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------------ launches
 template <typename F, typename... Args>
-cudaError_t start(F* kernel, int64_t blocks, int threads, int shared, cudaStream_t s, Args... args)
+cudaError_t start(F* kernel, dim3 grid, int threads, int shared, cudaStream_t s, Args... args)
 {
-    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)shared;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename F, typename... Args>
+cudaError_t start(F* kernel, int64_t blocks, int threads, int shared, cudaStream_t s, Args... args)
+{
+    return blocks > 0x7FFFFFFF ? cudaErrorInvalidValue : start(kernel, dim3((unsigned)blocks), threads, shared, s, args...);
 }
 
 // How a run is cut.
@@ -607,21 +644,32 @@ cudaError_t launch_scan(ScanArgs A, const ScanCut& c, cudaStream_t s)
     return wide ? launch_scan<T, true>(A, c, s) : launch_scan<T, false>(A, c, s);
 }
 
-template <typename T, int VEC>
-cudaError_t launch_step(const ScanArgs& A, cudaStream_t s)
+template <typename T, int VEC, int PIECES, int AHEAD, bool UNITS>
+cudaError_t launch_step(const ScanArgs& A, int per, cudaStream_t s)
 {
     const int units = (A.states + VEC - 1) / VEC;
     int L = 1;
     while (L < 32 && L < units) L *= 2;
-    const int pieces = (units + L - 1) / L;
-    const int64_t x = (A.channels + 128 / L - 1) / (128 / L);
-    if (A.batch >= 16 && VEC == 4) return start(sr_scan_step_kernel<T, VEC, 4>, x * ((A.batch + 3) / 4), 128, 0, s, A, L, pieces);
-    return start(sr_scan_step_kernel<T, VEC, 1>, x * A.batch, 128, 0, s, A, L, pieces);
+    const int64_t parts = ((int64_t)A.channels + 128 / L - 1) / (128 / L);
+    per = std::max(per, (A.batch + 65534) / 65535);
+    return start(sr_scan_step_kernel<T, VEC, PIECES, AHEAD, UNITS>, dim3((unsigned)parts, (unsigned)((A.batch + per - 1) / per)), 128, 0, s, A, L, per);
 }
 template <typename T>
 cudaError_t launch_step(const ScanArgs& A, cudaStream_t s)
 {
-    return A.states % 4 == 0 && !((uintptr_t)A.state_out & 15) && !((uintptr_t)A.a & 15) ? launch_step<T, 4>(A, s) : launch_step<T, 1>(A, s);
+    auto units = [&](int vec) {
+        auto lies = [&](const void* p, const sr_attention_strides& st) {
+            return (uintptr_t)p % std::min<size_t>(16, vec * sizeof(T)) == 0 && (A.batch < 2 || st.sequence % vec == 0) && (A.groups < 2 || st.head % vec == 0);
+        };
+        return lies(A.b, A.sb) && lies(A.c, A.sc);
+    };
+    // 256 sequences of 4096 channels with 16 states: 28.1 us (5.1 TB/s); with the loads of one sequence ahead 30.3, with four states to a thread and four sequences at once 45
+    constexpr int AHEAD = sizeof(T) == 2 ? 3 : 2;
+    const int per = std::max(1, std::min(16, A.batch / 16));
+    if (A.states % 4 || ((uintptr_t)A.state_out & 15) || ((uintptr_t)A.a & 15))
+        return A.states <= 32 ? launch_step<T, 1, 1, AHEAD, false>(A, per, s) : launch_step<T, 1, 4, 1, false>(A, per, s);
+    if (A.batch >= 16 && A.states % 8 == 0 && units(8)) return launch_step<T, 8, 1, AHEAD, true>(A, per, s);
+    return units(4) ? launch_step<T, 4, 1, AHEAD, true>(A, per, s) : launch_step<T, 4, 1, AHEAD, false>(A, per, s);
 }
 
 // ------------------------------------------------------------------------------------------ checks
