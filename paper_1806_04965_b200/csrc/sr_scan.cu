@@ -35,7 +35,7 @@ struct ScanArgs {
     void* out;
     float* sums;                                       // [slot][channels][states]: states after a segment that none enter, then those that enter it
     float* steps;                                      // [slot][channels]: sum of r over a segment
-    int64_t frames, segment, whole;                    // segment 0: whole sequences; whole: packed sequences are not cut where none is longer
+    int64_t frames, segment, whole, count;             // segment 0: whole sequences; whole: packed sequences are not cut where none is longer; count: segments of each of others
     int32_t batch, channels, states, groups, share, softplus, tiles;      // share: channels of a group; tiles: CTAs side by side over them
     sr_frame_strides su, sdt, sz, so;
     sr_attention_strides sb, sc;
@@ -83,34 +83,32 @@ __device__ __forceinline__ void copy_4(void* dst, const void* src)
 // column or frame stays what it was.
 template <typename T, int COLS, int THREADS, bool UNITS>
 struct Rows {
-    static constexpr int UNIT = UNITS ? 16 / (int)sizeof(T) : 1, PER_ROW = COLS / UNIT > 0 ? COLS / UNIT : 1, COPIES = (kBlock * PER_ROW + THREADS - 1) / THREADS;
-    __device__ __forceinline__ static int frame(int e, int tid) { return (e * THREADS + tid) / PER_ROW; }
-    __device__ __forceinline__ static int col(int tid) { return tid % PER_ROW * UNIT; }       // (of all its copies)
-    static_assert(THREADS % PER_ROW == 0 || PER_ROW % THREADS == 0);
-    // from: the thread's first row and column
+    static constexpr int UNIT = UNITS ? 16 / (int)sizeof(T) : 1, PER_ROW = COLS / UNIT > 0 ? COLS / UNIT : 1;
+    static constexpr int AT_ONCE = THREADS / PER_ROW, COPIES = AT_ONCE ? (kBlock + AT_ONCE - 1) / (AT_ONCE ? AT_ONCE : 1) : kBlock * (PER_ROW / THREADS);
+    static_assert(AT_ONCE || PER_ROW % THREADS == 0);
+    // The thread's first place; its copy e; whether that is one of `left` rows' and `cols` columns'.
+    __device__ __forceinline__ static int frame(int e, int tid) { return AT_ONCE ? e * AT_ONCE + tid / PER_ROW : e / (PER_ROW / THREADS ? PER_ROW / THREADS : 1); }
+    __device__ __forceinline__ static int col(int e, int tid)
+    {
+        return (AT_ONCE ? tid % PER_ROW : e % (PER_ROW / THREADS ? PER_ROW / THREADS : 1) * THREADS + tid) * UNIT;
+    }
+    __device__ __forceinline__ static bool there(int e, int tid, int cols, int left)
+    {
+        return (!AT_ONCE || THREADS % PER_ROW == 0 || tid < AT_ONCE * PER_ROW) && (kBlock % (AT_ONCE ? AT_ONCE : 1) == 0 || frame(e, tid) < kBlock) && frame(e, tid) < left && col(e, tid) < cols;
+    }
+    __device__ __forceinline__ static int64_t start(int tid, int64_t stride) { return frame(0, tid) * stride + col(0, tid); }
+    __device__ __forceinline__ static int64_t away(int e, int tid, int64_t stride) { return (frame(e, tid) - frame(0, tid)) * stride + (col(e, tid) - col(0, tid)); }
+    // from: the thread's first place
     __device__ __forceinline__ static void copy(T (*to)[COLS], const T* from, int64_t stride, int cols, int left, int tid)
     {
-        if constexpr (PER_ROW <= THREADS) {
-            if (col(tid) >= cols) return;
 #pragma unroll
-            for (int e = 0; e < COPIES; ++e) {
-                const int f = frame(e, tid);
-                if (f < left) one(&to[f][col(tid)], from + e * (THREADS / PER_ROW) * stride);
-            }
-        } else {
-#pragma unroll
-            for (int f = 0; f < kBlock; ++f)
-#pragma unroll
-                for (int c = 0; c < PER_ROW; c += THREADS)
-                    if (f < left && (c + tid) * UNIT < cols) one(&to[f][(c + tid) * UNIT], from + f * stride + c * UNIT);
+        for (int e = 0; e < COPIES; ++e) {
+            if (!there(e, tid, cols, left)) continue;
+            T* place = &to[frame(e, tid)][col(e, tid)];
+            if constexpr (UNITS) copy_16(place, from + away(e, tid, stride));
+            else if constexpr (sizeof(T) == 4) copy_4(place, from + away(e, tid, stride));
+            else *place = from[away(e, tid, stride)];
         }
-    }
-    __device__ __forceinline__ static int64_t start(int tid, int64_t stride) { return PER_ROW <= THREADS ? frame(0, tid) * stride + col(tid) : tid * UNIT; }
-    __device__ __forceinline__ static void one(T* to, const T* from)
-    {
-        if constexpr (UNITS) copy_16(to, from);
-        else if constexpr (sizeof(T) == 4) copy_4(to, from);
-        else *to = *from;
     }
 };
 
@@ -141,8 +139,15 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     int b = (int)slot;
     int64_t seg = 0;
     const int64_t segment = MODE == kWhole ? 0 : segment_of(A);
-    if (MODE != kWhole) find_slot(A.offsets, A.frames, A.batch, segment, slot, b, seg);
-    if (b < 0) return;
+    if (MODE != kWhole) {
+        if (A.offsets) {
+            find_slot(A.offsets, A.frames, A.batch, segment, slot, b, seg);
+            if (b < 0) return;
+        } else {
+            b = (int)((uint32_t)slot / (uint32_t)A.count);         // (there are not more slots than blocks)
+            seg = slot - b * A.count;
+        }
+    }
     const FrameSpan span = frame_span(A.offsets, A.frames, b);
     const int64_t t0 = seg * segment, n = MODE == kWhole ? span.n : min(segment, span.n - t0);
     const bool last = t0 + n >= span.n;
@@ -162,8 +167,8 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     // ---- copies
     using Wide = Rows<T, CHANNELS, THREADS, WIDE>;
     using Some = Rows<T, NP, THREADS, false>;
-    using Units = Rows<T, NP, THREADS, true>;
-    constexpr bool CAN = NP * sizeof(T) >= 16;         // rows of b and c in whole units
+    using Units = Rows<T, NP, THREADS, NP * sizeof(T) % 16 == 0>;
+    constexpr bool CAN = NP * sizeof(T) % 16 == 0;     // rows of b and c in whole units
     const T* gu = static_cast<const T*>(A.u) + first * A.su.frame + span.b * A.su.sequence + ch0 + Wide::start(tid, A.su.frame);
     const T* gdt = static_cast<const T*>(A.dt) + first * A.sdt.frame + span.b * A.sdt.sequence + ch0 + Wide::start(tid, A.sdt.frame);
     const T* gz = gated ? static_cast<const T*>(A.z) + first * A.sz.frame + span.b * A.sz.sequence + ch0 + Wide::start(tid, A.sz.frame) : nullptr;
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     };
 
     auto widen = [&](int half, int left) {             // b and c as floats: a thread's neighbouring states, all of a frame; zeros behind the last frame and state
-        constexpr int PART = kBlock * NP > THREADS ? (kBlock * NP / THREADS < 8 ? kBlock * NP / THREADS : 8) : 1, PER = NP / PART;
+        constexpr int MOST = kBlock * NP / THREADS, PART = MOST >= 8 && NP % 8 == 0 ? 8 : MOST > 2 && NP % 4 == 0 ? 4 : MOST == 2 ? 2 : 1, PER = NP / PART;
 #pragma unroll
         for (int i = tid; i < kBlock * PER; i += THREADS) {
             const int f = i / PER, c = i % PER * PART;
@@ -220,21 +225,16 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     };
     T* go = OUT ? static_cast<T*>(A.out) + first * A.so.frame + span.b * A.so.sequence + ch0 + Wide::start(tid, A.so.frame) : nullptr;
     auto put = [&](int left) {                         // a stage's outputs
-        if constexpr (Wide::PER_ROW <= THREADS) {
-            if (Wide::col(tid) < channels)
 #pragma unroll
-                for (int e = 0; e < Wide::COPIES; ++e) {
-                    const int f = Wide::frame(e, tid);
-                    T* to = go + e * (THREADS / Wide::PER_ROW) * A.so.frame;
-                    if (f < left) {
-                        if constexpr (WIDE) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&S.out[OUT ? f : 0][Wide::col(tid)]);
-                        else *to = S.out[OUT ? f : 0][Wide::col(tid)];
-                    }
-                }
+        for (int e = 0; e < Wide::COPIES; ++e) {
+            if (!Wide::there(e, tid, channels, left)) continue;
+            T* to = go + Wide::away(e, tid, A.so.frame);
+            const T* place = &S.out[OUT ? Wide::frame(e, tid) : 0][Wide::col(e, tid)];
+            if constexpr (WIDE) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(place);
+            else *to = *place;
         }
         go += kBlock * A.so.frame;
     };
-    static_assert(Wide::PER_ROW <= THREADS);
     const float bias = A.bias ? A.bias[ch] : 0.0f, skip = OUT && A.d ? A.d[ch] : 0.0f;
 
     fetch(0, frames_from(0));
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
         return make_float4(one(i), one(i + 1), one(i + 2), one(i + 3));
     };
     {
-        const int64_t entering = seg ? slot - 1 : slot + segments_of(span.n, segment) - 1;       // (see sr_scan_join_kernel)
+        const int64_t entering = seg ? slot - 1 : slot + (A.offsets ? segments_of(span.n, segment) : A.count) - 1;       // (see sr_scan_join_kernel)
         const float* from = MODE == kSums ? nullptr : MODE == kOutputs && !(seg == 0 && last) ? A.sums + (entering * A.channels + ch) * A.states
                                                     : A.state_in ? A.state_in + ((int64_t)b * A.channels + ch) * A.states : nullptr;
         const float* a = A.a + (int64_t)ch * A.states;
@@ -351,57 +351,55 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     if (MODE == kSums && there && p == 0) A.steps[slot * A.channels + ch] = (float)total;
 }
 
-// The states that enter the segments of sequences that have several, from their sums: one thread for a state of a channel of a sequence, over its segments.  What
-// enters a segment takes the place of the sum before it, what enters the first that of the last one's, which is not made (state_in may be state_out, which the last
-// segment writes).
-__global__ void __launch_bounds__(128) sr_scan_join_kernel(const __grid_constant__ ScanArgs A)
+// The states that enter the segments of sequences that have several, from their sums, one thread for a state of a channel.  What enters a segment takes the place of the sum before it,
+// what enters the first that of the last one's, which is not made (state_in may be state_out, which the last segment writes).  Bound by the latency of a load for every eight segments;
+// warps that share a state's segments took longer (24 us instead of 5 for 16 segments of 66660 states, 40 instead of 64 for 512 of 16384).
+constexpr int kJoinThreads = 128, kJoinAhead = 8;
+__global__ void __launch_bounds__(kJoinThreads) sr_scan_join_kernel(const __grid_constant__ ScanArgs A)
 {
+    __shared__ int64_t count_of, slot0_of;
     srx::let_successor_start();
     srx::wait_for_predecessor();
-    const int64_t per = (int64_t)A.channels * A.states, parts = (per + 127) / 128;
-    const int b = (int)(blockIdx.x / parts);
-    const int64_t segment = segment_of(A), count = segments_of(frame_span(A.offsets, A.frames, b).n, segment);
-    if (count < 2) return;
-    const int64_t slot0 = first_slot(A.offsets, A.frames, segment, b), i = (blockIdx.x - b * parts) * 128 + threadIdx.x;
-    if (i >= per) return;
+    const int64_t per = (int64_t)A.channels * A.states, mine = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x, i = min(mine, per - 1);
     const int64_t ch = per <= 0xFFFFFFFF ? (uint32_t)i / (uint32_t)A.states : i / A.states;
     const float a2 = srx::decay_base2(A.a[i]);
-    float h = A.state_in ? A.state_in[b * per + i] : 0.0f;
-    float* at = A.sums + slot0 * per + i;
-    const float* steps = A.steps + slot0 * A.channels + ch;
-    at[(count - 1) * per] = h;
-    constexpr int AHEAD = 8;
-    float sum[AHEAD], step[AHEAD];
-    int64_t left = count - 1;                          // (the last segment's sums are not made)
-    for (; left >= AHEAD; left -= AHEAD) {
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            sum[k] = at[k * per];
-            step[k] = steps[k * A.channels];
+    for (int b = blockIdx.y; b < A.batch; b += gridDim.y) {
+        if (A.offsets) {
+            if (threadIdx.x < 32) {
+                const int64_t segment = segment_of(A), n = segments_of(frame_span(A.offsets, A.frames, b).n, segment), slot0 = first_slot(A.offsets, A.frames, segment, b);
+                if (threadIdx.x == 0) {
+                    count_of = n;
+                    slot0_of = slot0;
+                }
+            }
+            __syncthreads();
         }
+        const int64_t count = A.offsets ? count_of : A.count, slot0 = A.offsets ? slot0_of : b * A.count;
+        if (A.offsets) __syncthreads();
+        if (count < 2) continue;
+        float h = A.state_in ? A.state_in[b * per + i] : 0.0f;
+        float* at = A.sums + slot0 * per + i;
+        const float* steps = A.steps + slot0 * A.channels + ch;
+        if (mine < per) at[(count - 1) * per] = h;
+        for (int64_t s = 0; s < count - 1; s += kJoinAhead) {      // (the last segment's sums are not made)
+            const int left = (int)min(count - 1 - s, (int64_t)kJoinAhead);
+            float sum[kJoinAhead], step[kJoinAhead];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            h = fmaf(srx::exp2_exact(a2 * step[k]), h, sum[k]);
-            at[k * per] = h;
-        }
-        at += AHEAD * per;
-        steps += AHEAD * A.channels;
-    }
+            for (int k = 0; k < kJoinAhead; ++k) {
+                if (k < left) {
+                    sum[k] = at[k * per];
+                    step[k] = steps[k * A.channels];
+                }
+            }
 #pragma unroll
-    for (int k = 0; k < AHEAD - 1; ++k) {
-        if (k < left) {
-            sum[k] = at[k * per];
-            step[k] = steps[k * A.channels];
-        }
-    }
-#pragma unroll 1
-    for (int k = 0; k < left; ++k) {
-        h = fmaf(srx::exp2_exact(a2 * step[0]), h, sum[0]);
-        at[k * per] = h;
-#pragma unroll
-        for (int j = 0; j + 1 < AHEAD; ++j) {
-            sum[j] = sum[j + 1];
-            step[j] = step[j + 1];
+            for (int k = 0; k < kJoinAhead; ++k) {
+                if (k < left) {
+                    h = fmaf(srx::exp2_exact(a2 * step[k]), h, sum[k]);
+                    if (mine < per) at[k * per] = h;
+                }
+            }
+            at += kJoinAhead * per;
+            steps += kJoinAhead * A.channels;
         }
     }
 }
@@ -523,12 +521,13 @@ __global__ void __launch_bounds__(128, 4) sr_scan_step_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------------ launches
+// early: while the kernel before drains.
 template <typename F, typename... Args>
-cudaError_t start(F* kernel, dim3 grid, int threads, int shared, cudaStream_t s, Args... args)
+cudaError_t start(F* kernel, bool early, dim3 grid, int threads, int shared, cudaStream_t s, Args... args)
 {
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
@@ -539,9 +538,9 @@ cudaError_t start(F* kernel, dim3 grid, int threads, int shared, cudaStream_t s,
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 template <typename F, typename... Args>
-cudaError_t start(F* kernel, int64_t blocks, int threads, int shared, cudaStream_t s, Args... args)
+cudaError_t start(F* kernel, bool early, int64_t blocks, int threads, int shared, cudaStream_t s, Args... args)
 {
-    return blocks > 0x7FFFFFFF ? cudaErrorInvalidValue : start(kernel, dim3((unsigned)blocks), threads, shared, s, args...);
+    return blocks > 0x7FFFFFFF ? cudaErrorInvalidValue : start(kernel, early, dim3((unsigned)blocks), threads, shared, s, args...);
 }
 
 // How a run is cut.
@@ -549,11 +548,12 @@ struct ScanCut {
     int held, lanes;
     int64_t segment, slots, whole;                     // segment 0: whole sequences
 };
-// Cycles that `warps` warps, spread over all schedulers, take for a frame: one to a scheduler 365 (latency), four 227 each (special function units and issue slots);
-// measured for 16 states.
+// Cycles that cutting costs besides: two launches, a load's latency for every eight segments, and the segments' states, which are written, joined and read (16 bytes each).
+int64_t joining(const sr_scan_desc* d, int64_t count) { return 16000 + count / 8 * 2000 + d->batch * count * d->channels / 200 * d->states; }
+// Cycles that `warps` warps, spread over all schedulers, take for a frame; measured for 16 states in bf16 (fp32: 1.5 times as many).
 int64_t cycles_of(int64_t warps, int64_t schedulers)
 {
-    constexpr int kOf[5] = {0, 365, 508, 708, 908};
+    constexpr int kOf[5] = {0, 427, 545, 705, 880};
     const int64_t each = (warps + schedulers - 1) / schedulers;
     return each / 4 * kOf[4] + kOf[each % 4];
 }
@@ -568,11 +568,12 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
     while (padded < d->states) padded *= 2;
     c.held = std::min(padded, 16);
     c.lanes = padded / c.held;
+    if (c.held == 16 && c.lanes <= 2 && d->states <= 12 * c.lanes) c.held = 12;
     c.slots = d->batch;
-    if (d->frames <= 2 * kChunk || !d->batch) return c;
+    if (d->frames <= kChunk || !d->batch) return c;
     const int64_t per = threads_of(c.lanes) / c.lanes, tiles = (d->channels / d->groups + per - 1) / per;
     const int64_t warps = d->groups * tiles * (threads_of(c.lanes) / 32), schedulers = 4 * (int64_t)std::max(sms, 1);          // of a sequence
-    auto whole_chunks = [](int64_t frames) { return std::max<int64_t>((frames + kChunk - 1) / kChunk, 2) * kChunk; };
+    auto whole_chunks = [](int64_t frames) { return std::max<int64_t>((frames + kChunk - 1) / kChunk, 1) * kChunk; };
     if (packed) {
         const int64_t even = d->frames * warps / (schedulers * 4);
         c.whole = whole_chunks(even * 7 / 4);
@@ -582,10 +583,9 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
         return c;
     }
     int64_t best = d->frames * cycles_of(warps * d->batch, schedulers);
-    for (int64_t n = 2; n <= 512 && n * kChunk <= d->frames; n += (n + 7) / 8) {
-        const int64_t segment = whole_chunks((d->frames + n - 1) / n), count = segments_of(d->frames, segment);
-        if (count < 2) continue;
-        const int64_t cycles = segment * (cycles_of(warps * d->batch * count, schedulers) + cycles_of(warps * d->batch * (count - 1), schedulers) * 7 / 10) + 16000;
+    for (int64_t chunks = 1; chunks * kChunk < d->frames; chunks += (chunks + 7) / 8) {
+        const int64_t segment = chunks * kChunk, count = segments_of(d->frames, segment);
+        const int64_t cycles = segment * (cycles_of(warps * d->batch * count, schedulers) + cycles_of(warps * d->batch * (count - 1), schedulers) * 7 / 10) + joining(d, count);
         if (cycles < best) {
             best = cycles;
             c.segment = segment;
@@ -608,7 +608,10 @@ cudaError_t launch_mode(const ScanArgs& A, int64_t grid, cudaStream_t s)
         const cudaError_t e = limit.raise(sr_scan_kernel<T, K, L, MODE, WIDE>, bytes);
         if (e != cudaSuccess) return e;
     }
-    return start(sr_scan_kernel<T, K, L, MODE, WIDE>, grid, threads_of(L), bytes, s, A);
+    // Blocks that come while others drain go where those have left room: unless they nearly fill the SMs anyway some of these get more than their part, and the time is theirs (512 frames of
+    // 16 sequences, 2048 channels: 196 us, one after the other 150).
+    const int64_t most = (int64_t)sr_device_sms() * kWarps / (threads_of(L) / 32) * 3 / 4;
+    return start(sr_scan_kernel<T, K, L, MODE, WIDE>, grid >= most || grid <= sr_device_sms(), grid, threads_of(L), bytes, s, A);
 }
 template <typename T, int K, int L, bool WIDE>
 cudaError_t launch_scan(const ScanArgs& A, const ScanCut& c, cudaStream_t s)
@@ -616,7 +619,9 @@ cudaError_t launch_scan(const ScanArgs& A, const ScanCut& c, cudaStream_t s)
     const int64_t grid = c.slots * A.groups * A.tiles;
     if (!c.segment) return launch_mode<T, K, L, kWhole, WIDE>(A, grid, s);
     cudaError_t e = launch_mode<T, K, L, kSums, WIDE>(A, grid, s);
-    if (e == cudaSuccess) e = start(sr_scan_join_kernel, ((int64_t)A.channels * A.states + 127) / 128 * A.batch, 128, 0, s, A);
+    const int64_t blocks = ((int64_t)A.channels * A.states + kJoinThreads - 1) / kJoinThreads;
+    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    if (e == cudaSuccess) e = start(sr_scan_join_kernel, true, dim3((unsigned)blocks, (unsigned)std::min(A.batch, 65535)), kJoinThreads, 0, s, A);
     if (e == cudaSuccess) e = launch_mode<T, K, L, kOutputs, WIDE>(A, grid, s);
     return e;
 }
@@ -624,7 +629,8 @@ template <typename T, bool WIDE>
 cudaError_t launch_scan(const ScanArgs& A, const ScanCut& c, cudaStream_t s)
 {
     if (c.held == 4) return launch_scan<T, 4, 1, WIDE>(A, c, s);
-    if (c.held == 8) return c.lanes == 2 ? launch_scan<T, 8, 2, WIDE>(A, c, s) : launch_scan<T, 8, 1, WIDE>(A, c, s);
+    if (c.held == 8) return launch_scan<T, 8, 1, WIDE>(A, c, s);
+    if (c.held == 12) return c.lanes == 1 ? launch_scan<T, 12, 1, WIDE>(A, c, s) : launch_scan<T, 12, 2, WIDE>(A, c, s);
     if (c.lanes == 1) return launch_scan<T, 16, 1, WIDE>(A, c, s);
     if (c.lanes == 2) return launch_scan<T, 16, 2, WIDE>(A, c, s);
     if (c.lanes == 4) return launch_scan<T, 16, 4, WIDE>(A, c, s);
@@ -652,7 +658,7 @@ cudaError_t launch_step(const ScanArgs& A, int per, cudaStream_t s)
     while (L < 32 && L < units) L *= 2;
     const int64_t parts = ((int64_t)A.channels + 128 / L - 1) / (128 / L);
     per = std::max(per, (A.batch + 65534) / 65535);
-    return start(sr_scan_step_kernel<T, VEC, PIECES, AHEAD, UNITS>, dim3((unsigned)parts, (unsigned)((A.batch + per - 1) / per)), 128, 0, s, A, L, per);
+    return start(sr_scan_step_kernel<T, VEC, PIECES, AHEAD, UNITS>, true, dim3((unsigned)parts, (unsigned)((A.batch + per - 1) / per)), 128, 0, s, A, L, per);
 }
 template <typename T>
 cudaError_t launch_step(const ScanArgs& A, cudaStream_t s)
@@ -769,6 +775,7 @@ sr_status sr_selective_scan_run(const sr_scan_desc* d, const void* u, const void
     A.state_out = state_out;
     A.segment = cut.segment;
     A.whole = cut.whole;
+    A.count = cut.segment ? segments_of(d->frames, cut.segment) : 1;
     A.sums = static_cast<float*>(workspace);
     A.steps = A.sums + cut.slots * d->channels * d->states;
     const int per = threads_of(cut.lanes) / cut.lanes;
