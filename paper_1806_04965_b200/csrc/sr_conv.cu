@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? 4 : 1) sr_co
     const int64_t slot = blockIdx.x / A.tiles;
     int b;
     int64_t seg;
-    find_slot(A.offsets, A.frames, A.batch, A.segment, slot, b, seg);
+    if (A.offsets) packed_slot(A.offsets, A.frames, A.batch, A.segment, slot, b, seg);
+    else find_slot(nullptr, A.frames, A.batch, A.segment, slot, b, seg);
     if (b < 0) return;
     const int64_t c0 = (int64_t)(blockIdx.x % A.tiles) * kThreads * VEC, c = c0 + threadIdx.x * VEC;
     const FrameSpan span = frame_span(A.offsets, A.frames, b);
@@ -334,6 +335,7 @@ sr_status check(const sr_conv_desc* d)
     if (!d || (d->dtype != SR_DTYPE_F32 && d->dtype != SR_DTYPE_BF16) || d->batch < 0 || d->channels < 1 || d->width < 1 || d->frames < 0 || (d->act != 0 && d->act != 1) ||
         d->x.frame < 0 || d->x.sequence < 0 || d->out.frame < 0 || d->out.sequence < 0)
         return SR_ERR_INVALID_ARG;
+    if ((double)d->frames * d->channels > 0x1p45 || (double)d->batch * d->channels * d->width > 0x1p45) return SR_ERR_INVALID_ARG;          // (no memory holds them)
     return d->width > 8 ? SR_ERR_UNSUPPORTED : SR_OK;
 }
 bool aligned(const void* p, int dtype) { return !((uintptr_t)p & (dtype == SR_DTYPE_F32 ? 3 : 1)); }

@@ -11,6 +11,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "../../include/sr_rollout.h"
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     const int64_t segment = MODE == kWhole ? 0 : segment_of(A);
     if (MODE != kWhole) {
         if (A.offsets) {
-            find_slot(A.offsets, A.frames, A.batch, segment, slot, b, seg);
+            packed_slot(A.offsets, A.frames, A.batch, segment, slot, b, seg);
             if (b < 0) return;
         } else {
             b = (int)((uint32_t)slot / (uint32_t)A.count);         // (there are not more slots than blocks)
@@ -366,7 +367,7 @@ __global__ void __launch_bounds__(kJoinThreads) sr_scan_join_kernel(const __grid
     for (int b = blockIdx.y; b < A.batch; b += gridDim.y) {
         if (A.offsets) {
             if (threadIdx.x < 32) {
-                const int64_t segment = segment_of(A), n = segments_of(frame_span(A.offsets, A.frames, b).n, segment), slot0 = first_slot(A.offsets, A.frames, segment, b);
+                const int64_t segment = segment_of(A), n = segments_of(frame_span(A.offsets, A.frames, b).n, segment), slot0 = packed_first(A.offsets, A.frames, segment, b);
                 if (threadIdx.x == 0) {
                     count_of = n;
                     slot0_of = slot0;
@@ -549,13 +550,13 @@ struct ScanCut {
     int64_t segment, slots, whole;                     // segment 0: whole sequences
 };
 // Cycles that cutting costs besides: two launches, a load's latency for every eight segments, and the segments' states, which are written, joined and read (16 bytes each).
-int64_t joining(const sr_scan_desc* d, int64_t count) { return 16000 + count / 8 * 2000 + d->batch * count * d->channels / 200 * d->states; }
+double joining(const sr_scan_desc* d, int64_t count) { return 16000.0 + count / 8 * 2000.0 + (double)d->batch * count * d->channels * d->states / 200; }
 // Cycles that `warps` warps, spread over all schedulers, take for a frame; measured for 16 states in bf16 (fp32: 1.5 times as many).
-int64_t cycles_of(int64_t warps, int64_t schedulers)
+double cycles_of(double warps, int64_t schedulers)
 {
-    constexpr int kOf[5] = {0, 427, 545, 705, 880};
-    const int64_t each = (warps + schedulers - 1) / schedulers;
-    return each / 4 * kOf[4] + kOf[each % 4];
+    constexpr double kOf[5] = {0, 427, 545, 705, 880};
+    const double each = std::ceil(warps / schedulers), rounds = std::floor(each / 4);
+    return rounds * kOf[4] + kOf[(int)(each - 4 * rounds)];
 }
 // Whole sequences where their channels fill the schedulers; otherwise segments, whose sums cost 0.7 of their outputs, and two launches more.
 // Side by side: the number of segments with the smallest estimate.  Packed: only the GPU knows the lengths.  There are segments of a third of the frames that there are for each
@@ -575,17 +576,18 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
     const int64_t warps = d->groups * tiles * (threads_of(c.lanes) / 32), schedulers = 4 * (int64_t)std::max(sms, 1);          // of a sequence
     auto whole_chunks = [](int64_t frames) { return std::max<int64_t>((frames + kChunk - 1) / kChunk, 1) * kChunk; };
     if (packed) {
-        const int64_t even = d->frames * warps / (schedulers * 4);
+        const int64_t even = (int64_t)std::min((double)d->frames * warps / (schedulers * 4), 1e12);
         c.whole = whole_chunks(even * 7 / 4);
         if (c.whole >= d->frames) return c;
         c.segment = whole_chunks(even / 3);
         c.slots = d->frames / c.segment + d->batch;
         return c;
     }
-    int64_t best = d->frames * cycles_of(warps * d->batch, schedulers);
-    for (int64_t chunks = 1; chunks * kChunk < d->frames; chunks += (chunks + 7) / 8) {
+    auto cycles_for = [&](int64_t frames, int64_t count) { return frames * cycles_of((double)warps * d->batch * count, schedulers); };
+    double best = cycles_for(d->frames, 1);
+    for (int64_t chunks = 1; chunks * kChunk < d->frames; chunks += (chunks + 3) / 4) {
         const int64_t segment = chunks * kChunk, count = segments_of(d->frames, segment);
-        const int64_t cycles = segment * (cycles_of(warps * d->batch * count, schedulers) + cycles_of(warps * d->batch * (count - 1), schedulers) * 7 / 10) + joining(d, count);
+        const double cycles = cycles_for(segment, count) + 0.7 * cycles_for(segment, count - 1) + joining(d, count);
         if (cycles < best) {
             best = cycles;
             c.segment = segment;
@@ -689,6 +691,7 @@ sr_status check(const sr_scan_desc* d)
         !fits(d->c))
         return SR_ERR_INVALID_ARG;
     if (d->states > 128) return SR_ERR_UNSUPPORTED;
+    if ((double)d->frames * d->channels > 0x1p45 || (double)d->batch * d->channels * d->states > 0x1p45) return SR_ERR_INVALID_ARG;          // (no memory holds them)
     return SR_OK;
 }
 bool aligned(const void* p, int dtype) { return !((uintptr_t)p & (dtype == SR_DTYPE_F32 ? 3 : 1)); }
@@ -779,7 +782,7 @@ sr_status sr_selective_scan_run(const sr_scan_desc* d, const void* u, const void
     A.sums = static_cast<float*>(workspace);
     A.steps = A.sums + cut.slots * d->channels * d->states;
     const int per = threads_of(cut.lanes) / cut.lanes;
-    A.tiles = (A.share + per - 1) / per;
+    A.tiles = (A.share - 1) / per + 1;
     const cudaError_t e = d->dtype == SR_DTYPE_F32 ? launch_scan<float>(A, cut, s) : launch_scan<__nv_bfloat16>(A, cut, s);
     return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
 }

@@ -62,10 +62,43 @@ __device__ __forceinline__ int64_t longest_span(const int64_t* offsets, int64_t 
 {
     if (!offsets) return frames;
     int64_t most = 0;
+#pragma unroll 8
     for (int i = threadIdx.x & 31; i < batch; i += 32) most = max(most, frame_span(offsets, frames, i).n);
 #pragma unroll
     for (int d = 16; d; d /= 2) most = max(most, (int64_t)__shfl_xor_sync(0xFFFFFFFFu, most, d));
     return most;
+}
+// Packed sequences, slots that need no sum over the sequences before: sequence b has those from offsets[b] / segment + b on, as many as its segments at least, and all of them are
+// frames / segment + batch.
+__device__ __forceinline__ int64_t packed_first(const int64_t* offsets, int64_t frames, int64_t segment, int b)
+{
+    const int64_t o = min(max(offsets[b], (int64_t)0), frames);
+    return (((uint64_t)o | (uint64_t)segment) >> 32 ? o / segment : (int64_t)((uint32_t)o / (uint32_t)segment)) + b;
+}
+// The sequence (-1: none) and segment of such a slot: a search in which every lane looks at one place.  (All lanes of a warp.)
+__device__ __forceinline__ void packed_slot(const int64_t* offsets, int64_t frames, int batch, int64_t segment, int64_t slot, int& b, int64_t& seg)
+{
+    int lo = 0, n = batch;
+    seg = 0;
+    for (;;) {
+        const int step = (n + 31) / 32, at = (threadIdx.x & 31) * step;
+        const bool here = at < n;
+        const int64_t first = here ? packed_first(offsets, frames, segment, lo + at) : 0;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, here && first <= slot);
+        if (!who) {
+            b = -1;
+            return;
+        }
+        const int last = 31 - __clz(who);
+        if (step == 1) {
+            b = lo + last;
+            seg = slot - __shfl_sync(0xFFFFFFFFu, first, last);
+            if (seg && seg * segment >= frame_span(offsets, frames, b).n) b = -1;       // (the sequence has no more segments)
+            return;
+        }
+        lo += last * step;
+        n = min(step, n - last * step);
+    }
 }
 // The first slot of sequence b.  (All lanes of a warp.)
 __device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int64_t frames, int64_t segment, int b)

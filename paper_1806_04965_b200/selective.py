@@ -71,6 +71,13 @@ def _library():
     return _lib
 
 
+def _there(call: str, **needed):
+    """What may not be left out."""
+    for name, t in needed.items():
+        if not isinstance(t, torch.Tensor):
+            _refuse(call, "%s: tensors are required" % name)
+
+
 def _pointer(t):
     return None if t is None else t.data_ptr()
 
@@ -138,6 +145,7 @@ def causal_conv_run(x, weight, bias=None, silu: bool = False, state=None, offset
     if fast is not None:
         return (fast[0] if out is None else out), (fast[1] if state_out is None else state_out)
     call = "causal_conv_run"
+    _there(call, x=x, weight=weight)
     device = _tensors(call, x, weight, bias, state, offsets, out, state_out)
     packed = offsets is not None
     _offsets(call, offsets)
@@ -166,6 +174,7 @@ def causal_conv_step(x, weight, state, bias=None, silu: bool = False):
     if fast is not None:
         return fast
     call = "causal_conv_step"
+    _there(call, x=x, weight=weight, state=state)
     device = _tensors(call, x, weight, state, bias)
     lead = _lead(call, x, False, True)
     out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -208,6 +217,7 @@ def selective_scan_run(u, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: b
     if fast is not None:
         return (fast[0] if out is None else out), (fast[1] if state_out is None else state_out)
     call = "selective_scan_run"
+    _there(call, u=u, dt=dt, a=a, b=b, c=c)
     device = _tensors(call, u, dt, a, b, c, d, z, dt_bias, state, offsets, out, state_out)
     packed = offsets is not None
     _offsets(call, offsets)
@@ -242,6 +252,7 @@ def selective_scan_step(u, dt, a, b, c, state, d=None, z=None, dt_bias=None, sof
     if fast is not None:
         return fast
     call = "selective_scan_step"
+    _there(call, u=u, dt=dt, a=a, b=b, c=c, state=state)
     device = _tensors(call, u, dt, a, b, c, state, d, z, dt_bias)
     lead = _lead(call, u, False, True)
     out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
@@ -285,6 +296,7 @@ def block_norm(y, residual, weight_after=None, weight_before=None, gate=None, ga
             out = m
         return out, h
     call = "block_norm"
+    _there(call, y=y, residual=residual)
     device = _tensors(call, y, residual, weight_after, weight_before, gate)
     if kinds < 0 or gate_act not in _GATES:
         _refuse(call, "norms is one of %s, gate_act one of %s" % (", ".join(_NORMS), ", ".join(_GATES)))

@@ -192,6 +192,161 @@ def test_scan_what_is_not_finite_stays_in_its_channel(what, value):
         assert not torch.isfinite(out[30, 1, 7])
 
 
+def longer(frames, states, groups, dtype, seed=0):
+    """One sequence that is cut into segments."""
+    x, o = scan_inputs(frames, 1, 2 * groups, states, groups, dtype, seed=seed)
+    plan = selective.scan_plan(DT[dtype], 1, frames, 2 * groups, states, groups)
+    assert 0 < plan["segment"] < frames and plan["held"] * plan["lanes"] >= states
+    return x, o
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("states,groups", [(3, 1), (8, 2), (12, 1), (16, 3), (24, 1), (32, 1), (60, 1), (128, 1)])
+def test_scan_in_segments_and_in_place(states, groups, dtype):
+    x, o = longer(333, states, groups, dtype)
+    state = randn(9, 1, 2 * groups, states)
+    kept = state.clone()
+    out, last = sr.selective_scan_run(**x, **o, state=state, state_out=state)
+    assert last is state
+    check_scan({k: v if k == "a" else v[:, 0] for k, v in x.items()}, dict(o, z=o["z"][:, 0]), True, kept[0], out[:, 0], state[0], (states, groups), dtype)
+
+
+def test_scan_states_do_not_drift():
+    """4000 frames of states that lose a ten-thousandth to a hundredth of themselves in each: a chunk's 32 approximate exponentials (2^-22 each) enter a value once, the rest are carried
+    over by chunks, with 2^-23 and a rounding each."""
+    T, C, N = 4000, 8, 16
+    x, o = scan_inputs(T, 1, C, N, 1, "fp32")
+    x["a"] = -(10.0 ** torch.linspace(-2, 0, N, device=DEV)).repeat(C, 1).contiguous()
+    x["dt"] = 0.01 * (1 + 0.3 * torch.rand(T, 1, C, generator=torch.Generator().manual_seed(5)).to(DEV))
+    x["u"] = x["u"].abs() + 0.5
+    x["b"] = x["b"].abs() + 0.1                                   # (no cancellation: the sums are their terms' magnitudes)
+    out, last = sr.selective_scan_run(**x, softplus=False)
+    _, want, _, m, _ = oracle.scan(*(host(x[k] if k == "a" else x[k][:, 0]) for k in ("u", "dt", "a", "b", "c")), plus=False)
+    # exponents add up to 0.4 to 50: an exponent's rounding is 2^-23 of it, of which a state that has lost e^-s keeps s e^-s < 1
+    within(host(last[0]), want, (32 * 2.0 ** -22 + T / 32 * 2 * 2.0 ** -23 + 2.0 ** -21) * m)
+
+
+@pytest.mark.parametrize("lengths", [[0, 3, 900, 1, 40, 0], [60] * 9 + [0, 64, 1], [0, 0, 0, 400, 0]], ids=["one_long", "none_long", "all_in_one"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_scan_packed_cut_where_one_is_long(lengths, dtype):
+    at, offsets = spans(lengths)
+    total, C = int(at[-1]), 24
+    x, o = scan_inputs(total, len(lengths), C, 16, 2, dtype, packed=True)
+    assert selective.scan_plan(DT[dtype], len(lengths), total, C, 16, 2, packed=True)["segment"] > 0
+    state = randn(9, len(lengths), C, 16)
+    kept = state.clone()
+    out, _ = sr.selective_scan_run(**x, **o, state=state, offsets=offsets, state_out=state)
+    for b, n in enumerate(lengths):
+        s = slice(at[b], at[b + 1])
+        if n:
+            check_scan({k: v if k == "a" else v[s] for k, v in x.items()}, dict(o, z=o["z"][s]), True, kept[b], out[s], state[b], b, dtype)
+        else:
+            assert torch.equal(state[b], kept[b])
+
+
+def test_many_short_sequences():
+    rng = np.random.default_rng(3)
+    lengths = rng.integers(0, 6, 1500).tolist() + [300]
+    at, offsets = spans(lengths)
+    total, C = int(at[-1]), 10
+    x, o = scan_inputs(total, len(lengths), C, 4, 1, "fp32", packed=True)
+    state, taps = randn(9, len(lengths), C, 4), randn(10, len(lengths), 3, C)
+    w = randn(11, C, 4)
+    out, last = sr.selective_scan_run(**x, **o, state=state, offsets=offsets)
+    conv, left = sr.causal_conv_run(x["u"], w, silu=True, state=taps, offsets=offsets)
+    for b in list(range(0, 1500, 61)) + [1499, 1500]:
+        s = slice(at[b], at[b + 1])
+        if lengths[b]:
+            check_scan({k: v if k == "a" else v[s] for k, v in x.items()}, dict(o, z=o["z"][s]), True, state[b], out[s], last[b], b, "fp32")
+            check_conv(x["u"][s], w, None, True, taps[b], conv[s], left[b], b, "fp32")
+        else:
+            assert torch.equal(last[b], state[b]) and torch.equal(left[b], taps[b])
+
+
+def test_offsets_outside_the_frames_are_taken_as_the_nearest():
+    x, o = scan_inputs(50, 3, 16, 8, 1, "fp32", packed=True)
+    w = randn(11, 16, 3)
+    good, bad = (torch.tensor(v, dtype=torch.int64, device=DEV) for v in ([0, 20, 50, 50], [-7, 20, 50 + (1 << 40), 1 << 62]))
+    for call in (lambda f: sr.selective_scan_run(**x, **o, offsets=f), lambda f: sr.causal_conv_run(x["u"], w, offsets=f)):
+        for a, b in zip(call(good), call(bad)):
+            assert torch.equal(a, b)
+
+
+def test_inputs_that_strides_repeat():
+    T, B, C, N = 40, 3, 32, 16
+    x, o = scan_inputs(T, B, C, N, 1, "bf16")
+    x = {k: v if k == "a" else v[:, :1].expand(T, B, *v.shape[2:]) for k, v in x.items()}
+    x["b"] = x["b"][:1].expand(T, B, 1, N)
+    whole = {k: v.contiguous() for k, v in x.items()}
+    z = o["z"][:1].expand(T, B, C)
+    for a, b in zip(sr.selective_scan_run(**x, **dict(o, z=z)), sr.selective_scan_run(**whole, **dict(o, z=z.contiguous()))):
+        assert torch.equal(a, b)
+    w = randn(11, C, 4)
+    for a, b in zip(sr.causal_conv_run(x["u"], w), sr.causal_conv_run(whole["u"], w)):
+        assert torch.equal(a, b)
+    first = {k: v if k == "a" else v[0] for k, v in x.items()}
+    s1, s2 = randn(9, B, C, N), randn(9, B, C, N)
+    assert torch.equal(sr.selective_scan_step(*first.values(), s1, **dict(o, z=z[0])), sr.selective_scan_step(*(v.contiguous() for v in first.values()), s2, **dict(o, z=z[0])))
+    assert torch.equal(s1, s2)
+
+
+def test_nothing_to_do():
+    x, o = scan_inputs(4, 2, 8, 4, 1, "fp32")
+    none = {k: v if k == "a" else v[:0] for k, v in x.items()}
+    state = randn(9, 2, 8, 4)
+    out, last = sr.selective_scan_run(**none, d=o["d"], state=state)
+    assert out.shape == (0, 2, 8) and torch.equal(last, state)
+    assert not sr.selective_scan_run(**none)[1].any()
+    w = randn(11, 8, 4)
+    taps = randn(10, 2, 3, 8)
+    out, last = sr.causal_conv_run(none["u"], w, state=taps)
+    assert out.shape == (0, 2, 8) and torch.equal(last, taps) and not sr.causal_conv_run(none["u"], w)[1].any()
+    nobody = {k: v if k == "a" else v[:, :0] for k, v in x.items()}
+    assert sr.selective_scan_run(**nobody)[0].shape == (4, 0, 8) and sr.causal_conv_run(nobody["u"], w)[1].shape == (0, 3, 8)
+    assert sr.selective_scan_step(*(v if k == "a" else v[0] for k, v in nobody.items()), randn(9, 0, 8, 4)).shape == (0, 8)
+    assert sr.block_norm(x["u"][:0, 0], x["dt"][:0, 0])[0].shape == (0, 8)
+
+
+def test_what_is_written_in_place_gets_a_new_version():
+    x, o = scan_inputs(4, 2, 8, 4, 1, "fp32")
+    w, state, taps, out = randn(11, 8, 4), randn(9, 2, 8, 4), randn(10, 2, 3, 8), torch.empty(4, 2, 8, device=DEV)
+    before = [t._version for t in (state, taps, out)]
+    sr.selective_scan_run(**x, state_out=state, out=out)
+    sr.causal_conv_step(x["u"][0], w, taps)
+    assert [t._version for t in (state, taps, out)] == [v + 1 for v in before]
+
+
+# ------------------------------------------------------------------------------------------ refusals that need a device
+def test_refusals():
+    x, o = scan_inputs(6, 2, 8, 4, 2, "fp32")
+    w, state = randn(11, 8, 4), randn(9, 2, 8, 4)
+    taps = randn(10, 2, 3, 8)
+    bad = [
+        lambda: sr.selective_scan_run(**dict(x, dt=x["dt"].bfloat16())), lambda: sr.selective_scan_run(**dict(x, dt=x["dt"][:5])), lambda: sr.selective_scan_run(**dict(x, u=x["u"][..., :7])),
+        lambda: sr.selective_scan_run(**dict(x, a=x["a"].bfloat16())), lambda: sr.selective_scan_run(**dict(x, a=x["a"].t().contiguous().t())),
+        lambda: sr.selective_scan_run(**dict(x, c=x["c"][..., :3])), lambda: sr.selective_scan_run(**dict(x, b=x["b"][:, :, :1])), lambda: sr.selective_scan_run(**dict(x, dt=None)),
+        lambda: sr.selective_scan_run(**x, d=o["d"][:7]), lambda: sr.selective_scan_run(**x, z=o["z"][:, :1]), lambda: sr.selective_scan_run(**x, state=state[:1]),
+        lambda: sr.selective_scan_run(**x, state=state.double()), lambda: sr.selective_scan_run(**x, out=torch.empty(6, 2, 9, device=DEV)), lambda: sr.selective_scan_run(**x, out=x["dt"]),
+        lambda: sr.selective_scan_run(**x, offsets=torch.zeros(3, dtype=torch.int64, device=DEV)), lambda: sr.selective_scan_run(**{k: v if k == "a" else v.half() for k, v in x.items()}),
+        lambda: sr.selective_scan_run(**dict(x, u=x["u"].transpose(0, 2).contiguous().transpose(0, 2))), lambda: sr.selective_scan_run(**dict(x, u=x["u"].cpu())),
+        lambda: sr.selective_scan_step(x["u"], x["dt"][0], x["a"], x["b"][0], x["c"][0], state), lambda: sr.selective_scan_step(x["u"][0], x["dt"][0], x["a"], x["b"][0], x["c"][0], None),
+        lambda: sr.causal_conv_run(x["u"], w[:7]), lambda: sr.causal_conv_run(x["u"], randn(1, 8, 9)), lambda: sr.causal_conv_run(x["u"], w, bias=randn(1, 7)),
+        lambda: sr.causal_conv_run(x["u"], w, state=taps.bfloat16()), lambda: sr.causal_conv_run(x["u"], w, state=taps[:, :2]), lambda: sr.causal_conv_step(x["u"][0], w, taps[:, :2]),
+        lambda: sr.causal_conv_step(x["u"][0], w, None), lambda: sr.causal_conv_run(x["u"][0], w),
+        lambda: sr.block_norm(x["u"][0], x["dt"][1][:1]), lambda: sr.block_norm(x["u"][0], x["dt"][0].bfloat16()), lambda: sr.block_norm(x["u"][0], None),
+        lambda: sr.block_norm(x["u"][0], x["dt"][0], gate=x["dt"][0][:, :7]), lambda: sr.block_norm(x["u"][0], x["dt"][0], weight_after=randn(1, 7)),
+        lambda: sr.block_norm(x["u"][0], x["dt"][0], norms="all"), lambda: sr.block_norm(x["u"][0], x["dt"][0], gate_act="tanh"), lambda: sr.block_norm(x["u"][0], x["dt"][0], format="mx6"),
+        lambda: sr.block_norm(x["u"][0], x["dt"][0], norms="after", format="mx8"), lambda: sr.block_norm(x["u"][0], x["dt"][0], eps=-1.0),
+    ]
+    for k, call in enumerate(bad):
+        with pytest.raises(sr.SrError):
+            call()
+            pytest.fail("call %d was taken" % k)
+    many = scan_inputs(2, 1, 2, 129, 1, "fp32")[0]
+    with pytest.raises(sr.SrError):
+        sr.selective_scan_run(**many)
+
+
 # ------------------------------------------------------------------------------------------ norms around a block
 def check_block(y, r, after, before, gate, act, scale, eps, norms, out, h, dtype):
     want, wh, mag = oracle.block(host(y), host(r), *(None if t is None else host(t) for t in (after, before, gate)), act, scale, eps, norms)
@@ -363,7 +518,40 @@ def test_head_behind_a_rollout():
         G.rollout(frames, head=sr.SelectiveHead(w, channels, 64, 8, 4, 3, spec.batch + 1, format="mx8", dtype="fp32"))
 
 
-# ------------------------------------------------------------------------------------------ streams, devices, threads
+# ------------------------------------------------------------------------------------------ streams, threads
+def test_calls_of_two_threads():
+    import threading
+    x, o = scan_inputs(200, 2, 32, 16, 1, "bf16")
+    w = randn(7, 32, 4)
+    y = [randn(30 + k, 400, 520, dtype="bf16") for k in range(3)]
+    calls = (lambda: sr.selective_scan_run(**x, **o), lambda: sr.causal_conv_run(x["u"], w, silu=True), lambda: sr.block_norm(*y[:2], gate=y[2]))
+    want = [f() for f in calls]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = [calls[(k + j) % 3]() for j in range(30)]
+            torch.cuda.current_stream().synchronize()
+            wrong.extend(j for j, g in enumerate(got) if not all(torch.equal(a, b) for a, b in zip(g, want[(k + j) % 3])))
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not wrong
+
+
+def test_block_norm_goes_over_many_rows():
+    """More rows than blocks, so that blocks go over several."""
+    for rows, cols, norms in ((6000, 40, "both"), (5001, 1030, "after"), (3000, 2048, "before"), (2500, 999, "both")):
+        y, r, gate = (randn(k, rows, cols, dtype="bf16") for k in (1, 2, 3))
+        got = sr.block_norm(y, r, gate=gate, scale=0.5, norms=norms)
+        out, h = got if norms in ("both", "before") else (None, got)
+        check_block(y, r, None, None, gate, "sigmoid", 0.5, 1e-6, norms, out, h, "bf16")
+
+
 def test_calls_side_by_side_on_streams_and_replayed():
     x, o = scan_inputs(400, 1, 64, 16, 1, "bf16")
     y, p = scan_inputs(300, 2, 64, 16, 1, "bf16", seed=20)

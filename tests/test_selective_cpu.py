@@ -135,6 +135,23 @@ def test_scan_plans_need_no_device():
         selective.scan_plan(torch.bfloat16, 4, 1000, 512, 129, sms=148)
 
 
+def test_scan_plans_cut_what_leaves_schedulers_idle():
+    def plan(batch, frames, channels, states=16, packed=False, dtype=torch.bfloat16):
+        return selective.scan_plan(dtype, batch, frames, channels, states, packed=packed, sms=148)
+
+    assert plan(32, 128, 2048)["segment"] == 0                    # enough channels
+    assert plan(1, 32, 64)["segment"] == 0                        # too short
+    for batch, frames, channels in ((1, 16384, 1024), (5, 500, 1111), (1, 300, 8)):
+        p = plan(batch, frames, channels)
+        assert p["segment"] % 32 == 0 and p["segments"] == batch * -(-frames // p["segment"]) and p["segment"] < frames
+    p = plan(16, 16384, 1024, packed=True)
+    assert p["segment"] % 32 == 0 and p["segments"] == 16384 // p["segment"] + 16
+    assert {(plan(1, 64, 64, n)["held"], plan(1, 64, 64, n)["lanes"]) for n in (4, 8, 12, 16, 24, 32, 64, 128)} == {(4, 1), (8, 1), (12, 1), (16, 1), (12, 2), (16, 2), (16, 4), (16, 8)}
+    for big in (dict(frames=1 << 50, channels=64), dict(frames=8, channels=1 << 30, batch=1 << 30)):
+        with pytest.raises(SrError):
+            plan(**dict(dict(batch=1), **big))
+
+
 def test_oracle_scan_is_the_sum_it_stands_for():
     rng = np.random.default_rng(0)
     T, C, N = 7, 4, 3
