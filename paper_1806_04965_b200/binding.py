@@ -302,7 +302,7 @@ class Graph:
 
     def rollout(self, frames, head=None):
         """frames: one tensor [T+1][B][H][W][C] per input node (frames 0..T).  Resets to frame 0,
-        runs T updates, returns the outputs [T][B][C_out] (float32).  With a `TemporalHead` the outputs are its features: it is
+        runs T updates, returns the outputs [T][B][C_out] (float32).  With a `TemporalHead` or `SelectiveHead` the outputs are its features: it is
         reset, too, and what it gives for the T frames is returned."""
         check = getattr(head, "check_features", None)               # (anything with reset and run may stand behind a rollout)
         if check is not None:

@@ -1,7 +1,9 @@
 // Causal convolution of every channel over the last frames: out[t, c] = act(bias[c] + sum_j weight[c, j] x[t - (W - 1) + j, c]).
 //
 // Bound by memory: x once, out once.  A thread has VEC neighbouring channels and goes over a segment of frames with the last W - 1 of them in registers, so that only
-// the W - 1 frames ahead of a segment are read twice; eight frames are loaded at a time, and stay as they lie in memory until they are used.
+// the W - 1 frames ahead of a segment are read twice.  Units of 16 bytes come through a ring in shared memory that is the thread's own, so that nothing waits for others; narrower
+// ones through registers, the next eight under way while eight are worked on.  64 sequences of 128 frames, 4096 channels, four taps, bf16: 30 us (4.6 TB/s), 26 without the
+// activation, 512 frames 94 (5.7 TB/s): beginning and end of a launch, and the activation's exponentials and reciprocals (15 us of the special function units).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
