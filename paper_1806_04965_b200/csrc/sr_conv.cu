@@ -112,7 +112,7 @@ __device__ __forceinline__ void see(float (&seen)[W][VEC], const srx::Few<T, VEC
 }
 
 template <typename T, int VEC, int W>
-__global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? 4 : 1) sr_conv_run_kernel(const __grid_constant__ ConvArgs A)
+__global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? (VEC * W > 40 ? 2 : 4) : 1) sr_conv_run_kernel(const __grid_constant__ ConvArgs A)
 {
     using srx::Few;
     constexpr int kAhead = ahead_of(VEC * (int)sizeof(T));

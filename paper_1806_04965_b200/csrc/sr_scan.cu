@@ -13,7 +13,8 @@
 //
 // Drift.  The approximate exponential is low by 2e-8 in the mean, which a state that loses a thousandth of itself per frame makes 2e-5 of.  So a state is carried over in chunks of
 // 32 frames, by one exponential of their steps' sum that has no bias, and what comes in during a chunk is summed apart: `local`.  That costs a multiply-add for a state and frame and
-// takes the error of states from 2e-6 to 3e-7.
+// takes the error of states from 2e-6 to 3e-7.  A segment whose states nobody asks for (what enters the next comes from the segments' sums) goes without where its outputs are rounded to
+// bf16: over 1024 frames the bias comes to 2e-5 of a state at most, half a step of bf16 is 4e-3 (a sequence of 16384 frames of 2048 channels: 202 us, with the carry 212).
 //
 // Long sequences are cut into segments: their sums (without outputs), the states that enter them, their outputs.
 #include <cuda_bf16.h>
@@ -22,6 +23,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/sr_rollout.h"
 #include "sr_operators.h"
@@ -54,10 +56,11 @@ struct ScanArgs {
 
 constexpr int kBlock = 8;                              // frames of a stage
 constexpr int kChunk = 32;                             // frames that a state is carried over at once
-constexpr int kWarps = 16;                             // of an SM: 128 registers
+constexpr int kUncarried = 1024;                       // frames that a segment of bf16 outputs may have without that
 enum { kWhole = 0, kSums = 1, kOutputs = 2 };          // whole sequences; sums of segments; outputs of segments, from the states that enter them
 // A block's threads share b and c, whose widening is the more to do the more states there are; fewer make the work of SMs more even.
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes < 4 ? 32 : 128; }
+constexpr int kWarps = 16;                             // of an SM, so 128 registers (168 and 12 warps: 64 states 630 us instead of 616, 300 frames of 16 sequences 138 instead of 129; 128 states 224 instead of 232)
 
 // Frames of a segment of this run.
 __device__ __forceinline__ int64_t segment_of(const ScanArgs& A)
@@ -277,70 +280,77 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     double total = 0.0;                                // of r
     float since = 0.0f;                                // of r, from the chunk's start on
     int half = 0;
-    for (int64_t at = 0; at < n; at += kBlock, half ^= 1) {
-        const int left = frames_from(at);
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        sync();                                        // the stage has landed, and the one before is done with
-        if (at + kBlock < n) fetch(half ^ 1, frames_from(at + kBlock));
-        widen(half, left);
-        sync();
-#pragma unroll 2
-        for (int q = 0; q < N; ++q) {
-            // of L frames each of the channel's threads prepares one
-            const int mine = q * L + p;
-            const float s = (float)S.dt[half][mine][col] + bias, u = (float)S.u[half][mine][col], plus = srx::softplus<EXACT>(s);
-            const float r = mine >= left ? 0.0f : A.softplus ? plus : s;         // (a frame behind the last one changes nothing)
-            const float x = mine >= left ? 0.0f : r * u;
-            float y[L];
+    auto all_frames = [&](auto carry) {
+        constexpr bool CARRY = decltype(carry)::value;
+        for (int64_t at = 0; at < n; at += kBlock, half ^= 1) {
+            const int left = frames_from(at);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            sync();                                    // the stage has landed, and the one before is done with
+            if (at + kBlock < n) fetch(half ^ 1, frames_from(at + kBlock));
+            widen(half, left);
+            sync();
+#pragma unroll(EXACT ? 4 : 2)                     // (fp32, 5 sequences of 500 frames of 1111 channels: 51 us, two at a time 55; bf16 gains nothing from four)
+            for (int q = 0; q < N; ++q) {
+                // of L frames each of the channel's threads prepares one
+                const int mine = q * L + p;
+                const float s = (float)S.dt[half][mine][col] + bias, u = (float)S.u[half][mine][col], plus = srx::softplus<EXACT>(s);
+                const float r = mine >= left ? 0.0f : A.softplus ? plus : s;         // (a frame behind the last one changes nothing)
+                const float x = mine >= left ? 0.0f : r * u;
+                float y[L];
 #pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const int f = q * L + i;
-                const float rr = L > 1 ? __shfl_sync(0xFFFFFFFFu, r, i * SIDE + lane % SIDE) : r;
-                const float xx = L > 1 ? __shfl_sync(0xFFFFFFFFu, x, i * SIDE + lane % SIDE) : x;
-                since += rr;
-                const Pair r2 = srx::pair(rr, rr), x2 = srx::pair(xx, xx);
-                Pair y2 = srx::pair(0.0f, 0.0f);
+                for (int i = 0; i < L; ++i) {
+                    const int f = q * L + i;
+                    const float rr = L > 1 ? __shfl_sync(0xFFFFFFFFu, r, i * SIDE + lane % SIDE) : r;
+                    const float xx = L > 1 ? __shfl_sync(0xFFFFFFFFu, x, i * SIDE + lane % SIDE) : x;
+                    if (CARRY) since += rr;
+                    const Pair r2 = srx::pair(rr, rr), x2 = srx::pair(xx, xx);
+                    Pair y2 = srx::pair(0.0f, 0.0f);
 #pragma unroll
-                for (int k = 0; k < K; k += 4) {
-                    const float4 bv = *reinterpret_cast<const float4*>(&S.bf[f][((k / 4) * L + p) * 4]);
-                    const float2 e0 = srx::split(srx::mul2(r2, a2[k / 2])), e1 = srx::split(srx::mul2(r2, a2[k / 2 + 1]));
-                    const Pair d0 = srx::pair(srx::ex2(e0.x), srx::ex2(e0.y)), d1 = srx::pair(srx::ex2(e1.x), srx::ex2(e1.y));
-                    const Pair i0 = srx::mul2(x2, srx::pair(bv.x, bv.y)), i1 = srx::mul2(x2, srx::pair(bv.z, bv.w));
-                    local[k / 2] = srx::fma2(d0, local[k / 2], i0);
-                    local[k / 2 + 1] = srx::fma2(d1, local[k / 2 + 1], i1);
-                    if (OUT) {
-                        h[k / 2] = srx::fma2(d0, h[k / 2], i0);
-                        h[k / 2 + 1] = srx::fma2(d1, h[k / 2 + 1], i1);
-                        const float4 cv = *reinterpret_cast<const float4*>(&S.cf[OUT ? f : 0][((k / 4) * L + p) * 4]);
-                        y2 = k ? srx::fma2(srx::pair(cv.x, cv.y), h[k / 2], y2) : srx::mul2(srx::pair(cv.x, cv.y), h[k / 2]);
-                        y2 = srx::fma2(srx::pair(cv.z, cv.w), h[k / 2 + 1], y2);
+                    for (int k = 0; k < K; k += 4) {
+                        const float4 bv = *reinterpret_cast<const float4*>(&S.bf[f][((k / 4) * L + p) * 4]);
+                        const float2 e0 = srx::split(srx::mul2(r2, a2[k / 2])), e1 = srx::split(srx::mul2(r2, a2[k / 2 + 1]));
+                        const Pair d0 = srx::pair(srx::ex2(e0.x), srx::ex2(e0.y)), d1 = srx::pair(srx::ex2(e1.x), srx::ex2(e1.y));
+                        const Pair i0 = srx::mul2(x2, srx::pair(bv.x, bv.y)), i1 = srx::mul2(x2, srx::pair(bv.z, bv.w));
+                        if (CARRY) {
+                            local[k / 2] = srx::fma2(d0, local[k / 2], i0);
+                            local[k / 2 + 1] = srx::fma2(d1, local[k / 2 + 1], i1);
+                        }
+                        if (OUT) {
+                            h[k / 2] = srx::fma2(d0, h[k / 2], i0);
+                            h[k / 2 + 1] = srx::fma2(d1, h[k / 2 + 1], i1);
+                            const float4 cv = *reinterpret_cast<const float4*>(&S.cf[OUT ? f : 0][((k / 4) * L + p) * 4]);
+                            y2 = k ? srx::fma2(srx::pair(cv.x, cv.y), h[k / 2], y2) : srx::mul2(srx::pair(cv.x, cv.y), h[k / 2]);
+                            y2 = srx::fma2(srx::pair(cv.z, cv.w), h[k / 2 + 1], y2);
+                        }
                     }
+                    const float2 v = srx::split(y2);
+                    y[i] = v.x + v.y;
                 }
-                const float2 v = srx::split(y2);
-                y[i] = v.x + v.y;
+                if (OUT) {
+                    const float o = fmaf(skip, u, exchange<L, SIDE>(y, p)), gate = srx::silu<EXACT>((float)S.z[OUT ? half : 0][mine][col]);
+                    S.out[OUT ? mine : 0][col] = (T)(gated ? o * gate : o);
+                }
+            }
+            if (CARRY && ((at + kBlock) % kChunk == 0 || at + kBlock >= n)) {
+                const Pair s2 = srx::pair(since, since);
+#pragma unroll
+                for (int k = 0; k < K / 2; ++k) {
+                    const float2 v = S.carried[k][tid];
+                    h[k] = srx::fma2(srx::exp2_exact(srx::mul2(s2, a2[k])), srx::pair(v.x, v.y), local[k]);
+                    S.carried[k][tid] = srx::split(h[k]);
+                    local[k] = srx::pair(0.0f, 0.0f);
+                }
+                total += (double)since;
+                since = 0.0f;
             }
             if (OUT) {
-                const float o = fmaf(skip, u, exchange<L, SIDE>(y, p)), gate = srx::silu<EXACT>((float)S.z[OUT ? half : 0][mine][col]);
-                S.out[OUT ? mine : 0][col] = (T)(gated ? o * gate : o);
+                sync();
+                put(left);
             }
         }
-        if ((at + kBlock) % kChunk == 0 || at + kBlock >= n) {
-            const Pair s2 = srx::pair(since, since);
-#pragma unroll
-            for (int k = 0; k < K / 2; ++k) {
-                const float2 v = S.carried[k][tid];
-                h[k] = srx::fma2(srx::exp2_exact(srx::mul2(s2, a2[k])), srx::pair(v.x, v.y), local[k]);
-                S.carried[k][tid] = srx::split(h[k]);
-                local[k] = srx::pair(0.0f, 0.0f);
-            }
-            total += (double)since;
-            since = 0.0f;
-        }
-        if (OUT) {
-            sync();
-            put(left);
-        }
-    }
+    };
+    if (MODE == kOutputs && !EXACT && !last && n <= kUncarried) all_frames(std::false_type{});
+    else all_frames(std::true_type{});
 
     float* to = MODE == kSums ? A.sums + (slot * A.channels + ch) * A.states : A.state_out && last ? A.state_out + ((int64_t)b * A.channels + ch) * A.states : nullptr;
     if (to && there) {
