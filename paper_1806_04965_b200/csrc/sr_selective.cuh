@@ -66,23 +66,6 @@ __device__ __forceinline__ float softplus(float x)
     return fmaf(s, p, fmaxf(x, 0.0f));
 }
 
-// The same for two values.
-template <bool EXACT>
-__device__ __forceinline__ Pair softplus(Pair x)
-{
-    const float2 v = split(x);
-    if constexpr (EXACT) return pair(softplus<true>(v.x), softplus<true>(v.y));
-    const Pair e = pair(ex2(-kLog2e * fabsf(v.x)), ex2(-kLog2e * fabsf(v.y)));
-    const float2 n = split(add2(e, pair(2.0f, 2.0f)));
-    const Pair s = mul2(e, pair(reciprocal(n.x), reciprocal(n.y))), w = mul2(s, s);
-    Pair p = pair(0.28191549f, 0.28191549f);
-    p = fma2(p, w, pair(0.27957666f, 0.27957666f));
-    p = fma2(p, w, pair(0.40025115f, 0.40025115f));
-    p = fma2(p, w, pair(0.66666311f, 0.66666311f));
-    p = fma2(p, w, pair(2.0f, 2.0f));
-    return fma2(s, p, pair(fmaxf(v.x, 0.0f), fmaxf(v.y, 0.0f)));
-}
-
 // 1 / (1 + exp(-x)); EXACT: to the last two bits of 32 (the approximate reciprocal is off by one), else to more than those of bf16
 template <bool EXACT>
 __device__ __forceinline__ float sigmoid(float x)

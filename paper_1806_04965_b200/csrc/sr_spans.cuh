@@ -100,14 +100,4 @@ __device__ __forceinline__ void packed_slot(const int64_t* offsets, int64_t fram
         n = min(step, n - last * step);
     }
 }
-// The first slot of sequence b.  (All lanes of a warp.)
-__device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int64_t frames, int64_t segment, int b)
-{
-    if (!offsets) return b * segments_of(frames, segment);
-    int64_t sum = 0;
-    for (int i = threadIdx.x & 31; i < b; i += 32) sum += segments_of(frame_span(offsets, frames, i).n, segment);
-#pragma unroll
-    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    return sum;
-}
 #endif

@@ -244,6 +244,32 @@ def test_scan_packed_cut_where_one_is_long(lengths, dtype):
             assert torch.equal(state[b], kept[b])
 
 
+def test_scan_in_segments_of_thousands_of_frames():
+    """The same inputs in every frame, so that frame t's state is x (1 - q^t) / (1 - q), q = exp(r a).  A state remembers 1000 frames at most: 32 approximate exponentials (2^-22 each), 1000 / 32
+    carries (2^-23, and a rounding, each), the steps' sums (32 roundings of a chunk's, which is 1 over all that is remembered), and a few roundings of the output's sum."""
+    lengths, C, N = [119000, 0, 1000], 2048, 4
+    at, offsets = spans(lengths)
+    T = int(at[-1])
+    plan = selective.scan_plan(torch.bfloat16, len(lengths), T, C, N, packed=True)
+    assert plan["segment"] > 1024
+    a = -(10.0 ** torch.linspace(-1, 0, N, device=DEV)).repeat(C, 1).contiguous()
+    u, dt, b, c = (randn(k, *s, dtype="bf16").abs() for k, s in enumerate(((C,), (C,), (1, N), (1, N))))
+    dt = (0.01 + 0.03 * dt.float().clamp(max=1.0)).bfloat16()
+    state = randn(9, len(lengths), C, N).abs()
+    out, last = sr.selective_scan_run(u.expand(T, C), dt.expand(T, C), a, b.expand(T, 1, N), c.expand(T, 1, N), softplus=False, state=state, offsets=offsets)
+    e = 32 * 2.0 ** -22 + (1000 / 32 + 1) * 2 * 2.0 ** -23 + 32 * 2.0 ** -23 + 2.0 ** -21
+    some = slice(0, C, 37)
+    for s, n in enumerate(lengths):
+        times = np.unique(np.concatenate([np.arange(1, min(n, 3)), np.arange(1, n + 1, 311), plan["segment"] * np.arange(1, n // plan["segment"] + 1), [n]]))[:, None, None] if n else np.zeros((1, 1, 1))
+        r, A, x = host(dt[some])[None, :, None], host(a[some])[None], host(dt[some])[None, :, None] * host(u[some])[None, :, None] * host(b)[None]
+        grown = -np.expm1(r * A * times)                          # 1 - q^t
+        h = (1 - grown) * host(state[s, some])[None] + x * grown / -np.expm1(r * A)
+        if n:
+            want = (h * host(c)[None]).sum(-1)
+            within(host(out[at[s]:at[s + 1]][torch.from_numpy(times[:, 0, 0] - 1).to(DEV)][:, some]), want, oracle.HALF_STEP["bf16"] * want + e * want, s)
+        within(host(last[s, some]), h[-1], e * h[-1], s)
+
+
 def test_many_short_sequences():
     rng = np.random.default_rng(3)
     lengths = rng.integers(0, 6, 1500).tolist() + [300]
