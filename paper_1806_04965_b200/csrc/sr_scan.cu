@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
             if (at + kBlock < n) fetch(half ^ 1, frames_from(at + kBlock));
             widen(half, left);
             sync();
-#pragma unroll(EXACT ? 4 : 2)                     // (fp32, 5 sequences of 500 frames of 1111 channels: 51 us, two at a time 55; bf16 gains nothing from four)
+#pragma unroll(EXACT ? 4 : 2)                     // (fp32: two at a time cost 7 % more; bf16 gains nothing from four)
             for (int q = 0; q < N; ++q) {
                 // of L frames each of the channel's threads prepares one
                 const int mine = q * L + p;
@@ -570,15 +570,17 @@ struct ScanCut {
 };
 // Cycles that cutting costs besides: two launches, a load's latency for every eight segments, and the segments' states, which are written, joined and read (16 bytes each).
 double joining(const sr_scan_desc* d, int64_t count) { return 16000.0 + count / 8 * 2000.0 + (double)d->batch * count * d->channels * d->states / 200; }
-// Cycles that `warps` warps, spread over all schedulers, take for a frame; measured for 16 states in bf16 (fp32: 1.5 times as many).
+// Cycles that `warps` warps, spread over all schedulers, take for a frame; measured for 16 states in bf16 (fp32: 1.5 times as many).  Rounds of four follow each other without a gap, and what one
+// SM is behind in one another makes up for in the next (8192 frames of 8192 channels: 778 us in one round, 736 in two, 697 in four).
 double cycles_of(double warps, int64_t schedulers)
 {
     constexpr double kOf[5] = {0, 427, 545, 705, 880};
     const double each = std::ceil(warps / schedulers), rounds = std::floor(each / 4);
-    return rounds * kOf[4] + kOf[(int)(each - 4 * rounds)];
+    return (rounds * kOf[4] + kOf[(int)(each - 4 * rounds)]) * (each > 4 ? 0.92 + 0.32 / each : 1.0);
 }
 // Whole sequences where their channels fill the schedulers; otherwise segments, whose sums cost 0.7 of their outputs, and two launches more.
-// Side by side: the number of segments with the smallest estimate.  Packed: only the GPU knows the lengths.  There are segments of a third of the frames that there are for each
+// Side by side: of the numbers of segments that just give every scheduler one to four warps, or rounds of four, the one with the smallest estimate (5 sequences of 500 frames, 1111 channels, fp32:
+// 46 us with segments of 40 frames, 50 with 32).  Packed: only the GPU knows the lengths.  There are segments of a third of the frames that there are for each
 // scheduler's warp where some sequence has more than 1.75 times those, that is, would take longer than all of them in segments; else, as the kernels find, no
 // sequence is cut.
 ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
@@ -602,10 +604,14 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
         c.slots = d->frames / c.segment + d->batch;
         return c;
     }
-    auto cycles_for = [&](int64_t frames, int64_t count) { return frames * cycles_of((double)warps * d->batch * count, schedulers); };
+    const int64_t at_once = warps * d->batch;
+    auto cycles_for = [&](int64_t frames, int64_t count) { return frames * cycles_of((double)at_once * count, schedulers); };
     double best = cycles_for(d->frames, 1);
-    for (int64_t chunks = 1; chunks * kChunk < d->frames; chunks += (chunks + 3) / 4) {
-        const int64_t segment = chunks * kChunk, count = segments_of(d->frames, segment);
+    for (int each = 1; each <= 64; each += each < 4 ? 1 : 4) {
+        const int64_t most = each * schedulers / at_once;
+        if (most < 2) continue;
+        const int64_t segment = std::max<int64_t>((d->frames + kBlock * most - 1) / (kBlock * most) * kBlock, kChunk), count = segments_of(d->frames, segment);
+        if (count < 2) continue;
         const double cycles = cycles_for(segment, count) + 0.7 * cycles_for(segment, count - 1) + joining(d, count);
         if (cycles < best) {
             best = cycles;

@@ -143,7 +143,7 @@ def test_scan_plans_cut_what_leaves_schedulers_idle():
     assert plan(1, 32, 64)["segment"] == 0                        # too short
     for batch, frames, channels in ((1, 16384, 1024), (5, 500, 1111), (1, 300, 8)):
         p = plan(batch, frames, channels)
-        assert p["segment"] % 32 == 0 and p["segments"] == batch * -(-frames // p["segment"]) and p["segment"] < frames
+        assert p["segment"] % 8 == 0 and p["segments"] == batch * -(-frames // p["segment"]) and p["segment"] < frames
     p = plan(16, 16384, 1024, packed=True)
     assert p["segment"] % 32 == 0 and p["segments"] == 16384 // p["segment"] + 16
     assert {(plan(1, 64, 64, n)["held"], plan(1, 64, 64, n)["lanes"]) for n in (4, 8, 12, 16, 24, 32, 64, 128)} == {(4, 1), (8, 1), (12, 1), (16, 1), (12, 2), (16, 2), (16, 4), (16, 8)}
