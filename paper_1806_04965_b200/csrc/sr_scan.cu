@@ -580,9 +580,10 @@ double cycles_of(double warps, int64_t schedulers)
 }
 // Whole sequences where their channels fill the schedulers; otherwise segments, whose sums cost 0.7 of their outputs, and two launches more.
 // Side by side: of the numbers of segments that just give every scheduler one to four warps, or rounds of four, the one with the smallest estimate (5 sequences of 500 frames, 1111 channels, fp32:
-// 46 us with segments of 40 frames, 50 with 32).  Packed: only the GPU knows the lengths.  There are segments of a third of the frames that there are for each
-// scheduler's warp where some sequence has more than 1.75 times those, that is, would take longer than all of them in segments; else, as the kernels find, no
-// sequence is cut.
+// 46 us with segments of 40 frames, 50 with 32).
+// Packed: only the GPU knows the lengths.  There are segments of a third of the frames that there are for each scheduler's warp (16 sequences, 1024 channels of 64 states: 619 us, of half of them 637,
+// all 731), but not below 72 where there are as many (7500 frames, 700 channels of 12: 76 us, with 32 frames 92), where some sequence has more than 1.75 times those, that is, would
+// take longer than all of them in segments; else, as the kernels find, no sequence is cut.
 ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
 {
     ScanCut c{};
@@ -600,7 +601,7 @@ ScanCut scan_cut(const sr_scan_desc* d, bool packed, int sms)
         const int64_t even = (int64_t)std::min((double)d->frames * warps / (schedulers * 4), 1e12);
         c.whole = whole_chunks(even * 7 / 4);
         if (c.whole >= d->frames) return c;
-        c.segment = whole_chunks(even / 3);
+        c.segment = std::max<int64_t>((std::max(even / 3, std::min<int64_t>(even, 72)) + kBlock - 1) / kBlock * kBlock, kChunk);
         c.slots = d->frames / c.segment + d->batch;
         return c;
     }

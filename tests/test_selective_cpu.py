@@ -145,7 +145,7 @@ def test_scan_plans_cut_what_leaves_schedulers_idle():
         p = plan(batch, frames, channels)
         assert p["segment"] % 8 == 0 and p["segments"] == batch * -(-frames // p["segment"]) and p["segment"] < frames
     p = plan(16, 16384, 1024, packed=True)
-    assert p["segment"] % 32 == 0 and p["segments"] == 16384 // p["segment"] + 16
+    assert p["segment"] % 8 == 0 and p["segments"] == 16384 // p["segment"] + 16
     assert {(plan(1, 64, 64, n)["held"], plan(1, 64, 64, n)["lanes"]) for n in (4, 8, 12, 16, 24, 32, 64, 128)} == {(4, 1), (8, 1), (12, 1), (16, 1), (12, 2), (16, 2), (16, 4), (16, 8)}
     for big in (dict(frames=1 << 50, channels=64), dict(frames=8, channels=1 << 30, batch=1 << 30)):
         with pytest.raises(SrError):
