@@ -371,18 +371,22 @@ __global__ void __launch_bounds__(threads_of(L), kWarps * 32 / threads_of(L)) sr
     if (MODE == kSums && there && p == 0) A.steps[slot * A.channels + ch] = (float)total;
 }
 
-// The states that enter the segments of sequences that have several, from their sums, one thread for a state of a channel.  What enters a segment takes the place of the sum before it,
-// what enters the first that of the last one's, which is not made (state_in may be state_out, which the last segment writes).  Bound by the latency of a load for every eight segments;
-// warps that share a state's segments took longer (24 us instead of 5 for 16 segments of 66660 states, 40 instead of 64 for 512 of 16384).
-constexpr int kJoinThreads = 128, kJoinAhead = 8;
+// The states that enter the segments of sequences that have several, from their sums, one thread for VEC states of a channel.  What enters a segment takes the place of the sum before it,
+// what enters the first that of the last one's, which is not made (state_in may be state_out, which the last segment writes).  Bound by the latency of a load for every AHEAD segments, or, where
+// there are so many states that blocks come in several rounds, by what a block does before its first load: then four states to a thread (16 packed sequences of 1024 channels of 64 states, the
+// whole run: 613 us, with one 629; one sequence of 16384 frames, 1024 channels of 16 states: 209, with one state and 16 segments ahead 198).  Warps that shared a
+// state's segments took 24 us instead of 5 for 16 segments of 66660 states, and less (40, not 64) only for 512 of 16384, which no run is cut into.
+constexpr int kJoinThreads = 128;
+template <int VEC, int AHEAD>
 __global__ void __launch_bounds__(kJoinThreads) sr_scan_join_kernel(const __grid_constant__ ScanArgs A)
 {
     __shared__ int64_t count_of, slot0_of;
     srx::let_successor_start();
     srx::wait_for_predecessor();
-    const int64_t per = (int64_t)A.channels * A.states, mine = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x, i = min(mine, per - 1);
+    const int64_t per = (int64_t)A.channels * A.states, mine = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * VEC, i = min(mine, per - VEC);
     const int64_t ch = per <= 0xFFFFFFFF ? (uint32_t)i / (uint32_t)A.states : i / A.states;
-    const float a2 = srx::decay_base2(A.a[i]);
+    Few<float, VEC> a, h, sum[AHEAD];
+    a.get(A.a + i);
     for (int b = blockIdx.y; b < A.batch; b += gridDim.y) {
         if (A.offsets) {
             if (threadIdx.x < 32) {
@@ -397,29 +401,37 @@ __global__ void __launch_bounds__(kJoinThreads) sr_scan_join_kernel(const __grid
         const int64_t count = A.offsets ? count_of : A.count, slot0 = A.offsets ? slot0_of : b * A.count;
         if (A.offsets) __syncthreads();
         if (count < 2) continue;
-        float h = A.state_in ? A.state_in[b * per + i] : 0.0f;
+        float now[VEC] = {};
+        if (A.state_in) {
+            h.get(A.state_in + b * per + i);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) now[e] = h[e];
+        }
         float* at = A.sums + slot0 * per + i;
         const float* steps = A.steps + slot0 * A.channels + ch;
-        if (mine < per) at[(count - 1) * per] = h;
-        for (int64_t s = 0; s < count - 1; s += kJoinAhead) {      // (the last segment's sums are not made)
-            const int left = (int)min(count - 1 - s, (int64_t)kJoinAhead);
-            float sum[kJoinAhead], step[kJoinAhead];
+        h.set(now);
+        if (mine < per) h.put(at + (count - 1) * per);
+        for (int64_t s = 0; s < count - 1; s += AHEAD) {           // (the last segment's sums are not made)
+            const int left = (int)min(count - 1 - s, (int64_t)AHEAD);
+            float step[AHEAD];
 #pragma unroll
-            for (int k = 0; k < kJoinAhead; ++k) {
+            for (int k = 0; k < AHEAD; ++k) {
                 if (k < left) {
-                    sum[k] = at[k * per];
+                    sum[k].get(at + k * per);
                     step[k] = steps[k * A.channels];
                 }
             }
 #pragma unroll
-            for (int k = 0; k < kJoinAhead; ++k) {
+            for (int k = 0; k < AHEAD; ++k) {
                 if (k < left) {
-                    h = fmaf(srx::exp2_exact(a2 * step[k]), h, sum[k]);
-                    if (mine < per) at[k * per] = h;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) now[e] = fmaf(srx::exp2_exact(srx::decay_base2(a[e]) * step[k]), now[e], sum[k][e]);
+                    h.set(now);
+                    if (mine < per) h.put(at + k * per);
                 }
             }
-            at += kJoinAhead * per;
-            steps += kJoinAhead * A.channels;
+            at += AHEAD * per;
+            steps += AHEAD * A.channels;
         }
     }
 }
@@ -568,7 +580,7 @@ struct ScanCut {
     int held, lanes;
     int64_t segment, slots, whole;                     // segment 0: whole sequences
 };
-// Cycles that cutting costs besides: two launches, a load's latency for every eight segments, and the segments' states, which are written, joined and read (16 bytes each).
+// Cycles that cutting costs besides: two launches, the latency of the join's loads, and the segments' states, which are written, joined and read (16 bytes each).
 double joining(const sr_scan_desc* d, int64_t count) { return 16000.0 + count / 8 * 2000.0 + (double)d->batch * count * d->channels * d->states / 200; }
 // Cycles that `warps` warps, spread over all schedulers, take for a frame; measured for 16 states in bf16 (fp32: 1.5 times as many).  Rounds of four follow each other without a gap, and what one
 // SM is behind in one another makes up for in the next (8192 frames of 8192 channels: 778 us in one round, 736 in two, 697 in four).
@@ -647,9 +659,15 @@ cudaError_t launch_scan(const ScanArgs& A, const ScanCut& c, cudaStream_t s)
     const int64_t grid = c.slots * A.groups * A.tiles;
     if (!c.segment) return launch_mode<T, K, L, kWhole, WIDE>(A, grid, s);
     cudaError_t e = launch_mode<T, K, L, kSums, WIDE>(A, grid, s);
-    const int64_t blocks = ((int64_t)A.channels * A.states + kJoinThreads - 1) / kJoinThreads;
-    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
-    if (e == cudaSuccess) e = start(sr_scan_join_kernel, true, dim3((unsigned)blocks, (unsigned)std::min(A.batch, 65535)), kJoinThreads, 0, s, A);
+    if (e == cudaSuccess) {
+        const int64_t states = (int64_t)A.channels * A.states;
+        auto join = [&](auto* kernel, int vec) {
+            const int64_t blocks = (states / vec + kJoinThreads - 1) / kJoinThreads;
+            return blocks > 0x7FFFFFFF ? cudaErrorInvalidValue : start(kernel, true, dim3((unsigned)blocks, (unsigned)std::min(A.batch, 65535)), kJoinThreads, 0, s, A);
+        };
+        const bool many = (double)states * A.batch >= 4096.0 * sr_device_sms();
+        e = A.quads && many ? join(sr_scan_join_kernel<4, 8>, 4) : join(sr_scan_join_kernel<1, 16>, 1);
+    }
     if (e == cudaSuccess) e = launch_mode<T, K, L, kOutputs, WIDE>(A, grid, s);
     return e;
 }

@@ -244,6 +244,23 @@ def test_scan_packed_cut_where_one_is_long(lengths, dtype):
             assert torch.equal(state[b], kept[b])
 
 
+@pytest.mark.parametrize("states", [16, 15])
+def test_scan_packed_cut_with_many_states(states):
+    lengths = [1, 0, 5] * 14 + [700, 2]
+    at, offsets = spans(lengths)
+    total, C = int(at[-1]), 1024
+    x, o = scan_inputs(total, len(lengths), C, states, 1, "bf16", packed=True)
+    assert 0 < selective.scan_plan(torch.bfloat16, len(lengths), total, C, states, packed=True)["segment"] < 300
+    state = randn(9, len(lengths), C, states)
+    out, last = sr.selective_scan_run(**x, **o, state=state, offsets=offsets)
+    for b in (0, 1, 2, 41, 42, 43):
+        s = slice(at[b], at[b + 1])
+        if lengths[b]:
+            check_scan({k: v if k == "a" else v[s] for k, v in x.items()}, dict(o, z=o["z"][s]), True, state[b], out[s], last[b], b, "bf16")
+        else:
+            assert torch.equal(last[b], state[b])
+
+
 def test_scan_in_segments_of_thousands_of_frames():
     """The same inputs in every frame, so that frame t's state is x (1 - q^t) / (1 - q), q = exp(r a).  A state remembers 1000 frames at most: 32 approximate exponentials (2^-22 each), 1000 / 32
     carries (2^-23, and a rounding, each), the steps' sums (32 roundings of a chunk's, which is 1 over all that is remembered), and a few roundings of the output's sum."""
