@@ -14,7 +14,7 @@
 // Drift.  The approximate exponential is low by 2e-8 in the mean, which a state that loses a thousandth of itself per frame makes 2e-5 of.  So a state is carried over in chunks of
 // 32 frames, by one exponential of their steps' sum that has no bias, and what comes in during a chunk is summed apart: `local`.  That costs a multiply-add for a state and frame and
 // takes the error of states from 2e-6 to 3e-7.  A segment whose states nobody asks for (what enters the next comes from the segments' sums) goes without where its outputs are rounded to
-// bf16: over 1024 frames the bias comes to 2e-5 of a state at most, half a step of bf16 is 4e-3 (a sequence of 16384 frames of 2048 channels: 202 us, with the carry 212).
+// bf16: over 1024 frames the bias comes to 2e-5 of a state at most, half a step of bf16 is 4e-3 (a sequence of 16384 frames of 1024 channels: 202 us, with the carry 212).
 //
 // Long sequences are cut into segments: their sums (without outputs), the states that enter them, their outputs.
 #include <cuda_bf16.h>
@@ -60,7 +60,9 @@ constexpr int kUncarried = 1024;                       // frames that a segment 
 enum { kWhole = 0, kSums = 1, kOutputs = 2 };          // whole sequences; sums of segments; outputs of segments, from the states that enter them
 // A block's threads share b and c, whose widening is the more to do the more states there are; fewer make the work of SMs more even.
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes < 4 ? 32 : 128; }
-constexpr int kWarps = 16;                             // of an SM, so 128 registers (168 and 12 warps: 64 states 630 us instead of 616, 300 frames of 16 sequences 138 instead of 129; 128 states 224 instead of 232)
+// Of an SM, so 128 registers.  With 12 warps and 168: 16 packed sequences, 1024 channels of 64 states 630 us instead of 616, side by side with 300 frames each 138 instead of 129, of 128 states 224
+// instead of 232.
+constexpr int kWarps = 16;
 
 // Frames of a segment of this run.
 __device__ __forceinline__ int64_t segment_of(const ScanArgs& A)
