@@ -27,7 +27,8 @@ __device__ __forceinline__ float reciprocal(float x)
 
 // 2^x for two values, to the last bit but one, and without a bias: what a state is multiplied with over thousands of frames may not drift (ex2 is low by 2e-8 in the mean, which
 // a state that loses a thousandth of itself per frame makes 2e-5 of).  x = n + f, |f| <= 1/2, by adding 1.5 * 2^23; 2^f = 1 + f q(f) with q of degree 4 for the smallest
-// largest error of f q(f) (9e-8 f, by Remez' exchange); n goes into the exponent.  Below -126: 2^-126; from 128 on: 2^128 but a little; a NaN stays one.
+// largest error of f q(f) (9e-8 f, by Remez' exchange); n goes into the exponent.  Below -126: 2^-126; from 128 on: 2^128 but a little.  A NaN stays one: its bits and the exponent's could
+// add up to any number, so it is chosen at the end.
 __device__ __forceinline__ Pair exp2_exact(Pair x)
 {
     const float2 v = split(x);
@@ -44,7 +45,8 @@ __device__ __forceinline__ Pair exp2_exact(Pair x)
     q = fma2(q, f, pair(0.24022235f, 0.24022235f));
     q = fma2(q, f, pair(0.69314724f, 0.69314724f));
     const float2 m = split(fma2(q, f, pair(1.0f, 1.0f))), n = split(t);
-    return pair(__float_as_uint(m.x) + (__float_as_uint(n.x) << 23), __float_as_uint(m.y) + (__float_as_uint(n.y) << 23));
+    const float a = __uint_as_float(__float_as_uint(m.x) + (__float_as_uint(n.x) << 23)), b = __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(n.y) << 23));
+    return pair(v.x != v.x ? v.x : a, v.y != v.y ? v.y : b);
 }
 __device__ __forceinline__ float exp2_exact(float x) { return split(exp2_exact(pair(x, x))).x; }
 

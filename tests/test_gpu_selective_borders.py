@@ -1,0 +1,88 @@
+"""The selective head's operators where they can go wrong: what is not finite, frame by frame and in runs."""
+import pytest
+import torch
+
+import paper_1806_04965_b200 as sr
+from paper_1806_04965_b200 import selective
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+DEV = "cuda:0"
+NAN = float("nan")
+
+
+def randn(seed, *shape, dtype="fp32"):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(DT[dtype]).to(DEV)
+
+
+def inputs(lead, channels, states, groups, dtype, gap=0, seed=0):
+    """gap: elements ahead of b in the rows that b and c are taken from."""
+    low = randn(seed + 1, *lead, gap + 2 * groups * states, dtype=dtype)
+    b, c = (low[..., gap + k * groups * states:gap + (k + 1) * groups * states].unflatten(-1, (groups, states)) for k in (0, 1))
+    a = -torch.arange(1, states + 1, device=DEV).float() * torch.exp(0.2 * randn(seed + 3, channels, states))
+    return dict(u=randn(seed + 2, *lead, channels, dtype=dtype), dt=randn(seed + 4, *lead, channels, dtype=dtype), a=a.contiguous(), b=b, c=c,
+                d=randn(seed + 5, channels), z=randn(seed + 7, *lead, channels, dtype=dtype), dt_bias=randn(seed + 6, channels) - 3.0)
+
+
+# ------------------------------------------------------------------------------------------ what is not finite
+# What is NaN: where in the tensor, and what of the states [sequences][channels][states] and outputs [sequences][channels] is NaN then.  (Two groups of channels, channel 3 in the first.)
+def reaches(what, batch, channels, states):
+    h = torch.zeros(batch, channels, states, dtype=torch.bool, device=DEV)
+    y = torch.zeros(batch, channels, dtype=torch.bool, device=DEV)
+    half = channels // 2
+    place = {"a": (3, 1), "u": (1, 3), "dt": (1, 3), "z": (1, 3), "b": (1, 0, 1), "c": (1, 0, 1), "d": (3,), "dt_bias": (3,), "state": (1, 3, 1)}[what]
+    if what == "a":
+        h[:, 3, 1] = True
+    elif what in ("u", "dt"):
+        h[1, 3] = True
+    elif what == "dt_bias":
+        h[:, 3] = True
+    elif what == "b":
+        h[1, :half, 1] = True
+    elif what == "state":
+        h[1, 3, 1] = True
+    elif what == "c":
+        y[1, :half] = True
+    elif what == "z":
+        y[1, 3] = True
+    else:
+        y[:, 3] = True
+    return place, h, y | h.any(-1)
+
+
+NOT_FINITE = ["a", "u", "dt", "z", "b", "c", "d", "dt_bias", "state"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("batch,states,gap", [(2, 16, 0), (20, 16, 0), (3, 5, 3), (4, 20, 5), (3, 100, 1), (2, 128, 0)])
+@pytest.mark.parametrize("what", NOT_FINITE)
+def test_single_frames_keep_what_is_not_a_number(what, batch, states, gap, dtype):
+    channels = 12
+    place, bad_h, bad_y = reaches(what, batch, channels, states)
+    for entering in (torch.zeros(batch, channels, states, device=DEV), randn(9, batch, channels, states)):
+        x = inputs((batch,), channels, states, 2, dtype, gap)
+        clean = entering.clone()
+        want = sr.selective_scan_step(state=clean, **x)
+        state = entering.clone()
+        dict(x, state=state)[what][place] = NAN
+        _, run = sr.selective_scan_run(**{k: v if k in ("a", "d", "dt_bias") else v[None] for k, v in x.items()}, state=state.clone())
+        out = sr.selective_scan_step(state=state, **x)
+        assert torch.equal(torch.isnan(state), bad_h) and torch.equal(torch.isnan(out), bad_y) and torch.equal(torch.isnan(run), bad_h)
+        assert torch.equal(state[~bad_h], clean[~bad_h]) and torch.equal(out[~bad_y], want[~bad_y])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("frames,states", [(40, 16), (40, 5), (333, 12), (333, 32), (333, 128)])
+@pytest.mark.parametrize("what", ["a", "d", "dt_bias", "state"])
+def test_runs_keep_what_is_not_a_number(what, frames, states, dtype):
+    channels, batch = 12, 2
+    assert (selective.scan_plan(DT[dtype], batch, frames, channels, states, 2)["segment"] > 0) == (frames > 40)
+    place, bad_h, bad_y = reaches(what, batch, channels, states)
+    for entering in (torch.zeros(batch, channels, states, device=DEV), randn(9, batch, channels, states)):
+        x = inputs((frames, batch), channels, states, 2, dtype)
+        want, clean = sr.selective_scan_run(state=entering, **x)
+        state = entering.clone()
+        dict(x, state=state)[what][place] = NAN
+        out, last = sr.selective_scan_run(state=state, **x)
+        assert torch.equal(torch.isnan(last), bad_h) and torch.equal(torch.isnan(out), bad_y.expand_as(out))
+        assert torch.equal(last[~bad_h], clean[~bad_h]) and torch.equal(out[:, ~bad_y], want[:, ~bad_y])
