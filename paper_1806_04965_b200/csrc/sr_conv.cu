@@ -337,8 +337,8 @@ cudaError_t launch(const ConvArgs& A, int width, bool step, cudaStream_t s)
 
 sr_status check(const sr_conv_desc* d)
 {
-    if (!d || (d->dtype != SR_DTYPE_F32 && d->dtype != SR_DTYPE_BF16) || d->batch < 0 || d->channels < 1 || d->width < 1 || d->frames < 0 || (d->act != 0 && d->act != 1) ||
-        d->x.frame < 0 || d->x.sequence < 0 || d->out.frame < 0 || d->out.sequence < 0)
+    if (!d || (d->dtype != SR_DTYPE_F32 && d->dtype != SR_DTYPE_BF16) || d->batch < 0 || d->batch > kMostSequences || d->channels < 1 || d->width < 1 ||
+        d->frames < 0 || (d->act != 0 && d->act != 1) || d->x.frame < 0 || d->x.sequence < 0 || d->out.frame < 0 || d->out.sequence < 0)
         return SR_ERR_INVALID_ARG;
     if ((double)d->frames * d->channels > 0x1p45 || (double)d->batch * d->channels * d->width > 0x1p45) return SR_ERR_INVALID_ARG;          // (no memory holds them)
     return d->width > 8 ? SR_ERR_UNSUPPORTED : SR_OK;

@@ -732,8 +732,8 @@ bool fits(const sr_attention_strides& s) { return s.frame >= 0 && s.sequence >= 
 
 sr_status check(const sr_scan_desc* d)
 {
-    if (!d || (d->dtype != SR_DTYPE_F32 && d->dtype != SR_DTYPE_BF16) || d->batch < 0 || d->channels < 1 || d->states < 1 || d->groups < 1 ||
-        d->channels % d->groups || d->frames < 0 || (d->softplus != 0 && d->softplus != 1) || !fits(d->u) || !fits(d->dt) || !fits(d->z) || !fits(d->out) || !fits(d->b) ||
+    if (!d || (d->dtype != SR_DTYPE_F32 && d->dtype != SR_DTYPE_BF16) || d->batch < 0 || d->batch > kMostSequences || d->channels < 1 || d->states < 1 ||
+        d->groups < 1 || d->channels % d->groups || d->frames < 0 || (d->softplus != 0 && d->softplus != 1) || !fits(d->u) || !fits(d->dt) || !fits(d->z) || !fits(d->out) || !fits(d->b) ||
         !fits(d->c))
         return SR_ERR_INVALID_ARG;
     if (d->states > 128) return SR_ERR_UNSUPPORTED;

@@ -8,6 +8,8 @@
 struct FrameSpan {
     int64_t first, n, b;
 };
+// Searches and rounds over the sequences count up to 65535 places further in 32 bits.
+constexpr int32_t kMostSequences = 0x7FFF0000;
 
 #ifdef __CUDACC__
 // offsets NULL: sequences of `frames` frames side by side.  Offsets outside 0 .. frames are taken as the nearest of the two, a decreasing one as an empty sequence.

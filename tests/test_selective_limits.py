@@ -1,0 +1,26 @@
+"""What the selective head's calls in C refuse at their limits: nothing here reaches a GPU."""
+import ctypes
+
+import pytest
+
+from paper_1806_04965_b200 import selective
+from tests.test_selective_cpu import INVALID, conv_desc, conv_run, conv_step, scan_desc, scan_run, scan_step
+
+P3 = ctypes.c_void_p(1 << 23)
+
+
+@pytest.mark.parametrize("batch", [(1 << 31) - (1 << 16) + 1, (1 << 31) - 31, (1 << 31) - 1])
+def test_sequences_that_32_bits_cannot_count_past_are_refused(batch):
+    """A search over the sequences adds 31 to their number, a launch over them 65534."""
+    small = dict(batch=batch, channels=1)
+    strides = dict(x=(batch, 1), out=(batch, 1))
+    assert conv_run(conv_desc(width=2, frames=4, **small, **strides), offsets=P3) == INVALID
+    assert conv_run(conv_desc(width=2, frames=4, **small, **strides)) == INVALID
+    assert conv_step(conv_desc(width=2, **small, **strides)) == INVALID
+    d = scan_desc(states=1, groups=1, frames=40, **small)
+    size, plan = ctypes.c_size_t(), selective._ScanPlan()
+    assert scan_run(d, offsets=P3) == INVALID and scan_run(d) == INVALID and scan_step(d) == INVALID
+    for packed in (0, 1):
+        assert selective._library().sr_selective_scan_workspace_bytes(ctypes.byref(d), packed, ctypes.byref(size)) == INVALID
+        assert selective._library().sr_selective_scan_plan(ctypes.byref(d), packed, 148, ctypes.byref(plan)) == INVALID
+    assert selective._library().sr_selective_scan_plan(ctypes.byref(scan_desc(batch=(1 << 31) - (1 << 16), channels=1, states=1, groups=1, frames=1)), 0, 148, ctypes.byref(plan)) == 0
