@@ -388,7 +388,8 @@ sr_status sr_linear_attention_step(const sr_attention_desc* desc, const void* q_
 /*
  * Selective head: blocks of a projection, a short convolution over the frames, a selective scan and the way back onto the stream.
  * Conventions are those of the temporal head's operators; sequences side by side or packed (offsets) as in sr_linear_attention_run, but outputs and states are
- * undefined where offsets decrease.  There are at most 2^31 - 2^16 sequences.
+ * undefined where offsets decrease.  There are at most 2^31 - 2^16 sequences.  Inputs may repeat by strides (0, for one); frames and sequences of outputs lie at least their channels
+ * apart.
  *
  * Causal convolution of every channel over the frames:
  *     out[t, c] = act(bias[c] + sum_{j < width} weight[c, j] * x[t - (width - 1) + j, c]),   act: 0 identity, 1 x * sigmoid(x).

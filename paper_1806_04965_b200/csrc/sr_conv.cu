@@ -348,7 +348,9 @@ bool aligned(const void* p, int dtype) { return !((uintptr_t)p & (dtype == SR_DT
 sr_status call(const sr_conv_desc* d, const void* x, const float* weight, const float* bias, const int64_t* offsets, const void* state_in, void* state_out, void* out,
                bool step, cudaStream_t s)
 {
-    if (!x || !weight || !out || !aligned(x, d->dtype) || !aligned(out, d->dtype) || ((uintptr_t)weight & 3) || ((uintptr_t)bias & 3) || out == x) return SR_ERR_INVALID_ARG;
+    if (!x || !weight || !out || !aligned(x, d->dtype) || !aligned(out, d->dtype) || ((uintptr_t)weight & 3) || ((uintptr_t)bias & 3) || out == x ||
+        frames_overlap(d->out.frame, d->out.sequence, step ? 1 : d->frames, offsets ? 1 : d->batch, d->channels))
+        return SR_ERR_INVALID_ARG;
     ConvArgs A{};
     A.x = x;
     A.weight = weight;

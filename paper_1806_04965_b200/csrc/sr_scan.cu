@@ -816,6 +816,7 @@ sr_status sr_selective_scan_run(const sr_scan_desc* d, const void* u, const void
                                                                                : cudaMemsetAsync(state_out, 0, bytes, s);
         return e == cudaSuccess ? SR_OK : SR_ERR_CUDA;
     }
+    if (frames_overlap(d->out.frame, d->out.sequence, d->frames, offsets ? 1 : d->batch, d->channels)) return SR_ERR_INVALID_ARG;
     const ScanCut cut = scan_cut(d, offsets != nullptr, sr_device_sms());
     const size_t needed = cut_bytes(d, cut);
     if (needed && (!workspace || workspace_bytes < needed || ((uintptr_t)workspace & 255))) return SR_ERR_INVALID_ARG;
@@ -840,7 +841,8 @@ sr_status sr_selective_scan_step(const sr_scan_desc* d, const void* u, const voi
     if (st != SR_OK) return st;
     if (!d->batch) return SR_OK;
     ScanArgs A{};
-    if (!tensors(d, A, u, dt, a, b, c, skip, z, bias, out) || !state || ((uintptr_t)state & 3)) return SR_ERR_INVALID_ARG;
+    if (!tensors(d, A, u, dt, a, b, c, skip, z, bias, out) || !state || ((uintptr_t)state & 3) || frames_overlap(0, d->out.sequence, 1, d->batch, d->channels))
+        return SR_ERR_INVALID_ARG;
     A.state_out = state;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = d->dtype == SR_DTYPE_F32 ? launch_step<float>(A, s) : launch_step<__nv_bfloat16>(A, s);

@@ -11,6 +11,12 @@ struct FrameSpan {
 // Searches and rounds over the sequences count up to 65535 places further in 32 bits.
 constexpr int32_t kMostSequences = 0x7FFF0000;
 
+// Whether neighbouring frames or sequences of `channels` elements would be written on top of each other.
+inline bool frames_overlap(int64_t frame, int64_t sequence, int64_t frames, int64_t batch, int64_t channels)
+{
+    return (frames > 1 && frame < channels) || (batch > 1 && sequence < channels);
+}
+
 #ifdef __CUDACC__
 // offsets NULL: sequences of `frames` frames side by side.  Offsets outside 0 .. frames are taken as the nearest of the two, a decreasing one as an empty sequence.
 __device__ __forceinline__ FrameSpan frame_span(const int64_t* offsets, int64_t frames, int64_t b)

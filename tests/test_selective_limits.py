@@ -24,3 +24,13 @@ def test_sequences_that_32_bits_cannot_count_past_are_refused(batch):
         assert selective._library().sr_selective_scan_workspace_bytes(ctypes.byref(d), packed, ctypes.byref(size)) == INVALID
         assert selective._library().sr_selective_scan_plan(ctypes.byref(d), packed, 148, ctypes.byref(plan)) == INVALID
     assert selective._library().sr_selective_scan_plan(ctypes.byref(scan_desc(batch=(1 << 31) - (1 << 16), channels=1, states=1, groups=1, frames=1)), 0, 148, ctypes.byref(plan)) == 0
+
+
+@pytest.mark.parametrize("run,step,desc,channels", [(conv_run, conv_step, conv_desc, 64), (scan_run, scan_step, scan_desc, 64)], ids=["conv", "scan"])
+def test_outputs_on_top_of_each_other_are_refused(run, step, desc, channels):
+    for frame, sequence in ((0, channels), (channels - 1, 1000), (2 * channels, 0), (2 * channels, channels - 1), (0, 0)):
+        assert run(desc(out=(frame, sequence))) == INVALID, (frame, sequence)
+    for frame in (0, 1, channels - 1):
+        assert run(desc(out=(frame, channels)), offsets=P3) == INVALID, frame
+    for sequence in (0, channels - 1):
+        assert step(desc(out=(0, sequence))) == INVALID, sequence
