@@ -65,16 +65,20 @@ __device__ __forceinline__ void find_slot(const int64_t* offsets, int64_t frames
         before += __shfl_sync(0xFFFFFFFFu, sum, 31);
     }
 }
-// The frames of the longest sequence.  (All lanes of a warp.)
-__device__ __forceinline__ int64_t longest_span(const int64_t* offsets, int64_t frames, int batch)
+// The largest of a warp's values.
+__device__ __forceinline__ int64_t most_of_warp(int64_t most)
 {
-    if (!offsets) return frames;
-    int64_t most = 0;
-#pragma unroll 8
-    for (int i = threadIdx.x & 31; i < batch; i += 32) most = max(most, frame_span(offsets, frames, i).n);
 #pragma unroll
     for (int d = 16; d; d /= 2) most = max(most, (int64_t)__shfl_xor_sync(0xFFFFFFFFu, most, d));
     return most;
+}
+// The frames of the longest of the packed sequences first, first + step and so on of a warp's lanes together.  (All of them.)
+__device__ __forceinline__ int64_t longest_span(const int64_t* offsets, int64_t frames, int batch, int first, int step)
+{
+    int64_t most = 0;
+#pragma unroll 8
+    for (int i = first; i < batch; i += step) most = max(most, frame_span(offsets, frames, i).n);
+    return most_of_warp(most);
 }
 // Packed sequences, slots that need no sum over the sequences before: sequence b has those from offsets[b] / segment + b on, as many as its segments at least, and all of them are
 // frames / segment + batch.

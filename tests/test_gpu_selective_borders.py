@@ -86,3 +86,35 @@ def test_runs_keep_what_is_not_a_number(what, frames, states, dtype):
         out, last = sr.selective_scan_run(state=state, **x)
         assert torch.equal(torch.isnan(last), bad_h) and torch.equal(torch.isnan(out), bad_y.expand_as(out))
         assert torch.equal(last[~bad_h], clean[~bad_h]) and torch.equal(out[:, ~bad_y], want[:, ~bad_y])
+
+
+# ------------------------------------------------------------------------------------------ many packed sequences
+@pytest.mark.parametrize("longest", [2000, 3], ids=["one_long", "none_long"])
+def test_packed_sequences_more_than_a_launch_has_rows(longest):
+    """More than 65535, the long one among the last; and in a time that grows with the sequences, not with their square (70000 of them, each looked at by a block for each: seconds)."""
+    import numpy as np
+    from tests.test_gpu_selective import check_scan, spans
+    rng = np.random.default_rng(7)
+    B, C, N = 70000, 8, 4
+    lengths = rng.integers(0, 4, B)
+    lengths[66001] = longest
+    at, offsets = spans(lengths)
+    total = int(at[-1])
+    assert selective.scan_plan(torch.float32, B, total, C, N, 1, packed=True)["segment"] > 0
+    x = inputs((total,), C, N, 1, "fp32")
+    o = {k: x.pop(k) for k in ("d", "z", "dt_bias")}
+    state = randn(9, B, C, N)
+    entering = state.clone()
+    sr.selective_scan_run(**x, **o, state=state, offsets=offsets)
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    out, last = sr.selective_scan_run(**x, **o, state=state, offsets=offsets, state_out=state)
+    end.record()
+    end.synchronize()
+    assert begin.elapsed_time(end) < 30.0
+    for b in [0, 1, 2, *range(3, B, 3511), 65534, 65535, 65536, 66000, 66001, 66002, B - 1]:
+        s = slice(at[b], at[b + 1])
+        if lengths[b]:
+            check_scan({k: v if k == "a" else v[s] for k, v in x.items()}, dict(o, z=o["z"][s]), True, entering[b], out[s], last[b], b, "fp32")
+        else:
+            assert torch.equal(last[b], entering[b])
