@@ -215,7 +215,7 @@ def test_calls_without_the_compiled_module_are_the_same(monkeypatch):
             y, p = scan_inputs((60, B), C, N, G, dtype, seed=20)
             state, taps, w, bias = randn(9, B, C, N), randn(10, B, 3, C, dtype=dtype), randn(11, C, 4), randn(12, C)
             kept, conv = torch.full((T, C), 7.0, dtype=DT[dtype], device=DEV), torch.full((T, C), 7.0, dtype=DT[dtype], device=DEV)
-            got += sr.selective_scan_run(**x, **o, state=state, offsets=offsets) + sr.selective_scan_run(**y, **p) + sr.selective_scan_run(**y, softplus=False, d=p["d"])
+            got += sr.selective_scan_run(**x, **o, state=state, offsets=offsets) + sr.selective_scan_run(**y, **p) + sr.selective_scan_run(**y, softplus=False, d=p["d"])         # (the last one grows beyond all bounds)
             got += sr.causal_conv_run(x["u"], w, bias=bias, silu=True, state=taps, offsets=offsets) + sr.causal_conv_run(y["u"], w)
             got.append(sr.selective_scan_step(*(v if k == "a" else v[0] for k, v in y.items()), state, d=p["d"], z=p["z"][0], dt_bias=p["dt_bias"]))
             got.append(sr.causal_conv_step(y["u"][0], w, taps, bias=bias, silu=True))
@@ -231,7 +231,8 @@ def test_calls_without_the_compiled_module_are_the_same(monkeypatch):
                 got += h if isinstance(h, tuple) else (h,)
             for format in ("mx4", "mx8"):
                 m, h = sr.block_norm(r[:, :70], r[:, 3:73], gate=None, format=format)
-                got += [m.data, m.scales, m.values(), h]
+                got += [m.data, m.values(), h]                # (scales are padded to whole tiles with anything)
         results.append(got)
     assert len(results[0]) == len(results[1])
-    assert all(torch.equal(a, b) and a.dtype is b.dtype for a, b in zip(*results))
+    for k, (a, b) in enumerate(zip(*results)):
+        torch.testing.assert_close(a, b, rtol=0, atol=0, equal_nan=True, msg=str(k))
