@@ -482,7 +482,8 @@ class TemporalHead(_Head):
             w[name] = quantize(w[name], format)
         self._w = w
         self.scale = float(dk) ** -0.5
-        self.state = torch.zeros((batch, groups, dk, dv), dtype=torch.float32, device=device)
+        with torch.inference_mode(False):              # (a state of inference mode could not be written outside of it)
+            self.state = torch.zeros((batch, groups, dk, dv), dtype=torch.float32, device=device)
 
     @property
     def device(self):

@@ -376,8 +376,9 @@ class SelectiveHead(_Head):
                 b[name] = quantize(b[name], format)
         w["out"] = quantize(w["out"], format)
         self._w, self._blocks = w, blocks
-        self._states = [(torch.zeros((batch, width - 1, inner), dtype=self.tdtype, device=self.device),
-                         torch.zeros((batch, inner, states), dtype=torch.float32, device=self.device)) for _ in blocks]
+        with torch.inference_mode(False):              # (states of inference mode could not be written outside of it)
+            self._states = [(torch.zeros((batch, width - 1, inner), dtype=self.tdtype, device=self.device),
+                             torch.zeros((batch, inner, states), dtype=torch.float32, device=self.device)) for _ in blocks]
 
     def reset(self):
         """Before the first frame: no memory."""

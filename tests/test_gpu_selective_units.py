@@ -236,3 +236,21 @@ def test_calls_without_the_compiled_module_are_the_same(monkeypatch):
     assert len(results[0]) == len(results[1])
     for k, (a, b) in enumerate(zip(*results)):
         torch.testing.assert_close(a, b, rtol=0, atol=0, equal_nan=True, msg=str(k))
+
+
+@pytest.mark.parametrize("kind", ["selective", "temporal"])
+def test_heads_made_in_inference_mode_run_outside_of_it(kind):
+    from tests.test_operator_refusals import weights
+    with torch.inference_mode():
+        head = sr.SelectiveHead(head_weights(32, 32, 8, 2, 4, 1, 3, 1), 32, 32, 8, 2, 4, 2) if kind == "selective" else sr.TemporalHead(weights(channels=32), 32, 4, 2, 32, 48, 2)
+        x = randn(2, 5, 2, 32)
+        one = head.run(x)
+        head.reset()
+    assert torch.equal(head.run(x), one)
+    state = head.get_state()
+    head.reset()
+    assert torch.equal(head.run(x), one)
+    head.set_state(state)
+    with torch.inference_mode():
+        head.reset()
+        assert torch.equal(head.run(x), one)
