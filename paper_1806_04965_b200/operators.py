@@ -130,6 +130,12 @@ def _written(*tensors):
             torch.autograd.graph.increment_version(t)
 
 
+def _counts(call: str, *sizes):
+    """Sizes that the calls in C take in 32 bits (ctypes would cut them off)."""
+    if max(sizes) > 0x7FFFFFFF:
+        _refuse(call, "a size is out of range")
+
+
 def _float_vector(call: str, name: str, t, n: int):
     if t is None:
         return None
@@ -326,6 +332,7 @@ def _desc(call: str, device: int, q, k, v, log_decay, packed: bool, step: bool, 
             s.frame, s.sequence, s.head = st[0], st[1], st[2]
         return s
 
+    _counts(call, batch, heads, groups, dk, dv)
     out = tuple(q.shape[:-1]) + (dv,)                # without gaps
     d = _AttentionDesc(_DTYPES[q.dtype], batch, heads, groups, dk, dv, 1 if step else q.shape[0], scale, strides(q.stride()), strides(k.stride()),
                        strides(v.stride()), strides(tuple(math.prod(out[i + 1:]) for i in range(len(out)))))
@@ -344,6 +351,7 @@ def _desc(call: str, device: int, q, k, v, log_decay, packed: bool, step: bool, 
 
 def attention_plan(dtype, batch: int, frames: int, heads: int, groups: int, dk: int, dv: int, packed: bool = False, sms: int = 0) -> dict:
     """How a run over tensors of these sizes is cut (sr_linear_attention_plan) on the current device or one of `sms` SMs; packed: `frames` in all."""
+    _counts("attention_plan", batch, heads, groups, dk, dv)
     d = _AttentionDesc(_DTYPES[dtype], batch, heads, groups, dk, dv, frames, 1.0)
     p = _AttentionPlan()
     code = _library().sr_linear_attention_plan(ctypes.byref(d), 1 if packed else 0, sms, ctypes.byref(p))

@@ -18,7 +18,7 @@ import torch
 
 from . import operators as ops
 from .binding import SrError
-from .operators import FORMATS, Microscaled, _call, _DTYPES, _float_vector, _Head, _refuse, _rows, _Strides, _tensors, _written, product, quantize, rms_norm
+from .operators import FORMATS, Microscaled, _call, _counts, _DTYPES, _float_vector, _Head, _refuse, _rows, _Strides, _tensors, _written, product, quantize, rms_norm
 
 _compiled = ops._compiled
 _GATES = {"none": 0, "sigmoid": 1, "silu": 2}
@@ -130,6 +130,7 @@ def _conv_desc(call: str, x, weight, bias, silu, lead: int, step: bool, batch: i
         _refuse(call, "the weight has to be [channels][width]")
     _matrix(call, "the weight", weight, (channels, weight.shape[1]))
     _float_vector(call, "the bias", bias, channels)
+    _counts(call, batch, channels, weight.shape[1])
     return _ConvDesc(_DTYPES[x.dtype], batch, channels, weight.shape[1], 1 if silu else 0, 1 if step else x.shape[0], _strides(x, lead, step), _strides(out, lead, step))
 
 
@@ -200,6 +201,7 @@ def _scan_desc(call: str, u, dt, a, b, c, d, z, dt_bias, softplus, lead: int, st
     _matrix(call, "a", a, (channels, states))
     _float_vector(call, "d", d, channels)
     _float_vector(call, "dt_bias", dt_bias, channels)
+    _counts(call, batch, channels, states, groups)
     return _ScanDesc(_DTYPES[u.dtype], batch, channels, states, groups, 1 if softplus else 0, 1 if step else u.shape[0], _strides(u, lead, step), _strides(dt, lead, step),
                      _FrameStrides() if z is None else _strides(z, lead, step), _strides(out, lead, step), _strides(b, lead, step, 2), _strides(c, lead, step, 2))
 
@@ -266,6 +268,7 @@ def selective_scan_step(u, dt, a, b, c, state, d=None, z=None, dt_bias=None, sof
 
 def scan_plan(dtype, batch: int, frames: int, channels: int, states: int, groups: int = 1, packed: bool = False, sms: int = 0) -> dict:
     """How a run over tensors of these sizes is cut (sr_selective_scan_plan) on the current device or one of `sms` SMs; packed: `frames` in all."""
+    _counts("scan_plan", batch, channels, states, groups)
     d = _ScanDesc(_DTYPES[dtype], batch, channels, states, groups, 1, frames)
     p = _ScanPlan()
     code = _library().sr_selective_scan_plan(ctypes.byref(d), 1 if packed else 0, sms, ctypes.byref(p))

@@ -2,8 +2,9 @@
 import ctypes
 
 import pytest
+import torch
 
-from paper_1806_04965_b200 import selective
+from paper_1806_04965_b200 import SrError, operators, selective
 from tests.test_selective_cpu import INVALID, conv_desc, conv_run, conv_step, scan_desc, scan_run, scan_step
 
 P3 = ctypes.c_void_p(1 << 23)
@@ -34,3 +35,17 @@ def test_outputs_on_top_of_each_other_are_refused(run, step, desc, channels):
         assert run(desc(out=(frame, channels)), offsets=P3) == INVALID, frame
     for sequence in (0, channels - 1):
         assert step(desc(out=(0, sequence))) == INVALID, sequence
+
+
+def test_sizes_beyond_32_bits_are_not_cut_off():
+    """2^32 + 5 sequences are not 5."""
+    many = (1 << 32) + 5
+    x, w, a, b = torch.zeros(1, 1, 1).expand(1, many, 1), torch.zeros(1, 1), torch.zeros(1, 1), torch.zeros(1, 1, 1, 1).expand(1, many, 1, 1)
+    calls = [lambda: selective._conv_desc("causal_conv_run", x, w, None, False, 2, False, many, x), lambda: selective._conv_desc("causal_conv_step", x[0], w, None, False, 1, True, many, x[0]),
+             lambda: selective._scan_desc("selective_scan_run", x, x, a, b, b, None, None, None, True, 2, False, many, x),
+             lambda: selective.scan_plan(torch.float32, many, 1, 1, 1, sms=148), lambda: selective.scan_plan(torch.float32, 1, 1, many, 1, sms=148),
+             lambda: operators.attention_plan(torch.float32, many, 1, 1, 1, 8, 8, sms=148), lambda: operators.attention_plan(torch.float32, 1, 1, 1, 1, 8, many, sms=148)]
+    for k, call in enumerate(calls):
+        with pytest.raises(SrError):
+            call()
+            pytest.fail("call %d was taken" % k)
