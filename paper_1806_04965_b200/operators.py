@@ -441,7 +441,7 @@ class _Head:
     """What heads behind a rollout share: `batch` sequences, `channels` features of a frame, and a device."""
 
     def _fits(self, call: str, features, lead: int):
-        if features.dim() <= lead or features.shape[lead - 1] != self.batch or math.prod(features.shape[lead:]) != self.channels:
+        if not isinstance(features, torch.Tensor) or features.dim() <= lead or features.shape[lead - 1] != self.batch or math.prod(features.shape[lead:]) != self.channels:
             _refuse("%s.%s" % (type(self).__name__, call), "the head takes %s[%d sequences][%d channels]" % ("[frames]" if lead == 2 else "", self.batch, self.channels))
 
     def check_features(self, shape, device):
@@ -505,7 +505,7 @@ class TemporalHead(_Head):
         return self.state.clone()
 
     def set_state(self, state):
-        if state.shape != self.state.shape or state.dtype is not torch.float32:
+        if not isinstance(state, torch.Tensor) or state.shape != self.state.shape or state.dtype is not torch.float32:
             _refuse("TemporalHead.set_state", "the state has to be float32 %s" % (tuple(self.state.shape),))
         self.state.copy_(state)
 

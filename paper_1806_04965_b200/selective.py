@@ -394,8 +394,10 @@ class SelectiveHead(_Head):
         return [(conv.clone(), scan.clone()) for conv, scan in self._states]
 
     def set_state(self, state):
-        if len(state) != len(self._states) or any(len(s) != 2 or s[0].shape != c.shape or s[0].dtype is not c.dtype or s[1].shape != h.shape or s[1].dtype is not h.dtype
-                                                  for s, (c, h) in zip(state, self._states)):
+        def fits(given, own):
+            return isinstance(given, (list, tuple)) and len(given) == 2 and all(isinstance(t, torch.Tensor) and t.shape == o.shape and t.dtype is o.dtype for t, o in zip(given, own))
+
+        if not isinstance(state, (list, tuple)) or len(state) != len(self._states) or not all(map(fits, state, self._states)):
             _refuse("SelectiveHead.set_state", "the state has to be what get_state gives")
         for s, (conv, scan) in zip(state, self._states):
             conv.copy_(s[0])

@@ -118,3 +118,116 @@ def test_packed_sequences_more_than_a_launch_has_rows(longest):
             check_scan({k: v if k == "a" else v[s] for k, v in x.items()}, dict(o, z=o["z"][s]), True, entering[b], out[s], last[b], b, "fp32")
         else:
             assert torch.equal(last[b], entering[b])
+
+
+def test_packed_sequences_captured_with_other_lengths():
+    """The sizes say how a run is cut; what is long is found when it is replayed."""
+    from tests.test_gpu_selective import check_scan
+    B, T, C, N = 300, 1200, 8, 4
+    x = inputs((T,), C, N, 1, "fp32")
+    o = {k: x.pop(k) for k in ("d", "z", "dt_bias")}
+    state = randn(9, B, C, N)
+    offsets = torch.arange(B + 1, device=DEV) * 4
+    assert selective.scan_plan(torch.float32, B, T, C, N, packed=True)["segment"] > 0
+    sr.selective_scan_run(**x, **o, state=state, offsets=offsets)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, last = sr.selective_scan_run(**x, **o, state=state, offsets=offsets)
+    one_long = torch.full((B,), 2, device=DEV)
+    one_long[211] = T - 2 * (B - 1)
+    for lengths in (torch.full((B,), 4, device=DEV), one_long, torch.full((B,), 4, device=DEV)):
+        offsets[1:] = lengths.cumsum(0)
+        out.fill_(float("nan"))
+        graph.replay()
+        at = offsets.tolist()
+        assert torch.isfinite(out).all()
+        for b in (0, 1, 210, 211, 212, 299):
+            s = slice(at[b], at[b + 1])
+            check_scan({k: v if k == "a" else v[s] for k, v in x.items()}, dict(o, z=o["z"][s]), True, state[b], out[s], last[b], b, "fp32")
+
+
+# ------------------------------------------------------------------------------------------ sizes
+def test_places_beyond_32_bits():
+    """More than 2^31 elements: the last frames, or sequences, are those of a call on them alone."""
+    T, C, W, tail = 1 << 19, 4104, 4, 3000
+    x = torch.empty(T, 1, C, dtype=torch.bfloat16, device=DEV)
+    x.view(-1, 64, C)[:] = randn(1, 64, C, dtype="bf16")
+    x[-tail:] = randn(2, tail, 1, C, dtype="bf16")
+    assert x.numel() > 1 << 31
+    w = randn(3, C, W)
+    out, last = sr.causal_conv_run(x, w, silu=True)
+    part, left = sr.causal_conv_run(x[-tail - 3:], w, silu=True)
+    assert torch.equal(out[-tail:], part[3:]) and torch.equal(last, left)
+    del out
+    # states that lose two thirds of themselves in a frame at least: 200 frames later nothing is left of what came before
+    a, bc, dt = -1.0 - torch.rand(C, 4, device=DEV), randn(4, 1, 1, 1, 4, dtype="bf16").expand(T, 1, 1, 4), torch.ones(1, 1, C, dtype=torch.bfloat16, device=DEV).expand(T, 1, C)
+    out, last = sr.selective_scan_run(x, dt, a, bc, bc, softplus=False)
+    part, left = sr.selective_scan_run(x[-tail:], dt[-tail:], a, bc[-tail:], bc[-tail:], softplus=False)
+    # (a step of bf16 between two roundings of nearly the same value)
+    torch.testing.assert_close(out[-tail + 200:].float(), part[200:].float(), rtol=2.0 ** -7, atol=1e-4)
+    torch.testing.assert_close(last, left, rtol=1e-4, atol=1e-5)
+    del out
+    y = x.view(T, C)
+    h, g = sr.block_norm(y, y, gate=y, norms="both")
+    ph, pg = sr.block_norm(y[-tail:], y[-tail:], gate=y[-tail:], norms="both")
+    assert torch.equal(h[-tail:], ph) and torch.equal(g[-tail:], pg)
+    del h, g
+    taps = torch.zeros(T, 1, C, dtype=torch.bfloat16, device=DEV)
+    taps[-tail:, 0] = y[:tail]
+    some = taps[-tail:].clone()
+    out = sr.causal_conv_step(y, w[:, :2].contiguous(), taps)
+    assert torch.equal(out[-tail:], sr.causal_conv_step(y[-tail:], w[:, :2].contiguous(), some)) and torch.equal(taps[-tail:], some)
+    del out, taps
+    state = torch.zeros(T, C, 1, device=DEV)
+    state[-tail:, :, 0] = y[:tail].float()
+    some = state[-tail:].clone()
+    args = lambda n: (dt[:n, 0].expand(n, C), a[:, :1].contiguous(), bc[:n, 0, :, :1], bc[:n, 0, :, :1])
+    out = sr.selective_scan_step(y, *args(T), state, softplus=False)
+    assert torch.equal(out[-tail:], sr.selective_scan_step(y[-tail:], *args(tail), some, softplus=False)) and torch.equal(state[-tail:], some)
+
+
+def test_more_sequences_than_32_bits_count_are_refused():
+    many = (1 << 32) + 5
+    x, w, a = torch.zeros(1, 1, 1, device=DEV).expand(1, many, 1), torch.zeros(1, 1, device=DEV), torch.zeros(1, 1, device=DEV)
+    bc = x[..., None]
+    for call in (lambda: sr.causal_conv_run(x, w, out=None), lambda: sr.selective_scan_run(x, x, a, bc, bc), lambda: sr.causal_conv_run(x[:, :(1 << 31) - 1], w)):
+        with pytest.raises(sr.SrError):
+            call()
+    torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------ heads
+def heads():
+    from tests.test_gpu_selective import head_weights
+    from tests.test_operator_refusals import weights
+    return lambda batch: sr.SelectiveHead(head_weights(32, 32, 8, 2, 4, 1, 3, 1), 32, 32, 8, 2, 4, batch), lambda batch: sr.TemporalHead(weights(channels=32), 32, 4, 2, 32, 48, batch)
+
+
+@pytest.mark.parametrize("kind", [0, 1], ids=["selective", "temporal"])
+def test_heads_of_no_frames_and_of_no_sequences(kind):
+    make = heads()[kind]
+    head = make(2)
+    x = randn(1, 5, 2, 32)
+    one = head.run(x)
+    head.reset()
+    parts = [head.run(x[:0]), head.run(x[:3]), head.run(x[3:3]), head.run(x[3:])]
+    assert [tuple(p.shape) for p in parts] == [(n, 2, head.outputs) for n in (0, 3, 0, 2)]
+    torch.testing.assert_close(torch.cat(parts), one, rtol=0.1, atol=0.1 * float(one.abs().max()))
+    nobody = make(0)
+    assert nobody.run(x[:, :0]).shape == (5, 0, head.outputs) and nobody.step(x[0, :0]).shape == (0, head.outputs)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", [0, 1], ids=["selective", "temporal"])
+def test_heads_refuse_what_is_no_tensor(kind):
+    import numpy as np
+    head = heads()[kind](2)
+    x = randn(1, 5, 2, 32)
+    one = head.run(x)
+    head.reset()
+    for no in (None, 3, "x", [1.0], np.zeros((5, 2, 32), np.float32), [None], [(None, None)], [(3, 4)], {}):
+        for call in (head.run, head.step, head.set_state):
+            with pytest.raises(sr.SrError):
+                call(no)
+    assert torch.equal(head.run(x), one)
