@@ -93,11 +93,9 @@ struct Taps {
         }
     }
 };
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from)
+__device__ __forceinline__ void copy_16(void* to, const void* from)
 {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(srx::smem_u32(to)), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(srx::smem_u32(to)), "l"(from), "n"(BYTES) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(srx::smem_u32(to)), "l"(from) : "memory");
 }
 // `next` becomes the last of W frames.
 template <typename T, int VEC, int W>
@@ -112,7 +110,7 @@ __device__ __forceinline__ void see(float (&seen)[W][VEC], const srx::Few<T, VEC
 }
 
 // Single values: eight blocks to an SM, six of more than four taps (16 packed sequences, 1111 channels, three taps, fp32: 16.4 us, with as many registers as wanted 17.9).
-// Four blocks as long as weights and frames of units fit 128 registers: with eight channels up to five taps (64 sequences of 128 frames, 4096 channels, eight taps: 44 us with two blocks, 139 with
+// Four blocks as long as weights and frames of units all but fit 128 registers (24 bytes of spills with four and five taps): with eight channels up to five taps (64 sequences of 128 frames, 4096 channels, eight taps: 44 us with two blocks, 139 with
 // four; six taps 37 and 46).
 template <typename T, int VEC, int W>
 __global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? (VEC * W > 40 ? 2 : 4) : W > 4 ? 6 : 8) sr_conv_run_kernel(const __grid_constant__ ConvArgs A)
@@ -162,19 +160,19 @@ __global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? (VEC * W > 4
     uint8_t* mine = memory + threadIdx.x * UNIT;
     Few<T, VEC> next[ASYNC ? 1 : kAhead], held[ASYNC ? 1 : kAhead];
     const T* px = x + t0 * A.sx.frame;
-    auto load = [&](int64_t t, int place) {            // the eight frames from t on
+    auto load = [&](int64_t t, int place) {            // the kAhead frames from t on
         const int there = (int)min(n - t, (int64_t)kAhead);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (k < there) {
-                if constexpr (ASYNC) copy_async<UNIT>(mine + (place * kAhead + k) * kThreads * UNIT, px + k * A.sx.frame);
+                if constexpr (ASYNC) copy_16(mine + (place * kAhead + k) * kThreads * UNIT, px + k * A.sx.frame);
                 else next[k].get(px + k * A.sx.frame);
             }
         }
         px += kAhead * A.sx.frame;
         if (ASYNC) asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto work = [&](auto usual, int left, int place) { // usual: eight frames, with their activation
+    auto work = [&](auto usual, int left, int place) { // usual: all kAhead frames, with their activation
         constexpr bool USUAL = decltype(usual)::value;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {

@@ -163,11 +163,6 @@ struct Few {
             for (int i = 0; i < N; i += 2) w[i / 2] = round_bf16(pair(f[i], f[i + 1]));
         }
     }
-    __device__ __forceinline__ void put_one(T* p, int i) const
-    {
-        if constexpr (sizeof(T) == 4) *p = __uint_as_float(w[i]);
-        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[i / 2] >> (i & 1 ? 16 : 0));
-    }
 };
 
 }  // namespace srx
