@@ -421,6 +421,7 @@ sr_status sr_causal_conv_step(const sr_conv_desc* desc, const void* x_dev, const
  * side; b, c of `dtype`, element (frame, sequence, group, n) at frame * .frame + sequence * .sequence + group * .head + n.  States [batch][channels][states] (float, without
  * gaps): state_in NULL: zeros; state_out NULL: not wanted, may be state_in.  A sequence without frames hands its state through.  1 <= states <= 128.
  * What is not finite stays in its sequence and, for u, dt and z, in its channel; where the formula has an infinity the result may be NaN.
+ * A decay below 2^-126, of a single frame or of as many as a run carries over at once, counts as that (a state of 3e38 leaves 4 behind); sigmoids below it are zero.
  * States are meant to decay (r a <= 0).  Growth is followed as the formula has it as long as it stays below 2^128 over any run of frames; beyond that a state may come out too small.
  */
 typedef struct {

@@ -314,8 +314,8 @@ cudaError_t launch(const ConvArgs& A, int width, bool step, cudaStream_t s)
         default: return launch<T, VEC, 8>(A, step, s);
     }
 }
-// 16 bytes at a time where every row of every tensor allows it.  Single frames: 8 bytes, for more threads (256 sequences of 4096 channels 3.9 us, with 16 bytes 5.3), and where there
-// are few sequences pairs of bf16 (one of 4096 channels 1.7, with 16 bytes 2.2).
+// 16 bytes at a time where every row of every tensor allows it.  Single frames: 8 bytes, for more threads (256 sequences of 4096 channels 4.6 us, with 16 bytes 5.3), and where there
+// are few sequences pairs of bf16 (one of 4096 channels 1.6, with 16 bytes 2.1).
 template <typename T>
 cudaError_t launch(const ConvArgs& A, int width, bool step, cudaStream_t s)
 {

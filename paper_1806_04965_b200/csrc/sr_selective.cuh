@@ -68,7 +68,7 @@ __device__ __forceinline__ float softplus(float x)
     return fmaf(s, p, fmaxf(x, 0.0f));
 }
 
-// 1 / (1 + exp(-x)); EXACT: to the last two bits of 32 (the approximate reciprocal is off by one), else to more than those of bf16
+// 1 / (1 + exp(-x)), zero where that is below 2^-126; EXACT: to the last two bits of 32 (the approximate reciprocal is off by one), else to more than those of bf16
 template <bool EXACT>
 __device__ __forceinline__ float sigmoid(float x)
 {
