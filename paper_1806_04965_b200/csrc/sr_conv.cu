@@ -93,10 +93,6 @@ struct Taps {
         }
     }
 };
-__device__ __forceinline__ void copy_16(void* to, const void* from)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(srx::smem_u32(to)), "l"(from) : "memory");
-}
 // `next` becomes the last of W frames.
 template <typename T, int VEC, int W>
 __device__ __forceinline__ void see(float (&seen)[W][VEC], const srx::Few<T, VEC>& next)
@@ -165,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? (VEC * W > 4
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (k < there) {
-                if constexpr (ASYNC) copy_16(mine + (place * kAhead + k) * kThreads * UNIT, px + k * A.sx.frame);
+                if constexpr (ASYNC) srx::copy_16(mine + (place * kAhead + k) * kThreads * UNIT, px + k * A.sx.frame);
                 else next[k].get(px + k * A.sx.frame);
             }
         }

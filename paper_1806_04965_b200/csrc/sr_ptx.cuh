@@ -8,6 +8,11 @@
 namespace srx {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// A unit of 16 bytes into shared memory, under way until the thread waits for it.
+__device__ __forceinline__ void copy_16(void* to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
 
 // These kernels may be scheduled while the one before them still runs (programmatic dependent launch): they touch nothing of their caller's before
 // wait_for_predecessor returns.  One that takes tensor memory does so between the two calls: it neither holds any while it waits, nor lets a successor, which

@@ -103,10 +103,6 @@ __device__ __forceinline__ float exchange(float (&y)[L], int p)
     return y[0];
 }
 
-__device__ __forceinline__ void copy_16(void* dst, const void* src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(srx::smem_u32(dst)), "l"(src) : "memory");
-}
 __device__ __forceinline__ void copy_4(void* dst, const void* src)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(srx::smem_u32(dst)), "l"(src) : "memory");
@@ -137,7 +133,7 @@ struct Rows {
         for (int e = 0; e < COPIES; ++e) {
             if (!there(e, tid, cols, left)) continue;
             T* place = &to[frame(e, tid)][col(e, tid)];
-            if constexpr (UNITS) copy_16(place, from + away(e, tid, stride));
+            if constexpr (UNITS) srx::copy_16(place, from + away(e, tid, stride));
             else if constexpr (sizeof(T) == 4) copy_4(place, from + away(e, tid, stride));
             else *place = from[away(e, tid, stride)];
         }
