@@ -106,8 +106,8 @@ __device__ __forceinline__ void see(float (&seen)[W][VEC], const srx::Few<T, VEC
 }
 
 // Single values: eight blocks to an SM, six of more than four taps (16 packed sequences, 1111 channels, three taps, fp32: 16.4 us, with as many registers as wanted 17.9).
-// Four blocks as long as weights and frames of units all but fit 128 registers (24 bytes of spills with four and five taps): with eight channels up to five taps (64 sequences of 128 frames, 4096 channels, eight taps: 44 us with two blocks, 139 with
-// four; six taps 37 and 46).
+// Four blocks as long as weights and frames of units all but fit 128 registers (24 bytes of spills with four and five taps): with eight channels up to five taps (64 sequences of 128 frames,
+// 4096 channels, eight taps: 44 us with two blocks, 139 with four; six taps 37 and 46).
 template <typename T, int VEC, int W>
 __global__ void __launch_bounds__(kThreads, VEC * sizeof(T) == 16 ? (VEC * W > 40 ? 2 : 4) : W > 4 ? 6 : 8) sr_conv_run_kernel(const __grid_constant__ ConvArgs A)
 {
